@@ -227,6 +227,91 @@ dynts_status_t dynts_evict_noalloc_status(void* stream);
  * re-encoded.  Choose scale ~ max|x| / 448 of the tensor to use the format's range. */
 dynts_status_t dynts_cache_set_kv_scale(dynts_cache_t* c, float k_scale, float v_scale);
 
+/* ---- a chunk of new tokens against the cache ------------------------------------------------ */
+
+/* Several new tokens of a sequence at once, behind the rows the cache holds: the next question of a
+ * conversation, a piece of a long prompt, drafted tokens to check, ragged prompts packed one after
+ * another into empty sequences, or one token per sequence in a model that needs the options below.
+ * What dynts_decode_attn does for one token is done for every token of the chunk (Eq. 4-6):
+ * token i of a sequence that held n rows attends to rows [0, n + i], its own row included.
+ *
+ * The options, all off when zero (opts == NULL: all off):
+ *   softcap   c > 0: a logit x = q.k / sqrt(d) becomes c tanh(x / c)
+ *   slopes    device [Hq] fp32: slopes[h] * |p_i - p_j| is subtracted from the (capped) logit.  p are
+ *             the rows' positions, counted in tokens seen: rows that survived an eviction keep theirs
+ *   window    w > 0: only rows with |p_i - p_j| < w are seen (positions ascend with the rows, as every
+ *             call of this library leaves them; rows imported otherwise are not supported with a window)
+ *   prefix    host [Nb]: the first prefix[b] tokens of the chunk are seen by every token of the chunk,
+ *             those before them included
+ *   s_new     device [n_total] fp32: the new rows' scores in every layer and KV head (+inf keeps a row
+ *             for as long as the target has room for it); NULL: 0
+ *   mass      device [L, Nb, Hkv, cap] fp32: receives, for every row, the attention mass it got from all
+ *             the chunk's tokens and the group's heads (rows [0, n + n_new[b]) of the sequences with new
+ *             tokens are overwritten, the rest untouched).  Each layer's part is written by its layer.
+ *   stage     1: the rows are stored behind the sequences' ends but the sequences do not grow: the
+ *             lengths, positions counted and scores of the rows held stay as they are, and a
+ *             dynts_extend_commit may follow (checking of drafted tokens)
+ *   q_stride, k_stride, v_stride   elements from one token to the next, 0: contiguous.  Multiples of
+ *             16 bytes; the tensors of dynts_extend_attn's layers follow one another after n_total tokens
+ *
+ * In the score source DYNTS_SCORE_ATTENTION (and not staged) the mass is added to the rows' scores,
+ * in one addition per row and chunk; a chunk of T tokens then leaves what T decode steps leave, up to
+ * rounding.  In DYNTS_SCORE_EXTERNAL the scores stay. */
+typedef struct dynts_extend_opts {
+  float softcap;
+  const float* slopes;
+  int window;
+  const int* prefix;
+  const float* s_new;
+  float* mass;
+  int stage;
+  long long q_stride, k_stride, v_stride;
+} dynts_extend_opts_t;
+
+/* One chunk for all layers.  n_new: host [Nb], tokens of each sequence, 0 for none (a sequence that was
+ * reset, or never filled, begins with its chunk).  The tokens of the sequences follow one another:
+ *   q, out:        device [L, n_total, Hq, d]   (cache dtype; out contiguous, not overlapping q)
+ *   k_new, v_new:  device [L, n_total, Hkv, d]  n_total = sum of n_new
+ *   scratch:       device memory of dynts_extend_scratch_bytes(c, n_new, L) bytes, 16-byte aligned,
+ *                  caller-owned; contents need not be preserved between calls.  Calls that may overlap
+ *                  on the GPU (two caches, two captured graphs) need one each.
+ * Types as the cache's; with 8-bit rows the chunk's rows are encoded first and read as stored, as in a
+ * decode step.  DYNTS_ERR_CAPACITY if a sequence would outgrow its slab.  Nothing behind the last token
+ * of out is written.  May be captured into a graph: the rows held are read from the device at replay
+ * (n_new, prefix and the options are those of the capture), and as for decode steps the host's copy
+ * of the lengths does not follow replays. */
+size_t dynts_extend_scratch_bytes(const dynts_cache_t* c, const int* n_new, int n_layers);
+dynts_status_t dynts_extend_attn(dynts_cache_t* c, const void* q, const void* k_new, const void* v_new, void* out, const int* n_new,
+                                 const dynts_extend_opts_t* opts, void* scratch, size_t scratch_bytes);
+
+/* The same for one layer: q, out: device [n_total, Hq, d]; k_new, v_new: device [n_total, Hkv, d];
+ * scratch of dynts_extend_scratch_bytes(c, n_new, 1).  Layers in order 0 .. L-1 with the same n_new and
+ * stage; the lengths grow after layer L-1. */
+dynts_status_t dynts_extend_attn_layer(dynts_cache_t* c, int layer, const void* q, const void* k_new, const void* v_new, void* out,
+                                       const int* n_new, const dynts_extend_opts_t* opts, void* scratch, size_t scratch_bytes);
+
+/* Takes over the first n_accept[b] (host [Nb]) rows of the chunk staged last: the sequences grow by
+ * them, the other staged rows are forgotten.  Their scores are what s_new gave (or 0).
+ * DYNTS_ERR_STATE if a call that changes rows or lengths came between. */
+dynts_status_t dynts_extend_commit(dynts_cache_t* c, const int* n_accept);
+
+/* Rotary positions with one or several axes, for the queries and keys handed to this library (which
+ * stores keys as given).  Pair i (0 <= i < rot_dim / 2) of a head turns by pos[axis(i)][t] *
+ * theta^(-2 i / rot_dim); the columns behind rot_dim pass through.
+ *   q, q_out: device [n_tokens, q_heads, head_dim];  k, k_out: device [n_tokens, kv_heads, head_dim], or
+ *   k NULL: the queries alone.  bf16 or fp32 (dtype), rounded once.  In place (q_out == q with the same
+ *   stride) is allowed, any other overlap is not.
+ *   pos: device [n_axes][n_tokens] int32;  sections: host [n_axes], pairs of each axis (sum rot_dim / 2),
+ *   or NULL for one axis.  The axes take their pairs in blocks, or with DYNTS_ROPE_ROUND_ROBIN in turn
+ *   (an axis whose section is used up is passed over).  Pairs are columns (i, i + rot_dim / 2), or with
+ *   DYNTS_ROPE_ADJACENT columns (2 i, 2 i + 1).
+ *   strides: host [4], elements from one token to the next of q, k, q_out, k_out (0: contiguous), or NULL.
+ * One launch on `stream`; allocates nothing. */
+enum { DYNTS_ROPE_ADJACENT = 1, DYNTS_ROPE_ROUND_ROBIN = 2 };
+dynts_status_t dynts_rope(const void* q, const void* k, const int* pos, void* q_out, void* k_out, int n_tokens, int q_heads, int kv_heads,
+                          int head_dim, int rot_dim, int n_axes, const int* sections, int flags, double theta, int dtype,
+                          const long long* strides, void* stream);
+
 /* ---- predictor scores and the paper's own trigger ------------------------------------------ */
 
 /* Where the importance scores come from.  DYNTS_SCORE_ATTENTION (default): every decode step

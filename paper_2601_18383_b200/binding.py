@@ -27,6 +27,8 @@ DYNTS_FP32 = 1
 DYNTS_BF16_KV8 = 2
 DYNTS_SCORE_ATTENTION = 0
 DYNTS_SCORE_EXTERNAL = 1
+DYNTS_ROPE_ADJACENT = 1
+DYNTS_ROPE_ROUND_ROBIN = 2
 
 _STATUS_NAMES = {
     0: "DYNTS_OK", 1: "DYNTS_ERR_INVALID_ARG", 2: "DYNTS_ERR_OOM", 3: "DYNTS_ERR_CAPACITY",
@@ -47,6 +49,13 @@ class dynts_config_t(C.Structure):
         ("capacity", C.c_int), ("dtype", C.c_int),
         ("seq_budgets", C.POINTER(C.c_int)),
         ("storage", C.c_void_p), ("storage_bytes", C.c_size_t), ("stream", C.c_void_p),
+    ]
+
+
+class dynts_extend_opts_t(C.Structure):
+    _fields_ = [
+        ("softcap", C.c_float), ("slopes", C.c_void_p), ("window", C.c_int), ("prefix", C.c_void_p), ("s_new", C.c_void_p),
+        ("mass", C.c_void_p), ("stage", C.c_int), ("q_stride", C.c_longlong), ("k_stride", C.c_longlong), ("v_stride", C.c_longlong),
     ]
 
 
@@ -99,6 +108,11 @@ _sigs = {
     "dynts_evict_at_budget": (C.c_int, [_P, C.c_int, C.c_double]),
     "dynts_predictor_mlp_scratch_bytes": (C.c_size_t, [C.c_int, C.c_int]),
     "dynts_predictor_mlp": (C.c_int, [_P] * 7 + [C.c_int, C.c_int, C.c_int, _P, C.c_size_t, _P, _P]),
+    "dynts_extend_scratch_bytes": (C.c_size_t, [_P, _P, C.c_int]),
+    "dynts_extend_attn": (C.c_int, [_P] * 6 + [C.POINTER(dynts_extend_opts_t), _P, C.c_size_t]),
+    "dynts_extend_attn_layer": (C.c_int, [_P, C.c_int] + [_P] * 5 + [C.POINTER(dynts_extend_opts_t), _P, C.c_size_t]),
+    "dynts_extend_commit": (C.c_int, [_P, _P]),
+    "dynts_rope": (C.c_int, [_P] * 5 + [C.c_int] * 6 + [_P, C.c_int, C.c_double, C.c_int, _P, _P]),
     "dynts_evict_stats": (C.c_int, [_P, C.POINTER(C.c_longlong), C.POINTER(C.c_longlong)]),
     "dynts_last_error": (C.c_char_p, []),
     "dynts_version": (C.c_char_p, []),
@@ -319,6 +333,91 @@ def dynts_predictor_mlp(h, W1, b1, W2, b2, W3, b3, d, batch, activation, scratch
                                           activation, _ptr(scratch), scratch_bytes, _ptr(scores), stream))
 
 
+def _host_ints(x):
+    """(address, keep-alive) of host int32 values: a CPU int32 tensor or array as it is, else a copy of a sequence."""
+    if hasattr(x, "data_ptr"):
+        if str(x.dtype) != "torch.int32" or x.is_cuda or not x.is_contiguous():
+            raise DyntsError(DYNTS_ERR_INVALID_ARG, "host counts must be a contiguous int32 tensor on the CPU, or a sequence of ints")
+        return x.data_ptr(), x
+    if hasattr(x, "ctypes") and str(x.dtype) == "int32" and x.flags["C_CONTIGUOUS"]:
+        return x.ctypes.data, x
+    arr = (C.c_int * len(x))(*[int(v) for v in x])
+    return C.addressof(arr), arr
+
+
+def dynts_extend_scratch_bytes(c, n_new, n_layers) -> int:
+    p, keep = _host_ints(n_new)
+    return lib.dynts_extend_scratch_bytes(c, p, n_layers)
+
+
+def dynts_extend_attn(c, q, k_new, v_new, out, n_new, opts, scratch, scratch_bytes):
+    p, keep = _host_ints(n_new)
+    return _check(lib.dynts_extend_attn(c, _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(out), p, C.byref(opts) if opts is not None else None,
+                                        _ptr(scratch), scratch_bytes))
+
+
+def dynts_extend_attn_layer(c, layer, q, k_new, v_new, out, n_new, opts, scratch, scratch_bytes):
+    p, keep = _host_ints(n_new)
+    return _check(lib.dynts_extend_attn_layer(c, layer, _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(out), p,
+                                              C.byref(opts) if opts is not None else None, _ptr(scratch), scratch_bytes))
+
+
+def dynts_extend_commit(c, n_accept):
+    p, keep = _host_ints(n_accept)
+    return _check(lib.dynts_extend_commit(c, p))
+
+
+def dynts_rope(q, k, pos, q_out, k_out, n_tokens, q_heads, kv_heads, head_dim, rot_dim, n_axes, sections, flags, theta, dtype, strides=None,
+               stream=None):
+    sec = (C.c_int * n_axes)(*sections) if sections is not None else None
+    st = (C.c_longlong * 4)(*strides) if strides is not None else None
+    return _check(lib.dynts_rope(_ptr(q), _ptr(k), _ptr(pos), _ptr(q_out), _ptr(k_out), n_tokens, q_heads, kv_heads, head_dim, rot_dim,
+                                 n_axes, sec, flags, theta, dtype, st, stream))
+
+
+def _invalid(message):
+    raise DyntsError(DYNTS_ERR_INVALID_ARG, message)
+
+
+def rope(q, k, positions, q_out=None, k_out=None, theta=10000.0, sections=None, rot_dim=None, adjacent=False, round_robin=False):
+    """dynts_rope on torch tensors: q [n, Hq, d], k [n, Hkv, d] or None, positions int32 [n] or [axes, n].  The outputs are new
+    tensors unless given (q_out=q, k_out=k: in place).  Rows of a token are contiguous, tokens may be strided.  Runs on torch's
+    current stream of q's device.  Returns (q_out, k_out)."""
+    import torch
+    if q_out is None:
+        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    if k is not None and k_out is None:
+        k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device)
+    n, hq, d = q.shape
+    dtype = DYNTS_BF16 if q.dtype == torch.bfloat16 else DYNTS_FP32 if q.dtype == torch.float32 else _invalid("q must be bf16 or fp32")
+    for x, y in ((q, q_out), (k, k_out)):
+        if x is None:
+            continue
+        for z in (x, y):
+            if not z.is_cuda or z.device != q.device or z.dtype != q.dtype or z.dim() != 3 or z.shape != x.shape or x.shape[0] != n or x.shape[2] != d:
+                _invalid("q, k and the outputs must be CUDA tensors [n, heads, d] of one type on one device")
+            if z.numel() and (z.stride(2) != 1 or (z.shape[1] > 1 and z.stride(1) != d) or (n > 1 and z.stride(0) < z.shape[1] * d)):
+                _invalid("the heads of a token must be contiguous and the tokens in order")
+    if positions.device != q.device or positions.dtype != torch.int32 or not positions.is_contiguous():
+        _invalid("positions must be a contiguous int32 tensor on q's device")
+    axes = 1 if positions.dim() == 1 else positions.shape[0]
+    if positions.dim() > 2 or positions.shape[-1] != n or (sections is not None and len(sections) != axes):
+        _invalid("positions are [n] or [axes, n], with a section for each axis")
+    hkv = 0 if k is None else k.shape[1]
+    st = None
+    if n > 1:
+        st = (q.stride(0), 0 if k is None else k.stride(0), q_out.stride(0), 0 if k is None else k_out.stride(0))
+    flags = (DYNTS_ROPE_ADJACENT if adjacent else 0) | (DYNTS_ROPE_ROUND_ROBIN if round_robin else 0)
+    args = (q, k, positions, q_out, k_out, n, hq, hkv, d, d if rot_dim is None else rot_dim, axes, sections, flags, float(theta), dtype, st)
+    stream = torch.cuda.current_stream(q.device).cuda_stream
+    if torch.cuda.current_device() != q.device.index:
+        with torch.cuda.device(q.device):
+            dynts_rope(*args, stream)
+    else:
+        dynts_rope(*args, stream)
+    return q_out, k_out
+
+
 def dynts_evict_stats(c):
     """(rows scanned, rows moved) of the most recent eviction."""
     a, b = C.c_longlong(0), C.c_longlong(0)
@@ -358,12 +457,14 @@ class Cache:
             self.handle = dynts_cache_create_ex(cfg)
         self.nbytes = nbytes
         self.capacity = dynts_cache_capacity(self.handle)
+        self._scratch = []        # scratch of the chunk calls; outgrown pieces are kept for the work and graphs that still use them
 
     def close(self):
         if getattr(self, "handle", None):
             dynts_cache_destroy(self.handle)
             self.handle = None
             self.storage = None
+            self._scratch = []
 
     def __del__(self):
         try:
@@ -401,6 +502,69 @@ class Cache:
 
     def decode_attn_host(self, q, k_new, v_new, out):
         return dynts_decode_attn_host(self.handle, q, k_new, v_new, out)
+
+    def _extend(self, layer, q, k, v, out, n_new, s_new, mass, softcap, slopes, window, prefix, stage):
+        torch = self.torch
+        counts, keep_n = _host_ints(n_new)
+        if len(n_new) != self.batch:
+            _invalid("n_new needs a count for each sequence")
+        lead = () if layer is not None else (self.layers,)
+        total = q.shape[-3]
+        dt, dev, d = self.torch_dtype, self.storage.device, self.head_dim
+        strides = []
+        for x, heads in ((q, self.q_heads), (k, self.kv_heads), (v, self.kv_heads), (out, self.q_heads)):
+            if x.dtype != dt or x.device != dev or tuple(x.shape) != lead + (total, heads, d):
+                _invalid(f"q, k, v and out must be {dt} tensors {lead + ('n_total', 'heads', d)} on {dev}")
+            step = x.stride(-3) if total > 1 else heads * d
+            if x.numel() and (x.stride(-1) != 1 or (heads > 1 and x.stride(-2) != d) or step < heads * d or
+                              (lead and self.layers > 1 and x.stride(0) != total * step)):
+                _invalid("the heads of a token must be contiguous, the tokens in order and the layers adjoining")
+            strides.append(step)
+        if strides[3] != self.q_heads * d:
+            _invalid("out must be contiguous")
+        for x, shape in ((s_new, (total,)), (mass, (self.layers, self.batch, self.kv_heads, self.capacity)), (slopes, (self.q_heads,))):
+            if x is not None and (x.dtype != torch.float32 or x.device != dev or tuple(x.shape) != shape or not x.is_contiguous()):
+                _invalid(f"s_new, mass and slopes must be contiguous fp32 tensors on {dev} (here: {shape})")
+        opts = dynts_extend_opts_t()
+        opts.softcap, opts.window, opts.stage = softcap, window, 1 if stage else 0
+        opts.slopes, opts.s_new, opts.mass = _ptr(slopes), _ptr(s_new), _ptr(mass)
+        opts.q_stride, opts.k_stride, opts.v_stride = strides[0], strides[1], strides[2]
+        if prefix is not None:
+            if len(prefix) != self.batch:
+                _invalid("prefix needs a count for each sequence")
+            opts.prefix, keep_p = _host_ints(prefix)
+        if int(sum(n_new.tolist() if hasattr(n_new, "tolist") else n_new)) != total:
+            _invalid("n_new does not add up to the tokens of q")
+        need = lib.dynts_extend_scratch_bytes(self.handle, counts, 1 if layer is not None else self.layers)
+        if not self._scratch or self._scratch[-1].numel() < need:
+            # (never given back before the cache: the stream and captured graphs may still use it)
+            self._scratch.append(torch.empty(max(need, 2 * self._scratch[-1].numel() if self._scratch else 0), dtype=torch.uint8, device=dev))
+        scratch = self._scratch[-1]
+
+        def call():
+            if layer is None:
+                return _check(lib.dynts_extend_attn(self.handle, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), counts, C.byref(opts),
+                                                    scratch.data_ptr(), scratch.numel()))
+            return _check(lib.dynts_extend_attn_layer(self.handle, layer, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), counts,
+                                                      C.byref(opts), scratch.data_ptr(), scratch.numel()))
+
+        if torch.cuda.current_device() == dev.index:
+            return call()
+        with torch.cuda.device(dev):
+            return call()
+
+    def extend_attn(self, q, k, v, out, n_new, s_new=None, mass=None, softcap=0.0, slopes=None, window=0, prefix=None, stage=False):
+        """A chunk of n_new[b] tokens per sequence for all layers: q, out [L, n_total, Hq, d], k, v [L, n_total, Hkv, d]."""
+        return self._extend(None, q, k, v, out, n_new, s_new, mass, softcap, slopes, window, prefix, stage)
+
+    def extend_attn_layer(self, layer, q, k, v, out, n_new, s_new=None, mass=None, softcap=0.0, slopes=None, window=0, prefix=None,
+                          stage=False):
+        return self._extend(int(layer), q, k, v, out, n_new, s_new, mass, softcap, slopes, window, prefix, stage)
+
+    def extend_commit(self, n_accept):
+        if len(n_accept) != self.batch:
+            _invalid("n_accept needs a count for each sequence")
+        return dynts_extend_commit(self.handle, n_accept)
 
     def evict(self, budget=0):
         return dynts_evict(self.handle, budget)

@@ -19,8 +19,10 @@
 #include "decode_attn.cuh"
 #include "decode_stream.cuh"
 #include "evict.cuh"
+#include "extend.cuh"
 #include "predictor.cuh"
 #include "prefill_attn.cuh"
+#include "rope.cuh"
 
 namespace {
 
@@ -130,7 +132,11 @@ struct dynts_cache {
   int* err_host = nullptr;   // pinned, mapped
   int* err_dev = nullptr;
   std::vector<int> seq_budget, len_h, tot_h, pinned_h, target_h, active_h;  // host mirrors of the per-sequence state
-  int layer_cursor = 0;      // next layer expected by dynts_decode_attn_layer
+  int layer_cursor = 0;      // next layer expected by dynts_decode_attn_layer or dynts_extend_attn_layer
+  bool extending = false;    // the layer-by-layer step in progress is a chunk (dynts_extend_attn_layer)
+  bool chunk_staged = false; // ... and it is staged
+  std::vector<int> chunk_h;  // ... and its tokens per sequence
+  std::vector<int> staged_h; // rows per sequence that a staged chunk left behind the ends (empty: none)
   int cluster = 0, variant = 0;
   unsigned int wait_limit = dynts::kStSpinLimit;  // polls of a bounded device-side wait
   int drop_item = -1;        // one-shot: the next streaming decode launch omits this tile load of CTA 0 (timeout-path test)
@@ -143,7 +149,7 @@ struct dynts_cache {
   char* stage_dev = nullptr;
   size_t stage_bytes = 0;
   bool attr_generic_f32 = false, attr_generic_bf16 = false, attr_generic_kv8 = false, attr_mma = false, attr_select = false;
-  bool attr_stream = false, attr_fused = false, attr_prefill = false;
+  bool attr_stream = false, attr_fused = false, attr_prefill = false, attr_extend = false;
   bool have_maps = false;    // tensor maps of the K and V slabs for the streaming kernel
   CUtensorMap map_KV;
   int sm_count = 0;
@@ -316,6 +322,7 @@ dynts_status_t launch_decode(dynts_cache* c, int layer0, int n_layers, const voi
     n_max = std::max(n_max, c->len_h[b] + 1);
   }
   if (!any) return DYNTS_OK;
+  c->staged_h.clear();
 
   const int units = n_layers * Nb * f.kv_heads;
   const int S = pick_cluster(c, units, n_max);
@@ -561,6 +568,7 @@ dynts_status_t do_prefill(dynts_cache* c, int seq, const void* k, const void* v,
     dynts_status_t fs_ = flush_pending(c);
     if (fs_ != DYNTS_OK) return fs_;
   }
+  c->staged_h.clear();
   dynts::PrefillParams p;
   p.k = k;
   p.v = v;
@@ -623,6 +631,7 @@ dynts_status_t do_evict(dynts_cache* c, const int* targets /* host [Nb], validat
     any = true;
   }
   if (!any) return DYNTS_OK;
+  c->staged_h.clear();
   bool same = true;
   for (int b = 0; b < Nb; ++b) same = same && c->target_h[b] == targets[b];
   if (!same) {
@@ -918,6 +927,7 @@ dynts_status_t dynts_cache_refresh_lengths(dynts_cache_t* c) {
   if (!c->ready) return DYNTS_OK;
   if (c->layer_cursor != 0) return fail(DYNTS_ERR_STATE, "a layer-by-layer step is in progress");
   CUDA_TRY(cudaStreamSynchronize(c->stream));
+  c->staged_h.clear();  // a replayed step may have overwritten the rows behind the ends
   const int Nb = c->cfg.batch;
   CUDA_TRY(cudaMemcpy(c->len_h.data(), c->len(), Nb * sizeof(int), cudaMemcpyDeviceToHost));
   CUDA_TRY(cudaMemcpy(c->tot_h.data(), c->tot(), Nb * sizeof(int), cudaMemcpyDeviceToHost));
@@ -960,7 +970,9 @@ dynts_status_t dynts_decode_attn_layer(dynts_cache_t* c, int layer, const void* 
   if (st != DYNTS_OK) return st;
   if (layer != c->layer_cursor)
     return fail(DYNTS_ERR_STATE, "layer %d called, layer %d expected", layer, c->layer_cursor);
+  if (layer != 0 && c->extending) return fail(DYNTS_ERR_STATE, "the step in progress is a chunk (dynts_extend_attn_layer)");
   const bool last = layer == c->cfg.layers - 1;
+  c->extending = false;
   st = launch_decode(c, layer, 1, q, k_new, v_new, out, scores, last);
   if (st == DYNTS_OK) c->layer_cursor = last ? 0 : layer + 1;
   return st;
@@ -1081,6 +1093,7 @@ dynts_status_t dynts_seq_reset(dynts_cache_t* c, int seq) {
     dynts_status_t fs_ = flush_pending(c);
     if (fs_ != DYNTS_OK) return fs_;
   }
+  c->staged_h.clear();
   CUDA_TRY(cudaMemsetAsync(c->len() + seq, 0, sizeof(int), c->stream));
   CUDA_TRY(cudaMemsetAsync(c->tot() + seq, 0, sizeof(int), c->stream));
   CUDA_TRY(cudaMemsetAsync(c->pinned() + seq, 0, sizeof(int), c->stream));
@@ -1147,6 +1160,7 @@ dynts_status_t dynts_cache_import(dynts_cache_t* c, int layer, int seq, int head
     dynts_status_t fs_ = flush_pending(c);
     if (fs_ != DYNTS_OK) return fs_;
   }
+  c->staged_h.clear();
   CUDA_TRY(cudaStreamSynchronize(c->stream));
   const size_t slab = ((size_t)layer * c->cfg.batch + seq) * c->cfg.kv_heads + head;
   const size_t row_bytes = (size_t)c->cfg.head_dim * c->kv_elt;
@@ -1305,6 +1319,377 @@ dynts_status_t dynts_evict_stats(dynts_cache_t* c, long long* rows_scanned, long
   }
   if (rows_scanned) *rows_scanned = scanned;
   if (rows_moved) *rows_moved = moved;
+  return DYNTS_OK;
+}
+
+}  // extern "C"
+
+/* ---- a chunk of new tokens against the cache ---------------------------------------------- */
+
+namespace {
+
+// What a chunk's launches need beside the cache: each query row's log-sum-exp.
+size_t extend_scratch(const dynts_config_t& f, long long total, int n_layers) {
+  return align_up((size_t)n_layers * total * f.q_heads * sizeof(float), 256);
+}
+
+struct ExtendCall {
+  const void *q, *k, *v;
+  void* out;
+  const int* n_new;
+  dynts_extend_opts_t o;
+  char* scratch;
+  size_t scratch_bytes;
+};
+
+// Everything that can be told before the storage exists: nothing is allocated or launched for a call that is refused.
+dynts_status_t check_extend(const dynts_cache* c, const ExtendCall& a, int n_layers, long long* total_out) {
+  const dynts_config_t& f = c->cfg;
+  int cap = 0;
+  if (!config_ok(&f, &cap)) return fail(DYNTS_ERR_INVALID_ARG, "invalid cache configuration");
+  if (c->ready) cap = c->cap;
+  if (!a.n_new) return fail(DYNTS_ERR_INVALID_ARG, "NULL n_new");
+  long long total = 0;
+  for (int b = 0; b < f.batch; ++b) {
+    if (a.n_new[b] < 0) return fail(DYNTS_ERR_INVALID_ARG, "sequence %d: %d new tokens", b, a.n_new[b]);
+    total += a.n_new[b];
+    if (a.o.prefix && (a.o.prefix[b] < 0 || a.o.prefix[b] > a.n_new[b]))
+      return fail(DYNTS_ERR_INVALID_ARG, "sequence %d: prefix %d outside [0, %d]", b, a.o.prefix[b], a.n_new[b]);
+  }
+  if (total >= (1ll << 30) / f.q_heads) return fail(DYNTS_ERR_INVALID_ARG, "%lld new tokens are beyond the launch limits", total);
+  for (int b = 0; b < f.batch; ++b) {
+    const int held = c->ready ? c->len_h[b] : 0;
+    if ((long long)held + a.n_new[b] > cap)
+      return fail(DYNTS_ERR_CAPACITY, "sequence %d: %d rows and %d new tokens exceed the capacity %d", b, held, a.n_new[b], cap);
+  }
+  if (!(a.o.softcap >= 0.f) || std::isinf(a.o.softcap)) return fail(DYNTS_ERR_INVALID_ARG, "softcap must be 0 or positive and finite");
+  if (a.o.window < 0) return fail(DYNTS_ERR_INVALID_ARG, "window must not be negative");
+  if (a.o.stage != 0 && a.o.stage != 1) return fail(DYNTS_ERR_INVALID_ARG, "stage must be 0 or 1");
+  const long long per16 = 16 / elt_bytes_of(f.dtype);
+  const long long qs = a.o.q_stride, ks = a.o.k_stride, vs = a.o.v_stride, qd = (long long)f.q_heads * f.head_dim, kd = (long long)f.kv_heads * f.head_dim;
+  if ((qs != 0 && (qs < qd || qs % per16)) || (ks != 0 && (ks < kd || ks % per16)) || (vs != 0 && (vs < kd || vs % per16)))
+    return fail(DYNTS_ERR_INVALID_ARG, "token strides must cover a token and be multiples of 16 bytes (%lld, %lld, %lld)", qs, ks, vs);
+  if (std::max(qs, std::max(ks, vs)) >= (1ll << 36)) return fail(DYNTS_ERR_INVALID_ARG, "token strides are beyond the launch limits");
+  if ((long long)n_layers * f.kv_heads > 65535) return fail(DYNTS_ERR_INVALID_ARG, "layers x KV heads %lld are beyond the launch limits", (long long)n_layers * f.kv_heads);
+  if (total > 0) {
+    if (!a.q || !a.k || !a.v || !a.out) return fail(DYNTS_ERR_INVALID_ARG, "NULL tensor pointer");
+    if (!aligned16(a.q) || !aligned16(a.k) || !aligned16(a.v) || !aligned16(a.out))
+      return fail(DYNTS_ERR_INVALID_ARG, "tensor pointers must be 16-byte aligned");
+    const size_t need = extend_scratch(f, total, n_layers);
+    if (!a.scratch || !aligned16(a.scratch)) return fail(DYNTS_ERR_INVALID_ARG, "scratch must be non-NULL and 16-byte aligned");
+    if (a.scratch_bytes < need) return fail(DYNTS_ERR_OOM, "scratch too small: %zu < %zu bytes", a.scratch_bytes, need);
+  }
+  *total_out = total;
+  return DYNTS_OK;
+}
+
+template <typename Kern, typename... Args>
+cudaError_t launch_dependent(Kern kern, dim3 grid, unsigned threads, size_t smem, cudaStream_t st, Args... args) {
+  cudaLaunchConfig_t lc;
+  memset(&lc, 0, sizeof(lc));
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;  // see griddepcontrol.wait in the kernels
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  lc.attrs = at;
+  lc.numAttrs = 1;
+  lc.stream = st;
+  lc.gridDim = grid;
+  lc.blockDim = dim3(threads, 1, 1);
+  lc.dynamicSmemBytes = smem;
+  return cudaLaunchKernelEx(&lc, kern, args...);
+}
+
+template <typename T, bool KV8>
+dynts_status_t launch_extend_generic(dynts_cache* c, dynts::ExtendParams& p, bool want_mass) {
+  const int d = p.d;
+  const size_t smem = dynts::ext_generic_smem(d), smem_m = dynts::ext_generic_mass_smem(d);
+  if (!c->attr_extend) {  // (the largest head size's need: the attribute belongs to the kernel, not to the cache)
+    CUDA_TRY(cudaFuncSetAttribute(dynts::extend_generic_kernel<T, KV8>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                  (int)dynts::ext_generic_smem(256)));
+    CUDA_TRY(cudaFuncSetAttribute(dynts::extend_generic_mass_kernel<T, KV8>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                  (int)dynts::ext_generic_mass_smem(256)));
+    c->attr_extend = true;
+  }
+  const int n_seq = p.seqs.n;
+  p.seqs.item0[0] = 0;
+  for (int s = 0; s < n_seq; ++s) {
+    const long long rows = (long long)(p.seqs.tok0[s + 1] - p.seqs.tok0[s]) * p.G;
+    p.seqs.item0[s + 1] = p.seqs.item0[s] + (int)((rows + dynts::kExtGenericRows - 1) / dynts::kExtGenericRows);
+  }
+  const unsigned ny = (unsigned)(p.n_layers * p.Hkv);
+  CUDA_TRY(launch_dependent(dynts::extend_generic_kernel<T, KV8>, dim3((unsigned)p.seqs.item0[n_seq], ny, 1), dynts::kExtGenericThreads, smem,
+                            c->stream, p));
+  c->launches += 1;
+  if (want_mass) {
+    // grid over the capacity, not over the host's copy of the lengths: a replayed graph may hold longer sequences
+    const unsigned nx = (unsigned)((c->cap + dynts::kExtGenericKeys - 1) / dynts::kExtGenericKeys);
+    dynts::extend_generic_mass_kernel<T, KV8><<<dim3(nx, ny, (unsigned)n_seq), dynts::kExtGenericThreads, smem_m, c->stream>>>(p);
+    CUDA_TRY(cudaGetLastError());
+    c->launches += 1;
+  }
+  return DYNTS_OK;
+}
+
+dynts_status_t launch_extend(dynts_cache* c, int layer0, int n_layers, const ExtendCall& a, long long total, bool publish) {
+  const dynts_config_t& f = c->cfg;
+  {
+    dynts_status_t fs = flush_pending(c);  // the chunk's mass is added to the scores behind it
+    if (fs != DYNTS_OK) return fs;
+  }
+  c->staged_h.clear();
+  if (total == 0) return DYNTS_OK;
+  dynts::ExtendParams p;
+  p.q = a.q;
+  p.k = a.k;
+  p.v = a.v;
+  p.out = a.out;
+  p.q_stride = a.o.q_stride ? a.o.q_stride : (long long)f.q_heads * f.head_dim;
+  p.k_stride = a.o.k_stride ? a.o.k_stride : (long long)f.kv_heads * f.head_dim;
+  p.v_stride = a.o.v_stride ? a.o.v_stride : (long long)f.kv_heads * f.head_dim;
+  p.K = c->K();
+  p.V = c->V();
+  p.pos = c->pos();
+  p.score = c->score();
+  p.comp = c->comp();
+  p.len = c->len();
+  p.tot = c->tot();
+  p.active = c->active();
+  p.err = c->err_dev;
+  p.ticket = c->ticket() + 40;  // a spare word of the ticket block, zero between launches
+  p.s_new = a.o.s_new;
+  p.accumulate = (c->score_source == DYNTS_SCORE_ATTENTION && !a.o.stage) ? 1 : 0;
+  p.mass = a.o.mass;
+  const bool want_mass = p.accumulate || p.mass;
+  p.lse = want_mass ? reinterpret_cast<float*>(a.scratch) : nullptr;
+  p.slopes = a.o.slopes;
+  p.layer0 = layer0;
+  p.n_layers = n_layers;
+  p.total = (int)total;
+  p.Nb = f.batch;
+  p.Hq = f.q_heads;
+  p.Hkv = f.kv_heads;
+  p.G = c->G;
+  p.d = f.head_dim;
+  p.cap = c->cap;
+  p.window = a.o.window;
+  p.publish = publish ? 1 : 0;
+  const bool kv8 = f.dtype == DYNTS_BF16_KV8;
+  p.scale = (float)((kv8 ? (double)c->k_scale : 1.0) / std::sqrt((double)f.head_dim));
+  p.cap_logit = a.o.softcap;
+  p.k_scale = c->k_scale;
+  p.v_scale = c->v_scale;
+  p.zero_tail = 0;
+
+  long long tok = 0;
+  for (int b0 = 0; b0 < f.batch; b0 += dynts::kExtSeqs) {
+    const int n_seq = std::min(dynts::kExtSeqs, f.batch - b0);
+    p.seqs.n = n_seq;
+    p.seqs.b0 = b0;
+    for (int s = 0; s < n_seq; ++s) {
+      p.seqs.tok0[s] = (int)tok;
+      p.seqs.prefix[s] = a.o.prefix ? a.o.prefix[b0 + s] : 0;
+      tok += a.n_new[b0 + s];
+    }
+    p.seqs.tok0[n_seq] = (int)tok;
+    const int n_tok = p.seqs.tok0[n_seq] - p.seqs.tok0[0];
+    if (n_tok == 0) continue;
+    p.published = 0;
+    // one 16-byte piece of K and of V per thread, up to a few CTAs per SM
+    const long long pieces = (long long)n_layers * n_tok * f.kv_heads * (f.head_dim * c->elt / 16);
+    const unsigned grid = (unsigned)std::max<long long>(1, std::min<long long>((pieces + 255) / 256, 8ll * c->sm_count));
+    if (kv8) dynts::extend_store_kernel<__nv_bfloat16, true><<<grid, 256, 0, c->stream>>>(p);
+    else if (f.dtype == DYNTS_FP32) dynts::extend_store_kernel<float, false><<<grid, 256, 0, c->stream>>>(p);
+    else dynts::extend_store_kernel<__nv_bfloat16, false><<<grid, 256, 0, c->stream>>>(p);
+    CUDA_TRY(cudaGetLastError());
+    c->launches += 1;
+    p.published = p.publish;
+    dynts_status_t st = kv8 ? launch_extend_generic<__nv_bfloat16, true>(c, p, want_mass)
+                        : f.dtype == DYNTS_FP32 ? launch_extend_generic<float, false>(c, p, want_mass)
+                                                : launch_extend_generic<__nv_bfloat16, false>(c, p, want_mass);
+    if (st != DYNTS_OK) return st;
+  }
+  return DYNTS_OK;
+}
+
+// The host's copy of the lengths after a chunk whose last layer has been issued.
+void finish_extend(dynts_cache* c, const int* n_new, bool stage) {
+  for (int b = 0; b < c->cfg.batch; ++b) {
+    if (n_new[b] == 0 || stage) continue;
+    c->len_h[b] += n_new[b];
+    c->tot_h[b] += n_new[b];
+    c->active_h[b] = 1;
+  }
+  if (stage) c->staged_h.assign(n_new, n_new + c->cfg.batch);
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t dynts_extend_scratch_bytes(const dynts_cache_t* c, const int* n_new, int n_layers) {
+  if (!c || !n_new || n_layers < 1 || n_layers > c->cfg.layers) return 0;
+  long long total = 0;
+  for (int b = 0; b < c->cfg.batch; ++b) {
+    if (n_new[b] < 0) return 0;
+    total += n_new[b];
+  }
+  return std::max<size_t>(256, extend_scratch(c->cfg, total, n_layers));
+}
+
+dynts_status_t dynts_extend_attn(dynts_cache_t* c, const void* q, const void* k_new, const void* v_new, void* out, const int* n_new,
+                                 const dynts_extend_opts_t* opts, void* scratch, size_t scratch_bytes) {
+  if (!c) return fail(DYNTS_ERR_INVALID_ARG, "NULL cache");
+  try {
+    if (c->layer_cursor != 0) return fail(DYNTS_ERR_STATE, "a layer-by-layer step is in progress");
+    ExtendCall a{q, k_new, v_new, out, n_new, {}, static_cast<char*>(scratch), scratch_bytes};
+    if (opts) a.o = *opts;
+    long long total = 0;
+    dynts_status_t st = check_extend(c, a, c->cfg.layers, &total);
+    if (st != DYNTS_OK) return st;
+    st = materialise(c);
+    if (st != DYNTS_OK) return st;
+    st = launch_extend(c, 0, c->cfg.layers, a, total, !a.o.stage);
+    if (st == DYNTS_OK) finish_extend(c, n_new, a.o.stage != 0);
+    return st;
+  } catch (const std::bad_alloc&) {
+    return fail(DYNTS_ERR_OOM, "out of host memory");
+  }
+}
+
+dynts_status_t dynts_extend_attn_layer(dynts_cache_t* c, int layer, const void* q, const void* k_new, const void* v_new, void* out,
+                                       const int* n_new, const dynts_extend_opts_t* opts, void* scratch, size_t scratch_bytes) {
+  if (!c) return fail(DYNTS_ERR_INVALID_ARG, "NULL cache");
+  try {
+    if (layer != c->layer_cursor || layer >= c->cfg.layers)
+      return fail(DYNTS_ERR_STATE, "layer %d called, layer %d expected", layer, c->layer_cursor);
+    if (layer != 0 && !c->extending) return fail(DYNTS_ERR_STATE, "the step in progress is a decode step");
+    ExtendCall a{q, k_new, v_new, out, n_new, {}, static_cast<char*>(scratch), scratch_bytes};
+    if (opts) a.o = *opts;
+    long long total = 0;
+    dynts_status_t st = check_extend(c, a, 1, &total);
+    if (st != DYNTS_OK) return st;
+    st = materialise(c);
+    if (st != DYNTS_OK) return st;
+    if (layer == 0) {
+      c->chunk_h.assign(n_new, n_new + c->cfg.batch);
+      c->chunk_staged = a.o.stage != 0;
+    } else if (!std::equal(c->chunk_h.begin(), c->chunk_h.end(), n_new) || c->chunk_staged != (a.o.stage != 0)) {
+      return fail(DYNTS_ERR_STATE, "layer %d: n_new and stage must be those of layer 0", layer);
+    }
+    const bool last = layer == c->cfg.layers - 1;
+    st = launch_extend(c, layer, 1, a, total, last && !a.o.stage);
+    if (st != DYNTS_OK) return st;
+    c->extending = !last;
+    c->layer_cursor = last ? 0 : layer + 1;
+    if (last) finish_extend(c, n_new, a.o.stage != 0);
+    return DYNTS_OK;
+  } catch (const std::bad_alloc&) {
+    return fail(DYNTS_ERR_OOM, "out of host memory");
+  }
+}
+
+dynts_status_t dynts_extend_commit(dynts_cache_t* c, const int* n_accept) {
+  if (!c || !n_accept) return fail(DYNTS_ERR_INVALID_ARG, "NULL argument");
+  if (!c->ready || c->staged_h.empty()) return fail(DYNTS_ERR_STATE, "no staged chunk lies behind the sequences' ends");
+  if (c->layer_cursor != 0) return fail(DYNTS_ERR_STATE, "a layer-by-layer step is in progress");
+  const int Nb = c->cfg.batch;
+  for (int b = 0; b < Nb; ++b)
+    if (n_accept[b] < 0 || n_accept[b] > c->staged_h[b])
+      return fail(DYNTS_ERR_INVALID_ARG, "sequence %d: %d rows accepted of %d staged", b, n_accept[b], c->staged_h[b]);
+  {
+    dynts_status_t fs = flush_pending(c);
+    if (fs != DYNTS_OK) return fs;
+  }
+  for (int b0 = 0; b0 < Nb; b0 += dynts::kExtSeqs) {
+    dynts::ExtendSeqs q;
+    q.n = std::min(dynts::kExtSeqs, Nb - b0);
+    q.b0 = b0;
+    q.tok0[0] = 0;
+    for (int s = 0; s < q.n; ++s) q.tok0[s + 1] = q.tok0[s] + n_accept[b0 + s];
+    if (q.tok0[q.n] == 0) continue;
+    dynts::extend_commit_kernel<<<1, dynts::kExtSeqs, 0, c->stream>>>(q, c->len(), c->tot(), c->active(), c->cap, c->err_dev);
+    CUDA_TRY(cudaGetLastError());
+    c->launches += 1;
+  }
+  c->staged_h.clear();
+  for (int b = 0; b < Nb; ++b) {
+    if (n_accept[b] == 0) continue;
+    c->len_h[b] += n_accept[b];
+    c->tot_h[b] += n_accept[b];
+    c->active_h[b] = 1;
+  }
+  return DYNTS_OK;
+}
+
+/* ---- rotary positions --------------------------------------------------------------------- */
+
+dynts_status_t dynts_rope(const void* q, const void* k, const int* pos, void* q_out, void* k_out, int n_tokens, int q_heads, int kv_heads,
+                          int head_dim, int rot_dim, int n_axes, const int* sections, int flags, double theta, int dtype,
+                          const long long* strides, void* stream) {
+  if (n_tokens < 0 || q_heads < 1 || kv_heads < 0 || head_dim < 2 || head_dim > 256)
+    return fail(DYNTS_ERR_INVALID_ARG, "bad shape: %d tokens, %d / %d heads of %d", n_tokens, q_heads, kv_heads, head_dim);
+  if (rot_dim < 2 || rot_dim % 2 || rot_dim > head_dim) return fail(DYNTS_ERR_INVALID_ARG, "rot_dim %d must be even and at most head_dim", rot_dim);
+  if (n_axes < 1 || n_axes > dynts::kRopeMaxAxes) return fail(DYNTS_ERR_INVALID_ARG, "1 to %d axes", dynts::kRopeMaxAxes);
+  if (flags & ~(DYNTS_ROPE_ADJACENT | DYNTS_ROPE_ROUND_ROBIN)) return fail(DYNTS_ERR_INVALID_ARG, "unknown flags 0x%x", flags);
+  if (dtype != DYNTS_BF16 && dtype != DYNTS_FP32) return fail(DYNTS_ERR_INVALID_ARG, "dtype must be DYNTS_BF16 or DYNTS_FP32");
+  if (!(theta > 0.0) || std::isinf(theta)) return fail(DYNTS_ERR_INVALID_ARG, "theta must be positive and finite");
+  dynts::RopeParams p;
+  if (sections) {
+    int sum = 0;
+    for (int x = 0; x < n_axes; ++x) {
+      if (sections[x] < 0 || sections[x] > rot_dim / 2) return fail(DYNTS_ERR_INVALID_ARG, "section %d of axis %d", sections[x], x);
+      sum += sections[x];
+    }
+    if (sum != rot_dim / 2) return fail(DYNTS_ERR_INVALID_ARG, "the sections hold %d pairs, rot_dim has %d", sum, rot_dim / 2);
+  } else if (n_axes != 1) {
+    return fail(DYNTS_ERR_INVALID_ARG, "several axes need their sections");
+  }
+  for (int x = 0; x < dynts::kRopeMaxAxes; ++x) p.section[x] = x < n_axes ? (sections ? sections[x] : rot_dim / 2) : 0;
+  if (n_tokens == 0) return DYNTS_OK;
+  if (!k) kv_heads = 0;
+  const bool with_k = kv_heads > 0;
+  if (!q || !q_out || !pos || (with_k && !k_out)) return fail(DYNTS_ERR_INVALID_ARG, "NULL tensor pointer");
+  if (!aligned16(q) || !aligned16(q_out) || (with_k && (!aligned16(k) || !aligned16(k_out))))
+    return fail(DYNTS_ERR_INVALID_ARG, "tensor pointers must be 16-byte aligned");
+  const long long qd = (long long)q_heads * head_dim, kd = (long long)kv_heads * head_dim;
+  p.q_stride = strides && strides[0] ? strides[0] : qd;
+  p.k_stride = strides && strides[1] ? strides[1] : kd;
+  p.qo_stride = strides && strides[2] ? strides[2] : qd;
+  p.ko_stride = strides && strides[3] ? strides[3] : kd;
+  if (p.q_stride < qd || p.qo_stride < qd || p.k_stride < kd || p.ko_stride < kd)
+    return fail(DYNTS_ERR_INVALID_ARG, "token strides must cover a token");
+  p.q = q;
+  p.k = with_k ? k : nullptr;
+  p.q_out = q_out;
+  p.k_out = k_out;
+  p.pos = pos;
+  p.n_tokens = n_tokens;
+  p.Hq = q_heads;
+  p.Hkv = kv_heads;
+  p.d = head_dim;
+  p.rot = rot_dim;
+  p.axes = n_axes;
+  p.adjacent = (flags & DYNTS_ROPE_ADJACENT) ? 1 : 0;
+  p.round_robin = (flags & DYNTS_ROPE_ROUND_ROBIN) ? 1 : 0;
+  p.log2_theta = std::log2(theta);
+  // Several tokens per CTA once the batch fills the GPU's SMs several times over.
+  p.tokens_per_cta = n_tokens >= 148 * 8 * dynts::kRopeTokens ? dynts::kRopeTokens : 1;
+  const unsigned grid = (unsigned)((n_tokens + p.tokens_per_cta - 1) / p.tokens_per_cta);
+  const int V = dtype == DYNTS_FP32 ? 4 : 8;
+  const int part = p.adjacent ? rot_dim : rot_dim / 2;
+  const bool wide = part % V == 0 && (head_dim - rot_dim) % V == 0 && head_dim % V == 0 && p.q_stride % V == 0 && p.k_stride % V == 0 &&
+                    p.qo_stride % V == 0 && p.ko_stride % V == 0;
+  const cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (dtype == DYNTS_FP32) {
+    if (wide) dynts::rope_kernel<float, 4><<<grid, dynts::kRopeThreads, 0, st>>>(p);
+    else if (p.adjacent) dynts::rope_kernel<float, 2><<<grid, dynts::kRopeThreads, 0, st>>>(p);
+    else dynts::rope_kernel<float, 1><<<grid, dynts::kRopeThreads, 0, st>>>(p);
+  } else {
+    if (wide) dynts::rope_kernel<__nv_bfloat16, 8><<<grid, dynts::kRopeThreads, 0, st>>>(p);
+    else if (p.adjacent) dynts::rope_kernel<__nv_bfloat16, 2><<<grid, dynts::kRopeThreads, 0, st>>>(p);
+    else dynts::rope_kernel<__nv_bfloat16, 1><<<grid, dynts::kRopeThreads, 0, st>>>(p);
+  }
+  CUDA_TRY(cudaGetLastError());
   return DYNTS_OK;
 }
 

@@ -1,0 +1,417 @@
+// A chunk of new tokens per sequence against the rows a cache holds (Eq. 4-6 for several queries at
+// once): the rows are stored behind the sequence's end, token i of a chunk that begins at row n
+// attends to the rows [0, n + i], and -- if wanted -- every row receives the attention mass the
+// chunk's queries gave it.  This file holds what every shape shares (parameters, the definition of
+// a logit and of visibility, the kernel that stores the rows and publishes the lengths) and the
+// fp32-FMA kernels that serve every type and head size; extend_tc.cuh holds the tensor-core kernels
+// for head_dim 128.
+//
+// Definitions, for query token i of a sequence and row j (p = positions, kept by rows that survive
+// an eviction):
+//   x   = q_i . k_j / sqrt(d)
+//   x   = c tanh(x / c)                      if a cap c > 0 is given
+//   x  -= slope_h |p_i - p_j|                if slopes are given
+//   row j is visible  <=>  j <= n + i, or j is one of the chunk's first `prefix` rows;
+//                          and |p_i - p_j| < window, if a window is given
+// A token always sees itself, so no row of weights is empty.  All logits are kept in base-2 units
+// (times log2 e), sums and maxima in fp32.
+#pragma once
+
+#include <math_constants.h>
+
+#include "common.cuh"
+
+namespace dynts {
+
+constexpr int kExtSeqs = 128;          // sequences of one launch (a larger batch takes several)
+constexpr int kExtGenericRows = 32;    // query rows (token, head of the group) per CTA of the generic kernel
+constexpr int kExtGenericKeys = 32;    // keys per tile of the generic kernels
+constexpr int kExtGenericThreads = 256;
+constexpr int kExtTileKeys = 64;       // keys per tile of the tensor-core kernel; rows up to its end are zeroed behind the chunk
+
+struct ExtendSeqs {
+  int n;                          // sequences of this launch, b0 .. b0 + n - 1
+  int b0;
+  int tok0[kExtSeqs + 1];         // first packed token of each (the chunk of sequence s: tok0[s] .. tok0[s + 1] - 1)
+  int item0[kExtSeqs + 1];        // first work item of each (what an item is depends on the kernel)
+  int prefix[kExtSeqs];           // leading tokens of the chunk that every token of the chunk sees
+};
+
+struct ExtendParams {
+  const void* q;      // [n_layers][total][Hq][d], token stride q_stride elements
+  const void* k;      // [n_layers][total][Hkv][d]
+  const void* v;
+  void* out;          // [n_layers][total][Hq][d], contiguous
+  long long q_stride, k_stride, v_stride;
+  void* K;            // full [L, Nb, Hkv, cap, d]
+  void* V;
+  int* pos;
+  float* score;
+  float* comp;
+  int* len;           // [Nb]
+  int* tot;
+  int* active;
+  int* err;
+  unsigned int* ticket;
+  const float* s_new; // [total] scores of the new rows, or NULL: 0
+  float* lse;         // [n_layers][total][Hq] log2 of the sum of the weights' exponentials, or NULL
+  float* mass;        // full [L, Nb, Hkv, cap], or NULL
+  const float* slopes;  // [Hq] or NULL
+  int layer0, n_layers, total;
+  int Nb, Hq, Hkv, G, d, cap;
+  int window;         // 0: none
+  int publish;        // the storing kernel advances the lengths when it is done
+  int published;      // the lengths on the device include the chunk already
+  int accumulate;     // the mass is added to the scores
+  int zero_tail;      // the storing kernel clears the V rows from the chunk's end to the end of the key tile
+  float scale;        // 1 / sqrt(d), times k_scale for 8-bit rows
+  float cap_logit;    // c, or 0
+  float k_scale, v_scale;  // 8-bit rows
+  ExtendSeqs seqs;
+};
+
+__device__ __forceinline__ int ext_find(const int* first, int n, int x) {  // the s with first[s] <= x < first[s + 1]
+  int lo = 0, hi = n;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (first[mid] <= x) lo = mid;
+    else hi = mid;
+  }
+  return lo;
+}
+
+// Rows held and tokens seen before the chunk.
+struct ExtSeq {
+  int b, t, n, tot;
+  bool ok;  // the chunk fits the slab (what the host's mirror checked before the launch)
+};
+__device__ __forceinline__ ExtSeq ext_seq(const ExtendParams& p, int s) {
+  ExtSeq e;
+  e.b = p.seqs.b0 + s;
+  e.t = p.seqs.tok0[s + 1] - p.seqs.tok0[s];
+  e.n = p.len[e.b] - (p.published ? e.t : 0);
+  e.tot = p.tot[e.b] - (p.published ? e.t : 0);
+  e.ok = e.n >= 0 && e.n + e.t <= p.cap;
+  return e;
+}
+
+// Stores the chunk's rows: K and V (encoded for 8-bit slabs), position, score; with `publish` the
+// last CTA to finish advances the lengths.  Bandwidth-bound and short: a row is read and written once.
+template <typename T, bool KV8>
+__global__ void __launch_bounds__(256) extend_store_kernel(const __grid_constant__ ExtendParams p) {
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // the next kernel's set-up may begin; it waits for this grid before it reads
+  constexpr int E = 16 / (int)sizeof(T);  // elements per 16-byte piece of the source
+  const int pieces = p.d / E;
+  const int tok_begin = p.seqs.tok0[0], n_tok = p.seqs.tok0[p.seqs.n] - tok_begin;
+  const long long work = (long long)p.n_layers * n_tok * p.Hkv * pieces;
+  const long long stride = (long long)gridDim.x * blockDim.x;
+  const long long first = (long long)blockIdx.x * blockDim.x + threadIdx.x;
+  for (long long w = first; w < work; w += stride) {
+    const int piece = (int)(w % pieces);
+    long long r = w / pieces;
+    const int h = (int)(r % p.Hkv);
+    r /= p.Hkv;
+    const int tok = tok_begin + (int)(r % n_tok), layer = (int)(r / n_tok);
+    const int s = ext_find(p.seqs.tok0, p.seqs.n, tok);
+    ExtSeq e;
+    e.b = p.seqs.b0 + s;
+    e.t = p.seqs.tok0[s + 1] - p.seqs.tok0[s];
+    e.n = p.len[e.b];
+    const int i = tok - p.seqs.tok0[s];
+    if (e.n < 0 || e.n + e.t > p.cap) {
+      if (piece == 0 && h == 0 && i == 0) atomicOr(p.err, kErrLenOverflow);
+      continue;
+    }
+    const size_t slab = ((size_t)(p.layer0 + layer) * p.Nb + e.b) * p.Hkv + h;
+    const size_t row = slab * p.cap + e.n + i;
+    const size_t src_tok = (size_t)layer * p.total + tok;
+    const uint4 kk = *reinterpret_cast<const uint4*>(static_cast<const T*>(p.k) + src_tok * p.k_stride + (size_t)h * p.d + piece * E);
+    const uint4 vv = *reinterpret_cast<const uint4*>(static_cast<const T*>(p.v) + src_tok * p.v_stride + (size_t)h * p.d + piece * E);
+    if constexpr (KV8) {
+      const __nv_bfloat16* kx = reinterpret_cast<const __nv_bfloat16*>(&kk);
+      const __nv_bfloat16* vx = reinterpret_cast<const __nv_bfloat16*>(&vv);
+      uint32_t kc[2] = {0u, 0u}, vc[2] = {0u, 0u};
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        kc[u >> 2] |= (uint32_t)store_e4m3(__bfloat162float(kx[u]), p.k_scale) << (8 * (u & 3));
+        vc[u >> 2] |= (uint32_t)store_e4m3(__bfloat162float(vx[u]), p.v_scale) << (8 * (u & 3));
+      }
+      *reinterpret_cast<uint2*>(static_cast<uint8_t*>(p.K) + row * p.d + piece * 8) = make_uint2(kc[0], kc[1]);
+      *reinterpret_cast<uint2*>(static_cast<uint8_t*>(p.V) + row * p.d + piece * 8) = make_uint2(vc[0], vc[1]);
+    } else {
+      *reinterpret_cast<uint4*>(static_cast<T*>(p.K) + row * p.d + piece * E) = kk;
+      *reinterpret_cast<uint4*>(static_cast<T*>(p.V) + row * p.d + piece * E) = vv;
+    }
+    if (piece == 0) {
+      p.pos[row] = p.tot[e.b] + i;
+      p.score[row] = p.s_new ? p.s_new[tok] : 0.f;
+      p.comp[row] = 0.f;
+    }
+  }
+  if (p.zero_tail) {
+    // The tensor-core kernel multiplies whole key tiles: weight zero times whatever lies behind the
+    // chunk's end must be zero, so the V rows up to the end of that tile are cleared (rows behind a
+    // sequence's end belong to nobody).
+    constexpr int KE = KV8 ? 16 : E;
+    const int kp = p.d / KE;
+    const long long tail = (long long)p.n_layers * p.seqs.n * p.Hkv * (kExtTileKeys - 1) * kp;
+    for (long long w = first; w < tail; w += stride) {
+      const int piece = (int)(w % kp);
+      long long r = w / kp;
+      const int x = (int)(r % (kExtTileKeys - 1));
+      r /= kExtTileKeys - 1;
+      const int h = (int)(r % p.Hkv);
+      r /= p.Hkv;
+      const int s = (int)(r % p.seqs.n), layer = (int)(r / p.seqs.n);
+      const int b = p.seqs.b0 + s, t = p.seqs.tok0[s + 1] - p.seqs.tok0[s];
+      const int end = p.len[b] + t, row = end + x;
+      if (t == 0 || row >= p.cap || row >= (end + kExtTileKeys - 1) / kExtTileKeys * kExtTileKeys) continue;
+      const size_t slab = ((size_t)(p.layer0 + layer) * p.Nb + b) * p.Hkv + h;
+      char* dst = static_cast<char*>(p.V) + ((slab * p.cap + row) * p.d + (size_t)piece * KE) * (KV8 ? 1 : sizeof(T));
+      *reinterpret_cast<uint4*>(dst) = make_uint4(0u, 0u, 0u, 0u);
+    }
+  }
+  if (p.publish) {
+    // every CTA has read the lengths before it takes its ticket; the last one advances them
+    __syncthreads();
+    __shared__ int last;
+    if (threadIdx.x == 0) last = atomicAdd(p.ticket, 1u) == gridDim.x - 1;
+    __syncthreads();
+    if (last) {
+      for (int s = threadIdx.x; s < p.seqs.n; s += blockDim.x) {
+        const int b = p.seqs.b0 + s, t = p.seqs.tok0[s + 1] - p.seqs.tok0[s];
+        if (t > 0 && p.len[b] + t <= p.cap) {
+          p.len[b] += t;
+          p.tot[b] += t;
+          p.active[b] = 1;
+        }
+      }
+      if (threadIdx.x == 0) *p.ticket = 0u;
+    }
+  }
+}
+
+// Advances the lengths by the accepted part of a staged chunk.  One block; tok0 holds the running sums.
+__global__ void __launch_bounds__(kExtSeqs) extend_commit_kernel(const ExtendSeqs q, int* len, int* tot, int* active, int cap, int* err) {
+  const int s = threadIdx.x;
+  if (s >= q.n) return;
+  const int t = q.tok0[s + 1] - q.tok0[s], b = q.b0 + s;
+  if (t == 0) return;
+  if (len[b] + t > cap) {
+    atomicOr(err, kErrLenOverflow);
+    return;
+  }
+  len[b] += t;
+  tot[b] += t;
+  active[b] = 1;
+}
+
+// A logit in base-2 units (before the visibility test), from the raw dot product.
+__device__ __forceinline__ float ext_logit_exact(const ExtendParams& p, float dot, float slope, int apart) {
+  float x = dot * p.scale;
+  if (p.cap_logit > 0.f) x = p.cap_logit * tanhf(x / p.cap_logit);
+  x -= slope * (float)apart;
+  return x * 1.4426950408889634f;
+}
+
+template <typename T, bool KV8>
+__device__ __forceinline__ float ext_row_value(const void* base, size_t idx, float scale) {
+  if constexpr (KV8) return e4m3_to_float(static_cast<const uint8_t*>(base)[idx]) * scale;
+  else return to_float(static_cast<const T*>(base)[idx]);
+}
+
+constexpr size_t ext_generic_smem(int d) {  // Q [32][d], K [32][d + 4], V [32][d], positions of the tile
+  return ((size_t)kExtGenericRows * d + (size_t)kExtGenericKeys * (d + 4) + (size_t)kExtGenericKeys * d + kExtGenericKeys) * sizeof(float);
+}
+
+// Any type, any head size: fp32 FMA.  CTA = 32 query rows of one (layer, sequence, KV head), four per
+// warp; lane = key for the products and the softmax, lane = column of head_dim for the output.  The
+// weights are exact fp32 (exp2f, tanhf).  Bound by FMA and shared-memory issue; it serves fp32 slabs
+// (where the tensor cores' formats could not hold 2e-5) and head sizes other than 128.
+template <typename T, bool KV8>
+__global__ void __launch_bounds__(kExtGenericThreads) extend_generic_kernel(const __grid_constant__ ExtendParams p) {
+  extern __shared__ __align__(16) float ext_sm[];
+  const int d = p.d, ldk = d + 4;
+  float* sQ = ext_sm;
+  float* sK = sQ + kExtGenericRows * d;
+  float* sV = sK + kExtGenericKeys * ldk;
+  int* sP = reinterpret_cast<int*>(sV + kExtGenericKeys * d);
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const int s = ext_find(p.seqs.item0, p.seqs.n, blockIdx.x);
+  const ExtSeq e = ext_seq(p, s);
+  if (!e.ok) return;
+  const int layer = blockIdx.y / p.Hkv, h = blockIdx.y % p.Hkv;
+  const int r0 = ((int)blockIdx.x - p.seqs.item0[s]) * kExtGenericRows;
+  const int rows = min(kExtGenericRows, e.t * p.G - r0);
+  const size_t tok_base = (size_t)layer * p.total + p.seqs.tok0[s];
+  const size_t slab = ((size_t)(p.layer0 + layer) * p.Nb + e.b) * p.Hkv + h;
+  for (int x = tid; x < kExtGenericRows * d; x += kExtGenericThreads) {
+    const int r = x / d, c = x - r * d;
+    float y = 0.f;
+    if (r < rows) {
+      const int i = (r0 + r) / p.G, g = (r0 + r) - i * p.G;
+      y = to_float(static_cast<const T*>(p.q)[(tok_base + i) * p.q_stride + (size_t)(h * p.G + g) * d + c]);
+    }
+    sQ[x] = y;
+  }
+  // this warp's rows
+  int tok[4];
+  float slope[4], m[4], l[4], acc[4][8];
+#pragma unroll
+  for (int u = 0; u < 4; ++u) {
+    const int r = r0 + warp * 4 + u;
+    tok[u] = min(r / p.G, e.t - 1);
+    slope[u] = p.slopes ? p.slopes[h * p.G + r % p.G] : 0.f;
+    m[u] = -CUDART_INF_F;
+    l[u] = 0.f;
+#pragma unroll
+    for (int c = 0; c < 8; ++c) acc[u][c] = 0.f;
+  }
+  const int prefix = p.seqs.prefix[s];
+  const int i0 = r0 / p.G, i1 = min(e.t - 1, (r0 + rows - 1) / p.G);
+  const int end = e.n + max(i1 + 1, prefix);
+  // (positions ascend with the rows, so a row more than `window` rows back is more than `window` positions back)
+  const int begin = p.window > 0 ? max(0, e.n + i0 - p.window + 1) : 0;
+  for (int k0 = begin / kExtGenericKeys * kExtGenericKeys; k0 < end; k0 += kExtGenericKeys) {
+    __syncthreads();
+    for (int x = tid; x < kExtGenericKeys * d; x += kExtGenericThreads) {
+      const int r = x / d, c = x - r * d;
+      const bool in = k0 + r < e.n + e.t;
+      const size_t idx = (slab * p.cap + k0 + r) * d + c;
+      sK[r * ldk + c] = in ? ext_row_value<T, KV8>(p.K, idx, 1.f) : 0.f;  // (k_scale is part of p.scale)
+      sV[r * d + c] = in ? ext_row_value<T, KV8>(p.V, idx, p.v_scale) : 0.f;
+    }
+    if (tid < kExtGenericKeys) sP[tid] = k0 + tid < e.n + e.t ? p.pos[slab * p.cap + k0 + tid] : 0;
+    __syncthreads();
+    float dot[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int c = 0; c < d; c += 4) {
+      const float4 kv = *reinterpret_cast<const float4*>(sK + lane * ldk + c);
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const float4 qv = *reinterpret_cast<const float4*>(sQ + (warp * 4 + u) * d + c);
+        dot[u] = fmaf(qv.x, kv.x, fmaf(qv.y, kv.y, fmaf(qv.z, kv.z, fmaf(qv.w, kv.w, dot[u]))));
+      }
+    }
+    const int j = k0 + lane;
+    float w[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int apart = abs(e.tot + tok[u] - sP[lane]);
+      const bool visible = j < e.n + max(tok[u] + 1, prefix) && (p.window == 0 || apart < p.window);
+      const float x = visible ? ext_logit_exact(p, dot[u], slope[u], apart) : -CUDART_INF_F;
+      float mx = x;
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+      const float m_new = fmaxf(m[u], mx);
+      const float alpha = m[u] == -CUDART_INF_F ? 0.f : exp2f(m[u] - m_new);
+      w[u] = visible ? exp2f(x - m_new) : 0.f;
+      float sum = w[u];
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+      l[u] = l[u] * alpha + sum;
+      m[u] = m_new;
+#pragma unroll
+      for (int c = 0; c < 8; ++c) acc[u][c] *= alpha;
+    }
+    for (int kk = 0; kk < kExtGenericKeys; ++kk) {
+      float wk[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) wk[u] = __shfl_sync(0xffffffffu, w[u], kk);
+#pragma unroll
+      for (int c = 0; c < 8; ++c) {
+        if (c * 32 >= d) break;
+        const int col = c * 32 + lane;
+        const float vv = col < d ? sV[kk * d + col] : 0.f;
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+          if (wk[u] != 0.f) acc[u][c] = fmaf(wk[u], vv, acc[u][c]);  // (a hidden row contributes nothing, whatever it holds)
+      }
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < 4; ++u) {
+    const int rl = warp * 4 + u;
+    if (rl >= rows) continue;
+    const int r = r0 + rl, i = r / p.G, head = h * p.G + r % p.G;
+    T* o = static_cast<T*>(p.out) + ((tok_base + i) * p.Hq + head) * d;
+#pragma unroll
+    for (int c = 0; c < 8; ++c) {
+      const int col = c * 32 + lane;
+      if (col < d) from_float(o + col, acc[u][c] / l[u]);
+    }
+    if (p.lse && lane == 0) p.lse[(tok_base + i) * p.Hq + head] = m[u] + log2f(l[u]);
+  }
+}
+
+// What the mass kernels do with a row's total: exactly one thread owns the row.
+__device__ __forceinline__ void ext_emit_mass(const ExtendParams& p, size_t row, float x) {
+  if (p.mass) p.mass[row] = x;
+  if (p.accumulate) {
+    float sc = p.score[row], c = p.comp[row];
+    kahan_add(sc, c, x);
+    p.score[row] = sc;
+    p.comp[row] = c;
+  }
+}
+
+constexpr size_t ext_generic_mass_smem(int d) {  // K [32][d + 4], one query row per warp, partial sums
+  return ((size_t)kExtGenericKeys * (d + 4) + (size_t)(kExtGenericThreads / 32) * d + (kExtGenericThreads / 32) * kExtGenericKeys) * sizeof(float);
+}
+
+// mass_j = sum over the chunk's tokens and the group's heads of the weight of row j, from the logits
+// and each query row's log-sum-exp.  CTA = 32 rows of one slab; the warps take the query rows in
+// turn, lane = key; the eight partial sums are added in a fixed order.
+template <typename T, bool KV8>
+__global__ void __launch_bounds__(kExtGenericThreads) extend_generic_mass_kernel(const __grid_constant__ ExtendParams p) {
+  extern __shared__ __align__(16) float ext_sm[];
+  const int d = p.d, ldk = d + 4;
+  constexpr int W = kExtGenericThreads / 32;
+  float* sK = ext_sm;
+  float* sQ = sK + kExtGenericKeys * ldk;
+  float* sS = sQ + W * d;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const int layer = blockIdx.y / p.Hkv, h = blockIdx.y % p.Hkv, s = blockIdx.z;
+  const ExtSeq e = ext_seq(p, s);
+  const int k0 = blockIdx.x * kExtGenericKeys;
+  if (!e.ok || e.t == 0 || k0 >= e.n + e.t) return;
+  const size_t tok_base = (size_t)layer * p.total + p.seqs.tok0[s];
+  const size_t slab = ((size_t)(p.layer0 + layer) * p.Nb + e.b) * p.Hkv + h;
+  for (int x = tid; x < kExtGenericKeys * d; x += kExtGenericThreads) {
+    const int r = x / d, c = x - r * d;
+    sK[r * ldk + c] = k0 + r < e.n + e.t ? ext_row_value<T, KV8>(p.K, (slab * p.cap + k0 + r) * d + c, 1.f) : 0.f;
+  }
+  __syncthreads();
+  const int j = k0 + lane;
+  const int pj = j < e.n + e.t ? p.pos[slab * p.cap + j] : 0;
+  const int prefix = p.seqs.prefix[s];
+  float sum = 0.f;
+  for (int r = warp; r < e.t * p.G; r += W) {
+    const int i = r / p.G, head = h * p.G + r % p.G;
+    if (e.n + max(i + 1, prefix) <= k0) continue;  // (uniform over the warp)
+    const T* q = static_cast<const T*>(p.q) + (tok_base + i) * p.q_stride + (size_t)head * d;
+    __syncwarp();
+    for (int c = lane; c < d; c += 32) sQ[warp * d + c] = to_float(q[c]);
+    __syncwarp();
+    float dot = 0.f;
+    for (int c = 0; c < d; c += 4) {
+      const float4 kv = *reinterpret_cast<const float4*>(sK + lane * ldk + c);
+      const float4 qv = *reinterpret_cast<const float4*>(sQ + warp * d + c);
+      dot = fmaf(qv.x, kv.x, fmaf(qv.y, kv.y, fmaf(qv.z, kv.z, fmaf(qv.w, kv.w, dot))));
+    }
+    const int apart = abs(e.tot + i - pj);
+    if (j < e.n + max(i + 1, prefix) && (p.window == 0 || apart < p.window))
+      sum += exp2f(ext_logit_exact(p, dot, p.slopes ? p.slopes[head] : 0.f, apart) - p.lse[(tok_base + i) * p.Hq + head]);
+  }
+  sS[warp * kExtGenericKeys + lane] = sum;
+  __syncthreads();
+  if (warp == 0 && j < e.n + e.t) {
+    float x = 0.f;
+#pragma unroll
+    for (int w = 0; w < W; ++w) x += sS[w * kExtGenericKeys + lane];
+    ext_emit_mass(p, slab * p.cap + j, x);
+  }
+}
+
+}  // namespace dynts
