@@ -20,6 +20,7 @@
 #include "decode_stream.cuh"
 #include "evict.cuh"
 #include "extend.cuh"
+#include "extend_tc.cuh"
 #include "predictor.cuh"
 #include "prefill_attn.cuh"
 #include "rope.cuh"
@@ -117,6 +118,10 @@ Layout make_layout(const dynts_config_t* c, int cap) {
 
 }  // namespace
 
+typedef CUresult (*tensor_map_encode_fn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
+                                         const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
+                                         CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
 struct dynts_cache {
   dynts_config_t cfg;
   int cap = 0;
@@ -150,8 +155,12 @@ struct dynts_cache {
   size_t stage_bytes = 0;
   bool attr_generic_f32 = false, attr_generic_bf16 = false, attr_generic_kv8 = false, attr_mma = false, attr_select = false;
   bool attr_stream = false, attr_fused = false, attr_prefill = false, attr_extend = false;
+  bool attr_extend_tc[2][2] = {{false, false}, {false, false}};
   bool have_maps = false;    // tensor maps of the K and V slabs for the streaming kernel
   CUtensorMap map_KV;
+  bool have_extend_maps = false;  // tensor maps of the K and V slabs for the chunk kernels
+  CUtensorMap map_XK{}, map_XV{};
+  tensor_map_encode_fn encode = nullptr;
   int sm_count = 0;
 
   void* K() const { return base + lay.K; }
@@ -181,10 +190,6 @@ bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) ==
 
 // Tensor map (TMA descriptor) over all K rows and all V rows, read in boxes of 32 rows with the
 // 128-byte shared-memory swizzle.
-typedef CUresult (*tensor_map_encode_fn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
-                                         const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
-                                         CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
 dynts_status_t make_slab_maps(dynts_cache* c) {
   void* fn = nullptr;
   cudaDriverEntryPointQueryResult qres;
@@ -1328,9 +1333,56 @@ dynts_status_t dynts_evict_stats(dynts_cache_t* c, long long* rows_scanned, long
 
 namespace {
 
-// What a chunk's launches need beside the cache: each query row's log-sum-exp.
-size_t extend_scratch(const dynts_config_t& f, long long total, int n_layers) {
-  return align_up((size_t)n_layers * total * f.q_heads * sizeof(float), 256);
+// What a chunk's launches need beside the cache, as offsets into the caller's scratch.
+struct ExtendScratch {
+  size_t lse, q16, part, counters, total;
+  int part_rows;    // query rows of a part of a cut tile
+  long long slots;  // items that the tensor-core kernel aims at when the tiles alone are fewer
+};
+
+bool extend_tc_shape(const dynts_config_t& f) { return f.dtype != DYNTS_FP32 && f.head_dim == 128; }
+
+// Tiles of 128 query rows of a launch's sequences, over layers and KV heads.
+long long extend_tiles(const dynts_config_t& f, const int* n_new, int n_seq, int n_layers) {
+  const int tpt = dynts::kXtRows / (f.q_heads / f.kv_heads);
+  long long tiles = 0;
+  for (int s = 0; s < n_seq; ++s) tiles += (n_new[s] + tpt - 1) / tpt;
+  return tiles * n_layers * f.kv_heads;
+}
+
+ExtendScratch extend_scratch(const dynts_cache* c, const int* n_new, int n_layers) {
+  const dynts_config_t& f = c->cfg;
+  ExtendScratch m;
+  long long total = 0, items = 0;
+  int longest = 0;
+  for (int b = 0; b < f.batch; ++b) {
+    total += n_new[b];
+    longest = std::max(longest, n_new[b]);
+  }
+  const int G = f.q_heads / f.kv_heads;
+  m.part_rows = (int)(((long long)std::min(longest, dynts::kXtRows / G) * G + 3) / 4 * 4);
+  // Two CTAs per SM.  Parts of few query rows cost little to join (a few KB each): four per CTA even out lengths that
+  // differ; parts of whole tiles (66 KB each) are made only to occupy every CTA once.
+  m.slots = 2ll * (c->sm_count > 0 ? c->sm_count : 148) * (m.part_rows <= 32 ? 4 : 1);
+  size_t off = 0;
+  auto take = [&](size_t bytes) {
+    const size_t o = off;
+    off = align_up(off + bytes, 256);
+    return o;
+  };
+  m.lse = take((size_t)n_layers * total * f.q_heads * sizeof(float));
+  m.q16 = m.part = m.counters = off;
+  if (extend_tc_shape(f)) {
+    if (f.dtype == DYNTS_BF16_KV8) m.q16 = take((size_t)n_layers * total * f.q_heads * f.head_dim * 2);
+    for (int b0 = 0; b0 < f.batch; b0 += dynts::kExtSeqs) {
+      const long long tiles = extend_tiles(f, n_new + b0, std::min(dynts::kExtSeqs, f.batch - b0), n_layers);
+      if (tiles < m.slots) items = std::max(items, tiles + m.slots);  // cut tiles: at most one part more than a whole share each
+    }
+    m.part = take((size_t)items * m.part_rows * dynts::kXtPartFloats * sizeof(float));
+    m.counters = take((size_t)items * sizeof(int));
+  }
+  m.total = std::max<size_t>(off, 256);
+  return m;
 }
 
 struct ExtendCall {
@@ -1375,7 +1427,7 @@ dynts_status_t check_extend(const dynts_cache* c, const ExtendCall& a, int n_lay
     if (!a.q || !a.k || !a.v || !a.out) return fail(DYNTS_ERR_INVALID_ARG, "NULL tensor pointer");
     if (!aligned16(a.q) || !aligned16(a.k) || !aligned16(a.v) || !aligned16(a.out))
       return fail(DYNTS_ERR_INVALID_ARG, "tensor pointers must be 16-byte aligned");
-    const size_t need = extend_scratch(f, total, n_layers);
+    const size_t need = extend_scratch(c, a.n_new, n_layers).total;
     if (!a.scratch || !aligned16(a.scratch)) return fail(DYNTS_ERR_INVALID_ARG, "scratch must be non-NULL and 16-byte aligned");
     if (a.scratch_bytes < need) return fail(DYNTS_ERR_OOM, "scratch too small: %zu < %zu bytes", a.scratch_bytes, need);
   }
@@ -1430,6 +1482,108 @@ dynts_status_t launch_extend_generic(dynts_cache* c, dynts::ExtendParams& p, boo
   return DYNTS_OK;
 }
 
+// Tensor maps of the K and V slabs, [slabs][cap][128] bf16 in boxes of 64 rows x 64 elements: made once per cache.
+dynts_status_t extend_maps(dynts_cache* c) {
+  if (c->encode == nullptr) {
+    void* fn = nullptr;
+    cudaDriverEntryPointQueryResult qres;
+    CUDA_TRY(cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &qres));
+    if (!fn || qres != cudaDriverEntryPointSuccess) return fail(DYNTS_ERR_CUDA, "the driver has no cuTensorMapEncodeTiled");
+    c->encode = reinterpret_cast<tensor_map_encode_fn>(fn);
+  }
+  if (c->cfg.dtype == DYNTS_BF16 && !c->have_extend_maps) {
+    const cuuint64_t dims[3] = {128, (cuuint64_t)c->cap, (cuuint64_t)c->slabs()};
+    const cuuint64_t strides[2] = {256, (cuuint64_t)c->cap * 256};
+    const cuuint32_t box[3] = {64, (cuuint32_t)dynts::kPfKeys, 1};
+    const cuuint32_t estr[3] = {1, 1, 1};
+    void* base[2] = {c->K(), c->V()};
+    CUtensorMap* map[2] = {&c->map_XK, &c->map_XV};
+    for (int i = 0; i < 2; ++i) {
+      const CUresult r = c->encode(map[i], CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, base[i], dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                                   CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+      if (r != CUDA_SUCCESS) return fail(DYNTS_ERR_CUDA, "cuTensorMapEncodeTiled failed (%d)", (int)r);
+    }
+    c->have_extend_maps = true;
+  }
+  return DYNTS_OK;
+}
+
+template <bool KV8, bool MODS>
+dynts_status_t launch_extend_tc_as(dynts_cache* c, dynts::ExtendTcParams& p, const CUtensorMap& mq, const CUtensorMap& mqs, bool want_mass) {
+  bool* attr = &c->attr_extend_tc[KV8 ? 1 : 0][MODS ? 1 : 0];
+  if (!*attr) {
+    CUDA_TRY(cudaFuncSetAttribute(dynts::extend_tc_kernel<KV8, MODS>, cudaFuncAttributeMaxDynamicSharedMemorySize, dynts::kXtSmemBytes));
+    CUDA_TRY(cudaFuncSetAttribute(dynts::extend_mass_tc_kernel<KV8, MODS>, cudaFuncAttributeMaxDynamicSharedMemorySize, dynts::kXmSmemBytes));
+    *attr = true;
+  }
+  const unsigned grid = (unsigned)std::min<long long>(p.n_work, 2ll * c->sm_count);
+  CUDA_TRY(launch_dependent(dynts::extend_tc_kernel<KV8, MODS>, dim3(grid, 1, 1), dynts::kXtThreads, dynts::kXtSmemBytes, c->stream, p, mq, c->map_XK, c->map_XV));
+  c->launches += 1;
+  if (want_mass) {
+    dynts::extend_mass_tc_kernel<KV8, MODS><<<2 * c->sm_count, dynts::kXtThreads, dynts::kXmSmemBytes, c->stream>>>(p, mqs, c->map_XK);
+    CUDA_TRY(cudaGetLastError());
+    c->launches += 1;
+  }
+  return DYNTS_OK;
+}
+
+// The tensor-core kernels: items, and how far a tile's key rows are cut.
+dynts_status_t launch_extend_tc(dynts_cache* c, const dynts::ExtendParams& x, const ExtendScratch& m, char* scratch, bool want_mass) {
+  dynts::ExtendTcParams p;
+  p.x = x;
+  const int G = c->G, n_seq = x.seqs.n, tpt = dynts::kXtRows / G;
+  p.tokens_per_tile = tpt;
+  p.lh = x.n_layers * x.Hkv;
+  p.part_rows = m.part_rows;
+  long long tiles = 0, key_tiles = 0;  // tiles of query rows; key tiles of all of them
+  int per_seq[dynts::kExtSeqs], n_tiles[dynts::kExtSeqs];
+  for (int s = 0; s < n_seq; ++s) {
+    const int t = x.seqs.tok0[s + 1] - x.seqs.tok0[s];
+    n_tiles[s] = (t + tpt - 1) / tpt;
+    // (the host's copy of the lengths only guides the cut: the kernel goes by the device's)
+    long long rows = c->len_h[x.seqs.b0 + s] + t;
+    if (x.window > 0) rows = std::min<long long>(rows, (long long)x.window + tpt + dynts::kPfKeys);
+    per_seq[s] = (int)std::max<long long>(1, (rows + dynts::kPfKeys - 1) / dynts::kPfKeys);
+    tiles += (long long)n_tiles[s] * p.lh;
+    key_tiles += (long long)n_tiles[s] * p.lh * per_seq[s];
+  }
+  // Fewer tiles than CTAs: the key rows of each are cut into parts of about an equal share, at least four key tiles
+  // (a part's pipeline takes about two key tiles' time to fill and drain).
+  const bool cut = tiles < m.slots;
+  const long long share = std::max<long long>(4, (key_tiles + m.slots - 1) / m.slots);
+  long long items = 0;
+  for (int s = 0; s < n_seq; ++s) {
+    p.parts[s] = cut ? (int)((per_seq[s] + share - 1) / share) : 1;
+    p.x.seqs.item0[s] = (int)items;
+    items += (long long)n_tiles[s] * p.parts[s];
+  }
+  p.x.seqs.item0[n_seq] = (int)items;
+  if (items * p.lh >= (1ll << 30)) return fail(DYNTS_ERR_INVALID_ARG, "%lld work items are beyond the launch limits", items * p.lh);
+  p.n_work = (int)(items * p.lh);
+  p.part = cut ? reinterpret_cast<float*>(scratch + m.part) : nullptr;
+  p.stop = reinterpret_cast<int*>(c->ticket()) + 41;  // a spare word of the ticket block (zero since the cache was created)
+  p.scale_log2 = (float)(1.4426950408889634 * (double)x.scale);
+  p.cap_log2 = (float)(1.4426950408889634 * (double)x.cap_logit);
+  p.cap_arg = x.cap_logit > 0.f ? (float)(2.0 * 1.4426950408889634 * (double)x.scale / (double)x.cap_logit) : 0.f;
+  // The queries, [layers x tokens][heads][128] in boxes of (tokens, the group's heads, 64 elements): a box is a tile's rows.
+  const bool kv8 = c->cfg.dtype == DYNTS_BF16_KV8;
+  const cuuint64_t dims[3] = {128, (cuuint64_t)x.Hq, (cuuint64_t)x.n_layers * x.total};
+  const cuuint64_t strides[2] = {256, (cuuint64_t)(kv8 ? (long long)x.Hq * 128 : x.q_stride) * 2};
+  const cuuint32_t estr[3] = {1, 1, 1};
+  const void* q = kv8 ? static_cast<const void*>(x.q16) : x.q;
+  CUtensorMap map[2];
+  for (int i = 0; i < (want_mass ? 2 : 1); ++i) {
+    const cuuint32_t box[3] = {64, (cuuint32_t)G, (cuuint32_t)((i == 0 ? dynts::kXtRows : dynts::kXmRows) / G)};
+    const CUresult r = c->encode(&map[i], kv8 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(q), dims, strides,
+                                 box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                                 CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS) return fail(DYNTS_ERR_CUDA, "cuTensorMapEncodeTiled failed (%d)", (int)r);
+  }
+  const bool mods = x.cap_logit > 0.f || x.slopes || x.window > 0;
+  if (kv8) return mods ? launch_extend_tc_as<true, true>(c, p, map[0], map[1], want_mass) : launch_extend_tc_as<true, false>(c, p, map[0], map[1], want_mass);
+  return mods ? launch_extend_tc_as<false, true>(c, p, map[0], map[1], want_mass) : launch_extend_tc_as<false, false>(c, p, map[0], map[1], want_mass);
+}
+
 dynts_status_t launch_extend(dynts_cache* c, int layer0, int n_layers, const ExtendCall& a, long long total, bool publish) {
   const dynts_config_t& f = c->cfg;
   {
@@ -1460,7 +1614,16 @@ dynts_status_t launch_extend(dynts_cache* c, int layer0, int n_layers, const Ext
   p.accumulate = (c->score_source == DYNTS_SCORE_ATTENTION && !a.o.stage) ? 1 : 0;
   p.mass = a.o.mass;
   const bool want_mass = p.accumulate || p.mass;
-  p.lse = want_mass ? reinterpret_cast<float*>(a.scratch) : nullptr;
+  const bool kv8 = f.dtype == DYNTS_BF16_KV8;
+  const bool tc = extend_tc_shape(f) && c->variant != 1;
+  const ExtendScratch m = extend_scratch(c, a.n_new, n_layers);
+  if (tc) {
+    dynts_status_t ms = extend_maps(c);
+    if (ms != DYNTS_OK) return ms;
+  }
+  p.lse = want_mass ? reinterpret_cast<float*>(a.scratch + m.lse) : nullptr;
+  p.q16 = tc && kv8 ? reinterpret_cast<__half*>(a.scratch + m.q16) : nullptr;
+  p.counters = reinterpret_cast<unsigned int*>(a.scratch + m.counters);
   p.slopes = a.o.slopes;
   p.layer0 = layer0;
   p.n_layers = n_layers;
@@ -1473,12 +1636,11 @@ dynts_status_t launch_extend(dynts_cache* c, int layer0, int n_layers, const Ext
   p.cap = c->cap;
   p.window = a.o.window;
   p.publish = publish ? 1 : 0;
-  const bool kv8 = f.dtype == DYNTS_BF16_KV8;
   p.scale = (float)((kv8 ? (double)c->k_scale : 1.0) / std::sqrt((double)f.head_dim));
   p.cap_logit = a.o.softcap;
   p.k_scale = c->k_scale;
   p.v_scale = c->v_scale;
-  p.zero_tail = 0;
+  p.zero_tail = tc && !kv8 ? 1 : 0;
 
   long long tok = 0;
   for (int b0 = 0; b0 < f.batch; b0 += dynts::kExtSeqs) {
@@ -1494,6 +1656,10 @@ dynts_status_t launch_extend(dynts_cache* c, int layer0, int n_layers, const Ext
     const int n_tok = p.seqs.tok0[n_seq] - p.seqs.tok0[0];
     if (n_tok == 0) continue;
     p.published = 0;
+    {
+      const long long tiles = tc ? extend_tiles(f, a.n_new + b0, n_seq, n_layers) : m.slots;
+      p.n_counters = tiles < m.slots ? (int)(tiles + m.slots) : 0;
+    }
     // one 16-byte piece of K and of V per thread, up to a few CTAs per SM
     const long long pieces = (long long)n_layers * n_tok * f.kv_heads * (f.head_dim * c->elt / 16);
     const unsigned grid = (unsigned)std::max<long long>(1, std::min<long long>((pieces + 255) / 256, 8ll * c->sm_count));
@@ -1503,7 +1669,8 @@ dynts_status_t launch_extend(dynts_cache* c, int layer0, int n_layers, const Ext
     CUDA_TRY(cudaGetLastError());
     c->launches += 1;
     p.published = p.publish;
-    dynts_status_t st = kv8 ? launch_extend_generic<__nv_bfloat16, true>(c, p, want_mass)
+    dynts_status_t st = tc ? launch_extend_tc(c, p, m, a.scratch, want_mass)
+                        : kv8 ? launch_extend_generic<__nv_bfloat16, true>(c, p, want_mass)
                         : f.dtype == DYNTS_FP32 ? launch_extend_generic<float, false>(c, p, want_mass)
                                                 : launch_extend_generic<__nv_bfloat16, false>(c, p, want_mass);
     if (st != DYNTS_OK) return st;
@@ -1528,12 +1695,9 @@ extern "C" {
 
 size_t dynts_extend_scratch_bytes(const dynts_cache_t* c, const int* n_new, int n_layers) {
   if (!c || !n_new || n_layers < 1 || n_layers > c->cfg.layers) return 0;
-  long long total = 0;
-  for (int b = 0; b < c->cfg.batch; ++b) {
+  for (int b = 0; b < c->cfg.batch; ++b)
     if (n_new[b] < 0) return 0;
-    total += n_new[b];
-  }
-  return std::max<size_t>(256, extend_scratch(c->cfg, total, n_layers));
+  return extend_scratch(c, n_new, n_layers).total;
 }
 
 dynts_status_t dynts_extend_attn(dynts_cache_t* c, const void* q, const void* k_new, const void* v_new, void* out, const int* n_new,

@@ -54,7 +54,7 @@ struct ExtendParams {
   int* err;
   unsigned int* ticket;
   const float* s_new; // [total] scores of the new rows, or NULL: 0
-  float* lse;         // [n_layers][total][Hq] log2 of the sum of the weights' exponentials, or NULL
+  float* lse;         // [n_layers][Hkv][total][G] log2 of the sum of the weights' exponentials, or NULL
   float* mass;        // full [L, Nb, Hkv, cap], or NULL
   const float* slopes;  // [Hq] or NULL
   int layer0, n_layers, total;
@@ -63,6 +63,9 @@ struct ExtendParams {
   int publish;        // the storing kernel advances the lengths when it is done
   int published;      // the lengths on the device include the chunk already
   int accumulate;     // the mass is added to the scores
+  __half* q16;        // 8-bit rows: [n_layers][total][Hq][d] f16 copies of the queries made by the storing kernel, or NULL
+  unsigned int* counters;  // words the storing kernel clears for the kernel behind it
+  int n_counters;
   int zero_tail;      // the storing kernel clears the V rows from the chunk's end to the end of the key tile
   float scale;        // 1 / sqrt(d), times k_scale for 8-bit rows
   float cap_logit;    // c, or 0
@@ -78,6 +81,11 @@ __device__ __forceinline__ int ext_find(const int* first, int n, int x) {  // th
     else hi = mid;
   }
   return lo;
+}
+
+// Where the log-sum-exps of a packed token's query rows begin: a KV head's rows (token, head of the group) adjoin.
+__device__ __forceinline__ size_t ext_lse_index(const ExtendParams& p, int layer, int h, int tok) {
+  return (((size_t)layer * p.Hkv + h) * p.total + tok) * p.G;
 }
 
 // Rows held and tokens seen before the chunk.
@@ -146,6 +154,27 @@ __global__ void __launch_bounds__(256) extend_store_kernel(const __grid_constant
       p.pos[row] = p.tot[e.b] + i;
       p.score[row] = p.s_new ? p.s_new[tok] : 0.f;
       p.comp[row] = 0.f;
+    }
+  }
+  for (long long w = first; w < p.n_counters; w += stride) p.counters[w] = 0u;
+  if constexpr (KV8) {
+    if (p.q16) {  // (8-bit codes are exact in f16 but not their products' other operand in bf16: both operands of an MMA have one type)
+      const int qp = p.d / 8;
+      const long long qwork = (long long)p.n_layers * n_tok * p.Hq * qp;
+      for (long long w = first; w < qwork; w += stride) {
+        const int piece = (int)(w % qp);
+        long long r = w / qp;
+        const int hd = (int)(r % p.Hq);
+        r /= p.Hq;
+        const size_t tok = (size_t)(r / n_tok) * p.total + tok_begin + (size_t)(r % n_tok);
+        const uint4 x = *reinterpret_cast<const uint4*>(static_cast<const T*>(p.q) + tok * p.q_stride + (size_t)hd * p.d + piece * 8);
+        const __nv_bfloat162* b2 = reinterpret_cast<const __nv_bfloat162*>(&x);
+        uint4 y;
+        __half2* h2 = reinterpret_cast<__half2*>(&y);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) h2[u] = __float22half2_rn(__bfloat1622float2(b2[u]));
+        *reinterpret_cast<uint4*>(p.q16 + (tok * p.Hq + hd) * p.d + piece * 8) = y;
+      }
     }
   }
   if (p.zero_tail) {
@@ -340,7 +369,7 @@ __global__ void __launch_bounds__(kExtGenericThreads) extend_generic_kernel(cons
       const int col = c * 32 + lane;
       if (col < d) from_float(o + col, acc[u][c] / l[u]);
     }
-    if (p.lse && lane == 0) p.lse[(tok_base + i) * p.Hq + head] = m[u] + log2f(l[u]);
+    if (p.lse && lane == 0) p.lse[ext_lse_index(p, layer, h, p.seqs.tok0[s]) + r] = m[u] + log2f(l[u]);
   }
 }
 
@@ -402,7 +431,7 @@ __global__ void __launch_bounds__(kExtGenericThreads) extend_generic_mass_kernel
     }
     const int apart = abs(e.tot + i - pj);
     if (j < e.n + max(i + 1, prefix) && (p.window == 0 || apart < p.window))
-      sum += exp2f(ext_logit_exact(p, dot, p.slopes ? p.slopes[head] : 0.f, apart) - p.lse[(tok_base + i) * p.Hq + head]);
+      sum += exp2f(ext_logit_exact(p, dot, p.slopes ? p.slopes[head] : 0.f, apart) - p.lse[ext_lse_index(p, layer, h, p.seqs.tok0[s]) + r]);
   }
   sS[warp * kExtGenericKeys + lane] = sum;
   __syncthreads();

@@ -209,7 +209,14 @@ def test_masked_tokens_of_the_chunk_do_not_matter():
     c.extend_attn(q, k2, v2, out, [80], stage=True)
     c.synchronize()
     c.poll_error()
-    assert torch.equal(out[0, :60, :4], good[0, :60, :4]) and torch.equal(out[0, :41, 4:], good[0, :41, 4:])
+    # The columns without such a value keep every bit.  In the others a kernel may compute an element a second way: one
+    # way rounds the weights (half a step of bf16, 2^-8) and the output (another), the other at least the output, so the
+    # two are at most 3 * 2^-8 * max |v| apart (an output is a mean of v's with weights that sum to one).
+    for heads, col, upto in ((slice(0, 4), 9, 60), (slice(4, 8), 5, 41)):
+        x, y = out[0, :upto, heads], good[0, :upto, heads]
+        rest = torch.arange(128, device="cuda") != col
+        assert torch.equal(x[..., rest], y[..., rest])
+        assert ((x - y).float().abs() <= 3 * 2.0 ** -8 * v.float().abs().max()).all()
     assert torch.isnan(out[0, 41:, 4:, 5].float()).all() and not torch.isfinite(out[0, 60:70, :4, 9].float()).any()
     assert torch.isnan(out[0, 70:, :4].float()).all()
     c.close()
