@@ -1336,24 +1336,16 @@ namespace {
 // What a chunk's launches need beside the cache, as offsets into the caller's scratch.
 struct ExtendScratch {
   size_t lse, q16, part, counters, total;
-  int part_rows;    // query rows of a part of a cut tile
-  long long slots;  // items that the tensor-core kernel aims at when the tiles alone are fewer
+  int part_rows;  // query rows of a part of an item that several CTAs share
+  int ctas;       // of the tensor-core kernel, at most
 };
 
 bool extend_tc_shape(const dynts_config_t& f) { return f.dtype != DYNTS_FP32 && f.head_dim == 128; }
 
-// Tiles of 128 query rows of a launch's sequences, over layers and KV heads.
-long long extend_tiles(const dynts_config_t& f, const int* n_new, int n_seq, int n_layers) {
-  const int tpt = dynts::kXtRows / (f.q_heads / f.kv_heads);
-  long long tiles = 0;
-  for (int s = 0; s < n_seq; ++s) tiles += (n_new[s] + tpt - 1) / tpt;
-  return tiles * n_layers * f.kv_heads;
-}
-
 ExtendScratch extend_scratch(const dynts_cache* c, const int* n_new, int n_layers) {
   const dynts_config_t& f = c->cfg;
   ExtendScratch m;
-  long long total = 0, items = 0;
+  long long total = 0;
   int longest = 0;
   for (int b = 0; b < f.batch; ++b) {
     total += n_new[b];
@@ -1361,9 +1353,7 @@ ExtendScratch extend_scratch(const dynts_cache* c, const int* n_new, int n_layer
   }
   const int G = f.q_heads / f.kv_heads;
   m.part_rows = (int)(((long long)std::min(longest, dynts::kXtRows / G) * G + 3) / 4 * 4);
-  // Two CTAs per SM.  Parts of few query rows cost little to join (a few KB each): four per CTA even out lengths that
-  // differ; parts of whole tiles (66 KB each) are made only to occupy every CTA once.
-  m.slots = 2ll * (c->sm_count > 0 ? c->sm_count : 148) * (m.part_rows <= 32 ? 4 : 1);
+  m.ctas = std::min(dynts::kXtMaxCtas, 2 * (c->sm_count > 0 ? c->sm_count : 148));
   size_t off = 0;
   auto take = [&](size_t bytes) {
     const size_t o = off;
@@ -1374,12 +1364,8 @@ ExtendScratch extend_scratch(const dynts_cache* c, const int* n_new, int n_layer
   m.q16 = m.part = m.counters = off;
   if (extend_tc_shape(f)) {
     if (f.dtype == DYNTS_BF16_KV8) m.q16 = take((size_t)n_layers * total * f.q_heads * f.head_dim * 2);
-    for (int b0 = 0; b0 < f.batch; b0 += dynts::kExtSeqs) {
-      const long long tiles = extend_tiles(f, n_new + b0, std::min(dynts::kExtSeqs, f.batch - b0), n_layers);
-      if (tiles < m.slots) items = std::max(items, tiles + m.slots);  // cut tiles: at most one part more than a whole share each
-    }
-    m.part = take((size_t)items * m.part_rows * dynts::kXtPartFloats * sizeof(float));
-    m.counters = take((size_t)items * sizeof(int));
+    m.part = take((size_t)2 * m.ctas * m.part_rows * dynts::kXtPartFloats * sizeof(float));
+    m.counters = take((size_t)m.ctas * sizeof(int));
   }
   m.total = std::max<size_t>(off, 256);
   return m;
@@ -1509,25 +1495,27 @@ dynts_status_t extend_maps(dynts_cache* c) {
 }
 
 template <bool KV8, bool MODS>
-dynts_status_t launch_extend_tc_as(dynts_cache* c, dynts::ExtendTcParams& p, const CUtensorMap& mq, const CUtensorMap& mqs, bool want_mass) {
+dynts_status_t launch_extend_tc_as(dynts_cache* c, dynts::ExtendTcParams& p, unsigned grid, const CUtensorMap& mq, const CUtensorMap& mqs,
+                                   bool want_mass) {
   bool* attr = &c->attr_extend_tc[KV8 ? 1 : 0][MODS ? 1 : 0];
   if (!*attr) {
     CUDA_TRY(cudaFuncSetAttribute(dynts::extend_tc_kernel<KV8, MODS>, cudaFuncAttributeMaxDynamicSharedMemorySize, dynts::kXtSmemBytes));
     CUDA_TRY(cudaFuncSetAttribute(dynts::extend_mass_tc_kernel<KV8, MODS>, cudaFuncAttributeMaxDynamicSharedMemorySize, dynts::kXmSmemBytes));
     *attr = true;
   }
-  const unsigned grid = (unsigned)std::min<long long>(p.n_work, 2ll * c->sm_count);
   CUDA_TRY(launch_dependent(dynts::extend_tc_kernel<KV8, MODS>, dim3(grid, 1, 1), dynts::kXtThreads, dynts::kXtSmemBytes, c->stream, p, mq, c->map_XK, c->map_XV));
   c->launches += 1;
   if (want_mass) {
-    dynts::extend_mass_tc_kernel<KV8, MODS><<<2 * c->sm_count, dynts::kXtThreads, dynts::kXmSmemBytes, c->stream>>>(p, mqs, c->map_XK);
+    dynts::extend_mass_tc_kernel<KV8, MODS><<<2 * c->sm_count, dynts::kXmThreads, dynts::kXmSmemBytes, c->stream>>>(p, mqs, c->map_XK);
     CUDA_TRY(cudaGetLastError());
     c->launches += 1;
   }
   return DYNTS_OK;
 }
 
-// The tensor-core kernels: items, and how far a tile's key rows are cut.
+constexpr int kExtendMinTiles = 3;  // key tiles per CTA below which the grid shrinks
+
+// The tensor-core kernels: the list of key tiles and its shares.
 dynts_status_t launch_extend_tc(dynts_cache* c, const dynts::ExtendParams& x, const ExtendScratch& m, char* scratch, bool want_mass) {
   dynts::ExtendTcParams p;
   p.x = x;
@@ -1535,32 +1523,36 @@ dynts_status_t launch_extend_tc(dynts_cache* c, const dynts::ExtendParams& x, co
   p.tokens_per_tile = tpt;
   p.lh = x.n_layers * x.Hkv;
   p.part_rows = m.part_rows;
-  long long tiles = 0, key_tiles = 0;  // tiles of query rows; key tiles of all of them
-  int per_seq[dynts::kExtSeqs], n_tiles[dynts::kExtSeqs];
+  long long key_tiles = 0, shares = 0;
   for (int s = 0; s < n_seq; ++s) {
     const int t = x.seqs.tok0[s + 1] - x.seqs.tok0[s];
-    n_tiles[s] = (t + tpt - 1) / tpt;
-    // (the host's copy of the lengths only guides the cut: the kernel goes by the device's)
-    long long rows = c->len_h[x.seqs.b0 + s] + t;
+    p.tiles[s] = (t + tpt - 1) / tpt;
+    // The key tiles of an item, on average over the chunk.  (The host's copy of the lengths only guides the cut: the
+    // kernel goes by the device's.)
+    long long rows = c->len_h[x.seqs.b0 + s] + std::max((t + 1) / 2, x.seqs.prefix[s]);
     if (x.window > 0) rows = std::min<long long>(rows, (long long)x.window + tpt + dynts::kPfKeys);
-    per_seq[s] = (int)std::max<long long>(1, (rows + dynts::kPfKeys - 1) / dynts::kPfKeys);
-    tiles += (long long)n_tiles[s] * p.lh;
-    key_tiles += (long long)n_tiles[s] * p.lh * per_seq[s];
+    const long long n = std::max<long long>(1, (rows + dynts::kPfKeys - 1) / dynts::kPfKeys), items = (long long)p.tiles[s] * p.lh;
+    if (items >= (1ll << 30)) return fail(DYNTS_ERR_INVALID_ARG, "%lld work items are beyond the launch limits", items);
+    p.per[s] = (unsigned)(n + 1);  // an item's beginning and end take about a key tile's time
+    key_tiles += items * n;
+    shares += items * (n + 1);
   }
-  // Fewer tiles than CTAs: the key rows of each are cut into parts of about an equal share, at least four key tiles
-  // (a part's pipeline takes about two key tiles' time to fill and drain).
-  const bool cut = tiles < m.slots;
-  const long long share = std::max<long long>(4, (key_tiles + m.slots - 1) / m.slots);
-  long long items = 0;
+  unsigned coarse = 1;  // shares are counted in 32 bits: very large calls count several key tiles as one
+  while (shares / coarse >= (1ll << 30)) coarse *= 2;
+  long long sum = 0;
   for (int s = 0; s < n_seq; ++s) {
-    p.parts[s] = cut ? (int)((per_seq[s] + share - 1) / share) : 1;
-    p.x.seqs.item0[s] = (int)items;
-    items += (long long)n_tiles[s] * p.parts[s];
+    p.per[s] = std::max(1u, p.per[s] / coarse);
+    p.cum[s] = (unsigned)sum;
+    sum += (long long)p.tiles[s] * p.lh * p.per[s];
+    if (sum >= (1ll << 31)) return fail(DYNTS_ERR_INVALID_ARG, "the call is beyond the launch limits");
   }
-  p.x.seqs.item0[n_seq] = (int)items;
-  if (items * p.lh >= (1ll << 30)) return fail(DYNTS_ERR_INVALID_ARG, "%lld work items are beyond the launch limits", items * p.lh);
-  p.n_work = (int)(items * p.lh);
-  p.part = cut ? reinterpret_cast<float*>(scratch + m.part) : nullptr;
+  p.cum[n_seq] = (unsigned)sum;
+  // Two CTAs per SM, with at least a few key tiles each.
+  const long long grid_ll = std::max<long long>(1, std::min<long long>(std::min<long long>(m.ctas, sum), key_tiles / kExtendMinTiles));
+  const unsigned grid = (unsigned)grid_ll;
+  p.share_q = (unsigned)(sum / grid);
+  p.share_rem = (unsigned)(sum % grid);
+  p.part = reinterpret_cast<float*>(scratch + m.part);
   p.stop = reinterpret_cast<int*>(c->ticket()) + 41;  // a spare word of the ticket block (zero since the cache was created)
   p.scale_log2 = (float)(1.4426950408889634 * (double)x.scale);
   p.cap_log2 = (float)(1.4426950408889634 * (double)x.cap_logit);
@@ -1580,8 +1572,8 @@ dynts_status_t launch_extend_tc(dynts_cache* c, const dynts::ExtendParams& x, co
     if (r != CUDA_SUCCESS) return fail(DYNTS_ERR_CUDA, "cuTensorMapEncodeTiled failed (%d)", (int)r);
   }
   const bool mods = x.cap_logit > 0.f || x.slopes || x.window > 0;
-  if (kv8) return mods ? launch_extend_tc_as<true, true>(c, p, map[0], map[1], want_mass) : launch_extend_tc_as<true, false>(c, p, map[0], map[1], want_mass);
-  return mods ? launch_extend_tc_as<false, true>(c, p, map[0], map[1], want_mass) : launch_extend_tc_as<false, false>(c, p, map[0], map[1], want_mass);
+  if (kv8) return mods ? launch_extend_tc_as<true, true>(c, p, grid, map[0], map[1], want_mass) : launch_extend_tc_as<true, false>(c, p, grid, map[0], map[1], want_mass);
+  return mods ? launch_extend_tc_as<false, true>(c, p, grid, map[0], map[1], want_mass) : launch_extend_tc_as<false, false>(c, p, grid, map[0], map[1], want_mass);
 }
 
 dynts_status_t launch_extend(dynts_cache* c, int layer0, int n_layers, const ExtendCall& a, long long total, bool publish) {
@@ -1656,13 +1648,14 @@ dynts_status_t launch_extend(dynts_cache* c, int layer0, int n_layers, const Ext
     const int n_tok = p.seqs.tok0[n_seq] - p.seqs.tok0[0];
     if (n_tok == 0) continue;
     p.published = 0;
-    {
-      const long long tiles = tc ? extend_tiles(f, a.n_new + b0, n_seq, n_layers) : m.slots;
-      p.n_counters = tiles < m.slots ? (int)(tiles + m.slots) : 0;
-    }
-    // one 16-byte piece of K and of V per thread, up to a few CTAs per SM
-    const long long pieces = (long long)n_layers * n_tok * f.kv_heads * (f.head_dim * c->elt / 16);
-    const unsigned grid = (unsigned)std::max<long long>(1, std::min<long long>((pieces + 255) / 256, 8ll * c->sm_count));
+    p.n_counters = tc ? m.ctas : 0;
+    // one 16-byte piece of K and of V (and of the rows to clear, and of the queries to copy) per thread, up to a few CTAs per SM
+    const long long pieces = f.head_dim * c->elt / 16, ny = (long long)n_layers * f.kv_heads;
+    long long work = std::max(n_tok * pieces, (long long)m.ctas);
+    if (p.zero_tail) work = std::max(work, (long long)n_seq * dynts::kExtTileKeys * pieces);
+    if (p.q16) work = std::max(work, (long long)n_tok * c->G * (f.head_dim / 8));
+    if (work >= (1ll << 31)) return fail(DYNTS_ERR_INVALID_ARG, "%d new tokens are beyond the launch limits", n_tok);
+    const dim3 grid((unsigned)std::max<long long>(1, std::min<long long>((work + 255) / 256, std::max<long long>(1, 16ll * c->sm_count / ny))), (unsigned)ny, 1);
     if (kv8) dynts::extend_store_kernel<__nv_bfloat16, true><<<grid, 256, 0, c->stream>>>(p);
     else if (f.dtype == DYNTS_FP32) dynts::extend_store_kernel<float, false><<<grid, 256, 0, c->stream>>>(p);
     else dynts::extend_store_kernel<__nv_bfloat16, false><<<grid, 256, 0, c->stream>>>(p);

@@ -105,36 +105,31 @@ __device__ __forceinline__ ExtSeq ext_seq(const ExtendParams& p, int s) {
 
 // Stores the chunk's rows: K and V (encoded for 8-bit slabs), position, score; with `publish` the
 // last CTA to finish advances the lengths.  Bandwidth-bound and short: a row is read and written once.
+// Grid: x over the 16-byte pieces of the tokens' rows, y over (layer, KV head).
 template <typename T, bool KV8>
 __global__ void __launch_bounds__(256) extend_store_kernel(const __grid_constant__ ExtendParams p) {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // the next kernel's set-up may begin; it waits for this grid before it reads
   constexpr int E = 16 / (int)sizeof(T);  // elements per 16-byte piece of the source
-  const int pieces = p.d / E;
-  const int tok_begin = p.seqs.tok0[0], n_tok = p.seqs.tok0[p.seqs.n] - tok_begin;
-  const long long work = (long long)p.n_layers * n_tok * p.Hkv * pieces;
-  const long long stride = (long long)gridDim.x * blockDim.x;
-  const long long first = (long long)blockIdx.x * blockDim.x + threadIdx.x;
-  for (long long w = first; w < work; w += stride) {
-    const int piece = (int)(w % pieces);
-    long long r = w / pieces;
-    const int h = (int)(r % p.Hkv);
-    r /= p.Hkv;
-    const int tok = tok_begin + (int)(r % n_tok), layer = (int)(r / n_tok);
+  const unsigned pieces = (unsigned)p.d / E;
+  const int tok_begin = p.seqs.tok0[0];
+  const unsigned n_tok = (unsigned)(p.seqs.tok0[p.seqs.n] - tok_begin);
+  const unsigned stride = gridDim.x * blockDim.x, first = blockIdx.x * blockDim.x + threadIdx.x;
+  const int layer = blockIdx.y / p.Hkv, h = blockIdx.y - layer * p.Hkv;
+  const size_t slab0 = (size_t)(p.layer0 + layer) * p.Nb;  // (times Hkv, plus the sequence's and head's part)
+  for (unsigned w = first; w < n_tok * pieces; w += stride) {
+    const unsigned rel = w / pieces, piece = w - rel * pieces;
+    const int tok = tok_begin + (int)rel;
     const int s = ext_find(p.seqs.tok0, p.seqs.n, tok);
-    ExtSeq e;
-    e.b = p.seqs.b0 + s;
-    e.t = p.seqs.tok0[s + 1] - p.seqs.tok0[s];
-    e.n = p.len[e.b];
-    const int i = tok - p.seqs.tok0[s];
-    if (e.n < 0 || e.n + e.t > p.cap) {
-      if (piece == 0 && h == 0 && i == 0) atomicOr(p.err, kErrLenOverflow);
-      continue;
-    }
-    const size_t slab = ((size_t)(p.layer0 + layer) * p.Nb + e.b) * p.Hkv + h;
-    const size_t row = slab * p.cap + e.n + i;
+    const int b = p.seqs.b0 + s, t = p.seqs.tok0[s + 1] - p.seqs.tok0[s], i = tok - p.seqs.tok0[s];
     const size_t src_tok = (size_t)layer * p.total + tok;
     const uint4 kk = *reinterpret_cast<const uint4*>(static_cast<const T*>(p.k) + src_tok * p.k_stride + (size_t)h * p.d + piece * E);
     const uint4 vv = *reinterpret_cast<const uint4*>(static_cast<const T*>(p.v) + src_tok * p.v_stride + (size_t)h * p.d + piece * E);
+    const int n = p.len[b];
+    if (n < 0 || n + t > p.cap) {
+      if (piece == 0 && h == 0 && i == 0) atomicOr(p.err, kErrLenOverflow);
+      continue;
+    }
+    const size_t row = ((slab0 + b) * p.Hkv + h) * p.cap + n + i;
     if constexpr (KV8) {
       const __nv_bfloat16* kx = reinterpret_cast<const __nv_bfloat16*>(&kk);
       const __nv_bfloat16* vx = reinterpret_cast<const __nv_bfloat16*>(&vv);
@@ -151,29 +146,26 @@ __global__ void __launch_bounds__(256) extend_store_kernel(const __grid_constant
       *reinterpret_cast<uint4*>(static_cast<T*>(p.V) + row * p.d + piece * E) = vv;
     }
     if (piece == 0) {
-      p.pos[row] = p.tot[e.b] + i;
+      p.pos[row] = p.tot[b] + i;
       p.score[row] = p.s_new ? p.s_new[tok] : 0.f;
       p.comp[row] = 0.f;
     }
   }
-  for (long long w = first; w < p.n_counters; w += stride) p.counters[w] = 0u;
+  if (blockIdx.y == 0)
+    for (unsigned w = first; w < (unsigned)p.n_counters; w += stride) p.counters[w] = 0u;
   if constexpr (KV8) {
-    if (p.q16) {  // (8-bit codes are exact in f16 but not their products' other operand in bf16: both operands of an MMA have one type)
-      const int qp = p.d / 8;
-      const long long qwork = (long long)p.n_layers * n_tok * p.Hq * qp;
-      for (long long w = first; w < qwork; w += stride) {
-        const int piece = (int)(w % qp);
-        long long r = w / qp;
-        const int hd = (int)(r % p.Hq);
-        r /= p.Hq;
-        const size_t tok = (size_t)(r / n_tok) * p.total + tok_begin + (size_t)(r % n_tok);
-        const uint4 x = *reinterpret_cast<const uint4*>(static_cast<const T*>(p.q) + tok * p.q_stride + (size_t)hd * p.d + piece * 8);
+    if (p.q16) {  // (8-bit codes are exact in f16, and both operands of an MMA have one type)
+      const unsigned qp = (unsigned)p.d / 8, per_tok = (unsigned)p.G * qp;
+      for (unsigned w = first; w < n_tok * per_tok; w += stride) {
+        const unsigned rel = w / per_tok, y = w - rel * per_tok;  // the group's heads adjoin
+        const size_t tok = (size_t)layer * p.total + tok_begin + rel, col = (size_t)h * p.G * p.d + y * 8;
+        const uint4 x = *reinterpret_cast<const uint4*>(static_cast<const T*>(p.q) + tok * p.q_stride + col);
         const __nv_bfloat162* b2 = reinterpret_cast<const __nv_bfloat162*>(&x);
-        uint4 y;
-        __half2* h2 = reinterpret_cast<__half2*>(&y);
+        uint4 o;
+        __half2* h2 = reinterpret_cast<__half2*>(&o);
 #pragma unroll
         for (int u = 0; u < 4; ++u) h2[u] = __float22half2_rn(__bfloat1622float2(b2[u]));
-        *reinterpret_cast<uint4*>(p.q16 + (tok * p.Hq + hd) * p.d + piece * 8) = y;
+        *reinterpret_cast<uint4*>(p.q16 + tok * p.Hq * p.d + col) = o;
       }
     }
   }
@@ -181,30 +173,20 @@ __global__ void __launch_bounds__(256) extend_store_kernel(const __grid_constant
     // The tensor-core kernel multiplies whole key tiles: weight zero times whatever lies behind the
     // chunk's end must be zero, so the V rows up to the end of that tile are cleared (rows behind a
     // sequence's end belong to nobody).
-    constexpr int KE = KV8 ? 16 : E;
-    const int kp = p.d / KE;
-    const long long tail = (long long)p.n_layers * p.seqs.n * p.Hkv * (kExtTileKeys - 1) * kp;
-    for (long long w = first; w < tail; w += stride) {
-      const int piece = (int)(w % kp);
-      long long r = w / kp;
-      const int x = (int)(r % (kExtTileKeys - 1));
-      r /= kExtTileKeys - 1;
-      const int h = (int)(r % p.Hkv);
-      r /= p.Hkv;
-      const int s = (int)(r % p.seqs.n), layer = (int)(r / p.seqs.n);
+    for (unsigned w = first; w < (unsigned)p.seqs.n * kExtTileKeys * pieces; w += stride) {
+      const unsigned rx = w / pieces, piece = w - rx * pieces;
+      const int s = (int)(rx / kExtTileKeys), x = (int)(rx % kExtTileKeys);
       const int b = p.seqs.b0 + s, t = p.seqs.tok0[s + 1] - p.seqs.tok0[s];
       const int end = p.len[b] + t, row = end + x;
       if (t == 0 || row >= p.cap || row >= (end + kExtTileKeys - 1) / kExtTileKeys * kExtTileKeys) continue;
-      const size_t slab = ((size_t)(p.layer0 + layer) * p.Nb + b) * p.Hkv + h;
-      char* dst = static_cast<char*>(p.V) + ((slab * p.cap + row) * p.d + (size_t)piece * KE) * (KV8 ? 1 : sizeof(T));
-      *reinterpret_cast<uint4*>(dst) = make_uint4(0u, 0u, 0u, 0u);
+      *reinterpret_cast<uint4*>(static_cast<T*>(p.V) + (((slab0 + b) * p.Hkv + h) * p.cap + row) * p.d + piece * E) = make_uint4(0u, 0u, 0u, 0u);
     }
   }
   if (p.publish) {
     // every CTA has read the lengths before it takes its ticket; the last one advances them
     __syncthreads();
     __shared__ int last;
-    if (threadIdx.x == 0) last = atomicAdd(p.ticket, 1u) == gridDim.x - 1;
+    if (threadIdx.x == 0) last = atomicAdd(p.ticket, 1u) == gridDim.x * gridDim.y - 1;
     __syncthreads();
     if (last) {
       for (int s = threadIdx.x; s < p.seqs.n; s += blockDim.x) {

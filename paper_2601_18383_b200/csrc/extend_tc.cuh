@@ -2,22 +2,33 @@
 // 8-bit rows: tcgen05.mma with the accumulators in tensor memory.
 //
 // extend_tc_kernel.  A tile of 128 query rows packs the group's G heads of floor(128 / G) neighbouring
-// tokens, so a row of K and V is read once for all of them whatever the chunk's length.  A work item =
-// (tile of query rows, KV head, layer, sequence, part of the key rows): where the tiles alone do not fill
-// the GPU (few tokens behind a long cache) the key rows of a tile are cut into parts that run side by
-// side; each leaves its unnormalised output, maximum and sum in the scratch, and the last part to finish
-// (a counter per tile) joins them in a fixed order.  Two CTAs per SM; per 64 keys
+// tokens, so a row of K and V is read once for all of them whatever the chunk's length.  An item = (tile of
+// query rows, KV head, layer, sequence).  All items' key tiles form one list, of which every CTA takes an equal
+// contiguous piece: few tokens behind a long cache, many ragged sequences and a whole prompt are cut alike.
+// An item that lies across CTAs is computed in parts side by side; each part leaves its normalised output and
+// log-sum-exp in the scratch, and the last part to finish (a counter per item) joins them in the order of the
+// rows.  Two CTAs per SM; per 64 keys
 //     S  = Q K^T      M 128 x N 64 x K 128     operands from shared memory
-//     P  = exp2(S * scale - max)               softmax warps, thread = query row = tensor-memory lane
+//     P  = exp2(S * scale - ref)               softmax warps, thread = query row = tensor-memory lane
 //     O += P V        M 128 x N 128 x K 64     P from tensor memory
-// The warps' roles, the double-buffered S, the lazy rescale and the barriers are those of the prompt
-// attention (prefill_attn.cuh); what differs is where the rows come from, the items, and the row
-// arithmetic, which knows caps, biases, windows and prefixes (MODS).  A warp whose 32 rows hold no
-// query (a short chunk) skips the arithmetic.
 //
-// Rows of 16 bits arrive by TMA from the slabs.  8-bit rows (KV8) are read by two warps as codes, one
-// tile ahead in registers, widened to f16 (exact) and stored into the same swizzled tiles; queries
-// (an f16 copy made by the storing kernel) and weights are then f16 too.
+// What bounds a tile is the chain wait - read S - exponentials - write P of a softmax warp (about 1700 cycles when one
+// group of four warps did every tile, against 512 for the two products and 512 for the exponentials' unit), so
+// two groups of four warps take the tiles in turn and four warps per scheduler hide one another's waits.  Both need
+// the same reference of a row's exponents without talking to each other, so it is fixed: the key tiles are
+// walked from the newest to the oldest, the first group takes the first tile (and, where a chunk's tokens see
+// different parts of it, the next ones until every token sees one whole tile), sets the reference kXtHeadroom
+// above the largest logit met there and hands it over.  Weights are bf16 (exponent range of fp32), so the logits
+// of the other tiles may lie up to 2^100 above the reference before a sum leaves the range; a row that does is
+// computed again by its warp alone, with a running maximum.  No maximum and no rescale in any other tile.
+// (From the newest tile on, because a distance bias only lowers the logits of older rows, and a window hides the oldest.)
+//
+// Warps: 0-3 and 4-7 the two groups, 8 loads Q and K, 9 loads V, 10 issues S, 11 issues O; they meet through mbarriers as
+// in the prompt attention (prefill_attn.cuh), the S buffer, stages and phases follow the flat tile index g.
+//
+// Rows of 16 bits arrive by TMA from the slabs.  8-bit rows (KV8) are read as codes by the two loading warps and
+// widened -- K to f16 (exact; queries are an f16 copy made by the storing kernel), V to bf16 (exact) -- into the same
+// swizzled tiles; the codes of coming tiles are asked into L2 meanwhile.
 //
 // A weight of zero times a value that is not finite is not a number, and the MMA multiplies whole
 // tiles: rows behind the chunk's end are zero (the storing kernel clears them, KV8 writes zeros), and an
@@ -33,19 +44,27 @@
 
 namespace dynts {
 
-constexpr int kXtThreads = 256;
+constexpr int kXtThreads = 384;
 constexpr int kXtRows = 128;
-constexpr int kXtPartFloats = 130;  // per query row of a part: 128 outputs, maximum, sum
+constexpr int kXtMaxCtas = 512;      // CTAs of a launch (two per SM)
+constexpr int kXtPartFloats = 129;   // per query row of a part: 128 outputs, log-sum-exp
+constexpr float kXtHeadroom = 40.f;  // the reference lies so far (base-2 units) above the first tiles' maximum
+constexpr float kXtSumMax = 1.2676506e30f;  // 2^100: a row whose sum of weights exceeds it is computed again
 constexpr int kXtSmemBytes = kPfQBytes + 4 * kPfKvBytes + kPfOutStageBytes + 128 + kExtSeqs * 4;
 
+// The list of key tiles is kept in shares: an item of sequence s counts per[s] shares whatever its exact number of
+// key tiles (which the kernel takes from the lengths on the device), a share's border inside an item is the same
+// fraction of its key tiles.  CTA c takes the shares [c * q + min(c, rem), ...).
 struct ExtendTcParams {
-  ExtendParams x;       // seqs.item0: first (tile, part) pair of each sequence; heads and layers multiply it
-  int parts[kExtSeqs];  // parts each tile's key rows are cut into
+  ExtendParams x;
+  unsigned cum[kExtSeqs + 1];  // shares before each sequence's first item
+  unsigned per[kExtSeqs];      // shares of an item
+  int tiles[kExtSeqs];         // tiles of query rows per (layer, KV head)
+  unsigned share_q, share_rem; // shares per CTA: share_q, one more for the first share_rem
   int tokens_per_tile;  // floor(128 / G)
   int lh;               // n_layers * Hkv
-  int n_work;           // items
   int part_rows;        // query rows a part's scratch has room for
-  float* part;          // [n_work][128 / 4 + 1][part_rows] float4 / float2 pieces, or NULL: no tile is cut
+  float* part;          // [2 per CTA]: [32][part_rows] float4, [part_rows] float
   int* stop;
   float scale_log2;     // log2(e) * scale
   float cap_log2;       // c * log2(e)
@@ -53,52 +72,82 @@ struct ExtendTcParams {
 };
 
 struct XtCursor {
-  int it, ord;            // position in this CTA's list; how many items came before
-  int j, nkt, kt0;        // tile within the item, tiles of the item, first key tile
-  int s, layer, h, lh, n; // sequence of the launch, layer, KV head; rows held
+  bool on;
+  int s, idx;             // sequence of the launch, item within it: (layer, KV head) slowest, tiles of query rows fastest
+  int ord;                // pieces of this CTA before this one
+  int j, nkt, kt0;        // tile within the piece (from its newest to its oldest), its tiles, its first key tile
+  int layer, h, n;        // rows held
   int i0, rows;           // first token of the chunk, query rows
-  int u0, split, n_split; // item index of the tile's first part; this part; parts that hold any keys
+  int b0, total;          // the item's first key tile, its key tiles
 };
 
-__device__ __forceinline__ void xt_seek(XtCursor& c, int it, int n_items, const ExtendTcParams& p, const int* s_n) {
+__device__ __forceinline__ unsigned xt_share0(const ExtendTcParams& p, unsigned cta) { return cta * p.share_q + min(cta, p.share_rem); }
+// Key tiles [lo, hi) of an item (total key tiles, shares [start, start + per)) that fall to the shares [v0, v1).
+__device__ __forceinline__ void xt_piece(unsigned v0, unsigned v1, unsigned start, unsigned per, int total, int& lo, int& hi) {
+  const unsigned a = v0 > start ? v0 - start : 0u, e = v1 - start < per ? v1 - start : per;
+  lo = a == 0u ? 0 : (int)((unsigned long long)(unsigned)total * a / per);
+  hi = e == per ? total : (int)((unsigned long long)(unsigned)total * e / per);
+}
+
+// The first piece of this CTA at or behind item c.idx of sequence c.s that holds any key tile.
+__device__ __forceinline__ void xt_settle(XtCursor& c, const ExtendTcParams& p, const int* s_n) {
+  const unsigned v0 = xt_share0(p, blockIdx.x), v1 = xt_share0(p, blockIdx.x + 1u);
   c.j = 0;
-  for (; it < n_items; ++it) {
-    const int slot = 2 * (int)blockIdx.x >= (int)gridDim.x ? n_items - 1 - it : it;
-    const int w = (int)blockIdx.x + slot * (int)gridDim.x;
-    const int u = w / p.lh;
-    c.lh = w - u * p.lh;
-    c.s = ext_find(p.x.seqs.item0, p.x.seqs.n, u);
-    const int S = p.parts[c.s], first = p.x.seqs.item0[c.s];
-    const int n_tiles = (p.x.seqs.item0[c.s + 1] - first) / S;
-    const int qi = (u - first) / S;
-    c.split = u - first - qi * S;
-    c.u0 = u - c.split;
+  c.on = false;
+  while (c.s < p.x.seqs.n) {
+    const int nq = p.tiles[c.s];
     c.n = s_n[c.s];
-    if (c.n < 0) continue;  // no room for the chunk: nothing was stored
+    if (c.n < 0 || c.idx >= nq * p.lh) {  // (no room for the chunk: nothing was stored)
+      ++c.s;
+      c.idx = 0;
+      continue;
+    }
+    const unsigned per = p.per[c.s], start = p.cum[c.s] + (unsigned)c.idx * per;
+    if (start >= v1) return;
+    const int lh = c.idx / nq, o = c.idx - lh * nq;
+    // tiles from both ends in turn: neighbours in the list hold about as many key tiles together as any other two
+    const int qt = (o & 1) ? nq - 1 - (o >> 1) : o >> 1;
     const int t = p.x.seqs.tok0[c.s + 1] - p.x.seqs.tok0[c.s];
-    c.i0 = (n_tiles - 1 - qi) * p.tokens_per_tile;  // heaviest first
+    c.i0 = qt * p.tokens_per_tile;
     const int i1 = min(t, c.i0 + p.tokens_per_tile);
     c.rows = (i1 - c.i0) * p.x.G;
     const int end = c.n + max(i1, p.x.seqs.prefix[c.s]);
     // (positions ascend with the rows, so a row more than `window` rows back is more than `window` positions back)
-    const int b = p.x.window > 0 ? max(0, c.n + c.i0 - p.x.window + 1) / kPfKeys : 0;
-    const int total = (end + kPfKeys - 1) / kPfKeys - b;
-    const int per = (total + S - 1) / S;
-    c.n_split = (total + per - 1) / per;
-    if (c.split >= c.n_split) continue;
-    c.kt0 = b + c.split * per;
-    c.nkt = min(per, total - c.split * per);
-    c.layer = c.lh / p.x.Hkv;
-    c.h = c.lh - c.layer * p.x.Hkv;
-    break;
+    c.b0 = p.x.window > 0 ? max(0, c.n + c.i0 - p.x.window + 1) / kPfKeys : 0;
+    c.total = (end + kPfKeys - 1) / kPfKeys - c.b0;
+    int lo, hi;
+    xt_piece(v0, v1, start, per, c.total, lo, hi);
+    if (lo < hi) {
+      c.kt0 = c.b0 + lo;
+      c.nkt = hi - lo;
+      c.layer = lh / p.x.Hkv;
+      c.h = lh - c.layer * p.x.Hkv;
+      c.on = true;
+      return;
+    }
+    ++c.idx;
   }
-  c.it = it;
 }
-__device__ __forceinline__ void xt_advance(XtCursor& c, int n_items, const ExtendTcParams& p, const int* s_n) {
-  if (++c.j == c.nkt) {
-    ++c.ord;
-    xt_seek(c, c.it + 1, n_items, p, s_n);
+// Where this CTA's shares begin (needs no lengths), then its first piece.
+__device__ __forceinline__ void xt_begin(XtCursor& c, const ExtendTcParams& p) {
+  const unsigned v0 = xt_share0(p, blockIdx.x);
+  int lo = 0, hi = p.x.seqs.n;
+  while (hi - lo > 1) {  // the last sequence that begins at or before the first share
+    const int mid = (lo + hi) >> 1;
+    if (p.cum[mid] <= v0) lo = mid;
+    else hi = mid;
   }
+  c.s = lo;
+  c.idx = (int)((v0 - p.cum[lo]) / p.per[lo]);
+  c.ord = 0;
+}
+__device__ __forceinline__ void xt_next_item(XtCursor& c, const ExtendTcParams& p, const int* s_n) {
+  ++c.ord;
+  ++c.idx;
+  xt_settle(c, p, s_n);
+}
+__device__ __forceinline__ void xt_advance(XtCursor& c, const ExtendTcParams& p, const int* s_n) {
+  if (++c.j == c.nkt) xt_next_item(c, p, s_n);
 }
 
 __device__ __forceinline__ float rcp_approx(float x) {
@@ -111,32 +160,61 @@ __device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
   return *reinterpret_cast<const uint32_t*>(&v);
 }
 
-// 64 rows of 128 codes, held by a warp as 16 pieces of 16 codes per lane (rows 4 i + lane / 8, piece lane % 8).
+// Codes to operand tiles.  A loading warp takes 64 rows of 128 codes in four quarters of 16 rows; a lane holds four pieces
+// of 16 codes (rows 4 i + lane / 8, piece lane % 8).  The tile is [2 halves of head_dim][rows][128 B], 16-byte
+// chunks swizzled by row; the lanes of the second half write their two chunks in the other order, so that a
+// store's eight lanes meet eight banks.
 struct XtCodes {
-  uint4 c[16];
+  uint4 c[4];
 };
-__device__ __forceinline__ void xt_load_codes(XtCodes& r, const uint8_t* base, int key0, int end, int lane) {
+__device__ __forceinline__ void xt_load_codes(XtCodes& r, const uint8_t* base, int row0, int end, int lane) {
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    const int row = key0 + 4 * i + (lane >> 3);
+  for (int i = 0; i < 4; ++i) {
+    const int row = row0 + 4 * i + (lane >> 3);
     r.c[i] = row < end ? ldg_stream(base + (size_t)row * 128 + (lane & 7) * 16) : make_uint4(0u, 0u, 0u, 0u);
   }
 }
-// ... widened into a tile [2 halves of head_dim][rows][128 B], 16-byte chunks swizzled by row.  The lanes of
-// the second half write their two chunks in the other order, so that a store's eight lanes meet eight banks.
-__device__ __forceinline__ void xt_store_codes(const XtCodes& r, uint8_t* tile, int half_bytes, int lane) {
+// Two codes in the low half of w (the other two: the high half) as a bf16 pair: the code's exponent and mantissa bits
+// in bf16's place are the value times 2^-120, subnormals included, and the product with 2^120 is exact.
+__device__ __forceinline__ uint32_t e4m3x2_to_bf16x2(uint32_t w, uint32_t sel) {
+  const uint32_t t = __byte_perm(w, 0u, sel);  // code << 8 in each half
+  const uint32_t u = (t & 0x80008000u) | ((t >> 4) & 0x07f007f0u);
+  const uint32_t big = 0x7b807b80u;  // 2^120
+  const __nv_bfloat162 y = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&u), *reinterpret_cast<const __nv_bfloat162*>(&big));
+  return *reinterpret_cast<const uint32_t*>(&y);
+}
+template <bool BF16>
+__device__ __forceinline__ void xt_store_codes(const XtCodes& r, uint8_t* tile, int half_bytes, int row0, int lane) {
   const int piece = lane & 7, half = piece >> 2;
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    const int row = 4 * i + (lane >> 3);
+  for (int i = 0; i < 4; ++i) {
+    const int row = row0 + 4 * i + (lane >> 3);
     uint8_t* dst = tile + half * half_bytes + row * 128;
     const uint32_t w[4] = {r.c[i].x, r.c[i].y, r.c[i].z, r.c[i].w};
     uint4 y[2];
     uint32_t* o = reinterpret_cast<uint32_t*>(y);
+    if constexpr (BF16) {
+      uint32_t nan = 0u;
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      o[2 * u] = e4m3x2_to_half2((unsigned short)(w[u] & 0xffffu));
-      o[2 * u + 1] = e4m3x2_to_half2((unsigned short)(w[u] >> 16));
+      for (int u = 0; u < 4; ++u) {
+        o[2 * u] = e4m3x2_to_bf16x2(w[u], 0x1404u);
+        o[2 * u + 1] = e4m3x2_to_bf16x2(w[u], 0x3424u);
+        nan |= __vcmpeq4(w[u] & 0x7f7f7f7fu, 0x7f7f7f7fu);
+      }
+      if (nan) {  // a code that is not a number
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+          const uint32_t two = (w[u >> 1] >> (16 * (u & 1))) & 0x7f7fu;
+          if ((two & 0xffu) == 0x7fu) o[u] |= 0x00007fffu;
+          if ((two >> 8) == 0x7fu) o[u] |= 0x7fff0000u;
+        }
+      }
+    } else {
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        o[2 * u] = e4m3x2_to_half2((unsigned short)(w[u] & 0xffffu));
+        o[2 * u + 1] = e4m3x2_to_half2((unsigned short)(w[u] >> 16));
+      }
     }
     const int c0 = 2 * (piece & 3);
     const uint4 a = half ? y[1] : y[0], b = half ? y[0] : y[1];
@@ -146,30 +224,52 @@ __device__ __forceinline__ void xt_store_codes(const XtCodes& r, uint8_t* tile, 
   }
 }
 
-// One query row again, by its whole warp, from the visible rows of [k0, k1) alone: sum of exp2(x_j - m) v_j,
-// lane = four columns.  For rows whose output is not finite (a hidden row held something that is not).
+// One query row again, by a whole warp, from the visible rows of [k0, k1) alone.  redo: lse is computed too (with the
+// true maximum); else the caller's is taken.  Returns the output over out_scale, lane = four columns.  For rows whose
+// fast result is not finite: a hidden row held something that is not, the weights' sum left its range, or the answer
+// is in truth not finite.
 template <bool KV8>
-__device__ __noinline__ float4 xt_row_again(const ExtendTcParams& p, int s, int layer, int h, int n, int i, int g, int k0, int k1, float m) {
+__device__ __noinline__ float4 xt_row_again(const ExtendTcParams& p, const XtCursor& c, int r, bool redo, float& lse) {
   const ExtendParams& x = p.x;
-  const int lane = threadIdx.x & 31, b = x.seqs.b0 + s, t = x.seqs.tok0[s + 1] - x.seqs.tok0[s];
-  const size_t slab = ((size_t)(x.layer0 + layer) * x.Nb + b) * x.Hkv + h;
-  const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(x.q) + ((size_t)layer * x.total + x.seqs.tok0[s] + i) * x.q_stride + (size_t)(h * x.G + g) * 128;
+  const int lane = threadIdx.x & 31, b = x.seqs.b0 + c.s, t = x.seqs.tok0[c.s + 1] - x.seqs.tok0[c.s];
+  const int i = c.i0 + r / x.G, g = r % x.G;
+  const size_t slab = ((size_t)(x.layer0 + c.layer) * x.Nb + b) * x.Hkv + c.h;
+  const __nv_bfloat16* q =
+      static_cast<const __nv_bfloat16*>(x.q) + ((size_t)c.layer * x.total + x.seqs.tok0[c.s] + i) * x.q_stride + (size_t)(c.h * x.G + g) * 128;
   const int tot = x.tot[b] - (x.published ? t : 0);
-  const float slope = x.slopes ? x.slopes[h * x.G + g] : 0.f;
-  const int lim = n + max(i + 1, x.seqs.prefix[s]);
-  float acc[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int kb = k0; kb < min(k1, lim); kb += 32) {
-    const int j = kb + lane;
-    float w = 0.f;
-    if (j < lim && j < k1) {
-      const int apart = abs(tot + i - x.pos[slab * x.cap + j]);
-      if (x.window == 0 || apart < x.window) {
-        float dot = 0.f;
-        for (int c = 0; c < 128; ++c)
-          dot = fmaf(__bfloat162float(q[c]), ext_row_value<__nv_bfloat16, KV8>(x.K, (slab * x.cap + j) * 128 + c, 1.f), dot);
-        w = fast_exp2(ext_logit_exact(x, dot, slope, apart) - m);
-      }
+  const float slope = x.slopes ? x.slopes[c.h * x.G + g] : 0.f;
+  const int k0 = c.kt0 * kPfKeys, end = min((c.kt0 + c.nkt) * kPfKeys, c.n + max(i + 1, x.seqs.prefix[c.s]));
+  auto logit = [&](int j, bool& visible) {
+    visible = false;
+    if (j >= end) return 0.f;
+    const int apart = abs(tot + i - x.pos[slab * x.cap + j]);
+    if (x.window > 0 && apart >= x.window) return 0.f;
+    visible = true;
+    float dot = 0.f;
+    for (int e = 0; e < 128; ++e) dot = fmaf(__bfloat162float(q[e]), ext_row_value<__nv_bfloat16, KV8>(x.K, (slab * x.cap + j) * 128 + e, 1.f), dot);
+    return ext_logit_exact(x, dot, slope, apart);
+  };
+  if (redo) {
+    float m = -CUDART_INF_F, l = 0.f;
+    for (int kb = k0; kb < end; kb += 32) {
+      bool visible;
+      const float y = logit(kb + lane, visible);
+      float mx = visible ? y : -CUDART_INF_F;
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+      const float mn = fmaxf(m, mx);
+      l = l * (m == -CUDART_INF_F ? 0.f : exp2f(m - mn)) + (visible ? exp2f(y - mn) : 0.f);  // (lane's own sum)
+      m = mn;
     }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+    lse = m + log2f(l);
+  }
+  float acc[4] = {0.f, 0.f, 0.f, 0.f};
+  for (int kb = k0; kb < end; kb += 32) {
+    bool visible;
+    const float y = logit(kb + lane, visible);
+    const float w = visible ? exp2f(y - lse) : 0.f;
     for (int kk = 0; kk < 32; ++kk) {
       const float wk = __shfl_sync(0xffffffffu, w, kk);
       if (wk == 0.f) continue;
@@ -181,157 +281,6 @@ __device__ __noinline__ float4 xt_row_again(const ExtendTcParams& p, int s, int 
   return make_float4(acc[0], acc[1], acc[2], acc[3]);
 }
 
-// The end of an item, by the softmax warps: its output (or its part's) from tensor memory.  A function of its own:
-// it runs once per item, and inlined its registers would cost the tile loop spills.
-template <bool KV8>
-__device__ __noinline__ void xt_epilogue(const ExtendTcParams& p, const XtCursor& c, float m, float l, uint32_t tO, uint32_t bar12,
-                                         volatile int* s_abort, uint8_t* s_out) {
-  const ExtendParams& x = p.x;
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const uint32_t lane_base = (uint32_t)(warp * 32) << 16;
-  const uint32_t g_inv = 65536u / (uint32_t)x.G + 1u;
-  uint8_t* stage = s_out + warp * (32 * 128);
-  const int r = tid;
-
-  // The row of O, normalised and rounded: half a row at a time through the warp's staging tile, so that the
-  // global stores are whole 128-byte lines (prefill_attn.cuh).
-  auto write_half = [&](const XtCursor& c, int c0, const uint32_t (&o)[2][32], float factor) {
-    const uint64_t f2 = tc5::f2_pack(factor, factor);
-#pragma unroll
-    for (int hh = 0; hh < 2; ++hh) {
-#pragma unroll
-      for (int e = 0; e < 32; e += 8) {
-        uint32_t w[4];
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          float y0, y1;
-          tc5::f2_unpack(tc5::f2_mul(tc5::f2_pack(__uint_as_float(o[hh][e + 2 * u]), __uint_as_float(o[hh][e + 2 * u + 1])), f2), y0, y1);
-          w[u] = pack_bf16x2(y0, y1);
-        }
-        const int chunk = 4 * hh + (e >> 3);
-        *reinterpret_cast<uint4*>(stage + lane * 128 + ((chunk ^ (lane & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
-      }
-    }
-    __syncwarp();
-    __nv_bfloat16* obase = static_cast<__nv_bfloat16*>(x.out) +
-                           (((size_t)c.layer * x.total + x.seqs.tok0[c.s] + c.i0) * x.Hq + c.h * x.G) * 128 + c0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int row = 4 * i + (lane >> 3), chunk = lane & 7;
-      const uint4 w = *reinterpret_cast<const uint4*>(stage + row * 128 + ((chunk ^ (row & 7)) << 4));
-      const int rr = warp * 32 + row;
-      const int ti = (int)((uint32_t)rr * g_inv >> 16);
-      if (rr < c.rows && !*s_abort) *reinterpret_cast<uint4*>(obase + ((size_t)ti * x.Hq + (rr - ti * x.G)) * 128 + chunk * 8) = w;
-    }
-    __syncwarp();
-  };
-  // Half a row of the unnormalised O from tensor memory; elements that are not finite are computed again.
-  auto read_half = [&](const XtCursor& c, int c0, uint32_t (&o)[2][32], float m) {
-    tc5::tmem_ld32(tO + lane_base + (uint32_t)c0, o[0]);
-    tc5::tmem_ld32(tO + lane_base + (uint32_t)c0 + 32u, o[1]);
-    tc5::tmem_wait_ld();
-    float probe = 0.f;  // 0 * finite = 0
-#pragma unroll
-    for (int e = 0; e < 32; ++e) probe = fmaf(__uint_as_float(o[0][e]), 0.f, fmaf(__uint_as_float(o[1][e]), 0.f, probe));
-    unsigned again = __ballot_sync(0xffffffffu, !(probe == 0.f) && r < c.rows);
-    while (again) {
-      const int who = __ffs(again) - 1;
-      again &= again - 1;
-      const int rr = warp * 32 + who, ti = (int)((uint32_t)rr * g_inv >> 16);
-      const float mm = __shfl_sync(0xffffffffu, m, who);
-      const float4 y = xt_row_again<KV8>(p, c.s, c.layer, c.h, c.n, c.i0 + ti, rr - ti * x.G, c.kt0 * kPfKeys, (c.kt0 + c.nkt) * kPfKeys, mm);
-      __syncwarp();
-      reinterpret_cast<float4*>(stage)[lane] = y;
-      __syncwarp();
-      if (lane == who) {
-#pragma unroll
-        for (int e = 0; e < 32; ++e) {
-          if (!(__uint_as_float(o[0][e]) * 0.f == 0.f)) o[0][e] = reinterpret_cast<const uint32_t*>(stage)[c0 + e];
-          if (!(__uint_as_float(o[1][e]) * 0.f == 0.f)) o[1][e] = reinterpret_cast<const uint32_t*>(stage)[c0 + 32 + e];
-        }
-      }
-      __syncwarp();
-    }
-  };
-  const float out_scale = KV8 ? x.v_scale : 1.f;
-
-  mbar_wait(bar12, (uint32_t)(c.ord & 1), s_abort, x.err, kPfSpinLimit);
-  tc5::fence_after_sync();
-  const bool live = warp * 32 < c.rows;
-  uint32_t o[2][32];
-  if (c.n_split == 1) {
-    if (!live) return;
-    const float f = out_scale / l;
-#pragma unroll 1
-    for (int c0 = 0; c0 < 128; c0 += 64) {
-      read_half(c, c0, o, m);
-      write_half(c, c0, o, f);
-    }
-    if (x.lse && r < c.rows) x.lse[ext_lse_index(x, c.layer, c.h, x.seqs.tok0[c.s] + c.i0) + r] = m + __log2f(l);
-    return;
-  }
-  // one of several parts: [32 pieces of four columns][part_rows] float4, then [part_rows] (m, l)
-  const size_t piece = (size_t)p.part_rows;
-  auto part_of = [&](int split) { return p.part + ((size_t)(c.u0 + split) * p.lh + c.lh) * (piece * kXtPartFloats); };
-  if (live) {
-    float* mine = part_of(c.split);
-#pragma unroll 1
-    for (int c0 = 0; c0 < 128; c0 += 64) {
-      read_half(c, c0, o, m);
-      if (r < c.rows && !*s_abort) {
-#pragma unroll
-        for (int hh = 0; hh < 2; ++hh)
-#pragma unroll
-          for (int e = 0; e < 32; e += 4)
-            __stcg(reinterpret_cast<float4*>(mine) + (size_t)(c0 / 4 + 8 * hh + e / 4) * piece + r,
-                   make_float4(__uint_as_float(o[hh][e]), __uint_as_float(o[hh][e + 1]), __uint_as_float(o[hh][e + 2]), __uint_as_float(o[hh][e + 3])));
-      }
-    }
-    if (r < c.rows && !*s_abort) __stcg(reinterpret_cast<float2*>(mine + 128 * piece) + r, make_float2(m, l));
-  }
-  __threadfence();
-  asm volatile("bar.sync 1, 128;" ::: "memory");
-  int* s_last = reinterpret_cast<int*>(s_out);  // (the first warp's staging tile is free here)
-  if (tid == 0) *s_last = atomicAdd(x.counters + (size_t)c.u0 * p.lh + c.lh, 1u) == (unsigned)(c.n_split - 1);
-  asm volatile("bar.sync 1, 128;" ::: "memory");
-  const bool last = *s_last != 0;
-  asm volatile("bar.sync 1, 128;" ::: "memory");
-  if (!last || !live) return;
-  __threadfence();
-  const int rr = min(r, c.rows - 1);  // (lanes without a row follow along)
-  float M = -CUDART_INF_F;
-  for (int k = 0; k < c.n_split; ++k) M = fmaxf(M, __ldcg(reinterpret_cast<const float2*>(part_of(k) + 128 * piece) + rr).x);
-  const float M0 = M == -CUDART_INF_F ? 0.f : M;
-  float Lsum = 0.f;
-  for (int k = 0; k < c.n_split; ++k) {
-    const float2 ml = __ldcg(reinterpret_cast<const float2*>(part_of(k) + 128 * piece) + rr);
-    Lsum += ml.y * fast_exp2(ml.x - M0);
-  }
-  const float f = out_scale / Lsum;
-#pragma unroll 1
-  for (int c0 = 0; c0 < 128; c0 += 64) {
-#pragma unroll
-    for (int e = 0; e < 32; ++e) o[0][e] = o[1][e] = 0u;
-#pragma unroll 1
-    for (int k = 0; k < c.n_split; ++k) {
-      const float* src = part_of(k);
-      const float wk = fast_exp2(__ldcg(reinterpret_cast<const float2*>(src + 128 * piece) + rr).x - M0);
-#pragma unroll
-      for (int hh = 0; hh < 2; ++hh)
-#pragma unroll
-        for (int e = 0; e < 32; e += 4) {
-          const float4 y = __ldcg(reinterpret_cast<const float4*>(src) + (size_t)(c0 / 4 + 8 * hh + e / 4) * piece + rr);
-          o[hh][e] = __float_as_uint(fmaf(wk, y.x, __uint_as_float(o[hh][e])));
-          o[hh][e + 1] = __float_as_uint(fmaf(wk, y.y, __uint_as_float(o[hh][e + 1])));
-          o[hh][e + 2] = __float_as_uint(fmaf(wk, y.z, __uint_as_float(o[hh][e + 2])));
-          o[hh][e + 3] = __float_as_uint(fmaf(wk, y.w, __uint_as_float(o[hh][e + 3])));
-        }
-    }
-    write_half(c, c0, o, f);
-  }
-  if (x.lse && r < c.rows) x.lse[ext_lse_index(x, c.layer, c.h, x.seqs.tok0[c.s] + c.i0) + r] = M + __log2f(Lsum);
-}
-
 template <bool KV8, bool MODS>
 __global__ void __launch_bounds__(kXtThreads, 2)
 extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
@@ -341,10 +290,10 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
   const uint32_t sQ = smem_u32(sm);                       // [2 halves of head_dim][128 rows][128 B]
   const uint32_t sK = sQ + kPfQBytes;                     // [2 stages][2 halves][64 rows][128 B]
   const uint32_t sV = sK + 2 * kPfKvBytes;                // the same
-  uint8_t* s_out = sm + kPfQBytes + 4 * kPfKvBytes;       // [4 softmax warps][32 rows][128 B]
+  uint8_t* s_out = sm + kPfQBytes + 4 * kPfKvBytes;       // [8 softmax warps][2 KB]
   uint64_t* bars = reinterpret_cast<uint64_t*>(s_out + kPfOutStageBytes);
-  // barriers: 0 Q, 1-2 K stages filled, 3-4 V stages filled, 5-6 S buffers complete, 7 O += P V complete, 8-9 P written
-  // (per S buffer), 10-11 V stages read, 12 the item's last O += P V complete, 13-14 drain (see prefill_attn.cuh)
+  // barriers: 0 Q, 1-2 K stages filled, 3-4 V stages filled, 5-6 S buffers complete, 7 O has been read, 8-9 P written (per S
+  // buffer), 10-11 V stages and P read, 12 the piece's last O += P V complete, 13-14 drain
   const uint32_t bar0 = smem_u32(bars);
   auto bar = [&](int i) { return bar0 + 8u * (uint32_t)i; };
   uint32_t* s_tmem = reinterpret_cast<uint32_t*>(bars + 15);
@@ -353,9 +302,8 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
   const ExtendParams& x = p.x;
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int n_items = (p.n_work - (int)blockIdx.x + (int)gridDim.x - 1) / (int)gridDim.x;
   if (tid == 0) {
-    for (int i = 0; i < 15; ++i) mbar_init(bar(i), (i == 8 || i == 9) ? kXtRows : 1);
+    for (int i = 0; i < 15; ++i) mbar_init(bar(i), i == 7 ? 2 * kXtRows : (i == 8 || i == 9) ? kXtRows : 1);
     *s_abort = 0;
     if ((smem_u32(sm) & 1023u) != 0u) {
       atomicOr(x.err, kErrStreamBounds);
@@ -364,10 +312,19 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
-  if (warp == 5) {
+  if (warp == 10) {
     tc5::tmem_alloc(smem_u32(s_tmem), kPfTmemCols);
     tc5::tmem_relinquish();
   }
+  if (tid == 9 * 32) {
+    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&tmQ)) : "memory");
+    if constexpr (!KV8) {
+      asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&tmK)) : "memory");
+      asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&tmV)) : "memory");
+    }
+  }
+  XtCursor first;
+  xt_begin(first, p);
   // The storing kernel may still be running; everything below waits until it has completed.
   asm volatile("griddepcontrol.wait;" ::: "memory");
   for (int s = tid; s < x.seqs.n; s += kXtThreads) {
@@ -379,92 +336,96 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
   tc5::fence_after_sync();
   const uint32_t tmem = *s_tmem;
   const uint32_t tS0 = tmem, tO = tmem + 128;  // S buffer b at column 64 b
-  XtCursor first;
-  first.ord = 0;
-  xt_seek(first, 0, n_items, p, s_n);
+  xt_settle(first, p, s_n);
   auto slab_of = [&](const XtCursor& c) { return ((x.layer0 + c.layer) * x.Nb + x.seqs.b0 + c.s) * x.Hkv + c.h; };
-  const uint32_t q_bytes = 256u * (uint32_t)(x.G * p.tokens_per_tile);
-  auto load_q = [&](const XtCursor& c) {
-    const int tok = c.layer * x.total + x.seqs.tok0[c.s] + c.i0;
-    mbar_arrive_expect_tx(bar(0), q_bytes);
-    pf_tma_load(sQ, &tmQ, 0, c.h * x.G, tok, bar(0));
-    pf_tma_load(sQ + kPfQBytes / 2, &tmQ, 64, c.h * x.G, tok, bar(0));
-  };
+  auto key0_of = [&](const XtCursor& c) { return (c.kt0 + c.nkt - 1 - c.j) * kPfKeys; };
   auto load_tile = [&](const CUtensorMap* tm, uint32_t base, int bar_i, const XtCursor& c, int g) {
     const uint32_t dst = base + (uint32_t)(g & 1) * kPfKvBytes, bb = bar(bar_i + (g & 1));
-    const int row = (c.kt0 + c.j) * kPfKeys, slab = slab_of(c);
+    const int row = key0_of(c), slab = slab_of(c);
     mbar_arrive_expect_tx(bb, kPfKvBytes);
     pf_tma_load(dst, tm, 0, row, slab, bb);
     pf_tma_load(dst + kPfKvBytes / 2, tm, 64, row, slab, bb);
   };
-  // 8-bit rows: the loading warps fill a stage themselves
-  XtCodes codes;
-  auto fetch_codes = [&](const void* base, const XtCursor& c) {
-    const int t = x.seqs.tok0[c.s + 1] - x.seqs.tok0[c.s];
-    xt_load_codes(codes, static_cast<const uint8_t*>(base) + (size_t)slab_of(c) * x.cap * 128, (c.kt0 + c.j) * kPfKeys, c.n + t, lane);
+  // 8-bit rows: a loading warp fills a stage itself, two quarters of the tile ahead in registers
+  XtCodes qa, qb;
+  auto codes_of = [&](const void* base, const XtCursor& c) { return static_cast<const uint8_t*>(base) + (size_t)slab_of(c) * x.cap * 128; };
+  auto ends_of = [&](const XtCursor& c) { return c.n + x.seqs.tok0[c.s + 1] - x.seqs.tok0[c.s]; };
+  auto begin_codes = [&](const void* base, const XtCursor& c) {
+    const uint8_t* src = codes_of(base, c);
+    const int k0 = key0_of(c), end = ends_of(c);
+    xt_load_codes(qa, src, k0, end, lane);
+    xt_load_codes(qb, src, k0 + 16, end, lane);
   };
-  auto fill_stage = [&](uint32_t off, int bar_i, int g) {
-    xt_store_codes(codes, sm + off + (uint32_t)(g & 1) * kPfKvBytes, kPfKvBytes / 2, lane);
+  // fills the stage of tile g with the tile of c and leaves c (and the registers) at the next tile
+  auto fill_stage = [&](auto bf16, const void* base, uint32_t off, int bar_i, XtCursor& c, int g) {
+    constexpr bool BF16 = decltype(bf16)::value;
+    uint8_t* tile = sm + off + (uint32_t)(g & 1) * kPfKvBytes;
+    const uint8_t* src = codes_of(base, c);
+    const int k0 = key0_of(c), end = ends_of(c);
+    // (the tile four further on towards the older rows: asked into L2 now)
+    if (lane == 0 && c.j + 4 < c.nkt)
+      asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(src + (size_t)(k0 - 4 * kPfKeys) * 128), "r"(kPfKeys * 128) : "memory");
+    xt_store_codes<BF16>(qa, tile, kPfKvBytes / 2, 0, lane);
+    xt_load_codes(qa, src, k0 + 32, end, lane);
+    xt_store_codes<BF16>(qb, tile, kPfKvBytes / 2, 16, lane);
+    xt_load_codes(qb, src, k0 + 48, end, lane);
+    xt_advance(c, p, s_n);
+    xt_store_codes<BF16>(qa, tile, kPfKvBytes / 2, 32, lane);
+    if (c.on) xt_load_codes(qa, codes_of(base, c), key0_of(c), ends_of(c), lane);
+    xt_store_codes<BF16>(qb, tile, kPfKvBytes / 2, 48, lane);
+    if (c.on) xt_load_codes(qb, codes_of(base, c), key0_of(c) + 16, ends_of(c), lane);
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     __syncwarp();
     if (lane == 0) mbar_arrive(bar(bar_i + (g & 1)));
     __syncwarp();
   };
 
-  if (warp == 4) {
+  if (warp == 8) {
     // ================= the warp that loads Q and K =================
     if (lane == 0 && *reinterpret_cast<volatile int*>(p.stop) != 0) *s_abort = 1;
     __syncwarp();
-    if (first.it < n_items && !*s_abort) {
+    const uint32_t q_bytes = 256u * (uint32_t)(x.G * p.tokens_per_tile);
+    auto load_q = [&](const XtCursor& c) {
+      const int tok = c.layer * x.total + x.seqs.tok0[c.s] + c.i0;
+      mbar_arrive_expect_tx(bar(0), q_bytes);
+      pf_tma_load(sQ, &tmQ, 0, c.h * x.G, tok, bar(0));
+      pf_tma_load(sQ + kPfQBytes / 2, &tmQ, 64, c.h * x.G, tok, bar(0));
+    };
+    if (first.on && !*s_abort) {
       if (tc5::elect_one()) load_q(first);
       __syncwarp();
       XtCursor cur = first, cK = first;
-      if constexpr (KV8) fetch_codes(x.K, cK);
-      for (int g = 0; g < 2 && cK.it < n_items; ++g) {
+      auto fill_k = [&](int g) {
         if constexpr (KV8) {
-          fill_stage(kPfQBytes, 1, g);
-          xt_advance(cK, n_items, p, s_n);
-          if (cK.it < n_items) fetch_codes(x.K, cK);
+          fill_stage(std::false_type{}, x.K, kPfQBytes, 1, cK, g);
         } else {
           if (tc5::elect_one()) load_tile(&tmK, sK, 1, cK, g);
           __syncwarp();
-          xt_advance(cK, n_items, p, s_n);
+          xt_advance(cK, p, s_n);
         }
-      }
-      XtCursor nq = first;  // the item after the current one
-      ++nq.ord;
-      xt_seek(nq, first.it + 1, n_items, p, s_n);
-      for (int g = 0; cur.it < n_items && !*s_abort; ++g) {
-        const bool next_q = cur.j == cur.nkt - 1 && nq.it < n_items;
-        if (cur.j == 0 && nq.it < n_items && tc5::elect_one()) {
+      };
+      if constexpr (KV8) begin_codes(x.K, cK);
+      for (int g = 0; g < 2 && cK.on; ++g) fill_k(g);
+      XtCursor nq = first;  // the piece after the current one
+      xt_next_item(nq, p, s_n);
+      for (int g = 0; cur.on && !*s_abort; ++g) {
+        const bool next_q = cur.j == cur.nkt - 1 && nq.on;
+        if (cur.j == 0 && nq.on && tc5::elect_one()) {
           const int tok = nq.layer * x.total + x.seqs.tok0[nq.s] + nq.i0;
           pf_tma_prefetch(&tmQ, 0, nq.h * x.G, tok);
           pf_tma_prefetch(&tmQ, 64, nq.h * x.G, tok);
         }
-        if (cK.it < n_items || next_q) {
+        if (cK.on || next_q) {
           mbar_wait(bar(5 + (g & 1)), (uint32_t)((g >> 1) & 1), s_abort, x.err, kPfSpinLimit);
           __syncwarp();
           if (*s_abort) break;
           if (next_q && tc5::elect_one()) load_q(nq);
           __syncwarp();
-          if (cK.it < n_items) {  // tile g + 2: the stage S_g read
-            if constexpr (KV8) {
-              fill_stage(kPfQBytes, 1, g);
-              xt_advance(cK, n_items, p, s_n);
-              if (cK.it < n_items) fetch_codes(x.K, cK);
-            } else {
-              if (tc5::elect_one()) load_tile(&tmK, sK, 1, cK, g);
-              __syncwarp();
-              xt_advance(cK, n_items, p, s_n);
-            }
-          }
+          if (cK.on) fill_k(g);  // tile g + 2: the stage S_g read
         }
         if (cur.j == cur.nkt - 1) {
           cur = nq;
-          if (nq.it < n_items) {
-            ++nq.ord;
-            xt_seek(nq, nq.it + 1, n_items, p, s_n);
-          }
+          if (nq.on) xt_next_item(nq, p, s_n);
         } else {
           ++cur.j;
         }
@@ -478,25 +439,23 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
           for (uint32_t w = 0; w < (1u << 16); ++w)
             if (mbar_try_wait(bar(i), ph)) break;
     }
-  } else if (warp == 7) {
+  } else if (warp == 9) {
     // ================= the warp that loads V =================
     XtCursor cV = first;
     if constexpr (KV8) {
-      if (cV.it < n_items) fetch_codes(x.V, cV);
+      if (cV.on) begin_codes(x.V, cV);
     }
-    for (int g = 0; cV.it < n_items && !*s_abort; ++g) {
+    for (int g = 0; cV.on && !*s_abort; ++g) {
       // V of tile g after O += P V of tile g - 2 has completed (the stage it read)
       if (g >= 2) mbar_wait(bar(10 + (g & 1)), (uint32_t)(((g - 2) >> 1) & 1), s_abort, x.err, kPfSpinLimit);
       __syncwarp();
       if (*s_abort) break;
       if constexpr (KV8) {
-        fill_stage(kPfQBytes + 2 * kPfKvBytes, 3, g);
-        xt_advance(cV, n_items, p, s_n);
-        if (cV.it < n_items) fetch_codes(x.V, cV);
+        fill_stage(std::true_type{}, x.V, kPfQBytes + 2 * kPfKvBytes, 3, cV, g);
       } else {
         if (tc5::elect_one()) load_tile(&tmV, sV, 3, cV, g);
         __syncwarp();
-        xt_advance(cV, n_items, p, s_n);
+        xt_advance(cV, p, s_n);
       }
     }
     if (!KV8 && *s_abort && lane == 0) {
@@ -506,46 +465,48 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
           for (uint32_t w = 0; w < (1u << 16); ++w)
             if (mbar_try_wait(bar(i), ph)) break;
     }
-  } else if (warp == 5) {
+  } else if (warp == 11) {
     // ================= the warp that issues O += P V =================
-    constexpr uint32_t idesc_o = KV8 ? tc5::idesc_f16_f32(kXtRows, 128, 0, 1) : tc5::idesc_bf16_f32(kXtRows, 128, 0, 1);
+    constexpr uint32_t idesc_o = tc5::idesc_bf16_f32(kXtRows, 128, 0, 1);
     const uint64_t dV = tc5::smem_desc_sw128(sV, kPfKvBytes / 2, 1024);
     XtCursor cur = first;
-    for (int g = 0; cur.it < n_items && !*s_abort; ++g) {
+    for (int g = 0; cur.on && !*s_abort; ++g) {
       const int st = g & 1;
       mbar_wait(bar(3 + st), (uint32_t)((g >> 1) & 1), s_abort, x.err, kPfSpinLimit);
       mbar_wait(bar(8 + st), (uint32_t)((g >> 1) & 1), s_abort, x.err, kPfSpinLimit);
+      if (cur.j == 0 && cur.ord > 0) mbar_wait(bar(7), (uint32_t)((cur.ord - 1) & 1), s_abort, x.err, kPfSpinLimit);  // O of the piece before
       __syncwarp();
       tc5::fence_after_sync();
       if (*s_abort) break;
       const uint64_t dVg = dV + (uint64_t)((uint32_t)st * (kPfKvBytes >> 4));
       if (tc5::elect_one()) {
 #pragma unroll
-        for (int kk = 0; kk < 4; ++kk)
+        for (int kk = 0; kk < 4; ++kk)  // 16 keys per step: 8 columns of P (over S buffer g & 1), two 8-row groups of V
           tc5::mma_bf16_ts(tO, tS0 + 64u * (uint32_t)st + 8u * (uint32_t)kk, dVg + (uint64_t)(kk * 128), idesc_o,
                            (cur.j > 0 || kk > 0) ? 1u : 0u);
-        tc5::mma_commit(bar(7));
         tc5::mma_commit(bar(10 + st));
         if (cur.j == cur.nkt - 1) tc5::mma_commit(bar(12));
       }
       __syncwarp();
-      xt_advance(cur, n_items, p, s_n);
+      xt_advance(cur, p, s_n);
     }
     if (*s_abort && tc5::elect_one()) {
+      // give the MMAs already issued a bounded time to finish before the tensor memory is released
       atomicOr(p.stop, 1);
       tc5::mma_commit(bar(13));
       for (uint32_t w = 0; w < kPfSpinLimit; ++w)
         if (mbar_try_wait(bar(13), 0u)) break;
     }
-  } else if (warp == 6) {
+  } else if (warp == 10) {
     // ================= the warp that issues S = Q K^T =================
     constexpr uint32_t idesc_s = KV8 ? tc5::idesc_f16_f32(kXtRows, kPfKeys, 0, 0) : tc5::idesc_bf16_f32(kXtRows, kPfKeys, 0, 0);
     const uint64_t dQ = tc5::smem_desc_sw128(sQ, 16, 1024);
     const uint64_t dK = tc5::smem_desc_sw128(sK, 16, 1024);
     XtCursor cur = first;
-    for (int g = 0; cur.it < n_items && !*s_abort; ++g) {
+    for (int g = 0; cur.on && !*s_abort; ++g) {
       const int st = g & 1;
       mbar_wait(bar(1 + st), (uint32_t)((g >> 1) & 1), s_abort, x.err, kPfSpinLimit);
+      // S of tile g overwrites the columns P of tile g - 2 is read from
       if (g >= 2) mbar_wait(bar(10 + st), (uint32_t)(((g - 2) >> 1) & 1), s_abort, x.err, kPfSpinLimit);
       if (cur.j == 0) mbar_wait(bar(0), (uint32_t)(cur.ord & 1), s_abort, x.err, kPfSpinLimit);
       __syncwarp();
@@ -561,7 +522,7 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
         }
         __syncwarp();
       }
-      xt_advance(cur, n_items, p, s_n);
+      xt_advance(cur, p, s_n);
     }
     if (*s_abort && tc5::elect_one()) {
       atomicOr(p.stop, 1);
@@ -571,76 +532,234 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
     }
   } else {
     // ================= softmax warps: thread = query row = tensor-memory lane =================
-    const uint32_t lane_base = (uint32_t)(warp * 32) << 16;
+    const int wg = warp >> 2, wq = warp & 3;              // group; warp within it (its lanes of tensor memory)
+    const uint32_t lane_base = (uint32_t)(wq * 32) << 16;
     const uint32_t g_inv = 65536u / (uint32_t)x.G + 1u;  // r / G == r * g_inv >> 16 for r < 128
-    uint8_t* stage = s_out + warp * (32 * 128);
-    const int r = tid;                                    // query row within the tile
+    uint8_t* stage = s_out + warp * 2048;
+    uint8_t* stage_other = s_out + (warp ^ 4) * 2048;     // the warp of the other group with the same rows
+    const int r = wq * 32 + lane;                         // query row within the tile
     const int ri = (int)((uint32_t)r * g_inv >> 16), rg = r - ri * x.G;
+    const float out_scale = KV8 ? x.v_scale : 1.f;
+    auto pair_sync = [&]() { asm volatile("bar.sync %0, 64;" ::"r"(2 + wq) : "memory"); };
+    auto all_sync = [&]() { asm volatile("bar.sync 1, 256;" ::: "memory"); };
 
-    bool ep_on = false;  // an item whose epilogue is still to run, and what it needs
-    XtCursor ep_c = first;
-    float ep_m = 0.f, ep_l = 0.f;
+    // The end of a piece: this group's 64 columns of the output, or of its part of an item that other CTAs share.
+    auto epilogue = [&](const XtCursor& c, float ref, float l) {
+      mbar_wait(bar(12), (uint32_t)(c.ord & 1), s_abort, x.err, kPfSpinLimit);
+      tc5::fence_after_sync();
+      const bool live = wq * 32 < c.rows, mine = r < c.rows, whole = c.nkt == c.total;
+      const unsigned per = p.per[c.s], start = p.cum[c.s] + (unsigned)c.idx * per;
+      // A part: [32 pieces of four columns][part_rows] float4, then [part_rows] log-sum-exps.  A CTA has two places, one for
+      // an item that began before its shares and one for an item that begins in them.
+      auto part_of = [&](unsigned place) { return p.part + (size_t)place * ((size_t)p.part_rows * kXtPartFloats); };
+      const size_t piece = (size_t)p.part_rows;
+      const bool redo = mine && !(l < kXtSumMax);  // out of range, or not a number
+      float lse = l > 0.f ? ref + __log2f(l) : -CUDART_INF_F;
+      const float f = l > 0.f ? 1.f / l : 0.f;
+      __nv_bfloat16* obase = static_cast<__nv_bfloat16*>(x.out) + (((size_t)c.layer * x.total + x.seqs.tok0[c.s] + c.i0) * x.Hq + c.h * x.G) * 128;
+      if (live) {
+#pragma unroll 1
+        for (int half = 0; half < 2; ++half) {
+          const int c0 = 64 * wg + 32 * half;
+          uint32_t o[32];
+          tc5::tmem_ld32(tO + lane_base + (uint32_t)c0, o);
+          tc5::tmem_wait_ld();
+          if (half == 1) {
+            tc5::fence_before_sync();
+            mbar_arrive(bar(7));  // O may be written again
+          }
+          float probe = 0.f;  // 0 * finite = 0
+#pragma unroll
+          for (int e = 0; e < 32; ++e) {
+            o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+            probe = fmaf(__uint_as_float(o[e]), 0.f, probe);
+          }
+          unsigned again = __ballot_sync(0xffffffffu, mine && (redo || !(probe == 0.f)));
+          while (again) {
+            const int who = __ffs(again) - 1;
+            again &= again - 1;
+            const bool full = __shfl_sync(0xffffffffu, redo ? 1 : 0, who) != 0;
+            float new_lse = __shfl_sync(0xffffffffu, lse, who);
+            const float4 y = xt_row_again<KV8>(p, c, wq * 32 + who, full, new_lse);
+            __syncwarp();
+            reinterpret_cast<float4*>(stage)[lane] = y;
+            __syncwarp();
+            if (lane == who) {
+              lse = new_lse;
+#pragma unroll
+              for (int e = 0; e < 32; ++e)
+                if (full || !(__uint_as_float(o[e]) * 0.f == 0.f)) o[e] = reinterpret_cast<const uint32_t*>(stage)[c0 + e];
+            }
+            __syncwarp();
+          }
+          if (whole) {
+            // rounded, through the warp's staging tile [32 rows][64 B] (16-byte chunks swizzled), so that the stores are
+            // 64-byte pieces of rows
+#pragma unroll
+            for (int e = 0; e < 32; e += 8) {
+              uint32_t w[4];
+#pragma unroll
+              for (int u = 0; u < 4; ++u)
+                w[u] = pack_bf16x2(__uint_as_float(o[e + 2 * u]) * out_scale, __uint_as_float(o[e + 2 * u + 1]) * out_scale);
+              *reinterpret_cast<uint4*>(stage + lane * 64 + (((e >> 3) ^ ((lane >> 1) & 3)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
+            }
+            __syncwarp();
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const int row = 8 * i + (lane >> 2), chunk = lane & 3;
+              const uint4 w = *reinterpret_cast<const uint4*>(stage + row * 64 + ((chunk ^ ((row >> 1) & 3)) << 4));
+              const int rr = wq * 32 + row, ti = (int)((uint32_t)rr * g_inv >> 16);
+              if (rr < c.rows && !*s_abort) *reinterpret_cast<uint4*>(obase + ((size_t)ti * x.Hq + (rr - ti * x.G)) * 128 + c0 + chunk * 8) = w;
+            }
+            __syncwarp();
+          } else if (mine && !*s_abort) {
+            float* dst = part_of(2u * blockIdx.x + (start >= xt_share0(p, blockIdx.x) ? 1u : 0u));
+#pragma unroll
+            for (int e = 0; e < 32; e += 4)
+              __stcg(reinterpret_cast<float4*>(dst) + (size_t)(c0 / 4 + e / 4) * piece + r,
+                     make_float4(__uint_as_float(o[e]), __uint_as_float(o[e + 1]), __uint_as_float(o[e + 2]), __uint_as_float(o[e + 3])));
+            if (wg == 0 && half == 1) __stcg(dst + 128 * piece + r, lse);
+          }
+        }
+      } else {
+        mbar_arrive(bar(7));
+      }
+      if (whole) {
+        if (wg == 0 && mine && x.lse) x.lse[ext_lse_index(x, c.layer, c.h, x.seqs.tok0[c.s] + c.i0) + r] = lse;
+        return;
+      }
+      __threadfence();
+      all_sync();
+      // the places of the item's parts, in the order of the list, and how many there are (the staging tiles are free here)
+      int* s_list = reinterpret_cast<int*>(s_out);            // [0] last to finish, [1] parts, [2 ...] places
+      float* s_lse = reinterpret_cast<float*>(s_out) + 1024;  // [128]
+      if (warp == 0) {
+        auto cta_of = [&](unsigned v) {
+          const unsigned big = p.share_rem * (p.share_q + 1u);
+          return v < big ? v / (p.share_q + 1u) : p.share_rem + (v - big) / p.share_q;
+        };
+        const unsigned ca = cta_of(start), cb = cta_of(start + per - 1u);
+        int count = 0;
+        for (unsigned c0 = ca; c0 <= cb; c0 += 32) {
+          const unsigned cc = c0 + (unsigned)lane;
+          int lo = 0, hi = 0;
+          if (cc <= cb) xt_piece(xt_share0(p, cc), xt_share0(p, cc + 1u), start, per, c.total, lo, hi);
+          const unsigned has = __ballot_sync(0xffffffffu, lo < hi);
+          if (lo < hi) s_list[2 + count + __popc(has & ((1u << lane) - 1u))] = (int)(2u * cc + (start >= xt_share0(p, cc) ? 1u : 0u));
+          count += __popc(has);
+        }
+        if (lane == 0) {
+          s_list[1] = count;
+          s_list[0] = atomicAdd(x.counters + ca, 1u) == (unsigned)(count - 1);
+        }
+      }
+      all_sync();
+      const int n_parts = s_list[1];
+      if (s_list[0]) {
+        __threadfence();
+        if (wg == 0 && mine) {  // thread = row: log2 of the sum over the parts
+          float M = -CUDART_INF_F, sum = 0.f;
+#pragma unroll 8
+          for (int k = 0; k < n_parts; ++k) M = fmaxf(M, __ldcg(part_of(s_list[2 + k]) + 128 * piece + r));
+          const float M0 = M == -CUDART_INF_F ? 0.f : M;
+#pragma unroll 8
+          for (int k = 0; k < n_parts; ++k) sum += exp2f(__ldcg(part_of(s_list[2 + k]) + 128 * piece + r) - M0);
+          const float all = M + __log2f(sum);
+          s_lse[r] = all;
+          if (x.lse) x.lse[ext_lse_index(x, c.layer, c.h, x.seqs.tok0[c.s] + c.i0) + r] = all;
+        }
+        all_sync();
+        // a warp takes 8 rows x 64 columns at a time, a lane four pieces of four columns of one row: 128-byte pieces of
+        // every part, whole sectors of the output
+        const int units = (c.rows + 7) / 8 * 2;
+        for (int u = warp; u < units; u += 8) {
+          const int row = (u >> 1) * 8 + (lane >> 2), c4 = (u & 1) * 16 + (lane & 3);
+          if (row < c.rows && !*s_abort) {
+            const float all = s_lse[row];
+            float acc[16];
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[e] = 0.f;
+#pragma unroll 2
+            for (int k = 0; k < n_parts; ++k) {
+              const float* src = part_of(s_list[2 + k]);
+              const float wk = fast_exp2(__ldcg(src + 128 * piece + row) - all);
+              float4 y[4];
+#pragma unroll
+              for (int e = 0; e < 4; ++e) y[e] = __ldcg(reinterpret_cast<const float4*>(src) + (size_t)(c4 + 4 * e) * piece + row);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                acc[4 * e] = fmaf(wk, y[e].x, acc[4 * e]);
+                acc[4 * e + 1] = fmaf(wk, y[e].y, acc[4 * e + 1]);
+                acc[4 * e + 2] = fmaf(wk, y[e].z, acc[4 * e + 2]);
+                acc[4 * e + 3] = fmaf(wk, y[e].w, acc[4 * e + 3]);
+              }
+            }
+            const int ti = (int)((uint32_t)row * g_inv >> 16);
+            __nv_bfloat16* dst = obase + ((size_t)ti * x.Hq + (row - ti * x.G)) * 128;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              *reinterpret_cast<uint2*>(dst + (c4 + 4 * e) * 4) =
+                  make_uint2(pack_bf16x2(acc[4 * e] * out_scale, acc[4 * e + 1] * out_scale), pack_bf16x2(acc[4 * e + 2] * out_scale, acc[4 * e + 3] * out_scale));
+          }
+        }
+      }
+      all_sync();  // the staging tiles are the warps' own again
+    };
+
     XtCursor cur = first;
-    int g = 0;  // flat tile index: S buffer g & 1
-    while (cur.it < n_items) {
-      const bool live = warp * 32 < cur.rows;
+    int g0 = 0;  // flat index of the piece's first tile
+    while (cur.on) {
+      const bool live = wq * 32 < cur.rows;
       const int prefix = x.seqs.prefix[cur.s];
-      const int row_c = min(r, cur.rows - 1);  // (a lane without a query repeats the last row's visibility)
-      const int ti = cur.i0 + (int)((uint32_t)row_c * g_inv >> 16);
-      const int lim = cur.n + max(ti + 1, prefix);  // rows [0, lim) are visible
-      const int lim_min = __shfl_sync(0xffffffffu, lim, 0), lim_max = __shfl_sync(0xffffffffu, lim, 31);
-      // MODS: positions relative to the chunk's first token, two per lane, one tile ahead
+      const int ti = cur.i0 + min(ri, (cur.rows - 1) / x.G);  // (a lane without a query repeats the last token's visibility)
+      const int lim = cur.n + max(ti + 1, prefix);            // rows [0, lim) are visible
+      // Tiles that some token of the query tile does not see whole: all of them, and one more, are the first group's.
+      const int ramp = min(cur.nkt, max(0, cur.kt0 + cur.nkt - 1 - (cur.n + max(cur.i0 + 1, prefix) - 1) / kPfKeys) + 1);
       const int* pos_row = nullptr;
-      int tot = 0, pos_a = 0, pos_b = 0;
+      int tot = 0;
       float slope = 0.f;
       if constexpr (MODS) {
         const int b = x.seqs.b0 + cur.s, t = x.seqs.tok0[cur.s + 1] - x.seqs.tok0[cur.s];
         tot = x.tot[b] - (x.published ? t : 0);
         pos_row = x.pos + (size_t)slab_of(cur) * x.cap;
         if (x.slopes) slope = x.slopes[cur.h * x.G + rg] * 1.4426950408889634f;
-        pos_a = pos_row[min(cur.kt0 * kPfKeys + lane, x.cap - 1)] - tot;
-        pos_b = pos_row[min(cur.kt0 * kPfKeys + 32 + lane, x.cap - 1)] - tot;
       }
-      float m = -CUDART_INF_F, l = 0.f;
-      for (int j = 0; j < cur.nkt; ++j, ++g) {
-        const int key0 = (cur.kt0 + j) * kPfKeys;
-        uint32_t s_lo[32], s_hi[32];
-        uint32_t pk[32];  // the row's 64 weights as 16-bit pairs
-        bool move = false;
-        float alpha = 1.f;
+      float ref = -CUDART_INF_F, l = 0.f;
+
+      // One tile: S of flat tile g to P.  RAMP: part of it may be hidden, the reference may not be set yet.
+      auto tile = [&](auto is_ramp, int j) {
+        constexpr bool RAMP = decltype(is_ramp)::value;
+        const int g = g0 + j, key0 = (cur.kt0 + cur.nkt - 1 - j) * kPfKeys;
+        const uint32_t ts = tS0 + lane_base + 64u * (uint32_t)(g & 1);
+        int pos_a = 0, pos_b = 0;
+        if constexpr (MODS) {  // positions relative to the chunk's first token, two per lane
+          pos_a = pos_row[min(key0 + lane, x.cap - 1)] - tot;
+          pos_b = pos_row[min(key0 + 32 + lane, x.cap - 1)] - tot;
+        }
         mbar_wait(bar(5 + (g & 1)), (uint32_t)((g >> 1) & 1), s_abort, x.err, kPfSpinLimit);  // S of this tile is complete
         tc5::fence_after_sync();
         if (live) {
-          tc5::tmem_ld32(tS0 + lane_base + 64u * (uint32_t)(g & 1), s_lo);
-          tc5::tmem_ld32(tS0 + lane_base + 64u * (uint32_t)(g & 1) + 32u, s_hi);
           bool border = false;
-          const int* ipos = nullptr;
+          const int* ipos = reinterpret_cast<const int*>(stage);
+          const float* fpos = reinterpret_cast<const float*>(stage) + 64;
           if constexpr (MODS) {
-            ipos = reinterpret_cast<const int*>(stage);
-            float* fpos = reinterpret_cast<float*>(stage) + 64;
             __syncwarp();
             reinterpret_cast<int*>(stage)[lane] = pos_a;
             reinterpret_cast<int*>(stage)[32 + lane] = pos_b;
-            fpos[lane] = (float)pos_a;
-            fpos[32 + lane] = (float)pos_b;
+            reinterpret_cast<float*>(stage)[64 + lane] = (float)pos_a;
+            reinterpret_cast<float*>(stage)[96 + lane] = (float)pos_b;
             if (x.window > 0) {
-              // the first and last position of the tile against the warp's first and last token
-              const int p0 = __shfl_sync(0xffffffffu, pos_a, 0), p1 = __shfl_sync(0xffffffffu, pos_b, 31);
-              const int ta = __shfl_sync(0xffffffffu, ti, 0), tb = __shfl_sync(0xffffffffu, ti, 31);
-              border = key0 + kPfKeys > cur.n || (long long)tb - p0 >= x.window || (long long)p1 - ta >= x.window;
-            }
-            if (j + 1 < cur.nkt) {
-              pos_a = pos_row[min(key0 + kPfKeys + lane, x.cap - 1)] - tot;
-              pos_b = pos_row[min(key0 + kPfKeys + 32 + lane, x.cap - 1)] - tot;
+              // the tile's first position against the warp's last token (in tiles with rows of the chunk: always compared)
+              const int p0 = __shfl_sync(0xffffffffu, pos_a, 0), tb = __shfl_sync(0xffffffffu, ti, 31);
+              border = key0 + kPfKeys > cur.n || (long long)tb - p0 >= x.window;
             }
             __syncwarp();
           }
-          tc5::tmem_wait_ld();
+          // logits in base-2 units: scaled in the exponent's multiply-add, or (MODS) here
           float scale_log2 = p.scale_log2;
-          if constexpr (MODS) {
-            const float* fpos = reinterpret_cast<const float*>(stage) + 64;
-            const float fi = (float)ti;
-            auto modify = [&](uint32_t (&sv)[32], int hb) {
+          if constexpr (MODS) scale_log2 = 1.f;
+          auto modify = [&](uint32_t (&sv)[32], int hb) {
+            if constexpr (MODS) {
               if (x.cap_logit > 0.f) {  // c tanh(y) = c - 2 c / (1 + e^(2 y))
 #pragma unroll
                 for (int c = 0; c < 32; ++c)
@@ -650,13 +769,14 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
                 for (int c = 0; c < 32; ++c) sv[c] = __float_as_uint(__uint_as_float(sv[c]) * p.scale_log2);
               }
               if (x.slopes) {
+                const float fi = (float)ti;
 #pragma unroll
                 for (int c = 0; c < 32; c += 4) {
-                  const float4 f = *reinterpret_cast<const float4*>(fpos + hb + c);
-                  sv[c] = __float_as_uint(fmaf(-slope, fabsf(fi - f.x), __uint_as_float(sv[c])));
-                  sv[c + 1] = __float_as_uint(fmaf(-slope, fabsf(fi - f.y), __uint_as_float(sv[c + 1])));
-                  sv[c + 2] = __float_as_uint(fmaf(-slope, fabsf(fi - f.z), __uint_as_float(sv[c + 2])));
-                  sv[c + 3] = __float_as_uint(fmaf(-slope, fabsf(fi - f.w), __uint_as_float(sv[c + 3])));
+                  const float4 y = *reinterpret_cast<const float4*>(fpos + hb + c);
+                  sv[c] = __float_as_uint(fmaf(-slope, fabsf(fi - y.x), __uint_as_float(sv[c])));
+                  sv[c + 1] = __float_as_uint(fmaf(-slope, fabsf(fi - y.y), __uint_as_float(sv[c + 1])));
+                  sv[c + 2] = __float_as_uint(fmaf(-slope, fabsf(fi - y.z), __uint_as_float(sv[c + 2])));
+                  sv[c + 3] = __float_as_uint(fmaf(-slope, fabsf(fi - y.w), __uint_as_float(sv[c + 3])));
                 }
               }
               if (border) {
@@ -664,113 +784,85 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
                 for (int c = 0; c < 32; ++c)
                   if (abs(ti - ipos[hb + c]) >= x.window) sv[c] = 0xff800000u;
               }
-            };
-            modify(s_lo, 0);
-            modify(s_hi, 32);
-            scale_log2 = 1.f;
-          }
-          // The mask, per warp and half tile: a half is fully visible, hidden, or compared column by column.
-          const int cv = lim - key0, cv_min = lim_min - key0, cv_max = lim_max - key0;
-          const bool lo_live = cv_max > 0, hi_live = cv_max > 32;
-          if (cv_min < 32) {
-#pragma unroll
-            for (int c = 0; c < 32; ++c)
-              if (c >= cv) s_lo[c] = 0xff800000u;  // -inf
-          }
-          if (hi_live && cv_min < 64) {
-#pragma unroll
-            for (int c = 0; c < 32; ++c)
-              if (c + 32 >= cv) s_hi[c] = 0xff800000u;
-          }
-          auto max_half = [](const uint32_t (&sv)[32]) {  // four chains of three-input maxima
-            float mx4[4] = {-CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F};
-#pragma unroll
-            for (int c = 0; c < 32; c += 8) {
-#pragma unroll
-              for (int u = 0; u < 4; ++u) mx4[u] = tc5::f_max3(mx4[u], __uint_as_float(sv[c + u]), __uint_as_float(sv[c + 4 + u]));
             }
-            return tc5::f_max3(fmaxf(mx4[0], mx4[1]), mx4[2], mx4[3]);
+            if constexpr (RAMP) {
+              const int cv = lim - key0 - hb;  // visible columns of this half
+#pragma unroll
+              for (int c = 0; c < 32; ++c)
+                if (c >= cv) sv[c] = 0xff800000u;  // -inf
+            }
           };
-          float mxr = -CUDART_INF_F;
-          if (lo_live) mxr = max_half(s_lo);
-          if (hi_live) mxr = fmaxf(mxr, max_half(s_hi));
-          const float mx = mxr * scale_log2;
-          // the reference maximum moves only when it is exceeded by more than 2^8 (see prefill_attn.cuh); a row that
-          // has seen nothing yet keeps -inf and weighs with exp2(-inf - 0) = 0
-          move = mx > m + 8.0f && r < cur.rows;
-          const float m_new = move ? mx : m;
-          alpha = move ? fast_exp2(m - m_new) : 1.0f;
-          const float neg_m = m_new == -CUDART_INF_F ? 0.f : -m_new;
-          const uint64_t scale2 = tc5::f2_pack(scale_log2, scale_log2), negm2 = tc5::f2_pack(neg_m, neg_m);
-          auto exp_half = [scale2, negm2](const uint32_t (&sv)[32], uint32_t* out) {
+          auto weigh = [&](const uint32_t (&sv)[32], int hb) {  // 32 logits to 16 columns of P
+            const float neg = ref == -CUDART_INF_F ? 0.f : -ref;
+            const uint64_t scale2 = tc5::f2_pack(scale_log2, scale_log2), neg2 = tc5::f2_pack(neg, neg);
             uint64_t sum2[4] = {0ull, 0ull, 0ull, 0ull};  // four chains of (even, odd) column sums
+            uint32_t pk[16];
 #pragma unroll
             for (int c = 0; c < 16; ++c) {
               float x0, x1;
-              tc5::f2_unpack(tc5::f2_fma(tc5::f2_pack(__uint_as_float(sv[2 * c]), __uint_as_float(sv[2 * c + 1])), scale2, negm2), x0, x1);
+              tc5::f2_unpack(tc5::f2_fma(tc5::f2_pack(__uint_as_float(sv[2 * c]), __uint_as_float(sv[2 * c + 1])), scale2, neg2), x0, x1);
               const float a0 = fast_exp2(x0), a1 = fast_exp2(x1);
               sum2[c & 3] = tc5::f2_add(sum2[c & 3], tc5::f2_pack(a0, a1));
-              out[c] = KV8 ? pack_f16x2(a0, a1) : pack_bf16x2(a0, a1);
+              pk[c] = pack_bf16x2(a0, a1);
             }
+            tc5::tmem_st16(ts + (uint32_t)(hb / 2), pk);
             float e, o;
             tc5::f2_unpack(tc5::f2_add(tc5::f2_add(sum2[0], sum2[1]), tc5::f2_add(sum2[2], sum2[3])), e, o);
-            return e + o;
+            l += e + o;
           };
-          float sum = 0.f;
-          if (lo_live) {
-            sum = exp_half(s_lo, pk);
+          uint32_t lo[32], hi[32];
+          tc5::tmem_ld32(ts, lo);
+          tc5::tmem_wait_ld();
+          tc5::tmem_ld32(ts + 32u, hi);
+          if constexpr (RAMP) {
+            tc5::tmem_wait_ld();
+            modify(lo, 0);
+            modify(hi, 32);
+            float mx4[4] = {-CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F};
+#pragma unroll
+            for (int c = 0; c < 32; c += 4)
+#pragma unroll
+              for (int u = 0; u < 4; ++u) mx4[u] = tc5::f_max3(mx4[u], __uint_as_float(lo[c + u]), __uint_as_float(hi[c + u]));
+            const float mx = tc5::f_max3(fmaxf(mx4[0], mx4[1]), mx4[2], mx4[3]) * scale_log2;
+            if (ref == -CUDART_INF_F) ref = mx + kXtHeadroom;
+            weigh(lo, 0);
+            weigh(hi, 32);
           } else {
-#pragma unroll
-            for (int c = 0; c < 16; ++c) pk[c] = 0u;
+            modify(lo, 0);
+            weigh(lo, 0);
+            tc5::tmem_wait_ld();
+            modify(hi, 32);
+            weigh(hi, 32);
           }
-          if (hi_live) {
-            sum += exp_half(s_hi, pk + 16);
-          } else {
-#pragma unroll
-            for (int c = 0; c < 16; ++c) pk[16 + c] = 0u;
-          }
-          l = l * alpha + sum;
-          m = m_new;
-          if (j > 0 && __any_sync(0xffffffffu, move)) {
-            // O += P V of the tile before must be complete before O is rescaled (see prefill_attn.cuh)
-            mbar_wait(bar(7), (uint32_t)((g - 1) & 1), s_abort, x.err, kPfSpinLimit);
-            tc5::fence_after_sync();
-#pragma unroll
-            for (int c0 = 0; c0 < 128; c0 += 32) {
-              uint32_t o[32];
-              tc5::tmem_ld32(tO + lane_base + (uint32_t)c0, o);
-              tc5::tmem_wait_ld();
-#pragma unroll
-              for (int c = 0; c < 32; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * alpha);
-              tc5::tmem_st32(tO + lane_base + (uint32_t)c0, o);
-            }
-          }
-        }
-        // The epilogue of the item before runs here, while its last O += P V completes; the first O = P V of
-        // this item cannot be issued before the P stored below.
-        if (ep_on) {
-          xt_epilogue<KV8>(p, ep_c, ep_m, ep_l, tO, bar(12), s_abort, s_out);
-          ep_on = false;
-        }
-        if (live) {
-          tc5::tmem_st32(tS0 + lane_base + 64u * (uint32_t)(g & 1), pk);
           tc5::tmem_wait_st();
         }
         tc5::fence_before_sync();
         mbar_arrive(bar(8 + (g & 1)));
+      };
+      if (wg == 0) {
+        for (int j = 0; j < ramp; ++j) tile(std::true_type{}, j);
+        reinterpret_cast<float*>(stage)[256 + lane] = ref;
+        pair_sync();
+        for (int j = ramp + 1; j < cur.nkt; j += 2) tile(std::false_type{}, j);
+      } else {
+        pair_sync();
+        ref = reinterpret_cast<const float*>(stage_other)[256 + lane];
+        for (int j = ramp; j < cur.nkt; j += 2) tile(std::false_type{}, j);
       }
-      ep_on = true;
-      ep_c = cur;
-      ep_m = m;
-      ep_l = l;
-      ++cur.ord;
-      xt_seek(cur, cur.it + 1, n_items, p, s_n);
+      g0 += cur.nkt;
+      // the other group's share of the row's sum
+      reinterpret_cast<float*>(stage)[288 + lane] = l;
+      pair_sync();
+      const float l_other = reinterpret_cast<const float*>(stage_other)[288 + lane];
+      l = wg == 0 ? l + l_other : l_other + l;
+      pair_sync();
+      epilogue(cur, ref, l);
+      xt_next_item(cur, p, s_n);
     }
-    if (ep_on) xt_epilogue<KV8>(p, ep_c, ep_m, ep_l, tO, bar(12), s_abort, s_out);
   }
   tc5::fence_before_sync();
   __syncthreads();
-  if (warp == 5) tc5::tmem_dealloc(tmem, kPfTmemCols);
+  if (warp == 10) tc5::tmem_dealloc(tmem, kPfTmemCols);
 }
 
 // extend_mass_tc_kernel: mass_j = sum over the chunk's tokens i and the group's heads of exp2(x_ij - lse_i).
@@ -779,6 +871,7 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
 // exactly one thread writes a row.  A work item = 128 rows of one slab against all query rows that see any of them;
 // persistent CTAs, two per SM.  K tiles (two stages, the next item's asked for when the item begins) and Q tiles (two
 // stages of 64 rows) by TMA, S in two buffers of 64 columns.  Bound by the exponentials like the attention itself.
+constexpr int kXmThreads = 256;
 constexpr int kXmKeys = 128;
 constexpr int kXmRows = 64;                       // query rows per step
 constexpr int kXmKBytes = kXmKeys * 256;
@@ -824,7 +917,7 @@ __device__ __forceinline__ void xm_seek(XmCursor& c, int it, int n_items, const 
 }
 
 template <bool KV8, bool MODS>
-__global__ void __launch_bounds__(kXtThreads, 2)
+__global__ void __launch_bounds__(kXmThreads, 2)
 extend_mass_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK) {
   extern __shared__ __align__(1024) uint8_t pf_smem[];
   uint8_t* sm = pf_smem;
@@ -863,7 +956,7 @@ extend_mass_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_con
   // are zero from here on, and their log-sum-exp is +inf, so that they weigh nothing.
   {
     const int pad = kXmRows - tps * x.G;
-    for (int i = tid; i < 4 * pad * 8; i += kXtThreads) {
+    for (int i = tid; i < 4 * pad * 8; i += kXmThreads) {
       const int chunk = i & 7, r = tps * x.G + (i >> 3) % pad, half_stage = (i >> 3) / pad;
       *reinterpret_cast<uint4*>(sm + 2 * kXmKBytes + half_stage * (kXmQBytes / 2) + r * 128 + chunk * 16) = make_uint4(0u, 0u, 0u, 0u);
     }
@@ -997,17 +1090,20 @@ extend_mass_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_con
       XmCursor cK;
       cK.ord = 0;
       xm_seek(cK, 0, n_items, p, sh, true);
-      XtCodes codes;
+      XtCodes codes[4];
       const int sub = 64 * (warp - 6);
       auto fetch = [&]() {
-        xt_load_codes(codes, static_cast<const uint8_t*>(x.K) + (size_t)slab_of(cK) * x.cap * 128, cK.k0 + sub, cK.n + cK.t, lane);
+        const uint8_t* src = static_cast<const uint8_t*>(x.K) + (size_t)slab_of(cK) * x.cap * 128;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) xt_load_codes(codes[q], src, cK.k0 + sub + 16 * q, cK.n + cK.t, lane);
       };
       if (cK.it < n_items) fetch();
       while (cK.it < n_items && !*s_abort) {
         if (cK.ord >= 2) mbar_wait(bar(8 + (cK.ord & 1)), (uint32_t)(((cK.ord - 2) >> 1) & 1), s_abort, x.err, kPfSpinLimit);
         __syncwarp();
         if (*s_abort) break;
-        xt_store_codes(codes, sm + (size_t)(cK.ord & 1) * kXmKBytes + sub * 128, kXmKBytes / 2, lane);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) xt_store_codes<false>(codes[q], sm + (size_t)(cK.ord & 1) * kXmKBytes, kXmKBytes / 2, sub + 16 * q, lane);
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
         if (lane == 0) mbar_arrive(bar(cK.ord & 1));

@@ -341,15 +341,24 @@ def test_captured_chunks_follow_the_lengths():
             run(a, out)
     a.set_stream(torch.cuda.current_stream())
     a.refresh_lengths()
+    # A capture keeps the cut of the key rows that its lengths suggested, an eager call cuts by the present ones, so the
+    # two may round differently: each rounds its weights (half a step of bf16, 2^-8, of at most max |v| in all: the weights
+    # sum to one) and its output (the same), so they are at most 4 * 2^-8 * max |v| apart.
+    vmax = max(float(a.export_slab(0, s, h)[1].float().abs().max()) for s in range(2) for h in range(2))
+    vmax = max(vmax, float(v.float().abs().max()))
     for step in range(70):                                         # across a tile's border
         g.replay()
         run(b, ref)
         torch.cuda.synchronize()
-        assert torch.equal(out, ref), step
+        assert ((out - ref).float().abs() <= 4 * 2.0 ** -8 * vmax).all(), step
     a.refresh_lengths()
     assert a.len(0) == b.len(0) == 131
     for h in range(2):
-        assert all(torch.equal(x, y) for x, y in zip(a.export_slab(0, 0, h), b.export_slab(0, 0, h)))
+        x, y = a.export_slab(0, 0, h), b.export_slab(0, 0, h)
+        assert all(torch.equal(x[i], y[i]) for i in range(3))
+        # each weight within 2 dz + 132 * 2^-23 of its value on either side, dz = (d + 8) 2^-23 sum |q||k| / sqrt(d) with
+        # sum |q||k| < 128 (normal values): 2 * 1.9e-4 + 1.6e-5 < 4e-4, so the sums are within 8e-4 of each other
+        assert ((x[3] - y[3]).abs() <= 8e-4 * y[3]).all()
     a.poll_error()
     a.close(), b.close()
 
