@@ -26,9 +26,10 @@
 // Warps: 0-3 and 4-7 the two groups, 8 loads Q and K, 9 loads V, 10 issues S, 11 issues O; they meet through mbarriers as
 // in the prompt attention (prefill_attn.cuh), the S buffer, stages and phases follow the flat tile index g.
 //
-// Rows of 16 bits arrive by TMA from the slabs.  8-bit rows (KV8) are read as codes by the two loading warps and
-// widened -- K to f16 (exact; queries are an f16 copy made by the storing kernel), V to bf16 (exact) -- into the same
-// swizzled tiles; the codes of coming tiles are asked into L2 meanwhile.
+// Rows of 16 bits arrive by TMA from the slabs.  8-bit rows (KV8) are read as codes and widened into the same swizzled
+// tiles: K to f16 (exact; queries are an f16 copy made by the storing kernel) by the two loading warps, a tile ahead in
+// registers; V to bf16 (exact; f16 weights would have no room for the fixed reference) by the group that weighs the
+// tile, while it waits for S.  The codes of coming tiles are asked into L2 meanwhile.
 //
 // A weight of zero times a value that is not finite is not a number, and the MMA multiplies whole
 // tiles: rows behind the chunk's end are zero (the storing kernel clears them, KV8 writes zeros), and an
@@ -46,11 +47,14 @@ namespace dynts {
 
 constexpr int kXtThreads = 384;
 constexpr int kXtRows = 128;
-constexpr int kXtMaxCtas = 512;      // CTAs of a launch (two per SM)
+constexpr int kXtMaxCtas = 380;      // CTAs of a launch (two per SM); the list of an item's parts has room for so many
 constexpr int kXtPartFloats = 129;   // per query row of a part: 128 outputs, log-sum-exp
 constexpr float kXtHeadroom = 40.f;  // the reference lies so far (base-2 units) above the first tiles' maximum
 constexpr float kXtSumMax = 1.2676506e30f;  // 2^100: a row whose sum of weights exceeds it is computed again
-constexpr int kXtSmemBytes = kPfQBytes + 4 * kPfKvBytes + kPfOutStageBytes + 128 + kExtSeqs * 4;
+constexpr int kXtStageBytes = 1024;  // per softmax warp
+constexpr int kXtCursors = 12;       // a cursor per warp
+constexpr int kXtCursorInts = 14;
+constexpr int kXtSmemBytes = kPfQBytes + 4 * kPfKvBytes + 8 * kXtStageBytes + 128 + kExtSeqs * 4 + kXtCursors * kXtCursorInts * 4 + (2 + kXtMaxCtas) * 4;
 
 // The list of key tiles is kept in shares: an item of sequence s counts per[s] shares whatever its exact number of
 // key tiles (which the kernel takes from the lengths on the device), a share's border inside an item is the same
@@ -71,29 +75,38 @@ struct ExtendTcParams {
   float cap_arg;        // 2 log2(e) * scale / c
 };
 
+// A piece of the list: what a CTA does of an item.  Every warp walks the pieces for itself; its cursor lies in shared
+// memory, since registers are what the kernel has least of.
 struct XtCursor {
-  bool on;
+  int on;
   int s, idx;             // sequence of the launch, item within it: (layer, KV head) slowest, tiles of query rows fastest
   int ord;                // pieces of this CTA before this one
-  int j, nkt, kt0;        // tile within the piece (from its newest to its oldest), its tiles, its first key tile
+  int nkt, kt0;           // key tiles of the piece (walked from the newest to the oldest), its first
   int layer, h, n;        // rows held
   int i0, rows;           // first token of the chunk, query rows
-  int b0, total;          // the item's first key tile, its key tiles
+  int total;              // key tiles of the item
+  int end;                // rows of the sequence, the chunk's included
+  int slab;
 };
+static_assert(sizeof(XtCursor) == kXtCursorInts * 4, "cursor size");
 
 __device__ __forceinline__ unsigned xt_share0(const ExtendTcParams& p, unsigned cta) { return cta * p.share_q + min(cta, p.share_rem); }
+// total * a / per, in 32 bits where that is enough (a 64-bit division takes several hundred cycles)
+__device__ __forceinline__ int xt_part(unsigned total, unsigned a, unsigned per) {
+  return (int)((total | a) < 65536u ? total * a / per : (unsigned)((unsigned long long)total * a / per));
+}
 // Key tiles [lo, hi) of an item (total key tiles, shares [start, start + per)) that fall to the shares [v0, v1).
 __device__ __forceinline__ void xt_piece(unsigned v0, unsigned v1, unsigned start, unsigned per, int total, int& lo, int& hi) {
   const unsigned a = v0 > start ? v0 - start : 0u, e = v1 - start < per ? v1 - start : per;
-  lo = a == 0u ? 0 : (int)((unsigned long long)(unsigned)total * a / per);
-  hi = e == per ? total : (int)((unsigned long long)(unsigned)total * e / per);
+  lo = a == 0u ? 0 : xt_part((unsigned)total, a, per);
+  hi = e == per ? total : xt_part((unsigned)total, e, per);
 }
 
-// The first piece of this CTA at or behind item c.idx of sequence c.s that holds any key tile.
-__device__ __forceinline__ void xt_settle(XtCursor& c, const ExtendTcParams& p, const int* s_n) {
+// The first piece of this CTA at or behind item c.idx of sequence c.s that holds any key tile.  The whole warp.
+__device__ __noinline__ void xt_settle(XtCursor* at, const ExtendTcParams& p, const int* s_n) {
+  XtCursor c = *at;
   const unsigned v0 = xt_share0(p, blockIdx.x), v1 = xt_share0(p, blockIdx.x + 1u);
-  c.j = 0;
-  c.on = false;
+  c.on = 0;
   while (c.s < p.x.seqs.n) {
     const int nq = p.tiles[c.s];
     c.n = s_n[c.s];
@@ -103,33 +116,38 @@ __device__ __forceinline__ void xt_settle(XtCursor& c, const ExtendTcParams& p, 
       continue;
     }
     const unsigned per = p.per[c.s], start = p.cum[c.s] + (unsigned)c.idx * per;
-    if (start >= v1) return;
-    const int lh = c.idx / nq, o = c.idx - lh * nq;
+    if (start >= v1) break;
+    const int lh = nq == 1 ? c.idx : c.idx / nq, o = c.idx - lh * nq;
     // tiles from both ends in turn: neighbours in the list hold about as many key tiles together as any other two
     const int qt = (o & 1) ? nq - 1 - (o >> 1) : o >> 1;
     const int t = p.x.seqs.tok0[c.s + 1] - p.x.seqs.tok0[c.s];
     c.i0 = qt * p.tokens_per_tile;
     const int i1 = min(t, c.i0 + p.tokens_per_tile);
-    c.rows = (i1 - c.i0) * p.x.G;
-    const int end = c.n + max(i1, p.x.seqs.prefix[c.s]);
+    const int seen = c.n + max(i1, p.x.seqs.prefix[c.s]);
     // (positions ascend with the rows, so a row more than `window` rows back is more than `window` positions back)
-    c.b0 = p.x.window > 0 ? max(0, c.n + c.i0 - p.x.window + 1) / kPfKeys : 0;
-    c.total = (end + kPfKeys - 1) / kPfKeys - c.b0;
+    const int b0 = p.x.window > 0 ? max(0, c.n + c.i0 - p.x.window + 1) / kPfKeys : 0;
+    c.total = (seen + kPfKeys - 1) / kPfKeys - b0;
     int lo, hi;
     xt_piece(v0, v1, start, per, c.total, lo, hi);
     if (lo < hi) {
-      c.kt0 = c.b0 + lo;
+      c.rows = (i1 - c.i0) * p.x.G;
+      c.kt0 = b0 + lo;
       c.nkt = hi - lo;
-      c.layer = lh / p.x.Hkv;
+      c.layer = p.x.n_layers == 1 ? 0 : lh / p.x.Hkv;
       c.h = lh - c.layer * p.x.Hkv;
-      c.on = true;
-      return;
+      c.end = c.n + t;
+      c.slab = ((p.x.layer0 + c.layer) * p.x.Nb + p.x.seqs.b0 + c.s) * p.x.Hkv + c.h;
+      c.on = 1;
+      break;
     }
     ++c.idx;
   }
+  __syncwarp();
+  if ((threadIdx.x & 31) == 0) *at = c;
+  __syncwarp();
 }
-// Where this CTA's shares begin (needs no lengths), then its first piece.
-__device__ __forceinline__ void xt_begin(XtCursor& c, const ExtendTcParams& p) {
+// Where this CTA's shares begin (needs no lengths); xt_settle then finds its first piece.
+__device__ __forceinline__ void xt_begin(XtCursor* at, const ExtendTcParams& p) {
   const unsigned v0 = xt_share0(p, blockIdx.x);
   int lo = 0, hi = p.x.seqs.n;
   while (hi - lo > 1) {  // the last sequence that begins at or before the first share
@@ -137,17 +155,21 @@ __device__ __forceinline__ void xt_begin(XtCursor& c, const ExtendTcParams& p) {
     if (p.cum[mid] <= v0) lo = mid;
     else hi = mid;
   }
-  c.s = lo;
-  c.idx = (int)((v0 - p.cum[lo]) / p.per[lo]);
-  c.ord = 0;
+  if ((threadIdx.x & 31) == 0) {
+    at->s = lo;
+    at->idx = (int)((v0 - p.cum[lo]) / p.per[lo]);
+    at->ord = 0;
+  }
+  __syncwarp();
 }
-__device__ __forceinline__ void xt_next_item(XtCursor& c, const ExtendTcParams& p, const int* s_n) {
-  ++c.ord;
-  ++c.idx;
-  xt_settle(c, p, s_n);
-}
-__device__ __forceinline__ void xt_advance(XtCursor& c, const ExtendTcParams& p, const int* s_n) {
-  if (++c.j == c.nkt) xt_next_item(c, p, s_n);
+__device__ __forceinline__ void xt_next(XtCursor* at, const ExtendTcParams& p, const int* s_n) {
+  __syncwarp();
+  if ((threadIdx.x & 31) == 0) {
+    ++at->ord;
+    ++at->idx;
+  }
+  __syncwarp();
+  xt_settle(at, p, s_n);
 }
 
 __device__ __forceinline__ float rcp_approx(float x) {
@@ -160,22 +182,20 @@ __device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
   return *reinterpret_cast<const uint32_t*>(&v);
 }
 
-// Codes to operand tiles.  A loading warp takes 64 rows of 128 codes in four quarters of 16 rows; a lane holds four pieces
-// of 16 codes (rows 4 i + lane / 8, piece lane % 8).  The tile is [2 halves of head_dim][rows][128 B], 16-byte
-// chunks swizzled by row; the lanes of the second half write their two chunks in the other order, so that a
-// store's eight lanes meet eight banks.
+// Codes to operand tiles [2 halves of head_dim][rows][128 B], 16-byte chunks swizzled by row.  A warp takes groups of 8
+// rows; a lane holds 16 codes of either half of row lane / 4, quarter lane % 4.  (A store's eight lanes then are two
+// neighbouring rows and meet eight different banks; a load's 64 bytes of a row are whole sectors.)
 struct XtCodes {
-  uint4 c[4];
+  uint4 c[2];
 };
 __device__ __forceinline__ void xt_load_codes(XtCodes& r, const uint8_t* base, int row0, int end, int lane) {
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int row = row0 + 4 * i + (lane >> 3);
-    r.c[i] = row < end ? ldg_stream(base + (size_t)row * 128 + (lane & 7) * 16) : make_uint4(0u, 0u, 0u, 0u);
-  }
+  const int row = row0 + (lane >> 2);
+  const uint8_t* src = base + (size_t)row * 128 + (lane & 3) * 16;
+  r.c[0] = row < end ? ldg_stream(src) : make_uint4(0u, 0u, 0u, 0u);
+  r.c[1] = row < end ? ldg_stream(src + 64) : make_uint4(0u, 0u, 0u, 0u);
 }
-// Two codes in the low half of w (the other two: the high half) as a bf16 pair: the code's exponent and mantissa bits
-// in bf16's place are the value times 2^-120, subnormals included, and the product with 2^120 is exact.
+// Two codes of w (bytes by `sel`) as a bf16 pair: the code's exponent and mantissa bits in bf16's place are the value
+// times 2^-120, subnormals included, and the product with 2^120 is exact.
 __device__ __forceinline__ uint32_t e4m3x2_to_bf16x2(uint32_t w, uint32_t sel) {
   const uint32_t t = __byte_perm(w, 0u, sel);  // code << 8 in each half
   const uint32_t u = (t & 0x80008000u) | ((t >> 4) & 0x07f007f0u);
@@ -185,23 +205,21 @@ __device__ __forceinline__ uint32_t e4m3x2_to_bf16x2(uint32_t w, uint32_t sel) {
 }
 template <bool BF16>
 __device__ __forceinline__ void xt_store_codes(const XtCodes& r, uint8_t* tile, int half_bytes, int row0, int lane) {
-  const int piece = lane & 7, half = piece >> 2;
+  const int row = row0 + (lane >> 2), c0 = 2 * (lane & 3);
+  uint8_t* dst = tile + row * 128;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int row = row0 + 4 * i + (lane >> 3);
-    uint8_t* dst = tile + half * half_bytes + row * 128;
-    const uint32_t w[4] = {r.c[i].x, r.c[i].y, r.c[i].z, r.c[i].w};
-    uint4 y[2];
-    uint32_t* o = reinterpret_cast<uint32_t*>(y);
+  for (int half = 0; half < 2; ++half) {
+    const uint32_t w[4] = {r.c[half].x, r.c[half].y, r.c[half].z, r.c[half].w};
+    uint32_t o[8];
     if constexpr (BF16) {
       uint32_t nan = 0u;
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
         o[2 * u] = e4m3x2_to_bf16x2(w[u], 0x1404u);
         o[2 * u + 1] = e4m3x2_to_bf16x2(w[u], 0x3424u);
-        nan |= __vcmpeq4(w[u] & 0x7f7f7f7fu, 0x7f7f7f7fu);
+        nan |= (w[u] & 0x7f7f7f7fu) + 0x01010101u;
       }
-      if (nan) {  // a code that is not a number
+      if (nan & 0x80808080u) {  // a code that is not a number
 #pragma unroll
         for (int u = 0; u < 8; ++u) {
           const uint32_t two = (w[u >> 1] >> (16 * (u & 1))) & 0x7f7fu;
@@ -216,11 +234,8 @@ __device__ __forceinline__ void xt_store_codes(const XtCodes& r, uint8_t* tile, 
         o[2 * u + 1] = e4m3x2_to_half2((unsigned short)(w[u] >> 16));
       }
     }
-    const int c0 = 2 * (piece & 3);
-    const uint4 a = half ? y[1] : y[0], b = half ? y[0] : y[1];
-    const int ca = c0 + half, cb = c0 + 1 - half;
-    *reinterpret_cast<uint4*>(dst + ((ca ^ (row & 7)) << 4)) = a;
-    *reinterpret_cast<uint4*>(dst + ((cb ^ (row & 7)) << 4)) = b;
+    *reinterpret_cast<uint4*>(dst + half * half_bytes + ((c0 ^ (row & 7)) << 4)) = make_uint4(o[0], o[1], o[2], o[3]);
+    *reinterpret_cast<uint4*>(dst + half * half_bytes + (((c0 + 1) ^ (row & 7)) << 4)) = make_uint4(o[4], o[5], o[6], o[7]);
   }
 }
 
@@ -290,20 +305,22 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
   const uint32_t sQ = smem_u32(sm);                       // [2 halves of head_dim][128 rows][128 B]
   const uint32_t sK = sQ + kPfQBytes;                     // [2 stages][2 halves][64 rows][128 B]
   const uint32_t sV = sK + 2 * kPfKvBytes;                // the same
-  uint8_t* s_out = sm + kPfQBytes + 4 * kPfKvBytes;       // [8 softmax warps][2 KB]
-  uint64_t* bars = reinterpret_cast<uint64_t*>(s_out + kPfOutStageBytes);
+  uint8_t* s_out = sm + kPfQBytes + 4 * kPfKvBytes;       // [8 softmax warps][1 KB]
+  uint64_t* bars = reinterpret_cast<uint64_t*>(s_out + 8 * kXtStageBytes);
   // barriers: 0 Q, 1-2 K stages filled, 3-4 V stages filled, 5-6 S buffers complete, 7 O has been read, 8-9 P written (per S
   // buffer), 10-11 V stages and P read, 12 the piece's last O += P V complete, 13-14 drain
   const uint32_t bar0 = smem_u32(bars);
   auto bar = [&](int i) { return bar0 + 8u * (uint32_t)i; };
   uint32_t* s_tmem = reinterpret_cast<uint32_t*>(bars + 15);
   volatile int* s_abort = reinterpret_cast<volatile int*>(s_tmem + 1);
-  int* s_n = reinterpret_cast<int*>(s_out + kPfOutStageBytes + 128);  // rows held by each sequence, -1: the chunk has no room
+  int* s_n = reinterpret_cast<int*>(s_out + 8 * kXtStageBytes + 128);  // rows held by each sequence, -1: the chunk has no room
+  XtCursor* s_cur = reinterpret_cast<XtCursor*>(s_n + kExtSeqs);
+  int* s_list = reinterpret_cast<int*>(s_cur + kXtCursors);  // an item's parts: [0] the others are done, [1] parts, [2 ...] their places
   const ExtendParams& x = p.x;
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (tid == 0) {
-    for (int i = 0; i < 15; ++i) mbar_init(bar(i), i == 7 ? 2 * kXtRows : (i == 8 || i == 9) ? kXtRows : 1);
+    for (int i = 0; i < 15; ++i) mbar_init(bar(i), i == 7 ? 2 * kXtRows : (i == 8 || i == 9) ? kXtRows : KV8 && (i == 1 || i == 2) ? 2 : 1);
     *s_abort = 0;
     if ((smem_u32(sm) & 1023u) != 0u) {
       atomicOr(x.err, kErrStreamBounds);
@@ -323,8 +340,8 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
       asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&tmV)) : "memory");
     }
   }
-  XtCursor first;
-  xt_begin(first, p);
+  XtCursor* const cur = s_cur + warp;
+  xt_begin(cur, p);
   // The storing kernel may still be running; everything below waits until it has completed.
   asm volatile("griddepcontrol.wait;" ::: "memory");
   for (int s = tid; s < x.seqs.n; s += kXtThreads) {
@@ -336,159 +353,102 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
   tc5::fence_after_sync();
   const uint32_t tmem = *s_tmem;
   const uint32_t tS0 = tmem, tO = tmem + 128;  // S buffer b at column 64 b
-  xt_settle(first, p, s_n);
-  auto slab_of = [&](const XtCursor& c) { return ((x.layer0 + c.layer) * x.Nb + x.seqs.b0 + c.s) * x.Hkv + c.h; };
-  auto key0_of = [&](const XtCursor& c) { return (c.kt0 + c.nkt - 1 - c.j) * kPfKeys; };
-  auto load_tile = [&](const CUtensorMap* tm, uint32_t base, int bar_i, const XtCursor& c, int g) {
-    const uint32_t dst = base + (uint32_t)(g & 1) * kPfKvBytes, bb = bar(bar_i + (g & 1));
-    const int row = key0_of(c), slab = slab_of(c);
-    mbar_arrive_expect_tx(bb, kPfKvBytes);
-    pf_tma_load(dst, tm, 0, row, slab, bb);
-    pf_tma_load(dst + kPfKvBytes / 2, tm, 64, row, slab, bb);
-  };
-  // 8-bit rows: a loading warp fills a stage itself, two quarters of the tile ahead in registers
-  XtCodes qa, qb;
-  auto codes_of = [&](const void* base, const XtCursor& c) { return static_cast<const uint8_t*>(base) + (size_t)slab_of(c) * x.cap * 128; };
-  auto ends_of = [&](const XtCursor& c) { return c.n + x.seqs.tok0[c.s + 1] - x.seqs.tok0[c.s]; };
-  auto begin_codes = [&](const void* base, const XtCursor& c) {
-    const uint8_t* src = codes_of(base, c);
-    const int k0 = key0_of(c), end = ends_of(c);
-    xt_load_codes(qa, src, k0, end, lane);
-    xt_load_codes(qb, src, k0 + 16, end, lane);
-  };
-  // fills the stage of tile g with the tile of c and leaves c (and the registers) at the next tile
-  auto fill_stage = [&](auto bf16, const void* base, uint32_t off, int bar_i, XtCursor& c, int g) {
-    constexpr bool BF16 = decltype(bf16)::value;
-    uint8_t* tile = sm + off + (uint32_t)(g & 1) * kPfKvBytes;
-    const uint8_t* src = codes_of(base, c);
-    const int k0 = key0_of(c), end = ends_of(c);
-    // (the tile four further on towards the older rows: asked into L2 now)
-    if (lane == 0 && c.j + 4 < c.nkt)
-      asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(src + (size_t)(k0 - 4 * kPfKeys) * 128), "r"(kPfKeys * 128) : "memory");
-    xt_store_codes<BF16>(qa, tile, kPfKvBytes / 2, 0, lane);
-    xt_load_codes(qa, src, k0 + 32, end, lane);
-    xt_store_codes<BF16>(qb, tile, kPfKvBytes / 2, 16, lane);
-    xt_load_codes(qb, src, k0 + 48, end, lane);
-    xt_advance(c, p, s_n);
-    xt_store_codes<BF16>(qa, tile, kPfKvBytes / 2, 32, lane);
-    if (c.on) xt_load_codes(qa, codes_of(base, c), key0_of(c), ends_of(c), lane);
-    xt_store_codes<BF16>(qb, tile, kPfKvBytes / 2, 48, lane);
-    if (c.on) xt_load_codes(qb, codes_of(base, c), key0_of(c) + 16, ends_of(c), lane);
-    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-    __syncwarp();
-    if (lane == 0) mbar_arrive(bar(bar_i + (g & 1)));
-    __syncwarp();
-  };
-
-  if (warp == 8) {
-    // ================= the warp that loads Q and K =================
+  xt_settle(cur, p, s_n);
+  if (warp == 8 || warp == 9) {
+    // ================= the warps that load: 8 Q and K, 9 V (8-bit rows: 8 Q and half of K, 9 the other half) =================
     if (lane == 0 && *reinterpret_cast<volatile int*>(p.stop) != 0) *s_abort = 1;
     __syncwarp();
-    const uint32_t q_bytes = 256u * (uint32_t)(x.G * p.tokens_per_tile);
-    auto load_q = [&](const XtCursor& c) {
-      const int tok = c.layer * x.total + x.seqs.tok0[c.s] + c.i0;
-      mbar_arrive_expect_tx(bar(0), q_bytes);
-      pf_tma_load(sQ, &tmQ, 0, c.h * x.G, tok, bar(0));
-      pf_tma_load(sQ + kPfQBytes / 2, &tmQ, 64, c.h * x.G, tok, bar(0));
+    const bool is_k = KV8 || warp == 8;
+    // a stage is filled again when the product that read it has completed: S of tile g - 2 (K), O += P V of it (V)
+    const int freed = is_k ? 5 : 10, filled = is_k ? 1 : 3;
+    const uint32_t base = is_k ? sK : sV;
+    XtCodes codes[4];
+    auto fetch = [&](int j) {  // 8-bit rows: this warp's 32 rows of the piece's tile j
+      const uint8_t* src = static_cast<const uint8_t*>(x.K) + (size_t)cur->slab * x.cap * 128;
+      const int k0 = (cur->kt0 + cur->nkt - 1 - j) * kPfKeys + 32 * (warp & 1), end = cur->end;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) xt_load_codes(codes[i], src, k0 + 8 * i, end, lane);
+      // (four tiles further on towards the older rows: asked into L2)
+      if (lane == 0 && j + 4 < cur->nkt)
+        asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(src + (size_t)(k0 - 4 * kPfKeys) * 128), "r"(32 * 128) : "memory");
     };
-    if (first.on && !*s_abort) {
-      if (tc5::elect_one()) load_q(first);
-      __syncwarp();
-      XtCursor cur = first, cK = first;
-      auto fill_k = [&](int g) {
+    int g = 0;
+    while (cur->on && !*s_abort) {
+      const int nkt = cur->nkt;
+      if constexpr (KV8) fetch(0);
+      for (int j = 0; j < nkt; ++j, ++g) {
+        if (g >= 2) mbar_wait(bar(freed + (g & 1)), (uint32_t)(((g - 2) >> 1) & 1), s_abort, x.err, kPfSpinLimit);
+        __syncwarp();
+        if (*s_abort) break;
+        const uint32_t bb = bar(filled + (g & 1));
         if constexpr (KV8) {
-          fill_stage(std::false_type{}, x.K, kPfQBytes, 1, cK, g);
-        } else {
-          if (tc5::elect_one()) load_tile(&tmK, sK, 1, cK, g);
+          uint8_t* tile = sm + kPfQBytes + (uint32_t)(g & 1) * kPfKvBytes;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) xt_store_codes<false>(codes[i], tile, kPfKvBytes / 2, 32 * (warp & 1) + 8 * i, lane);
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           __syncwarp();
-          xt_advance(cK, p, s_n);
+          if (lane == 0) mbar_arrive(bb);
+          if (j + 1 < nkt) fetch(j + 1);
+        } else if (tc5::elect_one()) {
+          const uint32_t dst = base + (uint32_t)(g & 1) * kPfKvBytes;
+          const CUtensorMap* tm = is_k ? &tmK : &tmV;
+          const int row = (cur->kt0 + nkt - 1 - j) * kPfKeys;
+          mbar_arrive_expect_tx(bb, kPfKvBytes);
+          pf_tma_load(dst, tm, 0, row, cur->slab, bb);
+          pf_tma_load(dst + kPfKvBytes / 2, tm, 64, row, cur->slab, bb);
         }
-      };
-      if constexpr (KV8) begin_codes(x.K, cK);
-      for (int g = 0; g < 2 && cK.on; ++g) fill_k(g);
-      XtCursor nq = first;  // the piece after the current one
-      xt_next_item(nq, p, s_n);
-      for (int g = 0; cur.on && !*s_abort; ++g) {
-        const bool next_q = cur.j == cur.nkt - 1 && nq.on;
-        if (cur.j == 0 && nq.on && tc5::elect_one()) {
-          const int tok = nq.layer * x.total + x.seqs.tok0[nq.s] + nq.i0;
-          pf_tma_prefetch(&tmQ, 0, nq.h * x.G, tok);
-          pf_tma_prefetch(&tmQ, 64, nq.h * x.G, tok);
-        }
-        if (cK.on || next_q) {
-          mbar_wait(bar(5 + (g & 1)), (uint32_t)((g >> 1) & 1), s_abort, x.err, kPfSpinLimit);
+        __syncwarp();
+        if (warp == 8 && j == 0) {
+          // the piece's Q, once the last S of the piece before has been computed from its own
+          if (g >= 1) mbar_wait(bar(5 + ((g - 1) & 1)), (uint32_t)(((g - 1) >> 1) & 1), s_abort, x.err, kPfSpinLimit);
           __syncwarp();
-          if (*s_abort) break;
-          if (next_q && tc5::elect_one()) load_q(nq);
+          if (!*s_abort && tc5::elect_one()) {
+            const int tok = cur->layer * x.total + x.seqs.tok0[cur->s] + cur->i0, head = cur->h * x.G;
+            mbar_arrive_expect_tx(bar(0), 256u * (uint32_t)(x.G * p.tokens_per_tile));
+            pf_tma_load(sQ, &tmQ, 0, head, tok, bar(0));
+            pf_tma_load(sQ + kPfQBytes / 2, &tmQ, 64, head, tok, bar(0));
+          }
           __syncwarp();
-          if (cK.on) fill_k(g);  // tile g + 2: the stage S_g read
-        }
-        if (cur.j == cur.nkt - 1) {
-          cur = nq;
-          if (nq.on) xt_next_item(nq, p, s_n);
-        } else {
-          ++cur.j;
         }
       }
+      xt_next(cur, p, s_n);
     }
     if (*s_abort && lane == 0) {
       // Something gave up: a bounded time for the loads this warp started (see prefill_attn.cuh).
       atomicOr(p.stop, 1);
-      for (int i = 0; i < (KV8 ? 1 : 3); ++i)
+      for (int i = 0; i < 5; ++i) {
+        if (i == 0 ? warp != 8 : KV8 || (i <= 2) != is_k) continue;
         for (uint32_t ph = 0; ph < 2; ++ph)
           for (uint32_t w = 0; w < (1u << 16); ++w)
             if (mbar_try_wait(bar(i), ph)) break;
-    }
-  } else if (warp == 9) {
-    // ================= the warp that loads V =================
-    XtCursor cV = first;
-    if constexpr (KV8) {
-      if (cV.on) begin_codes(x.V, cV);
-    }
-    for (int g = 0; cV.on && !*s_abort; ++g) {
-      // V of tile g after O += P V of tile g - 2 has completed (the stage it read)
-      if (g >= 2) mbar_wait(bar(10 + (g & 1)), (uint32_t)(((g - 2) >> 1) & 1), s_abort, x.err, kPfSpinLimit);
-      __syncwarp();
-      if (*s_abort) break;
-      if constexpr (KV8) {
-        fill_stage(std::true_type{}, x.V, kPfQBytes + 2 * kPfKvBytes, 3, cV, g);
-      } else {
-        if (tc5::elect_one()) load_tile(&tmV, sV, 3, cV, g);
-        __syncwarp();
-        xt_advance(cV, p, s_n);
       }
-    }
-    if (!KV8 && *s_abort && lane == 0) {
-      atomicOr(p.stop, 1);
-      for (int i = 3; i < 5; ++i)
-        for (uint32_t ph = 0; ph < 2; ++ph)
-          for (uint32_t w = 0; w < (1u << 16); ++w)
-            if (mbar_try_wait(bar(i), ph)) break;
     }
   } else if (warp == 11) {
     // ================= the warp that issues O += P V =================
     constexpr uint32_t idesc_o = tc5::idesc_bf16_f32(kXtRows, 128, 0, 1);
     const uint64_t dV = tc5::smem_desc_sw128(sV, kPfKvBytes / 2, 1024);
-    XtCursor cur = first;
-    for (int g = 0; cur.on && !*s_abort; ++g) {
-      const int st = g & 1;
-      mbar_wait(bar(3 + st), (uint32_t)((g >> 1) & 1), s_abort, x.err, kPfSpinLimit);
-      mbar_wait(bar(8 + st), (uint32_t)((g >> 1) & 1), s_abort, x.err, kPfSpinLimit);
-      if (cur.j == 0 && cur.ord > 0) mbar_wait(bar(7), (uint32_t)((cur.ord - 1) & 1), s_abort, x.err, kPfSpinLimit);  // O of the piece before
-      __syncwarp();
-      tc5::fence_after_sync();
-      if (*s_abort) break;
-      const uint64_t dVg = dV + (uint64_t)((uint32_t)st * (kPfKvBytes >> 4));
-      if (tc5::elect_one()) {
+    int g = 0;
+    while (cur->on && !*s_abort) {
+      const int nkt = cur->nkt, ord = cur->ord;
+      for (int j = 0; j < nkt; ++j, ++g) {
+        const int st = g & 1;
+        if constexpr (!KV8) mbar_wait(bar(3 + st), (uint32_t)((g >> 1) & 1), s_abort, x.err, kPfSpinLimit);  // (8-bit rows: written before P)
+        mbar_wait(bar(8 + st), (uint32_t)((g >> 1) & 1), s_abort, x.err, kPfSpinLimit);
+        if (j == 0 && ord > 0) mbar_wait(bar(7), (uint32_t)((ord - 1) & 1), s_abort, x.err, kPfSpinLimit);  // O of the piece before has been read
+        __syncwarp();
+        tc5::fence_after_sync();
+        if (*s_abort) break;
+        const uint64_t dVg = dV + (uint64_t)((uint32_t)st * (kPfKvBytes >> 4));
+        if (tc5::elect_one()) {
 #pragma unroll
-        for (int kk = 0; kk < 4; ++kk)  // 16 keys per step: 8 columns of P (over S buffer g & 1), two 8-row groups of V
-          tc5::mma_bf16_ts(tO, tS0 + 64u * (uint32_t)st + 8u * (uint32_t)kk, dVg + (uint64_t)(kk * 128), idesc_o,
-                           (cur.j > 0 || kk > 0) ? 1u : 0u);
-        tc5::mma_commit(bar(10 + st));
-        if (cur.j == cur.nkt - 1) tc5::mma_commit(bar(12));
+          for (int kk = 0; kk < 4; ++kk)  // 16 keys per step: 8 columns of P (over S buffer g & 1), two 8-row groups of V
+            tc5::mma_bf16_ts(tO, tS0 + 64u * (uint32_t)st + 8u * (uint32_t)kk, dVg + (uint64_t)(kk * 128), idesc_o, (j > 0 || kk > 0) ? 1u : 0u);
+          tc5::mma_commit(bar(10 + st));
+          if (j == nkt - 1) tc5::mma_commit(bar(12));
+        }
+        __syncwarp();
       }
-      __syncwarp();
-      xt_advance(cur, p, s_n);
+      xt_next(cur, p, s_n);
     }
     if (*s_abort && tc5::elect_one()) {
       // give the MMAs already issued a bounded time to finish before the tensor memory is released
@@ -502,16 +462,18 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
     constexpr uint32_t idesc_s = KV8 ? tc5::idesc_f16_f32(kXtRows, kPfKeys, 0, 0) : tc5::idesc_bf16_f32(kXtRows, kPfKeys, 0, 0);
     const uint64_t dQ = tc5::smem_desc_sw128(sQ, 16, 1024);
     const uint64_t dK = tc5::smem_desc_sw128(sK, 16, 1024);
-    XtCursor cur = first;
-    for (int g = 0; cur.on && !*s_abort; ++g) {
-      const int st = g & 1;
-      mbar_wait(bar(1 + st), (uint32_t)((g >> 1) & 1), s_abort, x.err, kPfSpinLimit);
-      // S of tile g overwrites the columns P of tile g - 2 is read from
-      if (g >= 2) mbar_wait(bar(10 + st), (uint32_t)(((g - 2) >> 1) & 1), s_abort, x.err, kPfSpinLimit);
-      if (cur.j == 0) mbar_wait(bar(0), (uint32_t)(cur.ord & 1), s_abort, x.err, kPfSpinLimit);
-      __syncwarp();
-      tc5::fence_after_sync();
-      if (!*s_abort) {
+    int g = 0;
+    while (cur->on && !*s_abort) {
+      const int nkt = cur->nkt, ord = cur->ord;
+      for (int j = 0; j < nkt; ++j, ++g) {
+        const int st = g & 1;
+        mbar_wait(bar(1 + st), (uint32_t)((g >> 1) & 1), s_abort, x.err, kPfSpinLimit);
+        // S of tile g overwrites the columns P of tile g - 2 is read from
+        if (g >= 2) mbar_wait(bar(10 + st), (uint32_t)(((g - 2) >> 1) & 1), s_abort, x.err, kPfSpinLimit);
+        if (j == 0) mbar_wait(bar(0), (uint32_t)(ord & 1), s_abort, x.err, kPfSpinLimit);
+        __syncwarp();
+        tc5::fence_after_sync();
+        if (*s_abort) break;
         const uint64_t dKg = dK + (uint64_t)((uint32_t)st * (kPfKvBytes >> 4));
         if (tc5::elect_one()) {
 #pragma unroll
@@ -522,7 +484,7 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
         }
         __syncwarp();
       }
-      xt_advance(cur, p, s_n);
+      xt_next(cur, p, s_n);
     }
     if (*s_abort && tc5::elect_one()) {
       atomicOr(p.stop, 1);
@@ -535,42 +497,80 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
     const int wg = warp >> 2, wq = warp & 3;              // group; warp within it (its lanes of tensor memory)
     const uint32_t lane_base = (uint32_t)(wq * 32) << 16;
     const uint32_t g_inv = 65536u / (uint32_t)x.G + 1u;  // r / G == r * g_inv >> 16 for r < 128
-    uint8_t* stage = s_out + warp * 2048;
-    uint8_t* stage_other = s_out + (warp ^ 4) * 2048;     // the warp of the other group with the same rows
+    uint8_t* stage = s_out + warp * kXtStageBytes;
+    const uint8_t* stage_other = s_out + (warp ^ 4) * kXtStageBytes;  // the warp of the other group with the same rows
     const int r = wq * 32 + lane;                         // query row within the tile
     const int ri = (int)((uint32_t)r * g_inv >> 16), rg = r - ri * x.G;
-    const float out_scale = KV8 ? x.v_scale : 1.f;
     auto pair_sync = [&]() { asm volatile("bar.sync %0, 64;" ::"r"(2 + wq) : "memory"); };
     auto all_sync = [&]() { asm volatile("bar.sync 1, 256;" ::: "memory"); };
 
     // The end of a piece: this group's 64 columns of the output, or of its part of an item that other CTAs share.
-    auto epilogue = [&](const XtCursor& c, float ref, float l) {
-      mbar_wait(bar(12), (uint32_t)(c.ord & 1), s_abort, x.err, kPfSpinLimit);
-      tc5::fence_after_sync();
-      const bool live = wq * 32 < c.rows, mine = r < c.rows, whole = c.nkt == c.total;
-      const unsigned per = p.per[c.s], start = p.cum[c.s] + (unsigned)c.idx * per;
+    auto epilogue = [&](float ref, float l) {
+      const XtCursor& c = *cur;
+      const float out_scale = KV8 ? x.v_scale : 1.f;
+      const int rows = c.rows;
+      const bool live = wq * 32 < rows, mine = r < rows, whole = c.nkt == c.total;
       // A part: [32 pieces of four columns][part_rows] float4, then [part_rows] log-sum-exps.  A CTA has two places, one for
       // an item that began before its shares and one for an item that begins in them.
-      auto part_of = [&](unsigned place) { return p.part + (size_t)place * ((size_t)p.part_rows * kXtPartFloats); };
       const size_t piece = (size_t)p.part_rows;
-      const bool redo = mine && !(l < kXtSumMax);  // out of range, or not a number
-      float lse = l > 0.f ? ref + __log2f(l) : -CUDART_INF_F;
-      const float f = l > 0.f ? 1.f / l : 0.f;
+      auto part_of = [&](int place) { return p.part + (size_t)place * (piece * kXtPartFloats); };
+      unsigned first_cta = 0;  // (warp 0)
+      int place = 0, n_parts = 1;
+      bool join = false;       // every other part lies in the scratch: this CTA joins them, with its own still in tensor memory
+      if (!whole) {
+        const unsigned per = p.per[c.s], start = p.cum[c.s] + (unsigned)c.idx * per;
+        place = (int)(2u * blockIdx.x + (start >= xt_share0(p, blockIdx.x) ? 1u : 0u));
+        all_sync();  // (the list of a piece before has been read)
+        if (warp == 0) {
+          auto cta_of = [&](unsigned v) {
+            const unsigned big = p.share_rem * (p.share_q + 1u);
+            return v < big ? v / (p.share_q + 1u) : p.share_rem + (v - big) / p.share_q;
+          };
+          first_cta = cta_of(start);
+          const unsigned cb = cta_of(start + per - 1u);
+          int count = 0;
+          for (unsigned c0 = first_cta; c0 <= cb; c0 += 32) {
+            const unsigned cc = c0 + (unsigned)lane;
+            int lo = 0, hi = 0;
+            if (cc <= cb) xt_piece(xt_share0(p, cc), xt_share0(p, cc + 1u), start, per, c.total, lo, hi);
+            const unsigned has = __ballot_sync(0xffffffffu, lo < hi);
+            if (lo < hi) s_list[2 + count + __popc(has & ((1u << lane) - 1u))] = (int)(2u * cc + (start >= xt_share0(p, cc) ? 1u : 0u));
+            count += __popc(has);
+          }
+          if (lane == 0) {
+            unsigned done;
+            asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(done) : "l"(x.counters + first_cta) : "memory");
+            s_list[1] = count;
+            s_list[0] = done == (unsigned)(count - 1);
+          }
+        }
+        all_sync();
+        n_parts = s_list[1];
+        // (with many parts the joint below, which spreads them over the warps, is faster than one thread per row)
+        join = n_parts <= 3 && s_list[0];
+      }
+      mbar_wait(bar(12), (uint32_t)(c.ord & 1), s_abort, x.err, kPfSpinLimit);
+      tc5::fence_after_sync();
       __nv_bfloat16* obase = static_cast<__nv_bfloat16*>(x.out) + (((size_t)c.layer * x.total + x.seqs.tok0[c.s] + c.i0) * x.Hq + c.h * x.G) * 128;
+      float* lse_out = x.lse ? x.lse + ext_lse_index(x, c.layer, c.h, x.seqs.tok0[c.s] + c.i0) : nullptr;
       if (live) {
+        const bool redo = mine && !(l < kXtSumMax);  // out of range, or not a number
+        float lse = l > 0.f ? ref + __log2f(l) : -CUDART_INF_F;
+        const float f = l > 0.f ? 1.f / l : 0.f;
+        float all = lse, w_own = 1.f, w[3] = {0.f, 0.f, 0.f};
+        bool joined = false;
 #pragma unroll 1
-        for (int half = 0; half < 2; ++half) {
-          const int c0 = 64 * wg + 32 * half;
-          uint32_t o[32];
-          tc5::tmem_ld32(tO + lane_base + (uint32_t)c0, o);
+        for (int c0 = 64 * wg; c0 < 64 * wg + 64; c0 += 16) {
+          uint32_t o[16];
+          tc5::tmem_ld16(tO + lane_base + (uint32_t)c0, o);
           tc5::tmem_wait_ld();
-          if (half == 1) {
+          if (c0 == 64 * wg + 48) {
             tc5::fence_before_sync();
             mbar_arrive(bar(7));  // O may be written again
           }
           float probe = 0.f;  // 0 * finite = 0
 #pragma unroll
-          for (int e = 0; e < 32; ++e) {
+          for (int e = 0; e < 16; ++e) {
             o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
             probe = fmaf(__uint_as_float(o[e]), 0.f, probe);
           }
@@ -586,158 +586,182 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
             __syncwarp();
             if (lane == who) {
               lse = new_lse;
+              if (!joined) all = lse;
 #pragma unroll
-              for (int e = 0; e < 32; ++e)
+              for (int e = 0; e < 16; ++e)
                 if (full || !(__uint_as_float(o[e]) * 0.f == 0.f)) o[e] = reinterpret_cast<const uint32_t*>(stage)[c0 + e];
             }
             __syncwarp();
           }
-          if (whole) {
-            // rounded, through the warp's staging tile [32 rows][64 B] (16-byte chunks swizzled), so that the stores are
-            // 64-byte pieces of rows
+          if (join) {
+            const int rr = min(r, rows - 1);
+            if (!joined) {  // in the order of the list, whoever joins: maximum, sum and weights of the parts
+              joined = true;
+              float M = -CUDART_INF_F, y[3];
 #pragma unroll
-            for (int e = 0; e < 32; e += 8) {
-              uint32_t w[4];
+              for (int k = 0; k < 3; ++k) {
+                y[k] = -CUDART_INF_F;
+                if (k < n_parts) y[k] = s_list[2 + k] == place ? lse : __ldcg(part_of(s_list[2 + k]) + 128 * piece + rr);
+                M = fmaxf(M, y[k]);
+              }
+              float sum = 0.f;
 #pragma unroll
-              for (int u = 0; u < 4; ++u)
-                w[u] = pack_bf16x2(__uint_as_float(o[e + 2 * u]) * out_scale, __uint_as_float(o[e + 2 * u + 1]) * out_scale);
-              *reinterpret_cast<uint4*>(stage + lane * 64 + (((e >> 3) ^ ((lane >> 1) & 3)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
+              for (int k = 0; k < 3; ++k) sum += y[k] == -CUDART_INF_F ? 0.f : exp2f(y[k] - M);
+              all = M + __log2f(sum);
+#pragma unroll
+              for (int k = 0; k < 3; ++k) {
+                w[k] = y[k] == -CUDART_INF_F ? 0.f : fast_exp2(y[k] - all);
+                if (k < n_parts && s_list[2 + k] == place) {
+                  w_own = w[k];
+                  w[k] = -1.f;
+                }
+              }
             }
+#pragma unroll
+            for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * w_own);
+#pragma unroll
+            for (int k = 0; k < 3; ++k) {
+              if (k >= n_parts || w[k] < 0.f) continue;
+              const float4* src = reinterpret_cast<const float4*>(part_of(s_list[2 + k])) + (size_t)c0 / 4 * piece + rr;
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const float4 y = __ldcg(src + e * piece);
+                o[4 * e] = __float_as_uint(fmaf(w[k], y.x, __uint_as_float(o[4 * e])));
+                o[4 * e + 1] = __float_as_uint(fmaf(w[k], y.y, __uint_as_float(o[4 * e + 1])));
+                o[4 * e + 2] = __float_as_uint(fmaf(w[k], y.z, __uint_as_float(o[4 * e + 2])));
+                o[4 * e + 3] = __float_as_uint(fmaf(w[k], y.w, __uint_as_float(o[4 * e + 3])));
+              }
+            }
+          }
+          if (whole || join) {
+            // rounded, through the warp's staging tile [32 rows][32 B] (16-byte chunks swizzled), so that the stores are whole
+            // sectors
+            uint32_t y[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) y[e] = pack_bf16x2(__uint_as_float(o[2 * e]) * out_scale, __uint_as_float(o[2 * e + 1]) * out_scale);
+            const int sw = (lane >> 2) & 1;
+            *reinterpret_cast<uint4*>(stage + lane * 32 + (sw << 4)) = make_uint4(y[0], y[1], y[2], y[3]);
+            *reinterpret_cast<uint4*>(stage + lane * 32 + ((sw ^ 1) << 4)) = make_uint4(y[4], y[5], y[6], y[7]);
             __syncwarp();
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const int row = 8 * i + (lane >> 2), chunk = lane & 3;
-              const uint4 w = *reinterpret_cast<const uint4*>(stage + row * 64 + ((chunk ^ ((row >> 1) & 3)) << 4));
+            for (int i = 0; i < 2; ++i) {
+              const int row = 16 * i + (lane >> 1), chunk = lane & 1;
+              const uint4 v = *reinterpret_cast<const uint4*>(stage + row * 32 + ((chunk ^ ((row >> 2) & 1)) << 4));
               const int rr = wq * 32 + row, ti = (int)((uint32_t)rr * g_inv >> 16);
-              if (rr < c.rows && !*s_abort) *reinterpret_cast<uint4*>(obase + ((size_t)ti * x.Hq + (rr - ti * x.G)) * 128 + c0 + chunk * 8) = w;
+              if (rr < rows && !*s_abort) *reinterpret_cast<uint4*>(obase + ((size_t)ti * x.Hq + (rr - ti * x.G)) * 128 + c0 + chunk * 8) = v;
             }
             __syncwarp();
           } else if (mine && !*s_abort) {
-            float* dst = part_of(2u * blockIdx.x + (start >= xt_share0(p, blockIdx.x) ? 1u : 0u));
+            float4* dst = reinterpret_cast<float4*>(part_of(place)) + (size_t)c0 / 4 * piece + r;
 #pragma unroll
-            for (int e = 0; e < 32; e += 4)
-              __stcg(reinterpret_cast<float4*>(dst) + (size_t)(c0 / 4 + e / 4) * piece + r,
-                     make_float4(__uint_as_float(o[e]), __uint_as_float(o[e + 1]), __uint_as_float(o[e + 2]), __uint_as_float(o[e + 3])));
-            if (wg == 0 && half == 1) __stcg(dst + 128 * piece + r, lse);
+            for (int e = 0; e < 4; ++e)
+              __stcg(dst + e * piece, make_float4(__uint_as_float(o[4 * e]), __uint_as_float(o[4 * e + 1]), __uint_as_float(o[4 * e + 2]),
+                                                  __uint_as_float(o[4 * e + 3])));
           }
         }
+        if (whole || join) {
+          if (wg == 0 && mine && lse_out) lse_out[r] = all;
+          return;
+        }
+        if (wg == 0 && mine && !*s_abort) __stcg(part_of(place) + 128 * piece + r, lse);
       } else {
         mbar_arrive(bar(7));
-      }
-      if (whole) {
-        if (wg == 0 && mine && x.lse) x.lse[ext_lse_index(x, c.layer, c.h, x.seqs.tok0[c.s] + c.i0) + r] = lse;
-        return;
+        if (whole || join) return;
       }
       __threadfence();
       all_sync();
-      // the places of the item's parts, in the order of the list, and how many there are (the staging tiles are free here)
-      int* s_list = reinterpret_cast<int*>(s_out);            // [0] last to finish, [1] parts, [2 ...] places
-      float* s_lse = reinterpret_cast<float*>(s_out) + 1024;  // [128]
-      if (warp == 0) {
-        auto cta_of = [&](unsigned v) {
-          const unsigned big = p.share_rem * (p.share_q + 1u);
-          return v < big ? v / (p.share_q + 1u) : p.share_rem + (v - big) / p.share_q;
-        };
-        const unsigned ca = cta_of(start), cb = cta_of(start + per - 1u);
-        int count = 0;
-        for (unsigned c0 = ca; c0 <= cb; c0 += 32) {
-          const unsigned cc = c0 + (unsigned)lane;
-          int lo = 0, hi = 0;
-          if (cc <= cb) xt_piece(xt_share0(p, cc), xt_share0(p, cc + 1u), start, per, c.total, lo, hi);
-          const unsigned has = __ballot_sync(0xffffffffu, lo < hi);
-          if (lo < hi) s_list[2 + count + __popc(has & ((1u << lane) - 1u))] = (int)(2u * cc + (start >= xt_share0(p, cc) ? 1u : 0u));
-          count += __popc(has);
-        }
-        if (lane == 0) {
-          s_list[1] = count;
-          s_list[0] = atomicAdd(x.counters + ca, 1u) == (unsigned)(count - 1);
-        }
-      }
+      if (tid == 0) s_list[0] = atomicAdd(x.counters + first_cta, 1u) == (unsigned)(n_parts - 1);
       all_sync();
-      const int n_parts = s_list[1];
       if (s_list[0]) {
+        // The last to finish joins the parts.  A warp takes 8 rows x 64 columns at a time, a lane four pieces of four columns
+        // of one row: 128-byte pieces of every part, whole sectors of the output.  Running maximum and sum over the parts.
         __threadfence();
-        if (wg == 0 && mine) {  // thread = row: log2 of the sum over the parts
-          float M = -CUDART_INF_F, sum = 0.f;
-#pragma unroll 8
-          for (int k = 0; k < n_parts; ++k) M = fmaxf(M, __ldcg(part_of(s_list[2 + k]) + 128 * piece + r));
-          const float M0 = M == -CUDART_INF_F ? 0.f : M;
-#pragma unroll 8
-          for (int k = 0; k < n_parts; ++k) sum += exp2f(__ldcg(part_of(s_list[2 + k]) + 128 * piece + r) - M0);
-          const float all = M + __log2f(sum);
-          s_lse[r] = all;
-          if (x.lse) x.lse[ext_lse_index(x, c.layer, c.h, x.seqs.tok0[c.s] + c.i0) + r] = all;
-        }
-        all_sync();
-        // a warp takes 8 rows x 64 columns at a time, a lane four pieces of four columns of one row: 128-byte pieces of
-        // every part, whole sectors of the output
-        const int units = (c.rows + 7) / 8 * 2;
+        const int units = (rows + 7) / 8 * 2;
         for (int u = warp; u < units; u += 8) {
           const int row = (u >> 1) * 8 + (lane >> 2), c4 = (u & 1) * 16 + (lane & 3);
-          if (row < c.rows && !*s_abort) {
-            const float all = s_lse[row];
-            float acc[16];
+          if (row < rows && !*s_abort) {
+            float M = -CUDART_INF_F, sum = 0.f, acc[16];
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[e] = 0.f;
 #pragma unroll 2
             for (int k = 0; k < n_parts; ++k) {
               const float* src = part_of(s_list[2 + k]);
-              const float wk = fast_exp2(__ldcg(src + 128 * piece + row) - all);
+              const float lk = __ldcg(src + 128 * piece + row);
               float4 y[4];
 #pragma unroll
               for (int e = 0; e < 4; ++e) y[e] = __ldcg(reinterpret_cast<const float4*>(src) + (size_t)(c4 + 4 * e) * piece + row);
+              const float Mn = fmaxf(M, lk);
+              const float keep = M == -CUDART_INF_F ? 0.f : fast_exp2(M - Mn), wk = lk == -CUDART_INF_F ? 0.f : fast_exp2(lk - Mn);
+              M = Mn;
+              sum = fmaf(sum, keep, wk);
 #pragma unroll
               for (int e = 0; e < 4; ++e) {
-                acc[4 * e] = fmaf(wk, y[e].x, acc[4 * e]);
-                acc[4 * e + 1] = fmaf(wk, y[e].y, acc[4 * e + 1]);
-                acc[4 * e + 2] = fmaf(wk, y[e].z, acc[4 * e + 2]);
-                acc[4 * e + 3] = fmaf(wk, y[e].w, acc[4 * e + 3]);
+                acc[4 * e] = fmaf(acc[4 * e], keep, wk * y[e].x);
+                acc[4 * e + 1] = fmaf(acc[4 * e + 1], keep, wk * y[e].y);
+                acc[4 * e + 2] = fmaf(acc[4 * e + 2], keep, wk * y[e].z);
+                acc[4 * e + 3] = fmaf(acc[4 * e + 3], keep, wk * y[e].w);
               }
             }
+            const float fs = out_scale / sum;
             const int ti = (int)((uint32_t)row * g_inv >> 16);
             __nv_bfloat16* dst = obase + ((size_t)ti * x.Hq + (row - ti * x.G)) * 128;
 #pragma unroll
             for (int e = 0; e < 4; ++e)
               *reinterpret_cast<uint2*>(dst + (c4 + 4 * e) * 4) =
-                  make_uint2(pack_bf16x2(acc[4 * e] * out_scale, acc[4 * e + 1] * out_scale), pack_bf16x2(acc[4 * e + 2] * out_scale, acc[4 * e + 3] * out_scale));
+                  make_uint2(pack_bf16x2(acc[4 * e] * fs, acc[4 * e + 1] * fs), pack_bf16x2(acc[4 * e + 2] * fs, acc[4 * e + 3] * fs));
+            if (c4 == 0 && lse_out) lse_out[row] = M + __log2f(sum);
           }
         }
       }
-      all_sync();  // the staging tiles are the warps' own again
     };
 
-    XtCursor cur = first;
     int g0 = 0;  // flat index of the piece's first tile
-    while (cur.on) {
-      const bool live = wq * 32 < cur.rows;
-      const int prefix = x.seqs.prefix[cur.s];
-      const int ti = cur.i0 + min(ri, (cur.rows - 1) / x.G);  // (a lane without a query repeats the last token's visibility)
-      const int lim = cur.n + max(ti + 1, prefix);            // rows [0, lim) are visible
+    while (cur->on) {
+      const int nkt = cur->nkt, kt_new = cur->kt0 + nkt - 1;  // its newest tile
+      const bool live = wq * 32 < cur->rows;
+      const int ti = cur->i0 + min(ri, (cur->rows - 1) / x.G);  // (a lane without a query repeats the last token's visibility)
+      const int lim = cur->n + max(ti + 1, x.seqs.prefix[cur->s]);  // rows [0, lim) are visible
       // Tiles that some token of the query tile does not see whole: all of them, and one more, are the first group's.
-      const int ramp = min(cur.nkt, max(0, cur.kt0 + cur.nkt - 1 - (cur.n + max(cur.i0 + 1, prefix) - 1) / kPfKeys) + 1);
+      const int ramp = min(nkt, max(0, kt_new - (cur->n + max(cur->i0 + 1, x.seqs.prefix[cur->s]) - 1) / kPfKeys) + 1);
       const int* pos_row = nullptr;
       int tot = 0;
       float slope = 0.f;
       if constexpr (MODS) {
-        const int b = x.seqs.b0 + cur.s, t = x.seqs.tok0[cur.s + 1] - x.seqs.tok0[cur.s];
-        tot = x.tot[b] - (x.published ? t : 0);
-        pos_row = x.pos + (size_t)slab_of(cur) * x.cap;
-        if (x.slopes) slope = x.slopes[cur.h * x.G + rg] * 1.4426950408889634f;
+        tot = x.tot[x.seqs.b0 + cur->s] - (x.published ? cur->end - cur->n : 0);
+        pos_row = x.pos + (size_t)cur->slab * x.cap;
+        if (x.slopes) slope = x.slopes[cur->h * x.G + rg] * 1.4426950408889634f;
       }
       float ref = -CUDART_INF_F, l = 0.f;
 
-      // One tile: S of flat tile g to P.  RAMP: part of it may be hidden, the reference may not be set yet.
+      // One tile: S of flat tile g to P, a chunk of columns at a time (the registers of 24 warps per SM hold no more).
+      // RAMP: part of the tile may be hidden and the reference may not be set yet; S is read twice.
+      constexpr int CH = MODS ? 16 : 32;
       auto tile = [&](auto is_ramp, int j) {
         constexpr bool RAMP = decltype(is_ramp)::value;
-        const int g = g0 + j, key0 = (cur.kt0 + cur.nkt - 1 - j) * kPfKeys;
+        const int g = g0 + j, key0 = (kt_new - j) * kPfKeys;
         const uint32_t ts = tS0 + lane_base + 64u * (uint32_t)(g & 1);
         int pos_a = 0, pos_b = 0;
         if constexpr (MODS) {  // positions relative to the chunk's first token, two per lane
           pos_a = pos_row[min(key0 + lane, x.cap - 1)] - tot;
           pos_b = pos_row[min(key0 + 32 + lane, x.cap - 1)] - tot;
         }
+        XtCodes vc[2];
+        if constexpr (KV8) {  // this warp's 16 rows of V
+          const uint8_t* src = static_cast<const uint8_t*>(x.V) + (size_t)cur->slab * x.cap * 128;
+          xt_load_codes(vc[0], src, key0 + 16 * wq, cur->end, lane);
+          xt_load_codes(vc[1], src, key0 + 16 * wq + 8, cur->end, lane);
+          if (lane == 0 && j + 4 < nkt)
+            asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(src + (size_t)(key0 + 16 * wq - 4 * kPfKeys) * 128), "r"(16 * 128) : "memory");
+        }
         mbar_wait(bar(5 + (g & 1)), (uint32_t)((g >> 1) & 1), s_abort, x.err, kPfSpinLimit);  // S of this tile is complete
         tc5::fence_after_sync();
+        if constexpr (KV8) {
+          // (S of this tile was issued after O += P V of tile g - 2 had read the stage)
+          uint8_t* vt = sm + kPfQBytes + (2 + (uint32_t)(g & 1)) * kPfKvBytes;
+          xt_store_codes<true>(vc[0], vt, kPfKvBytes / 2, 16 * wq, lane);
+          xt_store_codes<true>(vc[1], vt, kPfKvBytes / 2, 16 * wq + 8, lane);
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        }
         if (live) {
           bool border = false;
           const int* ipos = reinterpret_cast<const int*>(stage);
@@ -751,27 +775,31 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
             if (x.window > 0) {
               // the tile's first position against the warp's last token (in tiles with rows of the chunk: always compared)
               const int p0 = __shfl_sync(0xffffffffu, pos_a, 0), tb = __shfl_sync(0xffffffffu, ti, 31);
-              border = key0 + kPfKeys > cur.n || (long long)tb - p0 >= x.window;
+              border = key0 + kPfKeys > cur->n || (long long)tb - p0 >= x.window;
             }
             __syncwarp();
           }
           // logits in base-2 units: scaled in the exponent's multiply-add, or (MODS) here
-          float scale_log2 = p.scale_log2;
-          if constexpr (MODS) scale_log2 = 1.f;
-          auto modify = [&](uint32_t (&sv)[32], int hb) {
+          const float scale_log2 = MODS ? 1.f : p.scale_log2;
+          const int cv = lim - key0;  // visible columns
+          uint32_t sv[CH];
+          auto read = [&](int hb) {
+            if constexpr (CH == 32) tc5::tmem_ld32(ts + (uint32_t)hb, sv);
+            else tc5::tmem_ld16(ts + (uint32_t)hb, sv);
+            tc5::tmem_wait_ld();
             if constexpr (MODS) {
               if (x.cap_logit > 0.f) {  // c tanh(y) = c - 2 c / (1 + e^(2 y))
 #pragma unroll
-                for (int c = 0; c < 32; ++c)
+                for (int c = 0; c < CH; ++c)
                   sv[c] = __float_as_uint(fmaf(-2.f * p.cap_log2, rcp_approx(1.f + fast_exp2(__uint_as_float(sv[c]) * p.cap_arg)), p.cap_log2));
               } else {
 #pragma unroll
-                for (int c = 0; c < 32; ++c) sv[c] = __float_as_uint(__uint_as_float(sv[c]) * p.scale_log2);
+                for (int c = 0; c < CH; ++c) sv[c] = __float_as_uint(__uint_as_float(sv[c]) * p.scale_log2);
               }
               if (x.slopes) {
                 const float fi = (float)ti;
 #pragma unroll
-                for (int c = 0; c < 32; c += 4) {
+                for (int c = 0; c < CH; c += 4) {
                   const float4 y = *reinterpret_cast<const float4*>(fpos + hb + c);
                   sv[c] = __float_as_uint(fmaf(-slope, fabsf(fi - y.x), __uint_as_float(sv[c])));
                   sv[c + 1] = __float_as_uint(fmaf(-slope, fabsf(fi - y.y), __uint_as_float(sv[c + 1])));
@@ -781,83 +809,81 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
               }
               if (border) {
 #pragma unroll
-                for (int c = 0; c < 32; ++c)
-                  if (abs(ti - ipos[hb + c]) >= x.window) sv[c] = 0xff800000u;
+                for (int c = 0; c < CH; c += 4) {
+                  const int4 y = *reinterpret_cast<const int4*>(ipos + hb + c);
+                  if (abs(ti - y.x) >= x.window) sv[c] = 0xff800000u;  // -inf
+                  if (abs(ti - y.y) >= x.window) sv[c + 1] = 0xff800000u;
+                  if (abs(ti - y.z) >= x.window) sv[c + 2] = 0xff800000u;
+                  if (abs(ti - y.w) >= x.window) sv[c + 3] = 0xff800000u;
+                }
               }
             }
             if constexpr (RAMP) {
-              const int cv = lim - key0 - hb;  // visible columns of this half
 #pragma unroll
-              for (int c = 0; c < 32; ++c)
-                if (c >= cv) sv[c] = 0xff800000u;  // -inf
+              for (int c = 0; c < CH; ++c)
+                if (hb + c >= cv) sv[c] = 0xff800000u;
             }
           };
-          auto weigh = [&](const uint32_t (&sv)[32], int hb) {  // 32 logits to 16 columns of P
-            const float neg = ref == -CUDART_INF_F ? 0.f : -ref;
-            const uint64_t scale2 = tc5::f2_pack(scale_log2, scale_log2), neg2 = tc5::f2_pack(neg, neg);
-            uint64_t sum2[4] = {0ull, 0ull, 0ull, 0ull};  // four chains of (even, odd) column sums
-            uint32_t pk[16];
+          if constexpr (RAMP) {
+            float mx4[4] = {-CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F};
 #pragma unroll
-            for (int c = 0; c < 16; ++c) {
+            for (int hb = 0; hb < kPfKeys; hb += CH) {
+              read(hb);
+#pragma unroll
+              for (int c = 0; c < CH; c += 8)
+#pragma unroll
+                for (int u = 0; u < 4; ++u) mx4[u] = tc5::f_max3(mx4[u], __uint_as_float(sv[c + u]), __uint_as_float(sv[c + 4 + u]));
+            }
+            const float mx = tc5::f_max3(fmaxf(mx4[0], mx4[1]), mx4[2], mx4[3]) * scale_log2;
+            if (ref == -CUDART_INF_F) ref = mx + kXtHeadroom;
+          }
+          const float neg = ref == -CUDART_INF_F ? 0.f : -ref;
+          const uint64_t scale2 = tc5::f2_pack(scale_log2, scale_log2), neg2 = tc5::f2_pack(neg, neg);
+          uint64_t sum2[4] = {0ull, 0ull, 0ull, 0ull};  // four chains of (even, odd) column sums
+#pragma unroll
+          for (int hb = 0; hb < kPfKeys; hb += CH) {
+            read(hb);
+            uint32_t pk[CH / 2];
+#pragma unroll
+            for (int c = 0; c < CH / 2; ++c) {
               float x0, x1;
               tc5::f2_unpack(tc5::f2_fma(tc5::f2_pack(__uint_as_float(sv[2 * c]), __uint_as_float(sv[2 * c + 1])), scale2, neg2), x0, x1);
               const float a0 = fast_exp2(x0), a1 = fast_exp2(x1);
               sum2[c & 3] = tc5::f2_add(sum2[c & 3], tc5::f2_pack(a0, a1));
               pk[c] = pack_bf16x2(a0, a1);
             }
-            tc5::tmem_st16(ts + (uint32_t)(hb / 2), pk);
-            float e, o;
-            tc5::f2_unpack(tc5::f2_add(tc5::f2_add(sum2[0], sum2[1]), tc5::f2_add(sum2[2], sum2[3])), e, o);
-            l += e + o;
-          };
-          uint32_t lo[32], hi[32];
-          tc5::tmem_ld32(ts, lo);
-          tc5::tmem_wait_ld();
-          tc5::tmem_ld32(ts + 32u, hi);
-          if constexpr (RAMP) {
-            tc5::tmem_wait_ld();
-            modify(lo, 0);
-            modify(hi, 32);
-            float mx4[4] = {-CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F};
-#pragma unroll
-            for (int c = 0; c < 32; c += 4)
-#pragma unroll
-              for (int u = 0; u < 4; ++u) mx4[u] = tc5::f_max3(mx4[u], __uint_as_float(lo[c + u]), __uint_as_float(hi[c + u]));
-            const float mx = tc5::f_max3(fmaxf(mx4[0], mx4[1]), mx4[2], mx4[3]) * scale_log2;
-            if (ref == -CUDART_INF_F) ref = mx + kXtHeadroom;
-            weigh(lo, 0);
-            weigh(hi, 32);
-          } else {
-            modify(lo, 0);
-            weigh(lo, 0);
-            tc5::tmem_wait_ld();
-            modify(hi, 32);
-            weigh(hi, 32);
+            // (over columns of S that have been read)
+            if constexpr (CH == 32) tc5::tmem_st16(ts + (uint32_t)(hb / 2), pk);
+            else tc5::tmem_st8(ts + (uint32_t)(hb / 2), pk);
           }
+          float e, o;
+          tc5::f2_unpack(tc5::f2_add(tc5::f2_add(sum2[0], sum2[1]), tc5::f2_add(sum2[2], sum2[3])), e, o);
+          l += e + o;
           tc5::tmem_wait_st();
         }
         tc5::fence_before_sync();
         mbar_arrive(bar(8 + (g & 1)));
       };
+      int j = ramp;
       if (wg == 0) {
-        for (int j = 0; j < ramp; ++j) tile(std::true_type{}, j);
-        reinterpret_cast<float*>(stage)[256 + lane] = ref;
+        for (int i = 0; i < ramp; ++i) tile(std::true_type{}, i);
+        reinterpret_cast<float*>(stage)[128 + lane] = ref;
         pair_sync();
-        for (int j = ramp + 1; j < cur.nkt; j += 2) tile(std::false_type{}, j);
+        ++j;
       } else {
         pair_sync();
-        ref = reinterpret_cast<const float*>(stage_other)[256 + lane];
-        for (int j = ramp; j < cur.nkt; j += 2) tile(std::false_type{}, j);
+        ref = reinterpret_cast<const float*>(stage_other)[128 + lane];
       }
-      g0 += cur.nkt;
+      for (; j < nkt; j += 2) tile(std::false_type{}, j);
+      g0 += nkt;
       // the other group's share of the row's sum
-      reinterpret_cast<float*>(stage)[288 + lane] = l;
+      reinterpret_cast<float*>(stage)[160 + lane] = l;
       pair_sync();
-      const float l_other = reinterpret_cast<const float*>(stage_other)[288 + lane];
+      const float l_other = reinterpret_cast<const float*>(stage_other)[160 + lane];
       l = wg == 0 ? l + l_other : l_other + l;
       pair_sync();
-      epilogue(cur, ref, l);
-      xt_next_item(cur, p, s_n);
+      epilogue(ref, l);
+      xt_next(cur, p, s_n);
     }
   }
   tc5::fence_before_sync();
@@ -1090,12 +1116,12 @@ extend_mass_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_con
       XmCursor cK;
       cK.ord = 0;
       xm_seek(cK, 0, n_items, p, sh, true);
-      XtCodes codes[4];
+      XtCodes codes[8];
       const int sub = 64 * (warp - 6);
       auto fetch = [&]() {
         const uint8_t* src = static_cast<const uint8_t*>(x.K) + (size_t)slab_of(cK) * x.cap * 128;
 #pragma unroll
-        for (int q = 0; q < 4; ++q) xt_load_codes(codes[q], src, cK.k0 + sub + 16 * q, cK.n + cK.t, lane);
+        for (int q = 0; q < 8; ++q) xt_load_codes(codes[q], src, cK.k0 + sub + 8 * q, cK.n + cK.t, lane);
       };
       if (cK.it < n_items) fetch();
       while (cK.it < n_items && !*s_abort) {
@@ -1103,7 +1129,7 @@ extend_mass_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_con
         __syncwarp();
         if (*s_abort) break;
 #pragma unroll
-        for (int q = 0; q < 4; ++q) xt_store_codes<false>(codes[q], sm + (size_t)(cK.ord & 1) * kXmKBytes, kXmKBytes / 2, sub + 16 * q, lane);
+        for (int q = 0; q < 8; ++q) xt_store_codes<false>(codes[q], sm + (size_t)(cK.ord & 1) * kXmKBytes, kXmKBytes / 2, sub + 8 * q, lane);
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
         if (lane == 0) mbar_arrive(bar(cK.ord & 1));
