@@ -1335,7 +1335,7 @@ namespace {
 
 // What a chunk's launches need beside the cache, as offsets into the caller's scratch.
 struct ExtendScratch {
-  size_t lse, q16, part, counters, total;
+  size_t lse, q16, part, counters, plan, total;
   int part_rows;  // query rows of a part of an item that several CTAs share
   int ctas;       // of the tensor-core kernel, at most
 };
@@ -1361,11 +1361,18 @@ ExtendScratch extend_scratch(const dynts_cache* c, const int* n_new, int n_layer
     return o;
   };
   m.lse = take((size_t)n_layers * total * f.q_heads * sizeof(float));
-  m.q16 = m.part = m.counters = off;
+  m.q16 = m.part = m.counters = m.plan = off;
   if (extend_tc_shape(f)) {
     if (f.dtype == DYNTS_BF16_KV8) m.q16 = take((size_t)n_layers * total * f.q_heads * f.head_dim * 2);
     m.part = take((size_t)2 * m.ctas * m.part_rows * dynts::kXtPartFloats * sizeof(float));
     m.counters = take((size_t)m.ctas * sizeof(int));
+    long long items = 0;  // of the launch with the most sequences' worth (a batch beyond 128 sequences takes several)
+    for (int b0 = 0; b0 < f.batch; b0 += dynts::kExtSeqs) {
+      long long tiles = 0;
+      for (int b = b0; b < std::min(f.batch, b0 + dynts::kExtSeqs); ++b) tiles += (n_new[b] + dynts::kXtRows / G - 1) / (dynts::kXtRows / G);
+      items = std::max(items, tiles * n_layers * f.kv_heads);
+    }
+    m.plan = take((size_t)(items + m.ctas) * dynts::kPlanWords * sizeof(int));
   }
   m.total = std::max<size_t>(off, 256);
   return m;
@@ -1515,28 +1522,29 @@ dynts_status_t launch_extend_tc_as(dynts_cache* c, dynts::ExtendTcParams& p, uns
 
 constexpr int kExtendMinTiles = 3;  // key tiles per CTA below which the grid shrinks
 
-// The tensor-core kernels: the list of key tiles and its shares.
-dynts_status_t launch_extend_tc(dynts_cache* c, const dynts::ExtendParams& x, const ExtendScratch& m, char* scratch, bool want_mass) {
-  dynts::ExtendTcParams p;
-  p.x = x;
-  const int G = c->G, n_seq = x.seqs.n, tpt = dynts::kXtRows / G;
+// The list of key tiles and its shares (see ExtendPlan); *grid: CTAs of the tensor-core kernel.
+dynts_status_t plan_extend(const dynts_cache* c, const dynts::ExtendParams& x, const ExtendScratch& m, char* scratch, dynts::ExtendPlan& p, unsigned* grid) {
+  const int n_seq = x.seqs.n, tpt = dynts::kXtRows / c->G;
   p.tokens_per_tile = tpt;
   p.lh = x.n_layers * x.Hkv;
-  p.part_rows = m.part_rows;
-  long long key_tiles = 0, shares = 0;
+  p.words = reinterpret_cast<int*>(scratch + m.plan);
+  long long key_tiles = 0, shares = 0, items = 0;
   for (int s = 0; s < n_seq; ++s) {
     const int t = x.seqs.tok0[s + 1] - x.seqs.tok0[s];
     p.tiles[s] = (t + tpt - 1) / tpt;
     // The key tiles of an item, on average over the chunk.  (The host's copy of the lengths only guides the cut: the
-    // kernel goes by the device's.)
+    // kernels go by the device's.)
     long long rows = c->len_h[x.seqs.b0 + s] + std::max((t + 1) / 2, x.seqs.prefix[s]);
     if (x.window > 0) rows = std::min<long long>(rows, (long long)x.window + tpt + dynts::kPfKeys);
-    const long long n = std::max<long long>(1, (rows + dynts::kPfKeys - 1) / dynts::kPfKeys), items = (long long)p.tiles[s] * p.lh;
+    const long long n = std::max<long long>(1, (rows + dynts::kPfKeys - 1) / dynts::kPfKeys), mine = (long long)p.tiles[s] * p.lh;
+    p.item0[s] = (int)items;
+    items += mine;
     if (items >= (1ll << 30)) return fail(DYNTS_ERR_INVALID_ARG, "%lld work items are beyond the launch limits", items);
     p.per[s] = (unsigned)(n + 1);  // an item's beginning and end take about a key tile's time
-    key_tiles += items * n;
-    shares += items * (n + 1);
+    key_tiles += mine * n;
+    shares += mine * (n + 1);
   }
+  p.item0[n_seq] = (int)items;
   unsigned coarse = 1;  // shares are counted in 32 bits: very large calls count several key tiles as one
   while (shares / coarse >= (1ll << 30)) coarse *= 2;
   long long sum = 0;
@@ -1548,10 +1556,18 @@ dynts_status_t launch_extend_tc(dynts_cache* c, const dynts::ExtendParams& x, co
   }
   p.cum[n_seq] = (unsigned)sum;
   // Two CTAs per SM, with at least a few key tiles each.
-  const long long grid_ll = std::max<long long>(1, std::min<long long>(std::min<long long>(m.ctas, sum), key_tiles / kExtendMinTiles));
-  const unsigned grid = (unsigned)grid_ll;
-  p.share_q = (unsigned)(sum / grid);
-  p.share_rem = (unsigned)(sum % grid);
+  *grid = (unsigned)std::max<long long>(1, std::min<long long>(std::min<long long>(m.ctas, sum), key_tiles / kExtendMinTiles));
+  p.share_q = (unsigned)(sum / *grid);
+  p.share_rem = (unsigned)(sum % *grid);
+  return DYNTS_OK;
+}
+
+dynts_status_t launch_extend_tc(dynts_cache* c, const dynts::ExtendParams& x, const dynts::ExtendPlan& plan, unsigned grid, const ExtendScratch& m, char* scratch,
+                                bool want_mass) {
+  dynts::ExtendTcParams p;
+  p.x = x;
+  p.plan = plan;
+  p.part_rows = m.part_rows;
   p.part = reinterpret_cast<float*>(scratch + m.part);
   p.stop = reinterpret_cast<int*>(c->ticket()) + 41;  // a spare word of the ticket block (zero since the cache was created)
   p.scale_log2 = (float)(1.4426950408889634 * (double)x.scale);
@@ -1565,14 +1581,15 @@ dynts_status_t launch_extend_tc(dynts_cache* c, const dynts::ExtendParams& x, co
   const void* q = kv8 ? static_cast<const void*>(x.q16) : x.q;
   CUtensorMap map[2];
   for (int i = 0; i < (want_mass ? 2 : 1); ++i) {
-    const cuuint32_t box[3] = {64, (cuuint32_t)G, (cuuint32_t)((i == 0 ? dynts::kXtRows : dynts::kXmRows) / G)};
+    const cuuint32_t box[3] = {64, (cuuint32_t)c->G, (cuuint32_t)((i == 0 ? dynts::kXtRows : dynts::kXmRows) / c->G)};
     const CUresult r = c->encode(&map[i], kv8 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(q), dims, strides,
                                  box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     if (r != CUDA_SUCCESS) return fail(DYNTS_ERR_CUDA, "cuTensorMapEncodeTiled failed (%d)", (int)r);
   }
   const bool mods = x.cap_logit > 0.f || x.slopes || x.window > 0;
-  if (kv8) return mods ? launch_extend_tc_as<true, true>(c, p, grid, map[0], map[1], want_mass) : launch_extend_tc_as<true, false>(c, p, grid, map[0], map[1], want_mass);
+  if (kv8)
+    return mods ? launch_extend_tc_as<true, true>(c, p, grid, map[0], map[1], want_mass) : launch_extend_tc_as<true, false>(c, p, grid, map[0], map[1], want_mass);
   return mods ? launch_extend_tc_as<false, true>(c, p, grid, map[0], map[1], want_mass) : launch_extend_tc_as<false, false>(c, p, grid, map[0], map[1], want_mass);
 }
 
@@ -1656,13 +1673,20 @@ dynts_status_t launch_extend(dynts_cache* c, int layer0, int n_layers, const Ext
     if (p.q16) work = std::max(work, (long long)n_tok * c->G * (f.head_dim / 8));
     if (work >= (1ll << 31)) return fail(DYNTS_ERR_INVALID_ARG, "%d new tokens are beyond the launch limits", n_tok);
     const dim3 grid((unsigned)std::max<long long>(1, std::min<long long>((work + 255) / 256, std::max<long long>(1, 16ll * c->sm_count / ny))), (unsigned)ny, 1);
-    if (kv8) dynts::extend_store_kernel<__nv_bfloat16, true><<<grid, 256, 0, c->stream>>>(p);
-    else if (f.dtype == DYNTS_FP32) dynts::extend_store_kernel<float, false><<<grid, 256, 0, c->stream>>>(p);
-    else dynts::extend_store_kernel<__nv_bfloat16, false><<<grid, 256, 0, c->stream>>>(p);
+    dynts::ExtendPlan plan;
+    plan.words = nullptr;
+    unsigned tc_grid = 0;
+    if (tc) {
+      dynts_status_t st = plan_extend(c, p, m, a.scratch, plan, &tc_grid);
+      if (st != DYNTS_OK) return st;
+    }
+    if (kv8) dynts::extend_store_kernel<__nv_bfloat16, true><<<grid, 256, 0, c->stream>>>(p, plan);
+    else if (f.dtype == DYNTS_FP32) dynts::extend_store_kernel<float, false><<<grid, 256, 0, c->stream>>>(p, plan);
+    else dynts::extend_store_kernel<__nv_bfloat16, false><<<grid, 256, 0, c->stream>>>(p, plan);
     CUDA_TRY(cudaGetLastError());
     c->launches += 1;
     p.published = p.publish;
-    dynts_status_t st = tc ? launch_extend_tc(c, p, m, a.scratch, want_mass)
+    dynts_status_t st = tc ? launch_extend_tc(c, p, plan, tc_grid, m, a.scratch, want_mass)
                         : kv8 ? launch_extend_generic<__nv_bfloat16, true>(c, p, want_mass)
                         : f.dtype == DYNTS_FP32 ? launch_extend_generic<float, false>(c, p, want_mass)
                                                 : launch_extend_generic<__nv_bfloat16, false>(c, p, want_mass);

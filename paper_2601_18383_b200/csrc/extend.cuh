@@ -73,6 +73,43 @@ struct ExtendParams {
   ExtendSeqs seqs;
 };
 
+// The tensor-core kernel's work, laid out by the storing kernel (which knows the lengths on the device and runs before
+// it anyway): an item = (tile of query rows, KV head, layer, sequence); all items' key tiles form one list, of which
+// every CTA takes an equal contiguous piece.  The list is kept in shares: an item of sequence s counts per[s] shares
+// whatever its exact number of key tiles, a share's border inside an item is the same fraction of its key tiles.
+// CTA c takes the shares [c * q + min(c, rem), ...).  What CTA c does of item i is described by 32 words at slot i + c
+// (an item's parts and a CTA's pieces both lie side by side).
+constexpr int kPlanWords = 32;
+enum PlanWord { kPwTiles, kPwFirst, kPwTotal, kPwTok, kPwLayer, kPwHead, kPwHeld, kPwTok0, kPwRows, kPwNew, kPwSlab, kPwParts, kPwPlace, kPwBase, kPwCounter, kPwList, kPwPrefix, kPwSeen };
+struct ExtendPlan {
+  unsigned cum[kExtSeqs + 1];  // shares before each sequence's first item
+  unsigned per[kExtSeqs];      // shares of an item
+  int tiles[kExtSeqs];         // tiles of query rows per (layer, KV head)
+  int item0[kExtSeqs + 1];     // items before each sequence's
+  unsigned share_q, share_rem; // shares per CTA: share_q, one more for the first share_rem
+  int tokens_per_tile;         // floor(128 / G)
+  int lh;                      // n_layers * Hkv
+  int* words;                  // [items + CTAs][kPlanWords], or NULL: no plan is wanted
+};
+__device__ __forceinline__ unsigned plan_share0(const ExtendPlan& p, unsigned cta) { return cta * p.share_q + min(cta, p.share_rem); }
+__device__ __forceinline__ unsigned plan_cta_of(const ExtendPlan& p, unsigned share) {
+  const unsigned big = p.share_rem * (p.share_q + 1u);
+  return share < big ? share / (p.share_q + 1u) : p.share_rem + (share - big) / p.share_q;
+}
+__device__ __forceinline__ int plan_item_of(const ExtendPlan& p, int n_seq, unsigned share) {
+  int lo = 0, hi = n_seq;
+  while (hi - lo > 1) {  // the last sequence that begins at or before the share
+    const int mid = (lo + hi) >> 1;
+    if (p.cum[mid] <= share) lo = mid;
+    else hi = mid;
+  }
+  return p.item0[lo] + (int)((share - p.cum[lo]) / p.per[lo]);
+}
+// total * a / per, in 32 bits where that is enough (a 64-bit division takes several hundred cycles)
+__device__ __forceinline__ int plan_part(unsigned total, unsigned a, unsigned per) {
+  return (int)((total | a) < 65536u ? total * a / per : (unsigned)((unsigned long long)total * a / per));
+}
+
 __device__ __forceinline__ int ext_find(const int* first, int n, int x) {  // the s with first[s] <= x < first[s + 1]
   int lo = 0, hi = n;
   while (hi - lo > 1) {
@@ -106,8 +143,69 @@ __device__ __forceinline__ ExtSeq ext_seq(const ExtendParams& p, int s) {
 // Stores the chunk's rows: K and V (encoded for 8-bit slabs), position, score; with `publish` the
 // last CTA to finish advances the lengths.  Bandwidth-bound and short: a row is read and written once.
 // Grid: x over the 16-byte pieces of the tokens' rows, y over (layer, KV head).
+// The tensor-core kernel's plan: a warp per item, a lane per part.
+__device__ __forceinline__ void ext_write_plan(const ExtendParams& p, const ExtendPlan& q, int warp, int n_warps) {
+  const int lane = threadIdx.x & 31;
+  for (int item = warp; item < q.item0[p.seqs.n]; item += n_warps) {
+    const int s = ext_find(q.item0, p.seqs.n, item);
+    const int idx = item - q.item0[s], nq = q.tiles[s], lh = idx / nq, o = idx - lh * nq;
+    // tiles from both ends in turn: neighbours in the list hold about as many key tiles together as any other two
+    const int qt = (o & 1) ? nq - 1 - (o >> 1) : o >> 1;
+    const int b = p.seqs.b0 + s, t = p.seqs.tok0[s + 1] - p.seqs.tok0[s], n = p.len[b], prefix = p.seqs.prefix[s];
+    const int i0 = qt * q.tokens_per_tile, i1 = min(t, i0 + q.tokens_per_tile);
+    const bool ok = n >= 0 && n + t <= p.cap;  // (else nothing is stored and nothing computed)
+    const int seen = n + max(i1, prefix);
+    // (positions ascend with the rows, so a row more than `window` rows back is more than `window` positions back)
+    const int first = p.window > 0 ? max(0, n + i0 - p.window + 1) / kExtTileKeys : 0;
+    const int total = (seen + kExtTileKeys - 1) / kExtTileKeys - first;
+    const unsigned per = q.per[s], start = q.cum[s] + (unsigned)idx * per;
+    const unsigned ca = plan_cta_of(q, start), cb = plan_cta_of(q, start + per - 1u);
+    const int layer = lh / p.Hkv, h = lh - layer * p.Hkv;
+    int count = 0;
+    for (int pass = 0; pass < 2; ++pass) {  // how many parts hold any key tile; then the words
+      int rank = 0;
+      for (unsigned c0 = ca; c0 <= cb; c0 += 32) {
+        const unsigned c = c0 + (unsigned)lane;
+        int lo = 0, hi = 0;
+        if (c <= cb && ok) {
+          const unsigned v0 = plan_share0(q, c), v1 = plan_share0(q, c + 1u);
+          const unsigned a = v0 > start ? v0 - start : 0u, e = v1 - start < per ? v1 - start : per;
+          lo = a == 0u ? 0 : plan_part((unsigned)total, a, per);
+          hi = e == per ? total : plan_part((unsigned)total, e, per);
+        }
+        const unsigned has = __ballot_sync(0xffffffffu, lo < hi);
+        if (pass == 1 && c <= cb) {
+          int* w = q.words + (size_t)(item + (int)c) * kPlanWords;
+          // A CTA has two places for parts: one for an item that began before its shares, one for an item that begins in them.
+          const int place = (int)(2u * c) + (c == ca ? 1 : 0);
+          if (lo < hi) q.words[(size_t)(item + (int)ca + rank + __popc(has & ((1u << lane) - 1u))) * kPlanWords + kPwList] = place;
+          w[kPwTiles] = hi - lo;
+          w[kPwFirst] = first + lo;
+          w[kPwTotal] = total;
+          w[kPwTok] = p.seqs.tok0[s] + i0;
+          w[kPwLayer] = layer;
+          w[kPwHead] = h;
+          w[kPwHeld] = n;
+          w[kPwTok0] = i0;
+          w[kPwRows] = (i1 - i0) * p.G;
+          w[kPwNew] = t;
+          w[kPwSlab] = ((p.layer0 + layer) * p.Nb + b) * p.Hkv + h;
+          w[kPwParts] = count;
+          w[kPwPlace] = place;
+          w[kPwBase] = item + (int)ca;
+          w[kPwCounter] = (int)ca;
+          w[kPwPrefix] = prefix;
+          w[kPwSeen] = p.tot[b];
+        }
+        rank += __popc(has);
+      }
+      count = rank;
+    }
+  }
+}
+
 template <typename T, bool KV8>
-__global__ void __launch_bounds__(256) extend_store_kernel(const __grid_constant__ ExtendParams p) {
+__global__ void __launch_bounds__(256) extend_store_kernel(const __grid_constant__ ExtendParams p, const __grid_constant__ ExtendPlan plan) {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // the next kernel's set-up may begin; it waits for this grid before it reads
   constexpr int E = 16 / (int)sizeof(T);  // elements per 16-byte piece of the source
   const unsigned pieces = (unsigned)p.d / E;
@@ -150,6 +248,10 @@ __global__ void __launch_bounds__(256) extend_store_kernel(const __grid_constant
       p.score[row] = p.s_new ? p.s_new[tok] : 0.f;
       p.comp[row] = 0.f;
     }
+  }
+  if (plan.words) {
+    const int warps = (int)(gridDim.x * gridDim.y * blockDim.x / 32);
+    ext_write_plan(p, plan, (int)((blockIdx.y * gridDim.x + blockIdx.x) * (blockDim.x / 32) + threadIdx.x / 32), warps);
   }
   if (blockIdx.y == 0)
     for (unsigned w = first; w < (unsigned)p.n_counters; w += stride) p.counters[w] = 0u;

@@ -24,7 +24,11 @@
 // (From the newest tile on, because a distance bias only lowers the logits of older rows, and a window hides the oldest.)
 //
 // Warps: 0-3 and 4-7 the two groups, 8 loads Q and K, 9 loads V, 10 issues S, 11 issues O; they meet through mbarriers as
-// in the prompt attention (prefill_attn.cuh), the S buffer, stages and phases follow the flat tile index g.
+// in the prompt attention (prefill_attn.cuh), the S buffer, stages and phases follow the flat tile index g.  Every warp
+// walks the CTA's pieces by the plan the storing kernel wrote (extend.cuh), a word per lane, the next piece's
+// prefetched.  Two CTAs of 384 threads leave 80 registers per thread and hardly any L1: code that spills or does
+// not stay in the instruction caches cost several times its instructions, so the loops are rolled and the end of a piece
+// is a function of its own (4096 tokens behind 4096 rows: 453 us with cursors in registers and everything unrolled).
 //
 // Rows of 16 bits arrive by TMA from the slabs.  8-bit rows (KV8) are read as codes and widened into the same swizzled
 // tiles: K to f16 (exact; queries are an f16 copy made by the storing kernel) by the two loading warps, a tile ahead in
@@ -47,26 +51,16 @@ namespace dynts {
 
 constexpr int kXtThreads = 384;
 constexpr int kXtRows = 128;
-constexpr int kXtMaxCtas = 380;      // CTAs of a launch (two per SM); the list of an item's parts has room for so many
+constexpr int kXtMaxCtas = 380;      // CTAs of a launch (two per SM)
 constexpr int kXtPartFloats = 129;   // per query row of a part: 128 outputs, log-sum-exp
 constexpr float kXtHeadroom = 40.f;  // the reference lies so far (base-2 units) above the first tiles' maximum
 constexpr float kXtSumMax = 1.2676506e30f;  // 2^100: a row whose sum of weights exceeds it is computed again
 constexpr int kXtStageBytes = 1024;  // per softmax warp
-constexpr int kXtCursors = 12;       // a cursor per warp
-constexpr int kXtCursorInts = 14;
-constexpr int kXtSmemBytes = kPfQBytes + 4 * kPfKvBytes + 8 * kXtStageBytes + 128 + kExtSeqs * 4 + kXtCursors * kXtCursorInts * 4 + (2 + kXtMaxCtas) * 4;
+constexpr int kXtSmemBytes = kPfQBytes + 4 * kPfKvBytes + 8 * kXtStageBytes + 128 + 16;
 
-// The list of key tiles is kept in shares: an item of sequence s counts per[s] shares whatever its exact number of
-// key tiles (which the kernel takes from the lengths on the device), a share's border inside an item is the same
-// fraction of its key tiles.  CTA c takes the shares [c * q + min(c, rem), ...).
 struct ExtendTcParams {
   ExtendParams x;
-  unsigned cum[kExtSeqs + 1];  // shares before each sequence's first item
-  unsigned per[kExtSeqs];      // shares of an item
-  int tiles[kExtSeqs];         // tiles of query rows per (layer, KV head)
-  unsigned share_q, share_rem; // shares per CTA: share_q, one more for the first share_rem
-  int tokens_per_tile;  // floor(128 / G)
-  int lh;               // n_layers * Hkv
+  ExtendPlan plan;
   int part_rows;        // query rows a part's scratch has room for
   float* part;          // [2 per CTA]: [32][part_rows] float4, [part_rows] float
   int* stop;
@@ -74,103 +68,6 @@ struct ExtendTcParams {
   float cap_log2;       // c * log2(e)
   float cap_arg;        // 2 log2(e) * scale / c
 };
-
-// A piece of the list: what a CTA does of an item.  Every warp walks the pieces for itself; its cursor lies in shared
-// memory, since registers are what the kernel has least of.
-struct XtCursor {
-  int on;
-  int s, idx;             // sequence of the launch, item within it: (layer, KV head) slowest, tiles of query rows fastest
-  int ord;                // pieces of this CTA before this one
-  int nkt, kt0;           // key tiles of the piece (walked from the newest to the oldest), its first
-  int layer, h, n;        // rows held
-  int i0, rows;           // first token of the chunk, query rows
-  int total;              // key tiles of the item
-  int end;                // rows of the sequence, the chunk's included
-  int slab;
-};
-static_assert(sizeof(XtCursor) == kXtCursorInts * 4, "cursor size");
-
-__device__ __forceinline__ unsigned xt_share0(const ExtendTcParams& p, unsigned cta) { return cta * p.share_q + min(cta, p.share_rem); }
-// total * a / per, in 32 bits where that is enough (a 64-bit division takes several hundred cycles)
-__device__ __forceinline__ int xt_part(unsigned total, unsigned a, unsigned per) {
-  return (int)((total | a) < 65536u ? total * a / per : (unsigned)((unsigned long long)total * a / per));
-}
-// Key tiles [lo, hi) of an item (total key tiles, shares [start, start + per)) that fall to the shares [v0, v1).
-__device__ __forceinline__ void xt_piece(unsigned v0, unsigned v1, unsigned start, unsigned per, int total, int& lo, int& hi) {
-  const unsigned a = v0 > start ? v0 - start : 0u, e = v1 - start < per ? v1 - start : per;
-  lo = a == 0u ? 0 : xt_part((unsigned)total, a, per);
-  hi = e == per ? total : xt_part((unsigned)total, e, per);
-}
-
-// The first piece of this CTA at or behind item c.idx of sequence c.s that holds any key tile.  The whole warp.
-__device__ __noinline__ void xt_settle(XtCursor* at, const ExtendTcParams& p, const int* s_n) {
-  XtCursor c = *at;
-  const unsigned v0 = xt_share0(p, blockIdx.x), v1 = xt_share0(p, blockIdx.x + 1u);
-  c.on = 0;
-  while (c.s < p.x.seqs.n) {
-    const int nq = p.tiles[c.s];
-    c.n = s_n[c.s];
-    if (c.n < 0 || c.idx >= nq * p.lh) {  // (no room for the chunk: nothing was stored)
-      ++c.s;
-      c.idx = 0;
-      continue;
-    }
-    const unsigned per = p.per[c.s], start = p.cum[c.s] + (unsigned)c.idx * per;
-    if (start >= v1) break;
-    const int lh = nq == 1 ? c.idx : c.idx / nq, o = c.idx - lh * nq;
-    // tiles from both ends in turn: neighbours in the list hold about as many key tiles together as any other two
-    const int qt = (o & 1) ? nq - 1 - (o >> 1) : o >> 1;
-    const int t = p.x.seqs.tok0[c.s + 1] - p.x.seqs.tok0[c.s];
-    c.i0 = qt * p.tokens_per_tile;
-    const int i1 = min(t, c.i0 + p.tokens_per_tile);
-    const int seen = c.n + max(i1, p.x.seqs.prefix[c.s]);
-    // (positions ascend with the rows, so a row more than `window` rows back is more than `window` positions back)
-    const int b0 = p.x.window > 0 ? max(0, c.n + c.i0 - p.x.window + 1) / kPfKeys : 0;
-    c.total = (seen + kPfKeys - 1) / kPfKeys - b0;
-    int lo, hi;
-    xt_piece(v0, v1, start, per, c.total, lo, hi);
-    if (lo < hi) {
-      c.rows = (i1 - c.i0) * p.x.G;
-      c.kt0 = b0 + lo;
-      c.nkt = hi - lo;
-      c.layer = p.x.n_layers == 1 ? 0 : lh / p.x.Hkv;
-      c.h = lh - c.layer * p.x.Hkv;
-      c.end = c.n + t;
-      c.slab = ((p.x.layer0 + c.layer) * p.x.Nb + p.x.seqs.b0 + c.s) * p.x.Hkv + c.h;
-      c.on = 1;
-      break;
-    }
-    ++c.idx;
-  }
-  __syncwarp();
-  if ((threadIdx.x & 31) == 0) *at = c;
-  __syncwarp();
-}
-// Where this CTA's shares begin (needs no lengths); xt_settle then finds its first piece.
-__device__ __forceinline__ void xt_begin(XtCursor* at, const ExtendTcParams& p) {
-  const unsigned v0 = xt_share0(p, blockIdx.x);
-  int lo = 0, hi = p.x.seqs.n;
-  while (hi - lo > 1) {  // the last sequence that begins at or before the first share
-    const int mid = (lo + hi) >> 1;
-    if (p.cum[mid] <= v0) lo = mid;
-    else hi = mid;
-  }
-  if ((threadIdx.x & 31) == 0) {
-    at->s = lo;
-    at->idx = (int)((v0 - p.cum[lo]) / p.per[lo]);
-    at->ord = 0;
-  }
-  __syncwarp();
-}
-__device__ __forceinline__ void xt_next(XtCursor* at, const ExtendTcParams& p, const int* s_n) {
-  __syncwarp();
-  if ((threadIdx.x & 31) == 0) {
-    ++at->ord;
-    ++at->idx;
-  }
-  __syncwarp();
-  xt_settle(at, p, s_n);
-}
 
 __device__ __forceinline__ float rcp_approx(float x) {
   float y;
@@ -239,25 +136,25 @@ __device__ __forceinline__ void xt_store_codes(const XtCodes& r, uint8_t* tile, 
   }
 }
 
-// One query row again, by a whole warp, from the visible rows of [k0, k1) alone.  redo: lse is computed too (with the
+// One query row again, by a whole warp, from the visible rows of the piece alone.  redo: lse is computed too (with the
 // true maximum); else the caller's is taken.  Returns the output over out_scale, lane = four columns.  For rows whose
 // fast result is not finite: a hidden row held something that is not, the weights' sum left its range, or the answer
-// is in truth not finite.
+// is in truth not finite.  d: the piece's words, one per lane.
 template <bool KV8>
-__device__ __noinline__ float4 xt_row_again(const ExtendTcParams& p, const XtCursor& c, int r, bool redo, float& lse) {
+__device__ __noinline__ float4 xt_row_again(const ExtendTcParams& p, int d, int r, bool redo, float& lse) {
   const ExtendParams& x = p.x;
-  const int lane = threadIdx.x & 31, b = x.seqs.b0 + c.s, t = x.seqs.tok0[c.s + 1] - x.seqs.tok0[c.s];
-  const int i = c.i0 + r / x.G, g = r % x.G;
-  const size_t slab = ((size_t)(x.layer0 + c.layer) * x.Nb + b) * x.Hkv + c.h;
-  const __nv_bfloat16* q =
-      static_cast<const __nv_bfloat16*>(x.q) + ((size_t)c.layer * x.total + x.seqs.tok0[c.s] + i) * x.q_stride + (size_t)(c.h * x.G + g) * 128;
-  const int tot = x.tot[b] - (x.published ? t : 0);
-  const float slope = x.slopes ? x.slopes[c.h * x.G + g] : 0.f;
-  const int k0 = c.kt0 * kPfKeys, end = min((c.kt0 + c.nkt) * kPfKeys, c.n + max(i + 1, x.seqs.prefix[c.s]));
+  auto word = [&](int w) { return __shfl_sync(0xffffffffu, d, w); };
+  const int lane = threadIdx.x & 31;
+  const int ti = r / x.G, g = r - ti * x.G, h = word(kPwHead), layer = word(kPwLayer), i = word(kPwTok0) + ti;
+  const size_t slab = (size_t)word(kPwSlab);
+  const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(x.q) + ((size_t)layer * x.total + word(kPwTok) + ti) * x.q_stride + (size_t)(h * x.G + g) * 128;
+  const int me = word(kPwSeen) + i;
+  const float slope = x.slopes ? x.slopes[h * x.G + g] : 0.f;
+  const int kt0 = word(kPwFirst), k0 = kt0 * kPfKeys, end = min((kt0 + word(kPwTiles)) * kPfKeys, word(kPwHeld) + max(i + 1, word(kPwPrefix)));
   auto logit = [&](int j, bool& visible) {
     visible = false;
     if (j >= end) return 0.f;
-    const int apart = abs(tot + i - x.pos[slab * x.cap + j]);
+    const int apart = abs(me - x.pos[slab * x.cap + j]);
     if (x.window > 0 && apart >= x.window) return 0.f;
     visible = true;
     float dot = 0.f;
@@ -296,6 +193,204 @@ __device__ __noinline__ float4 xt_row_again(const ExtendTcParams& p, const XtCur
   return make_float4(acc[0], acc[1], acc[2], acc[3]);
 }
 
+// The last CTA to finish a part of an item joins the parts, eight warps.  A warp takes 8 rows x 64 columns at a time, a
+// lane four pieces of four columns of one row: 128-byte pieces of every part, whole sectors of the output.  Running
+// maximum and sum over the parts, in the order of the list.
+__device__ __noinline__ void xt_join_parts(const ExtendTcParams& p, int d, float out_scale, volatile int* s_abort) {
+  const ExtendParams& x = p.x;
+  auto word = [&](int w) { return __shfl_sync(0xffffffffu, d, w); };
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int rows = word(kPwRows), n_parts = word(kPwParts), h = word(kPwHead), layer = word(kPwLayer), tok = word(kPwTok);
+  const int* list = p.plan.words + (size_t)word(kPwBase) * kPlanWords + kPwList;
+  const size_t piece = (size_t)p.part_rows;
+  __nv_bfloat16* obase = static_cast<__nv_bfloat16*>(x.out) + (((size_t)layer * x.total + tok) * x.Hq + h * x.G) * 128;
+  const int units = (rows + 7) / 8 * 2;
+  for (int u = warp; u < units; u += 8) {
+    const int row = (u >> 1) * 8 + (lane >> 2), c4 = (u & 1) * 16 + (lane & 3);
+    if (row >= rows || *s_abort) continue;
+    float M = -CUDART_INF_F, sum = 0.f, acc[16];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) acc[e] = 0.f;
+#pragma unroll 2
+    for (int k = 0; k < n_parts; ++k) {
+      const float* src = p.part + (size_t)__ldcg(list + (size_t)k * kPlanWords) * (piece * kXtPartFloats);
+      const float lk = __ldcg(src + 128 * piece + row);
+      float4 y[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) y[e] = __ldcg(reinterpret_cast<const float4*>(src) + (size_t)(c4 + 4 * e) * piece + row);
+      const float Mn = fmaxf(M, lk);
+      const float keep = M == -CUDART_INF_F ? 0.f : fast_exp2(M - Mn), wk = lk == -CUDART_INF_F ? 0.f : fast_exp2(lk - Mn);
+      M = Mn;
+      sum = fmaf(sum, keep, wk);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        acc[4 * e] = fmaf(acc[4 * e], keep, wk * y[e].x);
+        acc[4 * e + 1] = fmaf(acc[4 * e + 1], keep, wk * y[e].y);
+        acc[4 * e + 2] = fmaf(acc[4 * e + 2], keep, wk * y[e].z);
+        acc[4 * e + 3] = fmaf(acc[4 * e + 3], keep, wk * y[e].w);
+      }
+    }
+    const float fs = out_scale / sum;
+    const int ti = row / x.G;
+    __nv_bfloat16* dst = obase + ((size_t)ti * x.Hq + (row - ti * x.G)) * 128;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      *reinterpret_cast<uint2*>(dst + (c4 + 4 * e) * 4) =
+          make_uint2(pack_bf16x2(acc[4 * e] * fs, acc[4 * e + 1] * fs), pack_bf16x2(acc[4 * e + 2] * fs, acc[4 * e + 3] * fs));
+    if (c4 == 0 && x.lse) x.lse[ext_lse_index(x, layer, h, tok) + row] = M + __log2f(sum);
+  }
+}
+
+// The end of a piece, by the eight softmax warps: a group's 64 columns of the output, or of its part of an item that
+// other CTAs share.  If every other part already lies in the scratch (and they are few), this CTA joins them with
+// its own still in tensor memory; else it leaves its part, and joins all if it turns out to be the last.
+template <bool KV8>
+__device__ __noinline__ void xt_epilogue(const ExtendTcParams& p, int d, int ord, float ref, float l, uint32_t tO, uint32_t bar0, volatile int* s_abort,
+                                         uint8_t* s_out, int* s_flag) {
+  const ExtendParams& x = p.x;
+  auto word = [&](int w) { return __shfl_sync(0xffffffffu, d, w); };
+  auto all_sync = [&]() { asm volatile("bar.sync 1, 256;" ::: "memory"); };
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, wg = warp >> 2, wq = warp & 3;
+  const int r = wq * 32 + lane, rows = word(kPwRows), n_parts = word(kPwParts), h = word(kPwHead), layer = word(kPwLayer), tok = word(kPwTok);
+  const uint32_t g_inv = 65536u / (uint32_t)x.G + 1u;
+  uint8_t* stage = s_out + warp * kXtStageBytes;
+  const float out_scale = KV8 ? x.v_scale : 1.f;
+  const bool live = wq * 32 < rows, mine = r < rows, whole = n_parts == 1;
+  const size_t piece = (size_t)p.part_rows;
+  float* part = p.part + (size_t)word(kPwPlace) * (piece * kXtPartFloats);
+  const int* list = p.plan.words + (size_t)word(kPwBase) * kPlanWords + kPwList;
+  unsigned* counter = x.counters + word(kPwCounter);
+  bool join = false;
+  if (n_parts == 2) {  // (with more, the joint by all warps is faster than one thread per row)
+    if (tid == 0) {
+      unsigned done;
+      asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(done) : "l"(counter) : "memory");
+      *s_flag = done == 1u;
+    }
+    all_sync();
+    join = *s_flag != 0;
+  }
+  mbar_wait(bar0 + 8 * 12, (uint32_t)(ord & 1), s_abort, x.err, kPfSpinLimit);
+  tc5::fence_after_sync();
+  if (live) {
+    const bool redo = mine && !(l < kXtSumMax);  // out of range, or not a number
+    float lse = l > 0.f ? ref + __log2f(l) : -CUDART_INF_F;
+    const float f = l > 0.f ? 1.f / l : 0.f;
+    float w_own = 1.f, w_other = 0.f, all = lse;
+    const float* other = nullptr;
+    bool weighed = false;
+    __nv_bfloat16* obase = static_cast<__nv_bfloat16*>(x.out) + (((size_t)layer * x.total + tok) * x.Hq + h * x.G) * 128;
+    const uint32_t t_row = tO + ((uint32_t)(wq * 32) << 16);
+#pragma unroll 1
+    for (int c0 = 64 * wg; c0 < 64 * wg + 64; c0 += 16) {
+      uint32_t o[16];
+      tc5::tmem_ld16(t_row + (uint32_t)c0, o);
+      tc5::tmem_wait_ld();
+      if (c0 == 64 * wg + 48) {
+        tc5::fence_before_sync();
+        mbar_arrive(bar0 + 8 * 7);  // O may be written again
+      }
+      float probe = 0.f;  // 0 * finite = 0
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+        probe = fmaf(__uint_as_float(o[e]), 0.f, probe);
+      }
+      unsigned again = __ballot_sync(0xffffffffu, mine && (redo || !(probe == 0.f)));
+      while (again) {
+        const int who = __ffs(again) - 1;
+        again &= again - 1;
+        const bool full = __shfl_sync(0xffffffffu, redo ? 1 : 0, who) != 0;
+        float new_lse = __shfl_sync(0xffffffffu, lse, who);
+        const float4 y = xt_row_again<KV8>(p, d, wq * 32 + who, full, new_lse);
+        __syncwarp();
+        reinterpret_cast<float4*>(stage)[lane] = y;
+        __syncwarp();
+        if (lane == who) {
+          lse = new_lse;
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            if (full || !(__uint_as_float(o[e]) * 0.f == 0.f)) o[e] = reinterpret_cast<const uint32_t*>(stage)[c0 + e];
+        }
+        __syncwarp();
+      }
+      if (!weighed) {
+        weighed = true;
+        all = lse;
+        if (join) {  // (the sum is symmetric: whoever joins gets the same)
+          const int a = __ldcg(list), b = __ldcg(list + kPlanWords), mine_at = word(kPwPlace);
+          other = p.part + (size_t)(a == mine_at ? b : a) * (piece * kXtPartFloats) + (size_t)min(r, rows - 1) * 4;
+          const float lo = __ldcg(other - (size_t)min(r, rows - 1) * 3 + 128 * piece);
+          const float M = fmaxf(lse, lo);
+          if (M > -CUDART_INF_F) {
+            all = M + __log2f((lse == -CUDART_INF_F ? 0.f : exp2f(lse - M)) + (lo == -CUDART_INF_F ? 0.f : exp2f(lo - M)));
+            w_own = lse == -CUDART_INF_F ? 0.f : fast_exp2(lse - all);
+            w_other = lo == -CUDART_INF_F ? 0.f : fast_exp2(lo - all);
+          } else {  // (not a number on one side: it stays one)
+            all = lse + lo;
+          }
+        }
+      }
+      if (join) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float4 y = __ldcg(reinterpret_cast<const float4*>(other + ((size_t)c0 / 4 + e) * piece * 4));
+          o[4 * e] = __float_as_uint(fmaf(w_other, y.x, w_own * __uint_as_float(o[4 * e])));
+          o[4 * e + 1] = __float_as_uint(fmaf(w_other, y.y, w_own * __uint_as_float(o[4 * e + 1])));
+          o[4 * e + 2] = __float_as_uint(fmaf(w_other, y.z, w_own * __uint_as_float(o[4 * e + 2])));
+          o[4 * e + 3] = __float_as_uint(fmaf(w_other, y.w, w_own * __uint_as_float(o[4 * e + 3])));
+        }
+      }
+      if (whole || join) {
+        // rounded, through the warp's staging tile [32 rows][32 B] (16-byte chunks swizzled), so that the stores are whole
+        // sectors
+        uint32_t y[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y[e] = pack_bf16x2(__uint_as_float(o[2 * e]) * out_scale, __uint_as_float(o[2 * e + 1]) * out_scale);
+        const int sw = (lane >> 2) & 1;
+        *reinterpret_cast<uint4*>(stage + lane * 32 + (sw << 4)) = make_uint4(y[0], y[1], y[2], y[3]);
+        *reinterpret_cast<uint4*>(stage + lane * 32 + ((sw ^ 1) << 4)) = make_uint4(y[4], y[5], y[6], y[7]);
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int row = 16 * i + (lane >> 1), chunk = lane & 1;
+          const uint4 v = *reinterpret_cast<const uint4*>(stage + row * 32 + ((chunk ^ ((row >> 2) & 1)) << 4));
+          const int rr = wq * 32 + row, ti = (int)((uint32_t)rr * g_inv >> 16);
+          if (rr < rows && !*s_abort) *reinterpret_cast<uint4*>(obase + ((size_t)ti * x.Hq + (rr - ti * x.G)) * 128 + c0 + chunk * 8) = v;
+        }
+        __syncwarp();
+      } else if (mine && !*s_abort) {
+        float4* dst = reinterpret_cast<float4*>(part) + (size_t)c0 / 4 * piece + r;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          __stcg(dst + e * piece,
+                 make_float4(__uint_as_float(o[4 * e]), __uint_as_float(o[4 * e + 1]), __uint_as_float(o[4 * e + 2]), __uint_as_float(o[4 * e + 3])));
+      }
+    }
+    if (wg == 0 && mine && !*s_abort) {
+      if (!whole && !join) __stcg(part + 128 * piece + r, lse);
+      else if (x.lse) x.lse[ext_lse_index(x, layer, h, tok) + r] = all;
+    }
+  } else {
+    mbar_arrive(bar0 + 8 * 7);
+  }
+  if (whole) return;
+  if (join) {
+    all_sync();  // (the flag has been read by all)
+    return;
+  }
+  __threadfence();
+  all_sync();
+  if (tid == 0) *s_flag = atomicAdd(counter, 1u) == (unsigned)(n_parts - 1);
+  all_sync();
+  const bool last = *s_flag != 0;
+  if (last) {
+    __threadfence();
+    xt_join_parts(p, d, out_scale, s_abort);
+  }
+  all_sync();
+}
+
 template <bool KV8, bool MODS>
 __global__ void __launch_bounds__(kXtThreads, 2)
 extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
@@ -313,9 +408,7 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
   auto bar = [&](int i) { return bar0 + 8u * (uint32_t)i; };
   uint32_t* s_tmem = reinterpret_cast<uint32_t*>(bars + 15);
   volatile int* s_abort = reinterpret_cast<volatile int*>(s_tmem + 1);
-  int* s_n = reinterpret_cast<int*>(s_out + 8 * kXtStageBytes + 128);  // rows held by each sequence, -1: the chunk has no room
-  XtCursor* s_cur = reinterpret_cast<XtCursor*>(s_n + kExtSeqs);
-  int* s_list = reinterpret_cast<int*>(s_cur + kXtCursors);  // an item's parts: [0] the others are done, [1] parts, [2 ...] their places
+  int* s_flag = reinterpret_cast<int*>(s_tmem + 2);
   const ExtendParams& x = p.x;
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -340,20 +433,30 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
       asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&tmV)) : "memory");
     }
   }
-  XtCursor* const cur = s_cur + warp;
-  xt_begin(cur, p);
+  // This CTA's pieces: the items of its first and its last share (lanes 0 and 1), slots side by side.
+  const unsigned share = lane == 0 ? plan_share0(p.plan, blockIdx.x) : plan_share0(p.plan, blockIdx.x + 1u) - 1u;
+  const int item = plan_item_of(p.plan, x.seqs.n, share) + (int)blockIdx.x;
+  int slot = __shfl_sync(0xffffffffu, item, 0);
+  const int slot_end = __shfl_sync(0xffffffffu, item, 1) + 1;
   // The storing kernel may still be running; everything below waits until it has completed.
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  for (int s = tid; s < x.seqs.n; s += kXtThreads) {
-    const ExtSeq e = ext_seq(x, s);
-    s_n[s] = e.ok ? e.n : -1;
-  }
+  int d = __ldcg(p.plan.words + (size_t)slot * kPlanWords + lane);  // the piece's words, one per lane
   tc5::fence_before_sync();
   __syncthreads();
   tc5::fence_after_sync();
   const uint32_t tmem = *s_tmem;
   const uint32_t tS0 = tmem, tO = tmem + 128;  // S buffer b at column 64 b
-  xt_settle(cur, p, s_n);
+  auto word = [&](int w) { return __shfl_sync(0xffffffffu, d, w); };
+  // the next piece that holds any key tile; its words are asked for when a piece begins
+  int d_next = 0;
+  auto ask_next = [&]() {
+    if (slot + 1 < slot_end) d_next = __ldcg(p.plan.words + (size_t)(slot + 1) * kPlanWords + lane);
+  };
+  auto go_next = [&]() {
+    ++slot;
+    d = d_next;
+  };
+
   if (warp == 8 || warp == 9) {
     // ================= the warps that load: 8 Q and K, 9 V (8-bit rows: 8 Q and half of K, 9 the other half) =================
     if (lane == 0 && *reinterpret_cast<volatile int*>(p.stop) != 0) *s_abort = 1;
@@ -362,22 +465,37 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
     // a stage is filled again when the product that read it has completed: S of tile g - 2 (K), O += P V of it (V)
     const int freed = is_k ? 5 : 10, filled = is_k ? 1 : 3;
     const uint32_t base = is_k ? sK : sV;
-    XtCodes codes[4];
-    auto fetch = [&](int j) {  // 8-bit rows: this warp's 32 rows of the piece's tile j
-      const uint8_t* src = static_cast<const uint8_t*>(x.K) + (size_t)cur->slab * x.cap * 128;
-      const int k0 = (cur->kt0 + cur->nkt - 1 - j) * kPfKeys + 32 * (warp & 1), end = cur->end;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) xt_load_codes(codes[i], src, k0 + 8 * i, end, lane);
-      // (four tiles further on towards the older rows: asked into L2)
-      if (lane == 0 && j + 4 < cur->nkt)
-        asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(src + (size_t)(k0 - 4 * kPfKeys) * 128), "r"(32 * 128) : "memory");
-    };
     int g = 0;
-    while (cur->on && !*s_abort) {
-      const int nkt = cur->nkt;
-      if constexpr (KV8) fetch(0);
+    for (; slot < slot_end && !*s_abort; go_next()) {
+      ask_next();
+      const int nkt = word(kPwTiles), kt_new = word(kPwFirst) + nkt - 1, slab = word(kPwSlab), end = word(kPwHeld) + word(kPwNew);
+      XtCodes codes[4];
+      auto fetch = [&](int j) {  // 8-bit rows: this warp's 32 rows of the piece's tile j
+        const uint8_t* src = static_cast<const uint8_t*>(x.K) + (size_t)slab * x.cap * 128;
+        const int k0 = (kt_new - j) * kPfKeys + 32 * (warp & 1);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) xt_load_codes(codes[i], src, k0 + 8 * i, end, lane);
+        // (four tiles further on towards the older rows: asked into L2)
+        if (lane == 0 && j + 4 < nkt)
+          asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(src + (size_t)(k0 - 4 * kPfKeys) * 128), "r"(32 * 128) : "memory");
+      };
+      if constexpr (KV8) {
+        if (nkt > 0) fetch(0);
+      }
       for (int j = 0; j < nkt; ++j, ++g) {
-        if (g >= 2) mbar_wait(bar(freed + (g & 1)), (uint32_t)(((g - 2) >> 1) & 1), s_abort, x.err, kPfSpinLimit);
+        if (warp == 8 && j == 0) {
+          // the piece's Q, once the last S of the piece before has been computed from its own
+          if (g >= 1) mbar_wait(bar(5 + ((g - 1) & 1)), (uint32_t)(((g - 1) >> 1) & 1), s_abort, x.err, kPfSpinLimit);
+          const int tok = word(kPwLayer) * x.total + word(kPwTok), head = word(kPwHead) * x.G;
+          if (!*s_abort && tc5::elect_one()) {
+            mbar_arrive_expect_tx(bar(0), 256u * (uint32_t)(x.G * p.plan.tokens_per_tile));
+            pf_tma_load(sQ, &tmQ, 0, head, tok, bar(0));
+            pf_tma_load(sQ + kPfQBytes / 2, &tmQ, 64, head, tok, bar(0));
+          }
+          __syncwarp();
+        } else if (g >= 2) {
+          mbar_wait(bar(freed + (g & 1)), (uint32_t)(((g - 2) >> 1) & 1), s_abort, x.err, kPfSpinLimit);
+        }
         __syncwarp();
         if (*s_abort) break;
         const uint32_t bb = bar(filled + (g & 1));
@@ -392,26 +510,13 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
         } else if (tc5::elect_one()) {
           const uint32_t dst = base + (uint32_t)(g & 1) * kPfKvBytes;
           const CUtensorMap* tm = is_k ? &tmK : &tmV;
-          const int row = (cur->kt0 + nkt - 1 - j) * kPfKeys;
+          const int row = (kt_new - j) * kPfKeys;
           mbar_arrive_expect_tx(bb, kPfKvBytes);
-          pf_tma_load(dst, tm, 0, row, cur->slab, bb);
-          pf_tma_load(dst + kPfKvBytes / 2, tm, 64, row, cur->slab, bb);
+          pf_tma_load(dst, tm, 0, row, slab, bb);
+          pf_tma_load(dst + kPfKvBytes / 2, tm, 64, row, slab, bb);
         }
         __syncwarp();
-        if (warp == 8 && j == 0) {
-          // the piece's Q, once the last S of the piece before has been computed from its own
-          if (g >= 1) mbar_wait(bar(5 + ((g - 1) & 1)), (uint32_t)(((g - 1) >> 1) & 1), s_abort, x.err, kPfSpinLimit);
-          __syncwarp();
-          if (!*s_abort && tc5::elect_one()) {
-            const int tok = cur->layer * x.total + x.seqs.tok0[cur->s] + cur->i0, head = cur->h * x.G;
-            mbar_arrive_expect_tx(bar(0), 256u * (uint32_t)(x.G * p.tokens_per_tile));
-            pf_tma_load(sQ, &tmQ, 0, head, tok, bar(0));
-            pf_tma_load(sQ + kPfQBytes / 2, &tmQ, 64, head, tok, bar(0));
-          }
-          __syncwarp();
-        }
       }
-      xt_next(cur, p, s_n);
     }
     if (*s_abort && lane == 0) {
       // Something gave up: a bounded time for the loads this warp started (see prefill_attn.cuh).
@@ -427,9 +532,10 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
     // ================= the warp that issues O += P V =================
     constexpr uint32_t idesc_o = tc5::idesc_bf16_f32(kXtRows, 128, 0, 1);
     const uint64_t dV = tc5::smem_desc_sw128(sV, kPfKvBytes / 2, 1024);
-    int g = 0;
-    while (cur->on && !*s_abort) {
-      const int nkt = cur->nkt, ord = cur->ord;
+    int g = 0, ord = 0;
+    for (; slot < slot_end && !*s_abort; go_next()) {
+      ask_next();
+      const int nkt = word(kPwTiles);
       for (int j = 0; j < nkt; ++j, ++g) {
         const int st = g & 1;
         if constexpr (!KV8) mbar_wait(bar(3 + st), (uint32_t)((g >> 1) & 1), s_abort, x.err, kPfSpinLimit);  // (8-bit rows: written before P)
@@ -448,7 +554,7 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
         }
         __syncwarp();
       }
-      xt_next(cur, p, s_n);
+      if (nkt > 0) ++ord;
     }
     if (*s_abort && tc5::elect_one()) {
       // give the MMAs already issued a bounded time to finish before the tensor memory is released
@@ -462,9 +568,10 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
     constexpr uint32_t idesc_s = KV8 ? tc5::idesc_f16_f32(kXtRows, kPfKeys, 0, 0) : tc5::idesc_bf16_f32(kXtRows, kPfKeys, 0, 0);
     const uint64_t dQ = tc5::smem_desc_sw128(sQ, 16, 1024);
     const uint64_t dK = tc5::smem_desc_sw128(sK, 16, 1024);
-    int g = 0;
-    while (cur->on && !*s_abort) {
-      const int nkt = cur->nkt, ord = cur->ord;
+    int g = 0, ord = 0;
+    for (; slot < slot_end && !*s_abort; go_next()) {
+      ask_next();
+      const int nkt = word(kPwTiles);
       for (int j = 0; j < nkt; ++j, ++g) {
         const int st = g & 1;
         mbar_wait(bar(1 + st), (uint32_t)((g >> 1) & 1), s_abort, x.err, kPfSpinLimit);
@@ -484,7 +591,7 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
         }
         __syncwarp();
       }
-      xt_next(cur, p, s_n);
+      if (nkt > 0) ++ord;
     }
     if (*s_abort && tc5::elect_one()) {
       atomicOr(p.stop, 1);
@@ -495,251 +602,46 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
   } else {
     // ================= softmax warps: thread = query row = tensor-memory lane =================
     const int wg = warp >> 2, wq = warp & 3;              // group; warp within it (its lanes of tensor memory)
-    const uint32_t lane_base = (uint32_t)(wq * 32) << 16;
-    const uint32_t g_inv = 65536u / (uint32_t)x.G + 1u;  // r / G == r * g_inv >> 16 for r < 128
     uint8_t* stage = s_out + warp * kXtStageBytes;
-    const uint8_t* stage_other = s_out + (warp ^ 4) * kXtStageBytes;  // the warp of the other group with the same rows
-    const int r = wq * 32 + lane;                         // query row within the tile
-    const int ri = (int)((uint32_t)r * g_inv >> 16), rg = r - ri * x.G;
+    const float* stage_other = reinterpret_cast<const float*>(s_out + (warp ^ 4) * kXtStageBytes);  // the warp of the other group with the same rows
+    const uint32_t t_row = tS0 + ((uint32_t)(wq * 32) << 16);
     auto pair_sync = [&]() { asm volatile("bar.sync %0, 64;" ::"r"(2 + wq) : "memory"); };
-    auto all_sync = [&]() { asm volatile("bar.sync 1, 256;" ::: "memory"); };
-
-    // The end of a piece: this group's 64 columns of the output, or of its part of an item that other CTAs share.
-    auto epilogue = [&](float ref, float l) {
-      const XtCursor& c = *cur;
-      const float out_scale = KV8 ? x.v_scale : 1.f;
-      const int rows = c.rows;
-      const bool live = wq * 32 < rows, mine = r < rows, whole = c.nkt == c.total;
-      // A part: [32 pieces of four columns][part_rows] float4, then [part_rows] log-sum-exps.  A CTA has two places, one for
-      // an item that began before its shares and one for an item that begins in them.
-      const size_t piece = (size_t)p.part_rows;
-      auto part_of = [&](int place) { return p.part + (size_t)place * (piece * kXtPartFloats); };
-      unsigned first_cta = 0;  // (warp 0)
-      int place = 0, n_parts = 1;
-      bool join = false;       // every other part lies in the scratch: this CTA joins them, with its own still in tensor memory
-      if (!whole) {
-        const unsigned per = p.per[c.s], start = p.cum[c.s] + (unsigned)c.idx * per;
-        place = (int)(2u * blockIdx.x + (start >= xt_share0(p, blockIdx.x) ? 1u : 0u));
-        all_sync();  // (the list of a piece before has been read)
-        if (warp == 0) {
-          auto cta_of = [&](unsigned v) {
-            const unsigned big = p.share_rem * (p.share_q + 1u);
-            return v < big ? v / (p.share_q + 1u) : p.share_rem + (v - big) / p.share_q;
-          };
-          first_cta = cta_of(start);
-          const unsigned cb = cta_of(start + per - 1u);
-          int count = 0;
-          for (unsigned c0 = first_cta; c0 <= cb; c0 += 32) {
-            const unsigned cc = c0 + (unsigned)lane;
-            int lo = 0, hi = 0;
-            if (cc <= cb) xt_piece(xt_share0(p, cc), xt_share0(p, cc + 1u), start, per, c.total, lo, hi);
-            const unsigned has = __ballot_sync(0xffffffffu, lo < hi);
-            if (lo < hi) s_list[2 + count + __popc(has & ((1u << lane) - 1u))] = (int)(2u * cc + (start >= xt_share0(p, cc) ? 1u : 0u));
-            count += __popc(has);
-          }
-          if (lane == 0) {
-            unsigned done;
-            asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(done) : "l"(x.counters + first_cta) : "memory");
-            s_list[1] = count;
-            s_list[0] = done == (unsigned)(count - 1);
-          }
-        }
-        all_sync();
-        n_parts = s_list[1];
-        // (with many parts the joint below, which spreads them over the warps, is faster than one thread per row)
-        join = n_parts <= 3 && s_list[0];
-      }
-      mbar_wait(bar(12), (uint32_t)(c.ord & 1), s_abort, x.err, kPfSpinLimit);
-      tc5::fence_after_sync();
-      __nv_bfloat16* obase = static_cast<__nv_bfloat16*>(x.out) + (((size_t)c.layer * x.total + x.seqs.tok0[c.s] + c.i0) * x.Hq + c.h * x.G) * 128;
-      float* lse_out = x.lse ? x.lse + ext_lse_index(x, c.layer, c.h, x.seqs.tok0[c.s] + c.i0) : nullptr;
-      if (live) {
-        const bool redo = mine && !(l < kXtSumMax);  // out of range, or not a number
-        float lse = l > 0.f ? ref + __log2f(l) : -CUDART_INF_F;
-        const float f = l > 0.f ? 1.f / l : 0.f;
-        float all = lse, w_own = 1.f, w[3] = {0.f, 0.f, 0.f};
-        bool joined = false;
-#pragma unroll 1
-        for (int c0 = 64 * wg; c0 < 64 * wg + 64; c0 += 16) {
-          uint32_t o[16];
-          tc5::tmem_ld16(tO + lane_base + (uint32_t)c0, o);
-          tc5::tmem_wait_ld();
-          if (c0 == 64 * wg + 48) {
-            tc5::fence_before_sync();
-            mbar_arrive(bar(7));  // O may be written again
-          }
-          float probe = 0.f;  // 0 * finite = 0
-#pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
-            probe = fmaf(__uint_as_float(o[e]), 0.f, probe);
-          }
-          unsigned again = __ballot_sync(0xffffffffu, mine && (redo || !(probe == 0.f)));
-          while (again) {
-            const int who = __ffs(again) - 1;
-            again &= again - 1;
-            const bool full = __shfl_sync(0xffffffffu, redo ? 1 : 0, who) != 0;
-            float new_lse = __shfl_sync(0xffffffffu, lse, who);
-            const float4 y = xt_row_again<KV8>(p, c, wq * 32 + who, full, new_lse);
-            __syncwarp();
-            reinterpret_cast<float4*>(stage)[lane] = y;
-            __syncwarp();
-            if (lane == who) {
-              lse = new_lse;
-              if (!joined) all = lse;
-#pragma unroll
-              for (int e = 0; e < 16; ++e)
-                if (full || !(__uint_as_float(o[e]) * 0.f == 0.f)) o[e] = reinterpret_cast<const uint32_t*>(stage)[c0 + e];
-            }
-            __syncwarp();
-          }
-          if (join) {
-            const int rr = min(r, rows - 1);
-            if (!joined) {  // in the order of the list, whoever joins: maximum, sum and weights of the parts
-              joined = true;
-              float M = -CUDART_INF_F, y[3];
-#pragma unroll
-              for (int k = 0; k < 3; ++k) {
-                y[k] = -CUDART_INF_F;
-                if (k < n_parts) y[k] = s_list[2 + k] == place ? lse : __ldcg(part_of(s_list[2 + k]) + 128 * piece + rr);
-                M = fmaxf(M, y[k]);
-              }
-              float sum = 0.f;
-#pragma unroll
-              for (int k = 0; k < 3; ++k) sum += y[k] == -CUDART_INF_F ? 0.f : exp2f(y[k] - M);
-              all = M + __log2f(sum);
-#pragma unroll
-              for (int k = 0; k < 3; ++k) {
-                w[k] = y[k] == -CUDART_INF_F ? 0.f : fast_exp2(y[k] - all);
-                if (k < n_parts && s_list[2 + k] == place) {
-                  w_own = w[k];
-                  w[k] = -1.f;
-                }
-              }
-            }
-#pragma unroll
-            for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * w_own);
-#pragma unroll
-            for (int k = 0; k < 3; ++k) {
-              if (k >= n_parts || w[k] < 0.f) continue;
-              const float4* src = reinterpret_cast<const float4*>(part_of(s_list[2 + k])) + (size_t)c0 / 4 * piece + rr;
-#pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                const float4 y = __ldcg(src + e * piece);
-                o[4 * e] = __float_as_uint(fmaf(w[k], y.x, __uint_as_float(o[4 * e])));
-                o[4 * e + 1] = __float_as_uint(fmaf(w[k], y.y, __uint_as_float(o[4 * e + 1])));
-                o[4 * e + 2] = __float_as_uint(fmaf(w[k], y.z, __uint_as_float(o[4 * e + 2])));
-                o[4 * e + 3] = __float_as_uint(fmaf(w[k], y.w, __uint_as_float(o[4 * e + 3])));
-              }
-            }
-          }
-          if (whole || join) {
-            // rounded, through the warp's staging tile [32 rows][32 B] (16-byte chunks swizzled), so that the stores are whole
-            // sectors
-            uint32_t y[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) y[e] = pack_bf16x2(__uint_as_float(o[2 * e]) * out_scale, __uint_as_float(o[2 * e + 1]) * out_scale);
-            const int sw = (lane >> 2) & 1;
-            *reinterpret_cast<uint4*>(stage + lane * 32 + (sw << 4)) = make_uint4(y[0], y[1], y[2], y[3]);
-            *reinterpret_cast<uint4*>(stage + lane * 32 + ((sw ^ 1) << 4)) = make_uint4(y[4], y[5], y[6], y[7]);
-            __syncwarp();
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-              const int row = 16 * i + (lane >> 1), chunk = lane & 1;
-              const uint4 v = *reinterpret_cast<const uint4*>(stage + row * 32 + ((chunk ^ ((row >> 2) & 1)) << 4));
-              const int rr = wq * 32 + row, ti = (int)((uint32_t)rr * g_inv >> 16);
-              if (rr < rows && !*s_abort) *reinterpret_cast<uint4*>(obase + ((size_t)ti * x.Hq + (rr - ti * x.G)) * 128 + c0 + chunk * 8) = v;
-            }
-            __syncwarp();
-          } else if (mine && !*s_abort) {
-            float4* dst = reinterpret_cast<float4*>(part_of(place)) + (size_t)c0 / 4 * piece + r;
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              __stcg(dst + e * piece, make_float4(__uint_as_float(o[4 * e]), __uint_as_float(o[4 * e + 1]), __uint_as_float(o[4 * e + 2]),
-                                                  __uint_as_float(o[4 * e + 3])));
-          }
-        }
-        if (whole || join) {
-          if (wg == 0 && mine && lse_out) lse_out[r] = all;
-          return;
-        }
-        if (wg == 0 && mine && !*s_abort) __stcg(part_of(place) + 128 * piece + r, lse);
-      } else {
-        mbar_arrive(bar(7));
-        if (whole || join) return;
-      }
-      __threadfence();
-      all_sync();
-      if (tid == 0) s_list[0] = atomicAdd(x.counters + first_cta, 1u) == (unsigned)(n_parts - 1);
-      all_sync();
-      if (s_list[0]) {
-        // The last to finish joins the parts.  A warp takes 8 rows x 64 columns at a time, a lane four pieces of four columns
-        // of one row: 128-byte pieces of every part, whole sectors of the output.  Running maximum and sum over the parts.
-        __threadfence();
-        const int units = (rows + 7) / 8 * 2;
-        for (int u = warp; u < units; u += 8) {
-          const int row = (u >> 1) * 8 + (lane >> 2), c4 = (u & 1) * 16 + (lane & 3);
-          if (row < rows && !*s_abort) {
-            float M = -CUDART_INF_F, sum = 0.f, acc[16];
-#pragma unroll
-            for (int e = 0; e < 16; ++e) acc[e] = 0.f;
-#pragma unroll 2
-            for (int k = 0; k < n_parts; ++k) {
-              const float* src = part_of(s_list[2 + k]);
-              const float lk = __ldcg(src + 128 * piece + row);
-              float4 y[4];
-#pragma unroll
-              for (int e = 0; e < 4; ++e) y[e] = __ldcg(reinterpret_cast<const float4*>(src) + (size_t)(c4 + 4 * e) * piece + row);
-              const float Mn = fmaxf(M, lk);
-              const float keep = M == -CUDART_INF_F ? 0.f : fast_exp2(M - Mn), wk = lk == -CUDART_INF_F ? 0.f : fast_exp2(lk - Mn);
-              M = Mn;
-              sum = fmaf(sum, keep, wk);
-#pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                acc[4 * e] = fmaf(acc[4 * e], keep, wk * y[e].x);
-                acc[4 * e + 1] = fmaf(acc[4 * e + 1], keep, wk * y[e].y);
-                acc[4 * e + 2] = fmaf(acc[4 * e + 2], keep, wk * y[e].z);
-                acc[4 * e + 3] = fmaf(acc[4 * e + 3], keep, wk * y[e].w);
-              }
-            }
-            const float fs = out_scale / sum;
-            const int ti = (int)((uint32_t)row * g_inv >> 16);
-            __nv_bfloat16* dst = obase + ((size_t)ti * x.Hq + (row - ti * x.G)) * 128;
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              *reinterpret_cast<uint2*>(dst + (c4 + 4 * e) * 4) =
-                  make_uint2(pack_bf16x2(acc[4 * e] * fs, acc[4 * e + 1] * fs), pack_bf16x2(acc[4 * e + 2] * fs, acc[4 * e + 3] * fs));
-            if (c4 == 0 && lse_out) lse_out[row] = M + __log2f(sum);
-          }
-        }
-      }
-    };
-
-    int g0 = 0;  // flat index of the piece's first tile
-    while (cur->on) {
-      const int nkt = cur->nkt, kt_new = cur->kt0 + nkt - 1;  // its newest tile
-      const bool live = wq * 32 < cur->rows;
-      const int ti = cur->i0 + min(ri, (cur->rows - 1) / x.G);  // (a lane without a query repeats the last token's visibility)
-      const int lim = cur->n + max(ti + 1, x.seqs.prefix[cur->s]);  // rows [0, lim) are visible
+    int g0 = 0, ord = 0;  // flat index of the piece's first tile, piece
+    for (; slot < slot_end; go_next()) {
+      ask_next();
+      const int nkt = word(kPwTiles);
+      if (nkt == 0) continue;
+      const int kt_new = word(kPwFirst) + nkt - 1;  // its newest tile
+      const int rows = word(kPwRows), held = word(kPwHeld), i0 = word(kPwTok0), prefix = word(kPwPrefix);
+      const bool live = wq * 32 < rows;
+      const int r = min(wq * 32 + lane, rows - 1);  // (a lane without a query repeats the last row's visibility)
+      const int ti = i0 + r / x.G;
+      const int lim = held + max(ti + 1, prefix);   // rows [0, lim) are visible
       // Tiles that some token of the query tile does not see whole: all of them, and one more, are the first group's.
-      const int ramp = min(nkt, max(0, kt_new - (cur->n + max(cur->i0 + 1, x.seqs.prefix[cur->s]) - 1) / kPfKeys) + 1);
+      const int ramp = min(nkt, max(0, kt_new - (held + max(i0 + 1, prefix) - 1) / kPfKeys) + 1);
       const int* pos_row = nullptr;
       int tot = 0;
       float slope = 0.f;
       if constexpr (MODS) {
-        tot = x.tot[x.seqs.b0 + cur->s] - (x.published ? cur->end - cur->n : 0);
-        pos_row = x.pos + (size_t)cur->slab * x.cap;
-        if (x.slopes) slope = x.slopes[cur->h * x.G + rg] * 1.4426950408889634f;
+        tot = word(kPwSeen);
+        pos_row = x.pos + (size_t)word(kPwSlab) * x.cap;
+        if (x.slopes) slope = x.slopes[word(kPwHead) * x.G + r % x.G] * 1.4426950408889634f;
       }
+      const uint8_t* v_codes = KV8 ? static_cast<const uint8_t*>(x.V) + (size_t)word(kPwSlab) * x.cap * 128 : nullptr;
+      const int end = held + word(kPwNew);
       float ref = -CUDART_INF_F, l = 0.f;
-
-      // One tile: S of flat tile g to P, a chunk of columns at a time (the registers of 24 warps per SM hold no more).
-      // RAMP: part of the tile may be hidden and the reference may not be set yet; S is read twice.
-      constexpr int CH = MODS ? 16 : 32;
-      auto tile = [&](auto is_ramp, int j) {
-        constexpr bool RAMP = decltype(is_ramp)::value;
+      int j = wg == 0 ? 0 : ramp;
+      if (wg == 1) {  // the reference comes from the first group's first tiles
+        pair_sync();
+        ref = stage_other[128 + lane];
+      }
+#pragma unroll 1
+      while (j < nkt) {
+        // One tile: S of flat tile g to P, a chunk of columns at a time.  In the ramp part of the tile may be hidden and
+        // the reference may not be set yet: S is read twice.
+        const bool in_ramp = j < ramp;
         const int g = g0 + j, key0 = (kt_new - j) * kPfKeys;
-        const uint32_t ts = tS0 + lane_base + 64u * (uint32_t)(g & 1);
+        const uint32_t ts = t_row + 64u * (uint32_t)(g & 1);
         int pos_a = 0, pos_b = 0;
         if constexpr (MODS) {  // positions relative to the chunk's first token, two per lane
           pos_a = pos_row[min(key0 + lane, x.cap - 1)] - tot;
@@ -747,11 +649,10 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
         }
         XtCodes vc[2];
         if constexpr (KV8) {  // this warp's 16 rows of V
-          const uint8_t* src = static_cast<const uint8_t*>(x.V) + (size_t)cur->slab * x.cap * 128;
-          xt_load_codes(vc[0], src, key0 + 16 * wq, cur->end, lane);
-          xt_load_codes(vc[1], src, key0 + 16 * wq + 8, cur->end, lane);
+          xt_load_codes(vc[0], v_codes, key0 + 16 * wq, end, lane);
+          xt_load_codes(vc[1], v_codes, key0 + 16 * wq + 8, end, lane);
           if (lane == 0 && j + 4 < nkt)
-            asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(src + (size_t)(key0 + 16 * wq - 4 * kPfKeys) * 128), "r"(16 * 128) : "memory");
+            asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(v_codes + (size_t)(key0 + 16 * wq - 4 * kPfKeys) * 128), "r"(16 * 128) : "memory");
         }
         mbar_wait(bar(5 + (g & 1)), (uint32_t)((g >> 1) & 1), s_abort, x.err, kPfSpinLimit);  // S of this tile is complete
         tc5::fence_after_sync();
@@ -763,6 +664,7 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         }
         if (live) {
+          constexpr int CH = MODS ? 16 : 32;
           bool border = false;
           const int* ipos = reinterpret_cast<const int*>(stage);
           const float* fpos = reinterpret_cast<const float*>(stage) + 64;
@@ -775,115 +677,111 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
             if (x.window > 0) {
               // the tile's first position against the warp's last token (in tiles with rows of the chunk: always compared)
               const int p0 = __shfl_sync(0xffffffffu, pos_a, 0), tb = __shfl_sync(0xffffffffu, ti, 31);
-              border = key0 + kPfKeys > cur->n || (long long)tb - p0 >= x.window;
+              border = key0 + kPfKeys > held || (long long)tb - p0 >= x.window;
             }
             __syncwarp();
           }
           // logits in base-2 units: scaled in the exponent's multiply-add, or (MODS) here
           const float scale_log2 = MODS ? 1.f : p.scale_log2;
-          const int cv = lim - key0;  // visible columns
-          uint32_t sv[CH];
-          auto read = [&](int hb) {
-            if constexpr (CH == 32) tc5::tmem_ld32(ts + (uint32_t)hb, sv);
-            else tc5::tmem_ld16(ts + (uint32_t)hb, sv);
-            tc5::tmem_wait_ld();
-            if constexpr (MODS) {
-              if (x.cap_logit > 0.f) {  // c tanh(y) = c - 2 c / (1 + e^(2 y))
+          float mx = -CUDART_INF_F;
+          uint64_t sum2[2] = {0ull, 0ull};  // two chains of (even, odd) column sums
+#pragma unroll 1
+          for (int pass = in_ramp ? 0 : 1; pass < 2; ++pass) {
+            if (pass == 1 && in_ramp && ref == -CUDART_INF_F) ref = mx * scale_log2 + kXtHeadroom;
+            const float neg = ref == -CUDART_INF_F ? 0.f : -ref;
+            const uint64_t scale2 = tc5::f2_pack(scale_log2, scale_log2), neg2 = tc5::f2_pack(neg, neg);
+#pragma unroll 1
+            for (int hb = 0; hb < kPfKeys; hb += CH) {
+              uint32_t sv[CH];
+              if constexpr (CH == 32) tc5::tmem_ld32(ts + (uint32_t)hb, sv);
+              else tc5::tmem_ld16(ts + (uint32_t)hb, sv);
+              tc5::tmem_wait_ld();
+              if constexpr (MODS) {
+                if (x.cap_logit > 0.f) {  // c tanh(y) = c - 2 c / (1 + e^(2 y))
+#pragma unroll
+                  for (int c = 0; c < CH; ++c)
+                    sv[c] = __float_as_uint(fmaf(-2.f * p.cap_log2, rcp_approx(1.f + fast_exp2(__uint_as_float(sv[c]) * p.cap_arg)), p.cap_log2));
+                } else {
+#pragma unroll
+                  for (int c = 0; c < CH; ++c) sv[c] = __float_as_uint(__uint_as_float(sv[c]) * p.scale_log2);
+                }
+                if (x.slopes) {
+                  const float fi = (float)ti;
+#pragma unroll
+                  for (int c = 0; c < CH; c += 4) {
+                    const float4 y = *reinterpret_cast<const float4*>(fpos + hb + c);
+                    sv[c] = __float_as_uint(fmaf(-slope, fabsf(fi - y.x), __uint_as_float(sv[c])));
+                    sv[c + 1] = __float_as_uint(fmaf(-slope, fabsf(fi - y.y), __uint_as_float(sv[c + 1])));
+                    sv[c + 2] = __float_as_uint(fmaf(-slope, fabsf(fi - y.z), __uint_as_float(sv[c + 2])));
+                    sv[c + 3] = __float_as_uint(fmaf(-slope, fabsf(fi - y.w), __uint_as_float(sv[c + 3])));
+                  }
+                }
+                if (border) {
+#pragma unroll
+                  for (int c = 0; c < CH; c += 4) {
+                    const int4 y = *reinterpret_cast<const int4*>(ipos + hb + c);
+                    if (abs(ti - y.x) >= x.window) sv[c] = 0xff800000u;  // -inf
+                    if (abs(ti - y.y) >= x.window) sv[c + 1] = 0xff800000u;
+                    if (abs(ti - y.z) >= x.window) sv[c + 2] = 0xff800000u;
+                    if (abs(ti - y.w) >= x.window) sv[c + 3] = 0xff800000u;
+                  }
+                }
+              }
+              if (in_ramp) {
+                const int cv = lim - key0 - hb;  // visible columns of the chunk
 #pragma unroll
                 for (int c = 0; c < CH; ++c)
-                  sv[c] = __float_as_uint(fmaf(-2.f * p.cap_log2, rcp_approx(1.f + fast_exp2(__uint_as_float(sv[c]) * p.cap_arg)), p.cap_log2));
+                  if (c >= cv) sv[c] = 0xff800000u;
+              }
+              if (pass == 0) {
+                float mx4[4] = {mx, mx, mx, mx};
+#pragma unroll
+                for (int c = 0; c < CH; c += 8)
+#pragma unroll
+                  for (int u = 0; u < 4; ++u) mx4[u] = tc5::f_max3(mx4[u], __uint_as_float(sv[c + u]), __uint_as_float(sv[c + 4 + u]));
+                mx = tc5::f_max3(fmaxf(mx4[0], mx4[1]), mx4[2], mx4[3]);
               } else {
+                uint32_t pk[CH / 2];
 #pragma unroll
-                for (int c = 0; c < CH; ++c) sv[c] = __float_as_uint(__uint_as_float(sv[c]) * p.scale_log2);
-              }
-              if (x.slopes) {
-                const float fi = (float)ti;
-#pragma unroll
-                for (int c = 0; c < CH; c += 4) {
-                  const float4 y = *reinterpret_cast<const float4*>(fpos + hb + c);
-                  sv[c] = __float_as_uint(fmaf(-slope, fabsf(fi - y.x), __uint_as_float(sv[c])));
-                  sv[c + 1] = __float_as_uint(fmaf(-slope, fabsf(fi - y.y), __uint_as_float(sv[c + 1])));
-                  sv[c + 2] = __float_as_uint(fmaf(-slope, fabsf(fi - y.z), __uint_as_float(sv[c + 2])));
-                  sv[c + 3] = __float_as_uint(fmaf(-slope, fabsf(fi - y.w), __uint_as_float(sv[c + 3])));
+                for (int c = 0; c < CH / 2; ++c) {
+                  float x0, x1;
+                  tc5::f2_unpack(tc5::f2_fma(tc5::f2_pack(__uint_as_float(sv[2 * c]), __uint_as_float(sv[2 * c + 1])), scale2, neg2), x0, x1);
+                  const float a0 = fast_exp2(x0), a1 = fast_exp2(x1);
+                  sum2[c & 1] = tc5::f2_add(sum2[c & 1], tc5::f2_pack(a0, a1));
+                  pk[c] = pack_bf16x2(a0, a1);
                 }
-              }
-              if (border) {
-#pragma unroll
-                for (int c = 0; c < CH; c += 4) {
-                  const int4 y = *reinterpret_cast<const int4*>(ipos + hb + c);
-                  if (abs(ti - y.x) >= x.window) sv[c] = 0xff800000u;  // -inf
-                  if (abs(ti - y.y) >= x.window) sv[c + 1] = 0xff800000u;
-                  if (abs(ti - y.z) >= x.window) sv[c + 2] = 0xff800000u;
-                  if (abs(ti - y.w) >= x.window) sv[c + 3] = 0xff800000u;
-                }
+                // (over columns of S that have been read)
+                if constexpr (CH == 32) tc5::tmem_st16(ts + (uint32_t)(hb / 2), pk);
+                else tc5::tmem_st8(ts + (uint32_t)(hb / 2), pk);
               }
             }
-            if constexpr (RAMP) {
-#pragma unroll
-              for (int c = 0; c < CH; ++c)
-                if (hb + c >= cv) sv[c] = 0xff800000u;
-            }
-          };
-          if constexpr (RAMP) {
-            float mx4[4] = {-CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F};
-#pragma unroll
-            for (int hb = 0; hb < kPfKeys; hb += CH) {
-              read(hb);
-#pragma unroll
-              for (int c = 0; c < CH; c += 8)
-#pragma unroll
-                for (int u = 0; u < 4; ++u) mx4[u] = tc5::f_max3(mx4[u], __uint_as_float(sv[c + u]), __uint_as_float(sv[c + 4 + u]));
-            }
-            const float mx = tc5::f_max3(fmaxf(mx4[0], mx4[1]), mx4[2], mx4[3]) * scale_log2;
-            if (ref == -CUDART_INF_F) ref = mx + kXtHeadroom;
-          }
-          const float neg = ref == -CUDART_INF_F ? 0.f : -ref;
-          const uint64_t scale2 = tc5::f2_pack(scale_log2, scale_log2), neg2 = tc5::f2_pack(neg, neg);
-          uint64_t sum2[4] = {0ull, 0ull, 0ull, 0ull};  // four chains of (even, odd) column sums
-#pragma unroll
-          for (int hb = 0; hb < kPfKeys; hb += CH) {
-            read(hb);
-            uint32_t pk[CH / 2];
-#pragma unroll
-            for (int c = 0; c < CH / 2; ++c) {
-              float x0, x1;
-              tc5::f2_unpack(tc5::f2_fma(tc5::f2_pack(__uint_as_float(sv[2 * c]), __uint_as_float(sv[2 * c + 1])), scale2, neg2), x0, x1);
-              const float a0 = fast_exp2(x0), a1 = fast_exp2(x1);
-              sum2[c & 3] = tc5::f2_add(sum2[c & 3], tc5::f2_pack(a0, a1));
-              pk[c] = pack_bf16x2(a0, a1);
-            }
-            // (over columns of S that have been read)
-            if constexpr (CH == 32) tc5::tmem_st16(ts + (uint32_t)(hb / 2), pk);
-            else tc5::tmem_st8(ts + (uint32_t)(hb / 2), pk);
           }
           float e, o;
-          tc5::f2_unpack(tc5::f2_add(tc5::f2_add(sum2[0], sum2[1]), tc5::f2_add(sum2[2], sum2[3])), e, o);
+          tc5::f2_unpack(tc5::f2_add(sum2[0], sum2[1]), e, o);
           l += e + o;
           tc5::tmem_wait_st();
         }
         tc5::fence_before_sync();
         mbar_arrive(bar(8 + (g & 1)));
-      };
-      int j = ramp;
-      if (wg == 0) {
-        for (int i = 0; i < ramp; ++i) tile(std::true_type{}, i);
-        reinterpret_cast<float*>(stage)[128 + lane] = ref;
-        pair_sync();
-        ++j;
-      } else {
-        pair_sync();
-        ref = reinterpret_cast<const float*>(stage_other)[128 + lane];
+        if (wg == 1) {
+          j += 2;
+        } else if (++j == ramp) {
+          reinterpret_cast<float*>(stage)[128 + lane] = ref;
+          pair_sync();
+          ++j;
+        } else if (j > ramp) {
+          ++j;
+        }
       }
-      for (; j < nkt; j += 2) tile(std::false_type{}, j);
       g0 += nkt;
       // the other group's share of the row's sum
       reinterpret_cast<float*>(stage)[160 + lane] = l;
       pair_sync();
-      const float l_other = reinterpret_cast<const float*>(stage_other)[160 + lane];
+      const float l_other = stage_other[160 + lane];
       l = wg == 0 ? l + l_other : l_other + l;
       pair_sync();
-      epilogue(ref, l);
-      xt_next(cur, p, s_n);
+      xt_epilogue<KV8>(p, d, ord, ref, l, tO, bar0, s_abort, s_out, s_flag);
+      ++ord;
     }
   }
   tc5::fence_before_sync();
@@ -923,7 +821,7 @@ __device__ __forceinline__ void xm_seek(XmCursor& c, int it, int n_items, const 
   const int tps = kXmRows / p.x.G;  // tokens per step
   for (; it < n_items; ++it) {
     const int w = (int)blockIdx.x + it * (int)gridDim.x;
-    const int u = w / p.lh, lh = w - u * p.lh;
+    const int u = w / p.plan.lh, lh = w - u * p.plan.lh;
     c.s = ext_find(sh.item0, p.x.seqs.n, u);
     c.n = sh.n[c.s];
     c.t = p.x.seqs.tok0[c.s + 1] - p.x.seqs.tok0[c.s];
@@ -1016,7 +914,7 @@ extend_mass_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_con
   __syncthreads();
   tc5::fence_after_sync();
   const uint32_t tmem = *s_tmem;
-  const XmShared sh{s_n, s_item0, s_item0[x.seqs.n] * p.lh};
+  const XmShared sh{s_n, s_item0, s_item0[x.seqs.n] * p.plan.lh};
   const int n_items = max(0, (sh.n_work - (int)blockIdx.x + (int)gridDim.x - 1) / (int)gridDim.x);
   auto slab_of = [&](const XmCursor& c) { return ((x.layer0 + c.layer) * x.Nb + x.seqs.b0 + c.s) * x.Hkv + c.h; };
   auto next = [&](XmCursor& c) {  // the step after this one
