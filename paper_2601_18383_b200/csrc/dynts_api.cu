@@ -1521,6 +1521,7 @@ dynts_status_t launch_extend_tc_as(dynts_cache* c, dynts::ExtendTcParams& p, uns
 }
 
 constexpr int kExtendMinTiles = 3;  // key tiles per CTA below which the grid shrinks
+constexpr int kExtendItemTiles = 4;  // an item's beginning and end take about so many key tiles' time
 
 // The list of key tiles and its shares (see ExtendPlan); *grid: CTAs of the tensor-core kernel.
 dynts_status_t plan_extend(const dynts_cache* c, const dynts::ExtendParams& x, const ExtendScratch& m, char* scratch, dynts::ExtendPlan& p, unsigned* grid) {
@@ -1540,9 +1541,9 @@ dynts_status_t plan_extend(const dynts_cache* c, const dynts::ExtendParams& x, c
     p.item0[s] = (int)items;
     items += mine;
     if (items >= (1ll << 30)) return fail(DYNTS_ERR_INVALID_ARG, "%lld work items are beyond the launch limits", items);
-    p.per[s] = (unsigned)(n + 1);  // an item's beginning and end take about a key tile's time
+    p.per[s] = (unsigned)(n + kExtendItemTiles);
     key_tiles += mine * n;
-    shares += mine * (n + 1);
+    shares += mine * (n + kExtendItemTiles);
   }
   p.item0[n_seq] = (int)items;
   unsigned coarse = 1;  // shares are counted in 32 bits: very large calls count several key tiles as one

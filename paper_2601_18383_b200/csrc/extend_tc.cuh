@@ -55,7 +55,7 @@ constexpr int kXtMaxCtas = 380;      // CTAs of a launch (two per SM)
 constexpr int kXtPartFloats = 129;   // per query row of a part: 128 outputs, log-sum-exp
 constexpr float kXtHeadroom = 40.f;  // the reference lies so far (base-2 units) above the first tiles' maximum
 constexpr float kXtSumMax = 1.2676506e30f;  // 2^100: a row whose sum of weights exceeds it is computed again
-constexpr int kXtStageBytes = 1024;  // per softmax warp
+constexpr int kXtStageBytes = 2048;  // per softmax warp
 constexpr int kXtSmemBytes = kPfQBytes + 4 * kPfKvBytes + 8 * kXtStageBytes + 128 + 16;
 
 struct ExtendTcParams {
@@ -205,15 +205,18 @@ __device__ __noinline__ void xt_join_parts(const ExtendTcParams& p, int d, float
   const size_t piece = (size_t)p.part_rows;
   __nv_bfloat16* obase = static_cast<__nv_bfloat16*>(x.out) + (((size_t)layer * x.total + tok) * x.Hq + h * x.G) * 128;
   const int units = (rows + 7) / 8 * 2;
+  const bool ok = *s_abort == 0;
+  int places = lane < n_parts ? __ldcg(list + (size_t)lane * kPlanWords) : 0;  // of the first 32 parts
   for (int u = warp; u < units; u += 8) {
-    const int row = (u >> 1) * 8 + (lane >> 2), c4 = (u & 1) * 16 + (lane & 3);
-    if (row >= rows || *s_abort) continue;
+    const int row = min((u >> 1) * 8 + (lane >> 2), rows - 1), c4 = (u & 1) * 16 + (lane & 3);
+    const bool mine = (u >> 1) * 8 + (lane >> 2) < rows;
     float M = -CUDART_INF_F, sum = 0.f, acc[16];
 #pragma unroll
     for (int e = 0; e < 16; ++e) acc[e] = 0.f;
 #pragma unroll 2
     for (int k = 0; k < n_parts; ++k) {
-      const float* src = p.part + (size_t)__ldcg(list + (size_t)k * kPlanWords) * (piece * kXtPartFloats);
+      const int place = k < 32 ? __shfl_sync(0xffffffffu, places, k & 31) : __ldcg(list + (size_t)k * kPlanWords);
+      const float* src = p.part + (size_t)place * (piece * kXtPartFloats);
       const float lk = __ldcg(src + 128 * piece + row);
       float4 y[4];
 #pragma unroll
@@ -230,6 +233,7 @@ __device__ __noinline__ void xt_join_parts(const ExtendTcParams& p, int d, float
         acc[4 * e + 3] = fmaf(acc[4 * e + 3], keep, wk * y[e].w);
       }
     }
+    if (!mine || !ok) continue;
     const float fs = out_scale / sum;
     const int ti = row / x.G;
     __nv_bfloat16* dst = obase + ((size_t)ti * x.Hq + (row - ti * x.G)) * 128;
@@ -277,26 +281,32 @@ __device__ __noinline__ void xt_epilogue(const ExtendTcParams& p, int d, int ord
     float lse = l > 0.f ? ref + __log2f(l) : -CUDART_INF_F;
     const float f = l > 0.f ? 1.f / l : 0.f;
     float w_own = 1.f, w_other = 0.f, all = lse;
-    const float* other = nullptr;
-    bool weighed = false;
+    const float4* other = nullptr;
     __nv_bfloat16* obase = static_cast<__nv_bfloat16*>(x.out) + (((size_t)layer * x.total + tok) * x.Hq + h * x.G) * 128;
     const uint32_t t_row = tO + ((uint32_t)(wq * 32) << 16);
 #pragma unroll 1
-    for (int c0 = 64 * wg; c0 < 64 * wg + 64; c0 += 16) {
-      uint32_t o[16];
-      tc5::tmem_ld16(t_row + (uint32_t)c0, o);
+    for (int c0 = 64 * wg; c0 < 64 * wg + 64; c0 += 32) {
+      uint32_t o[32];
+      tc5::tmem_ld32(t_row + (uint32_t)c0, o);
       tc5::tmem_wait_ld();
-      if (c0 == 64 * wg + 48) {
+      if (c0 == 64 * wg + 32) {
         tc5::fence_before_sync();
         mbar_arrive(bar0 + 8 * 7);  // O may be written again
       }
-      float probe = 0.f;  // 0 * finite = 0
+      const uint64_t f2 = tc5::f2_pack(f, f);
+      uint64_t probe[2] = {0ull, 0ull};  // 0 * finite = 0
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
-        o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
-        probe = fmaf(__uint_as_float(o[e]), 0.f, probe);
+        const uint64_t y = tc5::f2_mul(tc5::f2_pack(__uint_as_float(o[2 * e]), __uint_as_float(o[2 * e + 1])), f2);
+        probe[e & 1] = tc5::f2_fma(y, 0ull, probe[e & 1]);
+        float y0, y1;
+        tc5::f2_unpack(y, y0, y1);
+        o[2 * e] = __float_as_uint(y0);
+        o[2 * e + 1] = __float_as_uint(y1);
       }
-      unsigned again = __ballot_sync(0xffffffffu, mine && (redo || !(probe == 0.f)));
+      float p0, p1;
+      tc5::f2_unpack(tc5::f2_add(probe[0], probe[1]), p0, p1);
+      unsigned again = __ballot_sync(0xffffffffu, mine && (redo || !(p0 + p1 == 0.f)));
       while (again) {
         const int who = __ffs(again) - 1;
         again &= again - 1;
@@ -309,18 +319,18 @@ __device__ __noinline__ void xt_epilogue(const ExtendTcParams& p, int d, int ord
         if (lane == who) {
           lse = new_lse;
 #pragma unroll
-          for (int e = 0; e < 16; ++e)
+          for (int e = 0; e < 32; ++e)
             if (full || !(__uint_as_float(o[e]) * 0.f == 0.f)) o[e] = reinterpret_cast<const uint32_t*>(stage)[c0 + e];
         }
         __syncwarp();
       }
-      if (!weighed) {
-        weighed = true;
+      if (c0 == 64 * wg) {
         all = lse;
         if (join) {  // (the sum is symmetric: whoever joins gets the same)
-          const int a = __ldcg(list), b = __ldcg(list + kPlanWords), mine_at = word(kPwPlace);
-          other = p.part + (size_t)(a == mine_at ? b : a) * (piece * kXtPartFloats) + (size_t)min(r, rows - 1) * 4;
-          const float lo = __ldcg(other - (size_t)min(r, rows - 1) * 3 + 128 * piece);
+          const int a = __ldcg(list), b = __ldcg(list + kPlanWords), rr = min(r, rows - 1);
+          const float* base = p.part + (size_t)(a == word(kPwPlace) ? b : a) * (piece * kXtPartFloats);
+          other = reinterpret_cast<const float4*>(base) + rr;
+          const float lo = __ldcg(base + 128 * piece + rr);
           const float M = fmaxf(lse, lo);
           if (M > -CUDART_INF_F) {
             all = M + __log2f((lse == -CUDART_INF_F ? 0.f : exp2f(lse - M)) + (lo == -CUDART_INF_F ? 0.f : exp2f(lo - M)));
@@ -333,8 +343,8 @@ __device__ __noinline__ void xt_epilogue(const ExtendTcParams& p, int d, int ord
       }
       if (join) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float4 y = __ldcg(reinterpret_cast<const float4*>(other + ((size_t)c0 / 4 + e) * piece * 4));
+        for (int e = 0; e < 8; ++e) {
+          const float4 y = __ldcg(other + ((size_t)c0 / 4 + e) * piece);
           o[4 * e] = __float_as_uint(fmaf(w_other, y.x, w_own * __uint_as_float(o[4 * e])));
           o[4 * e + 1] = __float_as_uint(fmaf(w_other, y.y, w_own * __uint_as_float(o[4 * e + 1])));
           o[4 * e + 2] = __float_as_uint(fmaf(w_other, y.z, w_own * __uint_as_float(o[4 * e + 2])));
@@ -342,27 +352,36 @@ __device__ __noinline__ void xt_epilogue(const ExtendTcParams& p, int d, int ord
         }
       }
       if (whole || join) {
-        // rounded, through the warp's staging tile [32 rows][32 B] (16-byte chunks swizzled), so that the stores are whole
-        // sectors
-        uint32_t y[8];
+        // rounded, through the warp's staging tile [32 rows][64 B] (16-byte chunks swizzled), so that the stores are 64-byte
+        // pieces of rows
 #pragma unroll
-        for (int e = 0; e < 8; ++e) y[e] = pack_bf16x2(__uint_as_float(o[2 * e]) * out_scale, __uint_as_float(o[2 * e + 1]) * out_scale);
-        const int sw = (lane >> 2) & 1;
-        *reinterpret_cast<uint4*>(stage + lane * 32 + (sw << 4)) = make_uint4(y[0], y[1], y[2], y[3]);
-        *reinterpret_cast<uint4*>(stage + lane * 32 + ((sw ^ 1) << 4)) = make_uint4(y[4], y[5], y[6], y[7]);
+        for (int e = 0; e < 4; ++e) {
+          uint32_t y[4];
+#pragma unroll
+          for (int u = 0; u < 4; ++u) {
+            float y0 = __uint_as_float(o[8 * e + 2 * u]), y1 = __uint_as_float(o[8 * e + 2 * u + 1]);
+            if constexpr (KV8) {
+              y0 *= x.v_scale;
+              y1 *= x.v_scale;
+            }
+            y[u] = pack_bf16x2(y0, y1);
+          }
+          *reinterpret_cast<uint4*>(stage + lane * 64 + ((e ^ ((lane >> 1) & 3)) << 4)) = make_uint4(y[0], y[1], y[2], y[3]);
+        }
         __syncwarp();
+        const bool store = *s_abort == 0;
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const int row = 16 * i + (lane >> 1), chunk = lane & 1;
-          const uint4 v = *reinterpret_cast<const uint4*>(stage + row * 32 + ((chunk ^ ((row >> 2) & 1)) << 4));
+        for (int i = 0; i < 4; ++i) {
+          const int row = 8 * i + (lane >> 2), chunk = lane & 3;
+          const uint4 v = *reinterpret_cast<const uint4*>(stage + row * 64 + ((chunk ^ ((row >> 1) & 3)) << 4));
           const int rr = wq * 32 + row, ti = (int)((uint32_t)rr * g_inv >> 16);
-          if (rr < rows && !*s_abort) *reinterpret_cast<uint4*>(obase + ((size_t)ti * x.Hq + (rr - ti * x.G)) * 128 + c0 + chunk * 8) = v;
+          if (rr < rows && store) *reinterpret_cast<uint4*>(obase + (ti * x.Hq + (rr - ti * x.G)) * 128 + c0 + chunk * 8) = v;
         }
         __syncwarp();
       } else if (mine && !*s_abort) {
         float4* dst = reinterpret_cast<float4*>(part) + (size_t)c0 / 4 * piece + r;
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
+        for (int e = 0; e < 8; ++e)
           __stcg(dst + e * piece,
                  make_float4(__uint_as_float(o[4 * e]), __uint_as_float(o[4 * e + 1]), __uint_as_float(o[4 * e + 2]), __uint_as_float(o[4 * e + 3])));
       }
@@ -400,7 +419,7 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
   const uint32_t sQ = smem_u32(sm);                       // [2 halves of head_dim][128 rows][128 B]
   const uint32_t sK = sQ + kPfQBytes;                     // [2 stages][2 halves][64 rows][128 B]
   const uint32_t sV = sK + 2 * kPfKvBytes;                // the same
-  uint8_t* s_out = sm + kPfQBytes + 4 * kPfKvBytes;       // [8 softmax warps][1 KB]
+  uint8_t* s_out = sm + kPfQBytes + 4 * kPfKvBytes;       // [8 softmax warps][2 KB]
   uint64_t* bars = reinterpret_cast<uint64_t*>(s_out + 8 * kXtStageBytes);
   // barriers: 0 Q, 1-2 K stages filled, 3-4 V stages filled, 5-6 S buffers complete, 7 O has been read, 8-9 P written (per S
   // buffer), 10-11 V stages and P read, 12 the piece's last O += P V complete, 13-14 drain
@@ -643,7 +662,7 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
         const int g = g0 + j, key0 = (kt_new - j) * kPfKeys;
         const uint32_t ts = t_row + 64u * (uint32_t)(g & 1);
         int pos_a = 0, pos_b = 0;
-        if constexpr (MODS) {  // positions relative to the chunk's first token, two per lane
+        if constexpr (MODS) {  // positions, the chunk's first token being 0: two per lane
           pos_a = pos_row[min(key0 + lane, x.cap - 1)] - tot;
           pos_b = pos_row[min(key0 + 32 + lane, x.cap - 1)] - tot;
         }
@@ -664,97 +683,104 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         }
         if (live) {
-          constexpr int CH = MODS ? 16 : 32;
-          bool border = false;
-          const int* ipos = reinterpret_cast<const int*>(stage);
+          constexpr int CH = 32;
+          bool border = false, beside = false;
+          float at = 0.f;                                       // this row's token
+          const int* ipos = reinterpret_cast<const int*>(stage);             // positions behind the tile's first
           const float* fpos = reinterpret_cast<const float*>(stage) + 64;
+          int me = 0;
           if constexpr (MODS) {
+            const int p0 = __shfl_sync(0xffffffffu, pos_a, 0);
             __syncwarp();
-            reinterpret_cast<int*>(stage)[lane] = pos_a;
-            reinterpret_cast<int*>(stage)[32 + lane] = pos_b;
-            reinterpret_cast<float*>(stage)[64 + lane] = (float)pos_a;
-            reinterpret_cast<float*>(stage)[96 + lane] = (float)pos_b;
-            if (x.window > 0) {
-              // the tile's first position against the warp's last token (in tiles with rows of the chunk: always compared)
-              const int p0 = __shfl_sync(0xffffffffu, pos_a, 0), tb = __shfl_sync(0xffffffffu, ti, 31);
-              border = key0 + kPfKeys > held || (long long)tb - p0 >= x.window;
-            }
+            reinterpret_cast<int*>(stage)[lane] = pos_a - p0;
+            reinterpret_cast<int*>(stage)[32 + lane] = pos_b - p0;
+            reinterpret_cast<float*>(stage)[64 + lane] = (float)(pos_a - p0);
+            reinterpret_cast<float*>(stage)[96 + lane] = (float)(pos_b - p0);
+            me = ti - p0;
+            at = (float)me;
+            const bool fresh = key0 + kPfKeys > held;  // the tile holds rows of the chunk
+            // the tile's first position against the warp's last token (in tiles with rows of the chunk: always compared)
+            border = x.window > 0 && (fresh || __shfl_sync(0xffffffffu, me, 31) >= x.window);
+            beside = fresh && prefix > 0;  // rows of later positions may be visible
             __syncwarp();
           }
-          // logits in base-2 units: scaled in the exponent's multiply-add, or (MODS) here
+          // logits in base-2 units: scaled in the exponent's multiply-add, or (MODS) before it
           const float scale_log2 = MODS ? 1.f : p.scale_log2;
-          float mx = -CUDART_INF_F;
           uint64_t sum2[2] = {0ull, 0ull};  // two chains of (even, odd) column sums
+          // (a row's reference comes from the first half of the first tile it sees: the headroom is for all others)
 #pragma unroll 1
-          for (int pass = in_ramp ? 0 : 1; pass < 2; ++pass) {
-            if (pass == 1 && in_ramp && ref == -CUDART_INF_F) ref = mx * scale_log2 + kXtHeadroom;
-            const float neg = ref == -CUDART_INF_F ? 0.f : -ref;
-            const uint64_t scale2 = tc5::f2_pack(scale_log2, scale_log2), neg2 = tc5::f2_pack(neg, neg);
-#pragma unroll 1
-            for (int hb = 0; hb < kPfKeys; hb += CH) {
-              uint32_t sv[CH];
-              if constexpr (CH == 32) tc5::tmem_ld32(ts + (uint32_t)hb, sv);
-              else tc5::tmem_ld16(ts + (uint32_t)hb, sv);
-              tc5::tmem_wait_ld();
-              if constexpr (MODS) {
-                if (x.cap_logit > 0.f) {  // c tanh(y) = c - 2 c / (1 + e^(2 y))
-#pragma unroll
-                  for (int c = 0; c < CH; ++c)
-                    sv[c] = __float_as_uint(fmaf(-2.f * p.cap_log2, rcp_approx(1.f + fast_exp2(__uint_as_float(sv[c]) * p.cap_arg)), p.cap_log2));
-                } else {
-#pragma unroll
-                  for (int c = 0; c < CH; ++c) sv[c] = __float_as_uint(__uint_as_float(sv[c]) * p.scale_log2);
-                }
-                if (x.slopes) {
-                  const float fi = (float)ti;
-#pragma unroll
-                  for (int c = 0; c < CH; c += 4) {
-                    const float4 y = *reinterpret_cast<const float4*>(fpos + hb + c);
-                    sv[c] = __float_as_uint(fmaf(-slope, fabsf(fi - y.x), __uint_as_float(sv[c])));
-                    sv[c + 1] = __float_as_uint(fmaf(-slope, fabsf(fi - y.y), __uint_as_float(sv[c + 1])));
-                    sv[c + 2] = __float_as_uint(fmaf(-slope, fabsf(fi - y.z), __uint_as_float(sv[c + 2])));
-                    sv[c + 3] = __float_as_uint(fmaf(-slope, fabsf(fi - y.w), __uint_as_float(sv[c + 3])));
-                  }
-                }
-                if (border) {
-#pragma unroll
-                  for (int c = 0; c < CH; c += 4) {
-                    const int4 y = *reinterpret_cast<const int4*>(ipos + hb + c);
-                    if (abs(ti - y.x) >= x.window) sv[c] = 0xff800000u;  // -inf
-                    if (abs(ti - y.y) >= x.window) sv[c + 1] = 0xff800000u;
-                    if (abs(ti - y.z) >= x.window) sv[c + 2] = 0xff800000u;
-                    if (abs(ti - y.w) >= x.window) sv[c + 3] = 0xff800000u;
-                  }
-                }
-              }
-              if (in_ramp) {
-                const int cv = lim - key0 - hb;  // visible columns of the chunk
+          for (int step = in_ramp && __any_sync(0xffffffffu, ref == -CUDART_INF_F) ? -1 : 0; step < kPfKeys / CH; ++step) {
+            const int hb = step < 0 ? 0 : step * CH;
+            uint32_t sv[CH];
+            tc5::tmem_ld32(ts + (uint32_t)hb, sv);
+            tc5::tmem_wait_ld();
+            if constexpr (MODS) {
+              float scale = p.scale_log2;
+              if (x.cap_logit > 0.f) {  // c tanh(y) = c - 2 c / (1 + e^(2 y))
+                scale = 1.f;
 #pragma unroll
                 for (int c = 0; c < CH; ++c)
-                  if (c >= cv) sv[c] = 0xff800000u;
+                  sv[c] = __float_as_uint(fmaf(-2.f * p.cap_log2, rcp_approx(1.f + fast_exp2(__uint_as_float(sv[c]) * p.cap_arg)), p.cap_log2));
               }
-              if (pass == 0) {
-                float mx4[4] = {mx, mx, mx, mx};
+              const uint64_t scale2 = tc5::f2_pack(scale, scale);
+              if (beside) {
+#pragma unroll
+                for (int c = 0; c < CH; ++c) sv[c] = __float_as_uint(fmaf(__uint_as_float(sv[c]), scale, -slope * fabsf(at - fpos[hb + c])));
+              } else {  // - slope (me - pos) = slope pos - slope me, both counted from the tile's first row
+                const uint64_t slope2 = tc5::f2_pack(slope, slope), base2 = tc5::f2_pack(-slope * at, -slope * at);
+#pragma unroll
+                for (int c = 0; c < CH; c += 4) {
+                  const float4 y = *reinterpret_cast<const float4*>(fpos + hb + c);
+                  float x0, x1, x2, x3;
+                  tc5::f2_unpack(tc5::f2_fma(tc5::f2_pack(__uint_as_float(sv[c]), __uint_as_float(sv[c + 1])), scale2,
+                                             tc5::f2_fma(tc5::f2_pack(y.x, y.y), slope2, base2)), x0, x1);
+                  tc5::f2_unpack(tc5::f2_fma(tc5::f2_pack(__uint_as_float(sv[c + 2]), __uint_as_float(sv[c + 3])), scale2,
+                                             tc5::f2_fma(tc5::f2_pack(y.z, y.w), slope2, base2)), x2, x3);
+                  sv[c] = __float_as_uint(x0);
+                  sv[c + 1] = __float_as_uint(x1);
+                  sv[c + 2] = __float_as_uint(x2);
+                  sv[c + 3] = __float_as_uint(x3);
+                }
+              }
+              if (border) {
+#pragma unroll
+                for (int c = 0; c < CH; c += 4) {
+                  const int4 y = *reinterpret_cast<const int4*>(ipos + hb + c);
+                  if (abs(me - y.x) >= x.window) sv[c] = 0xff800000u;  // -inf
+                  if (abs(me - y.y) >= x.window) sv[c + 1] = 0xff800000u;
+                  if (abs(me - y.z) >= x.window) sv[c + 2] = 0xff800000u;
+                  if (abs(me - y.w) >= x.window) sv[c + 3] = 0xff800000u;
+                }
+              }
+            }
+            if (in_ramp) {
+              const int cv = lim - key0 - hb;  // visible columns of the chunk
+#pragma unroll
+              for (int c = 0; c < CH; ++c)
+                if (c >= cv) sv[c] = 0xff800000u;
+              // A row with a window may see nothing in the first half and something in the second.
+              if (ref == -CUDART_INF_F) {
+                float mx4[4] = {-CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F};
 #pragma unroll
                 for (int c = 0; c < CH; c += 8)
 #pragma unroll
                   for (int u = 0; u < 4; ++u) mx4[u] = tc5::f_max3(mx4[u], __uint_as_float(sv[c + u]), __uint_as_float(sv[c + 4 + u]));
-                mx = tc5::f_max3(fmaxf(mx4[0], mx4[1]), mx4[2], mx4[3]);
-              } else {
-                uint32_t pk[CH / 2];
-#pragma unroll
-                for (int c = 0; c < CH / 2; ++c) {
-                  float x0, x1;
-                  tc5::f2_unpack(tc5::f2_fma(tc5::f2_pack(__uint_as_float(sv[2 * c]), __uint_as_float(sv[2 * c + 1])), scale2, neg2), x0, x1);
-                  const float a0 = fast_exp2(x0), a1 = fast_exp2(x1);
-                  sum2[c & 1] = tc5::f2_add(sum2[c & 1], tc5::f2_pack(a0, a1));
-                  pk[c] = pack_bf16x2(a0, a1);
-                }
-                // (over columns of S that have been read)
-                if constexpr (CH == 32) tc5::tmem_st16(ts + (uint32_t)(hb / 2), pk);
-                else tc5::tmem_st8(ts + (uint32_t)(hb / 2), pk);
+                ref = tc5::f_max3(fmaxf(mx4[0], mx4[1]), mx4[2], mx4[3]) * scale_log2 + kXtHeadroom;
               }
+              if (step < 0) continue;
             }
+            const float neg = ref == -CUDART_INF_F ? 0.f : -ref;
+            const uint64_t scale2 = tc5::f2_pack(scale_log2, scale_log2), neg2 = tc5::f2_pack(neg, neg);
+            uint32_t pk[CH / 2];
+#pragma unroll
+            for (int c = 0; c < CH / 2; ++c) {
+              float x0, x1;
+              tc5::f2_unpack(tc5::f2_fma(tc5::f2_pack(__uint_as_float(sv[2 * c]), __uint_as_float(sv[2 * c + 1])), scale2, neg2), x0, x1);
+              const float a0 = fast_exp2(x0), a1 = fast_exp2(x1);
+              sum2[c & 1] = tc5::f2_add(sum2[c & 1], tc5::f2_pack(a0, a1));
+              pk[c] = pack_bf16x2(a0, a1);
+            }
+            tc5::tmem_st16(ts + (uint32_t)(hb / 2), pk);  // (over columns of S that have been read)
           }
           float e, o;
           tc5::f2_unpack(tc5::f2_add(sum2[0], sum2[1]), e, o);
