@@ -1335,10 +1335,12 @@ namespace {
 
 // What a chunk's launches need beside the cache, as offsets into the caller's scratch.
 struct ExtendScratch {
-  size_t lse, q16, part, counters, plan, total;
+  size_t lse, q16, part, counters, plan, mass, total;
   int part_rows;  // query rows of a part of an item that several CTAs share
   int ctas;       // of the tensor-core kernel, at most
 };
+
+constexpr int kMassParts = 8;  // parts of a mass item, at most
 
 bool extend_tc_shape(const dynts_config_t& f) { return f.dtype != DYNTS_FP32 && f.head_dim == 128; }
 
@@ -1361,11 +1363,12 @@ ExtendScratch extend_scratch(const dynts_cache* c, const int* n_new, int n_layer
     return o;
   };
   m.lse = take((size_t)n_layers * total * f.q_heads * sizeof(float));
-  m.q16 = m.part = m.counters = m.plan = off;
+  m.q16 = m.part = m.counters = m.plan = m.mass = off;
   if (extend_tc_shape(f)) {
     if (f.dtype == DYNTS_BF16_KV8) m.q16 = take((size_t)n_layers * total * f.q_heads * f.head_dim * 2);
     m.part = take((size_t)2 * m.ctas * m.part_rows * dynts::kXtPartFloats * sizeof(float));
-    m.counters = take((size_t)m.ctas * sizeof(int));
+    m.counters = take((size_t)2 * m.ctas * sizeof(int));  // of cut items, then of cut mass items
+    m.mass = take((size_t)m.ctas * kMassParts * dynts::kXmKeys * sizeof(float));
     long long items = 0;  // of the launch with the most sequences' worth (a batch beyond 128 sequences takes several)
     for (int b0 = 0; b0 < f.batch; b0 += dynts::kExtSeqs) {
       long long tiles = 0;
@@ -1574,6 +1577,23 @@ dynts_status_t launch_extend_tc(dynts_cache* c, const dynts::ExtendParams& x, co
   p.scale_log2 = (float)(1.4426950408889634 * (double)x.scale);
   p.cap_log2 = (float)(1.4426950408889634 * (double)x.cap_logit);
   p.cap_arg = x.cap_logit > 0.f ? (float)(2.0 * 1.4426950408889634 * (double)x.scale / (double)x.cap_logit) : 0.f;
+  // Mass items: 128 rows of a slab each.  Fewer than CTAs: their query rows are cut, in parts of at least two steps.
+  p.mass_part = reinterpret_cast<float*>(scratch + m.mass);
+  p.mass_counters = x.counters + m.ctas;
+  p.mass_items = m.ctas;
+  p.mass_parts = 1;
+  {
+    long long items = 0;
+    int longest = 0;
+    for (int s = 0; s < x.seqs.n; ++s) {
+      const int t = x.seqs.tok0[s + 1] - x.seqs.tok0[s];
+      if (t > 0) items += (c->len_h[x.seqs.b0 + s] + t + dynts::kXmKeys - 1) / dynts::kXmKeys;
+      longest = std::max(longest, t);
+    }
+    items *= plan.lh;
+    const int steps = (longest * c->G + dynts::kXmRows - 1) / dynts::kXmRows;
+    if (items > 0 && items < m.ctas) p.mass_parts = (int)std::max<long long>(1, std::min<long long>(std::min(kMassParts, steps / 2), (m.ctas + items - 1) / items));
+  }
   // The queries, [layers x tokens][heads][128] in boxes of (tokens, the group's heads, 64 elements): a box is a tile's rows.
   const bool kv8 = c->cfg.dtype == DYNTS_BF16_KV8;
   const cuuint64_t dims[3] = {128, (cuuint64_t)x.Hq, (cuuint64_t)x.n_layers * x.total};
@@ -1666,10 +1686,10 @@ dynts_status_t launch_extend(dynts_cache* c, int layer0, int n_layers, const Ext
     const int n_tok = p.seqs.tok0[n_seq] - p.seqs.tok0[0];
     if (n_tok == 0) continue;
     p.published = 0;
-    p.n_counters = tc ? m.ctas : 0;
+    p.n_counters = tc ? 2 * m.ctas : 0;
     // one 16-byte piece of K and of V (and of the rows to clear, and of the queries to copy) per thread, up to a few CTAs per SM
     const long long pieces = f.head_dim * c->elt / 16, ny = (long long)n_layers * f.kv_heads;
-    long long work = std::max(n_tok * pieces, (long long)m.ctas);
+    long long work = std::max(n_tok * pieces, 2ll * m.ctas);
     if (p.zero_tail) work = std::max(work, (long long)n_seq * dynts::kExtTileKeys * pieces);
     if (p.q16) work = std::max(work, (long long)n_tok * c->G * (f.head_dim / 8));
     if (work >= (1ll << 31)) return fail(DYNTS_ERR_INVALID_ARG, "%d new tokens are beyond the launch limits", n_tok);
