@@ -1367,7 +1367,7 @@ ExtendScratch extend_scratch(const dynts_cache* c, const int* n_new, int n_layer
   if (extend_tc_shape(f)) {
     if (f.dtype == DYNTS_BF16_KV8) m.q16 = take((size_t)n_layers * total * f.q_heads * f.head_dim * 2);
     m.part = take((size_t)2 * m.ctas * m.part_rows * dynts::kXtPartFloats * sizeof(float));
-    m.counters = take((size_t)2 * m.ctas * sizeof(int));  // of cut items, then of cut mass items
+    m.counters = take((size_t)m.ctas * sizeof(int));  // of cut mass items
     m.mass = take((size_t)m.ctas * kMassParts * dynts::kXmKeys * sizeof(float));
     long long items = 0;  // of the launch with the most sequences' worth (a batch beyond 128 sequences takes several)
     for (int b0 = 0; b0 < f.batch; b0 += dynts::kExtSeqs) {
@@ -1515,9 +1515,13 @@ dynts_status_t launch_extend_tc_as(dynts_cache* c, dynts::ExtendTcParams& p, uns
   }
   CUDA_TRY(launch_dependent(dynts::extend_tc_kernel<KV8, MODS>, dim3(grid, 1, 1), dynts::kXtThreads, dynts::kXtSmemBytes, c->stream, p, mq, c->map_XK, c->map_XV));
   c->launches += 1;
+  if (grid > 1) {  // items that lie across CTAs
+    CUDA_TRY(launch_dependent(dynts::extend_join_kernel, dim3(grid - 1, (unsigned)((p.part_rows + 7) / 8), 1), 256, 0, c->stream, p));
+    c->launches += 1;
+  }
   if (want_mass) {
-    dynts::extend_mass_tc_kernel<KV8, MODS><<<2 * c->sm_count, dynts::kXmThreads, dynts::kXmSmemBytes, c->stream>>>(p, mqs, c->map_XK);
-    CUDA_TRY(cudaGetLastError());
+    CUDA_TRY(launch_dependent(dynts::extend_mass_tc_kernel<KV8, MODS>, dim3((unsigned)(2 * c->sm_count), 1, 1), dynts::kXmThreads, dynts::kXmSmemBytes, c->stream, p, mqs,
+                              c->map_XK));
     c->launches += 1;
   }
   return DYNTS_OK;
@@ -1574,12 +1578,13 @@ dynts_status_t launch_extend_tc(dynts_cache* c, const dynts::ExtendParams& x, co
   p.part_rows = m.part_rows;
   p.part = reinterpret_cast<float*>(scratch + m.part);
   p.stop = reinterpret_cast<int*>(c->ticket()) + 41;  // a spare word of the ticket block (zero since the cache was created)
+  p.out_scale = c->cfg.dtype == DYNTS_BF16_KV8 ? c->v_scale : 1.f;
   p.scale_log2 = (float)(1.4426950408889634 * (double)x.scale);
   p.cap_log2 = (float)(1.4426950408889634 * (double)x.cap_logit);
   p.cap_arg = x.cap_logit > 0.f ? (float)(2.0 * 1.4426950408889634 * (double)x.scale / (double)x.cap_logit) : 0.f;
   // Mass items: 128 rows of a slab each.  Fewer than CTAs: their query rows are cut, in parts of at least two steps.
   p.mass_part = reinterpret_cast<float*>(scratch + m.mass);
-  p.mass_counters = x.counters + m.ctas;
+  p.mass_counters = x.counters;
   p.mass_items = m.ctas;
   p.mass_parts = 1;
   {
@@ -1686,10 +1691,10 @@ dynts_status_t launch_extend(dynts_cache* c, int layer0, int n_layers, const Ext
     const int n_tok = p.seqs.tok0[n_seq] - p.seqs.tok0[0];
     if (n_tok == 0) continue;
     p.published = 0;
-    p.n_counters = tc ? 2 * m.ctas : 0;
+    p.n_counters = tc && want_mass ? m.ctas : 0;
     // one 16-byte piece of K and of V (and of the rows to clear, and of the queries to copy) per thread, up to a few CTAs per SM
     const long long pieces = f.head_dim * c->elt / 16, ny = (long long)n_layers * f.kv_heads;
-    long long work = std::max(n_tok * pieces, 2ll * m.ctas);
+    long long work = std::max(n_tok * pieces, (long long)m.ctas);
     if (p.zero_tail) work = std::max(work, (long long)n_seq * dynts::kExtTileKeys * pieces);
     if (p.q16) work = std::max(work, (long long)n_tok * c->G * (f.head_dim / 8));
     if (work >= (1ll << 31)) return fail(DYNTS_ERR_INVALID_ARG, "%d new tokens are beyond the launch limits", n_tok);

@@ -80,7 +80,7 @@ struct ExtendParams {
 // CTA c takes the shares [c * q + min(c, rem), ...).  What CTA c does of item i is described by 32 words at slot i + c
 // (an item's parts and a CTA's pieces both lie side by side).
 constexpr int kPlanWords = 32;
-enum PlanWord { kPwTiles, kPwFirst, kPwTotal, kPwTok, kPwLayer, kPwHead, kPwHeld, kPwTok0, kPwRows, kPwNew, kPwSlab, kPwParts, kPwPlace, kPwBase, kPwCounter, kPwList, kPwPrefix, kPwSeen };
+enum PlanWord { kPwTiles, kPwFirst, kPwTotal, kPwTok, kPwLayer, kPwHead, kPwHeld, kPwTok0, kPwRows, kPwNew, kPwSlab, kPwParts, kPwPlace, kPwBase, kPwList, kPwPrefix, kPwSeen };
 struct ExtendPlan {
   unsigned cum[kExtSeqs + 1];  // shares before each sequence's first item
   unsigned per[kExtSeqs];      // shares of an item
@@ -193,7 +193,6 @@ __device__ __forceinline__ void ext_write_plan(const ExtendParams& p, const Exte
           w[kPwParts] = count;
           w[kPwPlace] = place;
           w[kPwBase] = item + (int)ca;
-          w[kPwCounter] = (int)ca;
           w[kPwPrefix] = prefix;
           w[kPwSeen] = p.tot[b];
         }

@@ -6,8 +6,9 @@
 // query rows, KV head, layer, sequence).  All items' key tiles form one list, of which every CTA takes an equal
 // contiguous piece: few tokens behind a long cache, many ragged sequences and a whole prompt are cut alike.
 // An item that lies across CTAs is computed in parts side by side; each part leaves its normalised output and
-// log-sum-exp in the scratch, and the last part to finish (a counter per item) joins them in the order of the
-// rows.  Two CTAs per SM; per 64 keys
+// log-sum-exp in the scratch, and extend_join_kernel joins them in the order of the list.  (The last part to finish
+// joined them at first: one CTA then read all parts of its items, up to 20 us after the others had ended.)
+// Two CTAs per SM; per 64 keys
 //     S  = Q K^T      M 128 x N 64 x K 128     operands from shared memory
 //     P  = exp2(S * scale - ref)               softmax warps, thread = query row = tensor-memory lane
 //     O += P V        M 128 x N 128 x K 64     P from tensor memory
@@ -23,8 +24,8 @@
 // computed again by its warp alone, with a running maximum.  No maximum and no rescale in any other tile.
 // (From the newest tile on, because a distance bias only lowers the logits of older rows, and a window hides the oldest.)
 //
-// Warps: 0-3 and 4-7 the two groups, 8 loads Q and K, 9 loads V, 10 issues S, 11 issues O; they meet through mbarriers as
-// in the prompt attention (prefill_attn.cuh), the S buffer, stages and phases follow the flat tile index g.  Every warp
+// Warps: 0-3 and 4-7 the two groups, two that load, one that issues S, one that issues O; they meet
+// through mbarriers as in the prompt attention (prefill_attn.cuh), the S buffer, stages and phases follow the flat tile index g.  Every warp
 // walks the CTA's pieces by the plan the storing kernel wrote (extend.cuh), a word per lane, the next piece's
 // prefetched.  Two CTAs of 384 threads leave 80 registers per thread and hardly any L1: code that spills or does
 // not stay in the instruction caches cost several times its instructions, so the loops are rolled and the end of a piece
@@ -68,6 +69,7 @@ struct ExtendTcParams {
   int mass_items;
   float* mass_part;     // [mass_items][mass_parts][128]
   unsigned int* mass_counters;  // [mass_items], cleared by the storing kernel
+  float out_scale;      // v_scale for 8-bit rows
   float scale_log2;     // log2(e) * scale
   float cap_log2;       // c * log2(e)
   float cap_arg;        // 2 log2(e) * scale / c
@@ -81,6 +83,40 @@ __device__ __forceinline__ float rcp_approx(float x) {
 __device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
   const __half2 v = __floats2half2_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&v);
+}
+
+// Shared memory by 32-bit address (a generic pointer is a second register).
+__device__ __forceinline__ float4 lds_f4(uint32_t a) {
+  float4 v;
+  asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(a) : "memory");
+  return v;
+}
+__device__ __forceinline__ int4 lds_i4(uint32_t a) {
+  int4 v;
+  asm volatile("ld.shared.v4.s32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
+  return v;
+}
+__device__ __forceinline__ float lds_f(uint32_t a) {
+  float v;
+  asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(a) : "memory");
+  return v;
+}
+__device__ __forceinline__ int lds_flag(uint32_t a) {
+  int v;
+  asm volatile("ld.volatile.shared.s32 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
+  return v;
+}
+__device__ __forceinline__ void sts_i(uint32_t a, int v) { asm volatile("st.shared.s32 [%0], %1;" ::"r"(a), "r"(v) : "memory"); }
+__device__ __forceinline__ void sts_f(uint32_t a, float v) { asm volatile("st.shared.f32 [%0], %1;" ::"r"(a), "f"(v) : "memory"); }
+// mbar_wait (decode_stream.cuh) with the abort flag by its shared address.
+__device__ __forceinline__ void xt_wait(uint32_t bar, uint32_t parity, uint32_t abort_flag, int* err) {
+  if (lds_flag(abort_flag)) return;
+  for (uint32_t i = 0; i < kPfSpinLimit; ++i) {
+    if (mbar_try_wait(bar, parity)) return;
+    if ((i & 1023u) == 1023u && lds_flag(abort_flag)) return;
+  }
+  sts_i(abort_flag, 1);
+  atomicOr(err, kErrTimeout);
 }
 
 // Codes to operand tiles [2 halves of head_dim][rows][128 B], 16-byte chunks swizzled by row.  A warp takes groups of 8
@@ -197,221 +233,157 @@ __device__ __noinline__ float4 xt_row_again(const ExtendTcParams& p, int d, int 
   return make_float4(acc[0], acc[1], acc[2], acc[3]);
 }
 
-// The last CTA to finish a part of an item joins the parts, eight warps.  A warp takes 8 rows x 64 columns at a time, a
-// lane four pieces of four columns of one row: 128-byte pieces of every part, whole sectors of the output.  Running
-// maximum and sum over the parts, in the order of the list.
-__device__ __noinline__ void xt_join_parts(const ExtendTcParams& p, int d, float out_scale, volatile int* s_abort) {
+// Joins the parts of the item that begins in CTA blockIdx.x's shares and ends behind them, if there is one: 8 rows per
+// block (y), a thread four columns of one row.  A part's 128-byte pieces are read whole, the output's sectors written whole.
+// Running maximum and sum over the parts, in the order of the list: bound by the latency of two loads (the list, then
+// all parts at once).
+__global__ void __launch_bounds__(256) extend_join_kernel(const __grid_constant__ ExtendTcParams p) {
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const ExtendParams& x = p.x;
-  auto word = [&](int w) { return __shfl_sync(0xffffffffu, d, w); };
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int rows = word(kPwRows), n_parts = word(kPwParts), h = word(kPwHead), layer = word(kPwLayer), tok = word(kPwTok);
-  const int* list = p.plan.words + (size_t)word(kPwBase) * kPlanWords + kPwList;
-  const size_t piece = (size_t)p.part_rows;
-  __nv_bfloat16* obase = static_cast<__nv_bfloat16*>(x.out) + (((size_t)layer * x.total + tok) * x.Hq + h * x.G) * 128;
-  const int units = (rows + 7) / 8 * 2;
-  const bool ok = *s_abort == 0;
+  const unsigned share = plan_share0(p.plan, blockIdx.x + 1u) - 1u;
+  const int slot = plan_item_of(p.plan, x.seqs.n, share) + (int)blockIdx.x;
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const int d = __ldcg(p.plan.words + (size_t)slot * kPlanWords + lane);
+  auto word = [&](int w) { return __shfl_sync(0xffffffffu, d, w); };
+  const int n_parts = word(kPwParts), rows = word(kPwRows), row = blockIdx.y * 8 + (lane >> 2), c4 = warp * 4 + (lane & 3);
+  if (n_parts < 2 || word(kPwBase) != slot) return;  // (an item that began before is another block's)
+  const int tok = word(kPwTok), h = word(kPwHead), layer = word(kPwLayer);
+  const int* list = p.plan.words + (size_t)slot * kPlanWords + kPwList;
   int places = lane < n_parts ? __ldcg(list + (size_t)lane * kPlanWords) : 0;  // of the first 32 parts
-  for (int u = warp; u < units; u += 8) {
-    const int row = min((u >> 1) * 8 + (lane >> 2), rows - 1), c4 = (u & 1) * 16 + (lane & 3);
-    const bool mine = (u >> 1) * 8 + (lane >> 2) < rows;
-    float M = -CUDART_INF_F, sum = 0.f, acc[16];
-#pragma unroll
-    for (int e = 0; e < 16; ++e) acc[e] = 0.f;
-#pragma unroll 2
-    for (int k = 0; k < n_parts; ++k) {
-      const int place = k < 32 ? __shfl_sync(0xffffffffu, places, k & 31) : __ldcg(list + (size_t)k * kPlanWords);
-      const float* src = p.part + (size_t)place * (piece * kXtPartFloats);
-      const float lk = __ldcg(src + 128 * piece + row);
-      float4 y[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) y[e] = __ldcg(reinterpret_cast<const float4*>(src) + (size_t)(c4 + 4 * e) * piece + row);
-      const float Mn = fmaxf(M, lk);
-      const float keep = M == -CUDART_INF_F ? 0.f : fast_exp2(M - Mn), wk = lk == -CUDART_INF_F ? 0.f : fast_exp2(lk - Mn);
-      M = Mn;
-      sum = fmaf(sum, keep, wk);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        acc[4 * e] = fmaf(acc[4 * e], keep, wk * y[e].x);
-        acc[4 * e + 1] = fmaf(acc[4 * e + 1], keep, wk * y[e].y);
-        acc[4 * e + 2] = fmaf(acc[4 * e + 2], keep, wk * y[e].z);
-        acc[4 * e + 3] = fmaf(acc[4 * e + 3], keep, wk * y[e].w);
-      }
-    }
-    if (!mine || !ok) continue;
-    const float fs = out_scale / sum;
-    const int ti = row / x.G;
-    __nv_bfloat16* dst = obase + ((size_t)ti * x.Hq + (row - ti * x.G)) * 128;
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-      *reinterpret_cast<uint2*>(dst + (c4 + 4 * e) * 4) =
-          make_uint2(pack_bf16x2(acc[4 * e] * fs, acc[4 * e + 1] * fs), pack_bf16x2(acc[4 * e + 2] * fs, acc[4 * e + 3] * fs));
-    if (c4 == 0 && x.lse) x.lse[ext_lse_index(x, layer, h, tok) + row] = M + __log2f(sum);
+  if ((int)blockIdx.y * 8 >= rows) return;
+  const int rr = min(row, rows - 1);
+  const size_t piece = (size_t)p.part_rows;
+  float M = -CUDART_INF_F, sum = 0.f;
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+  for (int k = 0; k < n_parts; ++k) {
+    if (k > 0 && (k & 31) == 0) places = k + lane < n_parts ? __ldcg(list + (size_t)(k + lane) * kPlanWords) : 0;
+    const float* src = p.part + (size_t)__shfl_sync(0xffffffffu, places, k & 31) * (piece * kXtPartFloats);
+    const float lk = __ldcg(src + 128 * piece + rr);
+    const float4 y = __ldcg(reinterpret_cast<const float4*>(src) + (size_t)c4 * piece + rr);
+    const float Mn = fmaxf(M, lk);
+    const float keep = M == -CUDART_INF_F ? 0.f : fast_exp2(M - Mn), w = lk == -CUDART_INF_F ? 0.f : fast_exp2(lk - Mn);
+    M = Mn;
+    sum = fmaf(sum, keep, w);
+    acc.x = fmaf(acc.x, keep, w * y.x);
+    acc.y = fmaf(acc.y, keep, w * y.y);
+    acc.z = fmaf(acc.z, keep, w * y.z);
+    acc.w = fmaf(acc.w, keep, w * y.w);
   }
+  if (row >= rows) return;
+  const float f = p.out_scale / sum;
+  const int ti = row / x.G;
+  __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(x.out) + (((size_t)layer * x.total + tok + ti) * x.Hq + h * x.G + (row - ti * x.G)) * 128 + c4 * 4;
+  *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16x2(acc.x * f, acc.y * f), pack_bf16x2(acc.z * f, acc.w * f));
+  if (c4 == 0 && x.lse) x.lse[ext_lse_index(x, layer, h, tok) + row] = M + __log2f(sum);
 }
 
 // The end of a piece, by the eight softmax warps: a group's 64 columns of the output, or of its part of an item that
-// other CTAs share.  If every other part already lies in the scratch (and they are few), this CTA joins them with
-// its own still in tensor memory; else it leaves its part, and joins all if it turns out to be the last.
+// other CTAs share.
 template <bool KV8>
 __device__ __noinline__ void xt_epilogue(const ExtendTcParams& p, int d, int ord, float ref, float l, uint32_t tO, uint32_t bar0, volatile int* s_abort,
-                                         uint8_t* s_out, int* s_flag) {
+                                         uint8_t* s_out) {
   const ExtendParams& x = p.x;
   auto word = [&](int w) { return __shfl_sync(0xffffffffu, d, w); };
-  auto all_sync = [&]() { asm volatile("bar.sync 1, 256;" ::: "memory"); };
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, wg = warp >> 2, wq = warp & 3;
-  const int r = wq * 32 + lane, rows = word(kPwRows), n_parts = word(kPwParts), h = word(kPwHead), layer = word(kPwLayer), tok = word(kPwTok);
-  const uint32_t g_inv = 65536u / (uint32_t)x.G + 1u;
-  uint8_t* stage = s_out + warp * kXtStageBytes;
-  const float out_scale = KV8 ? x.v_scale : 1.f;
-  const bool live = wq * 32 < rows, mine = r < rows, whole = n_parts == 1;
-  const size_t piece = (size_t)p.part_rows;
-  float* part = p.part + (size_t)word(kPwPlace) * (piece * kXtPartFloats);
-  const int* list = p.plan.words + (size_t)word(kPwBase) * kPlanWords + kPwList;
-  unsigned* counter = x.counters + word(kPwCounter);
-  bool join = false;
-  if (n_parts == 2) {  // (with more, the joint by all warps is faster than one thread per row)
-    if (tid == 0) {
-      unsigned done;
-      asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(done) : "l"(counter) : "memory");
-      *s_flag = done == 1u;
-    }
-    all_sync();
-    join = *s_flag != 0;
-  }
+  const int r = wq * 32 + lane, rows = word(kPwRows), h = word(kPwHead), layer = word(kPwLayer), tok = word(kPwTok);
+  const bool whole = word(kPwParts) == 1;
   mbar_wait(bar0 + 8 * 12, (uint32_t)(ord & 1), s_abort, x.err, kPfSpinLimit);
   tc5::fence_after_sync();
-  if (live) {
-    const bool redo = mine && !(l < kXtSumMax);  // out of range, or not a number
-    float lse = l > 0.f ? ref + __log2f(l) : -CUDART_INF_F;
-    const float f = l > 0.f ? 1.f / l : 0.f;
-    float w_own = 1.f, w_other = 0.f, all = lse;
-    const float4* other = nullptr;
-    __nv_bfloat16* obase = static_cast<__nv_bfloat16*>(x.out) + (((size_t)layer * x.total + tok) * x.Hq + h * x.G) * 128;
-    const uint32_t t_row = tO + ((uint32_t)(wq * 32) << 16);
-#pragma unroll 1
-    for (int c0 = 64 * wg; c0 < 64 * wg + 64; c0 += 32) {
-      uint32_t o[32];
-      tc5::tmem_ld32(t_row + (uint32_t)c0, o);
-      tc5::tmem_wait_ld();
-      if (c0 == 64 * wg + 32) {
-        tc5::fence_before_sync();
-        mbar_arrive(bar0 + 8 * 7);  // O may be written again
-      }
-      const uint64_t f2 = tc5::f2_pack(f, f);
-      uint64_t probe[2] = {0ull, 0ull};  // 0 * finite = 0
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const uint64_t y = tc5::f2_mul(tc5::f2_pack(__uint_as_float(o[2 * e]), __uint_as_float(o[2 * e + 1])), f2);
-        probe[e & 1] = tc5::f2_fma(y, 0ull, probe[e & 1]);
-        float y0, y1;
-        tc5::f2_unpack(y, y0, y1);
-        o[2 * e] = __float_as_uint(y0);
-        o[2 * e + 1] = __float_as_uint(y1);
-      }
-      float p0, p1;
-      tc5::f2_unpack(tc5::f2_add(probe[0], probe[1]), p0, p1);
-      unsigned again = __ballot_sync(0xffffffffu, mine && (redo || !(p0 + p1 == 0.f)));
-      while (again) {
-        const int who = __ffs(again) - 1;
-        again &= again - 1;
-        const bool full = __shfl_sync(0xffffffffu, redo ? 1 : 0, who) != 0;
-        float new_lse = __shfl_sync(0xffffffffu, lse, who);
-        const float4 y = xt_row_again<KV8>(p, d, wq * 32 + who, full, new_lse);
-        __syncwarp();
-        reinterpret_cast<float4*>(stage)[lane] = y;
-        __syncwarp();
-        if (lane == who) {
-          lse = new_lse;
-#pragma unroll
-          for (int e = 0; e < 32; ++e)
-            if (full || !(__uint_as_float(o[e]) * 0.f == 0.f)) o[e] = reinterpret_cast<const uint32_t*>(stage)[c0 + e];
-        }
-        __syncwarp();
-      }
-      if (c0 == 64 * wg) {
-        all = lse;
-        if (join) {  // (the sum is symmetric: whoever joins gets the same)
-          const int a = __ldcg(list), b = __ldcg(list + kPlanWords), rr = min(r, rows - 1);
-          const float* base = p.part + (size_t)(a == word(kPwPlace) ? b : a) * (piece * kXtPartFloats);
-          other = reinterpret_cast<const float4*>(base) + rr;
-          const float lo = __ldcg(base + 128 * piece + rr);
-          const float M = fmaxf(lse, lo);
-          if (M > -CUDART_INF_F) {
-            all = M + __log2f((lse == -CUDART_INF_F ? 0.f : exp2f(lse - M)) + (lo == -CUDART_INF_F ? 0.f : exp2f(lo - M)));
-            w_own = lse == -CUDART_INF_F ? 0.f : fast_exp2(lse - all);
-            w_other = lo == -CUDART_INF_F ? 0.f : fast_exp2(lo - all);
-          } else {  // (not a number on one side: it stays one)
-            all = lse + lo;
-          }
-        }
-      }
-      if (join) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float4 y = __ldcg(other + ((size_t)c0 / 4 + e) * piece);
-          o[4 * e] = __float_as_uint(fmaf(w_other, y.x, w_own * __uint_as_float(o[4 * e])));
-          o[4 * e + 1] = __float_as_uint(fmaf(w_other, y.y, w_own * __uint_as_float(o[4 * e + 1])));
-          o[4 * e + 2] = __float_as_uint(fmaf(w_other, y.z, w_own * __uint_as_float(o[4 * e + 2])));
-          o[4 * e + 3] = __float_as_uint(fmaf(w_other, y.w, w_own * __uint_as_float(o[4 * e + 3])));
-        }
-      }
-      if (whole || join) {
-        // rounded, through the warp's staging tile [32 rows][64 B] (16-byte chunks swizzled), so that the stores are 64-byte
-        // pieces of rows
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          uint32_t y[4];
-#pragma unroll
-          for (int u = 0; u < 4; ++u) {
-            float y0 = __uint_as_float(o[8 * e + 2 * u]), y1 = __uint_as_float(o[8 * e + 2 * u + 1]);
-            if constexpr (KV8) {
-              y0 *= x.v_scale;
-              y1 *= x.v_scale;
-            }
-            y[u] = pack_bf16x2(y0, y1);
-          }
-          *reinterpret_cast<uint4*>(stage + lane * 64 + ((e ^ ((lane >> 1) & 3)) << 4)) = make_uint4(y[0], y[1], y[2], y[3]);
-        }
-        __syncwarp();
-        const bool store = *s_abort == 0;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int row = 8 * i + (lane >> 2), chunk = lane & 3;
-          const uint4 v = *reinterpret_cast<const uint4*>(stage + row * 64 + ((chunk ^ ((row >> 1) & 3)) << 4));
-          const int rr = wq * 32 + row, ti = (int)((uint32_t)rr * g_inv >> 16);
-          if (rr < rows && store) *reinterpret_cast<uint4*>(obase + (ti * x.Hq + (rr - ti * x.G)) * 128 + c0 + chunk * 8) = v;
-        }
-        __syncwarp();
-      } else if (mine && !*s_abort) {
-        float4* dst = reinterpret_cast<float4*>(part) + (size_t)c0 / 4 * piece + r;
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-          __stcg(dst + e * piece,
-                 make_float4(__uint_as_float(o[4 * e]), __uint_as_float(o[4 * e + 1]), __uint_as_float(o[4 * e + 2]), __uint_as_float(o[4 * e + 3])));
-      }
-    }
-    if (wg == 0 && mine && !*s_abort) {
-      if (!whole && !join) __stcg(part + 128 * piece + r, lse);
-      else if (x.lse) x.lse[ext_lse_index(x, layer, h, tok) + r] = all;
-    }
-  } else {
+  if (wq * 32 >= rows) {  // no query in this warp's rows
     mbar_arrive(bar0 + 8 * 7);
-  }
-  if (whole) return;
-  if (join) {
-    all_sync();  // (the flag has been read by all)
     return;
   }
-  __threadfence();
-  all_sync();
-  if (tid == 0) *s_flag = atomicAdd(counter, 1u) == (unsigned)(n_parts - 1);
-  all_sync();
-  const bool last = *s_flag != 0;
-  if (last) {
-    __threadfence();
-    xt_join_parts(p, d, out_scale, s_abort);
+  const uint32_t g_inv = 65536u / (uint32_t)x.G + 1u;
+  uint8_t* stage = s_out + warp * kXtStageBytes;
+  const bool mine = r < rows;
+  const size_t piece = (size_t)p.part_rows;
+  float* part = p.part + (size_t)word(kPwPlace) * (piece * kXtPartFloats);
+  const bool redo = mine && !(l < kXtSumMax);  // out of range, or not a number
+  float lse = l > 0.f ? ref + __log2f(l) : -CUDART_INF_F;
+  const float f = l > 0.f ? 1.f / l : 0.f;
+  __nv_bfloat16* obase = static_cast<__nv_bfloat16*>(x.out) + (((size_t)layer * x.total + tok) * x.Hq + h * x.G) * 128;
+  const uint32_t t_row = tO + ((uint32_t)(wq * 32) << 16);
+#pragma unroll 1
+  for (int c0 = 64 * wg; c0 < 64 * wg + 64; c0 += 32) {
+    uint32_t o[32];
+    tc5::tmem_ld32(t_row + (uint32_t)c0, o);
+    tc5::tmem_wait_ld();
+    if (c0 == 64 * wg + 32) {
+      tc5::fence_before_sync();
+      mbar_arrive(bar0 + 8 * 7);  // O may be written again
+    }
+    const uint64_t f2 = tc5::f2_pack(f, f);
+    uint64_t probe[2] = {0ull, 0ull};  // 0 * finite = 0
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      const uint64_t y = tc5::f2_mul(tc5::f2_pack(__uint_as_float(o[2 * e]), __uint_as_float(o[2 * e + 1])), f2);
+      probe[e & 1] = tc5::f2_fma(y, 0ull, probe[e & 1]);
+      float y0, y1;
+      tc5::f2_unpack(y, y0, y1);
+      o[2 * e] = __float_as_uint(y0);
+      o[2 * e + 1] = __float_as_uint(y1);
+    }
+    float p0, p1;
+    tc5::f2_unpack(tc5::f2_add(probe[0], probe[1]), p0, p1);
+    unsigned again = __ballot_sync(0xffffffffu, mine && (redo || !(p0 + p1 == 0.f)));
+    while (again) {
+      const int who = __ffs(again) - 1;
+      again &= again - 1;
+      const bool full = __shfl_sync(0xffffffffu, redo ? 1 : 0, who) != 0;
+      float new_lse = __shfl_sync(0xffffffffu, lse, who);
+      const float4 y = xt_row_again<KV8>(p, d, wq * 32 + who, full, new_lse);
+      __syncwarp();
+      reinterpret_cast<float4*>(stage)[lane] = y;
+      __syncwarp();
+      if (lane == who) {
+        lse = new_lse;
+#pragma unroll
+        for (int e = 0; e < 32; ++e)
+          if (full || !(__uint_as_float(o[e]) * 0.f == 0.f)) o[e] = reinterpret_cast<const uint32_t*>(stage)[c0 + e];
+      }
+      __syncwarp();
+    }
+    if (whole) {
+      // rounded, through the warp's staging tile [32 rows][64 B] (16-byte chunks swizzled), so that the stores are 64-byte
+      // pieces of rows
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        uint32_t y[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          float y0 = __uint_as_float(o[8 * e + 2 * u]), y1 = __uint_as_float(o[8 * e + 2 * u + 1]);
+          if constexpr (KV8) {
+            y0 *= p.out_scale;
+            y1 *= p.out_scale;
+          }
+          y[u] = pack_bf16x2(y0, y1);
+        }
+        *reinterpret_cast<uint4*>(stage + lane * 64 + ((e ^ ((lane >> 1) & 3)) << 4)) = make_uint4(y[0], y[1], y[2], y[3]);
+      }
+      __syncwarp();
+      const bool store = *s_abort == 0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int row = 8 * i + (lane >> 2), chunk = lane & 3;
+        const uint4 v = *reinterpret_cast<const uint4*>(stage + row * 64 + ((chunk ^ ((row >> 1) & 3)) << 4));
+        const int rr = wq * 32 + row, ti = (int)((uint32_t)rr * g_inv >> 16);
+        if (rr < rows && store) *reinterpret_cast<uint4*>(obase + (ti * x.Hq + (rr - ti * x.G)) * 128 + c0 + chunk * 8) = v;
+      }
+      __syncwarp();
+    } else if (mine && !*s_abort) {
+      float4* dst = reinterpret_cast<float4*>(part) + (size_t)c0 / 4 * piece + r;
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        __stcg(dst + e * piece,
+               make_float4(__uint_as_float(o[4 * e]), __uint_as_float(o[4 * e + 1]), __uint_as_float(o[4 * e + 2]), __uint_as_float(o[4 * e + 3])));
+    }
   }
-  all_sync();
+  if (wg == 0 && mine && !*s_abort) {
+    if (!whole) __stcg(part + 128 * piece + r, lse);
+    else if (x.lse) x.lse[ext_lse_index(x, layer, h, tok) + r] = lse;
+  }
 }
 
 template <bool KV8, bool MODS>
@@ -431,10 +403,10 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
   auto bar = [&](int i) { return bar0 + 8u * (uint32_t)i; };
   uint32_t* s_tmem = reinterpret_cast<uint32_t*>(bars + 15);
   volatile int* s_abort = reinterpret_cast<volatile int*>(s_tmem + 1);
-  int* s_flag = reinterpret_cast<int*>(s_tmem + 2);
   const ExtendParams& x = p.x;
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  constexpr int kSWarp = 10, kOWarp = 11;  // the warps that issue S and O
   if (tid == 0) {
     for (int i = 0; i < 15; ++i) mbar_init(bar(i), i == 7 ? 2 * kXtRows : (i == 8 || i == 9) ? kXtRows : KV8 && (i == 1 || i == 2) ? 2 : 1);
     *s_abort = 0;
@@ -445,11 +417,11 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
-  if (warp == 10) {
+  if (warp == kSWarp) {
     tc5::tmem_alloc(smem_u32(s_tmem), kPfTmemCols);
     tc5::tmem_relinquish();
   }
-  if (tid == 9 * 32) {
+  if (tid == 8 * 32) {
     asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&tmQ)) : "memory");
     if constexpr (!KV8) {
       asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&tmK)) : "memory");
@@ -461,6 +433,7 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
   const int item = plan_item_of(p.plan, x.seqs.n, share) + (int)blockIdx.x;
   int slot = __shfl_sync(0xffffffffu, item, 0);
   const int slot_end = __shfl_sync(0xffffffffu, item, 1) + 1;
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // (the next kernel finds room when CTAs of this one end, and waits for all)
   // The storing kernel may still be running; everything below waits until it has completed.
   asm volatile("griddepcontrol.wait;" ::: "memory");
   int d = __ldcg(p.plan.words + (size_t)slot * kPlanWords + lane);  // the piece's words, one per lane
@@ -480,14 +453,10 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
     d = d_next;
   };
 
-  if (warp == 8 || warp == 9) {
-    // ================= the warps that load: 8 Q and K, 9 V (8-bit rows: 8 Q and half of K, 9 the other half) =================
+  if (warp >= 8 && warp < kSWarp) {
+    // ================= the warps that load: 8 Q and K, 9 V; 8-bit rows: 8 Q and half of K, 9 the other half =================
     if (lane == 0 && *reinterpret_cast<volatile int*>(p.stop) != 0) *s_abort = 1;
     __syncwarp();
-    const bool is_k = KV8 || warp == 8;
-    // a stage is filled again when the product that read it has completed: S of tile g - 2 (K), O += P V of it (V)
-    const int freed = is_k ? 5 : 10, filled = is_k ? 1 : 3;
-    const uint32_t base = is_k ? sK : sV;
     int g = 0;
     for (; slot < slot_end && !*s_abort; go_next()) {
       ask_next();
@@ -502,56 +471,60 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
         if (lane == 0 && j + 4 < nkt)
           asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(src + (size_t)(k0 - 4 * kPfKeys) * 128), "r"(32 * 128) : "memory");
       };
-      if constexpr (KV8) {
-        if (nkt > 0) fetch(0);
-      }
-      for (int j = 0; j < nkt; ++j, ++g) {
-        if (warp == 8 && j == 0) {
-          // the piece's Q, once the last S of the piece before has been computed from its own
-          if (g >= 1) mbar_wait(bar(5 + ((g - 1) & 1)), (uint32_t)(((g - 1) >> 1) & 1), s_abort, x.err, kPfSpinLimit);
-          const int tok = word(kPwLayer) * x.total + word(kPwTok), head = word(kPwHead) * x.G;
-          if (!*s_abort && tc5::elect_one()) {
-            mbar_arrive_expect_tx(bar(0), 256u * (uint32_t)(x.G * p.plan.tokens_per_tile));
-            pf_tma_load(sQ, &tmQ, 0, head, tok, bar(0));
-            pf_tma_load(sQ + kPfQBytes / 2, &tmQ, 64, head, tok, bar(0));
-          }
-          __syncwarp();
-        } else if (g >= 2) {
-          mbar_wait(bar(freed + (g & 1)), (uint32_t)(((g - 2) >> 1) & 1), s_abort, x.err, kPfSpinLimit);
-        }
-        __syncwarp();
-        if (*s_abort) break;
-        const uint32_t bb = bar(filled + (g & 1));
-        if constexpr (KV8) {
-          uint8_t* tile = sm + kPfQBytes + (uint32_t)(g & 1) * kPfKvBytes;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) xt_store_codes<false>(codes[i], tile, kPfKvBytes / 2, 32 * (warp & 1) + 8 * i, lane);
-          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-          __syncwarp();
-          if (lane == 0) mbar_arrive(bb);
-          if (j + 1 < nkt) fetch(j + 1);
-        } else if (tc5::elect_one()) {
-          const uint32_t dst = base + (uint32_t)(g & 1) * kPfKvBytes;
-          const CUtensorMap* tm = is_k ? &tmK : &tmV;
+      auto load_tile = [&](const CUtensorMap* tm, uint32_t base, int filled, int j) {
+        if (tc5::elect_one()) {
+          const uint32_t dst = base + (uint32_t)(g & 1) * kPfKvBytes, bb = bar(filled + (g & 1));
           const int row = (kt_new - j) * kPfKeys;
           mbar_arrive_expect_tx(bb, kPfKvBytes);
           pf_tma_load(dst, tm, 0, row, slab, bb);
           pf_tma_load(dst + kPfKvBytes / 2, tm, 64, row, slab, bb);
         }
         __syncwarp();
+      };
+      if constexpr (KV8) {
+        if (nkt > 0) fetch(0);
+      }
+      for (int j = 0; j < nkt; ++j, ++g) {
+        // The piece's Q, once the last S of the piece before has been computed from its own; a K stage is filled again when
+        // S of tile g - 2 has read it, a V stage when O += P V of tile g - 2 has.
+        const bool new_q = warp == 8 && j == 0;
+        const int done = new_q ? g - 1 : g - 2, freed = KV8 || warp == 8 ? 5 : 10;
+        if (done >= 0) mbar_wait(bar(freed + (done & 1)), (uint32_t)((done >> 1) & 1), s_abort, x.err, kPfSpinLimit);
+        __syncwarp();
+        if (*s_abort) break;
+        if (new_q) {
+          const int tok = word(kPwLayer) * x.total + word(kPwTok), head = word(kPwHead) * x.G;
+          if (tc5::elect_one()) {
+            mbar_arrive_expect_tx(bar(0), 256u * (uint32_t)(x.G * p.plan.tokens_per_tile));
+            pf_tma_load(sQ, &tmQ, 0, head, tok, bar(0));
+            pf_tma_load(sQ + kPfQBytes / 2, &tmQ, 64, head, tok, bar(0));
+          }
+          __syncwarp();
+        }
+        if constexpr (KV8) {
+          uint8_t* tile = sm + kPfQBytes + (uint32_t)(g & 1) * kPfKvBytes;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) xt_store_codes<false>(codes[i], tile, kPfKvBytes / 2, 32 * (warp & 1) + 8 * i, lane);
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar(1 + (g & 1)));
+          if (j + 1 < nkt) fetch(j + 1);
+          __syncwarp();
+        } else {
+          if (warp == 8) load_tile(&tmK, sK, 1, j);
+          else load_tile(&tmV, sV, 3, j);
+        }
       }
     }
     if (*s_abort && lane == 0) {
       // Something gave up: a bounded time for the loads this warp started (see prefill_attn.cuh).
       atomicOr(p.stop, 1);
-      for (int i = 0; i < 5; ++i) {
-        if (i == 0 ? warp != 8 : KV8 || (i <= 2) != is_k) continue;
+      for (int i = warp == 8 ? 0 : 3; i < (warp == 8 ? (KV8 ? 1 : 3) : (KV8 ? 3 : 5)); ++i)
         for (uint32_t ph = 0; ph < 2; ++ph)
           for (uint32_t w = 0; w < (1u << 16); ++w)
             if (mbar_try_wait(bar(i), ph)) break;
-      }
     }
-  } else if (warp == 11) {
+  } else if (warp == kOWarp) {
     // ================= the warp that issues O += P V =================
     constexpr uint32_t idesc_o = tc5::idesc_bf16_f32(kXtRows, 128, 0, 1);
     const uint64_t dV = tc5::smem_desc_sw128(sV, kPfKvBytes / 2, 1024);
@@ -586,7 +559,7 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
       for (uint32_t w = 0; w < kPfSpinLimit; ++w)
         if (mbar_try_wait(bar(13), 0u)) break;
     }
-  } else if (warp == 10) {
+  } else if (warp == kSWarp) {
     // ================= the warp that issues S = Q K^T =================
     constexpr uint32_t idesc_s = KV8 ? tc5::idesc_f16_f32(kXtRows, kPfKeys, 0, 0) : tc5::idesc_bf16_f32(kXtRows, kPfKeys, 0, 0);
     const uint64_t dQ = tc5::smem_desc_sw128(sQ, 16, 1024);
@@ -625,8 +598,8 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
   } else {
     // ================= softmax warps: thread = query row = tensor-memory lane =================
     const int wg = warp >> 2, wq = warp & 3;              // group; warp within it (its lanes of tensor memory)
-    uint8_t* stage = s_out + warp * kXtStageBytes;
-    const float* stage_other = reinterpret_cast<const float*>(s_out + (warp ^ 4) * kXtStageBytes);  // the warp of the other group with the same rows
+    const uint32_t stage = smem_u32(s_out) + (uint32_t)warp * kXtStageBytes;
+    const uint32_t abort_flag = bar0 + 124u;
     const uint32_t t_row = tS0 + ((uint32_t)(wq * 32) << 16);
     auto pair_sync = [&]() { asm volatile("bar.sync %0, 64;" ::"r"(2 + wq) : "memory"); };
     int g0 = 0, ord = 0;  // flat index of the piece's first tile, piece
@@ -656,7 +629,7 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
       int j = wg == 0 ? 0 : ramp;
       if (wg == 1) {  // the reference comes from the first group's first tiles
         pair_sync();
-        ref = stage_other[128 + lane];
+        ref = lds_f(smem_u32(s_out) + (uint32_t)(warp ^ 4) * kXtStageBytes + 512u + 4u * lane);  // (of the warp with the same rows)
       }
 #pragma unroll 1
       while (j < nkt) {
@@ -677,7 +650,7 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
           if (lane == 0 && j + 4 < nkt)
             asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(v_codes + (size_t)(key0 + 16 * wq - 4 * kPfKeys) * 128), "r"(16 * 128) : "memory");
         }
-        mbar_wait(bar(5 + (g & 1)), (uint32_t)((g >> 1) & 1), s_abort, x.err, kPfSpinLimit);  // S of this tile is complete
+        xt_wait(bar(5 + (g & 1)), (uint32_t)((g >> 1) & 1), abort_flag, x.err);  // S of this tile is complete
         tc5::fence_after_sync();
         if constexpr (KV8) {
           // (S of this tile was issued after O += P V of tile g - 2 had read the stage)
@@ -690,16 +663,15 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
           constexpr int CH = 32;
           bool border = false, beside = false;
           float at = 0.f;                                       // this row's token
-          const int* ipos = reinterpret_cast<const int*>(stage);             // positions behind the tile's first
-          const float* fpos = reinterpret_cast<const float*>(stage) + 64;
+          // (the staging tile: positions behind the tile's first, [64] as integers and [64] as floats)
           int me = 0;
           if constexpr (MODS) {
             const int p0 = __shfl_sync(0xffffffffu, pos_a, 0);
             __syncwarp();
-            reinterpret_cast<int*>(stage)[lane] = pos_a - p0;
-            reinterpret_cast<int*>(stage)[32 + lane] = pos_b - p0;
-            reinterpret_cast<float*>(stage)[64 + lane] = (float)(pos_a - p0);
-            reinterpret_cast<float*>(stage)[96 + lane] = (float)(pos_b - p0);
+            sts_i(stage + 4u * lane, pos_a - p0);
+            sts_i(stage + 128u + 4u * lane, pos_b - p0);
+            sts_f(stage + 256u + 4u * lane, (float)(pos_a - p0));
+            sts_f(stage + 384u + 4u * lane, (float)(pos_b - p0));
             me = ti - p0;
             at = (float)me;
             const bool fresh = key0 + kPfKeys > held;  // the tile holds rows of the chunk
@@ -729,12 +701,12 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
               const uint64_t scale2 = tc5::f2_pack(scale, scale);
               if (beside) {
 #pragma unroll
-                for (int c = 0; c < CH; ++c) sv[c] = __float_as_uint(fmaf(__uint_as_float(sv[c]), scale, -slope * fabsf(at - fpos[hb + c])));
+                for (int c = 0; c < CH; ++c) sv[c] = __float_as_uint(fmaf(__uint_as_float(sv[c]), scale, -slope * fabsf(at - lds_f(stage + 256u + 4u * (uint32_t)(hb + c)))));
               } else {  // - slope (me - pos) = slope pos - slope me, both counted from the tile's first row
                 const uint64_t slope2 = tc5::f2_pack(slope, slope), base2 = tc5::f2_pack(-slope * at, -slope * at);
 #pragma unroll
                 for (int c = 0; c < CH; c += 4) {
-                  const float4 y = *reinterpret_cast<const float4*>(fpos + hb + c);
+                  const float4 y = lds_f4(stage + 256u + 4u * (uint32_t)(hb + c));
                   float x0, x1, x2, x3;
                   tc5::f2_unpack(tc5::f2_fma(tc5::f2_pack(__uint_as_float(sv[c]), __uint_as_float(sv[c + 1])), scale2,
                                              tc5::f2_fma(tc5::f2_pack(y.x, y.y), slope2, base2)), x0, x1);
@@ -749,7 +721,7 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
               if (border) {
 #pragma unroll
                 for (int c = 0; c < CH; c += 4) {
-                  const int4 y = *reinterpret_cast<const int4*>(ipos + hb + c);
+                  const int4 y = lds_i4(stage + 4u * (uint32_t)(hb + c));
                   if (abs(me - y.x) >= x.window) sv[c] = 0xff800000u;  // -inf
                   if (abs(me - y.y) >= x.window) sv[c + 1] = 0xff800000u;
                   if (abs(me - y.z) >= x.window) sv[c + 2] = 0xff800000u;
@@ -796,7 +768,7 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
         if (wg == 1) {
           j += 2;
         } else if (++j == ramp) {
-          reinterpret_cast<float*>(stage)[128 + lane] = ref;
+          sts_f(stage + 512u + 4u * lane, ref);
           pair_sync();
           ++j;
         } else if (j > ramp) {
@@ -805,18 +777,18 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
       }
       g0 += nkt;
       // the other group's share of the row's sum
-      reinterpret_cast<float*>(stage)[160 + lane] = l;
+      sts_f(stage + 640u + 4u * lane, l);
       pair_sync();
-      const float l_other = stage_other[160 + lane];
+      const float l_other = lds_f(smem_u32(s_out) + (uint32_t)(warp ^ 4) * kXtStageBytes + 640u + 4u * lane);
       l = wg == 0 ? l + l_other : l_other + l;
       pair_sync();
-      xt_epilogue<KV8>(p, d, ord, ref, l, tO, bar0, s_abort, s_out, s_flag);
+      xt_epilogue<KV8>(p, d, ord, ref, l, tO, bar0, s_abort, s_out);
       ++ord;
     }
   }
   tc5::fence_before_sync();
   __syncthreads();
-  if (warp == 10) tc5::tmem_dealloc(tmem, kPfTmemCols);
+  if (warp == kSWarp) tc5::tmem_dealloc(tmem, kPfTmemCols);
 }
 
 // extend_mass_tc_kernel: mass_j = sum over the chunk's tokens i and the group's heads of exp2(x_ij - lse_i).
