@@ -1368,7 +1368,7 @@ ExtendScratch extend_scratch(const dynts_cache* c, const int* n_new, int n_layer
     if (f.dtype == DYNTS_BF16_KV8) m.q16 = take((size_t)n_layers * total * f.q_heads * f.head_dim * 2);
     m.part = take((size_t)2 * m.ctas * m.part_rows * dynts::kXtPartFloats * sizeof(float));
     m.counters = take((size_t)m.ctas * sizeof(int));  // of cut mass items
-    m.mass = take((size_t)m.ctas * kMassParts * dynts::kXmKeys * sizeof(float));
+    m.mass = take((size_t)m.ctas * kMassParts * dynts::kXmItemKeys * sizeof(float));
     long long items = 0;  // of the launch with the most sequences' worth (a batch beyond 128 sequences takes several)
     for (int b0 = 0; b0 < f.batch; b0 += dynts::kExtSeqs) {
       long long tiles = 0;
@@ -1582,7 +1582,7 @@ dynts_status_t launch_extend_tc(dynts_cache* c, const dynts::ExtendParams& x, co
   p.scale_log2 = (float)(1.4426950408889634 * (double)x.scale);
   p.cap_log2 = (float)(1.4426950408889634 * (double)x.cap_logit);
   p.cap_arg = x.cap_logit > 0.f ? (float)(2.0 * 1.4426950408889634 * (double)x.scale / (double)x.cap_logit) : 0.f;
-  // Mass items: 128 rows of a slab each.  Fewer than CTAs: their query rows are cut, in parts of at least two steps.
+  // Mass items: 256 rows of a slab each.  Fewer than CTAs: their query rows are cut, in parts of at least two steps.
   p.mass_part = reinterpret_cast<float*>(scratch + m.mass);
   p.mass_counters = x.counters;
   p.mass_items = m.ctas;
@@ -1592,7 +1592,7 @@ dynts_status_t launch_extend_tc(dynts_cache* c, const dynts::ExtendParams& x, co
     int longest = 0;
     for (int s = 0; s < x.seqs.n; ++s) {
       const int t = x.seqs.tok0[s + 1] - x.seqs.tok0[s];
-      if (t > 0) items += (c->len_h[x.seqs.b0 + s] + t + dynts::kXmKeys - 1) / dynts::kXmKeys;
+      if (t > 0) items += (c->len_h[x.seqs.b0 + s] + t + dynts::kXmItemKeys - 1) / dynts::kXmItemKeys;
       longest = std::max(longest, t);
     }
     items *= plan.lh;

@@ -67,7 +67,7 @@ struct ExtendTcParams {
   int* stop;
   int mass_parts;       // parts the query rows of a mass item are cut into, while there are at most mass_items items
   int mass_items;
-  float* mass_part;     // [mass_items][mass_parts][128]
+  float* mass_part;     // [mass_items][mass_parts][256]
   unsigned int* mass_counters;  // [mass_items], cleared by the storing kernel
   float out_scale;      // v_scale for 8-bit rows
   float scale_log2;     // log2(e) * scale
@@ -794,18 +794,20 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
 // extend_mass_tc_kernel: mass_j = sum over the chunk's tokens i and the group's heads of exp2(x_ij - lse_i).
 // The products are taken the other way round -- M = 128 keys, N = 64 query rows -- so that thread = key = tensor-
 // memory lane: the sum over the queries stays in one register, needs no exchange between lanes and no atomics, and
-// exactly one thread writes a row.  A work item = 128 rows of one slab against the query rows that see any of them;
-// where the items are fewer than the CTAs the query rows of each are cut into parts, whose sums the last part to
-// finish adds in order.  Persistent CTAs, two per SM; K tiles and Q tiles (64 rows) in two stages each, S in four
-// buffers of 64 columns, two groups of four warps that take the steps in turn (as in extend_tc_kernel; with one group
-// and two buffers the same work took 1.4 times as long).  Bound by the exponentials and the chain S - read - exponentials.
-constexpr int kXmThreads = 384;
-constexpr int kXmKeys = 128;
+// exactly one thread writes a row.  A work item = 256 rows of one slab, 128 for each of two groups of four warps, against
+// the query rows that see any of them, in steps of 64; where the items are fewer than the CTAs the steps of each are
+// cut into parts, whose sums the last part to finish adds in order.  Persistent CTAs, two per SM; K 64 KB, Q in two
+// stages, S in two buffers of 64 columns per group.  (With 128 rows per item the Q tiles, read again from L2 for
+// every item, and the products' own reads of K and Q from shared memory bounded it: 1.25 times as long.)  What bounds it
+// now is the exponentials' unit and the chain S - read - exponentials.
+constexpr int kXmThreads = 320;
+constexpr int kXmKeys = 128;                      // keys per group
+constexpr int kXmItemKeys = 2 * kXmKeys;
 constexpr int kXmRows = 64;                       // query rows per step
 constexpr int kXmKBytes = kXmKeys * 256;
 constexpr int kXmQBytes = kXmRows * 256;
 constexpr int kXmWarpFloats = 128;                // per compute warp: a step's additive constants, its columns' negated slopes
-constexpr int kXmSmemBytes = 2 * kXmKBytes + 2 * kXmQBytes + 192 + (8 * kXmWarpFloats + kXmRows + 2 * kXmKeys) * 4 + (2 * kExtSeqs + 1) * 4 + 12;
+constexpr int kXmSmemBytes = 2 * kXmKBytes + 2 * kXmQBytes + 192 + (8 * kXmWarpFloats + kXmRows) * 4 + (2 * kExtSeqs + 1) * 4 + 12;
 constexpr uint32_t kXmTmemCols = 256;
 
 struct XmCursor {
@@ -832,13 +834,13 @@ __device__ __forceinline__ void xm_seek(XmCursor& c, int it, int n_items, const 
     c.s = ext_find(sh.item0, p.x.seqs.n, u);
     c.n = sh.n[c.s];
     c.t = p.x.seqs.tok0[c.s + 1] - p.x.seqs.tok0[c.s];
-    c.k0 = (u - sh.item0[c.s]) * kXmKeys;
+    c.k0 = (u - sh.item0[c.s]) * kXmItemKeys;
     c.layer = p.x.n_layers == 1 ? 0 : lh / p.x.Hkv;
     c.h = lh - c.layer * p.x.Hkv;
     int lo = c.k0 < c.n + p.x.seqs.prefix[c.s] ? 0 : (c.k0 - c.n) / tps;
     int hi = (c.t + tps - 1) / tps;
     if (p.x.window > 0) {  // a token is at least as many positions behind a row as it is rows behind it
-      const long long last = (long long)p.x.window + c.k0 + kXmKeys - 1 - c.n;  // tokens from here on see none of the rows
+      const long long last = (long long)p.x.window + c.k0 + kXmItemKeys - 1 - c.n;  // tokens from here on see none of the rows
       hi = last <= 0 ? 0 : (int)min((long long)hi, (last + tps - 1) / tps);
     }
     hi = max(lo, hi);
@@ -859,10 +861,10 @@ __global__ void __launch_bounds__(kXmThreads, 2)
 extend_mass_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK) {
   extern __shared__ __align__(1024) uint8_t pf_smem[];
   uint8_t* sm = pf_smem;
-  const uint32_t sK = smem_u32(sm);             // [2 stages][2 halves of head_dim][128 rows][128 B]
+  const uint32_t sK = smem_u32(sm);             // [2 groups][2 halves of head_dim][128 rows][128 B]
   const uint32_t sQ = sK + 2 * kXmKBytes;       // [2 stages][2 halves][64 rows][128 B]
   uint64_t* bars = reinterpret_cast<uint64_t*>(sm + 2 * kXmKBytes + 2 * kXmQBytes);
-  // barriers: 0-1 K stages filled, 2-3 Q stages filled, 4-7 S buffers complete, 8-11 S buffers read, 12-13 K stages read, 14 drain
+  // barriers: 0 K filled, 1-2 Q stages filled, 3-6 S complete (2 x group + buffer), 7-10 S read (the same), 11 K read, 12 drain
   const uint32_t bar0 = smem_u32(bars);
   auto bar = [&](int i) { return bar0 + 8u * (uint32_t)i; };
   uint32_t* s_tmem = reinterpret_cast<uint32_t*>(bars + 15);
@@ -870,15 +872,14 @@ extend_mass_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_con
   int* s_flag = reinterpret_cast<int*>(s_tmem + 2);
   float* s_warp = reinterpret_cast<float*>(bars + 24);
   float* s_tok = s_warp + 8 * kXmWarpFloats;    // token of a column within its step
-  float* s_sum = s_tok + kXmRows;               // [2][128] the second group's sums
-  int* s_n = reinterpret_cast<int*>(s_sum + 2 * kXmKeys);
+  int* s_n = reinterpret_cast<int*>(s_tok + kXmRows);
   int* s_item0 = s_n + kExtSeqs;
   const ExtendParams& x = p.x;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int tps = kXmRows / x.G;
 
   if (tid == 0) {
-    for (int i = 0; i < 15; ++i) mbar_init(bar(i), i < 2 && KV8 ? 2 : (i >= 8 && i < 12) ? kXmKeys : 1);
+    for (int i = 0; i < 13; ++i) mbar_init(bar(i), i == 0 && KV8 ? 8 : (i >= 7 && i < 11) ? kXmKeys : 1);
     *s_abort = 0;
     if ((smem_u32(sm) & 1023u) != 0u) {
       atomicOr(x.err, kErrStreamBounds);
@@ -913,7 +914,7 @@ extend_mass_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_con
       if (s < x.seqs.n) {
         const ExtSeq e = ext_seq(x, s);
         s_n[s] = e.n;
-        v = e.ok && e.t > 0 ? (e.n + e.t + kXmKeys - 1) / kXmKeys : 0;
+        v = e.ok && e.t > 0 ? (e.n + e.t + kXmItemKeys - 1) / kXmItemKeys : 0;
       }
       int sum = v;
 #pragma unroll
@@ -940,57 +941,49 @@ extend_mass_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_con
     // ================= the warp that loads Q, and K of 16-bit rows =================
     if (lane == 0 && *reinterpret_cast<volatile int*>(p.stop) != 0) *s_abort = 1;
     __syncwarp();
-    XmCursor cur, cK;
+    XmCursor cur;
     cur.ord = 0;
     xm_seek(cur, 0, n_items, p, sh, true);
-    cK = cur;
-    auto load_k = [&]() {  // the item of cK; its stage is read by the item two before
-      if (cK.ord >= 2) mbar_wait(bar(12 + (cK.ord & 1)), (uint32_t)(((cK.ord - 2) >> 1) & 1), s_abort, x.err, kPfSpinLimit);
-      __syncwarp();
-      if (!*s_abort && tc5::elect_one()) {
-        const uint32_t dst = sK + (uint32_t)(cK.ord & 1) * kXmKBytes, bb = bar(cK.ord & 1);
-        const int slab = slab_of(cK);
-        mbar_arrive_expect_tx(bb, kXmKBytes);
-#pragma unroll
-        for (int q = 0; q < 4; ++q)  // (boxes of 64 rows x 64 elements, as the attention's; those behind the slab's end come back as zeros)
-          pf_tma_load(dst + (q >> 1) * (kXmKBytes / 2) + (q & 1) * (kXmKBytes / 4), &tmK, 64 * (q >> 1), cK.k0 + 64 * (q & 1), slab, bb);
-      }
-      __syncwarp();
-      ++cK.ord;
-      xm_seek(cK, cK.it + 1, n_items, p, sh, true);
-    };
-    if constexpr (!KV8) {
-      if (cK.it < n_items && !*s_abort) load_k();
-    }
     int g = 0;
     while (cur.it < n_items && !*s_abort) {
+      if constexpr (!KV8) {
+        if (cur.ord > 0) mbar_wait(bar(11), (uint32_t)((cur.ord - 1) & 1), s_abort, x.err, kPfSpinLimit);  // the item before has read its K
+        __syncwarp();
+        if (!*s_abort && tc5::elect_one()) {
+          const int slab = slab_of(cur);
+          mbar_arrive_expect_tx(bar(0), 2 * kXmKBytes);
+#pragma unroll
+          for (int q = 0; q < 8; ++q)  // (boxes of 64 rows x 64 elements, as the attention's; those behind the slab's end come back as zeros)
+            pf_tma_load(sK + (q >> 2) * kXmKBytes + ((q >> 1) & 1) * (kXmKBytes / 2) + (q & 1) * (kXmKBytes / 4), &tmK, 64 * ((q >> 1) & 1),
+                        cur.k0 + kXmKeys * (q >> 2) + 64 * (q & 1), slab, bar(0));
+        }
+        __syncwarp();
+      }
       for (int j = 0; j < cur.n_step; ++j, ++g) {
-        if (g >= 2) mbar_wait(bar(4 + ((g - 2) & 3)), (uint32_t)(((g - 2) >> 2) & 1), s_abort, x.err, kPfSpinLimit);  // S of step g - 2 has read the stage
+        if (g >= 2) mbar_wait(bar(5 + (g & 1)), (uint32_t)(((g - 2) >> 1) & 1), s_abort, x.err, kPfSpinLimit);  // both groups' S of step g - 2 have read the stage
         __syncwarp();
         if (*s_abort) break;
         if (tc5::elect_one()) {
-          const uint32_t dst = sQ + (uint32_t)(g & 1) * kXmQBytes, bb = bar(2 + (g & 1));
+          const uint32_t dst = sQ + (uint32_t)(g & 1) * kXmQBytes, bb = bar(1 + (g & 1));
           const int tok = cur.layer * x.total + x.seqs.tok0[cur.s] + (cur.lo + j) * tps;
           mbar_arrive_expect_tx(bb, 256u * (uint32_t)(x.G * tps));
           pf_tma_load(dst, &tmQ, 0, cur.h * x.G, tok, bb);
           pf_tma_load(dst + kXmQBytes / 2, &tmQ, 64, cur.h * x.G, tok, bb);
         }
         __syncwarp();
-        if constexpr (!KV8) {
-          if (j == 0 && cK.it < n_items) load_k();  // the next item's rows
-        }
       }
+      ++cur.ord;
       xm_seek(cur, cur.it + 1, n_items, p, sh, true);
     }
     if (*s_abort && lane == 0) {
       atomicOr(p.stop, 1);
-      for (int i = KV8 ? 2 : 0; i < 4; ++i)
+      for (int i = KV8 ? 1 : 0; i < 3; ++i)
         for (uint32_t ph = 0; ph < 2; ++ph)
           for (uint32_t w = 0; w < (1u << 16); ++w)
             if (mbar_try_wait(bar(i), ph)) break;
     }
   } else if (warp == 9) {
-    // ================= the warp that issues S = K Q^T =================
+    // ================= the warp that issues S = K Q^T, a group's after the other's =================
     constexpr uint32_t idesc = KV8 ? tc5::idesc_f16_f32(kXmKeys, kXmRows, 0, 0) : tc5::idesc_bf16_f32(kXmKeys, kXmRows, 0, 0);
     const uint64_t dK = tc5::smem_desc_sw128(sK, 16, 1024);
     const uint64_t dQ = tc5::smem_desc_sw128(sQ, 16, 1024);
@@ -999,81 +992,70 @@ extend_mass_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_con
     xm_seek(cur, 0, n_items, p, sh, true);
     int g = 0;
     while (cur.it < n_items && !*s_abort) {
-      const int ks = cur.ord & 1;
-      mbar_wait(bar(ks), (uint32_t)((cur.ord >> 1) & 1), s_abort, x.err, kPfSpinLimit);
+      mbar_wait(bar(0), (uint32_t)(cur.ord & 1), s_abort, x.err, kPfSpinLimit);
       for (int j = 0; j < cur.n_step; ++j, ++g) {
-        mbar_wait(bar(2 + (g & 1)), (uint32_t)((g >> 1) & 1), s_abort, x.err, kPfSpinLimit);
-        if (g >= 4) mbar_wait(bar(8 + (g & 3)), (uint32_t)(((g - 4) >> 2) & 1), s_abort, x.err, kPfSpinLimit);
-        __syncwarp();
-        tc5::fence_after_sync();
-        if (*s_abort) break;
-        const uint64_t dKg = dK + (uint64_t)((uint32_t)ks * (kXmKBytes >> 4)), dQg = dQ + (uint64_t)((uint32_t)(g & 1) * (kXmQBytes >> 4));
-        if (tc5::elect_one()) {
+        const int st = g & 1;
+        mbar_wait(bar(1 + st), (uint32_t)((g >> 1) & 1), s_abort, x.err, kPfSpinLimit);
 #pragma unroll
-          for (int kk = 0; kk < 8; ++kk)
-            tc5::mma_bf16_ss(tmem + 64u * (uint32_t)(g & 3), dKg + (uint64_t)((kk >> 2) * (kXmKBytes >> 5) + (kk & 3) * 2),
-                             dQg + (uint64_t)((kk >> 2) * (kXmQBytes >> 5) + (kk & 3) * 2), idesc, kk > 0);
-          tc5::mma_commit(bar(4 + (g & 3)));
-          if (j == cur.n_step - 1) tc5::mma_commit(bar(12 + ks));
+        for (int grp = 0; grp < 2; ++grp) {
+          if (g >= 2) mbar_wait(bar(7 + 2 * grp + st), (uint32_t)(((g - 2) >> 1) & 1), s_abort, x.err, kPfSpinLimit);
+          __syncwarp();
+          tc5::fence_after_sync();
+          if (*s_abort) break;
+          const uint64_t dKg = dK + (uint64_t)(grp * (kXmKBytes >> 4)), dQg = dQ + (uint64_t)((uint32_t)st * (kXmQBytes >> 4));
+          if (tc5::elect_one()) {
+#pragma unroll
+            for (int kk = 0; kk < 8; ++kk)
+              tc5::mma_bf16_ss(tmem + 64u * (uint32_t)(2 * grp + st), dKg + (uint64_t)((kk >> 2) * (kXmKBytes >> 5) + (kk & 3) * 2),
+                               dQg + (uint64_t)((kk >> 2) * (kXmQBytes >> 5) + (kk & 3) * 2), idesc, kk > 0);
+            tc5::mma_commit(bar(3 + 2 * grp + st));
+            if (grp == 1 && j == cur.n_step - 1) tc5::mma_commit(bar(11));
+          }
+          __syncwarp();
         }
-        __syncwarp();
+        if (*s_abort) break;
       }
       ++cur.ord;
       xm_seek(cur, cur.it + 1, n_items, p, sh, true);
     }
     if (*s_abort && tc5::elect_one()) {
       atomicOr(p.stop, 1);
-      tc5::mma_commit(bar(14));
+      tc5::mma_commit(bar(12));
       for (uint32_t w = 0; w < kPfSpinLimit; ++w)
-        if (mbar_try_wait(bar(14), 0u)) break;
-    }
-  } else if (warp >= 10) {
-    // ================= 8-bit rows: two warps widen the codes of a K tile, 64 rows each =================
-    if constexpr (KV8) {
-      XmCursor cK;
-      cK.ord = 0;
-      xm_seek(cK, 0, n_items, p, sh, true);
-      const int sub = 64 * (warp - 10);
-      while (cK.it < n_items && !*s_abort) {
-        const uint8_t* src = static_cast<const uint8_t*>(x.K) + (size_t)slab_of(cK) * x.cap * 128;
-        uint8_t* tile = sm + (size_t)(cK.ord & 1) * kXmKBytes;
-        XtCodes codes[4];
-#pragma unroll
-        for (int q = 0; q < 4; ++q) xt_load_codes(codes[q], src, cK.k0 + sub + 8 * q, cK.n + cK.t, lane);
-        if (cK.ord >= 2) mbar_wait(bar(12 + (cK.ord & 1)), (uint32_t)(((cK.ord - 2) >> 1) & 1), s_abort, x.err, kPfSpinLimit);
-        __syncwarp();
-        if (*s_abort) break;
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          xt_store_codes<false>(codes[q], tile, kXmKBytes / 2, sub + 8 * q, lane);
-          xt_load_codes(codes[q], src, cK.k0 + sub + 32 + 8 * q, cK.n + cK.t, lane);
-        }
-#pragma unroll
-        for (int q = 0; q < 4; ++q) xt_store_codes<false>(codes[q], tile, kXmKBytes / 2, sub + 32 + 8 * q, lane);
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bar(cK.ord & 1));
-        __syncwarp();
-        ++cK.ord;
-        xm_seek(cK, cK.it + 1, n_items, p, sh, true);
-      }
+        if (mbar_try_wait(bar(12), 0u)) break;
     }
   } else {
-    // ================= compute warps: thread = key = tensor-memory lane; the groups take the steps in turn =================
+    // ================= compute warps: thread = key = tensor-memory lane =================
     const int wg = warp >> 2, wq = warp & 3;
-    const int row_in = wq * 32 + lane;
-    const uint32_t t_row = tmem + ((uint32_t)(wq * 32) << 16);
-    float* s_add = s_warp + warp * kXmWarpFloats;  // a column's negated log-sum-exp, less its part of the bias
-    float* s_slope = s_add + kXmRows;              // a column's negated slope
+    const int row_in = wg * kXmKeys + wq * 32 + lane;
+    const uint32_t t_row = tmem + 128u * (uint32_t)wg + ((uint32_t)(wq * 32) << 16);
+    const uint32_t s_add = smem_u32(s_warp + warp * kXmWarpFloats);  // a column's negated log-sum-exp, less its part of the bias
+    const uint32_t s_slope = s_add + 4 * kXmRows;                    // a column's negated slope
+    const uint32_t s_token = smem_u32(s_tok), abort_flag = bar0 + 124u;
     XmCursor cur;
     cur.ord = 0;
     xm_seek(cur, 0, n_items, p, sh, false);
-    int g0 = 0, turn = 0;
+    int g = 0;
     while (cur.it < n_items) {
       const int j = cur.k0 + row_in;
       const bool mine = j < cur.n + cur.t;
       const size_t row = (size_t)slab_of(cur) * x.cap + j;
-      const int prefix = x.seqs.prefix[cur.s];
+      const int prefix = x.seqs.prefix[cur.s], n_step = cur.n_step;
+      if constexpr (KV8) {
+        // 8-bit rows: this warp widens its own 32 rows, once the item before has read its K
+        if (n_step > 0) {
+          const uint8_t* src = static_cast<const uint8_t*>(x.K) + (size_t)slab_of(cur) * x.cap * 128;
+          XtCodes codes[4];
+#pragma unroll
+          for (int q = 0; q < 4; ++q) xt_load_codes(codes[q], src, cur.k0 + wg * kXmKeys + wq * 32 + 8 * q, cur.n + cur.t, lane);
+          if (cur.ord > 0) xt_wait(bar(11), (uint32_t)((cur.ord - 1) & 1), abort_flag, x.err);
+#pragma unroll
+          for (int q = 0; q < 4; ++q) xt_store_codes<false>(codes[q], sm + wg * kXmKBytes, kXmKBytes / 2, wq * 32 + 8 * q, lane);
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar(0));
+        }
+      }
       // the tokens that see row j: [i_lo, i_hi)
       int i_lo = j < cur.n + prefix ? 0 : j - cur.n, i_hi = mine ? cur.t : 0;
       float rel = 0.f, sl_a = 0.f, sl_b = 0.f;  // (slopes of columns lane and lane + 32)
@@ -1090,8 +1072,8 @@ extend_mass_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_con
           sl_b = x.slopes[cur.h * x.G + (32 + lane) % x.G] * 1.4426950408889634f;
         }
         __syncwarp();
-        s_slope[lane] = -sl_a;
-        s_slope[32 + lane] = -sl_b;
+        sts_f(s_slope + 4u * lane, -sl_a);
+        sts_f(s_slope + 128u + 4u * lane, -sl_b);
       }
       const float* lse = x.lse + ext_lse_index(x, cur.layer, cur.h, x.seqs.tok0[cur.s]);
       const int all_rows = cur.t * x.G, step_rows = tps * x.G;
@@ -1099,22 +1081,20 @@ extend_mass_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_con
         const int r = (cur.lo + step) * step_rows + lane + off;
         return lane + off < step_rows && r < all_rows ? -__ldg(lse + r) : -CUDART_INF_F;
       };
-      int st = (g0 & 1) == wg ? 0 : 1;  // this group's first step
       float la = 0.f, lb = 0.f;
-      if (st < cur.n_step) {
-        la = ask(st, 0);
-        lb = ask(st, 32);
+      if (n_step > 0) {
+        la = ask(0, 0);
+        lb = ask(0, 32);
       }
       float total = 0.f;
 #pragma unroll 1
-      for (; st < cur.n_step; st += 2) {
-        const int g = g0 + st;
+      for (int st = 0; st < n_step; ++st, ++g) {
         __syncwarp();
-        s_add[lane] = MODS ? fmaf(-sl_a, s_tok[lane], la) : la;
-        s_add[32 + lane] = MODS ? fmaf(-sl_b, s_tok[32 + lane], lb) : lb;
-        if (st + 2 < cur.n_step) {
-          la = ask(st + 2, 0);
-          lb = ask(st + 2, 32);
+        sts_f(s_add + 4u * lane, MODS ? fmaf(-sl_a, lds_f(s_token + 4u * lane), la) : la);
+        sts_f(s_add + 128u + 4u * lane, MODS ? fmaf(-sl_b, lds_f(s_token + 128u + 4u * lane), lb) : lb);
+        if (st + 1 < n_step) {
+          la = ask(st + 1, 0);
+          lb = ask(st + 1, 32);
         }
         __syncwarp();
         const int i0 = (cur.lo + st) * tps;
@@ -1123,17 +1103,17 @@ extend_mass_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_con
         const bool full = __all_sync(0xffffffffu, c_lo == 0 && c_hi == step_rows);
         const float off0 = (float)i0 - rel;
         const bool beside = MODS && prefix > 0 && x.slopes;  // rows of later positions may be seen
-        mbar_wait(bar(4 + (g & 3)), (uint32_t)((g >> 2) & 1), s_abort, x.err, kPfSpinLimit);
+        xt_wait(bar(3 + 2 * wg + (g & 1)), (uint32_t)((g >> 1) & 1), abort_flag, x.err);
         tc5::fence_after_sync();
         uint64_t sum2[2] = {0ull, 0ull};
 #pragma unroll 1
         for (int hb = 0; hb < 64; hb += 32) {
           uint32_t sv[32];
-          tc5::tmem_ld32(t_row + 64u * (uint32_t)(g & 3) + (uint32_t)hb, sv);
+          tc5::tmem_ld32(t_row + 64u * (uint32_t)(g & 1) + (uint32_t)hb, sv);
           tc5::tmem_wait_ld();
           if (hb == 32) {  // both halves have been read: the buffer may be written again
             tc5::fence_before_sync();
-            mbar_arrive(bar(8 + (g & 3)));
+            mbar_arrive(bar(7 + 2 * wg + (g & 1)));
           }
           float scale = p.scale_log2;
           if constexpr (MODS) {
@@ -1145,66 +1125,64 @@ extend_mass_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_con
             }
           }
           const uint64_t scale2 = tc5::f2_pack(scale, scale), off2 = tc5::f2_pack(off0, off0);
+          auto add_up = [&](auto masked) {
 #pragma unroll
-          for (int c = 0; c < 32; c += 4) {
-            float4 add = *reinterpret_cast<const float4*>(s_add + hb + c);
-            if constexpr (MODS) {
-              // (the bias of column c: - slope_c (off0 + token_c); the token's part is in s_add)
-              const float4 ns = *reinterpret_cast<const float4*>(s_slope + hb + c);
-              if (beside) {
-                const float4 tk = *reinterpret_cast<const float4*>(s_tok + hb + c);
-                add.x += ns.x * (fabsf(off0 + tk.x) - tk.x);
-                add.y += ns.y * (fabsf(off0 + tk.y) - tk.y);
-                add.z += ns.z * (fabsf(off0 + tk.z) - tk.z);
-                add.w += ns.w * (fabsf(off0 + tk.w) - tk.w);
-              } else {
-                tc5::f2_unpack(tc5::f2_fma(tc5::f2_pack(ns.x, ns.y), off2, tc5::f2_pack(add.x, add.y)), add.x, add.y);
-                tc5::f2_unpack(tc5::f2_fma(tc5::f2_pack(ns.z, ns.w), off2, tc5::f2_pack(add.z, add.w)), add.z, add.w);
+            for (int c = 0; c < 32; c += 4) {
+              float4 add = lds_f4(s_add + 4u * (uint32_t)(hb + c));
+              if constexpr (MODS) {
+                // (the bias of column c: - slope_c (off0 + token_c); the token's part is in s_add)
+                const float4 ns = lds_f4(s_slope + 4u * (uint32_t)(hb + c));
+                if (beside) {
+                  const float4 tk = lds_f4(s_token + 4u * (uint32_t)(hb + c));
+                  add.x += ns.x * (fabsf(off0 + tk.x) - tk.x);
+                  add.y += ns.y * (fabsf(off0 + tk.y) - tk.y);
+                  add.z += ns.z * (fabsf(off0 + tk.z) - tk.z);
+                  add.w += ns.w * (fabsf(off0 + tk.w) - tk.w);
+                } else {
+                  tc5::f2_unpack(tc5::f2_fma(tc5::f2_pack(ns.x, ns.y), off2, tc5::f2_pack(add.x, add.y)), add.x, add.y);
+                  tc5::f2_unpack(tc5::f2_fma(tc5::f2_pack(ns.z, ns.w), off2, tc5::f2_pack(add.z, add.w)), add.z, add.w);
+                }
               }
-            }
-            float y[4];
-            tc5::f2_unpack(tc5::f2_fma(tc5::f2_pack(__uint_as_float(sv[c]), __uint_as_float(sv[c + 1])), scale2, tc5::f2_pack(add.x, add.y)), y[0], y[1]);
-            tc5::f2_unpack(tc5::f2_fma(tc5::f2_pack(__uint_as_float(sv[c + 2]), __uint_as_float(sv[c + 3])), scale2, tc5::f2_pack(add.z, add.w)), y[2], y[3]);
-            if (!full) {
+              float y[4];
+              tc5::f2_unpack(tc5::f2_fma(tc5::f2_pack(__uint_as_float(sv[c]), __uint_as_float(sv[c + 1])), scale2, tc5::f2_pack(add.x, add.y)), y[0], y[1]);
+              tc5::f2_unpack(tc5::f2_fma(tc5::f2_pack(__uint_as_float(sv[c + 2]), __uint_as_float(sv[c + 3])), scale2, tc5::f2_pack(add.z, add.w)), y[2], y[3]);
+              if constexpr (decltype(masked)::value) {
 #pragma unroll
-              for (int u = 0; u < 4; ++u)
-                if (hb + c + u < c_lo || hb + c + u >= c_hi) y[u] = -CUDART_INF_F;  // weight 0, whatever the logit is
+                for (int u = 0; u < 4; ++u)
+                  if (hb + c + u < c_lo || hb + c + u >= c_hi) y[u] = -CUDART_INF_F;  // weight 0, whatever the logit is
+              }
+              sum2[0] = tc5::f2_add(sum2[0], tc5::f2_pack(fast_exp2(y[0]), fast_exp2(y[1])));
+              sum2[1] = tc5::f2_add(sum2[1], tc5::f2_pack(fast_exp2(y[2]), fast_exp2(y[3])));
             }
-            sum2[0] = tc5::f2_add(sum2[0], tc5::f2_pack(fast_exp2(y[0]), fast_exp2(y[1])));
-            sum2[1] = tc5::f2_add(sum2[1], tc5::f2_pack(fast_exp2(y[2]), fast_exp2(y[3])));
-          }
+          };
+          if (full) add_up(std::false_type{});
+          else add_up(std::true_type{});
         }
         float e, o;
         tc5::f2_unpack(tc5::f2_add(sum2[0], sum2[1]), e, o);
         total += e + o;
       }
-      g0 += cur.n_step;
-      // the two groups' sums (two buffers: a pair of warps meets once per item)
-      if (wg == 1) s_sum[(turn & 1) * kXmKeys + row_in] = total;
-      asm volatile("bar.sync %0, 64;" ::"r"(2 + wq) : "memory");
-      if (wg == 0) {
-        total += s_sum[(turn & 1) * kXmKeys + row_in];
-        if (parts == 1) {
-          if (mine && !*s_abort) ext_emit_mass(x, row, total);
-        } else {
-          // a part: left in the scratch; the last to finish adds them in order
-          float* part = p.mass_part + (size_t)cur.item * parts * kXmKeys + row_in;
-          __stcg(part + cur.part * kXmKeys, total);
+      if (parts == 1) {
+        if (mine && !*s_abort) ext_emit_mass(x, row, total);
+      } else {
+        // a part: left in the scratch; the last to finish adds them in order
+        float* part = p.mass_part + (size_t)cur.item * parts * kXmItemKeys + row_in;
+        __stcg(part + cur.part * kXmItemKeys, total);
+        __threadfence();
+        asm volatile("bar.sync 1, 256;" ::: "memory");
+        if (tid == 0) *s_flag = atomicAdd(p.mass_counters + cur.item, 1u) == (unsigned)(parts - 1);
+        asm volatile("bar.sync 1, 256;" ::: "memory");
+        const bool last = *s_flag != 0;
+        asm volatile("bar.sync 1, 256;" ::: "memory");
+        if (last) {
           __threadfence();
-          asm volatile("bar.sync 1, 128;" ::: "memory");
-          if (tid == 0) *s_flag = atomicAdd(p.mass_counters + cur.item, 1u) == (unsigned)(parts - 1);
-          asm volatile("bar.sync 1, 128;" ::: "memory");
-          const bool last = *s_flag != 0;
-          asm volatile("bar.sync 1, 128;" ::: "memory");
-          if (last) {
-            __threadfence();
-            float sum = 0.f;
-            for (int k = 0; k < parts; ++k) sum += __ldcg(part + k * kXmKeys);
-            if (mine && !*s_abort) ext_emit_mass(x, row, sum);
-          }
+          float sum = 0.f;
+#pragma unroll 4
+          for (int k = 0; k < parts; ++k) sum += __ldcg(part + k * kXmItemKeys);
+          if (mine && !*s_abort) ext_emit_mass(x, row, sum);
         }
       }
-      ++turn;
+      if (n_step > 0) ++cur.ord;
       xm_seek(cur, cur.it + 1, n_items, p, sh, false);
     }
   }
