@@ -1513,10 +1513,10 @@ dynts_status_t launch_extend_tc_as(dynts_cache* c, dynts::ExtendTcParams& p, uns
     CUDA_TRY(cudaFuncSetAttribute(dynts::extend_mass_tc_kernel<KV8, MODS>, cudaFuncAttributeMaxDynamicSharedMemorySize, dynts::kXmSmemBytes));
     *attr = true;
   }
-  CUDA_TRY(launch_dependent(dynts::extend_tc_kernel<KV8, MODS>, dim3(grid, 1, 1), dynts::kXtThreads, dynts::kXtSmemBytes, c->stream, p, mq, c->map_XK, c->map_XV));
+  CUDA_TRY(launch_dependent(dynts::extend_tc_kernel<KV8, MODS>, dim3(grid, 1, 1), (unsigned)dynts::XtShape<KV8, MODS>::kThreads, dynts::kXtSmemBytes, c->stream, p, mq, c->map_XK, c->map_XV));
   c->launches += 1;
   if (grid > 1) {  // items that lie across CTAs
-    CUDA_TRY(launch_dependent(dynts::extend_join_kernel, dim3(grid - 1, (unsigned)((p.part_rows + 7) / 8), 1), 256, 0, c->stream, p));
+    CUDA_TRY(launch_dependent(dynts::extend_join_kernel, dim3(grid - 1, (unsigned)((p.part_rows + 31) / 32), 1), 256, 0, c->stream, p));
     c->launches += 1;
   }
   if (want_mass) {

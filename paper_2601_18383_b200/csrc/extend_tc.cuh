@@ -24,8 +24,8 @@
 // computed again by its warp alone, with a running maximum.  No maximum and no rescale in any other tile.
 // (From the newest tile on, because a distance bias only lowers the logits of older rows, and a window hides the oldest.)
 //
-// Warps: 0-3 and 4-7 the two groups, two that load, one that issues S, one that issues O; they meet
-// through mbarriers as in the prompt attention (prefill_attn.cuh), the S buffer, stages and phases follow the flat tile index g.  Every warp
+// Warps: 0-3 and 4-7 the two groups, one that issues S, one that issues O, two that load (see XtShape); they meet through
+// mbarriers as in the prompt attention (prefill_attn.cuh), the S buffer, stages and phases follow the flat tile index g.  Every warp
 // walks the CTA's pieces by the plan the storing kernel wrote (extend.cuh), a word per lane, the next piece's
 // prefetched.  Two CTAs of 384 threads leave 80 registers per thread and hardly any L1: code that spills or does
 // not stay in the instruction caches cost several times its instructions, so the loops are rolled and the end of a piece
@@ -50,7 +50,14 @@
 
 namespace dynts {
 
-constexpr int kXtThreads = 384;
+// 8-bit rows, and the plain row arithmetic: two warps of their own load (12 warps, 80 registers per thread).  With caps, biases
+// and windows the row arithmetic needs the registers more: the warps that issue the products load too (10 warps, 96).
+// (4096 behind 4096, plain: 386 us against 488 us; ragged prompts with a bias: 134 against 122 us.)
+template <bool KV8, bool MODS>
+struct XtShape {
+  static constexpr bool kLoaders = KV8 || !MODS;
+  static constexpr int kThreads = kLoaders ? 384 : 320;
+};
 constexpr int kXtRows = 128;
 constexpr int kXtMaxCtas = 380;      // CTAs of a launch (two per SM)
 constexpr int kXtPartFloats = 129;   // per query row of a part: 128 outputs, log-sum-exp
@@ -233,10 +240,10 @@ __device__ __noinline__ float4 xt_row_again(const ExtendTcParams& p, int d, int 
   return make_float4(acc[0], acc[1], acc[2], acc[3]);
 }
 
-// Joins the parts of the item that begins in CTA blockIdx.x's shares and ends behind them, if there is one: 8 rows per
-// block (y), a thread four columns of one row.  A part's 128-byte pieces are read whole, the output's sectors written whole.
-// Running maximum and sum over the parts, in the order of the list: bound by the latency of two loads (the list, then
-// all parts at once).
+// Joins the parts of the item that begins in CTA blockIdx.x's shares and ends behind them, if there is one: 32 rows per
+// block (y), a warp 8 rows x 64 columns, a thread four pieces of four columns of one row.  A part's 128-byte pieces
+// are read whole, the output's sectors written whole.  Running maximum and sum over the parts, in the order of the
+// list: bound by the latency of three loads (the plan, the list, then the parts, two at once).
 __global__ void __launch_bounds__(256) extend_join_kernel(const __grid_constant__ ExtendTcParams p) {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const ExtendParams& x = p.x;
@@ -246,36 +253,44 @@ __global__ void __launch_bounds__(256) extend_join_kernel(const __grid_constant_
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const int d = __ldcg(p.plan.words + (size_t)slot * kPlanWords + lane);
   auto word = [&](int w) { return __shfl_sync(0xffffffffu, d, w); };
-  const int n_parts = word(kPwParts), rows = word(kPwRows), row = blockIdx.y * 8 + (lane >> 2), c4 = warp * 4 + (lane & 3);
+  const int n_parts = word(kPwParts), rows = word(kPwRows), row = blockIdx.y * 32 + (warp & 3) * 8 + (lane >> 2), c4 = (warp >> 2) * 16 + (lane & 3);
   if (n_parts < 2 || word(kPwBase) != slot) return;  // (an item that began before is another block's)
+  if ((int)blockIdx.y * 32 + (warp & 3) * 8 >= rows) return;
   const int tok = word(kPwTok), h = word(kPwHead), layer = word(kPwLayer);
   const int* list = p.plan.words + (size_t)slot * kPlanWords + kPwList;
   int places = lane < n_parts ? __ldcg(list + (size_t)lane * kPlanWords) : 0;  // of the first 32 parts
-  if ((int)blockIdx.y * 8 >= rows) return;
   const int rr = min(row, rows - 1);
   const size_t piece = (size_t)p.part_rows;
-  float M = -CUDART_INF_F, sum = 0.f;
-  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
+  float M = -CUDART_INF_F, sum = 0.f, acc[16];
+#pragma unroll
+  for (int e = 0; e < 16; ++e) acc[e] = 0.f;
+#pragma unroll 2
   for (int k = 0; k < n_parts; ++k) {
     if (k > 0 && (k & 31) == 0) places = k + lane < n_parts ? __ldcg(list + (size_t)(k + lane) * kPlanWords) : 0;
     const float* src = p.part + (size_t)__shfl_sync(0xffffffffu, places, k & 31) * (piece * kXtPartFloats);
     const float lk = __ldcg(src + 128 * piece + rr);
-    const float4 y = __ldcg(reinterpret_cast<const float4*>(src) + (size_t)c4 * piece + rr);
+    float4 y[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] = __ldcg(reinterpret_cast<const float4*>(src) + (size_t)(c4 + 4 * e) * piece + rr);
     const float Mn = fmaxf(M, lk);
     const float keep = M == -CUDART_INF_F ? 0.f : fast_exp2(M - Mn), w = lk == -CUDART_INF_F ? 0.f : fast_exp2(lk - Mn);
     M = Mn;
     sum = fmaf(sum, keep, w);
-    acc.x = fmaf(acc.x, keep, w * y.x);
-    acc.y = fmaf(acc.y, keep, w * y.y);
-    acc.z = fmaf(acc.z, keep, w * y.z);
-    acc.w = fmaf(acc.w, keep, w * y.w);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      acc[4 * e] = fmaf(acc[4 * e], keep, w * y[e].x);
+      acc[4 * e + 1] = fmaf(acc[4 * e + 1], keep, w * y[e].y);
+      acc[4 * e + 2] = fmaf(acc[4 * e + 2], keep, w * y[e].z);
+      acc[4 * e + 3] = fmaf(acc[4 * e + 3], keep, w * y[e].w);
+    }
   }
   if (row >= rows) return;
   const float f = p.out_scale / sum;
   const int ti = row / x.G;
   __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(x.out) + (((size_t)layer * x.total + tok + ti) * x.Hq + h * x.G + (row - ti * x.G)) * 128 + c4 * 4;
-  *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16x2(acc.x * f, acc.y * f), pack_bf16x2(acc.z * f, acc.w * f));
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    *reinterpret_cast<uint2*>(dst + 16 * e) = make_uint2(pack_bf16x2(acc[4 * e] * f, acc[4 * e + 1] * f), pack_bf16x2(acc[4 * e + 2] * f, acc[4 * e + 3] * f));
   if (c4 == 0 && x.lse) x.lse[ext_lse_index(x, layer, h, tok) + row] = M + __log2f(sum);
 }
 
@@ -387,7 +402,7 @@ __device__ __noinline__ void xt_epilogue(const ExtendTcParams& p, int d, int ord
 }
 
 template <bool KV8, bool MODS>
-__global__ void __launch_bounds__(kXtThreads, 2)
+__global__ void __launch_bounds__((XtShape<KV8, MODS>::kThreads), 2)
 extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
                  const __grid_constant__ CUtensorMap tmV) {
   extern __shared__ __align__(1024) uint8_t pf_smem[];
@@ -406,7 +421,8 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
   const ExtendParams& x = p.x;
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  constexpr int kSWarp = 10, kOWarp = 11;  // the warps that issue S and O
+  constexpr bool kLoaders = XtShape<KV8, MODS>::kLoaders;
+  constexpr int kSWarp = kLoaders ? 10 : 8, kOWarp = kSWarp + 1;  // the warps that issue S and O
   if (tid == 0) {
     for (int i = 0; i < 15; ++i) mbar_init(bar(i), i == 7 ? 2 * kXtRows : (i == 8 || i == 9) ? kXtRows : KV8 && (i == 1 || i == 2) ? 2 : 1);
     *s_abort = 0;
@@ -421,7 +437,7 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
     tc5::tmem_alloc(smem_u32(s_tmem), kPfTmemCols);
     tc5::tmem_relinquish();
   }
-  if (tid == 8 * 32) {
+  if (tid == kOWarp * 32) {
     asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&tmQ)) : "memory");
     if constexpr (!KV8) {
       asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&tmK)) : "memory");
@@ -452,8 +468,28 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
     ++slot;
     d = d_next;
   };
+  auto load_q = [&]() {  // the piece's queries
+    const int tok = word(kPwLayer) * x.total + word(kPwTok), head = word(kPwHead) * x.G;
+    if (tc5::elect_one()) {
+      mbar_arrive_expect_tx(bar(0), 256u * (uint32_t)(x.G * p.plan.tokens_per_tile));
+      pf_tma_load(sQ, &tmQ, 0, head, tok, bar(0));
+      pf_tma_load(sQ + kPfQBytes / 2, &tmQ, 64, head, tok, bar(0));
+    }
+    __syncwarp();
+  };
 
-  if (warp >= 8 && warp < kSWarp) {
+  auto load_tile = [&](bool k, int g, int row, int slab) {  // a K or V tile by TMA into the stage of tile g
+    if (tc5::elect_one()) {
+      const uint32_t dst = (k ? sK : sV) + (uint32_t)(g & 1) * kPfKvBytes, bb = bar((k ? 1 : 3) + (g & 1));
+      const CUtensorMap* tm = k ? &tmK : &tmV;
+      mbar_arrive_expect_tx(bb, kPfKvBytes);
+      pf_tma_load(dst, tm, 0, row, slab, bb);
+      pf_tma_load(dst + kPfKvBytes / 2, tm, 64, row, slab, bb);
+    }
+    __syncwarp();
+  };
+
+  if (kLoaders && (warp == 8 || warp == 9)) {
     // ================= the warps that load: 8 Q and K, 9 V; 8-bit rows: 8 Q and half of K, 9 the other half =================
     if (lane == 0 && *reinterpret_cast<volatile int*>(p.stop) != 0) *s_abort = 1;
     __syncwarp();
@@ -471,16 +507,6 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
         if (lane == 0 && j + 4 < nkt)
           asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(src + (size_t)(k0 - 4 * kPfKeys) * 128), "r"(32 * 128) : "memory");
       };
-      auto load_tile = [&](const CUtensorMap* tm, uint32_t base, int filled, int j) {
-        if (tc5::elect_one()) {
-          const uint32_t dst = base + (uint32_t)(g & 1) * kPfKvBytes, bb = bar(filled + (g & 1));
-          const int row = (kt_new - j) * kPfKeys;
-          mbar_arrive_expect_tx(bb, kPfKvBytes);
-          pf_tma_load(dst, tm, 0, row, slab, bb);
-          pf_tma_load(dst + kPfKvBytes / 2, tm, 64, row, slab, bb);
-        }
-        __syncwarp();
-      };
       if constexpr (KV8) {
         if (nkt > 0) fetch(0);
       }
@@ -492,15 +518,7 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
         if (done >= 0) mbar_wait(bar(freed + (done & 1)), (uint32_t)((done >> 1) & 1), s_abort, x.err, kPfSpinLimit);
         __syncwarp();
         if (*s_abort) break;
-        if (new_q) {
-          const int tok = word(kPwLayer) * x.total + word(kPwTok), head = word(kPwHead) * x.G;
-          if (tc5::elect_one()) {
-            mbar_arrive_expect_tx(bar(0), 256u * (uint32_t)(x.G * p.plan.tokens_per_tile));
-            pf_tma_load(sQ, &tmQ, 0, head, tok, bar(0));
-            pf_tma_load(sQ + kPfQBytes / 2, &tmQ, 64, head, tok, bar(0));
-          }
-          __syncwarp();
-        }
+        if (new_q) load_q();
         if constexpr (KV8) {
           uint8_t* tile = sm + kPfQBytes + (uint32_t)(g & 1) * kPfKvBytes;
 #pragma unroll
@@ -511,8 +529,7 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
           if (j + 1 < nkt) fetch(j + 1);
           __syncwarp();
         } else {
-          if (warp == 8) load_tile(&tmK, sK, 1, j);
-          else load_tile(&tmV, sV, 3, j);
+          load_tile(warp == 8, g, (kt_new - j) * kPfKeys, slab);
         }
       }
     }
@@ -524,77 +541,120 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
           for (uint32_t w = 0; w < (1u << 16); ++w)
             if (mbar_try_wait(bar(i), ph)) break;
     }
-  } else if (warp == kOWarp) {
-    // ================= the warp that issues O += P V =================
-    constexpr uint32_t idesc_o = tc5::idesc_bf16_f32(kXtRows, 128, 0, 1);
-    const uint64_t dV = tc5::smem_desc_sw128(sV, kPfKvBytes / 2, 1024);
-    int g = 0, ord = 0;
-    for (; slot < slot_end && !*s_abort; go_next()) {
-      ask_next();
-      const int nkt = word(kPwTiles);
-      for (int j = 0; j < nkt; ++j, ++g) {
+  } else if (warp == kSWarp || warp == kOWarp) {
+    // ================= the warps that issue S = Q K^T and O += P V (and load, where no others do) =================
+    if (lane == 0 && *reinterpret_cast<volatile int*>(p.stop) != 0) *s_abort = 1;
+    __syncwarp();
+    auto issue = [&](auto which) {
+      constexpr bool is_s = decltype(which)::value;
+      constexpr uint32_t idesc = is_s ? (KV8 ? tc5::idesc_f16_f32(kXtRows, kPfKeys, 0, 0) : tc5::idesc_bf16_f32(kXtRows, kPfKeys, 0, 0))
+                                      : tc5::idesc_bf16_f32(kXtRows, 128, 0, 1);
+      const uint64_t dQ = tc5::smem_desc_sw128(sQ, 16, 1024);
+      const uint64_t dKV = is_s ? tc5::smem_desc_sw128(sK, 16, 1024) : tc5::smem_desc_sw128(sV, kPfKvBytes / 2, 1024);
+      int g = 0, ord = 0, j = 0, nkt = 0;
+      auto find = [&]() {  // the next piece that holds any key tile
+        while (slot < slot_end) {
+          ask_next();
+          nkt = word(kPwTiles);
+          if (nkt > 0) break;
+          go_next();
+        }
+        j = 0;
+      };
+      // Loads run two tiles ahead of the products, over the pieces' words a second time.
+      int l_slot = slot, l_d = d, l_j = 0, l_nkt = kLoaders ? 0 : word(kPwTiles);
+      auto load = [&](int gl) {  // K (or V) of tile gl, if there is one
+        while (l_slot < slot_end && l_j == l_nkt) {
+          if (++l_slot < slot_end) {
+            l_d = __ldcg(p.plan.words + (size_t)l_slot * kPlanWords + lane);
+            l_nkt = __shfl_sync(0xffffffffu, l_d, kPwTiles);
+            l_j = 0;
+          }
+        }
+        if (l_slot >= slot_end) return;
+        const int row = (__shfl_sync(0xffffffffu, l_d, kPwFirst) + l_nkt - 1 - l_j) * kPfKeys;
+        ++l_j;
+        load_tile(is_s, gl, row, __shfl_sync(0xffffffffu, l_d, kPwSlab));
+      };
+      find();
+      if constexpr (!kLoaders) {
+        if (!*s_abort) {
+          if (is_s && slot < slot_end) load_q();
+          load(0);
+          load(1);
+        }
+      }
+      while (slot < slot_end && !*s_abort) {
         const int st = g & 1;
-        if constexpr (!KV8) mbar_wait(bar(3 + st), (uint32_t)((g >> 1) & 1), s_abort, x.err, kPfSpinLimit);  // (8-bit rows: written before P)
-        mbar_wait(bar(8 + st), (uint32_t)((g >> 1) & 1), s_abort, x.err, kPfSpinLimit);
-        if (j == 0 && ord > 0) mbar_wait(bar(7), (uint32_t)((ord - 1) & 1), s_abort, x.err, kPfSpinLimit);  // O of the piece before has been read
+        if constexpr (is_s) {
+          mbar_wait(bar(1 + st), (uint32_t)((g >> 1) & 1), s_abort, x.err, kPfSpinLimit);
+          // S of tile g overwrites the columns P of tile g - 2 is read from
+          if (g >= 2) mbar_wait(bar(10 + st), (uint32_t)(((g - 2) >> 1) & 1), s_abort, x.err, kPfSpinLimit);
+          if (j == 0) mbar_wait(bar(0), (uint32_t)(ord & 1), s_abort, x.err, kPfSpinLimit);
+        } else {
+          if constexpr (!KV8) mbar_wait(bar(3 + st), (uint32_t)((g >> 1) & 1), s_abort, x.err, kPfSpinLimit);  // (8-bit rows: written before P)
+          mbar_wait(bar(8 + st), (uint32_t)((g >> 1) & 1), s_abort, x.err, kPfSpinLimit);
+          if (j == 0 && ord > 0) mbar_wait(bar(7), (uint32_t)((ord - 1) & 1), s_abort, x.err, kPfSpinLimit);  // O of the piece before has been read
+        }
         __syncwarp();
         tc5::fence_after_sync();
         if (*s_abort) break;
-        const uint64_t dVg = dV + (uint64_t)((uint32_t)st * (kPfKvBytes >> 4));
+        const uint64_t dg = dKV + (uint64_t)((uint32_t)st * (kPfKvBytes >> 4));
         if (tc5::elect_one()) {
+          if constexpr (is_s) {
 #pragma unroll
-          for (int kk = 0; kk < 4; ++kk)  // 16 keys per step: 8 columns of P (over S buffer g & 1), two 8-row groups of V
-            tc5::mma_bf16_ts(tO, tS0 + 64u * (uint32_t)st + 8u * (uint32_t)kk, dVg + (uint64_t)(kk * 128), idesc_o, (j > 0 || kk > 0) ? 1u : 0u);
-          tc5::mma_commit(bar(10 + st));
-          if (j == nkt - 1) tc5::mma_commit(bar(12));
+            for (int kk = 0; kk < 8; ++kk)
+              tc5::mma_bf16_ss(tS0 + 64u * (uint32_t)st, dQ + (uint64_t)((kk >> 2) * (kPfQBytes >> 5) + (kk & 3) * 2),
+                               dg + (uint64_t)((kk >> 2) * (kPfKvBytes >> 5) + (kk & 3) * 2), idesc, kk > 0);
+            tc5::mma_commit(bar(5 + st));
+          } else {
+#pragma unroll
+            for (int kk = 0; kk < 4; ++kk)  // 16 keys per step: 8 columns of P (over S buffer g & 1), two 8-row groups of V
+              tc5::mma_bf16_ts(tO, tS0 + 64u * (uint32_t)st + 8u * (uint32_t)kk, dg + (uint64_t)(kk * 128), idesc, (j > 0 || kk > 0) ? 1u : 0u);
+            tc5::mma_commit(bar(10 + st));
+            if (j == nkt - 1) tc5::mma_commit(bar(12));
+          }
         }
         __syncwarp();
+        const bool last = ++j == nkt;
+        if constexpr (!kLoaders) {
+          if (l_slot < slot_end || last) {  // the stage of this tile (and, with a piece's last S, Q) is free when its product is done
+            mbar_wait(bar((is_s ? 5 : 10) + st), (uint32_t)((g >> 1) & 1), s_abort, x.err, kPfSpinLimit);
+            __syncwarp();
+            if (*s_abort) break;
+            load(g + 2);
+          }
+        }
+        ++g;
+        if (last) {
+          ++ord;
+          go_next();
+          find();
+          if constexpr (!kLoaders) {
+            if (is_s && slot < slot_end) load_q();
+          }
+        }
       }
-      if (nkt > 0) ++ord;
-    }
-    if (*s_abort && tc5::elect_one()) {
-      // give the MMAs already issued a bounded time to finish before the tensor memory is released
-      atomicOr(p.stop, 1);
-      tc5::mma_commit(bar(13));
-      for (uint32_t w = 0; w < kPfSpinLimit; ++w)
-        if (mbar_try_wait(bar(13), 0u)) break;
-    }
-  } else if (warp == kSWarp) {
-    // ================= the warp that issues S = Q K^T =================
-    constexpr uint32_t idesc_s = KV8 ? tc5::idesc_f16_f32(kXtRows, kPfKeys, 0, 0) : tc5::idesc_bf16_f32(kXtRows, kPfKeys, 0, 0);
-    const uint64_t dQ = tc5::smem_desc_sw128(sQ, 16, 1024);
-    const uint64_t dK = tc5::smem_desc_sw128(sK, 16, 1024);
-    int g = 0, ord = 0;
-    for (; slot < slot_end && !*s_abort; go_next()) {
-      ask_next();
-      const int nkt = word(kPwTiles);
-      for (int j = 0; j < nkt; ++j, ++g) {
-        const int st = g & 1;
-        mbar_wait(bar(1 + st), (uint32_t)((g >> 1) & 1), s_abort, x.err, kPfSpinLimit);
-        // S of tile g overwrites the columns P of tile g - 2 is read from
-        if (g >= 2) mbar_wait(bar(10 + st), (uint32_t)(((g - 2) >> 1) & 1), s_abort, x.err, kPfSpinLimit);
-        if (j == 0) mbar_wait(bar(0), (uint32_t)(ord & 1), s_abort, x.err, kPfSpinLimit);
-        __syncwarp();
-        tc5::fence_after_sync();
-        if (*s_abort) break;
-        const uint64_t dKg = dK + (uint64_t)((uint32_t)st * (kPfKvBytes >> 4));
-        if (tc5::elect_one()) {
-#pragma unroll
-          for (int kk = 0; kk < 8; ++kk)
-            tc5::mma_bf16_ss(tS0 + 64u * (uint32_t)st, dQ + (uint64_t)((kk >> 2) * (kPfQBytes >> 5) + (kk & 3) * 2),
-                             dKg + (uint64_t)((kk >> 2) * (kPfKvBytes >> 5) + (kk & 3) * 2), idesc_s, kk > 0);
-          tc5::mma_commit(bar(5 + st));
+      if (*s_abort) {
+        // Something gave up: a bounded time for the loads this warp started and the MMAs already issued (see prefill_attn.cuh)
+        if (lane == 0) {
+          atomicOr(p.stop, 1);
+          if constexpr (!kLoaders)
+            for (int i = is_s ? 0 : 3; i < (is_s ? 3 : 5); ++i)
+              for (uint32_t ph = 0; ph < 2; ++ph)
+                for (uint32_t w = 0; w < (1u << 16); ++w)
+                  if (mbar_try_wait(bar(i), ph)) break;
         }
         __syncwarp();
+        if (tc5::elect_one()) {
+          tc5::mma_commit(bar(is_s ? 14 : 13));
+          for (uint32_t w = 0; w < kPfSpinLimit; ++w)
+            if (mbar_try_wait(bar(is_s ? 14 : 13), 0u)) break;
+        }
       }
-      if (nkt > 0) ++ord;
-    }
-    if (*s_abort && tc5::elect_one()) {
-      atomicOr(p.stop, 1);
-      tc5::mma_commit(bar(14));
-      for (uint32_t w = 0; w < kPfSpinLimit; ++w)
-        if (mbar_try_wait(bar(14), 0u)) break;
-    }
+    };
+    if (warp == kSWarp) issue(std::true_type{});
+    else issue(std::false_type{});
   } else {
     // ================= softmax warps: thread = query row = tensor-memory lane =================
     const int wg = warp >> 2, wq = warp & 3;              // group; warp within it (its lanes of tensor memory)
