@@ -336,13 +336,35 @@ def dynts_predictor_mlp(h, W1, b1, W2, b2, W3, b3, d, batch, activation, scratch
 def _host_ints(x):
     """(address, keep-alive) of host int32 values: a CPU int32 tensor or array as it is, else a copy of a sequence."""
     if hasattr(x, "data_ptr"):
-        if str(x.dtype) != "torch.int32" or x.is_cuda or not x.is_contiguous():
-            raise DyntsError(DYNTS_ERR_INVALID_ARG, "host counts must be a contiguous int32 tensor on the CPU, or a sequence of ints")
+        if x.dtype is not _torch().torch.int32 or x.is_cuda or x.dim() != 1 or not x.is_contiguous():
+            _invalid("host counts must be a contiguous int32 tensor on the CPU, or a sequence of ints")
         return x.data_ptr(), x
-    if hasattr(x, "ctypes") and str(x.dtype) == "int32" and x.flags["C_CONTIGUOUS"]:
+    if hasattr(x, "ctypes") and str(x.dtype) == "int32" and x.ndim == 1 and x.flags["C_CONTIGUOUS"]:
         return x.ctypes.data, x
     arr = (C.c_int * len(x))(*[int(v) for v in x])
     return C.addressof(arr), arr
+
+
+class _Torch:
+    """torch, and its current device and stream as plain integers (without a Python object for each call, where torch has that:
+    the operators below take a few microseconds on the GPU)."""
+
+    def __init__(self):
+        import torch
+        self.torch = torch
+        self.dtypes = {torch.bfloat16: DYNTS_BF16, torch.float32: DYNTS_FP32}
+        self.device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+        self.stream = getattr(torch._C, "_cuda_getCurrentRawStream", lambda i: torch.cuda.current_stream(i).cuda_stream)
+
+
+_torch_state = None
+
+
+def _torch():
+    global _torch_state
+    if _torch_state is None:
+        _torch_state = _Torch()
+    return _torch_state
 
 
 def dynts_extend_scratch_bytes(c, n_new, n_layers) -> int:
@@ -383,38 +405,50 @@ def rope(q, k, positions, q_out=None, k_out=None, theta=10000.0, sections=None, 
     """dynts_rope on torch tensors: q [n, Hq, d], k [n, Hkv, d] or None, positions int32 [n] or [axes, n].  The outputs are new
     tensors unless given (q_out=q, k_out=k: in place).  Rows of a token are contiguous, tokens may be strided.  Runs on torch's
     current stream of q's device.  Returns (q_out, k_out)."""
-    import torch
+    t = _torch()
     if q_out is None:
-        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        q_out = t.torch.empty(q.shape, dtype=q.dtype, device=q.device)
     if k is not None and k_out is None:
-        k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device)
+        k_out = t.torch.empty(k.shape, dtype=k.dtype, device=k.device)
+    dt, dev = q.dtype, q.get_device()
+    dtype = t.dtypes.get(dt)
+    if dtype is None:
+        _invalid("q must be bf16 or fp32")
     n, hq, d = q.shape
-    dtype = DYNTS_BF16 if q.dtype == torch.bfloat16 else DYNTS_FP32 if q.dtype == torch.float32 else _invalid("q must be bf16 or fp32")
+    hkv = 0
+    strided = False
     for x, y in ((q, q_out), (k, k_out)):
         if x is None:
             continue
+        shape = x.shape
         for z in (x, y):
-            if not z.is_cuda or z.device != q.device or z.dtype != q.dtype or z.dim() != 3 or z.shape != x.shape or x.shape[0] != n or x.shape[2] != d:
+            if z.get_device() != dev or dev < 0 or z.dtype is not dt or len(shape) != 3 or z.shape != shape or shape[0] != n or shape[2] != d:
                 _invalid("q, k and the outputs must be CUDA tensors [n, heads, d] of one type on one device")
-            if z.numel() and (z.stride(2) != 1 or (z.shape[1] > 1 and z.stride(1) != d) or (n > 1 and z.stride(0) < z.shape[1] * d)):
-                _invalid("the heads of a token must be contiguous and the tokens in order")
-    if positions.device != q.device or positions.dtype != torch.int32 or not positions.is_contiguous():
+            if not z.is_contiguous():
+                strided = True
+                if z.stride(2) != 1 or (shape[1] > 1 and z.stride(1) != d) or (n > 1 and z.stride(0) < shape[1] * d):
+                    _invalid("the heads of a token must be contiguous and the tokens in order")
+        if x is k:
+            hkv = shape[1]
+    shape = positions.shape
+    axes = 1 if len(shape) == 1 else shape[0]
+    if positions.get_device() != dev or positions.dtype is not t.torch.int32 or not positions.is_contiguous():
         _invalid("positions must be a contiguous int32 tensor on q's device")
-    axes = 1 if positions.dim() == 1 else positions.shape[0]
-    if positions.dim() > 2 or positions.shape[-1] != n or (sections is not None and len(sections) != axes):
+    if len(shape) not in (1, 2) or shape[-1] != n or (sections is not None and len(sections) != axes):
         _invalid("positions are [n] or [axes, n], with a section for each axis")
-    hkv = 0 if k is None else k.shape[1]
-    st = None
-    if n > 1:
-        st = (q.stride(0), 0 if k is None else k.stride(0), q_out.stride(0), 0 if k is None else k_out.stride(0))
+    st = sec = None
+    if strided and n > 1:
+        st = (C.c_longlong * 4)(q.stride(0), 0 if k is None else k.stride(0), q_out.stride(0), 0 if k is None else k_out.stride(0))
+    if sections is not None:
+        sec = (C.c_int * axes)(*sections)
     flags = (DYNTS_ROPE_ADJACENT if adjacent else 0) | (DYNTS_ROPE_ROUND_ROBIN if round_robin else 0)
-    args = (q, k, positions, q_out, k_out, n, hq, hkv, d, d if rot_dim is None else rot_dim, axes, sections, flags, float(theta), dtype, st)
-    stream = torch.cuda.current_stream(q.device).cuda_stream
-    if torch.cuda.current_device() != q.device.index:
-        with torch.cuda.device(q.device):
-            dynts_rope(*args, stream)
+    args = (q.data_ptr(), None if k is None else k.data_ptr(), positions.data_ptr(), q_out.data_ptr(), None if k is None else k_out.data_ptr(),
+            n, hq, hkv, d, d if rot_dim is None else rot_dim, axes, sec, flags, theta, dtype, st, t.stream(dev))
+    if t.device() == dev:
+        _check(lib.dynts_rope(*args))
     else:
-        dynts_rope(*args, stream)
+        with t.torch.cuda.device(dev):
+            _check(lib.dynts_rope(*args))
     return q_out, k_out
 
 
@@ -457,7 +491,10 @@ class Cache:
             self.handle = dynts_cache_create_ex(cfg)
         self.nbytes = nbytes
         self.capacity = dynts_cache_capacity(self.handle)
+        self.device_index = self.storage.get_device()
+        self.mass_shape = (layers, batch, kv_heads, self.capacity)
         self._scratch = []        # scratch of the chunk calls; outgrown pieces are kept for the work and graphs that still use them
+        self._scratch_ptr, self._scratch_bytes = None, 0
 
     def close(self):
         if getattr(self, "handle", None):
@@ -465,6 +502,7 @@ class Cache:
             self.handle = None
             self.storage = None
             self._scratch = []
+            self._scratch_ptr, self._scratch_bytes = None, 0
 
     def __del__(self):
         try:
@@ -504,54 +542,53 @@ class Cache:
         return dynts_decode_attn_host(self.handle, q, k_new, v_new, out)
 
     def _extend(self, layer, q, k, v, out, n_new, s_new, mass, softcap, slopes, window, prefix, stage):
-        torch = self.torch
+        t = _torch()
         counts, keep_n = _host_ints(n_new)
-        if len(n_new) != self.batch:
+        listed = n_new.tolist() if hasattr(n_new, "tolist") else n_new
+        if len(listed) != self.batch:
             _invalid("n_new needs a count for each sequence")
-        lead = () if layer is not None else (self.layers,)
-        total = q.shape[-3]
-        dt, dev, d = self.torch_dtype, self.storage.device, self.head_dim
-        strides = []
-        for x, heads in ((q, self.q_heads), (k, self.kv_heads), (v, self.kv_heads), (out, self.q_heads)):
-            if x.dtype != dt or x.device != dev or tuple(x.shape) != lead + (total, heads, d):
-                _invalid(f"q, k, v and out must be {dt} tensors {lead + ('n_total', 'heads', d)} on {dev}")
-            step = x.stride(-3) if total > 1 else heads * d
-            if x.numel() and (x.stride(-1) != 1 or (heads > 1 and x.stride(-2) != d) or step < heads * d or
-                              (lead and self.layers > 1 and x.stride(0) != total * step)):
-                _invalid("the heads of a token must be contiguous, the tokens in order and the layers adjoining")
-            strides.append(step)
-        if strides[3] != self.q_heads * d:
-            _invalid("out must be contiguous")
-        for x, shape in ((s_new, (total,)), (mass, (self.layers, self.batch, self.kv_heads, self.capacity)), (slopes, (self.q_heads,))):
-            if x is not None and (x.dtype != torch.float32 or x.device != dev or tuple(x.shape) != shape or not x.is_contiguous()):
-                _invalid(f"s_new, mass and slopes must be contiguous fp32 tensors on {dev} (here: {shape})")
-        opts = dynts_extend_opts_t()
-        opts.softcap, opts.window, opts.stage = softcap, window, 1 if stage else 0
-        opts.slopes, opts.s_new, opts.mass = _ptr(slopes), _ptr(s_new), _ptr(mass)
-        opts.q_stride, opts.k_stride, opts.v_stride = strides[0], strides[1], strides[2]
+        total = sum(listed)
+        layers, dt, dev, d = self.layers, self.torch_dtype, self.device_index, self.head_dim
+        wide = (total, self.q_heads, d) if layer is not None else (layers, total, self.q_heads, d)
+        narrow = (total, self.kv_heads, d) if layer is not None else (layers, total, self.kv_heads, d)
+        strides = [0, 0, 0]  # contiguous
+        for i, (x, shape) in enumerate(((q, wide), (k, narrow), (v, narrow), (out, wide))):
+            if x.dtype is not dt or x.get_device() != dev or x.shape != shape:
+                _invalid(f"q, k, v and out must be {dt} tensors on cuda:{dev}, here {wide} and {narrow} by n_new")
+            if not x.is_contiguous():
+                heads = shape[-2]
+                step = x.stride(-3) if total > 1 else heads * d
+                if i == 3:
+                    _invalid("out must be contiguous")
+                if (x.stride(-1) != 1 or (heads > 1 and x.stride(-2) != d) or step < heads * d or
+                        (layer is None and layers > 1 and x.stride(0) != total * step)):
+                    _invalid("the heads of a token must be contiguous, the tokens in order and the layers adjoining")
+                strides[i] = step
+        for x, shape in ((s_new, (total,)), (mass, self.mass_shape), (slopes, (self.q_heads,))):
+            if x is not None and (x.dtype is not t.torch.float32 or x.get_device() != dev or x.shape != shape or not x.is_contiguous()):
+                _invalid(f"s_new, mass and slopes must be contiguous fp32 tensors on cuda:{dev} (here: {shape})")
+        prefixes = None
         if prefix is not None:
             if len(prefix) != self.batch:
                 _invalid("prefix needs a count for each sequence")
-            opts.prefix, keep_p = _host_ints(prefix)
-        if int(sum(n_new.tolist() if hasattr(n_new, "tolist") else n_new)) != total:
-            _invalid("n_new does not add up to the tokens of q")
-        need = lib.dynts_extend_scratch_bytes(self.handle, counts, 1 if layer is not None else self.layers)
-        if not self._scratch or self._scratch[-1].numel() < need:
-            # (never given back before the cache: the stream and captured graphs may still use it)
-            self._scratch.append(torch.empty(max(need, 2 * self._scratch[-1].numel() if self._scratch else 0), dtype=torch.uint8, device=dev))
-        scratch = self._scratch[-1]
+            prefixes, keep_p = _host_ints(prefix)
+        opts = dynts_extend_opts_t(softcap, None if slopes is None else slopes.data_ptr(), window, prefixes, None if s_new is None else s_new.data_ptr(),
+                                   None if mass is None else mass.data_ptr(), 1 if stage else 0, *strides)
+        need = lib.dynts_extend_scratch_bytes(self.handle, counts, layers if layer is None else 1)
+        if need > self._scratch_bytes:
+            # (a piece is never given back before the cache: the stream and captured graphs may still use it)
+            self._scratch.append(t.torch.empty(max(need, 2 * self._scratch_bytes), dtype=t.torch.uint8, device=self.device))
+            self._scratch_ptr, self._scratch_bytes = self._scratch[-1].data_ptr(), self._scratch[-1].numel()
+        args = (q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), counts, C.byref(opts), self._scratch_ptr, self._scratch_bytes)
+        if t.device() != dev:
+            with t.torch.cuda.device(dev):
+                return self._extend_call(layer, args)
+        return self._extend_call(layer, args)
 
-        def call():
-            if layer is None:
-                return _check(lib.dynts_extend_attn(self.handle, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), counts, C.byref(opts),
-                                                    scratch.data_ptr(), scratch.numel()))
-            return _check(lib.dynts_extend_attn_layer(self.handle, layer, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), counts,
-                                                      C.byref(opts), scratch.data_ptr(), scratch.numel()))
-
-        if torch.cuda.current_device() == dev.index:
-            return call()
-        with torch.cuda.device(dev):
-            return call()
+    def _extend_call(self, layer, args):
+        if layer is None:
+            return _check(lib.dynts_extend_attn(self.handle, *args))
+        return _check(lib.dynts_extend_attn_layer(self.handle, layer, *args))
 
     def extend_attn(self, q, k, v, out, n_new, s_new=None, mass=None, softcap=0.0, slopes=None, window=0, prefix=None, stage=False):
         """A chunk of n_new[b] tokens per sequence for all layers: q, out [L, n_total, Hq, d], k, v [L, n_total, Hkv, d]."""

@@ -1706,10 +1706,10 @@ dynts_status_t launch_extend(dynts_cache* c, int layer0, int n_layers, const Ext
       dynts_status_t st = plan_extend(c, p, m, a.scratch, plan, &tc_grid);
       if (st != DYNTS_OK) return st;
     }
-    if (kv8) dynts::extend_store_kernel<__nv_bfloat16, true><<<grid, 256, 0, c->stream>>>(p, plan);
-    else if (f.dtype == DYNTS_FP32) dynts::extend_store_kernel<float, false><<<grid, 256, 0, c->stream>>>(p, plan);
-    else dynts::extend_store_kernel<__nv_bfloat16, false><<<grid, 256, 0, c->stream>>>(p, plan);
-    CUDA_TRY(cudaGetLastError());
+    CUDA_TRY(launch_dependent(kv8                      ? dynts::extend_store_kernel<__nv_bfloat16, true>
+                              : f.dtype == DYNTS_FP32 ? dynts::extend_store_kernel<float, false>
+                                                      : dynts::extend_store_kernel<__nv_bfloat16, false>,
+                              grid, 256, 0, c->stream, p, plan));
     c->launches += 1;
     p.published = p.publish;
     dynts_status_t st = tc ? launch_extend_tc(c, p, plan, tc_grid, m, a.scratch, want_mass)

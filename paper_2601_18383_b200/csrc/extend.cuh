@@ -206,6 +206,7 @@ __device__ __forceinline__ void ext_write_plan(const ExtendParams& p, const Exte
 template <typename T, bool KV8>
 __global__ void __launch_bounds__(256) extend_store_kernel(const __grid_constant__ ExtendParams p, const __grid_constant__ ExtendPlan plan) {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // the next kernel's set-up may begin; it waits for this grid before it reads
+  asm volatile("griddepcontrol.wait;" ::: "memory");
   constexpr int E = 16 / (int)sizeof(T);  // elements per 16-byte piece of the source
   const unsigned pieces = (unsigned)p.d / E;
   const int tok_begin = p.seqs.tok0[0];

@@ -240,6 +240,13 @@ __device__ __noinline__ float4 xt_row_again(const ExtendTcParams& p, int d, int 
   return make_float4(acc[0], acc[1], acc[2], acc[3]);
 }
 
+// x + log2(sum), with the whole part of the logarithm taken out exactly: the approximation is off by 2^-22 of its result,
+// which at sums of 2^-33 (a reference with headroom) is 8e-6, and every weight of a mass would carry it.
+__device__ __forceinline__ float xt_add_log2(float x, float sum) {
+  const int bits = __float_as_int(sum);
+  return (x + (float)((bits >> 23) - 127)) + __log2f(__int_as_float((bits & 0x7fffff) | 0x3f800000));
+}
+
 // Joins the parts of the item that begins in CTA blockIdx.x's shares and ends behind them, if there is one: 32 rows per
 // block (y), a warp 8 rows x 64 columns, a thread four pieces of four columns of one row.  A part's 128-byte pieces
 // are read whole, the output's sectors written whole.  Running maximum and sum over the parts, in the order of the
@@ -291,7 +298,7 @@ __global__ void __launch_bounds__(256) extend_join_kernel(const __grid_constant_
 #pragma unroll
   for (int e = 0; e < 4; ++e)
     *reinterpret_cast<uint2*>(dst + 16 * e) = make_uint2(pack_bf16x2(acc[4 * e] * f, acc[4 * e + 1] * f), pack_bf16x2(acc[4 * e + 2] * f, acc[4 * e + 3] * f));
-  if (c4 == 0 && x.lse) x.lse[ext_lse_index(x, layer, h, tok) + row] = M + __log2f(sum);
+  if (c4 == 0 && x.lse) x.lse[ext_lse_index(x, layer, h, tok) + row] = xt_add_log2(M, sum);
 }
 
 // The end of a piece, by the eight softmax warps: a group's 64 columns of the output, or of its part of an item that
@@ -316,7 +323,7 @@ __device__ __noinline__ void xt_epilogue(const ExtendTcParams& p, int d, int ord
   const size_t piece = (size_t)p.part_rows;
   float* part = p.part + (size_t)word(kPwPlace) * (piece * kXtPartFloats);
   const bool redo = mine && !(l < kXtSumMax);  // out of range, or not a number
-  float lse = l > 0.f ? ref + __log2f(l) : -CUDART_INF_F;
+  float lse = l > 0.f ? xt_add_log2(ref, l) : -CUDART_INF_F;
   const float f = l > 0.f ? 1.f / l : 0.f;
   __nv_bfloat16* obase = static_cast<__nv_bfloat16*>(x.out) + (((size_t)layer * x.total + tok) * x.Hq + h * x.G) * 128;
   const uint32_t t_row = tO + ((uint32_t)(wq * 32) << 16);
