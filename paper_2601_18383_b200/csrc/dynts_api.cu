@@ -1432,19 +1432,27 @@ dynts_status_t check_extend(const dynts_cache* c, const ExtendCall& a, int n_lay
 }
 
 template <typename Kern, typename... Args>
-cudaError_t launch_dependent(Kern kern, dim3 grid, unsigned threads, size_t smem, cudaStream_t st, Args... args) {
+cudaError_t launch_dependent_clusters(Kern kern, unsigned cluster, dim3 grid, unsigned threads, size_t smem, cudaStream_t st, Args... args) {
   cudaLaunchConfig_t lc;
   memset(&lc, 0, sizeof(lc));
-  cudaLaunchAttribute at[1];
+  cudaLaunchAttribute at[2];
   at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;  // see griddepcontrol.wait in the kernels
   at[0].val.programmaticStreamSerializationAllowed = 1;
+  at[1].id = cudaLaunchAttributeClusterDimension;
+  at[1].val.clusterDim.x = cluster;
+  at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
   lc.attrs = at;
-  lc.numAttrs = 1;
+  lc.numAttrs = cluster > 1 ? 2 : 1;
   lc.stream = st;
   lc.gridDim = grid;
   lc.blockDim = dim3(threads, 1, 1);
   lc.dynamicSmemBytes = smem;
   return cudaLaunchKernelEx(&lc, kern, args...);
+}
+
+template <typename Kern, typename... Args>
+cudaError_t launch_dependent(Kern kern, dim3 grid, unsigned threads, size_t smem, cudaStream_t st, Args... args) {
+  return launch_dependent_clusters(kern, 1, grid, threads, smem, st, args...);
 }
 
 template <typename T, bool KV8>
@@ -1465,8 +1473,15 @@ dynts_status_t launch_extend_generic(dynts_cache* c, dynts::ExtendParams& p, boo
     p.seqs.item0[s + 1] = p.seqs.item0[s] + (int)((rows + dynts::kExtGenericRows - 1) / dynts::kExtGenericRows);
   }
   const unsigned ny = (unsigned)(p.n_layers * p.Hkv);
-  CUDA_TRY(launch_dependent(dynts::extend_generic_kernel<T, KV8>, dim3((unsigned)p.seqs.item0[n_seq], ny, 1), dynts::kExtGenericThreads, smem,
-                            c->stream, p));
+  // Items that leave SMs idle take a cluster each, up to a CTA per key tile (by the host's copy of the lengths, which only
+  // guides the cut).
+  long long longest = 0;
+  for (int s = 0; s < n_seq; ++s) longest = std::max<long long>(longest, c->len_h[p.seqs.b0 + s] + p.seqs.tok0[s + 1] - p.seqs.tok0[s]);
+  if (p.window > 0) longest = std::min<long long>(longest, (long long)p.window + dynts::kExtGenericRows);
+  unsigned cluster = 1;
+  while (cluster < 8 && (long long)p.seqs.item0[n_seq] * ny * cluster * 2 <= c->sm_count && (long long)cluster * dynts::kExtGenericKeys < longest) cluster *= 2;
+  CUDA_TRY(launch_dependent_clusters(dynts::extend_generic_kernel<T, KV8>, cluster, dim3((unsigned)p.seqs.item0[n_seq] * cluster, ny, 1),
+                                     dynts::kExtGenericThreads, smem, c->stream, p, (int)cluster));
   c->launches += 1;
   if (want_mass) {
     // grid over the capacity, not over the host's copy of the lengths: a replayed graph may hold longer sequences

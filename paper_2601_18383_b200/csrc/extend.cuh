@@ -20,6 +20,7 @@
 #include <math_constants.h>
 
 #include "common.cuh"
+#include "evict.cuh"  // the cluster barrier
 
 namespace dynts {
 
@@ -333,44 +334,77 @@ __device__ __forceinline__ float ext_row_value(const void* base, size_t idx, flo
   else return to_float(static_cast<const T*>(base)[idx]);
 }
 
-constexpr size_t ext_generic_smem(int d) {  // Q [32][d], K [32][d + 4], V [32][d], positions of the tile
-  return ((size_t)kExtGenericRows * d + (size_t)kExtGenericKeys * (d + 4) + (size_t)kExtGenericKeys * d + kExtGenericKeys) * sizeof(float);
+// Four adjoining elements (head sizes are multiples of 8, token strides of 16 bytes).
+template <typename T, bool KV8>
+__device__ __forceinline__ float4 ext_row_value4(const void* base, size_t idx, float scale) {
+  if constexpr (KV8) {
+    const uint32_t c = *reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(base) + idx);
+    return make_float4(e4m3_to_float((uint8_t)c) * scale, e4m3_to_float((uint8_t)(c >> 8)) * scale, e4m3_to_float((uint8_t)(c >> 16)) * scale,
+                       e4m3_to_float((uint8_t)(c >> 24)) * scale);
+  } else if constexpr (sizeof(T) == 4) {
+    return *reinterpret_cast<const float4*>(static_cast<const T*>(base) + idx);
+  } else {
+    const uint2 y = *reinterpret_cast<const uint2*>(static_cast<const T*>(base) + idx);
+    return make_float4(__uint_as_float(y.x << 16), __uint_as_float(y.x & 0xffff0000u), __uint_as_float(y.y << 16), __uint_as_float(y.y & 0xffff0000u));
+  }
 }
 
-// Any type, any head size: fp32 FMA.  CTA = 32 query rows of one (layer, sequence, KV head), four per
-// warp; lane = key for the products and the softmax, lane = column of head_dim for the output.  The
-// weights are exact fp32 (exp2f, tanhf).  Bound by FMA and shared-memory issue; it serves fp32 slabs
-// (where the tensor cores' formats could not hold 2e-5) and head sizes other than 128.
+__device__ __forceinline__ float ext_peer_float(const float* mine, int rank) {  // the same word of another CTA of the cluster
+  uint32_t at;
+  float x;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"((uint32_t)__cvta_generic_to_shared(mine)), "r"(rank));
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(x) : "r"(at) : "memory");
+  return x;
+}
+
+constexpr int kExtWarps = kExtGenericThreads / 32;
+constexpr int kExtRowsPerWarp = kExtGenericRows / kExtWarps;
+static_assert(kExtRowsPerWarp == 4 && kExtGenericKeys == 32, "a lane's registers");
+
+constexpr size_t ext_generic_smem(int d) {  // Q [32][d], K [32][d + 4], V [32][d], a warp's weights [32][4], positions of the tile
+  return ((size_t)kExtGenericRows * d + (size_t)kExtGenericKeys * (d + 4) + (size_t)kExtGenericKeys * d + (size_t)kExtGenericRows * kExtGenericKeys +
+          kExtGenericKeys) * sizeof(float);
+}
+
+// Any type, any head size: fp32 FMA.  A work item = 32 query rows of one (layer, sequence, KV head), four per warp; lane =
+// key for the products and the softmax, lane = column of head_dim for the output.  The weights are exact fp32 (exp2f,
+// tanhf).  It serves fp32 slabs (where the tensor cores' formats could not hold 2e-5) and head sizes other than 128.
+// Bound by FMA and shared-memory issue where there are many items; where they are few, by the chain of a tile's
+// steps, so the key tiles of an item are dealt to a cluster of up to eight CTAs, which join their parts through
+// one another's shared memory, in the order of their ranks.
 template <typename T, bool KV8>
-__global__ void __launch_bounds__(kExtGenericThreads) extend_generic_kernel(const __grid_constant__ ExtendParams p) {
+__global__ void __launch_bounds__(kExtGenericThreads) extend_generic_kernel(const __grid_constant__ ExtendParams p, int cluster) {
   extern __shared__ __align__(16) float ext_sm[];
-  const int d = p.d, ldk = d + 4;
+  const int d = p.d, ldk = d + 4, pieces = d / 4;
   float* sQ = ext_sm;
   float* sK = sQ + kExtGenericRows * d;
   float* sV = sK + kExtGenericKeys * ldk;
-  int* sP = reinterpret_cast<int*>(sV + kExtGenericKeys * d);
+  float* sW = sV + kExtGenericKeys * d;
+  int* sP = reinterpret_cast<int*>(sW + kExtGenericRows * kExtGenericKeys);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int item = (int)blockIdx.x / cluster, rank = (int)blockIdx.x - item * cluster;
+  const unsigned piece_inv = 65536u / (unsigned)pieces + 1u;  // x / pieces = (x * piece_inv) >> 16 for x < 256 and up to 64 pieces
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  const int s = ext_find(p.seqs.item0, p.seqs.n, blockIdx.x);
+  const int s = ext_find(p.seqs.item0, p.seqs.n, item);
   const ExtSeq e = ext_seq(p, s);
-  if (!e.ok) return;
+  if (!e.ok) return;  // (the whole cluster)
   const int layer = blockIdx.y / p.Hkv, h = blockIdx.y % p.Hkv;
-  const int r0 = ((int)blockIdx.x - p.seqs.item0[s]) * kExtGenericRows;
+  const int r0 = (item - p.seqs.item0[s]) * kExtGenericRows;
   const int rows = min(kExtGenericRows, e.t * p.G - r0);
   const size_t tok_base = (size_t)layer * p.total + p.seqs.tok0[s];
   const size_t slab = ((size_t)(p.layer0 + layer) * p.Nb + e.b) * p.Hkv + h;
-  for (int x = tid; x < kExtGenericRows * d; x += kExtGenericThreads) {
-    const int r = x / d, c = x - r * d;
-    float y = 0.f;
+  for (int x = lane; x < kExtRowsPerWarp * pieces; x += 32) {  // a warp stages its own four rows
+    const int rl = (int)(((unsigned)x * piece_inv) >> 16), r = warp * kExtRowsPerWarp + rl, c = 4 * (x - rl * pieces);
+    float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
     if (r < rows) {
       const int i = (r0 + r) / p.G, g = (r0 + r) - i * p.G;
-      y = to_float(static_cast<const T*>(p.q)[(tok_base + i) * p.q_stride + (size_t)(h * p.G + g) * d + c]);
+      y = ext_row_value4<T, false>(p.q, (tok_base + i) * p.q_stride + (size_t)(h * p.G + g) * d + c, 1.f);
     }
-    sQ[x] = y;
+    *reinterpret_cast<float4*>(sQ + r * d + c) = y;
   }
   // this warp's rows
   int tok[4];
-  float slope[4], m[4], l[4], acc[4][8];
+  float slope[4], m[4], l[4], acc[4][8];  // l: this lane's part of the row's sum
 #pragma unroll
   for (int u = 0; u < 4; ++u) {
     const int r = r0 + warp * 4 + u;
@@ -386,18 +420,25 @@ __global__ void __launch_bounds__(kExtGenericThreads) extend_generic_kernel(cons
   const int end = e.n + max(i1 + 1, prefix);
   // (positions ascend with the rows, so a row more than `window` rows back is more than `window` positions back)
   const int begin = p.window > 0 ? max(0, e.n + i0 - p.window + 1) : 0;
-  for (int k0 = begin / kExtGenericKeys * kExtGenericKeys; k0 < end; k0 += kExtGenericKeys) {
+  for (int k0 = (begin / kExtGenericKeys + rank) * kExtGenericKeys; k0 < end; k0 += kExtGenericKeys * cluster) {
     __syncthreads();
-    for (int x = tid; x < kExtGenericKeys * d; x += kExtGenericThreads) {
-      const int r = x / d, c = x - r * d;
+#pragma unroll 2
+    for (int x = lane; x < 4 * pieces; x += 32) {  // a warp stages four rows of K and of V
+      const int rl = (int)(((unsigned)x * piece_inv) >> 16), r = warp * 4 + rl, c = 4 * (x - rl * pieces);
       const bool in = k0 + r < e.n + e.t;
       const size_t idx = (slab * p.cap + k0 + r) * d + c;
-      sK[r * ldk + c] = in ? ext_row_value<T, KV8>(p.K, idx, 1.f) : 0.f;  // (k_scale is part of p.scale)
-      sV[r * d + c] = in ? ext_row_value<T, KV8>(p.V, idx, p.v_scale) : 0.f;
+      float4 kk = make_float4(0.f, 0.f, 0.f, 0.f), vv = kk;
+      if (in) {
+        kk = ext_row_value4<T, KV8>(p.K, idx, 1.f);  // (k_scale is part of p.scale)
+        vv = ext_row_value4<T, KV8>(p.V, idx, p.v_scale);
+      }
+      *reinterpret_cast<float4*>(sK + r * ldk + c) = kk;
+      *reinterpret_cast<float4*>(sV + r * d + c) = vv;
     }
     if (tid < kExtGenericKeys) sP[tid] = k0 + tid < e.n + e.t ? p.pos[slab * p.cap + k0 + tid] : 0;
     __syncthreads();
     float dot[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
     for (int c = 0; c < d; c += 4) {
       const float4 kv = *reinterpret_cast<const float4*>(sK + lane * ldk + c);
 #pragma unroll
@@ -419,18 +460,18 @@ __global__ void __launch_bounds__(kExtGenericThreads) extend_generic_kernel(cons
       const float m_new = fmaxf(m[u], mx);
       const float alpha = m[u] == -CUDART_INF_F ? 0.f : exp2f(m[u] - m_new);
       w[u] = visible ? exp2f(x - m_new) : 0.f;
-      float sum = w[u];
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-      l[u] = l[u] * alpha + sum;
+      l[u] = l[u] * alpha + w[u];
       m[u] = m_new;
 #pragma unroll
       for (int c = 0; c < 8; ++c) acc[u][c] *= alpha;
     }
+    float* ww = sW + warp * 4 * kExtGenericKeys;  // the warp's weights, four rows of a key side by side
+    *reinterpret_cast<float4*>(ww + 4 * lane) = make_float4(w[0], w[1], w[2], w[3]);
+    __syncwarp();
+#pragma unroll 4
     for (int kk = 0; kk < kExtGenericKeys; ++kk) {
-      float wk[4];
-#pragma unroll
-      for (int u = 0; u < 4; ++u) wk[u] = __shfl_sync(0xffffffffu, w[u], kk);
+      const float4 w4 = *reinterpret_cast<const float4*>(ww + 4 * kk);
+      const float wk[4] = {w4.x, w4.y, w4.z, w4.w};
 #pragma unroll
       for (int c = 0; c < 8; ++c) {
         if (c * 32 >= d) break;
@@ -443,18 +484,71 @@ __global__ void __launch_bounds__(kExtGenericThreads) extend_generic_kernel(cons
     }
   }
 #pragma unroll
+  for (int u = 0; u < 4; ++u)
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) l[u] += __shfl_xor_sync(0xffffffffu, l[u], o);
+  auto write = [&](int r, int col, float y) {  // (col < d)
+    const int i = r / p.G, head = h * p.G + r - i * p.G;
+    from_float(static_cast<T*>(p.out) + ((tok_base + i) * p.Hq + head) * d + col, y);
+  };
+  if (cluster == 1) {
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int rl = warp * 4 + u;
+      if (rl >= rows) continue;
+#pragma unroll
+      for (int c = 0; c < 8; ++c)
+        if (c * 32 + lane < d) write(r0 + rl, c * 32 + lane, acc[u][c] / l[u]);
+      if (p.lse && lane == 0) p.lse[ext_lse_index(p, layer, h, p.seqs.tok0[s]) + r0 + rl] = m[u] + log2f(l[u]);
+    }
+    return;
+  }
+  // The parts join: every CTA leaves its own in shared memory (over K and V), and the rows are dealt to the cluster's warps.
+  float* sA = sK;                              // [32][d]
+  float* sML = sK + kExtGenericRows * d;       // [2][32]: maxima, sums
+  __syncthreads();
+#pragma unroll
   for (int u = 0; u < 4; ++u) {
     const int rl = warp * 4 + u;
-    if (rl >= rows) continue;
-    const int r = r0 + rl, i = r / p.G, head = h * p.G + r % p.G;
-    T* o = static_cast<T*>(p.out) + ((tok_base + i) * p.Hq + head) * d;
 #pragma unroll
-    for (int c = 0; c < 8; ++c) {
-      const int col = c * 32 + lane;
-      if (col < d) from_float(o + col, acc[u][c] / l[u]);
+    for (int c = 0; c < 8; ++c)
+      if (c * 32 + lane < d) sA[rl * d + c * 32 + lane] = acc[u][c];
+    if (lane == 0) {
+      sML[rl] = m[u];
+      sML[kExtGenericRows + rl] = l[u];
     }
-    if (p.lse && lane == 0) p.lse[ext_lse_index(p, layer, h, p.seqs.tok0[s]) + r] = m[u] + log2f(l[u]);
   }
+  cluster_arrive();
+  cluster_wait();
+  for (int rl = rank * kExtWarps + warp; rl < rows; rl += cluster * kExtWarps) {
+    const float pm = lane < cluster ? ext_peer_float(sML + rl, lane) : -CUDART_INF_F;
+    const float pl = lane < cluster ? ext_peer_float(sML + kExtGenericRows + rl, lane) : 0.f;
+    float M = pm;
+#pragma unroll
+    for (int o = 4; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));  // (clusters of up to eight)
+    M = __shfl_sync(0xffffffffu, M, 0);
+    const float f = pm == -CUDART_INF_F ? 0.f : exp2f(pm - M);
+    float sum = pl * f;
+#pragma unroll
+    for (int o = 4; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    sum = __shfl_sync(0xffffffffu, sum, 0);
+    float fs[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) fs[k] = __shfl_sync(0xffffffffu, f, k);
+    for (int col = lane; col < d; col += 32) {
+      float y[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) y[k] = k < cluster ? ext_peer_float(sA + rl * d + col, k) : 0.f;
+      float o = 0.f;
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        if (fs[k] != 0.f) o = fmaf(fs[k], y[k], o);
+      write(r0 + rl, col, o / sum);
+    }
+    if (p.lse && lane == 0) p.lse[ext_lse_index(p, layer, h, p.seqs.tok0[s]) + r0 + rl] = M + log2f(sum);
+  }
+  cluster_arrive();  // (no CTA ends while another reads from it)
+  cluster_wait();
 }
 
 // What the mass kernels do with a row's total: exactly one thread owns the row.
