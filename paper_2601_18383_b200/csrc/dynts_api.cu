@@ -1596,6 +1596,7 @@ dynts_status_t launch_extend_tc(dynts_cache* c, const dynts::ExtendParams& x, co
   p.out_scale = c->cfg.dtype == DYNTS_BF16_KV8 ? c->v_scale : 1.f;
   p.scale_log2 = (float)(1.4426950408889634 * (double)x.scale);
   p.cap_log2 = (float)(1.4426950408889634 * (double)x.cap_logit);
+  p.cap_y = x.cap_logit > 0.f ? (float)((double)x.scale / (double)x.cap_logit) : 0.f;
   p.cap_arg = x.cap_logit > 0.f ? (float)(2.0 * 1.4426950408889634 * (double)x.scale / (double)x.cap_logit) : 0.f;
   // Mass items: 256 rows of a slab each.  Fewer than CTAs: their query rows are cut, in parts of at least two steps.
   p.mass_part = reinterpret_cast<float*>(scratch + m.mass);

@@ -562,22 +562,22 @@ __device__ __forceinline__ void ext_emit_mass(const ExtendParams& p, size_t row,
   }
 }
 
-constexpr size_t ext_generic_mass_smem(int d) {  // K [32][d + 4], one query row per warp, partial sums
-  return ((size_t)kExtGenericKeys * (d + 4) + (size_t)(kExtGenericThreads / 32) * d + (kExtGenericThreads / 32) * kExtGenericKeys) * sizeof(float);
+constexpr size_t ext_generic_mass_smem(int d) {  // K [32][d + 4], four query rows per warp, partial sums
+  return ((size_t)kExtGenericKeys * (d + 4) + (size_t)kExtGenericRows * d + (size_t)kExtWarps * kExtGenericKeys) * sizeof(float);
 }
 
-// mass_j = sum over the chunk's tokens and the group's heads of the weight of row j, from the logits
-// and each query row's log-sum-exp.  CTA = 32 rows of one slab; the warps take the query rows in
-// turn, lane = key; the eight partial sums are added in a fixed order.
+// mass_j = sum over the chunk's tokens and the group's heads of the weight of row j, from the logits and each query
+// row's log-sum-exp.  CTA = 32 rows of one slab; the warps take the query rows in turn, four at once (one read of
+// K for four products), lane = key; the eight partial sums are added in a fixed order.
 template <typename T, bool KV8>
 __global__ void __launch_bounds__(kExtGenericThreads) extend_generic_mass_kernel(const __grid_constant__ ExtendParams p) {
   extern __shared__ __align__(16) float ext_sm[];
-  const int d = p.d, ldk = d + 4;
-  constexpr int W = kExtGenericThreads / 32;
+  const int d = p.d, ldk = d + 4, pieces = d / 4;
   float* sK = ext_sm;
   float* sQ = sK + kExtGenericKeys * ldk;
-  float* sS = sQ + W * d;
+  float* sS = sQ + kExtGenericRows * d;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const unsigned piece_inv = 65536u / (unsigned)pieces + 1u;  // x / pieces = (x * piece_inv) >> 16 for x < 256 and up to 64 pieces
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const int layer = blockIdx.y / p.Hkv, h = blockIdx.y % p.Hkv, s = blockIdx.z;
   const ExtSeq e = ext_seq(p, s);
@@ -585,38 +585,55 @@ __global__ void __launch_bounds__(kExtGenericThreads) extend_generic_mass_kernel
   if (!e.ok || e.t == 0 || k0 >= e.n + e.t) return;
   const size_t tok_base = (size_t)layer * p.total + p.seqs.tok0[s];
   const size_t slab = ((size_t)(p.layer0 + layer) * p.Nb + e.b) * p.Hkv + h;
-  for (int x = tid; x < kExtGenericKeys * d; x += kExtGenericThreads) {
-    const int r = x / d, c = x - r * d;
-    sK[r * ldk + c] = k0 + r < e.n + e.t ? ext_row_value<T, KV8>(p.K, (slab * p.cap + k0 + r) * d + c, 1.f) : 0.f;
+  const float* lse = p.lse + ext_lse_index(p, layer, h, p.seqs.tok0[s]);
+#pragma unroll 2
+  for (int x = lane; x < 4 * pieces; x += 32) {  // a warp stages four rows of K
+    const int rl = (int)(((unsigned)x * piece_inv) >> 16), r = warp * 4 + rl, c = 4 * (x - rl * pieces);
+    *reinterpret_cast<float4*>(sK + r * ldk + c) =
+        k0 + r < e.n + e.t ? ext_row_value4<T, KV8>(p.K, (slab * p.cap + k0 + r) * d + c, 1.f) : make_float4(0.f, 0.f, 0.f, 0.f);
   }
   __syncthreads();
   const int j = k0 + lane;
   const int pj = j < e.n + e.t ? p.pos[slab * p.cap + j] : 0;
-  const int prefix = p.seqs.prefix[s];
+  const int prefix = p.seqs.prefix[s], all = e.t * p.G;
+  // (a token that sees row j: i >= j - n, or any where j lies before n + prefix)
+  const int first = e.n + prefix > k0 ? 0 : max(0, k0 - e.n) * p.G;
+  float* q4 = sQ + warp * 4 * d;
   float sum = 0.f;
-  for (int r = warp; r < e.t * p.G; r += W) {
-    const int i = r / p.G, head = h * p.G + r % p.G;
-    if (e.n + max(i + 1, prefix) <= k0) continue;  // (uniform over the warp)
-    const T* q = static_cast<const T*>(p.q) + (tok_base + i) * p.q_stride + (size_t)head * d;
+  for (int r = first + 4 * warp; r < all; r += kExtGenericRows) {
     __syncwarp();
-    for (int c = lane; c < d; c += 32) sQ[warp * d + c] = to_float(q[c]);
+#pragma unroll 2
+    for (int x = lane; x < 4 * pieces; x += 32) {
+      const int rl = (int)(((unsigned)x * piece_inv) >> 16), c = 4 * (x - rl * pieces), row = min(r + rl, all - 1), i = row / p.G;
+      *reinterpret_cast<float4*>(q4 + rl * d + c) =
+          ext_row_value4<T, false>(p.q, (tok_base + i) * p.q_stride + (size_t)(h * p.G + row - i * p.G) * d + c, 1.f);
+    }
     __syncwarp();
-    float dot = 0.f;
+    float dot[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
     for (int c = 0; c < d; c += 4) {
       const float4 kv = *reinterpret_cast<const float4*>(sK + lane * ldk + c);
-      const float4 qv = *reinterpret_cast<const float4*>(sQ + warp * d + c);
-      dot = fmaf(qv.x, kv.x, fmaf(qv.y, kv.y, fmaf(qv.z, kv.z, fmaf(qv.w, kv.w, dot))));
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const float4 qv = *reinterpret_cast<const float4*>(q4 + u * d + c);
+        dot[u] = fmaf(qv.x, kv.x, fmaf(qv.y, kv.y, fmaf(qv.z, kv.z, fmaf(qv.w, kv.w, dot[u]))));
+      }
     }
-    const int apart = abs(e.tot + i - pj);
-    if (j < e.n + max(i + 1, prefix) && (p.window == 0 || apart < p.window))
-      sum += exp2f(ext_logit_exact(p, dot, p.slopes ? p.slopes[head] : 0.f, apart) - p.lse[ext_lse_index(p, layer, h, p.seqs.tok0[s]) + r]);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      if (r + u >= all) break;
+      const int i = (r + u) / p.G, head = h * p.G + r + u - i * p.G;
+      const int apart = abs(e.tot + i - pj);
+      if (j < e.n + max(i + 1, prefix) && (p.window == 0 || apart < p.window))
+        sum += exp2f(ext_logit_exact(p, dot[u], p.slopes ? p.slopes[head] : 0.f, apart) - lse[r + u]);
+    }
   }
   sS[warp * kExtGenericKeys + lane] = sum;
   __syncthreads();
   if (warp == 0 && j < e.n + e.t) {
     float x = 0.f;
 #pragma unroll
-    for (int w = 0; w < W; ++w) x += sS[w * kExtGenericKeys + lane];
+    for (int w = 0; w < kExtWarps; ++w) x += sS[w * kExtGenericKeys + lane];
     ext_emit_mass(p, slab * p.cap + j, x);
   }
 }

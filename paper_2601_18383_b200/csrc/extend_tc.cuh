@@ -80,6 +80,7 @@ struct ExtendTcParams {
   float scale_log2;     // log2(e) * scale
   float cap_log2;       // c * log2(e)
   float cap_arg;        // 2 log2(e) * scale / c
+  float cap_y;          // scale / c
 };
 
 __device__ __forceinline__ float rcp_approx(float x) {
@@ -238,6 +239,37 @@ __device__ __noinline__ float4 xt_row_again(const ExtendTcParams& p, int d, int 
     }
   }
   return make_float4(acc[0], acc[1], acc[2], acc[3]);
+}
+
+// Capped logits of 32 columns, c tanh(s / c), in units of the factor it returns.  While every |y| = |s / c| of the warp is
+// at most 3/4 -- what a cap is set for -- tanh(y) = y P(y^2) with P the polynomial of degree 5 of the least greatest
+// relative error there (3e-8, below a rounding): eight packed operations per two columns on the FMA units.  Beyond,
+// tanh(y) = 1 - 2 / (1 + e^(2 y)): two results of the exponentials' unit, which the softmax needs as well and which
+// bounds it then.
+__device__ __forceinline__ float xt_cap(uint32_t (&sv)[32], const ExtendTcParams& p) {
+  float top = 0.f;
+#pragma unroll
+  for (int c = 0; c < 32; c += 2) top = tc5::f_max3(top, fabsf(__uint_as_float(sv[c])), fabsf(__uint_as_float(sv[c + 1])));
+  if (__all_sync(0xffffffffu, top * p.cap_y <= 0.75f)) {
+    const uint64_t a2 = tc5::f2_pack(p.cap_y, p.cap_y);
+    const float k[6] = {0.999999971f, -0.333329589f, 0.13325406f, -0.0533444308f, 0.0195829087f, -0.00471625728f};
+#pragma unroll
+    for (int c = 0; c < 32; c += 2) {
+      const uint64_t y = tc5::f2_mul(tc5::f2_pack(__uint_as_float(sv[c]), __uint_as_float(sv[c + 1])), a2), z = tc5::f2_mul(y, y);
+      uint64_t t = tc5::f2_pack(k[5], k[5]);
+#pragma unroll
+      for (int e = 4; e >= 0; --e) t = tc5::f2_fma(t, z, tc5::f2_pack(k[e], k[e]));
+      float y0, y1;
+      tc5::f2_unpack(tc5::f2_mul(t, y), y0, y1);
+      sv[c] = __float_as_uint(y0);
+      sv[c + 1] = __float_as_uint(y1);
+    }
+    return p.cap_log2;
+  }
+#pragma unroll
+  for (int c = 0; c < 32; ++c)
+    sv[c] = __float_as_uint(fmaf(-2.f * p.cap_log2, rcp_approx(1.f + fast_exp2(__uint_as_float(sv[c]) * p.cap_arg)), p.cap_log2));
+  return 1.f;
 }
 
 // x + log2(sum), with the whole part of the logarithm taken out exactly: the approximation is off by 2^-22 of its result,
@@ -759,12 +791,7 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
             tc5::tmem_wait_ld();
             if constexpr (MODS) {
               float scale = p.scale_log2;
-              if (x.cap_logit > 0.f) {  // c tanh(y) = c - 2 c / (1 + e^(2 y))
-                scale = 1.f;
-#pragma unroll
-                for (int c = 0; c < CH; ++c)
-                  sv[c] = __float_as_uint(fmaf(-2.f * p.cap_log2, rcp_approx(1.f + fast_exp2(__uint_as_float(sv[c]) * p.cap_arg)), p.cap_log2));
-              }
+              if (x.cap_logit > 0.f) scale = xt_cap(sv, p);
               const uint64_t scale2 = tc5::f2_pack(scale, scale);
               if (beside) {
 #pragma unroll
@@ -1184,12 +1211,7 @@ extend_mass_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_con
           }
           float scale = p.scale_log2;
           if constexpr (MODS) {
-            if (x.cap_logit > 0.f) {
-              scale = 1.f;
-#pragma unroll
-              for (int c = 0; c < 32; ++c)
-                sv[c] = __float_as_uint(fmaf(-2.f * p.cap_log2, rcp_approx(1.f + fast_exp2(__uint_as_float(sv[c]) * p.cap_arg)), p.cap_log2));
-            }
+            if (x.cap_logit > 0.f) scale = xt_cap(sv, p);
           }
           const uint64_t scale2 = tc5::f2_pack(scale, scale), off2 = tc5::f2_pack(off0, off0);
           auto add_up = [&](auto masked) {
