@@ -1341,6 +1341,7 @@ struct ExtendScratch {
 };
 
 constexpr int kMassParts = 8;  // parts of a mass item, at most
+constexpr int kMassSteps = 6;  // steps of a part, at least, once every CTA has one
 
 bool extend_tc_shape(const dynts_config_t& f) { return f.dtype != DYNTS_FP32 && f.head_dim == 128; }
 
@@ -1367,7 +1368,7 @@ ExtendScratch extend_scratch(const dynts_cache* c, const int* n_new, int n_layer
   if (extend_tc_shape(f)) {
     if (f.dtype == DYNTS_BF16_KV8) m.q16 = take((size_t)n_layers * total * f.q_heads * f.head_dim * 2);
     m.part = take((size_t)2 * m.ctas * m.part_rows * dynts::kXtPartFloats * sizeof(float));
-    m.counters = take((size_t)m.ctas * sizeof(int));  // of cut mass items
+    m.counters = take((size_t)m.ctas * (kMassParts / 2) * sizeof(int));  // of cut mass items (two parts each at least)
     m.mass = take((size_t)m.ctas * kMassParts * dynts::kXmItemKeys * sizeof(float));
     long long items = 0;  // of the launch with the most sequences' worth (a batch beyond 128 sequences takes several)
     for (int b0 = 0; b0 < f.batch; b0 += dynts::kExtSeqs) {
@@ -1520,8 +1521,7 @@ dynts_status_t extend_maps(dynts_cache* c) {
 }
 
 template <bool KV8, bool MODS>
-dynts_status_t launch_extend_tc_as(dynts_cache* c, dynts::ExtendTcParams& p, unsigned grid, const CUtensorMap& mq, const CUtensorMap& mqs,
-                                   bool want_mass) {
+dynts_status_t launch_extend_tc_as(dynts_cache* c, dynts::ExtendTcParams& p, unsigned grid, const CUtensorMap& mq, bool want_mass) {
   bool* attr = &c->attr_extend_tc[KV8 ? 1 : 0][MODS ? 1 : 0];
   if (!*attr) {
     CUDA_TRY(cudaFuncSetAttribute(dynts::extend_tc_kernel<KV8, MODS>, cudaFuncAttributeMaxDynamicSharedMemorySize, dynts::kXtSmemBytes));
@@ -1535,7 +1535,7 @@ dynts_status_t launch_extend_tc_as(dynts_cache* c, dynts::ExtendTcParams& p, uns
     c->launches += 1;
   }
   if (want_mass) {
-    CUDA_TRY(launch_dependent(dynts::extend_mass_tc_kernel<KV8, MODS>, dim3((unsigned)(2 * c->sm_count), 1, 1), dynts::kXmThreads, dynts::kXmSmemBytes, c->stream, p, mqs,
+    CUDA_TRY(launch_dependent(dynts::extend_mass_tc_kernel<KV8, MODS>, dim3((unsigned)(2 * c->sm_count), 1, 1), dynts::kXmThreads, dynts::kXmSmemBytes, c->stream, p, mq,
                               c->map_XK));
     c->launches += 1;
   }
@@ -1598,11 +1598,12 @@ dynts_status_t launch_extend_tc(dynts_cache* c, const dynts::ExtendParams& x, co
   p.cap_log2 = (float)(1.4426950408889634 * (double)x.cap_logit);
   p.cap_y = x.cap_logit > 0.f ? (float)((double)x.scale / (double)x.cap_logit) : 0.f;
   p.cap_arg = x.cap_logit > 0.f ? (float)(2.0 * 1.4426950408889634 * (double)x.scale / (double)x.cap_logit) : 0.f;
-  // Mass items: 256 rows of a slab each.  Fewer than CTAs: their query rows are cut, in parts of at least two steps.
+  // Mass items: 256 rows of a slab each, against unlike numbers of query rows.  They are cut into parts of the query rows
+  // until there are four per CTA, but not below six steps a part (one, while there is less than a part per CTA: a chunk of
+  // 200 tokens behind 2112 rows 49 us against 52 us with two; three or ten instead of six measured alike).  (One part per
+  // CTA left the SMs idle for a quarter of the time: four ragged sequences, 290 items: 255 against 220 us.)
   p.mass_part = reinterpret_cast<float*>(scratch + m.mass);
   p.mass_counters = x.counters;
-  p.mass_items = m.ctas;
-  p.mass_parts = 1;
   {
     long long items = 0;
     int longest = 0;
@@ -1613,7 +1614,13 @@ dynts_status_t launch_extend_tc(dynts_cache* c, const dynts::ExtendParams& x, co
     }
     items *= plan.lh;
     const int steps = (longest * c->G + dynts::kXmRows - 1) / dynts::kXmRows;
-    if (items > 0 && items < m.ctas) p.mass_parts = (int)std::max<long long>(1, std::min<long long>(std::min(kMassParts, steps / 2), (m.ctas + items - 1) / items));
+    const long long room = (long long)m.ctas * kMassParts;
+    int parts = 1;
+    while (parts < kMassParts && items * parts < 4ll * m.ctas && items * (parts + 1) <= room &&
+           steps >= (parts + 1) * (items * parts < m.ctas ? 1 : kMassSteps))
+      ++parts;
+    p.mass_parts = parts;
+    p.mass_items = (int)(room / std::max(2, parts));
   }
   // The queries, [layers x tokens][heads][128] in boxes of (tokens, the group's heads, 64 elements): a box is a tile's rows.
   const bool kv8 = c->cfg.dtype == DYNTS_BF16_KV8;
@@ -1621,18 +1628,16 @@ dynts_status_t launch_extend_tc(dynts_cache* c, const dynts::ExtendParams& x, co
   const cuuint64_t strides[2] = {256, (cuuint64_t)(kv8 ? (long long)x.Hq * 128 : x.q_stride) * 2};
   const cuuint32_t estr[3] = {1, 1, 1};
   const void* q = kv8 ? static_cast<const void*>(x.q16) : x.q;
-  CUtensorMap map[2];
-  for (int i = 0; i < (want_mass ? 2 : 1); ++i) {
-    const cuuint32_t box[3] = {64, (cuuint32_t)c->G, (cuuint32_t)((i == 0 ? dynts::kXtRows : dynts::kXmRows) / c->G)};
-    const CUresult r = c->encode(&map[i], kv8 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(q), dims, strides,
-                                 box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                                 CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-    if (r != CUDA_SUCCESS) return fail(DYNTS_ERR_CUDA, "cuTensorMapEncodeTiled failed (%d)", (int)r);
-  }
+  CUtensorMap map;
+  const cuuint32_t box[3] = {64, (cuuint32_t)c->G, (cuuint32_t)(dynts::kXtRows / c->G)};
+  const CUresult r = c->encode(&map, kv8 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(q), dims, strides,
+                               box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS) return fail(DYNTS_ERR_CUDA, "cuTensorMapEncodeTiled failed (%d)", (int)r);
   const bool mods = x.cap_logit > 0.f || x.slopes || x.window > 0;
   if (kv8)
-    return mods ? launch_extend_tc_as<true, true>(c, p, grid, map[0], map[1], want_mass) : launch_extend_tc_as<true, false>(c, p, grid, map[0], map[1], want_mass);
-  return mods ? launch_extend_tc_as<false, true>(c, p, grid, map[0], map[1], want_mass) : launch_extend_tc_as<false, false>(c, p, grid, map[0], map[1], want_mass);
+    return mods ? launch_extend_tc_as<true, true>(c, p, grid, map, want_mass) : launch_extend_tc_as<true, false>(c, p, grid, map, want_mass);
+  return mods ? launch_extend_tc_as<false, true>(c, p, grid, map, want_mass) : launch_extend_tc_as<false, false>(c, p, grid, map, want_mass);
 }
 
 dynts_status_t launch_extend(dynts_cache* c, int layer0, int n_layers, const ExtendCall& a, long long total, bool publish) {
@@ -1707,10 +1712,10 @@ dynts_status_t launch_extend(dynts_cache* c, int layer0, int n_layers, const Ext
     const int n_tok = p.seqs.tok0[n_seq] - p.seqs.tok0[0];
     if (n_tok == 0) continue;
     p.published = 0;
-    p.n_counters = tc && want_mass ? m.ctas : 0;
+    p.n_counters = tc && want_mass ? m.ctas * (kMassParts / 2) : 0;
     // one 16-byte piece of K and of V (and of the rows to clear, and of the queries to copy) per thread, up to a few CTAs per SM
     const long long pieces = f.head_dim * c->elt / 16, ny = (long long)n_layers * f.kv_heads;
-    long long work = std::max(n_tok * pieces, (long long)m.ctas);
+    long long work = std::max(n_tok * pieces, (long long)p.n_counters);
     if (p.zero_tail) work = std::max(work, (long long)n_seq * dynts::kExtTileKeys * pieces);
     if (p.q16) work = std::max(work, (long long)n_tok * c->G * (f.head_dim / 8));
     if (work >= (1ll << 31)) return fail(DYNTS_ERR_INVALID_ARG, "%d new tokens are beyond the launch limits", n_tok);

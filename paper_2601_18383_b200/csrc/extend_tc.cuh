@@ -886,22 +886,22 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
 }
 
 // extend_mass_tc_kernel: mass_j = sum over the chunk's tokens i and the group's heads of exp2(x_ij - lse_i).
-// The products are taken the other way round -- M = 128 keys, N = 64 query rows -- so that thread = key = tensor-
+// The products are taken the other way round -- M = 128 keys, N = 128 query rows -- so that thread = key = tensor-
 // memory lane: the sum over the queries stays in one register, needs no exchange between lanes and no atomics, and
 // exactly one thread writes a row.  A work item = 256 rows of one slab, 128 for each of two groups of four warps, against
-// the query rows that see any of them, in steps of 64; where the items are fewer than the CTAs the steps of each are
-// cut into parts, whose sums the last part to finish adds in order.  Persistent CTAs, two per SM; K 64 KB, Q in two
-// stages, S in two buffers of 64 columns per group.  (With 128 rows per item the Q tiles, read again from L2 for
-// every item, and the products' own reads of K and Q from shared memory bounded it: 1.25 times as long.)  What bounds it
-// now is the exponentials' unit and the chain S - read - exponentials.
+// the query rows that see any of them, in steps of 128; where the items are fewer than the CTAs the steps of each are
+// cut into parts, whose sums the last part to finish adds in order.  Persistent CTAs, two per SM; K 64 KB, Q 32 KB, one S
+// of 128 columns per group: while a group's S is made the other three groups of the SM compute.  (With 128 keys per item
+// the Q tiles, read again from L2 for every item, bounded it: 1.25 times as long.  With steps of 64 query rows in two buffers
+// per group the products did: 57 cycles instead of 64 for half the work, as the keys' 4 KB are read all the same.)
 constexpr int kXmThreads = 320;
 constexpr int kXmKeys = 128;                      // keys per group
 constexpr int kXmItemKeys = 2 * kXmKeys;
-constexpr int kXmRows = 64;                       // query rows per step
+constexpr int kXmRows = kXtRows;                       // query rows per step
 constexpr int kXmKBytes = kXmKeys * 256;
 constexpr int kXmQBytes = kXmRows * 256;
-constexpr int kXmWarpFloats = 128;                // per compute warp: a step's additive constants, its columns' negated slopes
-constexpr int kXmSmemBytes = 2 * kXmKBytes + 2 * kXmQBytes + 192 + (8 * kXmWarpFloats + kXmRows) * 4 + (2 * kExtSeqs + 1) * 4 + 12;
+constexpr int kXmWarpFloats = 2 * kXmRows;                // per compute warp: a step's additive constants, its columns' negated slopes
+constexpr int kXmSmemBytes = 2 * kXmKBytes + kXmQBytes + 192 + (8 * kXmWarpFloats + kXmRows) * 4 + (2 * kExtSeqs + 1) * 4 + 12;
 constexpr uint32_t kXmTmemCols = 256;
 
 struct XmCursor {
@@ -956,9 +956,9 @@ extend_mass_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_con
   extern __shared__ __align__(1024) uint8_t pf_smem[];
   uint8_t* sm = pf_smem;
   const uint32_t sK = smem_u32(sm);             // [2 groups][2 halves of head_dim][128 rows][128 B]
-  const uint32_t sQ = sK + 2 * kXmKBytes;       // [2 stages][2 halves][64 rows][128 B]
-  uint64_t* bars = reinterpret_cast<uint64_t*>(sm + 2 * kXmKBytes + 2 * kXmQBytes);
-  // barriers: 0 K filled, 1-2 Q stages filled, 3-6 S complete (2 x group + buffer), 7-10 S read (the same), 11 K read, 12 drain
+  const uint32_t sQ = sK + 2 * kXmKBytes;       // [2 halves][128 rows][128 B]
+  uint64_t* bars = reinterpret_cast<uint64_t*>(sm + 2 * kXmKBytes + kXmQBytes);
+  // barriers: 0 K filled, 1 Q filled, 2-3 a group's S complete, 4-5 a group's S read, 6 K read, 7 drain
   const uint32_t bar0 = smem_u32(bars);
   auto bar = [&](int i) { return bar0 + 8u * (uint32_t)i; };
   uint32_t* s_tmem = reinterpret_cast<uint32_t*>(bars + 15);
@@ -973,7 +973,7 @@ extend_mass_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_con
   const int tps = kXmRows / x.G;
 
   if (tid == 0) {
-    for (int i = 0; i < 13; ++i) mbar_init(bar(i), i == 0 && KV8 ? 8 : (i >= 7 && i < 11) ? kXmKeys : 1);
+    for (int i = 0; i < 8; ++i) mbar_init(bar(i), i == 0 && KV8 ? 8 : i == 4 || i == 5 ? kXmKeys : 1);
     *s_abort = 0;
     if ((smem_u32(sm) & 1023u) != 0u) {
       atomicOr(x.err, kErrStreamBounds);
@@ -987,13 +987,13 @@ extend_mass_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_con
     tc5::tmem_relinquish();
   }
   if (tid < kXmRows) s_tok[tid] = (float)(tid / x.G);
-  // Columns of a step that hold no query (64 is not a multiple of G): no load writes their rows of the Q tiles, which
+  // Columns of a step that hold no query (128 is not a multiple of G): no load writes their rows of the Q tiles, which
   // are zero from here on, and their log-sum-exp is +inf, so that they weigh nothing.
   {
     const int pad = kXmRows - tps * x.G;
-    for (int i = tid; i < 4 * pad * 8; i += kXmThreads) {
-      const int chunk = i & 7, r = tps * x.G + (i >> 3) % pad, half_stage = (i >> 3) / pad;
-      *reinterpret_cast<uint4*>(sm + 2 * kXmKBytes + half_stage * (kXmQBytes / 2) + r * 128 + chunk * 16) = make_uint4(0u, 0u, 0u, 0u);
+    for (int i = tid; i < 2 * pad * 8; i += kXmThreads) {
+      const int chunk = i & 7, r = tps * x.G + (i >> 3) % pad, half = (i >> 3) / pad;
+      *reinterpret_cast<uint4*>(sm + 2 * kXmKBytes + half * (kXmQBytes / 2) + r * 128 + chunk * 16) = make_uint4(0u, 0u, 0u, 0u);
     }
     if (pad > 0) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
@@ -1041,7 +1041,7 @@ extend_mass_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_con
     int g = 0;
     while (cur.it < n_items && !*s_abort) {
       if constexpr (!KV8) {
-        if (cur.ord > 0) mbar_wait(bar(11), (uint32_t)((cur.ord - 1) & 1), s_abort, x.err, kPfSpinLimit);  // the item before has read its K
+        if (cur.ord > 0) mbar_wait(bar(6), (uint32_t)((cur.ord - 1) & 1), s_abort, x.err, kPfSpinLimit);  // the item before has read its K
         __syncwarp();
         if (!*s_abort && tc5::elect_one()) {
           const int slab = slab_of(cur);
@@ -1054,15 +1054,15 @@ extend_mass_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_con
         __syncwarp();
       }
       for (int j = 0; j < cur.n_step; ++j, ++g) {
-        if (g >= 2) mbar_wait(bar(5 + (g & 1)), (uint32_t)(((g - 2) >> 1) & 1), s_abort, x.err, kPfSpinLimit);  // both groups' S of step g - 2 have read the stage
+        if (g > 0) mbar_wait(bar(3), (uint32_t)((g - 1) & 1), s_abort, x.err, kPfSpinLimit);  // both groups' S of the step before have read its Q
         __syncwarp();
         if (*s_abort) break;
         if (tc5::elect_one()) {
-          const uint32_t dst = sQ + (uint32_t)(g & 1) * kXmQBytes, bb = bar(1 + (g & 1));
+          const uint32_t bb = bar(1);
           const int tok = cur.layer * x.total + x.seqs.tok0[cur.s] + (cur.lo + j) * tps;
           mbar_arrive_expect_tx(bb, 256u * (uint32_t)(x.G * tps));
-          pf_tma_load(dst, &tmQ, 0, cur.h * x.G, tok, bb);
-          pf_tma_load(dst + kXmQBytes / 2, &tmQ, 64, cur.h * x.G, tok, bb);
+          pf_tma_load(sQ, &tmQ, 0, cur.h * x.G, tok, bb);
+          pf_tma_load(sQ + kXmQBytes / 2, &tmQ, 64, cur.h * x.G, tok, bb);
         }
         __syncwarp();
       }
@@ -1071,7 +1071,7 @@ extend_mass_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_con
     }
     if (*s_abort && lane == 0) {
       atomicOr(p.stop, 1);
-      for (int i = KV8 ? 1 : 0; i < 3; ++i)
+      for (int i = KV8 ? 1 : 0; i < 2; ++i)
         for (uint32_t ph = 0; ph < 2; ++ph)
           for (uint32_t w = 0; w < (1u << 16); ++w)
             if (mbar_try_wait(bar(i), ph)) break;
@@ -1088,22 +1088,21 @@ extend_mass_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_con
     while (cur.it < n_items && !*s_abort) {
       mbar_wait(bar(0), (uint32_t)(cur.ord & 1), s_abort, x.err, kPfSpinLimit);
       for (int j = 0; j < cur.n_step; ++j, ++g) {
-        const int st = g & 1;
-        mbar_wait(bar(1 + st), (uint32_t)((g >> 1) & 1), s_abort, x.err, kPfSpinLimit);
+        mbar_wait(bar(1), (uint32_t)(g & 1), s_abort, x.err, kPfSpinLimit);
 #pragma unroll
         for (int grp = 0; grp < 2; ++grp) {
-          if (g >= 2) mbar_wait(bar(7 + 2 * grp + st), (uint32_t)(((g - 2) >> 1) & 1), s_abort, x.err, kPfSpinLimit);
+          if (g > 0) mbar_wait(bar(4 + grp), (uint32_t)((g - 1) & 1), s_abort, x.err, kPfSpinLimit);
           __syncwarp();
           tc5::fence_after_sync();
           if (*s_abort) break;
-          const uint64_t dKg = dK + (uint64_t)(grp * (kXmKBytes >> 4)), dQg = dQ + (uint64_t)((uint32_t)st * (kXmQBytes >> 4));
+          const uint64_t dKg = dK + (uint64_t)(grp * (kXmKBytes >> 4));
           if (tc5::elect_one()) {
 #pragma unroll
             for (int kk = 0; kk < 8; ++kk)
-              tc5::mma_bf16_ss(tmem + 64u * (uint32_t)(2 * grp + st), dKg + (uint64_t)((kk >> 2) * (kXmKBytes >> 5) + (kk & 3) * 2),
-                               dQg + (uint64_t)((kk >> 2) * (kXmQBytes >> 5) + (kk & 3) * 2), idesc, kk > 0);
-            tc5::mma_commit(bar(3 + 2 * grp + st));
-            if (grp == 1 && j == cur.n_step - 1) tc5::mma_commit(bar(11));
+              tc5::mma_bf16_ss(tmem + 128u * (uint32_t)grp, dKg + (uint64_t)((kk >> 2) * (kXmKBytes >> 5) + (kk & 3) * 2),
+                               dQ + (uint64_t)((kk >> 2) * (kXmQBytes >> 5) + (kk & 3) * 2), idesc, kk > 0);
+            tc5::mma_commit(bar(2 + grp));
+            if (grp == 1 && j == cur.n_step - 1) tc5::mma_commit(bar(6));
           }
           __syncwarp();
         }
@@ -1114,9 +1113,9 @@ extend_mass_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_con
     }
     if (*s_abort && tc5::elect_one()) {
       atomicOr(p.stop, 1);
-      tc5::mma_commit(bar(12));
+      tc5::mma_commit(bar(7));
       for (uint32_t w = 0; w < kPfSpinLimit; ++w)
-        if (mbar_try_wait(bar(12), 0u)) break;
+        if (mbar_try_wait(bar(7), 0u)) break;
     }
   } else {
     // ================= compute warps: thread = key = tensor-memory lane =================
@@ -1142,7 +1141,7 @@ extend_mass_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_con
           XtCodes codes[4];
 #pragma unroll
           for (int q = 0; q < 4; ++q) xt_load_codes(codes[q], src, cur.k0 + wg * kXmKeys + wq * 32 + 8 * q, cur.n + cur.t, lane);
-          if (cur.ord > 0) xt_wait(bar(11), (uint32_t)((cur.ord - 1) & 1), abort_flag, x.err);
+          if (cur.ord > 0) xt_wait(bar(6), (uint32_t)((cur.ord - 1) & 1), abort_flag, x.err);
 #pragma unroll
           for (int q = 0; q < 4; ++q) xt_store_codes<false>(codes[q], sm + wg * kXmKBytes, kXmKBytes / 2, wq * 32 + 8 * q, lane);
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -1152,7 +1151,7 @@ extend_mass_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_con
       }
       // the tokens that see row j: [i_lo, i_hi)
       int i_lo = j < cur.n + prefix ? 0 : j - cur.n, i_hi = mine ? cur.t : 0;
-      float rel = 0.f, sl_a = 0.f, sl_b = 0.f;  // (slopes of columns lane and lane + 32)
+      float rel = 0.f;
       if constexpr (MODS) {
         const int b = x.seqs.b0 + cur.s;
         const int at = mine ? x.pos[row] - (x.tot[b] - (x.published ? cur.t : 0)) : 0;  // the row's position, the chunk's first token being 0
@@ -1162,12 +1161,10 @@ extend_mass_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_con
           i_hi = (int)min((long long)i_hi, max(0ll, (long long)at + x.window));
         }
         if (x.slopes) {
-          sl_a = x.slopes[cur.h * x.G + lane % x.G] * 1.4426950408889634f;
-          sl_b = x.slopes[cur.h * x.G + (32 + lane) % x.G] * 1.4426950408889634f;
+          __syncwarp();
+#pragma unroll
+          for (int o = 0; o < kXmRows; o += 32) sts_f(s_slope + 4u * (uint32_t)(o + lane), x.slopes[cur.h * x.G + (o + lane) % x.G] * -1.4426950408889634f);
         }
-        __syncwarp();
-        sts_f(s_slope + 4u * lane, -sl_a);
-        sts_f(s_slope + 128u + 4u * lane, -sl_b);
       }
       const float* lse = x.lse + ext_lse_index(x, cur.layer, cur.h, x.seqs.tok0[cur.s]);
       const int all_rows = cur.t * x.G, step_rows = tps * x.G;
@@ -1175,39 +1172,38 @@ extend_mass_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_con
         const int r = (cur.lo + step) * step_rows + lane + off;
         return lane + off < step_rows && r < all_rows ? -__ldg(lse + r) : -CUDART_INF_F;
       };
-      float la = 0.f, lb = 0.f;
-      if (n_step > 0) {
-        la = ask(0, 0);
-        lb = ask(0, 32);
-      }
+      float la[kXmRows / 32];
+#pragma unroll
+      for (int o = 0; o < kXmRows / 32; ++o) la[o] = n_step > 0 ? ask(0, 32 * o) : 0.f;
+      const bool biased = MODS && x.slopes != nullptr;
       float total = 0.f;
 #pragma unroll 1
       for (int st = 0; st < n_step; ++st, ++g) {
         __syncwarp();
-        sts_f(s_add + 4u * lane, MODS ? fmaf(-sl_a, lds_f(s_token + 4u * lane), la) : la);
-        sts_f(s_add + 128u + 4u * lane, MODS ? fmaf(-sl_b, lds_f(s_token + 128u + 4u * lane), lb) : lb);
-        if (st + 1 < n_step) {
-          la = ask(st + 1, 0);
-          lb = ask(st + 1, 32);
+#pragma unroll
+        for (int o = 0; o < kXmRows / 32; ++o) {
+          const uint32_t at = 4u * (uint32_t)(32 * o + lane);
+          sts_f(s_add + at, biased ? fmaf(lds_f(s_slope + at), lds_f(s_token + at), la[o]) : la[o]);
+          if (st + 1 < n_step) la[o] = ask(st + 1, 32 * o);
         }
         __syncwarp();
         const int i0 = (cur.lo + st) * tps;
         const int rows = min(step_rows, all_rows - (cur.lo + st) * step_rows);
-        const int c_lo = min(64, max(0, (i_lo - i0) * x.G)), c_hi = min(rows, max(0, (min(i_hi, i0 + tps) - i0) * x.G));
+        const int c_lo = min(kXmRows, max(0, (i_lo - i0) * x.G)), c_hi = min(rows, max(0, (min(i_hi, i0 + tps) - i0) * x.G));
         const bool full = __all_sync(0xffffffffu, c_lo == 0 && c_hi == step_rows);
         const float off0 = (float)i0 - rel;
-        const bool beside = MODS && prefix > 0 && x.slopes;  // rows of later positions may be seen
-        xt_wait(bar(3 + 2 * wg + (g & 1)), (uint32_t)((g >> 1) & 1), abort_flag, x.err);
+        const bool beside = biased && prefix > 0;  // rows of later positions may be seen
+        xt_wait(bar(2 + wg), (uint32_t)(g & 1), abort_flag, x.err);
         tc5::fence_after_sync();
         uint64_t sum2[2] = {0ull, 0ull};
 #pragma unroll 1
-        for (int hb = 0; hb < 64; hb += 32) {
+        for (int hb = 0; hb < rows; hb += 32) {
           uint32_t sv[32];
-          tc5::tmem_ld32(t_row + 64u * (uint32_t)(g & 1) + (uint32_t)hb, sv);
+          tc5::tmem_ld32(t_row + (uint32_t)hb, sv);
           tc5::tmem_wait_ld();
-          if (hb == 32) {  // both halves have been read: the buffer may be written again
+          if (hb + 32 >= rows) {  // all has been read: S may be written again
             tc5::fence_before_sync();
-            mbar_arrive(bar(7 + 2 * wg + (g & 1)));
+            mbar_arrive(bar(4 + wg));
           }
           float scale = p.scale_log2;
           if constexpr (MODS) {
@@ -1220,8 +1216,10 @@ extend_mass_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_con
               float4 add = lds_f4(s_add + 4u * (uint32_t)(hb + c));
               if constexpr (MODS) {
                 // (the bias of column c: - slope_c (off0 + token_c); the token's part is in s_add)
-                const float4 ns = lds_f4(s_slope + 4u * (uint32_t)(hb + c));
-                if (beside) {
+                float4 ns = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (biased) ns = lds_f4(s_slope + 4u * (uint32_t)(hb + c));
+                if (!biased) {
+                } else if (beside) {
                   const float4 tk = lds_f4(s_token + 4u * (uint32_t)(hb + c));
                   add.x += ns.x * (fabsf(off0 + tk.x) - tk.x);
                   add.y += ns.y * (fabsf(off0 + tk.y) - tk.y);
