@@ -1542,8 +1542,8 @@ dynts_status_t launch_extend_tc_as(dynts_cache* c, dynts::ExtendTcParams& p, uns
   return DYNTS_OK;
 }
 
-constexpr int kExtendMinTiles = 3;  // key tiles per CTA below which the grid shrinks
-constexpr int kExtendItemTiles = 4;  // an item's beginning and end take about so many key tiles' time
+constexpr int kExtendMinTiles = 4;  // key tiles per CTA below which the grid shrinks (5 tokens behind 2048 rows: 33 us at 1, 25 at 3, 23 at 4 and 6)
+constexpr int kExtendItemTiles = 4;  // an item's beginning and end take about so many key tiles' time (packed prompts: 146 us at 2, 121 at 4 and 6)
 
 // The list of key tiles and its shares (see ExtendPlan); *grid: CTAs of the tensor-core kernel.
 dynts_status_t plan_extend(const dynts_cache* c, const dynts::ExtendParams& x, const ExtendScratch& m, char* scratch, dynts::ExtendPlan& p, unsigned* grid) {

@@ -282,7 +282,8 @@ __device__ __forceinline__ float xt_add_log2(float x, float sum) {
 // Joins the parts of the item that begins in CTA blockIdx.x's shares and ends behind them, if there is one: 32 rows per
 // block (y), a warp 8 rows x 64 columns, a thread four pieces of four columns of one row.  A part's 128-byte pieces
 // are read whole, the output's sectors written whole.  Running maximum and sum over the parts, in the order of the
-// list: bound by the latency of three loads (the plan, the list, then the parts, two at once).
+// list: bound by the latency of three loads (the plan, the list, then the parts, four at once).
+constexpr int kXtJoin = 4;
 __global__ void __launch_bounds__(256) extend_join_kernel(const __grid_constant__ ExtendTcParams p) {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const ExtendParams& x = p.x;
@@ -303,24 +304,32 @@ __global__ void __launch_bounds__(256) extend_join_kernel(const __grid_constant_
   float M = -CUDART_INF_F, sum = 0.f, acc[16];
 #pragma unroll
   for (int e = 0; e < 16; ++e) acc[e] = 0.f;
-#pragma unroll 2
-  for (int k = 0; k < n_parts; ++k) {
+#pragma unroll 1
+  for (int k = 0; k < n_parts; k += kXtJoin) {
     if (k > 0 && (k & 31) == 0) places = k + lane < n_parts ? __ldcg(list + (size_t)(k + lane) * kPlanWords) : 0;
-    const float* src = p.part + (size_t)__shfl_sync(0xffffffffu, places, k & 31) * (piece * kXtPartFloats);
-    const float lk = __ldcg(src + 128 * piece + rr);
-    float4 y[4];
+    float lk[kXtJoin];
+    float4 y[kXtJoin][4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) y[e] = __ldcg(reinterpret_cast<const float4*>(src) + (size_t)(c4 + 4 * e) * piece + rr);
-    const float Mn = fmaxf(M, lk);
-    const float keep = M == -CUDART_INF_F ? 0.f : fast_exp2(M - Mn), w = lk == -CUDART_INF_F ? 0.f : fast_exp2(lk - Mn);
-    M = Mn;
-    sum = fmaf(sum, keep, w);
+    for (int u = 0; u < kXtJoin; ++u) {  // (behind the last part: the last again, without weight)
+      const float* src = p.part + (size_t)__shfl_sync(0xffffffffu, places, min(k + u, n_parts - 1) & 31) * (piece * kXtPartFloats);
+      lk[u] = __ldcg(src + 128 * piece + rr);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      acc[4 * e] = fmaf(acc[4 * e], keep, w * y[e].x);
-      acc[4 * e + 1] = fmaf(acc[4 * e + 1], keep, w * y[e].y);
-      acc[4 * e + 2] = fmaf(acc[4 * e + 2], keep, w * y[e].z);
-      acc[4 * e + 3] = fmaf(acc[4 * e + 3], keep, w * y[e].w);
+      for (int e = 0; e < 4; ++e) y[u][e] = __ldcg(reinterpret_cast<const float4*>(src) + (size_t)(c4 + 4 * e) * piece + rr);
+    }
+#pragma unroll
+    for (int u = 0; u < kXtJoin; ++u) {
+      if (k + u >= n_parts) break;
+      const float Mn = fmaxf(M, lk[u]);
+      const float keep = M == -CUDART_INF_F ? 0.f : fast_exp2(M - Mn), w = lk[u] == -CUDART_INF_F ? 0.f : fast_exp2(lk[u] - Mn);
+      M = Mn;
+      sum = fmaf(sum, keep, w);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        acc[4 * e] = fmaf(acc[4 * e], keep, w * y[u][e].x);
+        acc[4 * e + 1] = fmaf(acc[4 * e + 1], keep, w * y[u][e].y);
+        acc[4 * e + 2] = fmaf(acc[4 * e + 2], keep, w * y[u][e].z);
+        acc[4 * e + 3] = fmaf(acc[4 * e + 3], keep, w * y[u][e].w);
+      }
     }
   }
   if (row >= rows) return;
