@@ -721,8 +721,10 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
       const int r = min(wq * 32 + lane, rows - 1);  // (a lane without a query repeats the last row's visibility)
       const int ti = i0 + r / x.G;
       const int lim = held + max(ti + 1, prefix);   // rows [0, lim) are visible
-      // Tiles that some token of the query tile does not see whole: all of them, and one more, are the first group's.
-      const int ramp = min(nkt, max(0, kt_new - (held + max(i0 + 1, prefix) - 1) / kPfKeys) + 1);
+      // Tiles that some token of the query tile does not see whole, and one more, are the first group's: after them every row
+      // that sees anything has its reference.  (With a window a token of a prefix may see only rows around its own: down to those.)
+      const int whole_to = held + (MODS && x.window > 0 ? i0 : max(i0 + 1, prefix) - 1);
+      const int ramp = min(nkt, max(0, kt_new - whole_to / kPfKeys) + 1);
       const int* pos_row = nullptr;
       int tot = 0;
       float slope = 0.f;
