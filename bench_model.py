@@ -15,6 +15,10 @@ attention-flop ratio.
 
     python bench_model.py [--tokens 4096] [--budget 3072] [--out model_loop.json]
 
+`--turn T` adds a second question: after the run, T further prompt tokens per sequence go through the
+model as one chunk (dynts_rope, dynts_extend_attn_layer) behind the rows each arm holds, and the time
+to its first answer token is reported.
+
 `--late-state` instead times 128 steps in the state a 16384-token decode reaches, the caches
 filled with seeded synthetic K/V rows (no trajectory, no evictions falling due).
 
@@ -95,6 +99,25 @@ class Model:
             x = x + (torch.nn.functional.silu(h @ w["wg"].T) * (h @ w["wu"].T)) @ w["wd"].T
         logits = self.rms(x[:, -1], self.nf) @ self.head.T
         return logits.argmax(-1)
+
+    def turn(self, prompt, start, cache):
+        """A further question [Nb, T] behind what the cache holds, its first token at position `start`: returns the first
+        token of every answer."""
+        import paper_2601_18383_b200 as Dn
+        Nb, T = prompt.shape
+        x = self.embed[prompt.reshape(-1)]                                   # [Nb T, HID]
+        pos = (start + torch.arange(T, device=x.device, dtype=torch.int32)).repeat(Nb)
+        n_new = torch.full((Nb,), T, dtype=torch.int32)
+        out = torch.empty((Nb * T, HQ, D), dtype=torch.bfloat16, device=x.device)
+        for l, w in enumerate(self.layers):
+            h = self.rms(x, w["n1"])
+            q, k, v = ((h @ w[n].T).view(Nb * T, -1, D) for n in ("wq", "wk", "wv"))
+            Dn.rope(q, k, pos, q, k, theta=THETA)
+            cache.extend_attn_layer(l, q, k, v, out, n_new)
+            x = x + out.view(Nb * T, HQ * D) @ w["wo"].T
+            h = self.rms(x, w["n2"])
+            x = x + (torch.nn.functional.silu(h @ w["wg"].T) * (h @ w["wu"].T)) @ w["wd"].T
+        return (self.rms(x.view(Nb, T, HID)[:, -1], self.nf) @ self.head.T).argmax(-1)
 
     def step(self, tokens, pos, cache, out_buf, attn_events=None):
         Nb = tokens.shape[0]
@@ -198,9 +221,9 @@ def run_trajectory(model, args, limited, device):
     import paper_2601_18383_b200 as Dn
     batch, M, E, B = args.batch, args.prompt, args.interval, args.budget
     if limited:
-        budget, cap = B, B + E
+        budget, cap = B, B + E + args.turn
     else:
-        cap = (M + args.tokens + 48 + 31) // 32 * 32
+        cap = (M + args.tokens + 48 + args.turn + 31) // 32 * 32
         budget = cap
     cache = Dn.Cache(L, batch, HQ, HKV, D, budget, args.window, E, dtype="bf16", capacity=cap, device=device)
     g = torch.Generator(device=device).manual_seed(11)
@@ -263,6 +286,20 @@ def run_trajectory(model, args, limited, device):
     total_ms = evict_ms_total + sum(ms * (d - (chunks[i - 1][0] if i else 1)) for i, (d, _, _, ms) in enumerate(chunks))
     tail = [(d, ms) for d, _, _, ms in chunks if d > args.tokens - 512]
     tail_ms = sum(ms for _, ms in tail) / max(1, len(tail))
+    turn = None
+    if args.turn:
+        question = torch.randint(0, VOCAB, (batch, args.turn), generator=g, device=device)
+        held = cache.len(0)
+        a, b = ev(), ev()
+        a.record()
+        model.turn(question, M + args.tokens, cache)
+        b.record()
+        torch.cuda.synchronize(device)
+        cache.poll_error()
+        assert cache.len(0) == held + args.turn
+        turn = {"tokens": args.turn, "rows_before": int(held), "ms_to_first_token": round(a.elapsed_time(b), 2)}
+        if limited:
+            cache.evict(0)
     # attention alone at the end of the run: the 32 layer calls of a step on fixed q, k, v
     gq = torch.Generator(device=device).manual_seed(5)
     aq = torch.randn((batch, HQ, D), generator=gq, device=device).to(torch.bfloat16)
@@ -290,6 +327,8 @@ def run_trajectory(model, args, limited, device):
            "rows_at_end": chunks[-1][2], "peak_rows_per_slab": int(peak_rows), "peak_kv_bytes": int(batch * peak_rows * kv_row_bytes),
            "allocated_cache_bytes": int(cache.nbytes), "lengths_match_closed_form": bool(ok),
            "evictions": sum(1 for _, r, a2, _ in chunks if a2 < r), "eviction_ms_total": round(evict_ms_total, 3)}
+    if turn:
+        res["second_question"] = turn
     series = [{"step": d, "rows": r, "rows_after_eviction": a2, "ms_per_step": round(ms, 4)} for d, r, a2, ms in chunks]
     cache.close()
     torch.cuda.empty_cache()
@@ -324,6 +363,7 @@ def main():
     ap.add_argument("--tokens", type=int, default=4096, help="tokens decoded per sequence in the default (trajectory) mode")
     ap.add_argument("--prompt", type=int, default=256)
     ap.add_argument("--out", default="", help="also write the summary and the per-chunk series to this JSON file")
+    ap.add_argument("--turn", type=int, default=0, help="tokens per sequence of a second question after the run (0: none)")
     ap.add_argument("--late-state", action="store_true", help="time --steps steps in the late-decode state on synthetic K/V fills")
     ap.add_argument("--batch", type=int, default=8)
     ap.add_argument("--steps", type=int, default=128)

@@ -131,5 +131,31 @@ class PresetRun:
         if c.len(0) < before:
             self.events += 1
 
+    def extend(self, q, k, v, out, predictor_scores=None, random_scores=None, **options):
+        """Known tokens as a chunk instead of one step each: the next question of a conversation, a text put in front.
+
+        q, out [L, Nb, T, Hq, d], k, v [L, Nb, T, Hkv, d], scores [Nb, T]; options as of `Cache.extend_attn` (softcap,
+        slopes, window).  The chunk is cut where the row count reaches the budget, and a selection follows each piece, so
+        the rows held and the events are those of T steps."""
+        c, p = self.cache, self.preset
+        T = q.shape[2]
+        scores = p.step_scores(predictor_scores, random_scores)
+        first = 0
+        while first < T:
+            held = max(c.len(b) for b in range(c.batch))
+            t = min(T - first, max(1, p.budget - held))
+            part = lambda x: x[:, :, first:first + t].reshape(c.layers, c.batch * t, x.shape[3], x.shape[4])
+            whole = t == T and out.is_contiguous()
+            o = part(out) if whole else c.torch.empty_like(part(q))
+            s = None if scores is None else scores[:, first:first + t].float().reshape(-1).contiguous()
+            c.extend_attn(part(q), part(k), part(v), o, [t] * c.batch, s_new=s, **options)
+            if not whole:
+                out[:, :, first:first + t].copy_(o.view(c.layers, c.batch, t, *o.shape[2:]))
+            before = c.len(0)
+            c.evict_at_budget(p.budget, p.ratio)
+            if c.len(0) < before:
+                self.events += 1
+            first += t
+
     def close(self):
         self.cache.close()
