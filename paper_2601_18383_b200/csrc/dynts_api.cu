@@ -1521,7 +1521,7 @@ dynts_status_t extend_maps(dynts_cache* c) {
 }
 
 template <bool KV8, bool MODS>
-dynts_status_t launch_extend_tc_as(dynts_cache* c, dynts::ExtendTcParams& p, unsigned grid, const CUtensorMap& mq, bool want_mass) {
+dynts_status_t launch_extend_tc_as(dynts_cache* c, dynts::ExtendTcParams& p, unsigned grid, bool whole, const CUtensorMap& mq, bool want_mass) {
   bool* attr = &c->attr_extend_tc[KV8 ? 1 : 0][MODS ? 1 : 0];
   if (!*attr) {
     CUDA_TRY(cudaFuncSetAttribute(dynts::extend_tc_kernel<KV8, MODS>, cudaFuncAttributeMaxDynamicSharedMemorySize, dynts::kXtSmemBytes));
@@ -1530,7 +1530,7 @@ dynts_status_t launch_extend_tc_as(dynts_cache* c, dynts::ExtendTcParams& p, uns
   }
   CUDA_TRY(launch_dependent(dynts::extend_tc_kernel<KV8, MODS>, dim3(grid, 1, 1), (unsigned)dynts::XtShape<KV8, MODS>::kThreads, dynts::kXtSmemBytes, c->stream, p, mq, c->map_XK, c->map_XV));
   c->launches += 1;
-  if (grid > 1) {  // items that lie across CTAs
+  if (!whole && grid > 1) {  // items that lie across CTAs
     CUDA_TRY(launch_dependent(dynts::extend_join_kernel, dim3(grid - 1, (unsigned)((p.part_rows + 31) / 32), 1), 256, 0, c->stream, p));
     c->launches += 1;
   }
@@ -1542,32 +1542,58 @@ dynts_status_t launch_extend_tc_as(dynts_cache* c, dynts::ExtendTcParams& p, uns
   return DYNTS_OK;
 }
 
-constexpr int kExtendMinTiles = 4;  // key tiles per CTA below which the grid shrinks (5 tokens behind 2048 rows: 33 us at 1, 25 at 3, 23 at 4 and 6)
-constexpr int kExtendItemTiles = 4;  // an item's beginning and end take about so many key tiles' time (packed prompts: 146 us at 2, 121 at 4 and 6)
+// How the tensor-core kernel's work is cut, in units of a key tile's time (0.7 us for a CTA alone, 1.1 us under load).
+// An item's beginning and end take about seven.  Cut anywhere (equal shares of all key tiles), a CTA begins and ends items that
+// others share and a second kernel joins them: another six, and up to twelve more where every CTA writes parts of 128 rows.
+// Whole items need no join but leave CTAs with unequal work.  Measured (8 KV heads, groups of four; us, cut / whole):
+// 1 token, 8 items of 8 tiles 15.6 / 14.6, of 16 tiles 16.9 / 20.0; 20 tokens in each of 33 sequences, 264 items of 16 tiles
+// 51.5 / 40.3; 70 in each of 16, 384 items of 9 tiles 47.3 / 40.8, of 17 tiles 57.7 / 58.3; prompts of 33 to 1100 tokens, 1528
+// items 122 / 106.
+constexpr double kExtendItemCost = 7, kExtendJoinCost = 6, kExtendPartCost = 12;
+constexpr int kExtendMinTiles = 4;   // key tiles per CTA below which the grid shrinks, if items are cut
+constexpr int kExtendItemTiles = 4;  // what an item counts beside its key tiles in the shares (packed prompts, cut: 146 us at 2, 121 at 4 and 6)
 
-// The list of key tiles and its shares (see ExtendPlan); *grid: CTAs of the tensor-core kernel.
-dynts_status_t plan_extend(const dynts_cache* c, const dynts::ExtendParams& x, const ExtendScratch& m, char* scratch, dynts::ExtendPlan& p, unsigned* grid) {
+// The list of key tiles and its shares (see ExtendPlan); *grid: CTAs of the tensor-core kernel; *whole: no item is cut.
+dynts_status_t plan_extend(const dynts_cache* c, const dynts::ExtendParams& x, const ExtendScratch& m, char* scratch, dynts::ExtendPlan& p, unsigned* grid, bool* whole) {
   const int n_seq = x.seqs.n, tpt = dynts::kXtRows / c->G;
   p.tokens_per_tile = tpt;
   p.lh = x.n_layers * x.Hkv;
   p.words = reinterpret_cast<int*>(scratch + m.plan);
-  long long key_tiles = 0, shares = 0, items = 0;
+  long long key_tiles = 0, shares = 0, items = 0, rows_all = 0, most = 0;
   for (int s = 0; s < n_seq; ++s) {
     const int t = x.seqs.tok0[s + 1] - x.seqs.tok0[s];
     p.tiles[s] = (t + tpt - 1) / tpt;
     // The key tiles of an item, on average over the chunk.  (The host's copy of the lengths only guides the cut: the
     // kernels go by the device's.)
-    long long rows = c->len_h[x.seqs.b0 + s] + std::max((t + 1) / 2, x.seqs.prefix[s]);
-    if (x.window > 0) rows = std::min<long long>(rows, (long long)x.window + tpt + dynts::kPfKeys);
+    long long rows = c->len_h[x.seqs.b0 + s] + std::max((t + 1) / 2, x.seqs.prefix[s]), full = c->len_h[x.seqs.b0 + s] + t;
+    if (x.window > 0) {
+      const long long seen = (long long)x.window + tpt + dynts::kPfKeys;
+      rows = std::min(rows, seen);
+      full = std::min(full, seen);
+    }
     const long long n = std::max<long long>(1, (rows + dynts::kPfKeys - 1) / dynts::kPfKeys), mine = (long long)p.tiles[s] * p.lh;
     p.item0[s] = (int)items;
     items += mine;
+    rows_all += (long long)t * c->G * p.lh;
+    most = std::max(most, mine > 0 ? (full + dynts::kPfKeys - 1) / dynts::kPfKeys : 0);
     if (items >= (1ll << 30)) return fail(DYNTS_ERR_INVALID_ARG, "%lld work items are beyond the launch limits", items);
     p.per[s] = (unsigned)(n + kExtendItemTiles);
     key_tiles += mine * n;
     shares += mine * (n + kExtendItemTiles);
   }
   p.item0[n_seq] = (int)items;
+  {
+    const double avg = (double)key_tiles / items, per_item = kExtendItemCost + avg;
+    const double cut = (double)std::max<long long>(1, std::min<long long>(m.ctas, key_tiles / kExtendMinTiles));
+    const double t_cut = std::max(items * per_item / cut, kExtendItemCost + kExtendMinTiles) + kExtendJoinCost +
+                         kExtendPartCost * rows_all / (items * (double)dynts::kXtRows) * cut / m.ctas;
+    const double t_whole = (items + m.ctas - 1) / m.ctas * per_item + 0.5 * (most - avg);
+    *whole = t_whole <= t_cut;
+  }
+  if (*whole) {
+    shares = items;
+    for (int s = 0; s < n_seq; ++s) p.per[s] = 1;
+  }
   unsigned coarse = 1;  // shares are counted in 32 bits: very large calls count several key tiles as one
   while (shares / coarse >= (1ll << 30)) coarse *= 2;
   long long sum = 0;
@@ -1579,13 +1605,13 @@ dynts_status_t plan_extend(const dynts_cache* c, const dynts::ExtendParams& x, c
   }
   p.cum[n_seq] = (unsigned)sum;
   // Two CTAs per SM, with at least a few key tiles each.
-  *grid = (unsigned)std::max<long long>(1, std::min<long long>(std::min<long long>(m.ctas, sum), key_tiles / kExtendMinTiles));
+  *grid = (unsigned)std::max<long long>(1, std::min<long long>(std::min<long long>(m.ctas, sum), *whole ? sum : key_tiles / kExtendMinTiles));
   p.share_q = (unsigned)(sum / *grid);
   p.share_rem = (unsigned)(sum % *grid);
   return DYNTS_OK;
 }
 
-dynts_status_t launch_extend_tc(dynts_cache* c, const dynts::ExtendParams& x, const dynts::ExtendPlan& plan, unsigned grid, const ExtendScratch& m, char* scratch,
+dynts_status_t launch_extend_tc(dynts_cache* c, const dynts::ExtendParams& x, const dynts::ExtendPlan& plan, unsigned grid, bool whole, const ExtendScratch& m, char* scratch,
                                 bool want_mass) {
   dynts::ExtendTcParams p;
   p.x = x;
@@ -1636,8 +1662,8 @@ dynts_status_t launch_extend_tc(dynts_cache* c, const dynts::ExtendParams& x, co
   if (r != CUDA_SUCCESS) return fail(DYNTS_ERR_CUDA, "cuTensorMapEncodeTiled failed (%d)", (int)r);
   const bool mods = x.cap_logit > 0.f || x.slopes || x.window > 0;
   if (kv8)
-    return mods ? launch_extend_tc_as<true, true>(c, p, grid, map, want_mass) : launch_extend_tc_as<true, false>(c, p, grid, map, want_mass);
-  return mods ? launch_extend_tc_as<false, true>(c, p, grid, map, want_mass) : launch_extend_tc_as<false, false>(c, p, grid, map, want_mass);
+    return mods ? launch_extend_tc_as<true, true>(c, p, grid, whole, map, want_mass) : launch_extend_tc_as<true, false>(c, p, grid, whole, map, want_mass);
+  return mods ? launch_extend_tc_as<false, true>(c, p, grid, whole, map, want_mass) : launch_extend_tc_as<false, false>(c, p, grid, whole, map, want_mass);
 }
 
 dynts_status_t launch_extend(dynts_cache* c, int layer0, int n_layers, const ExtendCall& a, long long total, bool publish) {
@@ -1723,8 +1749,9 @@ dynts_status_t launch_extend(dynts_cache* c, int layer0, int n_layers, const Ext
     dynts::ExtendPlan plan;
     plan.words = nullptr;
     unsigned tc_grid = 0;
+    bool whole = false;
     if (tc) {
-      dynts_status_t st = plan_extend(c, p, m, a.scratch, plan, &tc_grid);
+      dynts_status_t st = plan_extend(c, p, m, a.scratch, plan, &tc_grid, &whole);
       if (st != DYNTS_OK) return st;
     }
     CUDA_TRY(launch_dependent(kv8                      ? dynts::extend_store_kernel<__nv_bfloat16, true>
@@ -1733,7 +1760,7 @@ dynts_status_t launch_extend(dynts_cache* c, int layer0, int n_layers, const Ext
                               grid, 256, 0, c->stream, p, plan));
     c->launches += 1;
     p.published = p.publish;
-    dynts_status_t st = tc ? launch_extend_tc(c, p, plan, tc_grid, m, a.scratch, want_mass)
+    dynts_status_t st = tc ? launch_extend_tc(c, p, plan, tc_grid, whole, m, a.scratch, want_mass)
                         : kv8 ? launch_extend_generic<__nv_bfloat16, true>(c, p, want_mass)
                         : f.dtype == DYNTS_FP32 ? launch_extend_generic<float, false>(c, p, want_mass)
                                                 : launch_extend_generic<__nv_bfloat16, false>(c, p, want_mass);
