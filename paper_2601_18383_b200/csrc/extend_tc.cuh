@@ -7,7 +7,8 @@
 // contiguous piece: few tokens behind a long cache, many ragged sequences and a whole prompt are cut alike.
 // An item that lies across CTAs is computed in parts side by side; each part leaves its normalised output and
 // log-sum-exp in the scratch, and extend_join_kernel joins them in the order of the list.  (The last part to finish
-// joined them at first: one CTA then read all parts of its items, up to 20 us after the others had ended.)
+// joined them at first: one CTA then read all parts of its items, up to 20 us after the others had ended.)  Where the
+// join would cost more than it evens out, the pieces are whole items (the host's plan says which; it has the figures).
 // Two CTAs per SM; per 64 keys
 //     S  = Q K^T      M 128 x N 64 x K 128     operands from shared memory
 //     P  = exp2(S * scale - ref)               softmax warps, thread = query row = tensor-memory lane
@@ -29,7 +30,11 @@
 // walks the CTA's pieces by the plan the storing kernel wrote (extend.cuh), a word per lane, the next piece's
 // prefetched.  Two CTAs of 384 threads leave 80 registers per thread and hardly any L1: code that spills or does
 // not stay in the instruction caches cost several times its instructions, so the loops are rolled and the end of a piece
-// is a function of its own (4096 tokens behind 4096 rows: 453 us with cursors in registers and everything unrolled).
+// is a function of its own (4096 tokens behind 4096 rows: 453 us with cursors in registers and everything unrolled,
+// 388 us now: 1.06 PFLOP/s, 0.66 of what cuBLAS reaches.  The tensor cores and the exponentials' unit are each busy for
+// half of that time, in turns that the chain of a tile does not let overlap further: tiles of 128 keys with one S buffer,
+// or P over another CTA's wait, measured 390 to 400 us.)  Short items are bound by their own chain, about 7 us from the
+// load of Q to the store of the output, two of them per SM at a time.
 //
 // Rows of 16 bits arrive by TMA from the slabs.  8-bit rows (KV8) are read as codes and widened into the same swizzled
 // tiles: K to f16 (exact; queries are an f16 copy made by the storing kernel) by the two loading warps, a tile ahead in
