@@ -276,7 +276,9 @@ typedef struct dynts_extend_opts {
  *                  caller-owned; contents need not be preserved between calls.  Calls that may overlap
  *                  on the GPU (two caches, two captured graphs) need one each.
  * Types as the cache's; with 8-bit rows the chunk's rows are encoded first and read as stored, as in a
- * decode step.  DYNTS_ERR_CAPACITY if a sequence would outgrow its slab.  Nothing behind the last token
+ * decode step, and at head_dim 128 the queries are held in f16 (exact for magnitudes from 2^-14 to 65504;
+ * larger ones give no numbers).  head_dim 128 with bf16 or 8-bit rows runs on the tensor cores, with the
+ * weights rounded to bf16, any other shape in fp32; dynts_cache_set_launch variant 1 takes the latter for all.  DYNTS_ERR_CAPACITY if a sequence would outgrow its slab.  Nothing behind the last token
  * of out is written.  May be captured into a graph: the rows held are read from the device at replay
  * (n_new, prefix and the options are those of the capture), and as for decode steps the host's copy
  * of the lengths does not follow replays. */
