@@ -236,7 +236,7 @@ dynts_status_t dynts_cache_set_kv_scale(dynts_cache_t* c, float k_scale, float v
  * token i of a sequence that held n rows attends to rows [0, n + i], its own row included.
  *
  * The options, all off when zero (opts == NULL: all off):
- *   softcap   c > 0: a logit x = q.k / sqrt(d) becomes c tanh(x / c)
+ *   softcap   c > 0 (from 1e-20 to 1e20): a logit x = q.k / sqrt(d) becomes c tanh(x / c)
  *   slopes    device [Hq] fp32: slopes[h] * |p_i - p_j| is subtracted from the (capped) logit.  p are
  *             the rows' positions, counted in tokens seen: rows that survived an eviction keep theirs
  *   window    w > 0: only rows with |p_i - p_j| < w are seen (positions ascend with the rows, as every
@@ -301,7 +301,8 @@ dynts_status_t dynts_extend_commit(dynts_cache_t* c, const int* n_accept);
  * stores keys as given).  Pair i (0 <= i < rot_dim / 2) of a head turns by pos[axis(i)][t] *
  * theta^(-2 i / rot_dim); the columns behind rot_dim pass through.
  *   q, q_out: device [n_tokens, q_heads, head_dim];  k, k_out: device [n_tokens, kv_heads, head_dim], or
- *   k NULL: the queries alone.  bf16 or fp32 (dtype), rounded once.  In place (q_out == q with the same
+ *   k NULL: the queries alone.  bf16 or fp32 (dtype), rounded once; head_dim even, at most 256; 16-byte
+ *   aligned pointers.  In place (q_out == q with the same
  *   stride) is allowed, any other overlap is not.
  *   pos: device [n_axes][n_tokens] int32;  sections: host [n_axes], pairs of each axis (sum rot_dim / 2),
  *   or NULL for one axis.  The axes take their pairs in blocks, or with DYNTS_ROPE_ROUND_ROBIN in turn

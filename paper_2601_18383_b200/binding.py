@@ -487,7 +487,7 @@ class Cache:
             base = self.storage.data_ptr()
             cfg.storage = (base + 255) // 256 * 256
             cfg.storage_bytes = nbytes
-            cfg.stream = torch.cuda.current_stream(self.device).cuda_stream
+            cfg.stream = self._stream = torch.cuda.current_stream(self.device).cuda_stream
             self.handle = dynts_cache_create_ex(cfg)
         self.nbytes = nbytes
         self.capacity = dynts_cache_capacity(self.handle)
@@ -576,8 +576,11 @@ class Cache:
                                    None if mass is None else mass.data_ptr(), 1 if stage else 0, *strides)
         need = lib.dynts_extend_scratch_bytes(self.handle, counts, layers if layer is None else 1)
         if need > self._scratch_bytes:
-            # (a piece is never given back before the cache: the stream and captured graphs may still use it)
-            self._scratch.append(t.torch.empty(max(need, 2 * self._scratch_bytes), dtype=t.torch.uint8, device=self.device))
+            # (a piece is never given back before the cache: the stream and captured graphs may still use it.  It comes from the
+            # allocator's memory of the stream that will use it: another stream's may still be busy with what lay there.)
+            with t.torch.cuda.stream(t.torch.cuda.ExternalStream(self._stream, device=self.device) if self._stream
+                                     else t.torch.cuda.default_stream(self.device)):
+                self._scratch.append(t.torch.empty(max(need, 2 * self._scratch_bytes), dtype=t.torch.uint8, device=self.device))
             self._scratch_ptr, self._scratch_bytes = self._scratch[-1].data_ptr(), self._scratch[-1].numel()
         args = (q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), counts, C.byref(opts), self._scratch_ptr, self._scratch_bytes)
         if t.device() != dev:
@@ -634,7 +637,10 @@ class Cache:
         return dynts_cache_set_evict_launch(self.handle, split)
 
     def set_stream(self, stream):
-        return dynts_cache_set_stream(self.handle, stream.cuda_stream if hasattr(stream, "cuda_stream") else stream)
+        handle = stream.cuda_stream if hasattr(stream, "cuda_stream") else stream
+        dynts_cache_set_stream(self.handle, handle)
+        self._stream = handle or 0
+        return DYNTS_OK
 
     def synchronize(self):
         return dynts_synchronize(self.handle)

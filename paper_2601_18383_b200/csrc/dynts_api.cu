@@ -1411,7 +1411,8 @@ dynts_status_t check_extend(const dynts_cache* c, const ExtendCall& a, int n_lay
     if ((long long)held + a.n_new[b] > cap)
       return fail(DYNTS_ERR_CAPACITY, "sequence %d: %d rows and %d new tokens exceed the capacity %d", b, held, a.n_new[b], cap);
   }
-  if (!(a.o.softcap >= 0.f) || std::isinf(a.o.softcap)) return fail(DYNTS_ERR_INVALID_ARG, "softcap must be 0 or positive and finite");
+  if (!(a.o.softcap == 0.f || (a.o.softcap >= 1e-20f && a.o.softcap <= 1e20f)))  // (its reciprocal and squares stay in range)
+    return fail(DYNTS_ERR_INVALID_ARG, "softcap must be 0 or from 1e-20 to 1e20");
   if (a.o.window < 0) return fail(DYNTS_ERR_INVALID_ARG, "window must not be negative");
   if (a.o.stage != 0 && a.o.stage != 1) return fail(DYNTS_ERR_INVALID_ARG, "stage must be 0 or 1");
   const long long per16 = 16 / elt_bytes_of(f.dtype);
@@ -1881,7 +1882,7 @@ dynts_status_t dynts_extend_commit(dynts_cache_t* c, const int* n_accept) {
 dynts_status_t dynts_rope(const void* q, const void* k, const int* pos, void* q_out, void* k_out, int n_tokens, int q_heads, int kv_heads,
                           int head_dim, int rot_dim, int n_axes, const int* sections, int flags, double theta, int dtype,
                           const long long* strides, void* stream) {
-  if (n_tokens < 0 || q_heads < 1 || kv_heads < 0 || head_dim < 2 || head_dim > 256)
+  if (n_tokens < 0 || q_heads < 1 || q_heads > 65535 || kv_heads < 0 || kv_heads > 65535 || head_dim < 2 || head_dim % 2 || head_dim > 256)
     return fail(DYNTS_ERR_INVALID_ARG, "bad shape: %d tokens, %d / %d heads of %d", n_tokens, q_heads, kv_heads, head_dim);
   if (rot_dim < 2 || rot_dim % 2 || rot_dim > head_dim) return fail(DYNTS_ERR_INVALID_ARG, "rot_dim %d must be even and at most head_dim", rot_dim);
   if (n_axes < 1 || n_axes > dynts::kRopeMaxAxes) return fail(DYNTS_ERR_INVALID_ARG, "1 to %d axes", dynts::kRopeMaxAxes);
@@ -1913,6 +1914,8 @@ dynts_status_t dynts_rope(const void* q, const void* k, const int* pos, void* q_
   p.ko_stride = strides && strides[3] ? strides[3] : kd;
   if (p.q_stride < qd || p.qo_stride < qd || p.k_stride < kd || p.ko_stride < kd)
     return fail(DYNTS_ERR_INVALID_ARG, "token strides must cover a token");
+  if ((q_out == q && p.qo_stride != p.q_stride) || (with_k && k_out == k && p.ko_stride != p.k_stride))
+    return fail(DYNTS_ERR_INVALID_ARG, "in place, a tensor keeps its token stride");
   p.q = q;
   p.k = with_k ? k : nullptr;
   p.q_out = q_out;

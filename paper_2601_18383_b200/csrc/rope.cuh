@@ -1,8 +1,10 @@
 // Rotary positions with one or several axes (time, height, width) on the queries and keys of a batch
 // of tokens.  Pair i of a head's first `rot` columns turns by the angle
 //     phi_i = pos[axis(i)] * theta^(-2 i / rot),      (a, b) -> (a cos phi - b sin phi, a sin phi + b cos phi)
-// Bound by the bytes of q and k, each read and written once in 16-byte pieces: a CTA computes the
-// cosines and sines of its tokens once, in shared memory, and applies them to all heads.  The angle
+// Bound by the bytes of q and k, each read and written once in 16-byte pieces (where sizes and strides are
+// multiples of 16 bytes; element by element otherwise): a CTA computes the cosines and sines of its tokens
+// once, in shared memory, and applies them to all heads.  16384 tokens of 32 + 8 heads of 128 in bf16: 59 us, 5.7 TB/s
+// (0.87 of a copy).  The angle
 // is formed in 64 bits as a number of revolutions and reduced before it is rounded to 32: at a
 // position of a million an fp32 product would be off by 0.06 rad.
 #pragma once
@@ -60,20 +62,24 @@ __device__ __forceinline__ int rope_axis(const RopeParams& p, int i) {
   }
 }
 
-template <typename T, int V>  // V elements at a time: 16 bytes, or one
+template <typename T, int V>  // V elements at a time: 16 bytes, else one after another (no alignment is asked of them)
 struct RopeVec {
   T x[V];
   __device__ __forceinline__ void load(const T* p) {
-    if constexpr (V * sizeof(T) == 16) *reinterpret_cast<uint4*>(x) = *reinterpret_cast<const uint4*>(p);
-    else if constexpr (V * sizeof(T) == 4) *reinterpret_cast<uint32_t*>(x) = *reinterpret_cast<const uint32_t*>(p);
-    else if constexpr (V * sizeof(T) == 8) *reinterpret_cast<uint2*>(x) = *reinterpret_cast<const uint2*>(p);
-    else x[0] = *p;
+    if constexpr (V * sizeof(T) == 16) {
+      *reinterpret_cast<uint4*>(x) = *reinterpret_cast<const uint4*>(p);
+    } else {
+#pragma unroll
+      for (int e = 0; e < V; ++e) x[e] = p[e];
+    }
   }
   __device__ __forceinline__ void store(T* p) const {
-    if constexpr (V * sizeof(T) == 16) *reinterpret_cast<uint4*>(p) = *reinterpret_cast<const uint4*>(x);
-    else if constexpr (V * sizeof(T) == 4) *reinterpret_cast<uint32_t*>(p) = *reinterpret_cast<const uint32_t*>(x);
-    else if constexpr (V * sizeof(T) == 8) *reinterpret_cast<uint2*>(p) = *reinterpret_cast<const uint2*>(x);
-    else *p = x[0];
+    if constexpr (V * sizeof(T) == 16) {
+      *reinterpret_cast<uint4*>(p) = *reinterpret_cast<const uint4*>(x);
+    } else {
+#pragma unroll
+      for (int e = 0; e < V; ++e) p[e] = x[e];
+    }
   }
 };
 

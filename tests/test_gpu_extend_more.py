@@ -166,3 +166,42 @@ def test_one_scratch_grows_with_the_calls():
     c.poll_error()
     assert all(torch.equal(x, y) for x, y in zip(outs[:4], outs[4:]))
     c.close()
+
+
+def test_scratch_of_another_stream_than_the_current():
+    """The cache works on a stream of its own while the current one is busy with memory it has given back."""
+    ref, _ = build(q_heads=8, kv_heads=2, past=(300,), cap=1024)
+    q, k, v = chunk(ref, [700], 19)
+    want, out = torch.empty_like(q), torch.empty_like(q)
+    ref.extend_attn(q, k, v, want, [700], stage=True)
+    c, _ = build(q_heads=8, kv_heads=2, past=(300,), cap=1024)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    c.set_stream(side)
+    x = torch.ones((4096, 4096), device="cuda")
+    for _ in range(20):
+        x = (x @ x).clamp(max=1.0)                                   # keeps the current stream busy ...
+    for n in (1 << 22, 1 << 23, 1 << 24):
+        y = torch.empty(n, dtype=torch.uint8, device="cuda")
+        y.fill_(255)                                                 # ... with writes to blocks it gives back at once
+        del y
+    c.extend_attn(q, k, v, out, [700], stage=True)
+    torch.cuda.synchronize()
+    c.poll_error()
+    assert torch.equal(out, want)
+    c.close(), ref.close()
+
+
+@pytest.mark.parametrize("d,rot,stride", [(10, 6, 25), (6, 2, 13), (130, 66, 131 * 2 + 1)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("adjacent", [False, True])
+def test_rotation_of_odd_strides(d, rot, stride, dtype, adjacent):
+    from tests.test_gpu_rope import plain, tolerance
+    n, heads = 37, 2
+    base = torch.randn(n * stride + d, device="cuda").to(dtype)
+    q = torch.as_strided(base, (n, heads, d), (stride, d, 1))
+    pos = torch.arange(n, device="cuda", dtype=torch.int32) * 977
+    out, _ = D.rope(q, None, pos, theta=5e3, rot_dim=rot, adjacent=adjacent)
+    want, raw = plain(q, pos[None], 5e3, [rot // 2], rot, adjacent, False)
+    assert ((out.double().cpu() - want).abs() <= tolerance(want, raw, dtype)).all()
+    assert torch.equal(out[..., rot:], q[..., rot:])
