@@ -404,7 +404,7 @@ def _invalid(message):
 def rope(q, k, positions, q_out=None, k_out=None, theta=10000.0, sections=None, rot_dim=None, adjacent=False, round_robin=False):
     """dynts_rope on torch tensors: q [n, Hq, d], k [n, Hkv, d] or None, positions int32 [n] or [axes, n].  The outputs are new
     tensors unless given (q_out=q, k_out=k: in place).  Rows of a token are contiguous, tokens may be strided.  Runs on torch's
-    current stream of q's device.  Returns (q_out, k_out)."""
+    current stream of q's device.  rot_dim: by default what the sections hold, all of d without them.  Returns (q_out, k_out)."""
     t = _torch()
     if q_out is None:
         q_out = t.torch.empty(q.shape, dtype=q.dtype, device=q.device)
@@ -441,9 +441,11 @@ def rope(q, k, positions, q_out=None, k_out=None, theta=10000.0, sections=None, 
         st = (C.c_longlong * 4)(q.stride(0), 0 if k is None else k.stride(0), q_out.stride(0), 0 if k is None else k_out.stride(0))
     if sections is not None:
         sec = (C.c_int * axes)(*sections)
+    if rot_dim is None:
+        rot_dim = d if sections is None else 2 * sum(sections)
     flags = (DYNTS_ROPE_ADJACENT if adjacent else 0) | (DYNTS_ROPE_ROUND_ROBIN if round_robin else 0)
     args = (q.data_ptr(), None if k is None else k.data_ptr(), positions.data_ptr(), q_out.data_ptr(), None if k is None else k_out.data_ptr(),
-            n, hq, hkv, d, d if rot_dim is None else rot_dim, axes, sec, flags, theta, dtype, st, t.stream(dev))
+            n, hq, hkv, d, rot_dim, axes, sec, flags, theta, dtype, st, t.stream(dev))
     if t.device() == dev:
         _check(lib.dynts_rope(*args))
     else:

@@ -550,18 +550,15 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
     for (; slot < slot_end && !*s_abort; go_next()) {
       ask_next();
       const int nkt = word(kPwTiles), kt_new = word(kPwFirst) + nkt - 1, slab = word(kPwSlab), end = word(kPwHeld) + word(kPwNew);
+      // 8-bit rows: this warp's 32 rows of a tile, eight at a time, each eight a whole tile ahead in registers
       XtCodes codes[4];
-      auto fetch = [&](int j) {  // 8-bit rows: this warp's 32 rows of the piece's tile j
-        const uint8_t* src = static_cast<const uint8_t*>(x.K) + (size_t)slab * x.cap * 128;
-        const int k0 = (kt_new - j) * kPfKeys + 32 * (warp & 1);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) xt_load_codes(codes[i], src, k0 + 8 * i, end, lane);
-        // (four tiles further on towards the older rows: asked into L2)
-        if (lane == 0 && j + 4 < nkt)
-          asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(src + (size_t)(k0 - 4 * kPfKeys) * 128), "r"(32 * 128) : "memory");
-      };
+      const uint8_t* src = KV8 ? static_cast<const uint8_t*>(x.K) + (size_t)slab * x.cap * 128 : nullptr;
+      const int sub = 32 * (warp & 1);
       if constexpr (KV8) {
-        if (nkt > 0) fetch(0);
+        if (nkt > 0) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) xt_load_codes(codes[i], src, kt_new * kPfKeys + sub + 8 * i, end, lane);
+        }
       }
       for (int j = 0; j < nkt; ++j, ++g) {
         // The piece's Q, once the last S of the piece before has been computed from its own; a K stage is filled again when
@@ -574,12 +571,18 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
         if (new_q) load_q();
         if constexpr (KV8) {
           uint8_t* tile = sm + kPfQBytes + (uint32_t)(g & 1) * kPfKvBytes;
+          const int k0 = (kt_new - j - 1) * kPfKeys + sub;
+          // (four tiles further on towards the older rows: asked into L2)
+          if (lane == 0 && j + 4 < nkt)
+            asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(src + (size_t)(k0 - 3 * kPfKeys) * 128), "r"(32 * 128) : "memory");
 #pragma unroll
-          for (int i = 0; i < 4; ++i) xt_store_codes<false>(codes[i], tile, kPfKvBytes / 2, 32 * (warp & 1) + 8 * i, lane);
+          for (int i = 0; i < 4; ++i) {
+            xt_store_codes<false>(codes[i], tile, kPfKvBytes / 2, sub + 8 * i, lane);
+            if (j + 1 < nkt) xt_load_codes(codes[i], src, k0 + 8 * i, end, lane);
+          }
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           __syncwarp();
           if (lane == 0) mbar_arrive(bar(1 + (g & 1)));
-          if (j + 1 < nkt) fetch(j + 1);
           __syncwarp();
         } else {
           load_tile(warp == 8, g, (kt_new - j) * kPfKeys, slab);

@@ -205,3 +205,11 @@ def test_rotation_of_odd_strides(d, rot, stride, dtype, adjacent):
     want, raw = plain(q, pos[None], 5e3, [rot // 2], rot, adjacent, False)
     assert ((out.double().cpu() - want).abs() <= tolerance(want, raw, dtype)).all()
     assert torch.equal(out[..., rot:], q[..., rot:])
+
+
+def test_the_sections_say_how_much_turns():
+    q = torch.randn((50, 3, 128), device="cuda")
+    pos = torch.arange(100, device="cuda", dtype=torch.int32).view(2, 50)
+    a, _ = D.rope(q, None, pos, sections=[20, 12])
+    b, _ = D.rope(q, None, pos, sections=[20, 12], rot_dim=64)
+    assert torch.equal(a, b) and torch.equal(a[..., 64:], q[..., 64:]) and not torch.equal(a[..., 32:64], q[..., 32:64])
