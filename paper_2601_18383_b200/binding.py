@@ -352,6 +352,7 @@ class _Torch:
     def __init__(self):
         import torch
         self.torch = torch
+        self.int32, self.float32 = torch.int32, torch.float32
         self.dtypes = {torch.bfloat16: DYNTS_BF16, torch.float32: DYNTS_FP32}
         self.device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
         self.stream = getattr(torch._C, "_cuda_getCurrentRawStream", lambda i: torch.cuda.current_stream(i).cuda_stream)
@@ -410,42 +411,47 @@ def rope(q, k, positions, q_out=None, k_out=None, theta=10000.0, sections=None, 
         q_out = t.torch.empty(q.shape, dtype=q.dtype, device=q.device)
     if k is not None and k_out is None:
         k_out = t.torch.empty(k.shape, dtype=k.dtype, device=k.device)
-    dt, dev = q.dtype, q.get_device()
+    dt, dev, shape = q.dtype, q.get_device(), q.shape
     dtype = t.dtypes.get(dt)
     if dtype is None:
         _invalid("q must be bf16 or fp32")
-    n, hq, d = q.shape
-    hkv = 0
-    strided = False
-    for x, y in ((q, q_out), (k, k_out)):
-        if x is None:
-            continue
-        shape = x.shape
-        for z in (x, y):
-            if z.get_device() != dev or dev < 0 or z.dtype is not dt or len(shape) != 3 or z.shape != shape or shape[0] != n or shape[2] != d:
-                _invalid("q, k and the outputs must be CUDA tensors [n, heads, d] of one type on one device")
-            if not z.is_contiguous():
-                strided = True
-                if z.stride(2) != 1 or (shape[1] > 1 and z.stride(1) != d) or (n > 1 and z.stride(0) < shape[1] * d):
-                    _invalid("the heads of a token must be contiguous and the tokens in order")
-        if x is k:
-            hkv = shape[1]
+    fits = len(shape) == 3 and dev >= 0 and q_out.dtype is dt and q_out.get_device() == dev and q_out.shape == shape
+    strided = not (q.is_contiguous() and q_out.is_contiguous())
+    hkv, k_ptr, k_out_ptr = 0, None, None
+    if k is not None:
+        k_shape = k.shape
+        fits = (fits and len(k_shape) == 3 and k.dtype is dt and k.get_device() == dev and k_out.dtype is dt and k_out.get_device() == dev and
+                k_out.shape == k_shape and k_shape[0] == shape[0] and k_shape[2] == shape[2])
+        strided = strided or not (k.is_contiguous() and k_out.is_contiguous())
+        k_ptr, k_out_ptr = k.data_ptr(), k_out.data_ptr()
+    if not fits:
+        _invalid("q, k and the outputs must be CUDA tensors [n, heads, d] of one type on one device")
+    n, hq, d = shape
+    if k is not None:
+        hkv = k_shape[1]
+    st = sec = None
+    if strided:
+        for z in (q, q_out) if k is None else (q, q_out, k, k_out):
+            if z.stride(2) != 1 or (z.shape[1] > 1 and z.stride(1) != d) or (n > 1 and z.stride(0) < z.shape[1] * d):
+                _invalid("the heads of a token must be contiguous and the tokens in order")
+        if n > 1:
+            st = (C.c_longlong * 4)(q.stride(0), 0 if k is None else k.stride(0), q_out.stride(0), 0 if k is None else k_out.stride(0))
     shape = positions.shape
     axes = 1 if len(shape) == 1 else shape[0]
-    if positions.get_device() != dev or positions.dtype is not t.torch.int32 or not positions.is_contiguous():
+    if positions.get_device() != dev or positions.dtype is not t.int32 or not positions.is_contiguous():
         _invalid("positions must be a contiguous int32 tensor on q's device")
     if len(shape) not in (1, 2) or shape[-1] != n or (sections is not None and len(sections) != axes):
         _invalid("positions are [n] or [axes, n], with a section for each axis")
-    st = sec = None
-    if strided and n > 1:
-        st = (C.c_longlong * 4)(q.stride(0), 0 if k is None else k.stride(0), q_out.stride(0), 0 if k is None else k_out.stride(0))
     if sections is not None:
-        sec = (C.c_int * axes)(*sections)
+        if axes > 1:
+            sec = (C.c_int * axes)(*sections)
+        elif rot_dim is not None and 2 * sections[0] != rot_dim:
+            _invalid("the section of one axis holds all pairs")
     if rot_dim is None:
         rot_dim = d if sections is None else 2 * sum(sections)
     flags = (DYNTS_ROPE_ADJACENT if adjacent else 0) | (DYNTS_ROPE_ROUND_ROBIN if round_robin else 0)
-    args = (q.data_ptr(), None if k is None else k.data_ptr(), positions.data_ptr(), q_out.data_ptr(), None if k is None else k_out.data_ptr(),
-            n, hq, hkv, d, rot_dim, axes, sec, flags, theta, dtype, st, t.stream(dev))
+    args = (q.data_ptr(), k_ptr, positions.data_ptr(), q_out.data_ptr(), k_out_ptr, n, hq, hkv, d, rot_dim, axes, sec, flags, theta, dtype, st,
+            t.stream(dev))
     if t.device() == dev:
         _check(lib.dynts_rope(*args))
     else:
@@ -550,24 +556,19 @@ class Cache:
         if len(listed) != self.batch:
             _invalid("n_new needs a count for each sequence")
         total = sum(listed)
-        layers, dt, dev, d = self.layers, self.torch_dtype, self.device_index, self.head_dim
-        wide = (total, self.q_heads, d) if layer is not None else (layers, total, self.q_heads, d)
-        narrow = (total, self.kv_heads, d) if layer is not None else (layers, total, self.kv_heads, d)
-        strides = [0, 0, 0]  # contiguous
-        for i, (x, shape) in enumerate(((q, wide), (k, narrow), (v, narrow), (out, wide))):
-            if x.dtype is not dt or x.get_device() != dev or x.shape != shape:
-                _invalid(f"q, k, v and out must be {dt} tensors on cuda:{dev}, here {wide} and {narrow} by n_new")
-            if not x.is_contiguous():
-                heads = shape[-2]
-                step = x.stride(-3) if total > 1 else heads * d
-                if i == 3:
-                    _invalid("out must be contiguous")
-                if (x.stride(-1) != 1 or (heads > 1 and x.stride(-2) != d) or step < heads * d or
-                        (layer is None and layers > 1 and x.stride(0) != total * step)):
-                    _invalid("the heads of a token must be contiguous, the tokens in order and the layers adjoining")
-                strides[i] = step
+        dt, dev = self.torch_dtype, self.device_index
+        if layer is None:
+            wide, narrow = (self.layers, total, self.q_heads, self.head_dim), (self.layers, total, self.kv_heads, self.head_dim)
+        else:
+            wide, narrow = (total, self.q_heads, self.head_dim), (total, self.kv_heads, self.head_dim)
+        if not (q.dtype is dt and k.dtype is dt and v.dtype is dt and out.dtype is dt and q.get_device() == dev and k.get_device() == dev and
+                v.get_device() == dev and out.get_device() == dev and q.shape == wide and k.shape == narrow and v.shape == narrow and out.shape == wide):
+            _invalid(f"q, k, v and out must be {dt} tensors on cuda:{dev}, here {wide} and {narrow} by n_new")
+        if not out.is_contiguous():
+            _invalid("out must be contiguous")
+        strides = (0, 0, 0) if q.is_contiguous() and k.is_contiguous() and v.is_contiguous() else tuple(self._token_stride(x, total) for x in (q, k, v))
         for x, shape in ((s_new, (total,)), (mass, self.mass_shape), (slopes, (self.q_heads,))):
-            if x is not None and (x.dtype is not t.torch.float32 or x.get_device() != dev or x.shape != shape or not x.is_contiguous()):
+            if x is not None and (x.dtype is not t.float32 or x.get_device() != dev or x.shape != shape or not x.is_contiguous()):
                 _invalid(f"s_new, mass and slopes must be contiguous fp32 tensors on cuda:{dev} (here: {shape})")
         prefixes = None
         if prefix is not None:
@@ -576,7 +577,7 @@ class Cache:
             prefixes, keep_p = _host_ints(prefix)
         opts = dynts_extend_opts_t(softcap, None if slopes is None else slopes.data_ptr(), window, prefixes, None if s_new is None else s_new.data_ptr(),
                                    None if mass is None else mass.data_ptr(), 1 if stage else 0, *strides)
-        need = lib.dynts_extend_scratch_bytes(self.handle, counts, layers if layer is None else 1)
+        need = lib.dynts_extend_scratch_bytes(self.handle, counts, self.layers if layer is None else 1)
         if need > self._scratch_bytes:
             # (a piece is never given back before the cache: the stream and captured graphs may still use it.  It comes from the
             # allocator's memory of the stream that will use it: another stream's may still be busy with what lay there.)
@@ -589,6 +590,15 @@ class Cache:
             with t.torch.cuda.device(dev):
                 return self._extend_call(layer, args)
         return self._extend_call(layer, args)
+
+    def _token_stride(self, x, total):
+        """Elements from one token of a strided q, k or v to the next."""
+        heads, d = x.shape[-2], self.head_dim
+        step = x.stride(-3) if total > 1 else heads * d
+        if x.numel() and (x.stride(-1) != 1 or (heads > 1 and x.stride(-2) != d) or step < heads * d or
+                          (x.dim() == 4 and self.layers > 1 and x.stride(0) != total * step)):
+            _invalid("the heads of a token must be contiguous, the tokens in order and the layers adjoining")
+        return step
 
     def _extend_call(self, layer, args):
         if layer is None:
