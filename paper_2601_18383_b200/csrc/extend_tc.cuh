@@ -798,8 +798,6 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
             beside = fresh && prefix > 0;  // rows of later positions may be visible
             __syncwarp();
           }
-          // logits in base-2 units: scaled in the exponent's multiply-add, or (MODS) before it
-          const float scale_log2 = MODS ? 1.f : p.scale_log2;
           uint64_t sum2[2] = {0ull, 0ull};  // two chains of (even, odd) column sums
           // (a row's reference comes from the first half of the first tile it sees: the headroom is for all others)
 #pragma unroll 1
@@ -808,11 +806,14 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
             uint32_t sv[CH];
             tc5::tmem_ld32(ts + (uint32_t)hb, sv);
             tc5::tmem_wait_ld();
+            float scale_log2 = p.scale_log2;  // logits in base-2 units: scaled in the exponent's multiply-add, or with a bias before it
             if constexpr (MODS) {
-              float scale = p.scale_log2;
-              if (x.cap_logit > 0.f) scale = xt_cap(sv, p);
+              if (x.cap_logit > 0.f) scale_log2 = xt_cap(sv, p);
+              const float scale = scale_log2;
+              if (x.slopes) scale_log2 = 1.f;
               const uint64_t scale2 = tc5::f2_pack(scale, scale);
-              if (beside) {
+              if (!x.slopes) {
+              } else if (beside) {
 #pragma unroll
                 for (int c = 0; c < CH; ++c) sv[c] = __float_as_uint(fmaf(__uint_as_float(sv[c]), scale, -slope * fabsf(at - lds_f(stage + 256u + 4u * (uint32_t)(hb + c)))));
               } else {  // - slope (me - pos) = slope pos - slope me, both counted from the tile's first row
