@@ -57,7 +57,8 @@ namespace dynts {
 
 // 8-bit rows, and the plain row arithmetic: two warps of their own load (12 warps, 80 registers per thread).  With caps, biases
 // and windows the row arithmetic needs the registers more: the warps that issue the products load too (10 warps, 96).
-// (4096 behind 4096, plain: 386 us against 488 us; ragged prompts with a bias: 134 against 122 us.)
+// (Loading warps against none: 4096 behind 4096, plain, 386 us against 488 us; ragged prompts with a bias 127 against 116 us, 1500
+// capped tokens 149 against 137 us.)
 template <bool KV8, bool MODS>
 struct XtShape {
   static constexpr bool kLoaders = KV8 || !MODS;
@@ -768,15 +769,21 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
           if (lane == 0 && j + 4 < nkt)
             asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(v_codes + (size_t)(key0 + 16 * wq - 4 * kPfKeys) * 128), "r"(16 * 128) : "memory");
         }
-        xt_wait(bar(5 + (g & 1)), (uint32_t)((g >> 1) & 1), abort_flag, x.err);  // S of this tile is complete
-        tc5::fence_after_sync();
-        if constexpr (KV8) {
-          // (S of this tile was issued after O += P V of tile g - 2 had read the stage)
+        auto widen_v = [&]() {
           uint8_t* vt = sm + kPfQBytes + (2 + (uint32_t)(g & 1)) * kPfKvBytes;
           xt_store_codes<true>(vc[0], vt, kPfKvBytes / 2, 16 * wq, lane);
           xt_store_codes<true>(vc[1], vt, kPfKvBytes / 2, 16 * wq + 8, lane);
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        };
+        // 8-bit rows: V goes to its stage while S is computed, once O += P V of tile g - 2 has read it (4096 behind 4096: 580 -> 568 us);
+        // with caps, biases and windows after it, as the two waits cost more than they hide (a capped step of 64: 112 against 119 us).
+        if constexpr (KV8 && !MODS) {
+          if (g >= 2) xt_wait(bar(10 + (g & 1)), (uint32_t)(((g - 2) >> 1) & 1), abort_flag, x.err);
+          widen_v();
         }
+        xt_wait(bar(5 + (g & 1)), (uint32_t)((g >> 1) & 1), abort_flag, x.err);  // S of this tile is complete
+        tc5::fence_after_sync();
+        if constexpr (KV8 && MODS) widen_v();  // (S of this tile was issued after O += P V of tile g - 2 had read the stage)
         if (live) {
           constexpr int CH = 32;
           bool border = false, beside = false;
