@@ -213,3 +213,35 @@ def test_the_sections_say_how_much_turns():
     a, _ = D.rope(q, None, pos, sections=[20, 12])
     b, _ = D.rope(q, None, pos, sections=[20, 12], rot_dim=64)
     assert torch.equal(a, b) and torch.equal(a[..., 64:], q[..., 64:]) and not torch.equal(a[..., 32:64], q[..., 32:64])
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16_kv8", 128), ("fp32", 64)])
+def test_the_first_call_is_captured(dtype, d):
+    """Nothing has run on the cache before the capture: the scratch is taken within it and serves eager calls afterwards."""
+    a, _ = build(dtype=dtype, d=d, q_heads=8, kv_heads=2, past=(200, 30), cap=512, source="external")
+    b, _ = build(dtype=dtype, d=d, q_heads=8, kv_heads=2, past=(200, 30), cap=512, source="external")
+    q, k, v = chunk(a, [20, 3], 21)
+    out, want, mass, mass_b = torch.empty_like(q), torch.empty_like(q), *(torch.zeros((1, 2, 2, a.capacity), device="cuda") for _ in range(2))
+    b.extend_attn(q, k, v, want, [20, 3], mass=mass_b, stage=True)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(side):
+        a.set_stream(side)
+        with torch.cuda.graph(g, stream=side):
+            a.extend_attn(q, k, v, out, [20, 3], mass=mass, stage=True)
+    for _ in range(3):
+        out.zero_()
+        mass.zero_()
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want) and torch.equal(mass, mass_b)
+    a.set_stream(torch.cuda.current_stream())
+    a.extend_attn(q, k, v, out.zero_(), [20, 3], mass=mass.zero_(), stage=True)
+    torch.cuda.synchronize()
+    assert torch.equal(out, want) and torch.equal(mass, mass_b)
+    a.poll_error()
+    del g
+    a.close(), b.close()
