@@ -281,7 +281,8 @@ typedef struct dynts_extend_opts {
  * weights rounded to bf16, any other shape in fp32; dynts_cache_set_launch variant 1 takes the latter for all.  DYNTS_ERR_CAPACITY if a sequence would outgrow its slab.  Nothing behind the last token
  * of out is written.  May be captured into a graph: the rows held are read from the device at replay
  * (n_new, prefix and the options are those of the capture), and as for decode steps the host's copy
- * of the lengths does not follow replays. */
+ * of the lengths does not follow replays.  A sequence whose chunk no longer fits at a replay keeps its rows, scores and
+ * length, its outputs and mass are not written, and dynts_poll_error reports it; the others are served. */
 size_t dynts_extend_scratch_bytes(const dynts_cache_t* c, const int* n_new, int n_layers);
 dynts_status_t dynts_extend_attn(dynts_cache_t* c, const void* q, const void* k_new, const void* v_new, void* out, const int* n_new,
                                  const dynts_extend_opts_t* opts, void* scratch, size_t scratch_bytes);

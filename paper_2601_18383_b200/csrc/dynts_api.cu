@@ -1335,7 +1335,7 @@ namespace {
 
 // What a chunk's launches need beside the cache, as offsets into the caller's scratch.
 struct ExtendScratch {
-  size_t lse, q16, part, counters, plan, mass, total;
+  size_t held, lse, q16, part, counters, plan, mass, total;
   int part_rows;  // query rows of a part of an item that several CTAs share
   int ctas;       // of the tensor-core kernel, at most
 };
@@ -1363,6 +1363,7 @@ ExtendScratch extend_scratch(const dynts_cache* c, const int* n_new, int n_layer
     off = align_up(off + bytes, 256);
     return o;
   };
+  m.held = take((size_t)2 * dynts::kExtSeqs * sizeof(int));
   m.lse = take((size_t)n_layers * total * f.q_heads * sizeof(float));
   m.q16 = m.part = m.counters = m.plan = m.mass = off;
   if (extend_tc_shape(f)) {
@@ -1378,7 +1379,7 @@ ExtendScratch extend_scratch(const dynts_cache* c, const int* n_new, int n_layer
     }
     m.plan = take((size_t)(items + m.ctas) * dynts::kPlanWords * sizeof(int));
   }
-  m.total = std::max<size_t>(off, 256);
+  m.total = off;
   return m;
 }
 
@@ -1704,6 +1705,7 @@ dynts_status_t launch_extend(dynts_cache* c, int layer0, int n_layers, const Ext
     dynts_status_t ms = extend_maps(c);
     if (ms != DYNTS_OK) return ms;
   }
+  p.held = reinterpret_cast<int*>(a.scratch + m.held);
   p.lse = want_mass ? reinterpret_cast<float*>(a.scratch + m.lse) : nullptr;
   p.q16 = tc && kv8 ? reinterpret_cast<__half*>(a.scratch + m.q16) : nullptr;
   p.counters = reinterpret_cast<unsigned int*>(a.scratch + m.counters);
@@ -1738,7 +1740,6 @@ dynts_status_t launch_extend(dynts_cache* c, int layer0, int n_layers, const Ext
     p.seqs.tok0[n_seq] = (int)tok;
     const int n_tok = p.seqs.tok0[n_seq] - p.seqs.tok0[0];
     if (n_tok == 0) continue;
-    p.published = 0;
     p.n_counters = tc && want_mass ? m.ctas * (kMassParts / 2) : 0;
     // one 16-byte piece of K and of V (and of the rows to clear, and of the queries to copy) per thread, up to a few CTAs per SM
     const long long pieces = f.head_dim * c->elt / 16, ny = (long long)n_layers * f.kv_heads;
@@ -1760,7 +1761,6 @@ dynts_status_t launch_extend(dynts_cache* c, int layer0, int n_layers, const Ext
                                                       : dynts::extend_store_kernel<__nv_bfloat16, false>,
                               grid, 256, 0, c->stream, p, plan));
     c->launches += 1;
-    p.published = p.publish;
     dynts_status_t st = tc ? launch_extend_tc(c, p, plan, tc_grid, whole, m, a.scratch, want_mass)
                         : kv8 ? launch_extend_generic<__nv_bfloat16, true>(c, p, want_mass)
                         : f.dtype == DYNTS_FP32 ? launch_extend_generic<float, false>(c, p, want_mass)

@@ -62,7 +62,7 @@ struct ExtendParams {
   int Nb, Hq, Hkv, G, d, cap;
   int window;         // 0: none
   int publish;        // the storing kernel advances the lengths when it is done
-  int published;      // the lengths on the device include the chunk already
+  int* held;          // [2][kExtSeqs], written by the storing kernel: rows held before the chunk (-1: it does not fit), tokens seen before it
   int accumulate;     // the mass is added to the scores
   __half* q16;        // 8-bit rows: [n_layers][total][Hq][d] f16 copies of the queries made by the storing kernel, or NULL
   unsigned int* counters;  // words the storing kernel clears for the kernel behind it
@@ -126,18 +126,19 @@ __device__ __forceinline__ size_t ext_lse_index(const ExtendParams& p, int layer
   return (((size_t)layer * p.Hkv + h) * p.total + tok) * p.G;
 }
 
-// Rows held and tokens seen before the chunk.
+// Rows held and tokens seen before the chunk, as the storing kernel found them: the lengths may include the chunk by now,
+// and a sequence whose chunk did not fit (a replayed graph's may have grown) has kept its length.
 struct ExtSeq {
   int b, t, n, tot;
-  bool ok;  // the chunk fits the slab (what the host's mirror checked before the launch)
+  bool ok;  // the chunk fits the slab
 };
 __device__ __forceinline__ ExtSeq ext_seq(const ExtendParams& p, int s) {
   ExtSeq e;
   e.b = p.seqs.b0 + s;
   e.t = p.seqs.tok0[s + 1] - p.seqs.tok0[s];
-  e.n = p.len[e.b] - (p.published ? e.t : 0);
-  e.tot = p.tot[e.b] - (p.published ? e.t : 0);
-  e.ok = e.n >= 0 && e.n + e.t <= p.cap;
+  e.n = p.held[s];
+  e.tot = p.held[kExtSeqs + s];
+  e.ok = e.n >= 0;
   return e;
 }
 
@@ -251,6 +252,12 @@ __global__ void __launch_bounds__(256) extend_store_kernel(const __grid_constant
       p.comp[row] = 0.f;
     }
   }
+  if (blockIdx.x == 0 && blockIdx.y == 0)
+    for (int s = threadIdx.x; s < p.seqs.n; s += blockDim.x) {
+      const int b = p.seqs.b0 + s, n = p.len[b];
+      p.held[s] = n >= 0 && n + p.seqs.tok0[s + 1] - p.seqs.tok0[s] <= p.cap ? n : -1;
+      p.held[kExtSeqs + s] = p.tot[b];
+    }
   if (plan.words) {
     const int warps = (int)(gridDim.x * gridDim.y * blockDim.x / 32);
     ext_write_plan(p, plan, (int)((blockIdx.y * gridDim.x + blockIdx.x) * (blockDim.x / 32) + threadIdx.x / 32), warps);

@@ -1182,8 +1182,7 @@ extend_mass_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_con
       int i_lo = j < cur.n + prefix ? 0 : j - cur.n, i_hi = mine ? cur.t : 0;
       float rel = 0.f;
       if constexpr (MODS) {
-        const int b = x.seqs.b0 + cur.s;
-        const int at = mine ? x.pos[row] - (x.tot[b] - (x.published ? cur.t : 0)) : 0;  // the row's position, the chunk's first token being 0
+        const int at = mine ? x.pos[row] - x.held[kExtSeqs + cur.s] : 0;  // the row's position, the chunk's first token being 0
         rel = (float)at;
         if (x.window > 0) {
           i_lo = max(i_lo, at - x.window + 1);

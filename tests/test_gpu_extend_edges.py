@@ -1,0 +1,85 @@
+"""The chunk operators at the borders of what they accept: replayed calls that no longer fit, biases beside rows that lie far
+back, windows as wide as an int, logits of minus infinity, old keys far above the newest, slopes below zero, calls back to
+back, and the fp32 form at head_dim 128.  Plain 64-bit forms; bounds derived beside each test."""
+import math
+
+import pytest
+import torch
+
+import paper_2601_18383_b200 as D
+from tests import extend_reference as R
+from tests.test_gpu_extend import build, check, chunk
+
+pytestmark = pytest.mark.gpu
+
+TYPES = [("bf16", 128), ("bf16_kv8", 128), ("fp32", 64)]
+SCALE = 0.05                                                         # of the 8-bit rows that `build` makes
+
+
+def captured(c, call):
+    """A graph of `call` on a side stream; the cache is back on the current stream, its lengths are the device's."""
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(side):
+        c.set_stream(side)
+        with torch.cuda.graph(g, stream=side):
+            call()
+    c.set_stream(torch.cuda.current_stream())
+    c.refresh_lengths()
+    return g
+
+
+@pytest.mark.parametrize("by_layer", [False, True], ids=["one call", "by layers"])
+@pytest.mark.parametrize("dtype,d", TYPES)
+def test_a_replayed_chunk_that_does_not_fit(dtype, d, by_layer):
+    """The first sequence's chunk no longer fits at the second replay: it keeps its rows, scores and length, its outputs and
+    mass are not written, the status says so, and the other sequence's chunk is what it would have been."""
+    kw = dict(dtype=dtype, d=d, layers=2, q_heads=8, kv_heads=2, past=(60, 5), cap=64)
+    a, _ = build(**kw)
+    b, _ = build(**kw)
+    q, k, v = chunk(a, [2, 1], 7)
+    out, ref = torch.empty_like(q), torch.empty_like(q)
+    ma, mb = (torch.full((2, 2, 2, 64), -3.0, device="cuda") for _ in range(2))
+
+    def run(c, o, m):
+        if by_layer:
+            for l in range(2):
+                c.extend_attn_layer(l, q[l], k[l], v[l], o[l], [2, 1], mass=m)
+        else:
+            c.extend_attn(q, k, v, o, [2, 1], mass=m)
+
+    run(a, out, ma), run(b, ref, mb)
+    g = captured(a, lambda: run(a, out, ma))
+    g.replay()
+    run(b, ref, mb)
+    a.refresh_lengths()
+    a.poll_error()
+    assert a.len(0) == b.len(0) == 64 and a.len(1) == b.len(1) == 7
+    before = R.State(a).slab
+    out.fill_(7.0), ma.fill_(-3.0), mb.fill_(-3.0)
+    torch.cuda.synchronize()
+    g.replay()
+    one = lambda x: x[:, 2:].contiguous()
+    ref1 = torch.empty_like(one(q))
+    b.extend_attn(one(q), one(k), one(v), ref1, [0, 1], mass=mb)
+    torch.cuda.synchronize()
+    with pytest.raises(D.DyntsError) as e:
+        a.poll_error()
+    assert e.value.status == D.DYNTS_ERR_DEVICE
+    a.refresh_lengths()
+    assert a.len(0) == 64 and a.len(1) == b.len(1) == 8
+    after, want = R.State(a).slab, R.State(b).slab
+    for l in range(2):
+        for h in range(2):
+            assert all(torch.equal(x, y) for x, y in zip(before[l, 0, h], after[l, 0, h]))
+            x, y = after[l, 1, h], want[l, 1, h]
+            assert all(torch.equal(x[i], y[i]) for i in range(3))
+            # (weights within 4e-4 of their value on either side: sum |q||k| < 128, as for captured chunks elsewhere)
+            assert ((x[3] - y[3]).abs() <= 8e-4 * y[3]).all()
+    assert (out[:, :2] == 7.0).all() and (ma[:, 0] == -3.0).all()
+    assert ((ma[:, 1] - mb[:, 1]).abs() <= 8e-4 * mb[:, 1].abs()).all()
+    # (each side rounds its weights and its output: half a step of at most max |v| each)
+    vmax = max(float(want[l, 1, h][1].abs().max()) for l in range(2) for h in range(2))
+    assert ((out[:, 2:].float() - ref1.float()).abs() <= 4 * R.EPS[out.dtype] * vmax * (64 if dtype == "fp32" else 1)).all()
+    a.close(), b.close()
