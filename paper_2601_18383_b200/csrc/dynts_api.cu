@@ -1356,7 +1356,8 @@ ExtendScratch extend_scratch(const dynts_cache* c, const int* n_new, int n_layer
   }
   const int G = f.q_heads / f.kv_heads;
   m.part_rows = (int)(((long long)std::min(longest, dynts::kXtRows / G) * G + 3) / 4 * 4);
-  m.ctas = std::min(dynts::kXtMaxCtas, 2 * (c->sm_count > 0 ? c->sm_count : 148));
+  // (before its first call a cache does not know its device: room for the most CTAs, so that the launch, which does, needs no more)
+  m.ctas = c->sm_count > 0 ? std::min(dynts::kXtMaxCtas, 2 * c->sm_count) : dynts::kXtMaxCtas;
   size_t off = 0;
   auto take = [&](size_t bytes) {
     const size_t o = off;
