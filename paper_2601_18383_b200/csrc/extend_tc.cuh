@@ -788,10 +788,13 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
           constexpr int CH = 32;
           bool border = false, beside = false;
           float at = 0.f;                                       // this row's token
-          // (the staging tile: positions behind the tile's first, [64] as integers and [64] as floats)
+          // (the staging tile: positions counted from the tile's newest row, [64] as integers and [64] as floats)
           int me = 0;
           if constexpr (MODS) {
-            const int p0 = __shfl_sync(0xffffffffu, pos_a, 0);
+            // From the newest: a token is at most 64 positions closer to it than to any row it sees, so both terms of a
+            // bias are about as small as the bias.  (From the first, which may have survived evictions from far back, a recent
+            // row's bias would be the difference of two large products.)
+            const int last = min(kPfKeys, end - key0) - 1, p0 = __shfl_sync(0xffffffffu, last < 32 ? pos_a : pos_b, last & 31);
             __syncwarp();
             sts_i(stage + 4u * lane, pos_a - p0);
             sts_i(stage + 128u + 4u * lane, pos_b - p0);
@@ -801,7 +804,7 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
             at = (float)me;
             const bool fresh = key0 + kPfKeys > held;  // the tile holds rows of the chunk
             // the tile's first position against the warp's last token (in tiles with rows of the chunk: always compared)
-            border = x.window > 0 && (fresh || __shfl_sync(0xffffffffu, me, 31) >= x.window);
+            border = x.window > 0 && (fresh || __shfl_sync(0xffffffffu, ti, 31) - __shfl_sync(0xffffffffu, pos_a, 0) >= x.window);
             beside = fresh && prefix > 0;  // rows of later positions may be visible
             __syncwarp();
           }
@@ -823,7 +826,7 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
               } else if (beside) {
 #pragma unroll
                 for (int c = 0; c < CH; ++c) sv[c] = __float_as_uint(fmaf(__uint_as_float(sv[c]), scale, -slope * fabsf(at - lds_f(stage + 256u + 4u * (uint32_t)(hb + c)))));
-              } else {  // - slope (me - pos) = slope pos - slope me, both counted from the tile's first row
+              } else {  // - slope (me - pos) = slope pos - slope me, both counted from the tile's newest row
                 const uint64_t slope2 = tc5::f2_pack(slope, slope), base2 = tc5::f2_pack(-slope * at, -slope * at);
 #pragma unroll
                 for (int c = 0; c < CH; c += 4) {

@@ -83,3 +83,57 @@ def test_a_replayed_chunk_that_does_not_fit(dtype, d, by_layer):
     vmax = max(float(want[l, 1, h][1].abs().max()) for l in range(2) for h in range(2))
     assert ((out[:, 2:].float() - ref1.float()).abs() <= 4 * R.EPS[out.dtype] * vmax * (64 if dtype == "fp32" else 1)).all()
     a.close(), b.close()
+
+
+@pytest.mark.parametrize("far", [100_000, 1_000_000])
+@pytest.mark.parametrize("n,new,prefix", [(30, 5, 0), (30, 5, 3), (30, 90, 0), (66, 1, 0), (66, 40, 7), (104, 5, 0)])
+@pytest.mark.parametrize("dtype,d", TYPES)
+def test_a_bias_beside_rows_that_lie_far_back(dtype, d, n, new, prefix, far):
+    """Four rows from the beginning beside recent ones.  The bias of a recent row is small, and so has its rounding to be:
+    every logit's error is weighed with its weight, not with that of the farthest row."""
+    heads, kv_heads = 8, 2
+    c, _ = build(dtype=dtype, d=d, q_heads=heads, kv_heads=kv_heads, past=(n,), cap=256)
+    G = heads // kv_heads
+    pos = torch.cat([torch.arange(4), far + torch.arange(n - 4)]).to(torch.int32)
+    for h in range(kv_heads):
+        K, V, _, score = c.export_slab(0, 0, h)
+        c.import_slab(0, 0, h, K, V, pos, score, 0)
+    tot = far + n - 4
+    q, k, v = chunk(c, [new], 3)
+    slopes = 2.0 ** -torch.arange(1, heads + 1).float()
+    state = R.State(c, SCALE, SCALE)
+    out, mass = torch.empty_like(q), torch.zeros((1, 1, kv_heads, c.capacity), device="cuda")
+    c.extend_attn(q, k, v, out, [new], mass=mass, slopes=slopes.cuda(), prefix=[prefix] if prefix else None, stage=True)
+    c.synchronize()
+    c.poll_error()
+    i, j = torch.arange(new)[:, None], torch.arange(n + new)[None, :]
+    visible = (j <= n + i) | (j < n + prefix)
+    p_all = torch.cat([pos.long(), tot + torch.arange(new)])
+    apart = (p_all[n:, None] - p_all[None, :]).abs().double()
+    for h in range(kv_heads):
+        K, V, _, _ = state.slab[0, 0, h]
+        kn, vn = k[0, :, h].cpu(), v[0, :, h].cpu()
+        if dtype == "bf16_kv8":
+            kn, vn = R.e4m3(kn, SCALE).double() * SCALE, R.e4m3(vn, SCALE).double() * SCALE
+        K, V = torch.cat([K, kn.double()]), torch.cat([V, vn.double()])
+        m, mt = torch.zeros(n + new, dtype=torch.float64), torch.zeros(n + new, dtype=torch.float64)
+        for x in range(h * G, (h + 1) * G):
+            qx = q[0, :, x].cpu().double()
+            raw = qx @ K.T / math.sqrt(d)
+            z = raw - float(slopes[x]) * apart
+            # a dot product's error as in the shared reference; the bias and the logit a few half steps of themselves, the bias
+            # of a tile of 64 rows counted from any row of it
+            dz = (d + 8) * 2.0 ** -23 * (qx.abs() @ K.abs().T) / math.sqrt(d) + 8 * 2.0 ** -24 * (raw.abs() + z.abs() + float(slopes[x]) * (apart + 64))
+            p = torch.softmax(z.masked_fill(~visible, -math.inf), -1)
+            dz = dz.masked_fill(~visible, 0.0)
+            err = p * (dz + (p * dz).sum(-1, keepdim=True) + 132 * 2.0 ** -23) * 1.01       # its own logit, the sum's, exponentials
+            m += p.sum(0)
+            mt += err.sum(0)
+            o = p @ V
+            half = 0.0 if dtype == "fp32" else 2.0 ** -8
+            tol = err @ V.abs() + (half + (n + new) / 8 * 2.0 ** -23) * (p @ V.abs()) * 1.01 + R.EPS[q.dtype] * o.abs() * 1.01 + 1e-30
+            off = (out[0, :, x].double().cpu() - o).abs()
+            assert (off <= tol).all(), f"outputs: {(off / tol).max():.3g} of the bound"
+        off, tol = (mass[0, 0, h, : n + new].double().cpu() - m).abs(), mt + (new * G + 8) * 2.0 ** -24 * m + 1e-30
+        assert (off <= tol).all(), f"mass: {(off / tol).max():.3g} of the bound"
+    c.close()
