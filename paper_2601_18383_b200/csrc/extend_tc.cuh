@@ -1188,7 +1188,7 @@ extend_mass_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_con
         const int at = mine ? x.pos[row] - x.held[kExtSeqs + cur.s] : 0;  // the row's position, the chunk's first token being 0
         rel = (float)at;
         if (x.window > 0) {
-          i_lo = max(i_lo, at - x.window + 1);
+          i_lo = max(i_lo, (int)max(0ll, (long long)at - x.window + 1));  // (in 64 bits: a window may be as wide as an int)
           i_hi = (int)min((long long)i_hi, max(0ll, (long long)at + x.window));
         }
         if (x.slopes) {

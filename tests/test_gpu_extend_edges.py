@@ -137,3 +137,13 @@ def test_a_bias_beside_rows_that_lie_far_back(dtype, d, n, new, prefix, far):
         off, tol = (mass[0, 0, h, : n + new].double().cpu() - m).abs(), mt + (new * G + 8) * 2.0 ** -24 * m + 1e-30
         assert (off <= tol).all(), f"mass: {(off / tol).max():.3g} of the bound"
     c.close()
+
+
+@pytest.mark.parametrize("q_heads,kv_heads", [(2, 2), (8, 2), (14, 2)])
+@pytest.mark.parametrize("window", [2 ** 31 - 1, 2 ** 31 - 100])
+@pytest.mark.parametrize("dtype,d", TYPES)
+def test_windows_as_wide_as_an_int(dtype, d, window, q_heads, kv_heads):
+    """2^31 - 1 stands for no window: rows of any distance are seen, and receive their mass."""
+    c, seen = build(dtype=dtype, d=d, q_heads=q_heads, kv_heads=kv_heads, past=(150, 0, 333), cap=512, evict_to=200)
+    check(c, seen, [70, 33, 1], scale=SCALE, seed=23, window=window)
+    c.close()
