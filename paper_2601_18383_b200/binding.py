@@ -581,8 +581,7 @@ class Cache:
         if need > self._scratch_bytes:
             # (a piece is never given back before the cache: the stream and captured graphs may still use it.  It comes from the
             # allocator's memory of the stream that will use it: another stream's may still be busy with what lay there.)
-            with t.torch.cuda.stream(t.torch.cuda.ExternalStream(self._stream, device=self.device) if self._stream
-                                     else t.torch.cuda.default_stream(self.device)):
+            with t.torch.cuda.stream(self.torch_stream()):
                 self._scratch.append(t.torch.empty(max(need, 2 * self._scratch_bytes), dtype=t.torch.uint8, device=self.device))
             self._scratch_ptr, self._scratch_bytes = self._scratch[-1].data_ptr(), self._scratch[-1].numel()
         args = (q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), counts, C.byref(opts), self._scratch_ptr, self._scratch_bytes)
@@ -590,6 +589,11 @@ class Cache:
             with t.torch.cuda.device(dev):
                 return self._extend_call(layer, args)
         return self._extend_call(layer, args)
+
+    def torch_stream(self):
+        """The stream the cache works on, as a torch stream."""
+        cuda = self.torch.cuda
+        return cuda.ExternalStream(self._stream, device=self.device) if self._stream else cuda.default_stream(self.device)
 
     def _token_stride(self, x, total):
         """Elements from one token of a strided q, k or v to the next."""

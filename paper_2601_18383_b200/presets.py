@@ -136,7 +136,19 @@ class PresetRun:
 
         q, out [L, Nb, T, Hq, d], k, v [L, Nb, T, Hkv, d], scores [Nb, T]; options as of `Cache.extend_attn` (softcap,
         slopes, window).  The chunk is cut where the row count reaches the budget, and a selection follows each piece, so
-        the rows held and the events are those of T steps."""
+        the rows held and the events are those of T steps.  In order with torch's current stream, whichever stream the cache
+        works on."""
+        c = self.cache
+        current, own = c.torch.cuda.current_stream(c.device), c.torch_stream()
+        if own.cuda_stream == current.cuda_stream:
+            return self._extend(q, k, v, out, predictor_scores, random_scores, options)
+        # the pieces are copied, and their memory taken and given back, where the cache reads and writes them
+        own.wait_stream(current)
+        with c.torch.cuda.stream(own):
+            self._extend(q, k, v, out, predictor_scores, random_scores, options)
+        current.wait_stream(own)
+
+    def _extend(self, q, k, v, out, predictor_scores, random_scores, options):
         c, p = self.cache, self.preset
         T = q.shape[2]
         scores = p.step_scores(predictor_scores, random_scores)
