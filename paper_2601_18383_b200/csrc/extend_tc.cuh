@@ -139,11 +139,17 @@ __device__ __forceinline__ void xt_wait(uint32_t bar, uint32_t parity, uint32_t 
 struct XtCodes {
   uint4 c[2];
 };
+// (Not ld.global.nc: with programmatic launches the kernel may be resident while the one before it stores these rows.)
+__device__ __forceinline__ uint4 ld_stream(const void* p) {
+  uint4 r;
+  asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "l"(p));
+  return r;
+}
 __device__ __forceinline__ void xt_load_codes(XtCodes& r, const uint8_t* base, int row0, int end, int lane) {
   const int row = row0 + (lane >> 2);
   const uint8_t* src = base + (size_t)row * 128 + (lane & 3) * 16;
-  r.c[0] = row < end ? ldg_stream(src) : make_uint4(0u, 0u, 0u, 0u);
-  r.c[1] = row < end ? ldg_stream(src + 64) : make_uint4(0u, 0u, 0u, 0u);
+  r.c[0] = row < end ? ld_stream(src) : make_uint4(0u, 0u, 0u, 0u);
+  r.c[1] = row < end ? ld_stream(src + 64) : make_uint4(0u, 0u, 0u, 0u);
 }
 // Two codes of w (bytes by `sel`) as a bf16 pair: the code's exponent and mantissa bits in bf16's place are the value
 // times 2^-120, subnormals included, and the product with 2^120 is exact.
@@ -1201,7 +1207,7 @@ extend_mass_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_con
       const int all_rows = cur.t * x.G, step_rows = tps * x.G;
       auto ask = [&](int step, int off) {  // a step's negated log-sum-exp of column lane + off
         const int r = (cur.lo + step) * step_rows + lane + off;
-        return lane + off < step_rows && r < all_rows ? -__ldg(lse + r) : -CUDART_INF_F;
+        return lane + off < step_rows && r < all_rows ? -__ldcg(lse + r) : -CUDART_INF_F;
       };
       float la[kXmRows / 32];
 #pragma unroll

@@ -147,3 +147,28 @@ def test_windows_as_wide_as_an_int(dtype, d, window, q_heads, kv_heads):
     c, seen = build(dtype=dtype, d=d, q_heads=q_heads, kv_heads=kv_heads, past=(150, 0, 333), cap=512, evict_to=200)
     check(c, seen, [70, 33, 1], scale=SCALE, seed=23, window=window)
     c.close()
+
+
+@pytest.mark.parametrize("dtype", ["bf16_kv8", "bf16"])
+def test_calls_back_to_back_with_other_rows(dtype):
+    """Staged calls that overwrite one another's rows, nothing between them, equal the same calls each waited for."""
+    n_new = [30, 5, 0, 64]
+    kw = dict(dtype=dtype, q_heads=8, kv_heads=2, past=(200, 63, 7, 500), cap=640)
+    a, _ = build(**kw)
+    b, _ = build(**kw)
+    data = [chunk(a, n_new, 40 + i) for i in range(12)]
+    res = []
+    for c, wait in ((a, False), (b, True)):
+        outs = [torch.empty_like(q) for q, _, _ in data]
+        mass = [torch.zeros((1, 4, 2, 640), device="cuda") for _ in data]
+        torch.cuda.synchronize()
+        for (q, k, v), o, m in zip(data, outs, mass):
+            c.extend_attn(q, k, v, o, n_new, mass=m, stage=True)
+            if wait:
+                torch.cuda.synchronize()
+        torch.cuda.synchronize()
+        c.poll_error()
+        res.append((outs, mass))
+    for x, y in zip(res[0][0] + res[0][1], res[1][0] + res[1][1]):
+        assert torch.equal(x, y)
+    a.close(), b.close()
