@@ -13,7 +13,8 @@
 //   x  -= slope_h |p_i - p_j|                if slopes are given
 //   row j is visible  <=>  j <= n + i, or j is one of the chunk's first `prefix` rows;
 //                          and |p_i - p_j| < window, if a window is given
-// A token always sees itself, so no row of weights is empty.  All logits are kept in base-2 units
+// A token always sees itself, so no row of weights is empty.  (A logit of -inf weighs nothing; a token whose visible
+// logits are all -inf has no answer: NaN.)  All logits are kept in base-2 units
 // (times log2 e), sums and maxima in fp32.
 #pragma once
 
@@ -468,7 +469,8 @@ __global__ void __launch_bounds__(kExtGenericThreads) extend_generic_kernel(cons
       for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
       const float m_new = fmaxf(m[u], mx);
       const float alpha = m[u] == -CUDART_INF_F ? 0.f : exp2f(m[u] - m_new);
-      w[u] = visible ? exp2f(x - m_new) : 0.f;
+      // (all seen so far may be logits of -inf: they weigh nothing if any other follows, and leave 0 / 0 if none does)
+      w[u] = visible ? exp2f(x - (m_new == -CUDART_INF_F ? 0.f : m_new)) : 0.f;
       l[u] = l[u] * alpha + w[u];
       m[u] = m_new;
 #pragma unroll

@@ -230,18 +230,21 @@ __device__ __noinline__ float4 xt_row_again(const ExtendTcParams& p, int d, int 
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
       const float mn = fmaxf(m, mx);
-      l = l * (m == -CUDART_INF_F ? 0.f : exp2f(m - mn)) + (visible ? exp2f(y - mn) : 0.f);  // (lane's own sum)
+      l = l * (m == -CUDART_INF_F ? 0.f : exp2f(m - mn)) + (visible ? exp2f(y - (mn == -CUDART_INF_F ? 0.f : mn)) : 0.f);  // (lane's own sum)
       m = mn;
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
     lse = m + log2f(l);
   }
+  // (Without redo lse is -inf where this part of the item holds no logit above that: it weighs nothing beside the others.  With
+  // redo nothing the row sees weighs anything, and the weights are exp2(-inf + inf): NaN.)
+  const bool none = !redo && lse == -CUDART_INF_F;
   float acc[4] = {0.f, 0.f, 0.f, 0.f};
   for (int kb = k0; kb < end; kb += 32) {
     bool visible;
     const float y = logit(kb + lane, visible);
-    const float w = visible ? exp2f(y - lse) : 0.f;
+    const float w = visible && !none ? exp2f(y - lse) : 0.f;
     for (int kk = 0; kk < 32; ++kk) {
       const float wk = __shfl_sync(0xffffffffu, w, kk);
       if (wk == 0.f) continue;
@@ -375,7 +378,9 @@ __device__ __noinline__ void xt_epilogue(const ExtendTcParams& p, int d, int ord
   const bool mine = r < rows;
   const size_t piece = (size_t)p.part_rows;
   float* part = p.part + (size_t)word(kPwPlace) * (piece * kXtPartFloats);
-  const bool redo = mine && !(l < kXtSumMax);  // out of range, or not a number
+  // Out of range, or not a number; or the reference tiles held nothing above -inf, so that the sum has no reference (or the row
+  // of a whole item no sum: it sees itself, so all it sees is -inf).
+  const bool redo = mine && (!(l < kXtSumMax) || (ref == -CUDART_INF_F && (whole || l > 0.f)));
   float lse = l > 0.f ? xt_add_log2(ref, l) : -CUDART_INF_F;
   const float f = l > 0.f ? 1.f / l : 0.f;
   __nv_bfloat16* obase = static_cast<__nv_bfloat16*>(x.out) + (((size_t)layer * x.total + tok) * x.Hq + h * x.G) * 128;

@@ -149,6 +149,66 @@ def test_windows_as_wide_as_an_int(dtype, d, window, q_heads, kv_heads):
     c.close()
 
 
+def plain(state, q, k, v, n, dtype, kv_heads):
+    """Outputs of one sequence of one layer in 64 bits, causal: [t, Hq, d]."""
+    t, hq, d = q.shape
+    G = hq // kv_heads
+    i, j = torch.arange(t)[:, None], torch.arange(n + t)[None, :]
+    out = torch.empty((t, hq, d), dtype=torch.float64)
+    for h in range(kv_heads):
+        kn, vn = k[:, h].cpu(), v[:, h].cpu()
+        if dtype == "bf16_kv8":
+            kn, vn = R.e4m3(kn, SCALE).double() * SCALE, R.e4m3(vn, SCALE).double() * SCALE
+        K, V = state.slab[0, 0, h][:2] if n else (torch.zeros((0, d), dtype=torch.float64),) * 2
+        K, V = torch.cat([K, kn.double()]), torch.cat([V, vn.double()])
+        for x in range(h * G, (h + 1) * G):
+            z = (q[:, x].cpu().double() @ K.T / math.sqrt(d)).masked_fill(j > n + i, -math.inf)
+            out[:, x] = torch.softmax(z, -1) @ V
+    return out
+
+
+@pytest.mark.parametrize("past,low", [(0, [0]), (40, list(range(40))), (140, list(range(140))), (140, list(range(70, 140))), (2000, list(range(1900))),
+                                      (2000, list(range(2000)))])
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("fp32", 64), ("bf16", 64)])
+def test_logits_of_minus_infinity(dtype, d, past, low):
+    """Rows whose key makes every logit -inf (an infinite element against queries of one sign) weigh nothing, whole tiles of
+    them too; a token that sees nothing else has no answer: NaN, as its definition has."""
+    q_heads, kv_heads, t = 8, 2, 5
+    c, _ = build(dtype=dtype, d=d, q_heads=q_heads, kv_heads=kv_heads, past=(past,), cap=max(64, past + 32))
+    q, k, v = chunk(c, [t], 29)
+    q[..., 3] = -q[..., 3].abs() - 0.5
+    if past == 0:
+        k[0, 0, :, 3] = math.inf                                     # the first token sees only itself
+    else:
+        if len(low) == past:
+            k[0, :2, :, 3] = math.inf                                # the first two tokens see only such rows
+        for h in range(kv_heads):
+            K, V, pos, score = c.export_slab(0, 0, h)
+            K[low, 3] = math.inf
+            c.import_slab(0, 0, h, K, V, pos, score, 0)
+    state = R.State(c)
+    out = torch.empty_like(q)
+    mass = torch.zeros((1, 1, kv_heads, c.capacity), device="cuda")
+    c.extend_attn(q, k, v, out, [t], mass=mass, stage=True)
+    c.synchronize()
+    c.poll_error()
+    want, got = plain(state, q[0], k[0], v[0], past, dtype, kv_heads), out[0].double().cpu()
+    assert torch.equal(torch.isnan(got), torch.isnan(want))
+    fine = ~torch.isnan(want)
+    assert fine.any() and (past == 0 or len(low) < past or torch.isnan(want).any())
+    # logits off by less than 1e-3 (sum |q||k| < 64 among the finite), weights and outputs rounded: half a step of at most max |v|
+    vmax = float(max(v.float().abs().max(), max((s[1].abs().max() for s in state.slab.values() if s[1].numel()), default=0.0)))
+    assert ((got - want)[fine].abs() <= (2e-3 + 2 * R.EPS[torch.float32 if dtype == "fp32" else torch.bfloat16]) * vmax).all()
+    m = mass[0, 0, 0, : past + t].cpu()
+    if past and len(low) < past:
+        assert (m[low] == 0).all() and abs(float(m.double().sum()) - t * q_heads // kv_heads) < 1e-3
+    elif past:
+        assert torch.isnan(m[:past]).all() and torch.isfinite(m[past + 2:]).all()
+    else:
+        assert torch.isfinite(m[1:]).all()
+    c.close()
+
+
 @pytest.mark.parametrize("dtype", ["bf16_kv8", "bf16"])
 def test_calls_back_to_back_with_other_rows(dtype):
     """Staged calls that overwrite one another's rows, nothing between them, equal the same calls each waited for."""
