@@ -409,7 +409,8 @@ dynts_status_t dynts_synchronize(dynts_cache_t* c);
 dynts_status_t dynts_cache_set_launch(dynts_cache_t* c, int cluster, int variant);
 
 /* Device-side waits are bounded: a thread that waits for a tile or a hand-over inside the streaming
- * decode kernel polls at most `polls` times (default 2^22, seconds at worst); when a wait runs
+ * decode kernel or the tensor-core kernels of dynts_extend_attn polls at most `polls` times (default
+ * 2^22, seconds at worst; not counted while a warp of its CTA computes rows again); when a wait runs
  * out the CTA raises the timeout bit of the status word, every later wait of that CTA returns at
  * once, the kernel ends, and dynts_poll_error reports DYNTS_ERR_DEVICE (that step's results are
  * void; the context stays usable).  polls >= 64. */

@@ -1622,6 +1622,7 @@ dynts_status_t launch_extend_tc(dynts_cache* c, const dynts::ExtendParams& x, co
   p.part_rows = m.part_rows;
   p.part = reinterpret_cast<float*>(scratch + m.part);
   p.stop = reinterpret_cast<int*>(c->ticket()) + 41;  // a spare word of the ticket block (zero since the cache was created)
+  p.wait_limit = std::max(c->wait_limit, 2048u);  // (the waits look every 1024 polls whether rows are being computed again)
   p.out_scale = c->cfg.dtype == DYNTS_BF16_KV8 ? c->v_scale : 1.f;
   p.scale_log2 = (float)(1.4426950408889634 * (double)x.scale);
   p.cap_log2 = (float)(1.4426950408889634 * (double)x.cap_logit);

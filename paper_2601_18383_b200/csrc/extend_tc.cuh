@@ -78,6 +78,7 @@ struct ExtendTcParams {
   int part_rows;        // query rows a part's scratch has room for
   float* part;          // [2 per CTA]: [32][part_rows] float4, [part_rows] float
   int* stop;
+  unsigned int wait_limit;  // polls of a bounded wait, at least 2048
   int mass_parts;       // parts the query rows of a mass item are cut into, while there are at most mass_items items
   int mass_items;
   float* mass_part;     // [mass_items][mass_parts][256]
@@ -122,15 +123,24 @@ __device__ __forceinline__ int lds_flag(uint32_t a) {
 }
 __device__ __forceinline__ void sts_i(uint32_t a, int v) { asm volatile("st.shared.s32 [%0], %1;" ::"r"(a), "r"(v) : "memory"); }
 __device__ __forceinline__ void sts_f(uint32_t a, float v) { asm volatile("st.shared.f32 [%0], %1;" ::"r"(a), "f"(v) : "memory"); }
-// mbar_wait (decode_stream.cuh) with the abort flag by its shared address.
-__device__ __forceinline__ void xt_wait(uint32_t bar, uint32_t parity, uint32_t abort_flag, int* err) {
+// mbar_wait (decode_stream.cuh) with the abort flag by its shared address.  The word behind the flag says how many of the
+// CTA's warps are computing rows again: a wait that sees any begins anew, so that may take as long as the rows' keys do, and
+// a wait for something that never comes still ends.
+__device__ __forceinline__ void xt_wait(uint32_t bar, uint32_t parity, uint32_t abort_flag, const ExtendTcParams& p) {
   if (lds_flag(abort_flag)) return;
-  for (uint32_t i = 0; i < kPfSpinLimit; ++i) {
+#pragma unroll 1
+  for (uint32_t i = 0; i < p.wait_limit; ++i) {
     if (mbar_try_wait(bar, parity)) return;
-    if ((i & 1023u) == 1023u && lds_flag(abort_flag)) return;
+    if ((i & 1023u) == 1023u) {
+      if (lds_flag(abort_flag)) return;
+      if (lds_flag(abort_flag + 4u)) i = 0;
+    }
   }
   sts_i(abort_flag, 1);
-  atomicOr(err, kErrTimeout);
+  atomicOr(p.x.err, kErrTimeout);
+}
+__device__ __forceinline__ void xt_busy(uint32_t busy, int change) {  // one lane
+  asm volatile("red.shared.add.s32 [%0], %1;" ::"r"(busy), "r"(change) : "memory");
 }
 
 // Codes to operand tiles [2 halves of head_dim][rows][128 B], 16-byte chunks swizzled by row.  A warp takes groups of 8
@@ -199,9 +209,10 @@ __device__ __forceinline__ void xt_store_codes(const XtCodes& r, uint8_t* tile, 
 // One query row again, by a whole warp, from the visible rows of the piece alone.  redo: lse is computed too (with the
 // true maximum); else the caller's is taken.  Returns the output over out_scale, lane = four columns.  For rows whose
 // fast result is not finite: a hidden row held something that is not, the weights' sum left its range, or the answer
-// is in truth not finite.  d: the piece's words, one per lane.
+// is in truth not finite.  d: the piece's words, one per lane.  Far from the tensor cores' rate (512 tokens,
+// two KV heads, behind 16000 rows, slopes below zero so that every row comes here: 12 to 17 ms against 0.2), but without limit.
 template <bool KV8>
-__device__ __noinline__ float4 xt_row_again(const ExtendTcParams& p, int d, int r, bool redo, float& lse) {
+__device__ __forceinline__ float4 xt_row_again(const ExtendTcParams& p, int d, int r, bool redo, float& lse) {
   const ExtendParams& x = p.x;
   auto word = [&](int w) { return __shfl_sync(0xffffffffu, d, w); };
   const int lane = threadIdx.x & 31;
@@ -218,7 +229,20 @@ __device__ __noinline__ float4 xt_row_again(const ExtendTcParams& p, int d, int 
     if (x.window > 0 && apart >= x.window) return 0.f;
     visible = true;
     float dot = 0.f;
-    for (int e = 0; e < 128; ++e) dot = fmaf(__bfloat162float(q[e]), ext_row_value<__nv_bfloat16, KV8>(x.K, (slab * x.cap + j) * 128 + e, 1.f), dot);
+#pragma unroll 4
+    for (int e = 0; e < 128; e += 8) {
+      const uint4 qq = *reinterpret_cast<const uint4*>(q + e);
+      const size_t at = (slab * x.cap + j) * 128 + e;
+      const float4 k0 = ext_row_value4<__nv_bfloat16, KV8>(x.K, at, 1.f), k1 = ext_row_value4<__nv_bfloat16, KV8>(x.K, at + 4, 1.f);
+      dot = fmaf(__uint_as_float(qq.x << 16), k0.x, dot);
+      dot = fmaf(__uint_as_float(qq.x & 0xffff0000u), k0.y, dot);
+      dot = fmaf(__uint_as_float(qq.y << 16), k0.z, dot);
+      dot = fmaf(__uint_as_float(qq.y & 0xffff0000u), k0.w, dot);
+      dot = fmaf(__uint_as_float(qq.z << 16), k1.x, dot);
+      dot = fmaf(__uint_as_float(qq.z & 0xffff0000u), k1.y, dot);
+      dot = fmaf(__uint_as_float(qq.w << 16), k1.z, dot);
+      dot = fmaf(__uint_as_float(qq.w & 0xffff0000u), k1.w, dot);
+    }
     return ext_logit_exact(x, dot, slope, apart);
   };
   if (redo) {
@@ -245,12 +269,14 @@ __device__ __noinline__ float4 xt_row_again(const ExtendTcParams& p, int d, int 
     bool visible;
     const float y = logit(kb + lane, visible);
     const float w = visible && !none ? exp2f(y - lse) : 0.f;
-    for (int kk = 0; kk < 32; ++kk) {
+    for (unsigned some = __ballot_sync(0xffffffffu, w != 0.f); some; some &= some - 1) {
+      const int kk = __ffs(some) - 1;
       const float wk = __shfl_sync(0xffffffffu, w, kk);
-      if (wk == 0.f) continue;
-#pragma unroll
-      for (int u = 0; u < 4; ++u)
-        acc[u] = fmaf(wk, ext_row_value<__nv_bfloat16, KV8>(x.V, (slab * x.cap + kb + kk) * 128 + 4 * lane + u, 1.f), acc[u]);
+      const float4 v = ext_row_value4<__nv_bfloat16, KV8>(x.V, (slab * x.cap + kb + kk) * 128 + 4 * lane, 1.f);
+      acc[0] = fmaf(wk, v.x, acc[0]);
+      acc[1] = fmaf(wk, v.y, acc[1]);
+      acc[2] = fmaf(wk, v.z, acc[2]);
+      acc[3] = fmaf(wk, v.w, acc[3]);
     }
   }
   return make_float4(acc[0], acc[1], acc[2], acc[3]);
@@ -357,6 +383,51 @@ __global__ void __launch_bounds__(256) extend_join_kernel(const __grid_constant_
   if (c4 == 0 && x.lse) x.lse[ext_lse_index(x, layer, h, tok) + row] = xt_add_log2(M, sum);
 }
 
+// Of this warp's 32 rows (a bit each), those computed again whole (redo: nothing of them is stored yet; the two groups, which
+// agree on them, take every other one) and those with elements that are not finite among the group's columns as stored, which
+// are replaced.  lse: of each lane's row.  After the stores, for all of a piece in one call: what is rare stays out of the
+// way of the rest (called for a block of columns at a time, from their loop, it cost 5 tokens behind 2048 rows 0.7 of 25 us).
+template <bool KV8>
+__device__ __noinline__ void xt_rows_again(const ExtendTcParams& p, int d, unsigned redo, unsigned bad, float lse, uint32_t busy) {
+  const ExtendParams& x = p.x;
+  auto word = [&](int w) { return __shfl_sync(0xffffffffu, d, w); };
+  const int lane = threadIdx.x & 31, wg = threadIdx.x >> 7, wq = (threadIdx.x >> 5) & 3, h = word(kPwHead), layer = word(kPwLayer), tok = word(kPwTok);
+  const bool whole = word(kPwParts) == 1;
+  const size_t piece = (size_t)p.part_rows;
+  float* part = p.part + (size_t)word(kPwPlace) * (piece * kXtPartFloats);
+  if (lane == 0) xt_busy(busy, 1);
+  redo &= wg == 0 ? 0x55555555u : 0xaaaaaaaau;
+  for (unsigned left = redo | bad; left; left &= left - 1) {
+    const int who = __ffs(left) - 1, row = wq * 32 + who, ti = row / x.G;
+    const bool full = (redo >> who) & 1u;
+    float row_lse = __shfl_sync(0xffffffffu, lse, who);
+    float4 y = xt_row_again<KV8>(p, d, row, full, row_lse);
+    if (!full && (lane >> 4) != wg) continue;  // (the other group's columns)
+    auto keep = [](float was, float now) { return was * 0.f == 0.f ? was : now; };
+    if (whole) {
+      uint2* at = reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(x.out) + (((size_t)layer * x.total + tok + ti) * x.Hq + h * x.G + (row - ti * x.G)) * 128 + 4 * lane);
+      if constexpr (KV8) y = make_float4(y.x * p.out_scale, y.y * p.out_scale, y.z * p.out_scale, y.w * p.out_scale);
+      if (!full) {
+        const uint2 o = __ldcg(at);
+        y = make_float4(keep(__uint_as_float(o.x << 16), y.x), keep(__uint_as_float(o.x & 0xffff0000u), y.y), keep(__uint_as_float(o.y << 16), y.z),
+                        keep(__uint_as_float(o.y & 0xffff0000u), y.w));
+      }
+      *at = make_uint2(pack_bf16x2(y.x, y.y), pack_bf16x2(y.z, y.w));
+      if (full && lane == 0 && x.lse) x.lse[ext_lse_index(x, layer, h, tok) + row] = row_lse;
+    } else {
+      float4* at = reinterpret_cast<float4*>(part) + (size_t)lane * piece + row;
+      if (!full) {
+        const float4 o = __ldcg(at);
+        y = make_float4(keep(o.x, y.x), keep(o.y, y.y), keep(o.z, y.z), keep(o.w, y.w));
+      }
+      __stcg(at, y);
+      if (full && lane == 0) __stcg(part + 128 * piece + row, row_lse);
+    }
+  }
+  __syncwarp();
+  if (lane == 0) xt_busy(busy, -1);
+}
+
 // The end of a piece, by the eight softmax warps: a group's 64 columns of the output, or of its part of an item that
 // other CTAs share.
 template <bool KV8>
@@ -367,7 +438,8 @@ __device__ __noinline__ void xt_epilogue(const ExtendTcParams& p, int d, int ord
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, wg = warp >> 2, wq = warp & 3;
   const int r = wq * 32 + lane, rows = word(kPwRows), h = word(kPwHead), layer = word(kPwLayer), tok = word(kPwTok);
   const bool whole = word(kPwParts) == 1;
-  mbar_wait(bar0 + 8 * 12, (uint32_t)(ord & 1), s_abort, x.err, kPfSpinLimit);
+  const uint32_t abort_flag = bar0 + 124u, busy = bar0 + 128u;
+  xt_wait(bar0 + 8 * 12, (uint32_t)(ord & 1), abort_flag, p);
   tc5::fence_after_sync();
   if (wq * 32 >= rows) {  // no query in this warp's rows
     mbar_arrive(bar0 + 8 * 7);
@@ -380,11 +452,14 @@ __device__ __noinline__ void xt_epilogue(const ExtendTcParams& p, int d, int ord
   float* part = p.part + (size_t)word(kPwPlace) * (piece * kXtPartFloats);
   // Out of range, or not a number; or the reference tiles held nothing above -inf, so that the sum has no reference (or the row
   // of a whole item no sum: it sees itself, so all it sees is -inf).
-  const bool redo = mine && (!(l < kXtSumMax) || (ref == -CUDART_INF_F && (whole || l > 0.f)));
-  float lse = l > 0.f ? xt_add_log2(ref, l) : -CUDART_INF_F;
+  const bool gave_up = __any_sync(0xffffffffu, *s_abort != 0);  // (nothing is computed again then, nor stored)
+  const bool redo = mine && !gave_up && (!(l < kXtSumMax) || (ref == -CUDART_INF_F && (whole || l > 0.f)));
+  const float lse = l > 0.f ? xt_add_log2(ref, l) : -CUDART_INF_F;
   const float f = l > 0.f ? 1.f / l : 0.f;
   __nv_bfloat16* obase = static_cast<__nv_bfloat16*>(x.out) + (((size_t)layer * x.total + tok) * x.Hq + h * x.G) * 128;
   const uint32_t t_row = tO + ((uint32_t)(wq * 32) << 16);
+  const unsigned redone = __ballot_sync(0xffffffffu, redo);
+  bool finite = true;  // this row's columns here are
 #pragma unroll 1
   for (int c0 = 64 * wg; c0 < 64 * wg + 64; c0 += 32) {
     uint32_t o[32];
@@ -407,24 +482,7 @@ __device__ __noinline__ void xt_epilogue(const ExtendTcParams& p, int d, int ord
     }
     float p0, p1;
     tc5::f2_unpack(tc5::f2_add(probe[0], probe[1]), p0, p1);
-    unsigned again = __ballot_sync(0xffffffffu, mine && (redo || !(p0 + p1 == 0.f)));
-    while (again) {
-      const int who = __ffs(again) - 1;
-      again &= again - 1;
-      const bool full = __shfl_sync(0xffffffffu, redo ? 1 : 0, who) != 0;
-      float new_lse = __shfl_sync(0xffffffffu, lse, who);
-      const float4 y = xt_row_again<KV8>(p, d, wq * 32 + who, full, new_lse);
-      __syncwarp();
-      reinterpret_cast<float4*>(stage)[lane] = y;
-      __syncwarp();
-      if (lane == who) {
-        lse = new_lse;
-#pragma unroll
-        for (int e = 0; e < 32; ++e)
-          if (full || !(__uint_as_float(o[e]) * 0.f == 0.f)) o[e] = reinterpret_cast<const uint32_t*>(stage)[c0 + e];
-      }
-      __syncwarp();
-    }
+    finite = finite && p0 + p1 == 0.f;
     if (whole) {
       // rounded, through the warp's staging tile [32 rows][64 B] (16-byte chunks swizzled), so that the stores are 64-byte
       // pieces of rows
@@ -449,10 +507,10 @@ __device__ __noinline__ void xt_epilogue(const ExtendTcParams& p, int d, int ord
         const int row = 8 * i + (lane >> 2), chunk = lane & 3;
         const uint4 v = *reinterpret_cast<const uint4*>(stage + row * 64 + ((chunk ^ ((row >> 1) & 3)) << 4));
         const int rr = wq * 32 + row, ti = (int)((uint32_t)rr * g_inv >> 16);
-        if (rr < rows && store) *reinterpret_cast<uint4*>(obase + (ti * x.Hq + (rr - ti * x.G)) * 128 + c0 + chunk * 8) = v;
+        if (rr < rows && store && !((redone >> row) & 1u)) *reinterpret_cast<uint4*>(obase + (ti * x.Hq + (rr - ti * x.G)) * 128 + c0 + chunk * 8) = v;
       }
       __syncwarp();
-    } else if (mine && !*s_abort) {
+    } else if (mine && !redo && !*s_abort) {
       float4* dst = reinterpret_cast<float4*>(part) + (size_t)c0 / 4 * piece + r;
 #pragma unroll
       for (int e = 0; e < 8; ++e)
@@ -460,10 +518,13 @@ __device__ __noinline__ void xt_epilogue(const ExtendTcParams& p, int d, int ord
                make_float4(__uint_as_float(o[4 * e]), __uint_as_float(o[4 * e + 1]), __uint_as_float(o[4 * e + 2]), __uint_as_float(o[4 * e + 3])));
     }
   }
-  if (wg == 0 && mine && !*s_abort) {
+  if (wg == 0 && mine && !redo && !*s_abort) {
     if (!whole) __stcg(part + 128 * piece + r, lse);
     else if (x.lse) x.lse[ext_lse_index(x, layer, h, tok) + r] = lse;
   }
+  // Elements of the others that are not finite: something V holds, seen or hidden.
+  const unsigned bad = __ballot_sync(0xffffffffu, mine && !redo && !gave_up && !finite);
+  if (redone | bad) xt_rows_again<KV8>(p, d, redone, bad, lse, busy);
 }
 
 template <bool KV8, bool MODS>
@@ -491,6 +552,7 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
   if (tid == 0) {
     for (int i = 0; i < 15; ++i) mbar_init(bar(i), i == 7 ? 2 * kXtRows : (i == 8 || i == 9) ? kXtRows : KV8 && (i == 1 || i == 2) ? 2 : 1);
     *s_abort = 0;
+    s_abort[1] = 0;  // (warps that compute rows again)
     if ((smem_u32(sm) & 1023u) != 0u) {
       atomicOr(x.err, kErrStreamBounds);
       *s_abort = 1;
@@ -577,7 +639,7 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
         // S of tile g - 2 has read it, a V stage when O += P V of tile g - 2 has.
         const bool new_q = warp == 8 && j == 0;
         const int done = new_q ? g - 1 : g - 2, freed = KV8 || warp == 8 ? 5 : 10;
-        if (done >= 0) mbar_wait(bar(freed + (done & 1)), (uint32_t)((done >> 1) & 1), s_abort, x.err, kPfSpinLimit);
+        if (done >= 0) xt_wait(bar(freed + (done & 1)), (uint32_t)((done >> 1) & 1), bar0 + 124u, p);
         __syncwarp();
         if (*s_abort) break;
         if (new_q) load_q();
@@ -655,14 +717,14 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
       while (slot < slot_end && !*s_abort) {
         const int st = g & 1;
         if constexpr (is_s) {
-          mbar_wait(bar(1 + st), (uint32_t)((g >> 1) & 1), s_abort, x.err, kPfSpinLimit);
+          xt_wait(bar(1 + st), (uint32_t)((g >> 1) & 1), bar0 + 124u, p);
           // S of tile g overwrites the columns P of tile g - 2 is read from
-          if (g >= 2) mbar_wait(bar(10 + st), (uint32_t)(((g - 2) >> 1) & 1), s_abort, x.err, kPfSpinLimit);
-          if (j == 0) mbar_wait(bar(0), (uint32_t)(ord & 1), s_abort, x.err, kPfSpinLimit);
+          if (g >= 2) xt_wait(bar(10 + st), (uint32_t)(((g - 2) >> 1) & 1), bar0 + 124u, p);
+          if (j == 0) xt_wait(bar(0), (uint32_t)(ord & 1), bar0 + 124u, p);
         } else {
-          if constexpr (!KV8) mbar_wait(bar(3 + st), (uint32_t)((g >> 1) & 1), s_abort, x.err, kPfSpinLimit);  // (8-bit rows: written before P)
-          mbar_wait(bar(8 + st), (uint32_t)((g >> 1) & 1), s_abort, x.err, kPfSpinLimit);
-          if (j == 0 && ord > 0) mbar_wait(bar(7), (uint32_t)((ord - 1) & 1), s_abort, x.err, kPfSpinLimit);  // O of the piece before has been read
+          if constexpr (!KV8) xt_wait(bar(3 + st), (uint32_t)((g >> 1) & 1), bar0 + 124u, p);  // (8-bit rows: written before P)
+          xt_wait(bar(8 + st), (uint32_t)((g >> 1) & 1), bar0 + 124u, p);
+          if (j == 0 && ord > 0) xt_wait(bar(7), (uint32_t)((ord - 1) & 1), bar0 + 124u, p);  // O of the piece before has been read
         }
         __syncwarp();
         tc5::fence_after_sync();
@@ -687,7 +749,7 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
         const bool last = ++j == nkt;
         if constexpr (!kLoaders) {
           if (l_slot < slot_end || last) {  // the stage of this tile (and, with a piece's last S, Q) is free when its product is done
-            mbar_wait(bar((is_s ? 5 : 10) + st), (uint32_t)((g >> 1) & 1), s_abort, x.err, kPfSpinLimit);
+            xt_wait(bar((is_s ? 5 : 10) + st), (uint32_t)((g >> 1) & 1), bar0 + 124u, p);
             __syncwarp();
             if (*s_abort) break;
             load(g + 2);
@@ -789,10 +851,10 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
         // 8-bit rows: V goes to its stage while S is computed, once O += P V of tile g - 2 has read it (4096 behind 4096: 580 -> 568 us);
         // with caps, biases and windows after it, as the two waits cost more than they hide (a capped step of 64: 112 against 119 us).
         if constexpr (KV8 && !MODS) {
-          if (g >= 2) xt_wait(bar(10 + (g & 1)), (uint32_t)(((g - 2) >> 1) & 1), abort_flag, x.err);
+          if (g >= 2) xt_wait(bar(10 + (g & 1)), (uint32_t)(((g - 2) >> 1) & 1), abort_flag, p);
           widen_v();
         }
-        xt_wait(bar(5 + (g & 1)), (uint32_t)((g >> 1) & 1), abort_flag, x.err);  // S of this tile is complete
+        xt_wait(bar(5 + (g & 1)), (uint32_t)((g >> 1) & 1), abort_flag, p);  // S of this tile is complete
         tc5::fence_after_sync();
         if constexpr (KV8 && MODS) widen_v();  // (S of this tile was issued after O += P V of tile g - 2 had read the stage)
         if (live) {
@@ -1084,7 +1146,7 @@ extend_mass_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_con
     int g = 0;
     while (cur.it < n_items && !*s_abort) {
       if constexpr (!KV8) {
-        if (cur.ord > 0) mbar_wait(bar(6), (uint32_t)((cur.ord - 1) & 1), s_abort, x.err, kPfSpinLimit);  // the item before has read its K
+        if (cur.ord > 0) mbar_wait(bar(6), (uint32_t)((cur.ord - 1) & 1), s_abort, x.err, p.wait_limit);  // the item before has read its K
         __syncwarp();
         if (!*s_abort && tc5::elect_one()) {
           const int slab = slab_of(cur);
@@ -1097,7 +1159,7 @@ extend_mass_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_con
         __syncwarp();
       }
       for (int j = 0; j < cur.n_step; ++j, ++g) {
-        if (g > 0) mbar_wait(bar(3), (uint32_t)((g - 1) & 1), s_abort, x.err, kPfSpinLimit);  // both groups' S of the step before have read its Q
+        if (g > 0) mbar_wait(bar(3), (uint32_t)((g - 1) & 1), s_abort, x.err, p.wait_limit);  // both groups' S of the step before have read its Q
         __syncwarp();
         if (*s_abort) break;
         if (tc5::elect_one()) {
@@ -1129,12 +1191,12 @@ extend_mass_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_con
     xm_seek(cur, 0, n_items, p, sh, true);
     int g = 0;
     while (cur.it < n_items && !*s_abort) {
-      mbar_wait(bar(0), (uint32_t)(cur.ord & 1), s_abort, x.err, kPfSpinLimit);
+      mbar_wait(bar(0), (uint32_t)(cur.ord & 1), s_abort, x.err, p.wait_limit);
       for (int j = 0; j < cur.n_step; ++j, ++g) {
-        mbar_wait(bar(1), (uint32_t)(g & 1), s_abort, x.err, kPfSpinLimit);
+        mbar_wait(bar(1), (uint32_t)(g & 1), s_abort, x.err, p.wait_limit);
 #pragma unroll
         for (int grp = 0; grp < 2; ++grp) {
-          if (g > 0) mbar_wait(bar(4 + grp), (uint32_t)((g - 1) & 1), s_abort, x.err, kPfSpinLimit);
+          if (g > 0) mbar_wait(bar(4 + grp), (uint32_t)((g - 1) & 1), s_abort, x.err, p.wait_limit);
           __syncwarp();
           tc5::fence_after_sync();
           if (*s_abort) break;
@@ -1184,7 +1246,7 @@ extend_mass_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_con
           XtCodes codes[4];
 #pragma unroll
           for (int q = 0; q < 4; ++q) xt_load_codes(codes[q], src, cur.k0 + wg * kXmKeys + wq * 32 + 8 * q, cur.n + cur.t, lane);
-          if (cur.ord > 0) xt_wait(bar(6), (uint32_t)((cur.ord - 1) & 1), abort_flag, x.err);
+          if (cur.ord > 0) xt_wait(bar(6), (uint32_t)((cur.ord - 1) & 1), abort_flag, p);
 #pragma unroll
           for (int q = 0; q < 4; ++q) xt_store_codes<false>(codes[q], sm + wg * kXmKBytes, kXmKBytes / 2, wq * 32 + 8 * q, lane);
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -1235,7 +1297,7 @@ extend_mass_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_con
         const bool full = __all_sync(0xffffffffu, c_lo == 0 && c_hi == step_rows);
         const float off0 = (float)i0 - rel;
         const bool beside = biased && prefix > 0;  // rows of later positions may be seen
-        xt_wait(bar(2 + wg), (uint32_t)(g & 1), abort_flag, x.err);
+        xt_wait(bar(2 + wg), (uint32_t)(g & 1), abort_flag, p);
         tc5::fence_after_sync();
         uint64_t sum2[2] = {0ull, 0ull};
 #pragma unroll 1

@@ -209,6 +209,51 @@ def test_logits_of_minus_infinity(dtype, d, past, low):
     c.close()
 
 
+@pytest.mark.parametrize("dtype,scale", [("bf16", 1.0), ("bf16_kv8", 0.5)])
+@pytest.mark.parametrize("past,new,opt", [((2000,), (8,), {}), ((700,), (300,), {}), ((380,) * 33, (20,) * 33, {}), ((900, 300), (40, 1), dict(softcap=1000.0))],
+                         ids=["parts", "long", "whole items", "capped"])
+def test_old_keys_far_above_the_newest(dtype, scale, past, new, opt):
+    """The oldest rows' logits lie hundreds above all newer ones for every query: no reference taken from the newest rows
+    holds, every row's answer is finite."""
+    c, seen = build(dtype=dtype, q_heads=8, kv_heads=2, past=past, cap=max(p + t for p, t in zip(past, new)) + 20, scale=scale)
+    g = torch.Generator(device="cuda").manual_seed(31)
+    for b, n in enumerate(past):
+        k, v = (torch.randn((1, 2, n, 128), generator=g, device="cuda") for _ in range(2))
+        k[:, :, :64] *= 40.0
+        c.prefill_seq(b, k.to(torch.bfloat16), v.to(torch.bfloat16), n_pinned=0)
+    check(c, list(seen), list(new), scale=scale, seed=31, sharp=2.0, **opt)
+    c.close()
+
+
+@pytest.mark.parametrize("dtype,d", TYPES)
+@pytest.mark.parametrize("past,new", [((1500,), (30,)), ((64, 0, 500), (7, 120, 1))])
+def test_slopes_below_zero(dtype, d, past, new):
+    """A bias that grows with the distance: every row's largest logit is its oldest."""
+    c, seen = build(dtype=dtype, d=d, q_heads=8, kv_heads=2, past=past, cap=1600)
+    check(c, seen, list(new), scale=SCALE, seed=33, slopes=-2.0 ** -torch.arange(0, 8).float())
+    c.close()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "bf16_kv8"])
+def test_waits_outlast_rows_computed_again(dtype):
+    """Every row is computed again, which takes milliseconds, while the other warps of its CTA may poll a few thousand times."""
+    c, seen = build(dtype=dtype, q_heads=8, kv_heads=2, past=(6000,), cap=6400)
+    c.set_wait_limit(4096)
+    n_new = [300]
+    q, k, v = chunk(c, n_new, 37)
+    slopes = -2.0 ** -torch.arange(0, 8, device="cuda").float()
+    out, again = torch.empty_like(q), torch.empty_like(q)
+    c.extend_attn(q, k, v, out, n_new, slopes=slopes, stage=True)
+    c.synchronize()
+    c.poll_error()
+    c.set_wait_limit(1 << 22)
+    c.extend_attn(q, k, v, again, n_new, slopes=slopes, stage=True)
+    c.synchronize()
+    c.poll_error()
+    assert torch.isfinite(out.float()).all() and torch.equal(out, again)
+    c.close()
+
+
 @pytest.mark.parametrize("dtype", ["bf16_kv8", "bf16"])
 def test_calls_back_to_back_with_other_rows(dtype):
     """Staged calls that overwrite one another's rows, nothing between them, equal the same calls each waited for."""
