@@ -1068,7 +1068,7 @@ extend_mass_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_con
   auto bar = [&](int i) { return bar0 + 8u * (uint32_t)i; };
   uint32_t* s_tmem = reinterpret_cast<uint32_t*>(bars + 15);
   volatile int* s_abort = reinterpret_cast<volatile int*>(s_tmem + 1);
-  int* s_flag = reinterpret_cast<int*>(s_tmem + 2);
+  int* s_flag = reinterpret_cast<int*>(s_tmem + 3);  // (the word between stays 0: no rows are computed again here, see xt_wait)
   float* s_warp = reinterpret_cast<float*>(bars + 24);
   float* s_tok = s_warp + 8 * kXmWarpFloats;    // token of a column within its step
   int* s_n = reinterpret_cast<int*>(s_tok + kXmRows);
@@ -1080,6 +1080,7 @@ extend_mass_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_con
   if (tid == 0) {
     for (int i = 0; i < 8; ++i) mbar_init(bar(i), i == 0 && KV8 ? 8 : i == 4 || i == 5 ? kXmKeys : 1);
     *s_abort = 0;
+    s_abort[1] = 0;
     if ((smem_u32(sm) & 1023u) != 0u) {
       atomicOr(x.err, kErrStreamBounds);
       *s_abort = 1;
