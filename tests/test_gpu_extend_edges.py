@@ -277,3 +277,31 @@ def test_calls_back_to_back_with_other_rows(dtype):
     for x, y in zip(res[0][0] + res[0][1], res[1][0] + res[1][1]):
         assert torch.equal(x, y)
     a.close(), b.close()
+
+
+@pytest.mark.parametrize("opt", [dict(), dict(softcap=20.0, slopes=True, window=120, prefix=[3, 50, 0])], ids=["plain", "options"])
+@pytest.mark.parametrize("dtype", ["bf16", "bf16_kv8"])
+def test_the_fp32_form_at_head_dim_128(dtype, opt):
+    """Launch variant 1: nothing but the output is rounded to 16 bits."""
+    opt = dict(opt)
+    if opt.get("slopes"):
+        opt["slopes"] = 2.0 ** -torch.arange(1, 9).float()
+    c, seen = build(dtype=dtype, q_heads=8, kv_heads=2, past=(150, 0, 333), cap=512, evict_to=200)
+    c.set_launch(0, 1)
+    n_new = [6, 90, 33]
+    q, k, v = chunk(c, n_new, 35)
+    s = SCALE if dtype == "bf16_kv8" else 1.0
+    ref, mass, tol, mass_tol, rows = R.extend(R.State(c, s, s), seen, q, k, v, n_new, **opt)
+    lens = [c.len(b) for b in range(3)]
+    if "slopes" in opt:
+        opt["slopes"] = opt["slopes"].cuda()
+    out, buf = torch.empty_like(q), torch.zeros((1, 3, 2, 512), device="cuda")
+    c.extend_attn(q, k, v, out, n_new, mass=buf, **opt)
+    c.synchronize()
+    c.poll_error()
+    assert ((out.double().cpu() - ref).abs() <= tol).all()
+    for (l, b, h), m in mass.items():
+        assert ((buf[l, b, h, : lens[b] + n_new[b]].double().cpu() - m).abs() <= mass_tol[l, b, h]).all()
+        K, V, pos, _ = c.export_slab(l, b, h)
+        assert torch.equal(R.State.value(K, s), rows[l, b, h][0]) and torch.equal(R.State.value(V, s), rows[l, b, h][1])
+    c.close()
