@@ -295,7 +295,7 @@ dynts_status_t dynts_extend_attn_layer(dynts_cache_t* c, int layer, const void* 
 
 /* Takes over the first n_accept[b] (host [Nb]) rows of the chunk staged last: the sequences grow by
  * them, the other staged rows are forgotten.  Their scores are what s_new gave (or 0).
- * DYNTS_ERR_STATE if a call that changes rows or lengths came between. */
+ * DYNTS_ERR_STATE if a call that changes rows, lengths or the scales of 8-bit rows came between. */
 dynts_status_t dynts_extend_commit(dynts_cache_t* c, const int* n_accept);
 
 /* Rotary positions with one or several axes, for the queries and keys handed to this library (which

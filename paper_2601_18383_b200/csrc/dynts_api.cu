@@ -1268,6 +1268,8 @@ dynts_status_t dynts_cache_set_kv_scale(dynts_cache_t* c, float k_scale, float v
   if (c->ready)
     for (int b = 0; b < c->cfg.batch; ++b)
       if (c->len_h[b] > 0) return fail(DYNTS_ERR_STATE, "rows are already stored with the current scales");
+  if (c->layer_cursor != 0) return fail(DYNTS_ERR_STATE, "a layer-by-layer step is in progress");  // (its first layers' rows are stored)
+  c->staged_h.clear();  // rows staged behind empty sequences are codes of the old scales
   c->k_scale = k_scale;
   c->v_scale = v_scale;
   return DYNTS_OK;

@@ -305,3 +305,25 @@ def test_the_fp32_form_at_head_dim_128(dtype, opt):
         K, V, pos, _ = c.export_slab(l, b, h)
         assert torch.equal(R.State.value(K, s), rows[l, b, h][0]) and torch.equal(R.State.value(V, s), rows[l, b, h][1])
     c.close()
+
+
+def test_scales_between_a_staged_chunk_and_its_commit():
+    """Rows staged into an empty cache are codes of the scales then set: other scales later forget them; within a chunk that goes
+    layer by layer the scales stay."""
+    c, _ = build(dtype="bf16_kv8", layers=2, q_heads=8, kv_heads=2, past=(0, 0), cap=64)
+    q, k, v = chunk(c, [5, 2], 7)
+    out = torch.empty_like(q)
+    c.extend_attn(q, k, v, out, [5, 2], stage=True)
+    c.set_kv_scale(0.25, 0.25)
+    with pytest.raises(D.DyntsError) as e:
+        c.extend_commit([5, 2])
+    assert e.value.status == D.DYNTS_ERR_STATE and c.len(0) == 0
+    c.extend_attn_layer(0, q[0], k[0], v[0], out[0], [5, 2])
+    with pytest.raises(D.DyntsError) as e:
+        c.set_kv_scale(0.05, 0.05)
+    assert e.value.status == D.DYNTS_ERR_STATE
+    c.extend_attn_layer(1, q[1], k[1], v[1], out[1], [5, 2])
+    for l in range(2):
+        K, V, _, _ = c.export_slab(l, 0, 1)
+        assert torch.equal(K.view(torch.float8_e4m3fn).float(), R.e4m3(k[l, :5, 1].cpu(), 0.25).float())
+    c.close()
