@@ -341,7 +341,10 @@ def _host_ints(x):
         return x.data_ptr(), x
     if hasattr(x, "ctypes") and str(x.dtype) == "int32" and x.ndim == 1 and x.flags["C_CONTIGUOUS"]:
         return x.ctypes.data, x
-    arr = (C.c_int * len(x))(*[int(v) for v in x])
+    values = [int(v) for v in x]
+    if values and not (-2 ** 31 <= min(values) and max(values) < 2 ** 31):  # (ctypes would cut them)
+        _invalid("host counts must fit 32 bits")
+    arr = (C.c_int * len(values))(*values)
     return C.addressof(arr), arr
 
 
@@ -449,6 +452,8 @@ def rope(q, k, positions, q_out=None, k_out=None, theta=10000.0, sections=None, 
             _invalid("the section of one axis holds all pairs")
     if rot_dim is None:
         rot_dim = d if sections is None else 2 * sum(sections)
+    if rot_dim > d or (sections is not None and not 0 <= min(sections) <= max(sections) <= d):  # (also what ctypes would cut)
+        _invalid("the sections and rot_dim must lie within d")
     flags = (DYNTS_ROPE_ADJACENT if adjacent else 0) | (DYNTS_ROPE_ROUND_ROBIN if round_robin else 0)
     args = (q.data_ptr(), k_ptr, positions.data_ptr(), q_out.data_ptr(), k_out_ptr, n, hq, hkv, d, rot_dim, axes, sec, flags, theta, dtype, st,
             t.stream(dev))
@@ -575,6 +580,8 @@ class Cache:
             if len(prefix) != self.batch:
                 _invalid("prefix needs a count for each sequence")
             prefixes, keep_p = _host_ints(prefix)
+        if not 0 <= window < 2 ** 31:
+            _invalid("window must be an int of 32 bits, not negative")
         opts = dynts_extend_opts_t(softcap, None if slopes is None else slopes.data_ptr(), window, prefixes, None if s_new is None else s_new.data_ptr(),
                                    None if mass is None else mass.data_ptr(), 1 if stage else 0, *strides)
         need = lib.dynts_extend_scratch_bytes(self.handle, counts, self.layers if layer is None else 1)

@@ -149,6 +149,25 @@ def test_windows_as_wide_as_an_int(dtype, d, window, q_heads, kv_heads):
     c.close()
 
 
+def test_windows_beyond_an_int_are_refused():
+    c, _ = build(q_heads=8, kv_heads=2, past=(60,), cap=128)
+    q, k, v = chunk(c, [4], 7)
+    for bad in (dict(window=2 ** 31), dict(window=2 ** 32 + 5), dict(prefix=[2 ** 32 + 2])):
+        with pytest.raises(D.DyntsError) as e:
+            c.extend_attn(q, k, v, torch.empty_like(q), [4], stage=True, **bad)
+        assert e.value.status == D.DYNTS_ERR_INVALID_ARG
+    c.close()
+
+
+def test_sections_beyond_an_int_are_refused():
+    q = torch.randn((3, 2, 128), device="cuda")
+    pos = torch.zeros((2, 3), dtype=torch.int32, device="cuda")
+    for bad in (dict(sections=[2 ** 32 + 20, 12], rot_dim=64), dict(sections=[2 ** 32 + 20, 12]), dict(sections=[20, 12], rot_dim=2 ** 32 + 64), dict(sections=[-20, 52])):
+        with pytest.raises(D.DyntsError) as e:
+            D.rope(q, None, pos, **bad)
+        assert e.value.status == D.DYNTS_ERR_INVALID_ARG
+
+
 def plain(state, q, k, v, n, dtype, kv_heads):
     """Outputs of one sequence of one layer in 64 bits, causal: [t, Hq, d]."""
     t, hq, d = q.shape
