@@ -452,7 +452,7 @@ def rope(q, k, positions, q_out=None, k_out=None, theta=10000.0, sections=None, 
             _invalid("the section of one axis holds all pairs")
     if rot_dim is None:
         rot_dim = d if sections is None else 2 * sum(sections)
-    if rot_dim > d or (sections is not None and not 0 <= min(sections) <= max(sections) <= d):  # (also what ctypes would cut)
+    if rot_dim > d or (sections is not None and any(not 0 <= x <= d for x in sections)):  # (also what ctypes would cut)
         _invalid("the sections and rot_dim must lie within d")
     flags = (DYNTS_ROPE_ADJACENT if adjacent else 0) | (DYNTS_ROPE_ROUND_ROBIN if round_robin else 0)
     args = (q.data_ptr(), k_ptr, positions.data_ptr(), q_out.data_ptr(), k_out_ptr, n, hq, hkv, d, rot_dim, axes, sec, flags, theta, dtype, st,

@@ -82,7 +82,7 @@ struct ExtendParams {
 // CTA c takes the shares [c * q + min(c, rem), ...).  What CTA c does of item i is described by 32 words at slot i + c
 // (an item's parts and a CTA's pieces both lie side by side).
 constexpr int kPlanWords = 32;
-enum PlanWord { kPwTiles, kPwFirst, kPwTotal, kPwTok, kPwLayer, kPwHead, kPwHeld, kPwTok0, kPwRows, kPwNew, kPwSlab, kPwParts, kPwPlace, kPwBase, kPwList, kPwPrefix, kPwSeen };
+enum PlanWord { kPwTiles, kPwFirst, kPwTok, kPwLayer, kPwHead, kPwHeld, kPwTok0, kPwRows, kPwNew, kPwSlab, kPwParts, kPwPlace, kPwBase, kPwList, kPwPrefix, kPwSeen };
 struct ExtendPlan {
   unsigned cum[kExtSeqs + 1];  // shares before each sequence's first item
   unsigned per[kExtSeqs];      // shares of an item
@@ -181,7 +181,6 @@ __device__ __forceinline__ void ext_write_plan(const ExtendParams& p, const Exte
           if (lo < hi) q.words[(size_t)(item + (int)ca + rank + __popc(has & ((1u << lane) - 1u))) * kPlanWords + kPwList] = place;
           w[kPwTiles] = hi - lo;
           w[kPwFirst] = first + lo;
-          w[kPwTotal] = total;
           w[kPwTok] = p.seqs.tok0[s] + i0;
           w[kPwLayer] = layer;
           w[kPwHead] = h;
