@@ -1551,12 +1551,12 @@ dynts_status_t launch_extend_tc_as(dynts_cache* c, dynts::ExtendTcParams& p, uns
 // An item's beginning and end take about seven.  Cut anywhere (equal shares of all key tiles), a CTA begins and ends items that
 // others share and a second kernel joins them: another six, and up to twelve more where every CTA writes parts of 128 rows.
 // Whole items need no join but leave CTAs with unequal work.  Measured (8 KV heads, groups of four; us, cut / whole):
-// 1 token, 8 items of 8 tiles 15.6 / 14.6, of 16 tiles 16.9 / 20.0; 20 tokens in each of 33 sequences, 264 items of 16 tiles
-// 51.5 / 40.3; 70 in each of 16, 384 items of 9 tiles 47.3 / 40.8, of 17 tiles 57.7 / 58.3; prompts of 33 to 1100 tokens, 1528
-// items 122 / 106.
+// 1 token, 8 items of 8 tiles 15.0 / 14.0, of 16 tiles 16.0 / 18.9; 20 tokens in each of 33 sequences, 264 items of 16 tiles
+// 48.2 / 35.8; 70 in each of 16, 384 items of 9 tiles 41.6 / 35.7, of 17 tiles 51.9 / 51.7; prompts of 33 to 1100 tokens, 1528
+// items 111 / 108; 8-bit rows, 4096 tokens behind 4096 rows 540 / 580.
 constexpr double kExtendItemCost = 7, kExtendJoinCost = 6, kExtendPartCost = 12;
 constexpr int kExtendMinTiles = 4;   // key tiles per CTA below which the grid shrinks, if items are cut
-constexpr int kExtendItemTiles = 4;  // what an item counts beside its key tiles in the shares (packed prompts, cut: 146 us at 2, 121 at 4 and 6)
+constexpr int kExtendItemTiles = 4;  // what an item counts beside its key tiles in the shares (packed prompts, cut: 125 us at 2, 111 at 4)
 
 // The list of key tiles and its shares (see ExtendPlan); *grid: CTAs of the tensor-core kernel; *whole: no item is cut.
 dynts_status_t plan_extend(const dynts_cache* c, const dynts::ExtendParams& x, const ExtendScratch& m, char* scratch, dynts::ExtendPlan& p, unsigned* grid, bool* whole) {

@@ -380,7 +380,7 @@ constexpr size_t ext_generic_smem(int d) {  // Q [32][d], K [32][d + 4], V [32][
 // Bound by FMA and shared-memory issue where there are many items; where they are few, by the chain of a tile's
 // steps, so the key tiles of an item are dealt to a cluster of up to eight CTAs, which join their parts through
 // one another's shared memory, in the order of their ranks (fp32, head_dim 64, 48 tokens behind 131 rows, six items:
-// 44 us with a CTA per item, 11 us with clusters, the storing kernel included).
+// 44 us with a CTA per item, 11 to 12 us with clusters, the storing kernel included).
 template <typename T, bool KV8>
 __global__ void __launch_bounds__(kExtGenericThreads) extend_generic_kernel(const __grid_constant__ ExtendParams p, int cluster) {
   extern __shared__ __align__(16) float ext_sm[];

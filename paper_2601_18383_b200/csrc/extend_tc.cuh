@@ -29,17 +29,19 @@
 // mbarriers as in the prompt attention (prefill_attn.cuh), the S buffer, stages and phases follow the flat tile index g.  Every warp
 // walks the CTA's pieces by the plan the storing kernel wrote (extend.cuh), a word per lane, the next piece's
 // prefetched.  Two CTAs of 384 threads leave 80 registers per thread and hardly any L1: code that spills or does
-// not stay in the instruction caches cost several times its instructions, so the loops are rolled and the end of a piece
-// is a function of its own (4096 tokens behind 4096 rows: 453 us with cursors in registers and everything unrolled,
-// 388 us now: 1.06 PFLOP/s, 0.66 of what cuBLAS reaches.  The tensor cores and the exponentials' unit are each busy for
+// not stay in the instruction caches cost several times its instructions, so the loops are rolled, the end of a piece
+// is a function of its own, and what is rare is called once from its end (spills: 32 bytes in the plain kernel, none with caps
+// and biases, 16 and 36 with 8-bit rows).  4096 tokens behind 4096 rows: 433 us a call with changing inputs, 0.95 PFLOP/s; 375 to
+// 395 us replayed on one state, 1.04 to 1.10 PFLOP/s, 0.65 to 0.68 of what cuBLAS reaches.  (Cursors in registers and everything
+// unrolled: 453 us when this stood at 388.)  The tensor cores and the exponentials' unit are each busy for a little more than
 // half of that time, in turns that the chain of a tile does not let overlap further: tiles of 128 keys with one S buffer,
-// or P over another CTA's wait, measured 390 to 400 us.)  Short items are bound by their own chain, about 7 us from the
+// or P over another CTA's wait, measured 2 to 12 us more.  Short items are bound by their own chain, about 7 us from the
 // load of Q to the store of the output, two of them per SM at a time.
 //
 // Rows of 16 bits arrive by TMA from the slabs.  8-bit rows (KV8) are read as codes and widened into the same swizzled
 // tiles: K to f16 (exact; queries are an f16 copy made by the storing kernel) by the two loading warps, a tile ahead in
-// registers; V to bf16 (exact; f16 weights would have no room for the fixed reference) by the group that weighs the
-// tile, while it waits for S.  The codes of coming tiles are asked into L2 meanwhile.
+// registers; V to bf16 (exact; f16 weights would have no room for the fixed reference, so the weights are rounded to 8 bits
+// here where a decode step over the same rows keeps 11) by the group that weighs the tile, while it waits for S.  The codes of coming tiles are asked into L2 meanwhile.
 //
 // A weight of zero times a value that is not finite is not a number, and the MMA multiplies whole
 // tiles: rows behind the chunk's end are zero (the storing kernel clears them, KV8 writes zeros), and an
@@ -57,8 +59,8 @@ namespace dynts {
 
 // 8-bit rows, and the plain row arithmetic: two warps of their own load (12 warps, 80 registers per thread).  With caps, biases
 // and windows the row arithmetic needs the registers more: the warps that issue the products load too (10 warps, 96).
-// (Loading warps against none: 4096 behind 4096, plain, 386 us against 488 us; ragged prompts with a bias 127 against 116 us, 1500
-// capped tokens 149 against 137 us.)
+// (Loading warps against none: 4096 behind 4096, plain, 374 us against 455 us; ragged prompts with a bias 109 against 108 us, 1500
+// capped tokens 136 against 133 us.)
 template <bool KV8, bool MODS>
 struct XtShape {
   static constexpr bool kLoaders = KV8 || !MODS;
@@ -848,8 +850,8 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
           xt_store_codes<true>(vc[1], vt, kPfKvBytes / 2, 16 * wq + 8, lane);
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         };
-        // 8-bit rows: V goes to its stage while S is computed, once O += P V of tile g - 2 has read it (4096 behind 4096: 580 -> 568 us);
-        // with caps, biases and windows after it, as the two waits cost more than they hide (a capped step of 64: 112 against 119 us).
+        // 8-bit rows: V goes to its stage while S is computed, once O += P V of tile g - 2 has read it (4096 behind 4096: 550 -> 540 us);
+        // with caps, biases and windows after it, as the two waits cost more than they hide (a capped step of 64: 93 against 98 us).
         if constexpr (KV8 && !MODS) {
           if (g >= 2) xt_wait(bar(10 + (g & 1)), (uint32_t)(((g - 2) >> 1) & 1), abort_flag, p);
           widen_v();
@@ -997,8 +999,8 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
 // of 128 columns per group: while a group's S is made the other three groups of the SM compute.  (With 128 keys per item
 // the Q tiles, read again from L2 for every item, bounded it: 1.25 times as long.  With steps of 64 query rows in two buffers
 // per group the products did: 57 cycles instead of 64 for half the work, as the keys' 4 KB are read all the same.)
-// Four ragged sequences of 3782 new tokens behind 2000 to 6000 rows: 220 us, 0.56 PFLOP/s of products, the exponentials' unit
-// busy for 0.64 of the time; what is left is unlike parts (0.15) and the waits of a part's beginning and end.
+// Four ragged sequences of 3782 new tokens behind 2000 to 6000 rows: 215 us, 0.57 PFLOP/s of products, the exponentials' unit
+// busy for 0.66 of the time; what is left is unlike parts (0.15) and the waits of a part's beginning and end.
 constexpr int kXmThreads = 320;
 constexpr int kXmKeys = 128;                      // keys per group
 constexpr int kXmItemKeys = 2 * kXmKeys;
