@@ -397,6 +397,7 @@ __device__ __noinline__ void xt_rows_again(const ExtendTcParams& p, int d, unsig
   const bool whole = word(kPwParts) == 1;
   const size_t piece = (size_t)p.part_rows;
   float* part = p.part + (size_t)word(kPwPlace) * (piece * kXtPartFloats);
+  __syncwarp();  // (other lanes' stores of a row that is read back here)
   if (lane == 0) xt_busy(busy, 1);
   redo &= wg == 0 ? 0x55555555u : 0xaaaaaaaau;
   for (unsigned left = redo | bad; left; left &= left - 1) {
