@@ -316,8 +316,10 @@ __device__ __forceinline__ float xt_cap(uint32_t (&sv)[32], const ExtendTcParams
 }
 
 // x + log2(sum), with the whole part of the logarithm taken out exactly: the approximation is off by 2^-22 of its result,
-// which at sums of 2^-33 (a reference with headroom) is 8e-6, and every weight of a mass would carry it.
+// which at sums of 2^-33 (a reference with headroom) is 8e-6, and every weight of a mass would carry it.  (Sums that are no
+// normal number have no such parts: 0, infinite, or not a number, and so is the result.)
 __device__ __forceinline__ float xt_add_log2(float x, float sum) {
+  if (!(sum >= 1.17549435e-38f && sum <= 3.4028235e38f)) return x + __log2f(sum);
   const int bits = __float_as_int(sum);
   return (x + (float)((bits >> 23) - 127)) + __log2f(__int_as_float((bits & 0x7fffff) | 0x3f800000));
 }

@@ -228,6 +228,27 @@ def test_logits_of_minus_infinity(dtype, d, past, low):
     c.close()
 
 
+@pytest.mark.parametrize("past,new", [(2000, 5), (300, 150), (0, 40)], ids=["parts", "more parts", "whole"])
+@pytest.mark.parametrize("dtype,d", TYPES)
+def test_a_key_that_is_not_a_number(dtype, d, past, new):
+    """The tokens that see it have no answer, and nor has the mass of any row they see; the other head keeps its own."""
+    at = 3
+    c, _ = build(dtype=dtype, d=d, q_heads=8, kv_heads=2, past=(past,), cap=past + new + 20)
+    q, k, v = chunk(c, [new], 43)
+    out, want = torch.empty_like(q), torch.empty_like(q)
+    mass, other = (torch.full((1, 1, 2, c.capacity), -3.0, device="cuda") for _ in range(2))
+    c.extend_attn(q, k, v, want, [new], mass=other, stage=True)
+    k[0, at, 1, 5] = math.nan
+    c.extend_attn(q, k, v, out, [new], mass=mass, stage=True)
+    c.synchronize()
+    c.poll_error()
+    G = 4
+    assert torch.equal(out[:, :, :G], want[:, :, :G]) and torch.equal(mass[0, 0, 0], other[0, 0, 0])
+    assert torch.equal(out[:, :at, G:], want[:, :at, G:]) and torch.isnan(out[:, at:, G:].float()).all()
+    assert torch.isnan(mass[0, 0, 1, : past + new]).all() and (mass[0, 0, 1, past + new:] == -3.0).all()
+    c.close()
+
+
 @pytest.mark.parametrize("dtype,scale", [("bf16", 1.0), ("bf16_kv8", 0.5)])
 @pytest.mark.parametrize("past,new,opt", [((2000,), (8,), {}), ((700,), (300,), {}), ((380,) * 33, (20,) * 33, {}), ((900, 300), (40, 1), dict(softcap=1000.0))],
                          ids=["parts", "long", "whole items", "capped"])
