@@ -224,7 +224,9 @@ dynts_status_t dynts_evict_noalloc_status(void* stream);
 
 /* Scales of a DYNTS_BF16_KV8 cache (default 1, 1).  Host floats; k_scale, v_scale > 0 and finite.
  * Allowed only while no sequence holds rows (DYNTS_ERR_STATE otherwise): stored codes are not
- * re-encoded.  Choose scale ~ max|x| / 448 of the tensor to use the format's range. */
+ * re-encoded.  Choose scale ~ max|x| / 448 of the tensor to use the format's range.
+ * DYNTS_ERR_STATE while rows are held or a layer-by-layer step is in progress; rows staged behind empty
+ * sequences are forgotten. */
 dynts_status_t dynts_cache_set_kv_scale(dynts_cache_t* c, float k_scale, float v_scale);
 
 /* ---- a chunk of new tokens against the cache ------------------------------------------------ */
