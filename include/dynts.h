@@ -297,8 +297,50 @@ dynts_status_t dynts_extend_attn_layer(dynts_cache_t* c, int layer, const void* 
 
 /* Takes over the first n_accept[b] (host [Nb]) rows of the chunk staged last: the sequences grow by
  * them, the other staged rows are forgotten.  Their scores are what s_new gave (or 0).
- * DYNTS_ERR_STATE if a call that changes rows, lengths or the scales of 8-bit rows came between. */
+ * DYNTS_ERR_STATE if a call that changes rows, lengths or the scales of 8-bit rows came between, or if the chunk was a tree. */
 dynts_status_t dynts_extend_commit(dynts_cache_t* c, const int* n_accept);
+
+/* dynts_extend_attn (layer -1) and dynts_extend_attn_layer with further options, all off when zero (more == NULL: all off):
+ *   sinks     s > 0, beside a window: rows whose position is below s are seen whatever the window (by tokens that
+ *             are not before them).  Without a window it has no effect
+ *   tree      device [n_total][4] int32, 16-byte aligned, as dynts_tree_plan writes it: the chunk's tokens are the nodes of trees (drafted
+ *             tokens, several to a place).  A node attends to the rows held (within the window), to its ancestors and to
+ *             itself; its position is the tokens seen plus its depth.  Only with stage = 1 and without a prefix;
+ *             at most 1024 nodes per sequence.  s_new and mass are those of the nodes in their order */
+typedef struct dynts_extend_more {
+  int sinks;
+  const int* tree;
+} dynts_extend_more_t;
+dynts_status_t dynts_extend_attn_ex(dynts_cache_t* c, int layer, const void* q, const void* k_new, const void* v_new, void* out, const int* n_new,
+                                    const dynts_extend_opts_t* opts, const dynts_extend_more_t* more, void* scratch, size_t scratch_bytes);
+
+/* ---- trees of drafted tokens ---------------------------------------------------------------- */
+
+/* Numbers the trees of a chunk.  parents: device [n_total] int32, the parent of each node by its place among its sequence's nodes: before
+ * it, or -1 (it follows the rows held; there may be several such).  n_new: host [Nb], nodes per sequence, at most 1024.
+ *   tree:      device [n_total][4] int32, receives {place in a walk that visits a node before its children, nodes of its subtree,
+ *              depth, parent}: the same for every layer of a step
+ *   positions: device [n_total] int32 or NULL, receives tokens seen + depth (for dynts_rope)
+ * One launch on the cache's stream (per 128 sequences); may be captured.  A parent that is none of these counts as -1 and
+ * dynts_poll_error reports it. */
+dynts_status_t dynts_tree_plan(dynts_cache_t* c, const int* parents, const int* n_new, int* tree, int* positions);
+
+/* Which nodes of each tree were drawn.  Node 0 of a sequence (the token drawn last, whose row is new) is accepted; then, as long as there is
+ * one, the first child of the node reached whose drafted token is the token drawn from that node's logits.
+ *   parents, drafted, drawn: device [n_total] int32 (drawn: e.g. by dynts_sample for every node);  n_new: host [batch]
+ *   path:      device [batch][max_path], receives the accepted nodes from node 0 on, -1 behind them
+ *   accepted:  device [batch], nodes accepted (0 for a sequence without nodes), at most max_path
+ *   next:      device [batch], the token drawn at the last of them: the sequence's next token (-1: none)
+ * A drawn token below 0 (a row without a distribution) ends the path.  One launch per 128 sequences; allocates nothing. */
+dynts_status_t dynts_tree_accept(const int* parents, const int* drafted, const int* drawn, const int* n_new, int batch, int* path, int max_path, int* accepted,
+                                 int* next, void* stream);
+
+/* Takes over the rows of a path of the chunk staged last: rows path[b][0 .. n_accept[b]) of it (n_accept: host [Nb]; path: device
+ * [Nb][path_stride], as dynts_tree_accept writes it: ascending) move behind the rows held, in order, with positions
+ * counted on from the tokens seen and the scores s_new gave; the other staged rows are forgotten.  States as
+ * dynts_extend_commit.  A path that is not ascending or leaves the staged rows moves nothing, leaves its sequence's length and is reported by dynts_poll_error
+ * (dynts_cache_refresh_lengths then brings the host's copy in line). */
+dynts_status_t dynts_extend_commit_path(dynts_cache_t* c, const int* n_accept, const int* path, int path_stride);
 
 /* Rotary positions with one or several axes, for the queries and keys handed to this library (which
  * stores keys as given).  Pair i (0 <= i < rot_dim / 2) of a head turns by pos[axis(i)][t] *
@@ -317,6 +359,37 @@ enum { DYNTS_ROPE_ADJACENT = 1, DYNTS_ROPE_ROUND_ROBIN = 2 };
 dynts_status_t dynts_rope(const void* q, const void* k, const int* pos, void* q_out, void* k_out, int n_tokens, int q_heads, int kv_heads,
                           int head_dim, int rot_dim, int n_axes, const int* sections, int flags, double theta, int dtype,
                           const long long* strides, void* stream);
+
+/* ---- a token per row of logits ---------------------------------------------------------------- */
+
+/* Settings of dynts_sample, for all rows, or where the array is given (device, [n_rows]) for each.  opts == NULL: temperature 1,
+ * nothing cut off.  Scalars are checked on the host; array values outside the ranges count as: temperature not above 0 (or NaN)
+ * as 0, top_k below 1 as off, top_p above 1 (or NaN) as 1 and below 0 as 0 (the largest token alone), min_p below 0 (or NaN) as
+ * 0 and above 1 as 1. */
+typedef struct dynts_sample_opts {
+  float temperature; /* T >= 0, finite; 0: the largest logit, the lowest index among equals, with log-probability 0 */
+  int top_k;         /* 0: off */
+  float top_p;       /* above 0, at most 1; 1: off */
+  float min_p;       /* from 0 to 1; 0: off */
+  const float* temperatures;
+  const int* top_ks;
+  const float* top_ps;
+  const float* min_ps;
+} dynts_sample_opts_t;
+
+/* One token per row, from given random numbers.  With w_i = exp((x_i - max x) / T) and the tokens ranked by x, equal ones by
+ * the lower index: kept are the first top_k; of those the shortest run from the first on whose weights add up to at least top_p of
+ * the weights of all of those; of those the tokens with w >= min_p.  The token is the first, in the order of the vocabulary, at
+ * which the running sum of the kept weights exceeds u times their sum.
+ *   logits:   device [n_rows][vocab], bf16 or fp32 (dtype), rows row_stride elements apart (0: vocab); no alignment beyond an
+ *             element's; vocab at most 524287
+ *   u:        device [n_rows] fp32 in [0, 1) (outside, or NaN: the nearest of it, or 0)
+ *   tokens:   device [n_rows] int32;  logprobs: device [n_rows] fp32 or NULL, log of the token's share of the kept weights
+ * A logit of -inf has no weight.  A row that holds NaN or +inf, or nothing above -inf, has no distribution: token -1,
+ * log-probability NaN.  The weights are held to 2^-46 of the largest and their sums are exact, so the token does not depend on
+ * how the work is laid out.  One launch on `stream`; allocates nothing. */
+dynts_status_t dynts_sample(const void* logits, int dtype, int n_rows, int vocab, long long row_stride, const float* u, const dynts_sample_opts_t* opts, int* tokens,
+                            float* logprobs, void* stream);
 
 /* ---- predictor scores and the paper's own trigger ------------------------------------------ */
 

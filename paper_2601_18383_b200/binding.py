@@ -59,6 +59,17 @@ class dynts_extend_opts_t(C.Structure):
     ]
 
 
+class dynts_extend_more_t(C.Structure):
+    _fields_ = [("sinks", C.c_int), ("tree", C.c_void_p)]
+
+
+class dynts_sample_opts_t(C.Structure):
+    _fields_ = [
+        ("temperature", C.c_float), ("top_k", C.c_int), ("top_p", C.c_float), ("min_p", C.c_float),
+        ("temperatures", C.c_void_p), ("top_ks", C.c_void_p), ("top_ps", C.c_void_p), ("min_ps", C.c_void_p),
+    ]
+
+
 if not os.path.exists(LIB_PATH):
     raise ImportError(
         f"{LIB_PATH} is missing: build it with `python paper_2601_18383_b200/build.py` "
@@ -112,7 +123,12 @@ _sigs = {
     "dynts_extend_attn": (C.c_int, [_P] * 6 + [C.POINTER(dynts_extend_opts_t), _P, C.c_size_t]),
     "dynts_extend_attn_layer": (C.c_int, [_P, C.c_int] + [_P] * 5 + [C.POINTER(dynts_extend_opts_t), _P, C.c_size_t]),
     "dynts_extend_commit": (C.c_int, [_P, _P]),
+    "dynts_extend_attn_ex": (C.c_int, [_P, C.c_int] + [_P] * 5 + [C.POINTER(dynts_extend_opts_t), C.POINTER(dynts_extend_more_t), _P, C.c_size_t]),
+    "dynts_tree_plan": (C.c_int, [_P] * 5),
+    "dynts_tree_accept": (C.c_int, [_P] * 4 + [C.c_int, _P, C.c_int] + [_P] * 3),
+    "dynts_extend_commit_path": (C.c_int, [_P, _P, _P, C.c_int]),
     "dynts_rope": (C.c_int, [_P] * 5 + [C.c_int] * 6 + [_P, C.c_int, C.c_double, C.c_int, _P, _P]),
+    "dynts_sample": (C.c_int, [_P, C.c_int, C.c_int, C.c_int, C.c_longlong, _P, C.POINTER(dynts_sample_opts_t), _P, _P, _P]),
     "dynts_evict_stats": (C.c_int, [_P, C.POINTER(C.c_longlong), C.POINTER(C.c_longlong)]),
     "dynts_last_error": (C.c_char_p, []),
     "dynts_version": (C.c_char_p, []),
@@ -393,6 +409,27 @@ def dynts_extend_commit(c, n_accept):
     return _check(lib.dynts_extend_commit(c, p))
 
 
+def dynts_extend_attn_ex(c, layer, q, k_new, v_new, out, n_new, opts, more, scratch, scratch_bytes):
+    p, keep = _host_ints(n_new)
+    return _check(lib.dynts_extend_attn_ex(c, layer, _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(out), p, C.byref(opts) if opts is not None else None,
+                                           C.byref(more) if more is not None else None, _ptr(scratch), scratch_bytes))
+
+
+def dynts_tree_plan(c, parents, n_new, tree, positions=None):
+    p, keep = _host_ints(n_new)
+    return _check(lib.dynts_tree_plan(c, _ptr(parents), p, _ptr(tree), _ptr(positions)))
+
+
+def dynts_tree_accept(parents, drafted, drawn, n_new, batch, path, max_path, accepted, next, stream=None):
+    p, keep = _host_ints(n_new)
+    return _check(lib.dynts_tree_accept(_ptr(parents), _ptr(drafted), _ptr(drawn), p, batch, _ptr(path), max_path, _ptr(accepted), _ptr(next), stream))
+
+
+def dynts_extend_commit_path(c, n_accept, path, path_stride):
+    p, keep = _host_ints(n_accept)
+    return _check(lib.dynts_extend_commit_path(c, p, _ptr(path), path_stride))
+
+
 def dynts_rope(q, k, pos, q_out, k_out, n_tokens, q_heads, kv_heads, head_dim, rot_dim, n_axes, sections, flags, theta, dtype, strides=None,
                stream=None):
     sec = (C.c_int * n_axes)(*sections) if sections is not None else None
@@ -463,6 +500,80 @@ def rope(q, k, positions, q_out=None, k_out=None, theta=10000.0, sections=None, 
         with t.torch.cuda.device(dev):
             _check(lib.dynts_rope(*args))
     return q_out, k_out
+
+
+def dynts_sample(logits, dtype, n_rows, vocab, row_stride, u, opts, tokens, logprobs=None, stream=None):
+    return _check(lib.dynts_sample(_ptr(logits), dtype, n_rows, vocab, row_stride, _ptr(u), C.byref(opts) if opts is not None else None, _ptr(tokens),
+                                   _ptr(logprobs), stream))
+
+
+def sample(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, tokens=None, logprobs=None):
+    """dynts_sample on torch tensors: logits [n, vocab] bf16 or fp32 (rows may be strided), u fp32 [n] in [0, 1).  Each setting is a number, or a
+    tensor [n] on logits' device (fp32; top_k int32) with a value per row.  The outputs are new tensors unless given: tokens
+    int32 [n], logprobs fp32 [n].  Runs on torch's current stream of logits' device.  Returns (tokens, logprobs)."""
+    t = _torch()
+    dev, shape = logits.get_device(), logits.shape
+    dtype = t.dtypes.get(logits.dtype)
+    if dtype is None or dev < 0 or len(shape) != 2:
+        _invalid("logits must be a CUDA tensor [n, vocab] of bf16 or fp32")
+    n, vocab = shape
+    stride = logits.stride(0) if n > 1 else max(vocab, 1)
+    if (vocab > 1 and logits.stride(1) != 1) or stride < vocab:
+        _invalid("the logits of a row must be contiguous and the rows in order")
+    if tokens is None:
+        tokens = t.torch.empty((n,), dtype=t.int32, device=logits.device)
+    if logprobs is None:
+        logprobs = t.torch.empty((n,), dtype=t.float32, device=logits.device)
+    scalars, arrays = [1.0, 0, 1.0, 0.0], [None] * 4
+    checks = [(u, t.float32), (tokens, t.int32), (logprobs, t.float32)]
+    for i, x in enumerate((temperature, top_k, top_p, min_p)):
+        if hasattr(x, "data_ptr"):
+            checks.append((x, t.int32 if i == 1 else t.float32))
+            arrays[i] = x.data_ptr()
+        else:
+            scalars[i] = x
+    for x, want in checks:
+        if x.dtype is not want or x.get_device() != dev or x.shape != (n,) or not x.is_contiguous():
+            _invalid(f"u, tokens, logprobs and settings of each row must be contiguous tensors of {n} on logits' device (fp32; tokens and top_k int32)")
+    if not -2 ** 31 <= scalars[1] < 2 ** 31 or vocab >= 2 ** 31 or n >= 2 ** 31:  # (ctypes would cut them)
+        _invalid("top_k and the sizes must fit 32 bits")
+    opts = dynts_sample_opts_t(*scalars, *arrays)
+    args = (logits.data_ptr(), dtype, n, vocab, stride, u.data_ptr(), C.byref(opts), tokens.data_ptr(), logprobs.data_ptr(), t.stream(dev))
+    if t.device() == dev:
+        _check(lib.dynts_sample(*args))
+    else:
+        with t.torch.cuda.device(dev):
+            _check(lib.dynts_sample(*args))
+    return tokens, logprobs
+
+
+def tree_accept(parents, drafted, drawn, n_new, max_path=None, path=None, accepted=None, next_tokens=None):
+    """dynts_tree_accept on torch tensors: parents, drafted, drawn int32 [n], n_new[b] nodes of each sequence.  The outputs are new tensors
+    unless given: path [batch, max_path] (max_path: by default path's, or the most nodes of a sequence), accepted [batch],
+    next_tokens [batch], all int32.  Runs on torch's current stream of the tensors' device.  Returns the three."""
+    t = _torch()
+    counts, keep = _host_ints(n_new)
+    listed = n_new.tolist() if hasattr(n_new, "tolist") else [int(x) for x in n_new]
+    batch, total, dev = len(listed), sum(listed), parents.get_device()
+    if batch == 0 or min(listed) < 0:
+        _invalid("n_new needs a count for each sequence, none of them negative")
+    if max_path is None:
+        max_path = path.shape[1] if path is not None and path.dim() == 2 else max(1, max(listed))
+    new = lambda *shape: t.torch.empty(shape, dtype=t.int32, device=parents.device)
+    path = new(batch, max_path) if path is None else path
+    accepted = new(batch) if accepted is None else accepted
+    next_tokens = new(batch) if next_tokens is None else next_tokens
+    for x, shape in ((parents, (total,)), (drafted, (total,)), (drawn, (total,)), (path, (batch, max_path)), (accepted, (batch,)), (next_tokens, (batch,))):
+        if x.dtype is not t.int32 or x.get_device() != dev or dev < 0 or x.shape != shape or not x.is_contiguous():
+            _invalid(f"parents, drafted, drawn and the outputs must be contiguous int32 tensors on one CUDA device (here: {shape})")
+    args = (parents.data_ptr(), drafted.data_ptr(), drawn.data_ptr(), counts, batch, path.data_ptr(), max_path, accepted.data_ptr(), next_tokens.data_ptr(),
+            t.stream(dev))
+    if t.device() == dev:
+        _check(lib.dynts_tree_accept(*args))
+    else:
+        with t.torch.cuda.device(dev):
+            _check(lib.dynts_tree_accept(*args))
+    return path, accepted, next_tokens
 
 
 def dynts_evict_stats(c):
@@ -554,7 +665,7 @@ class Cache:
     def decode_attn_host(self, q, k_new, v_new, out):
         return dynts_decode_attn_host(self.handle, q, k_new, v_new, out)
 
-    def _extend(self, layer, q, k, v, out, n_new, s_new, mass, softcap, slopes, window, prefix, stage):
+    def _extend(self, layer, q, k, v, out, n_new, s_new, mass, softcap, slopes, window, prefix, stage, sinks, tree):
         t = _torch()
         counts, keep_n = _host_ints(n_new)
         listed = n_new.tolist() if hasattr(n_new, "tolist") else n_new
@@ -582,6 +693,11 @@ class Cache:
             prefixes, keep_p = _host_ints(prefix)
         if not 0 <= window < 2 ** 31:
             _invalid("window must be an int of 32 bits, not negative")
+        if not 0 <= sinks < 2 ** 31:
+            _invalid("sinks must be an int of 32 bits, not negative")
+        if tree is not None and (tree.dtype is not t.int32 or tree.get_device() != dev or tree.shape != (total, 4) or not tree.is_contiguous()):
+            _invalid(f"tree must be a contiguous int32 tensor {(total, 4)} on cuda:{dev}, as tree_plan returns it")
+        more = dynts_extend_more_t(sinks, None if tree is None else tree.data_ptr())
         opts = dynts_extend_opts_t(softcap, None if slopes is None else slopes.data_ptr(), window, prefixes, None if s_new is None else s_new.data_ptr(),
                                    None if mass is None else mass.data_ptr(), 1 if stage else 0, *strides)
         need = lib.dynts_extend_scratch_bytes(self.handle, counts, self.layers if layer is None else 1)
@@ -591,11 +707,16 @@ class Cache:
             with t.torch.cuda.stream(self.torch_stream()):
                 self._scratch.append(t.torch.empty(max(need, 2 * self._scratch_bytes), dtype=t.torch.uint8, device=self.device))
             self._scratch_ptr, self._scratch_bytes = self._scratch[-1].data_ptr(), self._scratch[-1].numel()
-        args = (q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), counts, C.byref(opts), self._scratch_ptr, self._scratch_bytes)
-        if t.device() != dev:
-            with t.torch.cuda.device(dev):
-                return self._extend_call(layer, args)
-        return self._extend_call(layer, args)
+        args = (self.handle, -1 if layer is None else layer, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), counts, C.byref(opts), C.byref(more),
+                self._scratch_ptr, self._scratch_bytes)
+        return self._on_device(lib.dynts_extend_attn_ex, args)
+
+    def _on_device(self, call, args):
+        t = _torch()
+        if t.device() != self.device_index:
+            with t.torch.cuda.device(self.device_index):
+                return _check(call(*args))
+        return _check(call(*args))
 
     def torch_stream(self):
         """The stream the cache works on, as a torch stream."""
@@ -611,23 +732,52 @@ class Cache:
             _invalid("the heads of a token must be contiguous, the tokens in order and the layers adjoining")
         return step
 
-    def _extend_call(self, layer, args):
-        if layer is None:
-            return _check(lib.dynts_extend_attn(self.handle, *args))
-        return _check(lib.dynts_extend_attn_layer(self.handle, layer, *args))
-
-    def extend_attn(self, q, k, v, out, n_new, s_new=None, mass=None, softcap=0.0, slopes=None, window=0, prefix=None, stage=False):
-        """A chunk of n_new[b] tokens per sequence for all layers: q, out [L, n_total, Hq, d], k, v [L, n_total, Hkv, d]."""
-        return self._extend(None, q, k, v, out, n_new, s_new, mass, softcap, slopes, window, prefix, stage)
+    def extend_attn(self, q, k, v, out, n_new, s_new=None, mass=None, softcap=0.0, slopes=None, window=0, prefix=None, stage=False, sinks=0,
+                    tree=None):
+        """A chunk of n_new[b] tokens per sequence for all layers: q, out [L, n_total, Hq, d], k, v [L, n_total, Hkv, d].
+        sinks: positions that stay visible beside a window; tree: the nodes' numbering (tree_plan), with stage=True."""
+        return self._extend(None, q, k, v, out, n_new, s_new, mass, softcap, slopes, window, prefix, stage, sinks, tree)
 
     def extend_attn_layer(self, layer, q, k, v, out, n_new, s_new=None, mass=None, softcap=0.0, slopes=None, window=0, prefix=None,
-                          stage=False):
-        return self._extend(int(layer), q, k, v, out, n_new, s_new, mass, softcap, slopes, window, prefix, stage)
+                          stage=False, sinks=0, tree=None):
+        layer = int(layer)
+        if layer < 0:
+            raise DyntsError(DYNTS_ERR_STATE, f"layer {layer} called")
+        return self._extend(layer, q, k, v, out, n_new, s_new, mass, softcap, slopes, window, prefix, stage, sinks, tree)
+
+    def tree_plan(self, parents, n_new, tree=None, positions=None):
+        """Numbers a chunk's trees: parents int32 [n_total], n_new[b] nodes of each sequence.  Returns (tree [n_total, 4], positions
+        [n_total]), int32, new tensors unless given: tree for extend_attn, positions for rope.  Runs on the cache's stream."""
+        t = _torch()
+        counts, keep = _host_ints(n_new)
+        listed = n_new.tolist() if hasattr(n_new, "tolist") else n_new
+        if len(listed) != self.batch:
+            _invalid("n_new needs a count for each sequence")
+        total, dev = sum(listed), self.device_index
+        new = lambda *shape: t.torch.empty(shape, dtype=t.int32, device=self.device)
+        if tree is None or positions is None:
+            with t.torch.cuda.stream(self.torch_stream()):  # (memory of the stream that will write it)
+                tree = new(total, 4) if tree is None else tree
+                positions = new(total) if positions is None else positions
+        for x, shape in ((parents, (total,)), (tree, (total, 4)), (positions, (total,))):
+            if x.dtype is not t.int32 or x.get_device() != dev or x.shape != shape or not x.is_contiguous():
+                _invalid(f"parents, tree and positions must be contiguous int32 tensors on cuda:{dev} (here: {shape})")
+        self._on_device(lib.dynts_tree_plan, (self.handle, parents.data_ptr(), counts, tree.data_ptr(), positions.data_ptr()))
+        return tree, positions
 
     def extend_commit(self, n_accept):
         if len(n_accept) != self.batch:
             _invalid("n_accept needs a count for each sequence")
         return dynts_extend_commit(self.handle, n_accept)
+
+    def extend_commit_path(self, n_accept, path):
+        """Takes over n_accept[b] rows (host) of the staged chunk, those path[b] names (int32 [batch, stride] on the cache's device)."""
+        if len(n_accept) != self.batch:
+            _invalid("n_accept needs a count for each sequence")
+        if path.dtype is not _torch().int32 or path.get_device() != self.device_index or path.dim() != 2 or path.shape[0] != self.batch or not path.is_contiguous():
+            _invalid(f"path must be a contiguous int32 tensor [{self.batch}, stride] on cuda:{self.device_index}")
+        counts, keep = _host_ints(n_accept)
+        return self._on_device(lib.dynts_extend_commit_path, (self.handle, counts, path.data_ptr(), path.shape[1]))
 
     def evict(self, budget=0):
         return dynts_evict(self.handle, budget)

@@ -6,6 +6,7 @@
 #include <cuda_runtime.h>
 
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
@@ -21,6 +22,8 @@
 #include "evict.cuh"
 #include "extend.cuh"
 #include "extend_tc.cuh"
+#include "tree.cuh"
+#include "sample.cuh"
 #include "predictor.cuh"
 #include "prefill_attn.cuh"
 #include "rope.cuh"
@@ -141,7 +144,9 @@ struct dynts_cache {
   bool extending = false;    // the layer-by-layer step in progress is a chunk (dynts_extend_attn_layer)
   bool chunk_staged = false; // ... and it is staged
   std::vector<int> chunk_h;  // ... and its tokens per sequence
+  bool chunk_tree = false;   // ... and it is a tree
   std::vector<int> staged_h; // rows per sequence that a staged chunk left behind the ends (empty: none)
+  bool staged_tree = false;  // ... as the nodes of trees
   int cluster = 0, variant = 0;
   unsigned int wait_limit = dynts::kStSpinLimit;  // polls of a bounded device-side wait
   int drop_item = -1;        // one-shot: the next streaming decode launch omits this tile load of CTA 0 (timeout-path test)
@@ -1391,6 +1396,7 @@ struct ExtendCall {
   void* out;
   const int* n_new;
   dynts_extend_opts_t o;
+  dynts_extend_more_t more;
   char* scratch;
   size_t scratch_bytes;
 };
@@ -1419,6 +1425,15 @@ dynts_status_t check_extend(const dynts_cache* c, const ExtendCall& a, int n_lay
     return fail(DYNTS_ERR_INVALID_ARG, "softcap must be 0 or from 1e-20 to 1e20");
   if (a.o.window < 0) return fail(DYNTS_ERR_INVALID_ARG, "window must not be negative");
   if (a.o.stage != 0 && a.o.stage != 1) return fail(DYNTS_ERR_INVALID_ARG, "stage must be 0 or 1");
+  if (a.more.sinks < 0) return fail(DYNTS_ERR_INVALID_ARG, "sinks must not be negative");
+  if (a.more.tree) {
+    if (!aligned16(a.more.tree)) return fail(DYNTS_ERR_INVALID_ARG, "tree must be 16-byte aligned");
+    if (!a.o.stage) return fail(DYNTS_ERR_INVALID_ARG, "a tree is staged: its accepted path is taken over by dynts_extend_commit_path");
+    for (int b = 0; b < f.batch; ++b) {
+      if (a.n_new[b] > dynts::kTreeNodes) return fail(DYNTS_ERR_INVALID_ARG, "sequence %d: a tree of %d nodes, at most %d", b, a.n_new[b], dynts::kTreeNodes);
+      if (a.o.prefix && a.o.prefix[b] > 0) return fail(DYNTS_ERR_INVALID_ARG, "sequence %d: a tree has no prefix", b);
+    }
+  }
   const long long per16 = 16 / elt_bytes_of(f.dtype);
   const long long qs = a.o.q_stride, ks = a.o.k_stride, vs = a.o.v_stride, qd = (long long)f.q_heads * f.head_dim, kd = (long long)f.kv_heads * f.head_dim;
   if ((qs != 0 && (qs < qd || qs % per16)) || (ks != 0 && (ks < kd || ks % per16)) || (vs != 0 && (vs < kd || vs % per16)))
@@ -1456,6 +1471,24 @@ cudaError_t launch_dependent_clusters(Kern kern, unsigned cluster, dim3 grid, un
   return cudaLaunchKernelEx(&lc, kern, args...);
 }
 
+// A launch in stream order, with clusters.
+template <typename Kern, typename... Args>
+cudaError_t launch_clusters(Kern kern, unsigned cluster, dim3 grid, unsigned threads, size_t smem, cudaStream_t st, Args... args) {
+  cudaLaunchConfig_t lc;
+  memset(&lc, 0, sizeof(lc));
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeClusterDimension;
+  at[0].val.clusterDim.x = cluster;
+  at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+  lc.attrs = at;
+  lc.numAttrs = cluster > 1 ? 1 : 0;
+  lc.stream = st;
+  lc.gridDim = grid;
+  lc.blockDim = dim3(threads, 1, 1);
+  lc.dynamicSmemBytes = smem;
+  return cudaLaunchKernelEx(&lc, kern, args...);
+}
+
 template <typename Kern, typename... Args>
 cudaError_t launch_dependent(Kern kern, dim3 grid, unsigned threads, size_t smem, cudaStream_t st, Args... args) {
   return launch_dependent_clusters(kern, 1, grid, threads, smem, st, args...);
@@ -1483,7 +1516,7 @@ dynts_status_t launch_extend_generic(dynts_cache* c, dynts::ExtendParams& p, boo
   // guides the cut).
   long long longest = 0;
   for (int s = 0; s < n_seq; ++s) longest = std::max<long long>(longest, c->len_h[p.seqs.b0 + s] + p.seqs.tok0[s + 1] - p.seqs.tok0[s]);
-  if (p.window > 0) longest = std::min<long long>(longest, (long long)p.window + dynts::kExtGenericRows);
+  if (p.window > 0) longest = std::min<long long>(longest, (long long)p.window + dynts::kExtGenericRows + p.sinks);
   unsigned cluster = 1;
   while (cluster < 8 && (long long)p.seqs.item0[n_seq] * ny * cluster * 2 <= c->sm_count && (long long)cluster * dynts::kExtGenericKeys < longest) cluster *= 2;
   CUDA_TRY(launch_dependent_clusters(dynts::extend_generic_kernel<T, KV8>, cluster, dim3((unsigned)p.seqs.item0[n_seq] * cluster, ny, 1),
@@ -1572,7 +1605,7 @@ dynts_status_t plan_extend(const dynts_cache* c, const dynts::ExtendParams& x, c
     // kernels go by the device's.)
     long long rows = c->len_h[x.seqs.b0 + s] + std::max((t + 1) / 2, x.seqs.prefix[s]), full = c->len_h[x.seqs.b0 + s] + t;
     if (x.window > 0) {
-      const long long seen = (long long)x.window + tpt + dynts::kPfKeys;
+      const long long seen = (long long)x.window + tpt + dynts::kPfKeys + ((long long)x.sinks + dynts::kPfKeys - 1) / dynts::kPfKeys * dynts::kPfKeys;
       rows = std::min(rows, seen);
       full = std::min(full, seen);
     }
@@ -1666,7 +1699,7 @@ dynts_status_t launch_extend_tc(dynts_cache* c, const dynts::ExtendParams& x, co
                                box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   if (r != CUDA_SUCCESS) return fail(DYNTS_ERR_CUDA, "cuTensorMapEncodeTiled failed (%d)", (int)r);
-  const bool mods = x.cap_logit > 0.f || x.slopes || x.window > 0;
+  const bool mods = x.cap_logit > 0.f || x.slopes || x.window > 0 || x.tree;
   if (kv8)
     return mods ? launch_extend_tc_as<true, true>(c, p, grid, whole, map, want_mass) : launch_extend_tc_as<true, false>(c, p, grid, whole, map, want_mass);
   return mods ? launch_extend_tc_as<false, true>(c, p, grid, whole, map, want_mass) : launch_extend_tc_as<false, false>(c, p, grid, whole, map, want_mass);
@@ -1724,6 +1757,8 @@ dynts_status_t launch_extend(dynts_cache* c, int layer0, int n_layers, const Ext
   p.d = f.head_dim;
   p.cap = c->cap;
   p.window = a.o.window;
+  p.sinks = a.o.window > 0 ? a.more.sinks : 0;
+  p.tree = reinterpret_cast<const int4*>(a.more.tree);
   p.publish = publish ? 1 : 0;
   p.scale = (float)((kv8 ? (double)c->k_scale : 1.0) / std::sqrt((double)f.head_dim));
   p.cap_logit = a.o.softcap;
@@ -1775,7 +1810,7 @@ dynts_status_t launch_extend(dynts_cache* c, int layer0, int n_layers, const Ext
 }
 
 // The host's copy of the lengths after a chunk whose last layer has been issued.
-void finish_extend(dynts_cache* c, const int* n_new, bool stage) {
+void finish_extend(dynts_cache* c, const int* n_new, bool stage, bool tree) {
   for (int b = 0; b < c->cfg.batch; ++b) {
     if (n_new[b] == 0 || stage) continue;
     c->len_h[b] += n_new[b];
@@ -1783,6 +1818,64 @@ void finish_extend(dynts_cache* c, const int* n_new, bool stage) {
     c->active_h[b] = 1;
   }
   if (stage) c->staged_h.assign(n_new, n_new + c->cfg.batch);
+  c->staged_tree = stage && tree;
+}
+
+dynts_status_t extend_all(dynts_cache* c, const ExtendCall& a) {
+  if (!c) return fail(DYNTS_ERR_INVALID_ARG, "NULL cache");
+  try {
+    if (c->layer_cursor != 0) return fail(DYNTS_ERR_STATE, "a layer-by-layer step is in progress");
+    long long total = 0;
+    dynts_status_t st = check_extend(c, a, c->cfg.layers, &total);
+    if (st != DYNTS_OK) return st;
+    st = materialise(c);
+    if (st != DYNTS_OK) return st;
+    st = launch_extend(c, 0, c->cfg.layers, a, total, !a.o.stage);
+    if (st == DYNTS_OK) finish_extend(c, a.n_new, a.o.stage != 0, a.more.tree != nullptr);
+    return st;
+  } catch (const std::bad_alloc&) {
+    return fail(DYNTS_ERR_OOM, "out of host memory");
+  }
+}
+
+dynts_status_t extend_layer(dynts_cache* c, int layer, const ExtendCall& a) {
+  if (!c) return fail(DYNTS_ERR_INVALID_ARG, "NULL cache");
+  try {
+    if (layer != c->layer_cursor || layer >= c->cfg.layers)
+      return fail(DYNTS_ERR_STATE, "layer %d called, layer %d expected", layer, c->layer_cursor);
+    if (layer != 0 && !c->extending) return fail(DYNTS_ERR_STATE, "the step in progress is a decode step");
+    long long total = 0;
+    dynts_status_t st = check_extend(c, a, 1, &total);
+    if (st != DYNTS_OK) return st;
+    st = materialise(c);
+    if (st != DYNTS_OK) return st;
+    const bool staged = a.o.stage != 0, tree = a.more.tree != nullptr;
+    if (layer == 0) {
+      c->chunk_h.assign(a.n_new, a.n_new + c->cfg.batch);
+      c->chunk_staged = staged;
+      c->chunk_tree = tree;
+    } else if (!std::equal(c->chunk_h.begin(), c->chunk_h.end(), a.n_new) || c->chunk_staged != staged || c->chunk_tree != tree) {
+      return fail(DYNTS_ERR_STATE, "layer %d: n_new, stage and whether there is a tree must be those of layer 0", layer);
+    }
+    const bool last = layer == c->cfg.layers - 1;
+    st = launch_extend(c, layer, 1, a, total, last && !staged);
+    if (st != DYNTS_OK) return st;
+    c->extending = !last;
+    c->layer_cursor = last ? 0 : layer + 1;
+    if (last) finish_extend(c, a.n_new, staged, tree);
+    return DYNTS_OK;
+  } catch (const std::bad_alloc&) {
+    return fail(DYNTS_ERR_OOM, "out of host memory");
+  }
+}
+
+// The sequences b0, b0 + 1, ... of a launch and their running counts.
+template <typename Count>
+void tree_seqs(dynts::TreeSeqs& q, int b0, int batch, int tok, Count&& count) {
+  q.n = std::min(dynts::kExtSeqs, batch - b0);
+  q.b0 = b0;
+  q.tok0[0] = tok;
+  for (int s = 0; s < q.n; ++s) q.tok0[s + 1] = q.tok0[s] + count(b0 + s);
 }
 
 }  // namespace
@@ -1798,60 +1891,30 @@ size_t dynts_extend_scratch_bytes(const dynts_cache_t* c, const int* n_new, int 
 
 dynts_status_t dynts_extend_attn(dynts_cache_t* c, const void* q, const void* k_new, const void* v_new, void* out, const int* n_new,
                                  const dynts_extend_opts_t* opts, void* scratch, size_t scratch_bytes) {
-  if (!c) return fail(DYNTS_ERR_INVALID_ARG, "NULL cache");
-  try {
-    if (c->layer_cursor != 0) return fail(DYNTS_ERR_STATE, "a layer-by-layer step is in progress");
-    ExtendCall a{q, k_new, v_new, out, n_new, {}, static_cast<char*>(scratch), scratch_bytes};
-    if (opts) a.o = *opts;
-    long long total = 0;
-    dynts_status_t st = check_extend(c, a, c->cfg.layers, &total);
-    if (st != DYNTS_OK) return st;
-    st = materialise(c);
-    if (st != DYNTS_OK) return st;
-    st = launch_extend(c, 0, c->cfg.layers, a, total, !a.o.stage);
-    if (st == DYNTS_OK) finish_extend(c, n_new, a.o.stage != 0);
-    return st;
-  } catch (const std::bad_alloc&) {
-    return fail(DYNTS_ERR_OOM, "out of host memory");
-  }
+  return dynts_extend_attn_ex(c, -1, q, k_new, v_new, out, n_new, opts, nullptr, scratch, scratch_bytes);
 }
 
 dynts_status_t dynts_extend_attn_layer(dynts_cache_t* c, int layer, const void* q, const void* k_new, const void* v_new, void* out,
                                        const int* n_new, const dynts_extend_opts_t* opts, void* scratch, size_t scratch_bytes) {
-  if (!c) return fail(DYNTS_ERR_INVALID_ARG, "NULL cache");
-  try {
-    if (layer != c->layer_cursor || layer >= c->cfg.layers)
-      return fail(DYNTS_ERR_STATE, "layer %d called, layer %d expected", layer, c->layer_cursor);
-    if (layer != 0 && !c->extending) return fail(DYNTS_ERR_STATE, "the step in progress is a decode step");
-    ExtendCall a{q, k_new, v_new, out, n_new, {}, static_cast<char*>(scratch), scratch_bytes};
-    if (opts) a.o = *opts;
-    long long total = 0;
-    dynts_status_t st = check_extend(c, a, 1, &total);
-    if (st != DYNTS_OK) return st;
-    st = materialise(c);
-    if (st != DYNTS_OK) return st;
-    if (layer == 0) {
-      c->chunk_h.assign(n_new, n_new + c->cfg.batch);
-      c->chunk_staged = a.o.stage != 0;
-    } else if (!std::equal(c->chunk_h.begin(), c->chunk_h.end(), n_new) || c->chunk_staged != (a.o.stage != 0)) {
-      return fail(DYNTS_ERR_STATE, "layer %d: n_new and stage must be those of layer 0", layer);
-    }
-    const bool last = layer == c->cfg.layers - 1;
-    st = launch_extend(c, layer, 1, a, total, last && !a.o.stage);
-    if (st != DYNTS_OK) return st;
-    c->extending = !last;
-    c->layer_cursor = last ? 0 : layer + 1;
-    if (last) finish_extend(c, n_new, a.o.stage != 0);
-    return DYNTS_OK;
-  } catch (const std::bad_alloc&) {
-    return fail(DYNTS_ERR_OOM, "out of host memory");
-  }
+  ExtendCall a{q, k_new, v_new, out, n_new, {}, {}, static_cast<char*>(scratch), scratch_bytes};
+  if (opts) a.o = *opts;
+  return extend_layer(c, layer, a);
+}
+
+dynts_status_t dynts_extend_attn_ex(dynts_cache_t* c, int layer, const void* q, const void* k_new, const void* v_new, void* out, const int* n_new,
+                                    const dynts_extend_opts_t* opts, const dynts_extend_more_t* more, void* scratch, size_t scratch_bytes) {
+  if (layer < -1) return fail(DYNTS_ERR_INVALID_ARG, "layer %d", layer);
+  ExtendCall a{q, k_new, v_new, out, n_new, {}, {}, static_cast<char*>(scratch), scratch_bytes};
+  if (opts) a.o = *opts;
+  if (more) a.more = *more;
+  return layer < 0 ? extend_all(c, a) : extend_layer(c, layer, a);
 }
 
 dynts_status_t dynts_extend_commit(dynts_cache_t* c, const int* n_accept) {
   if (!c || !n_accept) return fail(DYNTS_ERR_INVALID_ARG, "NULL argument");
   if (!c->ready || c->staged_h.empty()) return fail(DYNTS_ERR_STATE, "no staged chunk lies behind the sequences' ends");
   if (c->layer_cursor != 0) return fail(DYNTS_ERR_STATE, "a layer-by-layer step is in progress");
+  if (c->staged_tree) return fail(DYNTS_ERR_STATE, "the staged chunk is a tree: take over a path of it (dynts_extend_commit_path)");
   const int Nb = c->cfg.batch;
   for (int b = 0; b < Nb; ++b)
     if (n_accept[b] < 0 || n_accept[b] > c->staged_h[b])
@@ -1870,6 +1933,117 @@ dynts_status_t dynts_extend_commit(dynts_cache_t* c, const int* n_accept) {
     dynts::extend_commit_kernel<<<1, dynts::kExtSeqs, 0, c->stream>>>(q, c->len(), c->tot(), c->active(), c->cap, c->err_dev);
     CUDA_TRY(cudaGetLastError());
     c->launches += 1;
+  }
+  c->staged_h.clear();
+  for (int b = 0; b < Nb; ++b) {
+    if (n_accept[b] == 0) continue;
+    c->len_h[b] += n_accept[b];
+    c->tot_h[b] += n_accept[b];
+    c->active_h[b] = 1;
+  }
+  return DYNTS_OK;
+}
+
+/* ---- trees of drafted tokens --------------------------------------------------------------- */
+
+dynts_status_t dynts_tree_plan(dynts_cache_t* c, const int* parents, const int* n_new, int* tree, int* positions) {
+  if (!c || !n_new) return fail(DYNTS_ERR_INVALID_ARG, "NULL argument");
+  if (!config_ok(&c->cfg, nullptr)) return fail(DYNTS_ERR_INVALID_ARG, "invalid cache configuration");
+  const int Nb = c->cfg.batch;
+  long long total = 0;
+  for (int b = 0; b < Nb; ++b) {
+    if (n_new[b] < 0 || n_new[b] > dynts::kTreeNodes)
+      return fail(DYNTS_ERR_INVALID_ARG, "sequence %d: %d nodes, a tree has 0 to %d", b, n_new[b], dynts::kTreeNodes);
+    total += n_new[b];
+  }
+  if (total >= (1ll << 30)) return fail(DYNTS_ERR_INVALID_ARG, "%lld nodes are beyond the launch limits", total);
+  if (total == 0) return DYNTS_OK;
+  if (!parents || !tree) return fail(DYNTS_ERR_INVALID_ARG, "NULL tensor pointer");
+  if (!aligned16(tree) || (reinterpret_cast<uintptr_t>(parents) | reinterpret_cast<uintptr_t>(positions)) % 4)
+    return fail(DYNTS_ERR_INVALID_ARG, "tree must be 16-byte aligned, parents and positions 4-byte");
+  dynts_status_t st = materialise(c);
+  if (st != DYNTS_OK) return st;
+  int tok = 0;
+  for (int b0 = 0; b0 < Nb; b0 += dynts::kExtSeqs) {
+    dynts::TreeSeqs q;
+    int most = 0;
+    tree_seqs(q, b0, Nb, tok, [&](int b) {
+      most = std::max(most, n_new[b]);
+      return n_new[b];
+    });
+    tok = q.tok0[q.n];
+    if (most == 0) continue;
+    CUDA_TRY(launch_dependent(dynts::tree_plan_kernel, dim3((unsigned)q.n, 1, 1), (unsigned)(most + 31) / 32 * 32, 0, c->stream, q, parents, (const int*)c->tot(),
+                              reinterpret_cast<int4*>(tree), positions, c->err_dev));
+    c->launches += 1;
+  }
+  return DYNTS_OK;
+}
+
+dynts_status_t dynts_tree_accept(const int* parents, const int* drafted, const int* drawn, const int* n_new, int batch, int* path, int max_path, int* accepted,
+                                 int* next, void* stream) {
+  if (batch < 1 || max_path < 1 || !n_new) return fail(DYNTS_ERR_INVALID_ARG, "batch %d and max_path %d must be positive, n_new given", batch, max_path);
+  long long total = 0;
+  for (int b = 0; b < batch; ++b) {
+    if (n_new[b] < 0) return fail(DYNTS_ERR_INVALID_ARG, "sequence %d: %d nodes", b, n_new[b]);
+    total += n_new[b];
+  }
+  if (total >= (1ll << 30)) return fail(DYNTS_ERR_INVALID_ARG, "%lld nodes are beyond the launch limits", total);
+  if (!path || !accepted || !next || (total > 0 && (!parents || !drafted || !drawn))) return fail(DYNTS_ERR_INVALID_ARG, "NULL tensor pointer");
+  int tok = 0;
+  for (int b0 = 0; b0 < batch; b0 += dynts::kExtSeqs) {
+    dynts::TreeSeqs q;
+    tree_seqs(q, b0, batch, tok, [&](int b) { return n_new[b]; });
+    tok = q.tok0[q.n];
+    dynts::tree_accept_kernel<<<(unsigned)(q.n + 3) / 4, 128, 0, static_cast<cudaStream_t>(stream)>>>(q, parents, drafted, drawn, path, max_path, accepted, next);
+    CUDA_TRY(cudaGetLastError());
+  }
+  return DYNTS_OK;
+}
+
+dynts_status_t dynts_extend_commit_path(dynts_cache_t* c, const int* n_accept, const int* path, int path_stride) {
+  if (!c || !n_accept) return fail(DYNTS_ERR_INVALID_ARG, "NULL argument");
+  if (!c->ready || c->staged_h.empty()) return fail(DYNTS_ERR_STATE, "no staged chunk lies behind the sequences' ends");
+  if (c->layer_cursor != 0) return fail(DYNTS_ERR_STATE, "a layer-by-layer step is in progress");
+  const int Nb = c->cfg.batch;
+  long long total = 0;
+  for (int b = 0; b < Nb; ++b) {
+    if (n_accept[b] < 0 || n_accept[b] > c->staged_h[b])
+      return fail(DYNTS_ERR_INVALID_ARG, "sequence %d: %d rows accepted of %d staged", b, n_accept[b], c->staged_h[b]);
+    if (n_accept[b] > path_stride) return fail(DYNTS_ERR_INVALID_ARG, "sequence %d: a path of %d rows in a stride of %d", b, n_accept[b], path_stride);
+    total += n_accept[b];
+  }
+  if (total > 0 && (!path || reinterpret_cast<uintptr_t>(path) % 4)) return fail(DYNTS_ERR_INVALID_ARG, "path must be non-NULL and 4-byte aligned");
+  {
+    dynts_status_t fs = flush_pending(c);
+    if (fs != DYNTS_OK) return fs;
+  }
+  const unsigned nx = (unsigned)c->cfg.layers * (unsigned)c->cfg.kv_heads;
+  for (int b0 = 0; b0 < Nb; b0 += dynts::kExtSeqs) {
+    dynts::TreeMoveParams p;
+    tree_seqs(p.seqs, b0, Nb, 0, [&](int b) { return n_accept[b]; });
+    if (p.seqs.tok0[p.seqs.n] == 0) continue;
+    for (int s = 0; s < p.seqs.n; ++s) p.staged[s] = c->staged_h[b0 + s];
+    p.path = path;
+    p.path_stride = path_stride;
+    p.K = static_cast<uint8_t*>(c->K());
+    p.V = static_cast<uint8_t*>(c->V());
+    p.pos = c->pos();
+    p.score = c->score();
+    p.comp = c->comp();
+    p.len = c->len();
+    p.tot = c->tot();
+    p.active = c->active();
+    p.err = c->err_dev;
+    p.Nb = Nb;
+    p.Hkv = c->cfg.kv_heads;
+    p.cap = c->cap;
+    p.row_bytes = c->cfg.head_dim * c->kv_elt;
+    dynts::tree_move_kernel<<<dim3(nx, (unsigned)p.seqs.n, 1), 256, 0, c->stream>>>(p);
+    CUDA_TRY(cudaGetLastError());
+    dynts::tree_lengths_kernel<<<(unsigned)p.seqs.n, 128, 0, c->stream>>>(p);
+    CUDA_TRY(cudaGetLastError());
+    c->launches += 2;
   }
   c->staged_h.clear();
   for (int b = 0; b < Nb; ++b) {
@@ -1953,6 +2127,73 @@ dynts_status_t dynts_rope(const void* q, const void* k, const int* pos, void* q_
   }
   CUDA_TRY(cudaGetLastError());
   return DYNTS_OK;
+}
+
+/* ---- a token per row of logits ------------------------------------------------------------- */
+
+}  // extern "C"
+
+namespace {
+
+constexpr int kSampleDevices = 64;
+std::atomic<bool> g_sample_attr[kSampleDevices][2];  // function attributes are set once per device
+
+template <typename X>
+dynts_status_t launch_sample(const dynts::SampleParams& p, int n_rows, int which, cudaStream_t st) {
+  int dev = -1;
+  CUDA_TRY(cudaGetDevice(&dev));
+  if (dev < 0 || dev >= kSampleDevices || !g_sample_attr[dev][which]) {
+    CUDA_TRY(cudaFuncSetAttribute(dynts::sample_kernel<X>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)dynts::kSmSmemBytes));
+    if (dev >= 0 && dev < kSampleDevices) g_sample_attr[dev][which] = true;
+  }
+  CUDA_TRY(launch_clusters(dynts::sample_kernel<X>, (unsigned)p.cluster, dim3((unsigned)n_rows * (unsigned)p.cluster, 1, 1), dynts::kSmThreads, dynts::kSmSmemBytes, st, p));
+  return DYNTS_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+dynts_status_t dynts_sample(const void* logits, int dtype, int n_rows, int vocab, long long row_stride, const float* u, const dynts_sample_opts_t* opts, int* tokens,
+                            float* logprobs, void* stream) {
+  if (dtype != DYNTS_BF16 && dtype != DYNTS_FP32) return fail(DYNTS_ERR_INVALID_ARG, "dtype must be DYNTS_BF16 or DYNTS_FP32");
+  if (n_rows < 0 || vocab < 1 || vocab > dynts::kSmMaxVocab) return fail(DYNTS_ERR_INVALID_ARG, "%d rows of %d logits: a row has 1 to %d", n_rows, vocab, dynts::kSmMaxVocab);
+  if (n_rows > (1 << 27)) return fail(DYNTS_ERR_INVALID_ARG, "%d rows are beyond the launch limits", n_rows);
+  if (row_stride == 0) row_stride = vocab;
+  if (row_stride < vocab || row_stride >= (1ll << 40)) return fail(DYNTS_ERR_INVALID_ARG, "row stride %lld does not cover a row, or is beyond the launch limits", row_stride);
+  dynts_sample_opts_t o;
+  memset(&o, 0, sizeof(o));
+  o.temperature = o.top_p = 1.f;
+  if (opts) o = *opts;
+  if (!o.temperatures && !(o.temperature >= 0.f && !std::isinf(o.temperature))) return fail(DYNTS_ERR_INVALID_ARG, "temperature %g must be finite and not negative", o.temperature);
+  if (!o.top_ks && o.top_k < 0) return fail(DYNTS_ERR_INVALID_ARG, "top_k %d must not be negative", o.top_k);
+  if (!o.top_ps && !(o.top_p > 0.f && o.top_p <= 1.f)) return fail(DYNTS_ERR_INVALID_ARG, "top_p %g must be above 0 and at most 1", o.top_p);
+  if (!o.min_ps && !(o.min_p >= 0.f && o.min_p <= 1.f)) return fail(DYNTS_ERR_INVALID_ARG, "min_p %g must be from 0 to 1", o.min_p);
+  if (n_rows == 0) return DYNTS_OK;
+  if (!logits || !u || !tokens) return fail(DYNTS_ERR_INVALID_ARG, "NULL tensor pointer");
+  const uintptr_t words = reinterpret_cast<uintptr_t>(u) | reinterpret_cast<uintptr_t>(tokens) | reinterpret_cast<uintptr_t>(logprobs) | reinterpret_cast<uintptr_t>(o.temperatures) |
+                          reinterpret_cast<uintptr_t>(o.top_ks) | reinterpret_cast<uintptr_t>(o.top_ps) | reinterpret_cast<uintptr_t>(o.min_ps);
+  if (words % 4 || reinterpret_cast<uintptr_t>(logits) % (dtype == DYNTS_FP32 ? 4 : 2)) return fail(DYNTS_ERR_INVALID_ARG, "tensor pointers must be aligned to their elements");
+  dynts::SampleParams p;
+  p.logits = logits;
+  p.row_stride = row_stride;
+  p.u = u;
+  p.temperatures = o.temperatures;
+  p.top_ks = o.top_ks;
+  p.top_ps = o.top_ps;
+  p.min_ps = o.min_ps;
+  p.tokens = tokens;
+  p.logprobs = logprobs;
+  p.vocab = vocab;
+  p.temperature = o.temperature;
+  p.top_p = o.top_p;
+  p.min_p = o.min_p;
+  p.top_k = o.top_k;
+  // CTAs per row: while they fit the SMs at once, and have 2048 tokens each.
+  p.cluster = 1;
+  while (p.cluster < dynts::kSmMaxCluster && 2ll * p.cluster * n_rows <= 2 * 148 && vocab / (2 * p.cluster) >= 2048) p.cluster *= 2;
+  const cudaStream_t st = static_cast<cudaStream_t>(stream);
+  return dtype == DYNTS_FP32 ? launch_sample<float>(p, n_rows, 0, st) : launch_sample<__nv_bfloat16>(p, n_rows, 1, st);
 }
 
 /* ---- Importance Predictor head ------------------------------------------------------------ */

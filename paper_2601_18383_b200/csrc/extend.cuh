@@ -12,7 +12,13 @@
 //   x   = c tanh(x / c)                      if a cap c > 0 is given
 //   x  -= slope_h |p_i - p_j|                if slopes are given
 //   row j is visible  <=>  j <= n + i, or j is one of the chunk's first `prefix` rows;
-//                          and |p_i - p_j| < window, if a window is given
+//                          and |p_i - p_j| < window or p_j < sinks, if a window is given;
+//                          and, in a tree (tree.cuh), j < n, or row j's node is node i or an ancestor of it:
+//                          0 <= order_i - order_j < size_j
+// Positions ascend with the rows; a node's is the tokens seen plus its depth, and so at most what it would be in a line.
+// So the rows with p_j < sinks are among the first `sinks`, and a row more than `window` rows behind the first row of the
+// chunk (of the query tile, in a line) is outside every window there: an item's key tiles are those of the sinks and
+// those from the window's oldest on, two runs of tiles counted through ("virtual" tiles, see ext_tile_of).
 // A token always sees itself, so no row of weights is empty.  (A logit of -inf weighs nothing; a token whose visible
 // logits are all -inf has no answer: NaN.)  All logits are kept in base-2 units
 // (times log2 e), sums and maxima in fp32.
@@ -62,6 +68,8 @@ struct ExtendParams {
   int layer0, n_layers, total;
   int Nb, Hq, Hkv, G, d, cap;
   int window;         // 0: none
+  int sinks;          // rows of positions below it are visible whatever the window
+  const int4* tree;   // [total] {order, size, depth, parent} of the chunk's nodes, or NULL: a line
   int publish;        // the storing kernel advances the lengths when it is done
   int* held;          // [2][kExtSeqs], written by the storing kernel: rows held before the chunk (-1: it does not fit), tokens seen before it
   int accumulate;     // the mass is added to the scores
@@ -82,7 +90,7 @@ struct ExtendParams {
 // CTA c takes the shares [c * q + min(c, rem), ...).  What CTA c does of item i is described by 32 words at slot i + c
 // (an item's parts and a CTA's pieces both lie side by side).
 constexpr int kPlanWords = 32;
-enum PlanWord { kPwTiles, kPwFirst, kPwTok, kPwLayer, kPwHead, kPwHeld, kPwTok0, kPwRows, kPwNew, kPwSlab, kPwParts, kPwPlace, kPwBase, kPwList, kPwPrefix, kPwSeen };
+enum PlanWord { kPwTiles, kPwFirst, kPwTok, kPwLayer, kPwHead, kPwHeld, kPwTok0, kPwRows, kPwNew, kPwSlab, kPwParts, kPwPlace, kPwBase, kPwList, kPwPrefix, kPwSeen, kPwSinks, kPwJump };
 struct ExtendPlan {
   unsigned cum[kExtSeqs + 1];  // shares before each sequence's first item
   unsigned per[kExtSeqs];      // shares of an item
@@ -93,6 +101,21 @@ struct ExtendPlan {
   int lh;                      // n_layers * Hkv
   int* words;                  // [items + CTAs][kPlanWords], or NULL: no plan is wanted
 };
+// An item's key tiles: `sinks` tiles from row 0 on, and behind a gap of `jump` tiles the rest.
+struct ExtTiles {
+  int sinks, jump;
+};
+__device__ __forceinline__ int ext_tile_of(int v, int sinks, int jump) { return v < sinks ? v : v + jump; }
+// i0: the query tile's first token; K: rows of a tile.
+__device__ __forceinline__ ExtTiles ext_tiles(int window, int sinks, bool tree, int n, int i0, int K) {
+  ExtTiles e{0, 0};
+  if (window > 0) {
+    const int first = max(0, n + (tree ? 0 : i0) - window + 1) / K;
+    e.sinks = min(sinks / K + (sinks % K != 0 ? 1 : 0), first);
+    e.jump = first - e.sinks;
+  }
+  return e;
+}
 __device__ __forceinline__ unsigned plan_share0(const ExtendPlan& p, unsigned cta) { return cta * p.share_q + min(cta, p.share_rem); }
 __device__ __forceinline__ unsigned plan_cta_of(const ExtendPlan& p, unsigned share) {
   const unsigned big = p.share_rem * (p.share_q + 1u);
@@ -155,9 +178,8 @@ __device__ __forceinline__ void ext_write_plan(const ExtendParams& p, const Exte
     const int i0 = qt * q.tokens_per_tile, i1 = min(t, i0 + q.tokens_per_tile);
     const bool ok = n >= 0 && n + t <= p.cap;  // (else nothing is stored and nothing computed)
     const int seen = n + max(i1, prefix);
-    // (positions ascend with the rows, so a row more than `window` rows back is more than `window` positions back)
-    const int first = p.window > 0 ? max(0, n + i0 - p.window + 1) / kExtTileKeys : 0;
-    const int total = (seen + kExtTileKeys - 1) / kExtTileKeys - first;
+    const ExtTiles tiles = ext_tiles(p.window, p.sinks, p.tree != nullptr, n, i0, kExtTileKeys);
+    const int total = (seen + kExtTileKeys - 1) / kExtTileKeys - tiles.jump;
     const unsigned per = q.per[s], start = q.cum[s] + (unsigned)idx * per;
     const unsigned ca = plan_cta_of(q, start), cb = plan_cta_of(q, start + per - 1u);
     const int layer = lh / p.Hkv, h = lh - layer * p.Hkv;
@@ -180,7 +202,7 @@ __device__ __forceinline__ void ext_write_plan(const ExtendParams& p, const Exte
           const int place = (int)(2u * c) + (c == ca ? 1 : 0);
           if (lo < hi) q.words[(size_t)(item + (int)ca + rank + __popc(has & ((1u << lane) - 1u))) * kPlanWords + kPwList] = place;
           w[kPwTiles] = hi - lo;
-          w[kPwFirst] = first + lo;
+          w[kPwFirst] = lo;
           w[kPwTok] = p.seqs.tok0[s] + i0;
           w[kPwLayer] = layer;
           w[kPwHead] = h;
@@ -194,6 +216,8 @@ __device__ __forceinline__ void ext_write_plan(const ExtendParams& p, const Exte
           w[kPwBase] = item + (int)ca;
           w[kPwPrefix] = prefix;
           w[kPwSeen] = p.tot[b];
+          w[kPwSinks] = tiles.sinks;
+          w[kPwJump] = tiles.jump;
         }
         rank += __popc(has);
       }
@@ -247,7 +271,7 @@ __global__ void __launch_bounds__(256) extend_store_kernel(const __grid_constant
       *reinterpret_cast<uint4*>(static_cast<T*>(p.V) + row * p.d + piece * E) = vv;
     }
     if (piece == 0) {
-      p.pos[row] = p.tot[b] + i;
+      p.pos[row] = p.tot[b] + (p.tree ? p.tree[tok].z : i);
       p.score[row] = p.s_new ? p.s_new[tok] : 0.f;
       p.comp[row] = 0.f;
     }
@@ -327,6 +351,23 @@ __global__ void __launch_bounds__(kExtSeqs) extend_commit_kernel(const ExtendSeq
   tot[b] += t;
   active[b] = 1;
 }
+
+// Whether a query sees a row that is no later than it: by the window and the sinks, and in a tree by the row's node.
+__device__ __forceinline__ bool ext_in_window(const ExtendParams& p, int apart, int pos) { return p.window == 0 || apart < p.window || pos < p.sinks; }
+struct ExtNode {  // a row's node (rows held: of everything), or a query's
+  int order, size, depth;
+};
+__device__ __forceinline__ ExtNode ext_node(const ExtendParams& p, int tok0, int i, int in) {  // i < 0: a row held; in: nodes of the chunk
+  ExtNode e{0, 0x7fffffff, i};
+  if (p.tree && i >= 0 && i < in) {
+    const int4 w = p.tree[tok0 + i];
+    e.order = w.x;
+    e.size = w.y;
+    e.depth = w.z;
+  }
+  return e;
+}
+__device__ __forceinline__ bool ext_below(int order, const ExtNode& row) { return (unsigned)(order - row.order) < (unsigned)row.size; }
 
 // A logit in base-2 units (before the visibility test), from the raw dot product.
 __device__ __forceinline__ float ext_logit_exact(const ExtendParams& p, float dot, float slope, int apart) {
@@ -412,12 +453,15 @@ __global__ void __launch_bounds__(kExtGenericThreads) extend_generic_kernel(cons
     *reinterpret_cast<float4*>(sQ + r * d + c) = y;
   }
   // this warp's rows
-  int tok[4];
+  int tok[4], at[4], order[4];            // token, its position behind the tokens seen, its place in the tree
   float slope[4], m[4], l[4], acc[4][8];  // l: this lane's part of the row's sum
 #pragma unroll
   for (int u = 0; u < 4; ++u) {
     const int r = r0 + warp * 4 + u;
     tok[u] = min(r / p.G, e.t - 1);
+    const ExtNode node = ext_node(p, p.seqs.tok0[s], tok[u], e.t);
+    at[u] = node.depth;
+    order[u] = node.order;
     slope[u] = p.slopes ? p.slopes[h * p.G + r % p.G] : 0.f;
     m[u] = -CUDART_INF_F;
     l[u] = 0.f;
@@ -427,9 +471,10 @@ __global__ void __launch_bounds__(kExtGenericThreads) extend_generic_kernel(cons
   const int prefix = p.seqs.prefix[s];
   const int i0 = r0 / p.G, i1 = min(e.t - 1, (r0 + rows - 1) / p.G);
   const int end = e.n + max(i1 + 1, prefix);
-  // (positions ascend with the rows, so a row more than `window` rows back is more than `window` positions back)
-  const int begin = p.window > 0 ? max(0, e.n + i0 - p.window + 1) : 0;
-  for (int k0 = (begin / kExtGenericKeys + rank) * kExtGenericKeys; k0 < end; k0 += kExtGenericKeys * cluster) {
+  const ExtTiles tiles = ext_tiles(p.window, p.sinks, p.tree != nullptr, e.n, i0, kExtGenericKeys);
+  for (int v = rank;; v += cluster) {
+    const int k0 = ext_tile_of(v, tiles.sinks, tiles.jump) * kExtGenericKeys;
+    if (k0 >= end) break;
     __syncthreads();
 #pragma unroll 2
     for (int x = lane; x < 4 * pieces; x += 32) {  // a warp stages four rows of K and of V
@@ -457,11 +502,12 @@ __global__ void __launch_bounds__(kExtGenericThreads) extend_generic_kernel(cons
       }
     }
     const int j = k0 + lane;
+    const ExtNode row = ext_node(p, p.seqs.tok0[s], j - e.n, e.t);
     float w[4];
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
-      const int apart = abs(e.tot + tok[u] - sP[lane]);
-      const bool visible = j < e.n + max(tok[u] + 1, prefix) && (p.window == 0 || apart < p.window);
+      const int apart = abs(e.tot + at[u] - sP[lane]);
+      const bool visible = j < e.n + max(tok[u] + 1, prefix) && ext_in_window(p, apart, sP[lane]) && ext_below(order[u], row);
       const float x = visible ? ext_logit_exact(p, dot[u], slope[u], apart) : -CUDART_INF_F;
       float mx = x;
 #pragma unroll
@@ -605,6 +651,7 @@ __global__ void __launch_bounds__(kExtGenericThreads) extend_generic_mass_kernel
   __syncthreads();
   const int j = k0 + lane;
   const int pj = j < e.n + e.t ? p.pos[slab * p.cap + j] : 0;
+  const ExtNode row = ext_node(p, p.seqs.tok0[s], j - e.n, e.t);
   const int prefix = p.seqs.prefix[s], all = e.t * p.G;
   // (a token that sees row j: i >= j - n, or any where j lies before n + prefix)
   const int first = e.n + prefix > k0 ? 0 : max(0, k0 - e.n) * p.G;
@@ -614,9 +661,9 @@ __global__ void __launch_bounds__(kExtGenericThreads) extend_generic_mass_kernel
     __syncwarp();
 #pragma unroll 2
     for (int x = lane; x < 4 * pieces; x += 32) {
-      const int rl = (int)(((unsigned)x * piece_inv) >> 16), c = 4 * (x - rl * pieces), row = min(r + rl, all - 1), i = row / p.G;
+      const int rl = (int)(((unsigned)x * piece_inv) >> 16), c = 4 * (x - rl * pieces), qr = min(r + rl, all - 1), i = qr / p.G;
       *reinterpret_cast<float4*>(q4 + rl * d + c) =
-          ext_row_value4<T, false>(p.q, (tok_base + i) * p.q_stride + (size_t)(h * p.G + row - i * p.G) * d + c, 1.f);
+          ext_row_value4<T, false>(p.q, (tok_base + i) * p.q_stride + (size_t)(h * p.G + qr - i * p.G) * d + c, 1.f);
     }
     __syncwarp();
     float dot[4] = {0.f, 0.f, 0.f, 0.f};
@@ -633,8 +680,9 @@ __global__ void __launch_bounds__(kExtGenericThreads) extend_generic_mass_kernel
     for (int u = 0; u < 4; ++u) {
       if (r + u >= all) break;
       const int i = (r + u) / p.G, head = h * p.G + r + u - i * p.G;
-      const int apart = abs(e.tot + i - pj);
-      if (j < e.n + max(i + 1, prefix) && (p.window == 0 || apart < p.window))
+      const ExtNode node = ext_node(p, p.seqs.tok0[s], i, e.t);
+      const int apart = abs(e.tot + node.depth - pj);
+      if (j < e.n + max(i + 1, prefix) && ext_in_window(p, apart, pj) && ext_below(node.order, row))
         sum += exp2f(ext_logit_exact(p, dot[u], p.slopes ? p.slopes[head] : 0.f, apart) - lse[r + u]);
     }
   }

@@ -221,14 +221,18 @@ __device__ __forceinline__ float4 xt_row_again(const ExtendTcParams& p, int d, i
   const int ti = r / x.G, g = r - ti * x.G, h = word(kPwHead), layer = word(kPwLayer), i = word(kPwTok0) + ti;
   const size_t slab = (size_t)word(kPwSlab);
   const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(x.q) + ((size_t)layer * x.total + word(kPwTok) + ti) * x.q_stride + (size_t)(h * x.G + g) * 128;
-  const int me = word(kPwSeen) + i;
+  const int held = word(kPwHeld), chunk0 = word(kPwTok) - word(kPwTok0), in = word(kPwNew);
+  const ExtNode node = ext_node(x, chunk0, i, in);
+  const int me = word(kPwSeen) + node.depth;
   const float slope = x.slopes ? x.slopes[h * x.G + g] : 0.f;
-  const int kt0 = word(kPwFirst), k0 = kt0 * kPfKeys, end = min((kt0 + word(kPwTiles)) * kPfKeys, word(kPwHeld) + max(i + 1, word(kPwPrefix)));
+  const int v0 = word(kPwFirst) * kPfKeys, v_end = v0 + word(kPwTiles) * kPfKeys, end = held + max(i + 1, word(kPwPrefix));
+  const int sinks = word(kPwSinks), jump = word(kPwJump);
+  auto row_of = [&](int v) { return ext_tile_of(v / kPfKeys, sinks, jump) * kPfKeys + v % kPfKeys; };
   auto logit = [&](int j, bool& visible) {
     visible = false;
     if (j >= end) return 0.f;
-    const int apart = abs(me - x.pos[slab * x.cap + j]);
-    if (x.window > 0 && apart >= x.window) return 0.f;
+    const int pos = x.pos[slab * x.cap + j], apart = abs(me - pos);
+    if (!ext_in_window(x, apart, pos) || !ext_below(node.order, ext_node(x, chunk0, j - held, in))) return 0.f;
     visible = true;
     float dot = 0.f;
 #pragma unroll 4
@@ -249,9 +253,9 @@ __device__ __forceinline__ float4 xt_row_again(const ExtendTcParams& p, int d, i
   };
   if (redo) {
     float m = -CUDART_INF_F, l = 0.f;
-    for (int kb = k0; kb < end; kb += 32) {
+    for (int v = v0; v < v_end; v += 32) {
       bool visible;
-      const float y = logit(kb + lane, visible);
+      const float y = logit(row_of(v) + lane, visible);
       float mx = visible ? y : -CUDART_INF_F;
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
@@ -267,18 +271,19 @@ __device__ __forceinline__ float4 xt_row_again(const ExtendTcParams& p, int d, i
   // redo nothing the row sees weighs anything, and the weights are exp2(-inf + inf): NaN.)
   const bool none = !redo && lse == -CUDART_INF_F;
   float acc[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int kb = k0; kb < end; kb += 32) {
+  for (int v = v0; v < v_end; v += 32) {
+    const int kb = row_of(v);
     bool visible;
     const float y = logit(kb + lane, visible);
     const float w = visible && !none ? exp2f(y - lse) : 0.f;
     for (unsigned some = __ballot_sync(0xffffffffu, w != 0.f); some; some &= some - 1) {
       const int kk = __ffs(some) - 1;
       const float wk = __shfl_sync(0xffffffffu, w, kk);
-      const float4 v = ext_row_value4<__nv_bfloat16, KV8>(x.V, (slab * x.cap + kb + kk) * 128 + 4 * lane, 1.f);
-      acc[0] = fmaf(wk, v.x, acc[0]);
-      acc[1] = fmaf(wk, v.y, acc[1]);
-      acc[2] = fmaf(wk, v.z, acc[2]);
-      acc[3] = fmaf(wk, v.w, acc[3]);
+      const float4 vv = ext_row_value4<__nv_bfloat16, KV8>(x.V, (slab * x.cap + kb + kk) * 128 + 4 * lane, 1.f);
+      acc[0] = fmaf(wk, vv.x, acc[0]);
+      acc[1] = fmaf(wk, vv.y, acc[1]);
+      acc[2] = fmaf(wk, vv.z, acc[2]);
+      acc[3] = fmaf(wk, vv.w, acc[3]);
     }
   }
   return make_float4(acc[0], acc[1], acc[2], acc[3]);
@@ -628,7 +633,9 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
     int g = 0;
     for (; slot < slot_end && !*s_abort; go_next()) {
       ask_next();
-      const int nkt = word(kPwTiles), kt_new = word(kPwFirst) + nkt - 1, slab = word(kPwSlab), end = word(kPwHeld) + word(kPwNew);
+      const int nkt = word(kPwTiles), v_new = word(kPwFirst) + nkt - 1, slab = word(kPwSlab), end = word(kPwHeld) + word(kPwNew);
+      const int sinks = MODS ? word(kPwSinks) : 0, jump = MODS ? word(kPwJump) : 0;
+      auto tile_row = [&](int v) { return ext_tile_of(v, sinks, jump) * kPfKeys; };
       // 8-bit rows: this warp's 32 rows of a tile, eight at a time, each eight a whole tile ahead in registers
       XtCodes codes[4];
       const uint8_t* src = KV8 ? static_cast<const uint8_t*>(x.K) + (size_t)slab * x.cap * 128 : nullptr;
@@ -636,7 +643,7 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
       if constexpr (KV8) {
         if (nkt > 0) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) xt_load_codes(codes[i], src, kt_new * kPfKeys + sub + 8 * i, end, lane);
+          for (int i = 0; i < 4; ++i) xt_load_codes(codes[i], src, tile_row(v_new) + sub + 8 * i, end, lane);
         }
       }
       for (int j = 0; j < nkt; ++j, ++g) {
@@ -650,10 +657,10 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
         if (new_q) load_q();
         if constexpr (KV8) {
           uint8_t* tile = sm + kPfQBytes + (uint32_t)(g & 1) * kPfKvBytes;
-          const int k0 = (kt_new - j - 1) * kPfKeys + sub;
+          const int k0 = tile_row(v_new - j - 1) + sub;  // (of the piece's tiles, while j + 1 < nkt)
           // (four tiles further on towards the older rows: asked into L2)
           if (lane == 0 && j + 4 < nkt)
-            asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(src + (size_t)(k0 - 3 * kPfKeys) * 128), "r"(32 * 128) : "memory");
+            asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(src + (size_t)(tile_row(v_new - j - 4) + sub) * 128), "r"(32 * 128) : "memory");
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             xt_store_codes<false>(codes[i], tile, kPfKvBytes / 2, sub + 8 * i, lane);
@@ -664,7 +671,7 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
           if (lane == 0) mbar_arrive(bar(1 + (g & 1)));
           __syncwarp();
         } else {
-          load_tile(warp == 8, g, (kt_new - j) * kPfKeys, slab);
+          load_tile(warp == 8, g, tile_row(v_new - j), slab);
         }
       }
     }
@@ -707,7 +714,9 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
           }
         }
         if (l_slot >= slot_end) return;
-        const int row = (__shfl_sync(0xffffffffu, l_d, kPwFirst) + l_nkt - 1 - l_j) * kPfKeys;
+        int row = __shfl_sync(0xffffffffu, l_d, kPwFirst) + l_nkt - 1 - l_j;
+        if constexpr (MODS) row = ext_tile_of(row, __shfl_sync(0xffffffffu, l_d, kPwSinks), __shfl_sync(0xffffffffu, l_d, kPwJump));
+        row *= kPfKeys;
         ++l_j;
         load_tile(is_s, gl, row, __shfl_sync(0xffffffffu, l_d, kPwSlab));
       };
@@ -802,7 +811,7 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
       ask_next();
       const int nkt = word(kPwTiles);
       if (nkt == 0) continue;
-      const int kt_new = word(kPwFirst) + nkt - 1;  // its newest tile
+      const int v_new = word(kPwFirst) + nkt - 1;  // its newest tile
       const int rows = word(kPwRows), held = word(kPwHeld), i0 = word(kPwTok0), prefix = word(kPwPrefix);
       const bool live = wq * 32 < rows;
       const int r = min(wq * 32 + lane, rows - 1);  // (a lane without a query repeats the last row's visibility)
@@ -810,13 +819,21 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
       const int lim = held + max(ti + 1, prefix);   // rows [0, lim) are visible
       // Tiles that some token of the query tile does not see whole, and one more, are the first group's: after them every row
       // that sees anything has its reference.  (With a window a token of a prefix may see only rows around its own: down to those.)
-      const int whole_to = held + (MODS && x.window > 0 ? i0 : max(i0 + 1, prefix) - 1);
-      const int ramp = min(nkt, max(0, kt_new - whole_to / kPfKeys) + 1);
+      // (A tree's nodes see the rows held whole, or with a window around their own rows of the chunk.)
+      const bool tree = MODS && x.tree != nullptr;
+      const int whole_to = held + (tree ? (x.window > 0 ? 0 : -1) : MODS && x.window > 0 ? i0 : max(i0 + 1, prefix) - 1);
+      auto tile_row = [&](int v) { return (MODS ? ext_tile_of(v, word(kPwSinks), word(kPwJump)) : v) * kPfKeys; };
+      const int ramp = min(nkt, max(0, tile_row(v_new) / kPfKeys - whole_to / kPfKeys) + 1);
       const int* pos_row = nullptr;
-      int tot = 0;
+      int tot = 0, place = ti, order = 0;  // place: the token's position, the tokens seen not counted
       float slope = 0.f;
       if constexpr (MODS) {
         tot = word(kPwSeen);
+        if (tree) {
+          const int4 node = x.tree[word(kPwTok) - i0 + ti];
+          place = node.z;
+          order = node.x;
+        }
         pos_row = x.pos + (size_t)word(kPwSlab) * x.cap;
         if (x.slopes) slope = x.slopes[word(kPwHead) * x.G + r % x.G] * 1.4426950408889634f;
       }
@@ -833,7 +850,7 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
         // One tile: S of flat tile g to P, a chunk of columns at a time.  In the ramp part of the tile may be hidden and
         // the reference may not be set yet: S is read twice.
         const bool in_ramp = j < ramp;
-        const int g = g0 + j, key0 = (kt_new - j) * kPfKeys;
+        const int g = g0 + j, key0 = tile_row(v_new - j);
         const uint32_t ts = t_row + 64u * (uint32_t)(g & 1);
         int pos_a = 0, pos_b = 0;
         if constexpr (MODS) {  // positions, the chunk's first token being 0: two per lane
@@ -842,10 +859,11 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
         }
         XtCodes vc[2];
         if constexpr (KV8) {  // this warp's 16 rows of V
+          const int older = MODS && j + 4 < nkt ? tile_row(v_new - j - 4) : key0 - 4 * kPfKeys;
           xt_load_codes(vc[0], v_codes, key0 + 16 * wq, end, lane);
           xt_load_codes(vc[1], v_codes, key0 + 16 * wq + 8, end, lane);
           if (lane == 0 && j + 4 < nkt)
-            asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(v_codes + (size_t)(key0 + 16 * wq - 4 * kPfKeys) * 128), "r"(16 * 128) : "memory");
+            asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(v_codes + (size_t)(older + 16 * wq) * 128), "r"(16 * 128) : "memory");
         }
         auto widen_v = [&]() {
           uint8_t* vt = sm + kPfQBytes + (2 + (uint32_t)(g & 1)) * kPfKvBytes;
@@ -867,7 +885,8 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
           bool border = false, beside = false;
           float at = 0.f;                                       // this row's token
           // (the staging tile: positions counted from the tile's newest row, [64] as integers and [64] as floats)
-          int me = 0;
+          int me = 0, sink_to = 0;
+          bool branch = false;  // rows of other branches of the tree
           if constexpr (MODS) {
             // From the newest: a token is at most 64 positions closer to it than to any row it sees, so both terms of a
             // bias are about as small as the bias.  (From the first, which may have survived evictions from far back, a recent
@@ -878,11 +897,22 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
             sts_i(stage + 128u + 4u * lane, pos_b - p0);
             sts_f(stage + 256u + 4u * lane, (float)(pos_a - p0));
             sts_f(stage + 384u + 4u * lane, (float)(pos_b - p0));
-            me = ti - p0;
+            me = place - p0;
             at = (float)me;
+            sink_to = x.sinks - tot - p0;
             const bool fresh = key0 + kPfKeys > held;  // the tile holds rows of the chunk
             // the tile's first position against the warp's last token (in tiles with rows of the chunk: always compared)
-            border = x.window > 0 && (fresh || __shfl_sync(0xffffffffu, ti, 31) - __shfl_sync(0xffffffffu, pos_a, 0) >= x.window);
+            border = x.window > 0 && (fresh || __reduce_max_sync(0xffffffffu, place) - __shfl_sync(0xffffffffu, pos_a, 0) >= x.window);
+            branch = tree && fresh;
+            if (branch) {
+              const int chunk0 = word(kPwTok) - i0, in = end - held;
+#pragma unroll
+              for (int o = 0; o < kPfKeys; o += 32) {
+                const ExtNode node = ext_node(x, chunk0, key0 + o + lane - held, in);
+                sts_i(stage + 768u + 4u * (uint32_t)(o + lane), node.order);
+                sts_i(stage + 1024u + 4u * (uint32_t)(o + lane), node.size);
+              }
+            }
             beside = fresh && prefix > 0;  // rows of later positions may be visible
             __syncwarp();
           }
@@ -924,10 +954,20 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
 #pragma unroll
                 for (int c = 0; c < CH; c += 4) {
                   const int4 y = lds_i4(stage + 4u * (uint32_t)(hb + c));
-                  if (abs(me - y.x) >= x.window) sv[c] = 0xff800000u;  // -inf
-                  if (abs(me - y.y) >= x.window) sv[c + 1] = 0xff800000u;
-                  if (abs(me - y.z) >= x.window) sv[c + 2] = 0xff800000u;
-                  if (abs(me - y.w) >= x.window) sv[c + 3] = 0xff800000u;
+                  if (abs(me - y.x) >= x.window && y.x >= sink_to) sv[c] = 0xff800000u;  // -inf
+                  if (abs(me - y.y) >= x.window && y.y >= sink_to) sv[c + 1] = 0xff800000u;
+                  if (abs(me - y.z) >= x.window && y.z >= sink_to) sv[c + 2] = 0xff800000u;
+                  if (abs(me - y.w) >= x.window && y.w >= sink_to) sv[c + 3] = 0xff800000u;
+                }
+              }
+              if (branch) {
+#pragma unroll
+                for (int c = 0; c < CH; c += 4) {
+                  const int4 y = lds_i4(stage + 768u + 4u * (uint32_t)(hb + c)), z = lds_i4(stage + 1024u + 4u * (uint32_t)(hb + c));
+                  if ((unsigned)(order - y.x) >= (unsigned)z.x) sv[c] = 0xff800000u;
+                  if ((unsigned)(order - y.y) >= (unsigned)z.y) sv[c + 1] = 0xff800000u;
+                  if ((unsigned)(order - y.z) >= (unsigned)z.z) sv[c + 2] = 0xff800000u;
+                  if ((unsigned)(order - y.w) >= (unsigned)z.w) sv[c + 3] = 0xff800000u;
                 }
               }
             }
@@ -1043,7 +1083,7 @@ __device__ __forceinline__ void xm_seek(XmCursor& c, int it, int n_items, const 
     c.h = lh - c.layer * p.x.Hkv;
     int lo = c.k0 < c.n + p.x.seqs.prefix[c.s] ? 0 : (c.k0 - c.n) / tps;
     int hi = (c.t + tps - 1) / tps;
-    if (p.x.window > 0) {  // a token is at least as many positions behind a row as it is rows behind it
+    if (p.x.window > 0 && !p.x.tree && c.k0 >= p.x.sinks) {  // a token is at least as many positions behind a row as it is rows behind it
       const long long last = (long long)p.x.window + c.k0 + kXmItemKeys - 1 - c.n;  // tokens from here on see none of the rows
       hi = last <= 0 ? 0 : (int)min((long long)hi, (last + tps - 1) / tps);
     }
@@ -1263,10 +1303,17 @@ extend_mass_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_con
       // the tokens that see row j: [i_lo, i_hi)
       int i_lo = j < cur.n + prefix ? 0 : j - cur.n, i_hi = mine ? cur.t : 0;
       float rel = 0.f;
+      const bool tree = MODS && x.tree != nullptr;
+      ExtNode mine_node{0, 0x7fffffff, 0};
+      bool sink = true;  // no window concerns the row
+      int at = 0;
       if constexpr (MODS) {
-        const int at = mine ? x.pos[row] - x.held[kExtSeqs + cur.s] : 0;  // the row's position, the chunk's first token being 0
+        at = mine ? x.pos[row] - x.held[kExtSeqs + cur.s] : 0;  // the row's position, the chunk's first token being 0
         rel = (float)at;
-        if (x.window > 0) {
+        sink = x.window == 0 || at + x.held[kExtSeqs + cur.s] < x.sinks;
+        if (tree) {
+          mine_node = ext_node(x, x.seqs.tok0[cur.s], j - cur.n, cur.t);
+        } else if (!sink) {
           i_lo = max(i_lo, (int)max(0ll, (long long)at - x.window + 1));  // (in 64 bits: a window may be as wide as an int)
           i_hi = (int)min((long long)i_hi, max(0ll, (long long)at + x.window));
         }
@@ -1293,14 +1340,15 @@ extend_mass_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_con
 #pragma unroll
         for (int o = 0; o < kXmRows / 32; ++o) {
           const uint32_t at = 4u * (uint32_t)(32 * o + lane);
-          sts_f(s_add + at, biased ? fmaf(lds_f(s_slope + at), lds_f(s_token + at), la[o]) : la[o]);
+          sts_f(s_add + at, biased && !tree ? fmaf(lds_f(s_slope + at), lds_f(s_token + at), la[o]) : la[o]);
           if (st + 1 < n_step) la[o] = ask(st + 1, 32 * o);
         }
         __syncwarp();
         const int i0 = (cur.lo + st) * tps;
         const int rows = min(step_rows, all_rows - (cur.lo + st) * step_rows);
         const int c_lo = min(kXmRows, max(0, (i_lo - i0) * x.G)), c_hi = min(rows, max(0, (min(i_hi, i0 + tps) - i0) * x.G));
-        const bool full = __all_sync(0xffffffffu, c_lo == 0 && c_hi == step_rows);
+        // (in a tree rows of the chunk are seen by parts of it, and positions do not follow the tokens)
+        const bool full = __all_sync(0xffffffffu, c_lo == 0 && c_hi == step_rows && !(tree && (j >= cur.n || !sink)));
         const float off0 = (float)i0 - rel;
         const bool beside = biased && prefix > 0;  // rows of later positions may be seen
         xt_wait(bar(2 + wg), (uint32_t)(g & 1), abort_flag, p);
@@ -1320,6 +1368,12 @@ extend_mass_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_con
             if (x.cap_logit > 0.f) scale = xt_cap(sv, p);
           }
           const uint64_t scale2 = tc5::f2_pack(scale, scale), off2 = tc5::f2_pack(off0, off0);
+          int c_order = 0, c_depth = 0;  // of the node of column hb + lane
+          if (tree) {
+            const ExtNode node = ext_node(x, x.seqs.tok0[cur.s], min(i0 + (hb + lane) / x.G, cur.t - 1), cur.t);
+            c_order = node.order;
+            c_depth = node.depth;
+          }
           auto add_up = [&](auto masked) {
 #pragma unroll
             for (int c = 0; c < 32; c += 4) {
@@ -1329,6 +1383,11 @@ extend_mass_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_con
                 float4 ns = make_float4(0.f, 0.f, 0.f, 0.f);
                 if (biased) ns = lds_f4(s_slope + 4u * (uint32_t)(hb + c));
                 if (!biased) {
+                } else if (tree) {
+                  add.x += ns.x * fabsf((float)__shfl_sync(0xffffffffu, c_depth, c) - rel);
+                  add.y += ns.y * fabsf((float)__shfl_sync(0xffffffffu, c_depth, c + 1) - rel);
+                  add.z += ns.z * fabsf((float)__shfl_sync(0xffffffffu, c_depth, c + 2) - rel);
+                  add.w += ns.w * fabsf((float)__shfl_sync(0xffffffffu, c_depth, c + 3) - rel);
                 } else if (beside) {
                   const float4 tk = lds_f4(s_token + 4u * (uint32_t)(hb + c));
                   add.x += ns.x * (fabsf(off0 + tk.x) - tk.x);
@@ -1347,6 +1406,15 @@ extend_mass_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_con
 #pragma unroll
                 for (int u = 0; u < 4; ++u)
                   if (hb + c + u < c_lo || hb + c + u >= c_hi) y[u] = -CUDART_INF_F;  // weight 0, whatever the logit is
+                if constexpr (MODS) {
+                  if (tree) {
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) {
+                      const int o = __shfl_sync(0xffffffffu, c_order, c + u), z = __shfl_sync(0xffffffffu, c_depth, c + u);
+                      if (!ext_below(o, mine_node) || (!sink && abs(z - at) >= x.window)) y[u] = -CUDART_INF_F;
+                    }
+                  }
+                }
               }
               sum2[0] = tc5::f2_add(sum2[0], tc5::f2_pack(fast_exp2(y[0]), fast_exp2(y[1])));
               sum2[1] = tc5::f2_add(sum2[1], tc5::f2_pack(fast_exp2(y[2]), fast_exp2(y[3])));
