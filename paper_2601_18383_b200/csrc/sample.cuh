@@ -10,22 +10,24 @@
 // of 2^-45, whose sums are the same in every order (vocabularies below 2^19).  A sum over 128256 of them is within 2^-28 of the
 // exact one in the worst case and about 2^-38 in the mean, while an fp32 sum would move a border in one row of ten.
 //
-// A cluster of CTAs takes a row, every warp a run of it.  What a row needs depends on its settings:
-//   * top_k or top_p: few tokens decide.  Every lane keeps the maximum of what it read.  The r-th largest of a warp's 32 maxima
-//     has r tokens of the warp at or above it, so with c the smallest of those values over the warps, 16 r tokens or more of the CTA
-//     lie at or above c: with 16 r >= top_k the CTA's share of the top_k is among them.  The tokens from c on are collected
-//     in a second reading (from L1 and L2), a list per warp and so in order; the first CTA merges the lists and decides alone.
-//     For top_p the second reading also adds up all weights, and 16 r = 128 is tried; if the run is longer, or a list
-//     overflows, or top_k is beyond 512, the row is
-//   * selected by the whole cluster: three or four rounds of a histogram of 256 bins (tokens and weights) narrow the border down
-//     to one value; a border inside equal values is a count of them.
-//   * nothing cut off, or by min_p alone: no selection.
-// Where the kept tokens are not in a list, the warps' sums of kept weights are exchanged and the one warp in whose run the
-// token lies looks for it.
+// A cluster of CTAs takes a row, every warp a run of it.  Every cut keeps a prefix of the ranking, so a row's cuts come down to
+// one border, a (value, index) pair.  The first reading takes every lane's maximum; what follows depends on the row's settings:
+//   * top_k up to 768: with c the q-th largest of a CTA's 512 lanes' maxima, q tokens or more of the CTA lie at or above it; with
+//     q = top_k / CTAs and the smallest c of the cluster's, top_k tokens or more do.  The tokens from there on, about 1.2 top_k, are
+//     collected in a second reading, a list per warp and so in order; the first CTA merges the lists, sorts them, and decides alone.
+//   * top_p alone, or a larger top_k: a histogram of the weights (or of the tokens) over 512 equal steps of the
+//     distance to the maximum, a second reading of the step in which the border lies, and the first CTA sorts that.  Steps of many
+//     equal logits that overflow the lists are narrowed down by the bits of the value instead, and a border inside equal
+//     values is a count of them.
+//   * nothing cut off, or by min_p alone: no border is needed.
+// Where the kept tokens are not in a list, the warps add up theirs, exchange the sums, and the CTA in which the token lies looks
+// for it: sixteenths of the one warp's run, then the run of one warp.
 //
 // Bound by the bytes of the logits for many rows (and by the exponentials where all weights are added up), by the
-// chain load - maxima - second reading - exchange - decision for few.
+// chain of readings and exchanges for few.
 #pragma once
+
+#include <type_traits>
 
 #include "common.cuh"
 #include "evict.cuh"  // the cluster barrier
@@ -35,9 +37,10 @@ namespace dynts {
 constexpr int kSmThreads = 512;
 constexpr int kSmWarps = kSmThreads / 32;
 constexpr int kSmWarpList = 128;     // tokens a warp can collect
-constexpr int kSmList = 4096;        // tokens the first CTA can merge
+constexpr int kSmList = 1024;        // tokens the first CTA can merge
 constexpr int kSmMaxCluster = 8;
-constexpr int kSmTryP = 8;           // lanes' maxima per warp above the cut that top_p is tried with
+constexpr int kSmListK = 768;        // top_k that lists are tried with
+constexpr int kSmBins = kSmThreads;
 constexpr int kSmMaxVocab = (1 << 19) - 1;  // sums of 2^45 for each token fit 64 bits
 
 struct SampleParams {
@@ -57,47 +60,52 @@ struct SampleParams {
 
 typedef unsigned long long u64;
 
-struct SmHist {
-  unsigned count[256];
-  u64 weight[256];
-};
-
-// The border of a selection: values with a key above `key` are kept, and `ties` of those with it (the lowest indices).
-struct SmCut {
-  unsigned key, ties;
-  u64 above, total;  // weights of the keys above it; with the ties
+// Kept are the keys above `key` and those equal to it up to `index`.
+struct SmBorder {
+  unsigned key;
+  int index;
+  __device__ __forceinline__ bool keeps(unsigned k, int i) const { return k > key || (k == key && i <= index); }
 };
 
 struct SmShared {
   double table[16];       // 2^(j / 16)
-  float lane_cut[kSmWarps], warp_max[kSmWarps];
-  unsigned warp_count[kSmWarps];
-  u64 warp_sum[kSmWarps];
-  unsigned warp_ties[kSmWarps];
-  unsigned scan_u[kSmWarps];
-  u64 scan_w[kSmWarps];
+  float warp_max[kSmWarps], warp_min[kSmWarps];
+  u64 scan[kSmWarps];
   // what the other CTAs of the cluster read
-  float max, cut;
-  u64 sum;                // of all weights, relative to this CTA's maximum
-  int overflow;
-  int verdict;            // of the first CTA: 1 the row is done
-  unsigned peer_kmin;
-  // selection
-  int bin;
-  u64 above;
-  unsigned above_count;
-  SmHist hist, merged;
+  float max, cut, low;    // largest logit; a value that enough tokens reach; smallest of the lanes' maxima
+  unsigned lanes;         // that hold any
+  unsigned warp_count[kSmWarps];
+  unsigned warp_ties[kSmWarps];
+  u64 warp_sum[kSmWarps];
+  u64 outside;
+  int verdict;            // of the first CTA: 1 decided, 0 a list overflowed
+  int tie_index;
+  SmBorder border;
+  u64 hist[kSmBins];
+  unsigned radix_count[256];
+  u64 radix_weight[256];
   uint2 list[kSmWarps][kSmWarpList];  // key, index
-};
-struct SmMerged {  // of the first CTA of a cluster
-  unsigned key[kSmList], index[kSmList];
+  // the rest is a CTA's own
+  unsigned offset[kSmMaxCluster * kSmWarps + 1];
+  int bin;
+  u64 above, below;
+  unsigned count;
+  u64 merged_weight[256];
+  unsigned merged_count[256];
+  u64 sort[kSmThreads];
+  unsigned key[kSmList];  // the merged lists
+  int index[kSmList];
   u64 weight[kSmList];
 };
 
-__device__ __forceinline__ void sm_cluster_sync() {  // (also of shared memory within the CTA)
-  __syncwarp();
-  cluster_arrive();
-  cluster_wait();
+__device__ __forceinline__ void sm_cluster_sync(int cluster) {  // (also of shared memory within the CTA)
+  if (cluster > 1) {
+    __syncwarp();
+    cluster_arrive();
+    cluster_wait();
+  } else {
+    __syncthreads();
+  }
 }
 
 template <typename T>
@@ -143,160 +151,128 @@ __device__ __forceinline__ u64 sm_weight(double y, const double* table) {
   return (u64)__double_as_longlong(e + 128.0) - (u64)__double_as_longlong(128.0);  // (a unit of the sum's mantissa is 2^-45)
 }
 
-template <typename X>
-struct SmRow {
-  static constexpr int E = 16 / (int)sizeof(X);  // elements of a 16-byte vector
-  const X* base;   // aligned down to 16 bytes
-  int skew;        // elements between there and the row
-  int vocab;
-  int v0, v1;      // this warp's vectors
-  // Vector v as floats; what lies outside the row is -inf, which weighs nothing.
-  __device__ __forceinline__ void load(int v, float (&x)[E]) const {
-    const int i = v * E - skew;
-    if (i >= 0 && i + E <= vocab) {
-      const uint4 w = *reinterpret_cast<const uint4*>(base + (size_t)v * E);
-      if constexpr (E == 4) {
-        x[0] = __uint_as_float(w.x), x[1] = __uint_as_float(w.y), x[2] = __uint_as_float(w.z), x[3] = __uint_as_float(w.w);
-      } else {
-        const unsigned y[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-        for (int e = 0; e < 4; ++e) x[2 * e] = __uint_as_float(y[e] << 16), x[2 * e + 1] = __uint_as_float(y[e] & 0xffff0000u);
-      }
-    } else {
-#pragma unroll
-      for (int e = 0; e < E; ++e) x[e] = i + e >= 0 && i + e < vocab ? to_float(base[(size_t)v * E + e]) : -INFINITY;
-    }
-  }
-};
-
 __device__ __forceinline__ float sm_max_nan(float a, float b) {  // a NaN stays
   float y;
   asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
   return y;
 }
-
-// The border by count (pz < 0: the first `want` are kept) or by weight (the shortest run that reaches pz).  each(f) calls
-// f(key, weight()) for the tokens of this CTA; with `cluster` > 1 the histograms of all its CTAs are added up.
-template <typename Each>
-__device__ SmCut sm_select(SmShared& sh, Each each, int cluster, unsigned kmin, unsigned kmax, unsigned want, double pz) {
-  const int tid = threadIdx.x, lane = tid & 31;
-  const bool by_weight = pz >= 0.0;
-  int shift = max(0, 24 - __clz(kmax - kmin));
-  unsigned lo = kmin, bins = 256, above_count = 0, here = 0;
-  u64 above = 0, here_w = 0;
-  while (true) {
-    for (int i = tid; i < 256; i += kSmThreads) sh.hist.count[i] = 0, sh.hist.weight[i] = 0;
-    __syncthreads();
-    each([&](unsigned key, auto weight) {
-      const unsigned at = (key - lo) >> shift;
-      if (key < lo || at >= bins) return;
-      atomicAdd(&sh.hist.count[at], 1u);
-      const u64 w = weight();
-      if (w) atomicAdd(&sh.hist.weight[at], w);
-    });
-    if (cluster > 1) {
-      sm_cluster_sync();
-      if (tid < 256) {
-        unsigned c = 0;
-        u64 w = 0;
-        for (int r = 0; r < cluster; ++r) c += sm_peer(&sh.hist.count[tid], r), w += sm_peer(&sh.hist.weight[tid], r);
-        sh.merged.count[tid] = c;
-        sh.merged.weight[tid] = w;
-      }
-      sm_cluster_sync();  // (the histograms have been read)
-    } else {
-      __syncthreads();
-    }
-    const SmHist& h = cluster > 1 ? sh.merged : sh.hist;
-    if (tid < 32) {  // from the top bin down, eight per lane
-      unsigned c = 0;
-      u64 w = 0;
-      const int top = 255 - 8 * lane;
-      for (int k = 0; k < 8; ++k) c += h.count[top - k], w += h.weight[top - k];
-      unsigned cs = c;
-      u64 ws = w;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const unsigned c2 = __shfl_up_sync(0xffffffffu, cs, o);
-        const u64 w2 = __shfl_up_sync(0xffffffffu, ws, o);
-        if (lane >= o) cs += c2, ws += w2;
-      }
-      u64 aw = above + ws - w;
-      unsigned ac = above_count + cs - c;
-      int bin = -1;
-      for (int k = 0; k < 8 && bin < 0; ++k) {
-        const unsigned hc = h.count[top - k];
-        const u64 hw = h.weight[top - k];
-        if (hc > 0 && (by_weight ? (double)(aw + hw) >= pz : ac + hc >= want)) bin = top - k;
-        else ac += hc, aw += hw;
-      }
-      const unsigned found = __ballot_sync(0xffffffffu, bin >= 0);
-      // (the sums reach their own total; were it missed by a rounding, everything is kept)
-      if (found == 0 ? lane == 31 : lane == __ffs(found) - 1) {
-        sh.bin = bin;
-        sh.above = aw;
-        sh.above_count = ac;
-      }
-    }
-    __syncthreads();
-    const int bin = sh.bin;
-    above = sh.above;
-    above_count = sh.above_count;
-    if (bin < 0) {
-      __syncthreads();
-      return SmCut{0u, 0u, above, above};  // every key is above 0
-    }
-    here = h.count[bin];
-    here_w = h.weight[bin];
-    lo += (unsigned)bin << shift;
-    __syncthreads();
-    if (shift == 0) break;
-    const int next = max(0, shift - 8);
-    bins = 1u << (shift - next);
-    shift = next;
-  }
-  // one value: all its tokens weigh the same
-  const u64 w = here_w / here;
-  unsigned ties = want - above_count;
-  if (by_weight) {
-    ties = here;
-    if (w > 0) {
-      const double need = (pz - (double)above) / (double)w;
-      ties = need <= 1.0 ? 1u : need >= (double)here ? here : (unsigned)ceil(need);
-    }
-  }
-  return SmCut{lo, ties, above, above + w * ties};
+__device__ __forceinline__ unsigned sm_max2_nan(unsigned a, unsigned b) {  // of two bf16 each
+  unsigned y;
+  asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(y) : "r"(a), "r"(b));
+  return y;
 }
 
-// The running sum of a value over the CTA's threads (exclusive); every thread gets the total.
+// A row in 16-byte vectors, from the boundary at or before its first element; what lies outside the row reads as -inf, which
+// weighs nothing.
+template <typename X>
+struct SmRow {
+  static constexpr int E = 16 / (int)sizeof(X);
+  const X* base;   // aligned down to 16 bytes
+  int skew;        // elements between there and the row
+  int vocab;
+  int v0, v1;      // this warp's vectors
+  __device__ __forceinline__ uint4 load(int v) const {
+    const int i = v * E - skew;
+    if (i >= 0 && i + E <= vocab) return *reinterpret_cast<const uint4*>(base + (size_t)v * E);
+    unsigned w[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      if constexpr (E == 4) {
+        w[q] = i + q >= 0 && i + q < vocab ? __float_as_uint(base[(size_t)v * E + q]) : 0xff800000u;
+      } else {
+        w[q] = 0xff80ff80u;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int e = 2 * q + h;
+          if (i + e >= 0 && i + e < vocab) w[q] = (w[q] & (h ? 0x0000ffffu : 0xffff0000u)) | ((unsigned)__bfloat16_as_ushort(base[(size_t)v * E + e]) << (16 * h));
+        }
+      }
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+  }
+  static __device__ __forceinline__ float at(const uint4& w, int e) {
+    const unsigned q[4] = {w.x, w.y, w.z, w.w};
+    if constexpr (E == 4) return __uint_as_float(q[e]);
+    else return __uint_as_float((e & 1) ? q[e >> 1] & 0xffff0000u : q[e >> 1] << 16);
+  }
+  // Running maxima, a word: of floats, or of two bf16 (a NaN stays).
+  static __device__ __forceinline__ unsigned start() { return E == 4 ? 0xff800000u : 0xff80ff80u; }
+  static __device__ __forceinline__ unsigned more(unsigned m, const uint4& w) {
+    if constexpr (E == 4)
+      return __float_as_uint(sm_max_nan(sm_max_nan(sm_max_nan(__uint_as_float(m), __uint_as_float(w.x)), sm_max_nan(__uint_as_float(w.y), __uint_as_float(w.z))), __uint_as_float(w.w)));
+    else return sm_max2_nan(sm_max2_nan(m, sm_max2_nan(w.x, w.y)), sm_max2_nan(w.z, w.w));
+  }
+  static __device__ __forceinline__ float largest(unsigned m) {
+    if constexpr (E == 4) return __uint_as_float(m);
+    else return sm_max_nan(__uint_as_float(m << 16), __uint_as_float(m & 0xffff0000u));
+  }
+};
+
 template <typename V>
-__device__ __forceinline__ V sm_scan(V x, V* warps, V& total) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  V s = x;
+__device__ __forceinline__ V sm_warp_scan(V x) {  // inclusive
+  const int lane = threadIdx.x & 31;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const V y = __shfl_up_sync(0xffffffffu, s, o);
-    if (lane >= o) s += y;
+    const V y = __shfl_up_sync(0xffffffffu, x, o);
+    if (lane >= o) x += y;
   }
+  return x;
+}
+// The sum of what lies before, over the CTA's threads; every thread gets the total.
+__device__ __forceinline__ u64 sm_scan(u64 x, u64* warps, u64& total) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const u64 s = sm_warp_scan(x);
   __syncthreads();
   if (lane == 31) warps[warp] = s;
   __syncthreads();
-  V before = 0;
+  u64 before = 0;
   total = 0;
+#pragma unroll
   for (int w = 0; w < kSmWarps; ++w) {
-    if (w < warp) before += warps[w];
-    total += warps[w];
+    const u64 y = warps[w];
+    if (w < warp) before += y;
+    total += y;
   }
   return before + s - x;
 }
 
+// Sorted, the largest first: N values per thread, value q of thread t is place t + 512 q.
+template <int N>
+__device__ __forceinline__ void sm_sort(u64 (&x)[N], u64* smem) {
+  const int tid = threadIdx.x;
+  for (int k = 2; k <= N * kSmThreads; k <<= 1)
+    for (int o = k >> 1; o > 0; o >>= 1) {
+      if (N == 2 && o == kSmThreads) {  // (k = 1024: the largest first throughout)
+        const u64 a = x[0], b = x[N - 1];
+        x[0] = max(a, b);
+        x[N - 1] = min(a, b);
+        continue;
+      }
+#pragma unroll
+      for (int q = 0; q < N; ++q) {
+        u64 y;
+        if (o >= 32) {
+          __syncthreads();
+          smem[tid] = x[q];
+          __syncthreads();
+          y = smem[tid ^ o];
+        } else {
+          y = __shfl_xor_sync(0xffffffffu, x[q], o);
+        }
+        const int place = tid + q * kSmThreads;
+        x[q] = ((place & k) == 0) == ((place & o) == 0) ? max(x[q], y) : min(x[q], y);
+      }
+    }
+}
+
 template <typename X>
-__global__ void __launch_bounds__(kSmThreads) sample_kernel(const __grid_constant__ SampleParams p) {
+__global__ void __launch_bounds__(kSmThreads, 2) sample_kernel(const __grid_constant__ SampleParams p) {
   constexpr int E = SmRow<X>::E;
   extern __shared__ __align__(16) uint8_t sm_raw[];
   SmShared& sh = *reinterpret_cast<SmShared*>(sm_raw);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int cluster = p.cluster, row = (int)blockIdx.x / cluster, rank = (int)blockIdx.x - row * cluster;
+  const int lists = cluster * kSmWarps;
 
   SmRow<X> r;
   {
@@ -320,358 +296,518 @@ __global__ void __launch_bounds__(kSmThreads) sample_kernel(const __grid_constan
   top_p = fmaxf(top_p, 0.f);
   const bool cut_p = top_p < 1.f;
   const double inv_t = 1.0 / (double)T;
-  const int tries = top_k > 0 ? (top_k + kSmWarps - 1) / kSmWarps : kSmTryP;  // lanes' maxima per warp
-  const bool listed = (top_k > 0 || cut_p) && tries <= 32;
+  const int share = (top_k + cluster - 1) / cluster;  // of top_k, for each CTA
+  const bool listed = top_k > 0 && top_k <= kSmListK && share <= kSmThreads / 2;
   if (tid < 16) sh.table[tid] = exp2((double)tid / 16.0);
-  if (tid == 0) sh.overflow = listed ? 0 : 1, sh.verdict = 0;
+  sh.hist[tid] = 0;
 
   // ---- every lane's maximum
-  float top = -INFINITY;
-#pragma unroll 4
-  for (int v = r.v0 + lane; v < r.v1; v += 32) {
-    float x[E];
-    r.load(v, x);
-#pragma unroll
-    for (int e = 0; e < E; ++e) top = sm_max_nan(top, x[e]);
-  }
+  float top;
   {
-    float s = top;  // sorted over the lanes, the largest first (a NaN makes the row's answer void below)
-    if (listed) {
+    unsigned m = SmRow<X>::start();
+    int v = r.v0 + lane;
+    for (; v + 96 < r.v1; v += 128) {
+      uint4 w[4];
 #pragma unroll
-      for (int k = 2; k <= 32; k <<= 1)
+      for (int q = 0; q < 4; ++q) w[q] = r.load(v + 32 * q);
 #pragma unroll
-        for (int o = k >> 1; o > 0; o >>= 1) {
-          const float y = __shfl_xor_sync(0xffffffffu, s, o);
-          s = ((lane & k) == 0) == ((lane & o) == 0) ? fmaxf(s, y) : fminf(s, y);
-        }
+      for (int q = 0; q < 4; ++q) m = SmRow<X>::more(m, w[q]);
     }
-    const float cut = __shfl_sync(0xffffffffu, s, min(tries, 32) - 1);
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) top = sm_max_nan(top, __shfl_xor_sync(0xffffffffu, top, o));
-    if (lane == 0) sh.lane_cut[warp] = cut, sh.warp_max[warp] = top;
+    for (; v < r.v1; v += 32) m = SmRow<X>::more(m, r.load(v));
+    top = SmRow<X>::largest(m);
   }
-  __syncthreads();
-  float cut = sh.lane_cut[0];
-  top = sh.warp_max[0];
+  const float lane_top = top;
+  float least = top > -INFINITY ? top : INFINITY;  // of the lanes that hold anything
 #pragma unroll
-  for (int w = 1; w < kSmWarps; ++w) cut = fminf(cut, sh.lane_cut[w]), top = sm_max_nan(top, sh.warp_max[w]);
-  if (tid == 0) sh.max = top, sh.cut = cut;
-
-  // ---- the tokens from the cut on, and all weights where top_p needs their sum (relative to this CTA's maximum)
+  for (int o = 16; o > 0; o >>= 1) {
+    top = sm_max_nan(top, __shfl_xor_sync(0xffffffffu, top, o));
+    least = fminf(least, __shfl_xor_sync(0xffffffffu, least, o));
+  }
+  if (lane == 0) sh.warp_max[warp] = top, sh.warp_min[warp] = least;
+  const unsigned lanes = (unsigned)__syncthreads_count(lane_top > -INFINITY);
+#pragma unroll
+  for (int w = 0; w < kSmWarps; ++w) top = sm_max_nan(top, sh.warp_max[w]), least = fminf(least, sh.warp_min[w]);
+  float cut = -INFINITY;
   if (listed) {
-    const bool sum_all = cut_p && top_k == 0;
-    unsigned count = 0;
-    u64 sum = 0;
-    const double top_d = (double)top;
-    for (int vb = r.v0; vb < r.v1; vb += 32) {
-      const int v = vb + lane;
-      float x[E];
-      float best = -INFINITY;
-      if (v < r.v1) {
-        r.load(v, x);
-#pragma unroll
-        for (int e = 0; e < E; ++e) best = fmaxf(best, x[e]);
-        if (sum_all) {
-#pragma unroll
-          for (int e = 0; e < E; ++e) sum += sm_weight(((double)x[e] - top_d) * inv_t, sh.table);
-        }
-      }
-      const bool any = v < r.v1 && best >= cut && best > -INFINITY;
-      if (!__any_sync(0xffffffffu, any)) continue;
-      unsigned hits = 0;  // a bit for each of the lane's elements
-      if (any) {
-#pragma unroll
-        for (int e = 0; e < E; ++e) hits |= (x[e] >= cut && x[e] > -INFINITY ? 1u : 0u) << e;
-      }
-      const unsigned n = __popc(hits);
-      unsigned at = n;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const unsigned y = __shfl_up_sync(0xffffffffu, at, o);
-        if (lane >= o) at += y;
-      }
-      const unsigned all = __shfl_sync(0xffffffffu, at, 31);
-      at += count - n;
-#pragma unroll
-      for (int e = 0; e < E; ++e)
-        if ((hits >> e) & 1u) {
-          if (at < kSmWarpList) sh.list[warp][at] = make_uint2(sm_key(x[e]), (unsigned)(v * E + e - r.skew));
-          ++at;
-        }
-      count += all;
+    // a value that `share` of the lanes' maxima reach, close to the largest such: by a histogram of 512 equal steps
+    const float steps = top > least ? (kSmBins - 1) / (top - least) : 0.f;
+    int b = kSmBins;
+    if (lane_top > -INFINITY) {
+      b = min(kSmBins - 1, (int)((top - lane_top) * steps));
+      atomicAdd(reinterpret_cast<unsigned*>(&sh.hist[b]), 1u);
     }
-    if (count > kSmWarpList) sh.overflow = 1;
+    u64 all;
+    if (tid == 0) sh.bin = kSmBins;
+    const u64 before = (__syncthreads(), sm_scan(sh.hist[tid], sh.scan, all)), here = sh.hist[tid];
+    if (before < (u64)share && before + here >= (u64)share) sh.bin = tid;
+    __syncthreads();
+    if (sh.bin < kSmBins) {  // (fewer lanes hold anything: all is collected)
+      float reach = b <= sh.bin ? lane_top : INFINITY;
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    if (lane == 0) sh.warp_count[warp] = min(count, (unsigned)kSmWarpList), sh.warp_sum[warp] = sum;
-    __syncthreads();
-    if (tid == 0) {
-      u64 s = 0;
-      for (int w = 0; w < kSmWarps; ++w) s += sh.warp_sum[w];
-      sh.sum = s;
+      for (int o = 16; o > 0; o >>= 1) reach = fminf(reach, __shfl_xor_sync(0xffffffffu, reach, o));
+      if (lane == 0) sh.warp_min[warp] = reach;
+      __syncthreads();
+      cut = INFINITY;
+#pragma unroll
+      for (int w = 0; w < kSmWarps; ++w) cut = fminf(cut, sh.warp_min[w]);
     }
+    sh.hist[tid] = 0;
   }
-  if (cluster > 1) {
-    sm_cluster_sync();
-  } else {
-    __syncthreads();
-  }
-  float M = -INFINITY;
-  float cut_all = -INFINITY;
-  bool overflow = false;
-  for (int k = 0; k < cluster; ++k) {
-    M = sm_max_nan(M, sm_peer(&sh.max, k));
-    cut_all = fmaxf(cut_all, sm_peer(&sh.cut, k));
-    overflow = overflow || sm_peer(&sh.overflow, k) != 0;
+  if (tid == 0) sh.max = top, sh.cut = cut, sh.low = least, sh.lanes = lanes;
+  sm_cluster_sync(cluster);
+  float M, low_all;
+  unsigned lanes_all = 0;
+  {
+    float a = -INFINITY, b = INFINITY, c = INFINITY;
+    if (lane < cluster) a = sm_peer(&sh.max, lane), b = sm_peer(&sh.cut, lane), c = sm_peer(&sh.low, lane), lanes_all = sm_peer(&sh.lanes, lane);
+    lanes_all = __reduce_add_sync(0xffffffffu, lanes_all);
+#pragma unroll
+    for (int o = kSmMaxCluster / 2; o > 0; o >>= 1) {
+      a = sm_max_nan(a, __shfl_xor_sync(0xffffffffu, a, o));
+      b = fminf(b, __shfl_xor_sync(0xffffffffu, b, o));
+      c = fminf(c, __shfl_xor_sync(0xffffffffu, c, o));
+    }
+    M = __shfl_sync(0xffffffffu, a, 0);
+    cut = __shfl_sync(0xffffffffu, b, 0);
+    low_all = __shfl_sync(0xffffffffu, c, 0);
   }
   const double Md = (double)M;
-  const bool no_answer = !(M > -INFINITY && M < INFINITY);  // NaN or +inf somewhere, or nothing but -inf
-  const double x_min = min_p > 0.f ? Md + (double)T * log((double)min_p) : -INFINITY;  // (min_p > 1: nothing but the maximum is kept)
+  // what min_p keeps: x >= least_x (min_p > 1 counts as 1)
+  const double least_x = min_p > 0.f ? fmin(Md + (double)T * log((double)min_p), Md) : -INFINITY;
   auto weight_of = [&](float x) { return sm_weight(((double)x - Md) * inv_t, sh.table); };
   auto answer = [&](int token, float x, u64 total) {
     p.tokens[row] = token;
     if (p.logprobs) p.logprobs[row] = (float)(((double)x - Md) * inv_t - log((double)total * 2.842170943040401e-14));  // 2^-45
   };
-  if (no_answer) {
+  // The tokens for which wanted(x, key, index) holds, of vectors whose largest element is at least `reach`: a list per warp.
+  auto collect = [&](float reach, auto wanted) {
+    unsigned count = 0;
+#pragma unroll 2
+    for (int vb = r.v0; vb < r.v1; vb += 32) {
+      const int v = vb + lane;
+      uint4 w = make_uint4(0u, 0u, 0u, 0u);
+      bool any = false;
+      if (v < r.v1) {
+        w = r.load(v);
+        any = SmRow<X>::largest(SmRow<X>::more(SmRow<X>::start(), w)) >= reach;
+      }
+      if (!__any_sync(0xffffffffu, any)) continue;
+      unsigned hits = 0;  // a bit for each of the lane's elements
+      if (any) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          const float x = SmRow<X>::at(w, e);
+          hits |= (x > -INFINITY && wanted(x, sm_key(x), v * E + e - r.skew) ? 1u : 0u) << e;
+        }
+      }
+      const unsigned n = __popc(hits), upto = sm_warp_scan(n);
+      unsigned at = count + upto - n;
+#pragma unroll
+      for (int e = 0; e < E; ++e)
+        if ((hits >> e) & 1u) {
+          if (at < kSmWarpList) sh.list[warp][at] = make_uint2(sm_key(SmRow<X>::at(w, e)), (unsigned)(v * E + e - r.skew));
+          ++at;
+        }
+      count += __shfl_sync(0xffffffffu, upto, 31);
+    }
+    if (lane == 0) sh.warp_count[warp] = count;
+  };
+  // By the first CTA, behind a barrier: the lists as one, in order, with their weights.  How many; more than kSmList: overflowed.
+  auto merge = [&]() -> unsigned {
+    __syncthreads();
+    if (warp == 0) {
+      unsigned base = 0;
+      bool over = false;
+      for (int i0 = 0; i0 < lists; i0 += 32) {
+        const int i = i0 + lane;
+        const unsigned c = i < lists ? sm_peer(&sh.warp_count[i % kSmWarps], i / kSmWarps) : 0u;
+        over = over || c > kSmWarpList;
+        const unsigned upto = sm_warp_scan(min(c, (unsigned)kSmWarpList));
+        if (i < lists) sh.offset[i] = base + upto - min(c, (unsigned)kSmWarpList);
+        base += __shfl_sync(0xffffffffu, upto, 31);
+      }
+      over = __any_sync(0xffffffffu, over);
+      if (lane == 0) sh.offset[lists] = base, sh.count = over ? kSmList + 1 : base;
+    }
+    __syncthreads();
+    const unsigned n = sh.count;
+    if (n <= kSmList)
+      for (unsigned i = tid; i < n; i += kSmThreads) {
+        int lo = 0, hi = lists;  // the last list that begins at or before i (of equal ones the last, which holds it)
+        while (hi - lo > 1) {
+          const int mid = (lo + hi) >> 1;
+          if (sh.offset[mid] <= i) lo = mid;
+          else hi = mid;
+        }
+        const uint2 y = sm_peer(&sh.list[lo % kSmWarps][i - sh.offset[lo]], lo / kSmWarps);
+        sh.key[i] = y.x;
+        sh.index[i] = (int)y.y;
+        sh.weight[i] = weight_of(sm_value(y.x));
+      }
+    __syncthreads();
+    return n;
+  };
+  // By the first CTA: the border among the merged tokens: the first `want` are kept (0: all of them), of those the shortest run whose
+  // weights reach part of theirs (part < 0: all), or reach `goal` with `above` before them (goal >= 0).
+  auto rank_list = [&](unsigned n, unsigned want, double part, u64 above, double goal) -> SmBorder {
+    auto with = [&](auto per) {
+      constexpr int N = decltype(per)::value;
+      u64 x[N], w[N], run[N], before = 0, all;
+#pragma unroll
+      for (int q = 0; q < N; ++q) {
+        const unsigned i = tid + q * kSmThreads;
+        x[q] = i < n ? ((u64)sh.key[i] << 32) | (0xffffffffu - i) : 0ull;
+      }
+      sm_sort(x, sh.sort);
+#pragma unroll
+      for (int q = 0; q < N; ++q) {
+        const unsigned place = tid + q * kSmThreads;
+        const bool counts = place < n && (want == 0 || place < want);
+        w[q] = counts ? sh.weight[0xffffffffu - (unsigned)x[q]] : 0ull;
+        run[q] = before + sm_scan(w[q], sh.scan, all);
+        before += all;
+      }
+      const bool whole = goal < 0.0 && part < 0.0;
+      const double reach = goal >= 0.0 ? goal : part * (double)before;
+      if (tid == 0) sh.count = 0;
+      __syncthreads();
+#pragma unroll
+      for (int q = 0; q < N; ++q) {  // the last kept token is the border
+        const unsigned place = tid + q * kSmThreads;
+        const bool counts = place < n && (want == 0 || place < want);
+        const bool kept = counts && (whole || place + above == 0 || (double)(above + run[q]) < reach);
+        if (kept) atomicMax(&sh.count, place + 1);
+      }
+      __syncthreads();
+      const unsigned last = sh.count - 1;
+#pragma unroll
+      for (int q = 0; q < N; ++q)
+        if (tid + q * kSmThreads == last) {
+          const unsigned i = 0xffffffffu - (unsigned)x[q];
+          sh.border = SmBorder{sh.key[i], sh.index[i]};
+        }
+      __syncthreads();
+      return sh.border;
+    };
+    return n <= kSmThreads ? with(std::integral_constant<int, 1>{}) : with(std::integral_constant<int, 2>{});
+  };
+  bool done = false;
+  SmBorder border{0u, -1};  // (every key is above 0)
+  if (!(M > -INFINITY && M < INFINITY)) {  // NaN or +inf somewhere, or nothing but -inf
     if (rank == 0 && tid == 0) {
       p.tokens[row] = -1;
       if (p.logprobs) p.logprobs[row] = NAN;
     }
-  } else {
-    const double low = fmin(x_min, Md);
-    bool done = false;
-    if (!overflow) {
-      // ---- the first CTA merges the lists and decides
-      if (rank == 0) {
-        SmMerged& m = *reinterpret_cast<SmMerged*>(sm_raw + ((sizeof(SmShared) + 15) & ~(size_t)15));
-        unsigned base = 0;
-        unsigned kmax = sm_key(M);
-        double total = 0.0;
-        for (int k = 0; k < cluster; ++k) {
-          unsigned before = base;
-          for (int w = 0; w < kSmWarps; ++w) {
-            const unsigned c = sm_peer(&sh.warp_count[w], k);
-            if (w < warp) before += c;
-            base += c;
-          }
-          const unsigned c = sm_peer(&sh.warp_count[warp], k);
-          for (unsigned i = lane; i < c; i += 32) {
-            const uint2 y = sm_peer(&sh.list[warp][i], k);
-            if (before + i < kSmList) {
-              m.key[before + i] = y.x;
-              m.index[before + i] = y.y;
-              m.weight[before + i] = weight_of(sm_value(y.x));
-            }
-          }
-          if (cut_p && top_k == 0) total += (double)sm_peer(&sh.sum, k) * exp(((double)sm_peer(&sh.max, k) - Md) * inv_t);
+    done = true;
+  }
+  if (!done && listed) {
+    collect(cut, [&](float x, unsigned, int) { return x >= cut; });
+    sm_cluster_sync(cluster);
+    if (rank == 0) {
+      const unsigned n = merge();
+      if (n <= kSmList) {
+        const SmBorder b = rank_list(n, (unsigned)top_k, cut_p ? (double)top_p : -1.0, 0, -1.0);
+        // the kept tokens' running sums, in the order of the vocabulary: two neighbours per thread
+        u64 w[2], all;
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+          const unsigned i = 2 * tid + q;
+          w[q] = i < n && b.keeps(sh.key[i], sh.index[i]) && (double)sm_value(sh.key[i]) >= least_x ? sh.weight[i] : 0ull;
         }
-        const unsigned n = base, kcut = sm_key(cut_all);
-        __syncthreads();
-        bool fits = n <= kSmList;
-        if (fits) {
-          auto each = [&](auto f) {
-            for (unsigned i = tid; i < n; i += kSmThreads) {
-              const unsigned key = m.key[i];
-              f(key, [&]() { return m.weight[i]; });
-            }
-          };
-          SmCut c{0u, 0u, 0, 0};
-          if (top_k > 0) {
-            c = sm_select(sh, each, 1, kcut, kmax, (unsigned)top_k, -1.0);
-            total = (double)c.total;
-          }
-          if (cut_p) {
-            // (of the tokens below the cut some are missing; of those from top_k on nothing counts)
-            const SmCut q = sm_select(sh, each, 1, top_k > 0 ? max(c.key, kcut) : kcut, kmax, 0u, (double)top_p * total);
-            if (q.key == 0u) {
-              if (top_k == 0) fits = false;  // the run is longer than the list
-            } else {
-              const unsigned ties = top_k > 0 && q.key == c.key ? min(q.ties, c.ties) : q.ties;
-              c = q;
-              c.ties = ties;
-            }
-          }
-          if (fits) {
-            // the kept tokens' running sums, in the order of the vocabulary: a run of the list per thread
-            const unsigned per = (n + kSmThreads - 1) / kSmThreads, i0 = min(n, tid * per), i1 = min(n, i0 + per);
-            unsigned ties = 0, all_ties;
-            for (unsigned i = i0; i < i1; ++i) ties += m.key[i] == c.key;
-            const unsigned ties0 = sm_scan(ties, sh.scan_u, all_ties);
-            auto kept = [&](unsigned i, unsigned& seen) {
-              const unsigned key = m.key[i];
-              const bool tie = key == c.key;
-              const bool yes = (key > c.key || (tie && seen < c.ties)) && (double)sm_value(key) >= low;
-              seen += tie;
-              return yes ? m.weight[i] : 0ull;
-            };
-            u64 mine = 0, all;
-            unsigned seen = ties0;
-            for (unsigned i = i0; i < i1; ++i) mine += kept(i, seen);
-            u64 run = sm_scan(mine, sh.scan_w, all);
-            const u64 target = min((u64)__double2ull_rd((double)u * (double)all), all - 1);
-            if (run <= target && run + mine > target) {
-              seen = ties0;
-              for (unsigned i = i0; i < i1; ++i) {
-                run += kept(i, seen);
-                if (run > target) {
-                  answer((int)m.index[i], sm_value(m.key[i]), all);
-                  break;
-                }
-              }
-            }
-          }
+        const u64 run = sm_scan(w[0] + w[1], sh.scan, all);
+        const u64 target = min((u64)__double2ull_rd((double)u * (double)all), all - 1);
+        if (run <= target && run + w[0] + w[1] > target) {
+          const unsigned i = 2 * tid + (run + w[0] > target ? 0 : 1);
+          answer(sh.index[i], sm_value(sh.key[i]), all);
         }
-        if (tid == 0) sh.verdict = fits ? 1 : 0;
-        __syncthreads();
       }
-      if (cluster > 1) {
-        sm_cluster_sync();
-        done = sm_peer(&sh.verdict, 0) != 0;
-      } else {
-        done = sh.verdict != 0;
-      }
+      if (tid == 0) sh.verdict = n <= kSmList ? 1 : 0;
     }
-    if (!done) {
-      // ---- the whole row
-      SmCut c{0u, 0u, 0, 0};
-      auto each = [&](auto f) {
+    sm_cluster_sync(cluster);
+    done = sm_peer(&sh.verdict, 0) != 0;
+  }
+  if (!done) {
+    // ---- the border by a histogram: first of the tokens (top_k), then of the weights of those kept (top_p)
+    for (int which = 0; which < 2; ++which) {
+      const bool by_weight = which == 1;
+      if (by_weight ? !cut_p : top_k == 0) continue;
+      // Distances to the maximum up to `span` in 512 steps.  Weights: what lies beyond ln(V / (1 - p)) in units of T adds up to less than
+      // 1 - p of the largest, so no border lies there.  Tokens: the lanes' maxima reach down to low_all; beyond their number, the
+      // smallest logit does.
+      float span;
+      if (by_weight) {
+        span = T * fminf(32.f, logf((float)p.vocab / (1.f - top_p)) + 0.01f);
+      } else if ((unsigned)top_k <= lanes_all) {
+        span = M - low_all;
+      } else {
+        float least_all = INFINITY;
         for (int v = r.v0 + lane; v < r.v1; v += 32) {
-          float x[E];
-          r.load(v, x);
-#pragma unroll
-          for (int e = 0; e < E; ++e)
-            if (x[e] > -INFINITY) f(sm_key(x[e]), [&]() { return weight_of(x[e]); });
-        }
-      };
-      const unsigned kmax = sm_key(M), kmin = 0x00800000u;  // (finite values)
-      auto kept_sums = [&](u64& sum, unsigned& ties) {  // of this warp: weights above the border, tokens on it
-        sum = 0;
-        ties = 0;
-        for (int v = r.v0 + lane; v < r.v1; v += 32) {
-          float x[E];
-          r.load(v, x);
+          const uint4 w = r.load(v);
 #pragma unroll
           for (int e = 0; e < E; ++e) {
-            const unsigned key = sm_key(x[e]);
-            if (key > c.key && (double)x[e] >= low) sum += weight_of(x[e]);
-            ties += key == c.key ? 1u : 0u;
+            const float x = SmRow<X>::at(w, e);
+            if (x > -INFINITY) least_all = fminf(least_all, x);
           }
         }
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o), ties += __shfl_xor_sync(0xffffffffu, ties, o);
-      };
-      auto exchange = [&]() {
-        if (cluster > 1) {
-          sm_cluster_sync();
-        } else {
-          __syncthreads();
-        }
-      };
-      double total = 0.0;
-      if (top_k > 0) {
-        c = sm_select(sh, each, cluster, kmin, kmax, (unsigned)top_k, -1.0);
-        if (c.key == 0u) c = SmCut{0u, 0u, 0, 0};  // (fewer finite tokens than top_k)
-        total = (double)c.total;
+        for (int o = 16; o > 0; o >>= 1) least_all = fminf(least_all, __shfl_xor_sync(0xffffffffu, least_all, o));
+        __syncthreads();
+        if (lane == 0) sh.warp_min[warp] = least_all;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < kSmWarps; ++w) least_all = fminf(least_all, sh.warp_min[w]);
+        if (tid == 0) sh.low = least_all;
+        sm_cluster_sync(cluster);
+        for (int k = 0; k < cluster; ++k) least_all = fminf(least_all, sm_peer(&sh.low, k));
+        span = M - least_all;
       }
-      if (cut_p) {
-        if (top_k == 0) {
+      const float steps = span > 0.f ? fminf((kSmBins - 1) / span, 1e30f) : 0.f;
+      const float reach_all = M - span * 1.001f;
+      auto bin_of = [&](float x) {  // (never grows with x: every rounding is monotone)
+        const float y = (M - x) * steps;
+        return y < (float)kSmBins ? (int)y : kSmBins;
+      };
+      u64 outside = 0;
+#pragma unroll 2
+      for (int v = r.v0 + lane; v < r.v1; v += 32) {
+        const uint4 w = r.load(v);
+        if (!by_weight && !(SmRow<X>::largest(SmRow<X>::more(SmRow<X>::start(), w)) >= reach_all)) continue;
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          const float x = SmRow<X>::at(w, e);
+          if (!(x > -INFINITY) || !border.keeps(sm_key(x), v * E + e - r.skew)) continue;
+          const u64 amount = by_weight ? weight_of(x) : 1ull;
+          const int b = bin_of(x);
+          if (b < kSmBins) atomicAdd(&sh.hist[b], amount);
+          else outside += amount;
+        }
+      }
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) outside += __shfl_xor_sync(0xffffffffu, outside, o);
+      __syncthreads();
+      if (lane == 0) sh.scan[warp] = outside;
+      __syncthreads();
+      if (tid == 0) {
+        u64 s = 0;
+        for (int w = 0; w < kSmWarps; ++w) s += sh.scan[w];
+        sh.outside = s;
+        sh.bin = -1;
+      }
+      sm_cluster_sync(cluster);
+      u64 here = 0, beyond = 0, all;
+#pragma unroll
+      for (int k = 0; k < kSmMaxCluster; ++k)
+        if (k < cluster) here += sm_peer(&sh.hist[tid], k), beyond += sm_peer(&sh.outside, k);
+      const u64 before = sm_scan(here, sh.scan, all);
+      const double goal = by_weight ? (double)top_p * (double)(all + beyond) : (double)top_k;
+      if (here > 0 && (double)(before + here) >= goal && (before == 0 || (double)before < goal)) {
+        sh.bin = tid;
+        sh.above = before;
+      }
+      __syncthreads();
+      const int bin = sh.bin;
+      const u64 above = sh.above;
+      sm_cluster_sync(cluster);  // (the histograms have been read)
+      sh.hist[tid] = 0;
+      if (bin < 0) continue;     // fewer tokens than top_k; or a sum missed by a rounding: all are kept
+      const SmBorder outer = border;
+      auto in_bin = [&](float x, unsigned key, int i) { return bin_of(x) == bin && outer.keeps(key, i); };
+      // (a vector without an element of this bin or a nearer one is passed over: what the bin holds is at least this large)
+      const float reach = steps > 0.f ? M - (float)(bin + 2) / steps : -INFINITY;
+      collect(reach, in_bin);
+      sm_cluster_sync(cluster);
+      if (rank == 0) {
+        const unsigned n = merge();
+        if (n <= kSmList) rank_list(n, by_weight ? 0u : (unsigned)((u64)top_k - above), -1.0, above, by_weight ? goal : -1.0);
+        if (tid == 0) sh.verdict = n <= kSmList ? 1 : 0;
+      }
+      sm_cluster_sync(cluster);
+      if (sm_peer(&sh.verdict, 0) != 0) {
+        border.key = sm_peer(&sh.border.key, 0);
+        border.index = sm_peer(&sh.border.index, 0);
+        sm_cluster_sync(cluster);
+        continue;
+      }
+      // ---- too many tokens of one step: by the bits of their keys, eight at a time
+      unsigned lo = 0, at = 0;
+      u64 over = above, one = 0;  // what lies above; a token's weight
+      unsigned there = 0;         // tokens of the value
+      for (int shift = 24; shift >= 0; shift -= 8) {
+        if (tid < 256) sh.radix_count[tid] = 0, sh.radix_weight[tid] = 0;
+        __syncthreads();
+        for (int v = r.v0 + lane; v < r.v1; v += 32) {
+          const uint4 w = r.load(v);
+          if (!(SmRow<X>::largest(SmRow<X>::more(SmRow<X>::start(), w)) >= reach)) continue;
+#pragma unroll
+          for (int e = 0; e < E; ++e) {
+            const float x = SmRow<X>::at(w, e);
+            const unsigned key = sm_key(x);
+            if (!(x > -INFINITY) || !in_bin(x, key, v * E + e - r.skew) || (shift < 24 && (key ^ lo) >> (shift + 8) != 0)) continue;
+            atomicAdd(&sh.radix_count[(key >> shift) & 255u], 1u);
+            if (by_weight) atomicAdd(&sh.radix_weight[(key >> shift) & 255u], weight_of(x));
+          }
+        }
+        sm_cluster_sync(cluster);
+        if (tid < 256) {
+          unsigned c = 0;
           u64 s = 0;
-          each([&](unsigned, auto weight) { s += weight(); });
-#pragma unroll
-          for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-          if (lane == 0) sh.warp_sum[warp] = s;
-          exchange();
-          u64 z = 0;
-          for (int k = 0; k < cluster; ++k)
-            for (int w = 0; w < kSmWarps; ++w) z += sm_peer(&sh.warp_sum[w], k);
-          total = (double)z;
-          exchange();
+          for (int k = 0; k < cluster; ++k) c += sm_peer(&sh.radix_count[255 - tid], k), s += sm_peer(&sh.radix_weight[255 - tid], k);
+          sh.merged_count[tid] = c;  // (from the largest digit down)
+          sh.merged_weight[tid] = by_weight ? s : (u64)c;
         }
-        const SmCut q = sm_select(sh, each, cluster, max(kmin, c.key), kmax, 0u, (double)top_p * total);
-        if (q.key != 0u) {
-          const unsigned ties = top_k > 0 && q.key == c.key ? min(q.ties, c.ties) : q.ties;
-          c = q;
-          c.ties = ties;
+        if (tid == 0) sh.bin = -1;
+        sm_cluster_sync(cluster);
+        u64 sum;
+        const u64 mine = tid < 256 ? sh.merged_weight[tid] : 0, first = sm_scan(mine, sh.scan, sum) + over;
+        if (tid < 256 && sh.merged_count[tid] > 0 && (double)(first + mine) >= goal && (first == 0 || (double)first < goal)) {
+          sh.bin = tid;
+          sh.above = first;
         }
+        __syncthreads();
+        at = (unsigned)max(sh.bin, 0);  // (the step's sum reaches the goal, so a digit does)
+        over = sh.above;
+        there = sh.merged_count[at];
+        one = there > 0 ? sh.merged_weight[at] / there : 0;
+        lo |= (255u - at) << shift;
+        __syncthreads();
       }
-      u64 sum;
-      unsigned ties;
-      kept_sums(sum, ties);
-      if (lane == 0) sh.warp_sum[warp] = sum, sh.warp_ties[warp] = ties;
-      exchange();
-      // the warps' sums in order; a tie counts while fewer than c.ties lie before it
-      const float tie_x = sm_value(c.key);
-      const u64 tie_w = c.ties > 0 && (double)tie_x >= low ? weight_of(tie_x) : 0;
-      u64 all = 0, before = 0;
-      unsigned seen = 0, seen_mine = 0;
-      for (int k = 0; k < cluster; ++k)
-        for (int w = 0; w < kSmWarps; ++w) {
-          if (k == rank && w == warp) before = all, seen_mine = seen;
-          const unsigned t = sm_peer(&sh.warp_ties[w], k), take = seen < c.ties ? min(t, c.ties - seen) : 0u;
-          all += sm_peer(&sh.warp_sum[w], k) + tie_w * take;
-          seen += t;
-        }
-      const u64 mine = sum + tie_w * (seen_mine < c.ties ? min(ties, c.ties - seen_mine) : 0u);
-      const u64 target = min((u64)__double2ull_rd((double)u * (double)all), all - 1);
-      if (before <= target && before + mine > target) {
-        // the token lies in this warp's run
-        u64 run = before;
-        bool found = false;
-        for (int vb = r.v0; vb < r.v1 && !found; vb += 32) {
+      // one value: all its tokens weigh the same, and as many of them as it takes are kept, the lowest indices
+      unsigned ties = there;
+      if (one > 0) {
+        const double need = ceil((goal - (double)over) / (double)one);
+        ties = need <= 1.0 ? 1u : need >= (double)there ? there : (unsigned)need;
+      }
+      unsigned mine = 0;
+      auto is_tie = [&](float x, int i) { return sm_key(x) == lo && x > -INFINITY && in_bin(x, lo, i); };
+      const float lo_x = sm_value(lo);
+      for (int v = r.v0 + lane; v < r.v1; v += 32) {
+        const uint4 w = r.load(v);
+        if (!(SmRow<X>::largest(SmRow<X>::more(SmRow<X>::start(), w)) >= lo_x)) continue;
+#pragma unroll
+        for (int e = 0; e < E; ++e) mine += is_tie(SmRow<X>::at(w, e), v * E + e - r.skew) ? 1u : 0u;
+      }
+      mine = __reduce_add_sync(0xffffffffu, mine);
+      if (lane == 0) sh.warp_ties[warp] = mine;
+      if (tid == 0) sh.tie_index = -1;
+      sm_cluster_sync(cluster);
+      {
+        unsigned seen = 0;  // ties before this warp's
+        for (int i = lane; i < rank * kSmWarps + warp; i += 32) seen += sm_peer(&sh.warp_ties[i % kSmWarps], i / kSmWarps);
+        seen = __reduce_add_sync(0xffffffffu, seen);
+        if (seen < ties && seen + mine >= ties)
+          for (int vb = r.v0; vb < r.v1; vb += 32) {  // the last kept one is among them
+            const int v = vb + lane;
+            unsigned hits = 0;
+            if (v < r.v1) {
+              const uint4 w = r.load(v);
+#pragma unroll
+              for (int e = 0; e < E; ++e) hits |= (is_tie(SmRow<X>::at(w, e), v * E + e - r.skew) ? 1u : 0u) << e;
+            }
+            const unsigned n = __popc(hits), upto = sm_warp_scan(n);
+            unsigned place = seen + upto - n;
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+              if ((hits >> e) & 1u) {
+                if (++place == ties) sh.tie_index = v * E + e - r.skew;
+              }
+            seen += __shfl_sync(0xffffffffu, upto, 31);
+            if (seen >= ties) break;
+          }
+      }
+      sm_cluster_sync(cluster);
+      border.key = lo;
+      border.index = -1;
+      for (int k = 0; k < cluster; ++k) border.index = max(border.index, sm_peer(&sh.tie_index, k));
+      sm_cluster_sync(cluster);
+    }
+    // ---- the kept weights, warp by warp; the token lies where their running sum passes the target
+    auto kept_weight = [&](float x, int i) {
+      return x > -INFINITY && (double)x >= least_x && border.keeps(sm_key(x), i) ? weight_of(x) : 0ull;
+    };
+    const float reach = fmaxf(border.key ? sm_value(border.key) : -INFINITY, least_x > -1e38 ? (float)least_x - fabsf((float)least_x) * 1e-6f : -INFINITY);
+    auto sum_of = [&](int v0, int v1) {
+      u64 s = 0;
+#pragma unroll 2
+      for (int v = v0 + lane; v < v1; v += 32) {
+        const uint4 w = r.load(v);
+        if (!(SmRow<X>::largest(SmRow<X>::more(SmRow<X>::start(), w)) >= reach)) continue;
+#pragma unroll
+        for (int e = 0; e < E; ++e) s += kept_weight(SmRow<X>::at(w, e), v * E + e - r.skew);
+      }
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+      return s;
+    };
+    const u64 mine = sum_of(r.v0, r.v1);
+    if (lane == 0) sh.warp_sum[warp] = mine;
+    sm_cluster_sync(cluster);
+    u64 all = 0, start = 0;
+    int owner = 0;
+    u64 target;
+    {
+      u64 s[kSmMaxCluster * kSmWarps / 32], sum = 0;  // neighbouring warps' sums per lane
+      constexpr int N = kSmMaxCluster * kSmWarps / 32;
+#pragma unroll
+      for (int q = 0; q < N; ++q) {
+        const int i = lane * N + q;
+        s[q] = i < lists ? sm_peer(&sh.warp_sum[i % kSmWarps], i / kSmWarps) : 0ull;
+        sum += s[q];
+      }
+      const u64 upto = sm_warp_scan(sum);
+      all = __shfl_sync(0xffffffffu, upto, 31);
+      target = min((u64)__double2ull_rd((double)u * (double)all), all - 1);
+      u64 run = upto - sum;
+      int found = -1;
+#pragma unroll
+      for (int q = 0; q < N; ++q) {
+        if (found < 0 && run + s[q] > target) found = lane * N + q;
+        if (found < 0) run += s[q];
+      }
+      const int who = __ffs(__ballot_sync(0xffffffffu, found >= 0)) - 1;
+      owner = __shfl_sync(0xffffffffu, found, who);
+      start = __shfl_sync(0xffffffffu, run, who);
+    }
+    if (owner / kSmWarps == rank) {
+      // the owner's vectors in sixteenths, a warp each
+      if (tid == (owner % kSmWarps) * 32) sh.offset[0] = (unsigned)r.v0, sh.offset[1] = (unsigned)r.v1;
+      __syncthreads();
+      const int o0 = (int)sh.offset[0], o1 = (int)sh.offset[1], per = (o1 - o0 + kSmWarps - 1) / kSmWarps;
+      const int s0 = min(o1, o0 + warp * per), s1 = min(o1, s0 + per);
+      const u64 part = sum_of(s0, s1);
+      if (lane == 0) sh.scan[warp] = part;
+      __syncthreads();
+      u64 run = start;
+      for (int w = 0; w < warp; ++w) run += sh.scan[w];
+      if (run <= target && run + part > target)
+        for (int vb = s0; vb < s1; vb += 32) {
           const int v = vb + lane;
-          float x[E];
-          unsigned keys[E], t = 0;
-          if (v < r.v1) {
-            r.load(v, x);
-          } else {
-#pragma unroll
-            for (int e = 0; e < E; ++e) x[e] = -INFINITY;
-          }
-#pragma unroll
-          for (int e = 0; e < E; ++e) keys[e] = sm_key(x[e]), t += keys[e] == c.key ? 1u : 0u;
-          unsigned ts = t;
-#pragma unroll
-          for (int o = 1; o < 32; o <<= 1) {
-            const unsigned y = __shfl_up_sync(0xffffffffu, ts, o);
-            if (lane >= o) ts += y;
-          }
-          unsigned at = seen_mine + ts - t;
-          u64 w[E], s = 0;
+          uint4 w = make_uint4(0u, 0u, 0u, 0u);
+          u64 y[E], s = 0;
+          if (v < s1) w = r.load(v);
 #pragma unroll
           for (int e = 0; e < E; ++e) {
-            const bool tie = keys[e] == c.key;
-            w[e] = keys[e] > c.key && (double)x[e] >= low ? weight_of(x[e]) : tie && at < c.ties ? tie_w : 0ull;
-            at += tie ? 1u : 0u;
-            s += w[e];
+            y[e] = v < s1 ? kept_weight(SmRow<X>::at(w, e), v * E + e - r.skew) : 0ull;
+            s += y[e];
           }
-          u64 ss = s;
-#pragma unroll
-          for (int o = 1; o < 32; o <<= 1) {
-            const u64 y = __shfl_up_sync(0xffffffffu, ss, o);
-            if (lane >= o) ss += y;
-          }
-          u64 mine_run = run + ss - s;
-          const bool here = mine_run <= target && run + ss > target;
+          const u64 upto = sm_warp_scan(s);
+          u64 at = run + upto - s;
+          const bool here = at <= target && run + upto > target;
           if (here) {
 #pragma unroll
             for (int e = 0; e < E; ++e) {
-              const bool was = mine_run > target;
-              mine_run += w[e];
-              if (!was && mine_run > target) answer(v * E + e - r.skew, x[e], all);
+              const bool was = at > target;
+              at += y[e];
+              if (!was && at > target) answer(v * E + e - r.skew, SmRow<X>::at(w, e), all);
             }
           }
-          found = __any_sync(0xffffffffu, here);
-          run += __shfl_sync(0xffffffffu, ss, 31);
-          seen_mine += __shfl_sync(0xffffffffu, ts, 31);
+          if (__any_sync(0xffffffffu, here)) break;
+          run += __shfl_sync(0xffffffffu, upto, 31);
         }
-      }
     }
   }
-  if (cluster > 1) {
-    sm_cluster_sync();  // (no CTA ends while another reads from it)
-  }
+  sm_cluster_sync(cluster);  // (no CTA ends while another reads from it)
 }
 
-constexpr size_t kSmSmemBytes = ((sizeof(SmShared) + 15) & ~(size_t)15) + sizeof(SmMerged);
+constexpr size_t kSmSmemBytes = sizeof(SmShared);
 
 }  // namespace dynts
