@@ -37,10 +37,14 @@ namespace dynts {
 constexpr int kSmThreads = 512;
 constexpr int kSmWarps = kSmThreads / 32;
 constexpr int kSmWarpList = 128;     // tokens a warp can collect
-constexpr int kSmList = 1024;        // tokens the first CTA can merge
+constexpr int kSmList = 2048;        // tokens the first CTA can merge
 constexpr int kSmMaxCluster = 8;
 constexpr int kSmListK = 768;        // top_k that lists are tried with
-constexpr int kSmBins = kSmThreads;
+constexpr int kSmBins = 2 * kSmThreads;  // steps of a histogram
+constexpr int kSmTable = 16;
+constexpr int kSmGroups = 16;       // of a lane's vectors, whose maxima are kept
+constexpr int kSmPerSm = 2;         // CTAs
+constexpr int kSmNoStep = 1 << 20;   // of a token that weighs nothing
 constexpr int kSmMaxVocab = (1 << 19) - 1;  // sums of 2^45 for each token fit 64 bits
 
 struct SampleParams {
@@ -60,17 +64,18 @@ struct SampleParams {
 
 typedef unsigned long long u64;
 
-// Kept are the keys above `key` and those equal to it up to `index`.
+// Kept are the values above x and those equal to it up to `index`.
 struct SmBorder {
-  unsigned key;
+  float x;
   int index;
-  __device__ __forceinline__ bool keeps(unsigned k, int i) const { return k > key || (k == key && i <= index); }
+  __device__ __forceinline__ bool keeps(float y, int i) const { return y > x || (y == x && i <= index); }
 };
 
 struct SmShared {
-  double table[16];       // 2^(j / 16)
+  double table[kSmTable]; // 2^(j / 16): a bank each for the lanes' lookups
   float warp_max[kSmWarps], warp_min[kSmWarps];
   u64 scan[kSmWarps];
+  unsigned group_max[kSmGroups][kSmThreads];  // a word of maxima of each lane's groups
   // what the other CTAs of the cluster read
   float max, cut, low;    // largest logit; a value that enough tokens reach; smallest of the lanes' maxima
   unsigned lanes;         // that hold any
@@ -81,18 +86,22 @@ struct SmShared {
   int verdict;            // of the first CTA: 1 decided, 0 a list overflowed
   int tie_index;
   SmBorder border;
-  u64 hist[kSmBins];
+  unsigned hist[2][kSmBins];  // low and high halves of 64-bit sums
   unsigned radix_count[256];
-  u64 radix_weight[256];
+  unsigned radix_weight[2][256];
   uint2 list[kSmWarps][kSmWarpList];  // key, index
   // the rest is a CTA's own
   unsigned offset[kSmMaxCluster * kSmWarps + 1];
-  int bin;
+  int bin, digit;
   u64 above, below;
+  double goal;
   unsigned count;
   u64 merged_weight[256];
   unsigned merged_count[256];
   u64 sort[kSmThreads];
+  unsigned picked, key_min, key_max;
+  int found;
+  unsigned pick[kSmList];
   unsigned key[kSmList];  // the merged lists
   int index[kSmList];
   u64 weight[kSmList];
@@ -125,31 +134,52 @@ __device__ __forceinline__ T sm_peer(const T* mine, int rank) {  // the same var
   return x;
 }
 
+// Adds to a 64-bit sum in shared memory as two 32-bit words: the sum of the low words wraps around in exactly one of the
+// additions that carry.  (2.5 cycles per word and warp; one 64-bit addition is a loop of compare-and-swap, 19 to 57.)
+template <int N>
+__device__ __forceinline__ void sm_add(unsigned (&sum)[2][N], int at, u64 x) {
+  const unsigned lo = (unsigned)x, old = atomicAdd(&sum[0][at], lo), hi = (unsigned)(x >> 32) + (old + lo < lo ? 1u : 0u);
+  if (hi) atomicAdd(&sum[1][at], hi);
+}
+
 __device__ __forceinline__ unsigned sm_key(float x) {  // order-preserving; -0 and +0 alike
   const unsigned b = __float_as_uint(x + 0.f);
   return b ^ ((b >> 31) ? 0xffffffffu : 0x80000000u);
 }
 __device__ __forceinline__ float sm_value(unsigned key) { return __uint_as_float(key ^ ((key >> 31) ? 0x80000000u : 0xffffffffu)); }
 
-// exp(y) for y <= 0 in units of 2^-45: e^y = 2^(n / 16) e^f with n whole and |f| <= ln 2 / 32; the series of e^f to f^6 is off by
-// less than 5e-16 of it.  (y below -32, or not a number: less than half a unit, 0.)
-__device__ __forceinline__ u64 sm_weight(double y, const double* table) {
-  if (!(y > -32.0)) return 0;
-  const double magic = 6755399441055744.0;  // 1.5 * 2^52: the sum's low bits are the whole part
-  const double t = fma(y, 23.083120654223414, magic);  // 16 / ln 2
-  const int n = __double2loint(t);
-  const double f = fma(t - magic, -0.04332169878499658, y);  // ln 2 / 16
-  double e = 1.0 / 720.0;
-  e = fma(e, f, 1.0 / 120.0);
-  e = fma(e, f, 1.0 / 24.0);
-  e = fma(e, f, 1.0 / 6.0);
-  e = fma(e, f, 0.5);
-  e = fma(e, f, 1.0);
-  e = fma(e, f, 1.0);
-  e *= table[n & 15];
-  e = __hiloint2double(__double2hiint(e) + (n >> 4) * (1 << 20), __double2loint(e));
-  return (u64)__double_as_longlong(e + 128.0) - (u64)__double_as_longlong(128.0);  // (a unit of the sum's mantissa is 2^-45)
-}
+// A row's weights exp((x - M) / T) in units of 2^-45.  With y = (x - M) / T: e^y = 2^(n / 16) e^f, n whole and |f| <= ln 2 / 32; the
+// series of e^f to f^6 is off by less than 5e-16 of it.  Twelve operations in 64 bits: with the rest of a token's 25 instructions they
+// bound the rows whose weights are all added up.  (64 table entries and a series to f^4: bank conflicts cost more than two operations.)
+struct SmWeights {
+  double top, inv_t;
+  const double* table;
+  static __device__ __forceinline__ int fine(int n, double f) { return -2 * n + ((unsigned)__double2hiint(f) > 0x80000000u ? 1 : 0); }  // (-0 is no less than 0)
+  __device__ __forceinline__ int step(float x) const {
+    const double y = ((double)x - top) * inv_t, magic = 6755399441055744.0, t = fma(y, 23.083120654223414, magic);
+    if ((unsigned)__double2hiint(y) >= 0xc0400000u) return kSmNoStep;
+    return fine(__double2loint(t), fma(t - magic, -0.04332169878499658, y));
+  }
+  __device__ __forceinline__ u64 operator()(float x) const {
+    int n;
+    return with_step(x, n);
+  }
+  // n: its step, 32 to a binary order down from 1 (below 2^-46: kSmNoStep); it never grows with x.
+  __device__ __forceinline__ u64 with_step(float x, int& n) const {
+    const double y = ((double)x - top) * inv_t;  // (the difference first: a largest logit of any size leaves its precision alone)
+    const double magic = 6755399441055744.0;  // 1.5 * 2^52: the sum's low bits are the whole part
+    const double t = fma(y, 23.083120654223414, magic);  // 16 / ln 2
+    n = __double2loint(t);
+    const double f = fma(t - magic, -0.04332169878499658, y);  // ln 2 / 16
+    double e = fma(fma(fma(fma(fma(fma(1.0 / 720.0, f, 1.0 / 120.0), f, 1.0 / 24.0), f, 1.0 / 6.0), f, 0.5), f, 1.0), f, 1.0);
+    const double g = table[n & (kSmTable - 1)];
+    e = fma(__hiloint2double(__double2hiint(g) + (n >> 4) * (1 << 20), __double2loint(g)), e, 128.0);
+    const u64 w = (u64)__double_as_longlong(e) - 0x4060000000000000ull;  // (128, whose mantissa's unit is 2^-45)
+    const bool some = (unsigned)__double2hiint(y) < 0xc0400000u;  // (y <= -32: less than half a unit.  No branch: several tokens' chains side by side)
+    n = some ? fine(n, f) : kSmNoStep;
+    return some ? w : 0ull;
+  }
+};
 
 __device__ __forceinline__ float sm_max_nan(float a, float b) {  // a NaN stays
   float y;
@@ -162,6 +192,27 @@ __device__ __forceinline__ unsigned sm_max2_nan(unsigned a, unsigned b) {  // of
   return y;
 }
 
+// A vector that begins at element i of the row and is not all within it.
+template <typename X>
+__device__ __noinline__ uint4 sm_edge(const X* at, int i, int vocab) {
+  constexpr int E = 16 / (int)sizeof(X);
+  unsigned w[4];
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    if constexpr (E == 4) {
+      w[q] = i + q >= 0 && i + q < vocab ? __float_as_uint(at[q]) : 0xff800000u;
+    } else {
+      w[q] = 0xff80ff80u;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int e = 2 * q + h;
+        if (i + e >= 0 && i + e < vocab) w[q] = (w[q] & (h ? 0x0000ffffu : 0xffff0000u)) | ((unsigned)__bfloat16_as_ushort(at[e]) << (16 * h));
+      }
+    }
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
 // A row in 16-byte vectors, from the boundary at or before its first element; what lies outside the row reads as -inf, which
 // weighs nothing.
 template <typename X>
@@ -171,24 +222,11 @@ struct SmRow {
   int skew;        // elements between there and the row
   int vocab;
   int v0, v1;      // this warp's vectors
+  int rounds;      // of 128 vectors of a warp, in a group
   __device__ __forceinline__ uint4 load(int v) const {
     const int i = v * E - skew;
     if (i >= 0 && i + E <= vocab) return *reinterpret_cast<const uint4*>(base + (size_t)v * E);
-    unsigned w[4];
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      if constexpr (E == 4) {
-        w[q] = i + q >= 0 && i + q < vocab ? __float_as_uint(base[(size_t)v * E + q]) : 0xff800000u;
-      } else {
-        w[q] = 0xff80ff80u;
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const int e = 2 * q + h;
-          if (i + e >= 0 && i + e < vocab) w[q] = (w[q] & (h ? 0x0000ffffu : 0xffff0000u)) | ((unsigned)__bfloat16_as_ushort(base[(size_t)v * E + e]) << (16 * h));
-        }
-      }
-    }
-    return make_uint4(w[0], w[1], w[2], w[3]);
+    return sm_edge(base + (size_t)v * E, i, vocab);
   }
   static __device__ __forceinline__ float at(const uint4& w, int e) {
     const unsigned q[4] = {w.x, w.y, w.z, w.w};
@@ -207,6 +245,20 @@ struct SmRow {
     else return sm_max_nan(__uint_as_float(m << 16), __uint_as_float(m & 0xffff0000u));
   }
 };
+
+// This lane's vectors of a warp's run, four loads at a time.
+template <typename X, typename F>
+__device__ __forceinline__ void each_vector(const SmRow<X>& r, int v0, int v1, F f) {
+  for (int v = v0 + (int)(threadIdx.x & 31); v < v1; v += 128) {
+    uint4 w[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      if (v + 32 * q < v1) w[q] = r.load(v + 32 * q);
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      if (v + 32 * q < v1) f(v + 32 * q, w[q]);
+  }
+}
 
 template <typename V>
 __device__ __forceinline__ V sm_warp_scan(V x) {  // inclusive
@@ -236,37 +288,80 @@ __device__ __forceinline__ u64 sm_scan(u64 x, u64* warps, u64& total) {
   return before + s - x;
 }
 
-// Sorted, the largest first: N values per thread, value q of thread t is place t + 512 q.
-template <int N>
-__device__ __forceinline__ void sm_sort(u64 (&x)[N], u64* smem) {
+// Whether a running sum passes its goal with this addend: the first one does, or it had not been reached before.
+__device__ __forceinline__ bool sm_passes(u64 before, u64 here, double goal) {
+  return here > 0 && (double)(before + here) >= goal && (before == 0 || (double)before < goal);
+}
+
+// By all threads of a CTA: the token of the merged list at which the running sum down the ranking passes its goal, `above` lying before
+// them all: a histogram of the distance to `from` in steps, then the tokens of one step against one another.  Sums are of the weights or of
+// the tokens that `outer` keeps.  -1: the sum does not get there.
+__device__ __noinline__ int sm_pick(SmShared& sh, unsigned n, u64 above, double goal, bool by_weight, SmBorder outer, float from, float steps) {
   const int tid = threadIdx.x;
-  for (int k = 2; k <= N * kSmThreads; k <<= 1)
-    for (int o = k >> 1; o > 0; o >>= 1) {
-      if (N == 2 && o == kSmThreads) {  // (k = 1024: the largest first throughout)
-        const u64 a = x[0], b = x[N - 1];
-        x[0] = max(a, b);
-        x[N - 1] = min(a, b);
-        continue;
-      }
+  auto amount = [&](unsigned i) { return outer.keeps(sm_value(sh.key[i]), sh.index[i]) ? by_weight ? sh.weight[i] : 1ull : 0ull; };
+  auto step = [&](unsigned i) { return max(0, min(kSmBins - 1, (int)((from - sm_value(sh.key[i])) * steps))); };
+  for (int q = 0; q < 2; ++q) sh.hist[0][tid + q * kSmThreads] = sh.hist[1][tid + q * kSmThreads] = 0;
+  if (tid == 0) sh.digit = sh.found = -1, sh.picked = 0, sh.key_min = 0xffffffffu, sh.key_max = 0;
+  __syncthreads();
+  for (unsigned i = tid; i < n; i += kSmThreads) {
+    const u64 a = amount(i);
+    if (a) sm_add(sh.hist, step(i), a);
+  }
+  __syncthreads();
+  u64 here[2], all;
 #pragma unroll
-      for (int q = 0; q < N; ++q) {
-        u64 y;
-        if (o >= 32) {
-          __syncthreads();
-          smem[tid] = x[q];
-          __syncthreads();
-          y = smem[tid ^ o];
-        } else {
-          y = __shfl_xor_sync(0xffffffffu, x[q], o);
-        }
-        const int place = tid + q * kSmThreads;
-        x[q] = ((place & k) == 0) == ((place & o) == 0) ? max(x[q], y) : min(x[q], y);
+  for (int q = 0; q < 2; ++q) here[q] = sh.hist[0][2 * tid + q] + ((u64)sh.hist[1][2 * tid + q] << 32);
+  const u64 before = sm_scan(here[0] + here[1], sh.scan, all) + above;
+  if (sm_passes(before, here[0] + here[1], goal)) {
+    const bool second = !sm_passes(before, here[0], goal);
+    sh.digit = 2 * tid + (second ? 1 : 0);
+    sh.below = before + (second ? here[0] : 0ull);
+  }
+  __syncthreads();
+  const int bin = sh.digit;
+  if (bin >= 0) {
+    for (unsigned i = tid; i < n; i += kSmThreads)
+      if (step(i) == bin && amount(i)) {
+        sh.pick[atomicAdd(&sh.picked, 1u)] = i;
+        atomicMin(&sh.key_min, sh.key[i]);
+        atomicMax(&sh.key_max, sh.key[i]);
       }
+    __syncthreads();
+    const unsigned m = sh.picked;
+    if (m > 32 && sh.key_min == sh.key_max) {
+      // equal values (logits of 16 bits): the list is in the order of the vocabulary, so its place is a count
+      const u64 one = by_weight ? sh.weight[sh.pick[0]] : 1ull;
+      const double need = ceil((goal - (double)sh.below) / (double)one);
+      u64 t = need <= 1.0 ? 1ull : need >= (double)m ? (u64)m : (u64)need;
+      while (t > 1 && (double)(sh.below + (t - 1) * one) >= goal) --t;
+      while (t < m && (double)(sh.below + t * one) < goal) ++t;
+      constexpr unsigned N = kSmList / kSmThreads;
+      u64 mine = 0, ties;
+      for (unsigned i = N * tid; i < min(n, N * (tid + 1)); ++i) mine += step(i) == bin && amount(i) ? 1ull : 0ull;
+      u64 seen = sm_scan(mine, sh.scan, ties);
+      for (unsigned i = N * tid; i < min(n, N * (tid + 1)); ++i)
+        if (step(i) == bin && amount(i) && ++seen == t) sh.found = (int)i;
+    } else for (unsigned e = tid; e < m; e += kSmThreads) {
+      const unsigned i = sh.pick[e], key = sh.key[i];
+      const int index = sh.index[i];
+      u64 run = sh.below;
+      for (unsigned o = 0; o < m; ++o) {
+        const unsigned j = sh.pick[o], other = sh.key[j];
+        if (other > key || (other == key && sh.index[j] < index)) run += by_weight ? sh.weight[j] : 1ull;
+      }
+      if (sm_passes(run, by_weight ? sh.weight[i] : 1ull, goal)) sh.found = (int)i;
     }
+    __syncthreads();
+  }
+  const int found = sh.found;
+  __syncthreads();
+  for (int q = 0; q < 2; ++q) sh.hist[0][tid + q * kSmThreads] = sh.hist[1][tid + q * kSmThreads] = 0;
+  __syncthreads();
+  return found;
 }
 
 template <typename X>
-__global__ void __launch_bounds__(kSmThreads, 2) sample_kernel(const __grid_constant__ SampleParams p) {
+__global__ void __launch_bounds__(kSmThreads, kSmPerSm) sample_kernel(const __grid_constant__ SampleParams p) {
   constexpr int E = SmRow<X>::E;
   extern __shared__ __align__(16) uint8_t sm_raw[];
   SmShared& sh = *reinterpret_cast<SmShared*>(sm_raw);
@@ -284,6 +379,7 @@ __global__ void __launch_bounds__(kSmThreads, 2) sample_kernel(const __grid_cons
     const int c0 = min(vectors, rank * per), c1 = min(vectors, c0 + per), mine = (c1 - c0 + kSmWarps - 1) / kSmWarps;
     r.v0 = min(c1, c0 + warp * mine);
     r.v1 = min(c1, r.v0 + mine);
+    r.rounds = max(1, (mine + 128 * kSmGroups - 1) / (128 * kSmGroups));  // (the same in every warp)
   }
   // the row's settings
   float T = p.temperatures ? p.temperatures[row] : p.temperature, top_p = p.top_ps ? p.top_ps[row] : p.top_p;
@@ -295,27 +391,35 @@ __global__ void __launch_bounds__(kSmThreads, 2) sample_kernel(const __grid_cons
   if (top_k == 1 || !(top_p < 1.f)) top_p = 1.f;
   top_p = fmaxf(top_p, 0.f);
   const bool cut_p = top_p < 1.f;
-  const double inv_t = 1.0 / (double)T;
+  const double inv_t = 1.0 / (double)fminf(T, 3.0e38f);
   const int share = (top_k + cluster - 1) / cluster;  // of top_k, for each CTA
   const bool listed = top_k > 0 && top_k <= kSmListK && share <= kSmThreads / 2;
-  if (tid < 16) sh.table[tid] = exp2((double)tid / 16.0);
-  sh.hist[tid] = 0;
 
   // ---- every lane's maximum
   float top;
   {
     unsigned m = SmRow<X>::start();
-    int v = r.v0 + lane;
-    for (; v + 96 < r.v1; v += 128) {
+    unsigned mg = SmRow<X>::start();
+    int g = 0, left = r.rounds;
+    for (int v = r.v0 + lane; v < r.v1; v += 128) {
       uint4 w[4];
 #pragma unroll
-      for (int q = 0; q < 4; ++q) w[q] = r.load(v + 32 * q);
+      for (int q = 0; q < 4; ++q)
+        if (v + 32 * q < r.v1) w[q] = r.load(v + 32 * q);
 #pragma unroll
-      for (int q = 0; q < 4; ++q) m = SmRow<X>::more(m, w[q]);
+      for (int q = 0; q < 4; ++q)
+        if (v + 32 * q < r.v1) mg = SmRow<X>::more(mg, w[q]);
+      if (--left == 0 || v + 128 >= r.v1) {
+        sh.group_max[g++][tid] = mg;
+        m = SmRow<X>::more(m, make_uint4(mg, mg, mg, mg));
+        mg = SmRow<X>::start();
+        left = r.rounds;
+      }
     }
-    for (; v < r.v1; v += 32) m = SmRow<X>::more(m, r.load(v));
     top = SmRow<X>::largest(m);
   }
+  if (tid < kSmTable) sh.table[tid] = exp2((double)tid / kSmTable);
+  for (int q = 0; q < 2; ++q) sh.hist[0][tid + q * kSmThreads] = sh.hist[1][tid + q * kSmThreads] = 0;
   const float lane_top = top;
   float least = top > -INFINITY ? top : INFINITY;  // of the lanes that hold anything
 #pragma unroll
@@ -328,20 +432,22 @@ __global__ void __launch_bounds__(kSmThreads, 2) sample_kernel(const __grid_cons
 #pragma unroll
   for (int w = 0; w < kSmWarps; ++w) top = sm_max_nan(top, sh.warp_max[w]), least = fminf(least, sh.warp_min[w]);
   float cut = -INFINITY;
-  if (listed) {
+  if (listed && share == 1) {
+    cut = top;
+  } else if (listed) {
     // a value that `share` of the lanes' maxima reach, close to the largest such: by a histogram of 512 equal steps
-    const float steps = top > least ? (kSmBins - 1) / (top - least) : 0.f;
-    int b = kSmBins;
+    const float steps = top > least ? (kSmThreads - 1) / (top - least) : 0.f;
+    int b = kSmThreads;
     if (lane_top > -INFINITY) {
-      b = min(kSmBins - 1, (int)((top - lane_top) * steps));
-      atomicAdd(reinterpret_cast<unsigned*>(&sh.hist[b]), 1u);
+      b = min(kSmThreads - 1, (int)((top - lane_top) * steps));
+      atomicAdd(&sh.hist[0][b], 1u);
     }
     u64 all;
-    if (tid == 0) sh.bin = kSmBins;
-    const u64 before = (__syncthreads(), sm_scan(sh.hist[tid], sh.scan, all)), here = sh.hist[tid];
+    if (tid == 0) sh.bin = kSmThreads;
+    const u64 before = (__syncthreads(), sm_scan(sh.hist[0][tid], sh.scan, all)), here = sh.hist[0][tid];
     if (before < (u64)share && before + here >= (u64)share) sh.bin = tid;
     __syncthreads();
-    if (sh.bin < kSmBins) {  // (fewer lanes hold anything: all is collected)
+    if (sh.bin < kSmThreads) {  // (fewer lanes hold anything: all is collected)
       float reach = b <= sh.bin ? lane_top : INFINITY;
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) reach = fminf(reach, __shfl_xor_sync(0xffffffffu, reach, o));
@@ -351,7 +457,7 @@ __global__ void __launch_bounds__(kSmThreads, 2) sample_kernel(const __grid_cons
 #pragma unroll
       for (int w = 0; w < kSmWarps; ++w) cut = fminf(cut, sh.warp_min[w]);
     }
-    sh.hist[tid] = 0;
+    sh.hist[0][tid] = 0;
   }
   if (tid == 0) sh.max = top, sh.cut = cut, sh.low = least, sh.lanes = lanes;
   sm_cluster_sync(cluster);
@@ -373,42 +479,50 @@ __global__ void __launch_bounds__(kSmThreads, 2) sample_kernel(const __grid_cons
   }
   const double Md = (double)M;
   // what min_p keeps: x >= least_x (min_p > 1 counts as 1)
-  const double least_x = min_p > 0.f ? fmin(Md + (double)T * log((double)min_p), Md) : -INFINITY;
-  auto weight_of = [&](float x) { return sm_weight(((double)x - Md) * inv_t, sh.table); };
+  const float least_x = min_p > 0.f ? __double2float_ru(fmin(Md + (double)T * log((double)min_p), Md)) : -INFINITY;
+  const SmWeights weight_of{Md, inv_t, sh.table};
   auto answer = [&](int token, float x, u64 total) {
     p.tokens[row] = token;
     if (p.logprobs) p.logprobs[row] = (float)(((double)x - Md) * inv_t - log((double)total * 2.842170943040401e-14));  // 2^-45
   };
-  // The tokens for which wanted(x, key, index) holds, of vectors whose largest element is at least `reach`: a list per warp.
+  // The tokens for which wanted(x, index) holds, of vectors whose largest element is at least `reach`: a list per warp.
   auto collect = [&](float reach, auto wanted) {
     unsigned count = 0;
-#pragma unroll 2
-    for (int vb = r.v0; vb < r.v1; vb += 32) {
-      const int v = vb + lane;
-      uint4 w = make_uint4(0u, 0u, 0u, 0u);
-      bool any = false;
-      if (v < r.v1) {
-        w = r.load(v);
-        any = SmRow<X>::largest(SmRow<X>::more(SmRow<X>::start(), w)) >= reach;
-      }
-      if (!__any_sync(0xffffffffu, any)) continue;
-      unsigned hits = 0;  // a bit for each of the lane's elements
-      if (any) {
+    int g = 0, left = r.rounds;
+    for (int vb = r.v0; vb < r.v1; vb += 128) {
+      const bool look = vb + lane < r.v1 && SmRow<X>::largest(sh.group_max[g][tid]) >= reach;
+      if (--left == 0) ++g, left = r.rounds;
+      if (!__any_sync(0xffffffffu, look)) continue;
+      uint4 ws[4];
+      bool any[4];
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-          const float x = SmRow<X>::at(w, e);
-          hits |= (x > -INFINITY && wanted(x, sm_key(x), v * E + e - r.skew) ? 1u : 0u) << e;
-        }
-      }
-      const unsigned n = __popc(hits), upto = sm_warp_scan(n);
-      unsigned at = count + upto - n;
+      for (int q = 0; q < 4; ++q)
+        if (look && vb + 32 * q + lane < r.v1) ws[q] = r.load(vb + 32 * q + lane);
 #pragma unroll
-      for (int e = 0; e < E; ++e)
-        if ((hits >> e) & 1u) {
-          if (at < kSmWarpList) sh.list[warp][at] = make_uint2(sm_key(SmRow<X>::at(w, e)), (unsigned)(v * E + e - r.skew));
-          ++at;
+      for (int q = 0; q < 4; ++q) any[q] = look && vb + 32 * q + lane < r.v1 && SmRow<X>::largest(SmRow<X>::more(SmRow<X>::start(), ws[q])) >= reach;
+      if (!__any_sync(0xffffffffu, any[0] || any[1] || any[2] || any[3])) continue;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        if (!__any_sync(0xffffffffu, any[q])) continue;
+        const int v = vb + 32 * q + lane;
+        unsigned hits = 0;  // a bit for each of the lane's elements
+        if (any[q]) {
+#pragma unroll
+          for (int e = 0; e < E; ++e) {
+            const float x = SmRow<X>::at(ws[q], e);
+            hits |= (x > -INFINITY && wanted(x, v * E + e - r.skew) ? 1u : 0u) << e;
+          }
         }
-      count += __shfl_sync(0xffffffffu, upto, 31);
+        const unsigned n = __popc(hits), upto = sm_warp_scan(n);
+        unsigned at = count + upto - n;
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+          if ((hits >> e) & 1u) {
+            if (at < kSmWarpList) sh.list[warp][at] = make_uint2(sm_key(SmRow<X>::at(ws[q], e)), (unsigned)(v * E + e - r.skew));
+            ++at;
+          }
+        count += __shfl_sync(0xffffffffu, upto, 31);
+      }
     }
     if (lane == 0) sh.warp_count[warp] = count;
   };
@@ -416,18 +530,21 @@ __global__ void __launch_bounds__(kSmThreads, 2) sample_kernel(const __grid_cons
   auto merge = [&]() -> unsigned {
     __syncthreads();
     if (warp == 0) {
-      unsigned base = 0;
-      bool over = false;
-      for (int i0 = 0; i0 < lists; i0 += 32) {
-        const int i = i0 + lane;
-        const unsigned c = i < lists ? sm_peer(&sh.warp_count[i % kSmWarps], i / kSmWarps) : 0u;
-        over = over || c > kSmWarpList;
-        const unsigned upto = sm_warp_scan(min(c, (unsigned)kSmWarpList));
-        if (i < lists) sh.offset[i] = base + upto - min(c, (unsigned)kSmWarpList);
-        base += __shfl_sync(0xffffffffu, upto, 31);
+      constexpr int N = kSmMaxCluster * kSmWarps / 32;  // neighbouring lists per lane
+      unsigned c[N], sum = 0, most = 0;
+#pragma unroll
+      for (int q = 0; q < N; ++q) c[q] = lane * N + q < lists ? sm_peer(&sh.warp_count[(lane * N + q) % kSmWarps], (lane * N + q) / kSmWarps) : 0u;
+#pragma unroll
+      for (int q = 0; q < N; ++q) sum += c[q], most = max(most, c[q]);
+      const unsigned upto = sm_warp_scan(sum);
+      unsigned base = upto - sum;
+#pragma unroll
+      for (int q = 0; q < N; ++q) {
+        sh.offset[lane * N + q] = base;
+        base += c[q];
       }
-      over = __any_sync(0xffffffffu, over);
-      if (lane == 0) sh.offset[lists] = base, sh.count = over ? kSmList + 1 : base;
+      const bool over = __any_sync(0xffffffffu, most > kSmWarpList);
+      if (lane == 31) sh.count = over ? kSmList + 1 : upto;
     }
     __syncthreads();
     const unsigned n = sh.count;
@@ -447,52 +564,70 @@ __global__ void __launch_bounds__(kSmThreads, 2) sample_kernel(const __grid_cons
     __syncthreads();
     return n;
   };
-  // By the first CTA: the border among the merged tokens: the first `want` are kept (0: all of them), of those the shortest run whose
-  // weights reach part of theirs (part < 0: all), or reach `goal` with `above` before them (goal >= 0).
-  auto rank_list = [&](unsigned n, unsigned want, double part, u64 above, double goal) -> SmBorder {
-    auto with = [&](auto per) {
-      constexpr int N = decltype(per)::value;
-      u64 x[N], w[N], run[N], before = 0, all;
-#pragma unroll
-      for (int q = 0; q < N; ++q) {
-        const unsigned i = tid + q * kSmThreads;
-        x[q] = i < n ? ((u64)sh.key[i] << 32) | (0xffffffffu - i) : 0ull;
-      }
-      sm_sort(x, sh.sort);
-#pragma unroll
-      for (int q = 0; q < N; ++q) {
-        const unsigned place = tid + q * kSmThreads;
-        const bool counts = place < n && (want == 0 || place < want);
-        w[q] = counts ? sh.weight[0xffffffffu - (unsigned)x[q]] : 0ull;
-        run[q] = before + sm_scan(w[q], sh.scan, all);
-        before += all;
-      }
-      const bool whole = goal < 0.0 && part < 0.0;
-      const double reach = goal >= 0.0 ? goal : part * (double)before;
+  // By the first CTA: the border among the merged tokens: the first `want` are kept, of those the shortest run whose
+  // weights reach part of theirs (part < 0: all), or reach `goal` with `above` before them (goal >= 0).  from: no token is above it.
+  auto rank_list = [&](unsigned n, unsigned want, double part, u64 above, double goal, float from) -> SmBorder {
+    if (n <= kSmThreads / 2) {
+      // few: each token's rank and the weights before it by comparing it with all, several threads to a token
+      int per = 2;
+      while (per < 32 && per * 2 * n <= kSmThreads) per *= 2;
+      const unsigned i = tid / per, j0 = tid % per;
+      u64 mine = 0, run = 0, total = 0;
+      unsigned place = 0;
+      if (tid < n) sh.sort[tid] = ((u64)sh.key[tid] << 32) | (0xffffffffu - tid);
       if (tid == 0) sh.count = 0;
       __syncthreads();
-#pragma unroll
-      for (int q = 0; q < N; ++q) {  // the last kept token is the border
-        const unsigned place = tid + q * kSmThreads;
-        const bool counts = place < n && (want == 0 || place < want);
-        const bool kept = counts && (whole || place + above == 0 || (double)(above + run[q]) < reach);
-        if (kept) atomicMax(&sh.count, place + 1);
+      if (i < n) mine = sh.sort[i];
+      for (unsigned j = j0; j < n; j += per) {
+        const bool before = sh.sort[j] > mine;
+        place += before ? 1u : 0u;
+        run += before ? sh.weight[j] : 0ull;
       }
+      for (int o = per / 2; o > 0; o >>= 1) place += __shfl_xor_sync(0xffffffffu, place, o), run += __shfl_xor_sync(0xffffffffu, run, o);
+      const bool counts = i < n && place < want;
+      if (counts && j0 == 0 && place + 1 == min(n, want)) sh.below = run + sh.weight[i];  // of all that count
       __syncthreads();
-      const unsigned last = sh.count - 1;
-#pragma unroll
-      for (int q = 0; q < N; ++q)
-        if (tid + q * kSmThreads == last) {
-          const unsigned i = 0xffffffffu - (unsigned)x[q];
-          sh.border = SmBorder{sh.key[i], sh.index[i]};
-        }
+      total = sh.below;
+      const bool whole = goal < 0.0 && part < 0.0;
+      const double reach = goal >= 0.0 ? goal : part * (double)total;
+      const bool kept = counts && (whole || place + above == 0 || (double)(above + run) < reach);
+      const unsigned most = __reduce_max_sync(0xffffffffu, kept ? place + 1 : 0u);
+      if (lane == 0 && most > 0) atomicMax(&sh.count, most);
+      __syncthreads();
+      if (i < n && j0 == 0 && place + 1 == sh.count) sh.border = SmBorder{sm_value(sh.key[i]), sh.index[i]};
       __syncthreads();
       return sh.border;
+    }
+    float least = INFINITY;
+    for (unsigned i = tid; i < n; i += kSmThreads) least = fminf(least, sm_value(sh.key[i]));
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) least = fminf(least, __shfl_xor_sync(0xffffffffu, least, o));
+    if (lane == 0) sh.warp_min[warp] = least;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kSmWarps; ++w) least = fminf(least, sh.warp_min[w]);
+    const float steps = from > least ? fminf((kSmBins - 1) / (from - least), 1e30f) : 0.f;
+    SmBorder b{-INFINITY, -1};
+    auto take = [&](int at) {
+      if (at >= 0) b = SmBorder{sm_value(sh.key[at]), sh.index[at]};
     };
-    return n <= kSmThreads ? with(std::integral_constant<int, 1>{}) : with(std::integral_constant<int, 2>{});
+    if (goal >= 0.0) {
+      take(sm_pick(sh, n, above, goal, true, b, from, steps));
+    } else {
+      take(sm_pick(sh, n, 0, (double)min(want, n), false, b, from, steps));
+      if (part >= 0.0) {
+        u64 mine = 0, all;
+        for (unsigned i = tid; i < n; i += kSmThreads) mine += b.keeps(sm_value(sh.key[i]), sh.index[i]) ? sh.weight[i] : 0ull;
+        sm_scan(mine, sh.scan, all);
+        take(sm_pick(sh, n, 0, part * (double)all, true, b, from, steps));
+      }
+    }
+    if (tid == 0) sh.border = b;
+    __syncthreads();
+    return b;
   };
   bool done = false;
-  SmBorder border{0u, -1};  // (every key is above 0)
+  SmBorder border{-INFINITY, -1};
   if (!(M > -INFINITY && M < INFINITY)) {  // NaN or +inf somewhere, or nothing but -inf
     if (rank == 0 && tid == 0) {
       p.tokens[row] = -1;
@@ -501,23 +636,30 @@ __global__ void __launch_bounds__(kSmThreads, 2) sample_kernel(const __grid_cons
     done = true;
   }
   if (!done && listed) {
-    collect(cut, [&](float x, unsigned, int) { return x >= cut; });
+    collect(cut, [&](float x, int) { return x >= cut; });
     sm_cluster_sync(cluster);
     if (rank == 0) {
       const unsigned n = merge();
       if (n <= kSmList) {
-        const SmBorder b = rank_list(n, (unsigned)top_k, cut_p ? (double)top_p : -1.0, 0, -1.0);
-        // the kept tokens' running sums, in the order of the vocabulary: two neighbours per thread
-        u64 w[2], all;
+        const SmBorder b = rank_list(n, (unsigned)top_k, cut_p ? (double)top_p : -1.0, 0, -1.0, M);
+        // the kept tokens' running sums, in the order of the vocabulary: neighbours per thread
+        constexpr int N = kSmList / kSmThreads;
+        u64 w[N], sum = 0, all;
 #pragma unroll
-        for (int q = 0; q < 2; ++q) {
-          const unsigned i = 2 * tid + q;
-          w[q] = i < n && b.keeps(sh.key[i], sh.index[i]) && (double)sm_value(sh.key[i]) >= least_x ? sh.weight[i] : 0ull;
+        for (int q = 0; q < N; ++q) {
+          const unsigned i = N * tid + q;
+          w[q] = i < n && b.keeps(sm_value(sh.key[i]), sh.index[i]) && sm_value(sh.key[i]) >= least_x ? sh.weight[i] : 0ull;
+          sum += w[q];
         }
-        const u64 run = sm_scan(w[0] + w[1], sh.scan, all);
+        u64 run = sm_scan(sum, sh.scan, all);
         const u64 target = min((u64)__double2ull_rd((double)u * (double)all), all - 1);
-        if (run <= target && run + w[0] + w[1] > target) {
-          const unsigned i = 2 * tid + (run + w[0] > target ? 0 : 1);
+        if (run <= target && run + sum > target) {
+          unsigned i = N * tid;
+#pragma unroll
+          for (int q = 0; q < N - 1; ++q) {
+            run += w[q];
+            if (run <= target) i = N * tid + q + 1;
+          }
           answer(sh.index[i], sm_value(sh.key[i]), all);
         }
       }
@@ -531,24 +673,25 @@ __global__ void __launch_bounds__(kSmThreads, 2) sample_kernel(const __grid_cons
     for (int which = 0; which < 2; ++which) {
       const bool by_weight = which == 1;
       if (by_weight ? !cut_p : top_k == 0) continue;
-      // Distances to the maximum up to `span` in 512 steps.  Weights: what lies beyond ln(V / (1 - p)) in units of T adds up to less than
-      // 1 - p of the largest, so no border lies there.  Tokens: the lanes' maxima reach down to low_all; beyond their number, the
-      // smallest logit does.
-      float span;
+      // Weights: steps of a thirty-second of a binary order.  What lies beyond ln(V / (1 - p)) in units of T adds up to less than 1 - p of
+      // the largest, so no border lies there and no step is counted.  Tokens: equal steps of the distance to the maximum up to `span`;
+      // the lanes' maxima reach down to low_all; beyond their number, the smallest logit does.
+      float span = 0.f;
+      int bins = kSmBins, coarse = 0;  // (two steps as one where 1024 do not reach)
       if (by_weight) {
-        span = T * fminf(32.f, logf((float)p.vocab / (1.f - top_p)) + 0.01f);
+        bins = 2 + (int)(46.17f * (logf((float)p.vocab / (1.f - top_p)) + 0.01f));  // 32 / ln 2
+        if (bins > kSmBins) coarse = 1, bins = kSmBins;
       } else if ((unsigned)top_k <= lanes_all) {
         span = M - low_all;
       } else {
         float least_all = INFINITY;
-        for (int v = r.v0 + lane; v < r.v1; v += 32) {
-          const uint4 w = r.load(v);
+        each_vector(r, r.v0, r.v1, [&](int, const uint4& w) {
 #pragma unroll
           for (int e = 0; e < E; ++e) {
             const float x = SmRow<X>::at(w, e);
             if (x > -INFINITY) least_all = fminf(least_all, x);
           }
-        }
+        });
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) least_all = fminf(least_all, __shfl_xor_sync(0xffffffffu, least_all, o));
         __syncthreads();
@@ -562,26 +705,34 @@ __global__ void __launch_bounds__(kSmThreads, 2) sample_kernel(const __grid_cons
         span = M - least_all;
       }
       const float steps = span > 0.f ? fminf((kSmBins - 1) / span, 1e30f) : 0.f;
-      const float reach_all = M - span * 1.001f;
+      const float reach_all = M - span * 1.01f;  // (a step more than the span)
       auto bin_of = [&](float x) {  // (never grows with x: every rounding is monotone)
+        if (by_weight) {
+          const int n = weight_of.step(x) >> coarse;
+          return n < bins ? n : kSmBins;
+        }
         const float y = (M - x) * steps;
         return y < (float)kSmBins ? (int)y : kSmBins;
       };
       u64 outside = 0;
-#pragma unroll 2
-      for (int v = r.v0 + lane; v < r.v1; v += 32) {
-        const uint4 w = r.load(v);
-        if (!by_weight && !(SmRow<X>::largest(SmRow<X>::more(SmRow<X>::start(), w)) >= reach_all)) continue;
+      each_vector(r, r.v0, r.v1, [&](int v, const uint4& w) {
+        if (!by_weight && !(SmRow<X>::largest(SmRow<X>::more(SmRow<X>::start(), w)) >= reach_all)) return;
 #pragma unroll
         for (int e = 0; e < E; ++e) {
           const float x = SmRow<X>::at(w, e);
-          if (!(x > -INFINITY) || !border.keeps(sm_key(x), v * E + e - r.skew)) continue;
-          const u64 amount = by_weight ? weight_of(x) : 1ull;
-          const int b = bin_of(x);
-          if (b < kSmBins) atomicAdd(&sh.hist[b], amount);
-          else outside += amount;
+          if (!border.keeps(x, v * E + e - r.skew)) continue;
+          if (by_weight) {
+            int b;
+            const u64 w = weight_of.with_step(x, b);
+            b >>= coarse;
+            if (b < bins) sm_add(sh.hist, b, w);
+            else outside += w;
+          } else {
+            const int b = bin_of(x);
+            if (b < kSmBins) atomicAdd(&sh.hist[0][b], 1u);
+          }
         }
-      }
+      });
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) outside += __shfl_xor_sync(0xffffffffu, outside, o);
       __syncthreads();
@@ -594,36 +745,52 @@ __global__ void __launch_bounds__(kSmThreads, 2) sample_kernel(const __grid_cons
         sh.bin = -1;
       }
       sm_cluster_sync(cluster);
-      u64 here = 0, beyond = 0, all;
+      if (rank == 0) {
+        u64 here[2] = {0, 0}, beyond = 0, all;
 #pragma unroll
-      for (int k = 0; k < kSmMaxCluster; ++k)
-        if (k < cluster) here += sm_peer(&sh.hist[tid], k), beyond += sm_peer(&sh.outside, k);
-      const u64 before = sm_scan(here, sh.scan, all);
-      const double goal = by_weight ? (double)top_p * (double)(all + beyond) : (double)top_k;
-      if (here > 0 && (double)(before + here) >= goal && (before == 0 || (double)before < goal)) {
-        sh.bin = tid;
-        sh.above = before;
+        for (int q = 0; q < 2; ++q) {
+          unsigned part[2][kSmMaxCluster];
+#pragma unroll
+          for (int k = 0; k < kSmMaxCluster; ++k) {
+            part[0][k] = k < cluster ? sm_peer(&sh.hist[0][2 * tid + q], k) : 0u;
+            part[1][k] = by_weight && k < cluster ? sm_peer(&sh.hist[1][2 * tid + q], k) : 0u;
+          }
+#pragma unroll
+          for (int k = 0; k < kSmMaxCluster; ++k) here[q] += part[0][k] + ((u64)part[1][k] << 32);
+        }
+        if (by_weight)
+          for (int k = 0; k < cluster; ++k) beyond += sm_peer(&sh.outside, k);
+        const u64 before = sm_scan(here[0] + here[1], sh.scan, all);
+        const double g = by_weight ? (double)top_p * (double)(all + beyond) : (double)top_k;
+        if (sm_passes(before, here[0] + here[1], g)) {
+          const bool second = !sm_passes(before, here[0], g);
+          sh.bin = 2 * tid + (second ? 1 : 0);
+          sh.above = before + (second ? here[0] : 0ull);
+          sh.goal = g;
+        }
       }
-      __syncthreads();
-      const int bin = sh.bin;
-      const u64 above = sh.above;
-      sm_cluster_sync(cluster);  // (the histograms have been read)
-      sh.hist[tid] = 0;
+      sm_cluster_sync(cluster);
+      const int bin = sm_peer(&sh.bin, 0);
+      const u64 above = sm_peer(&sh.above, 0);
+      const double goal = sm_peer(&sh.goal, 0);
+      for (int q = 0; q < 2; ++q) sh.hist[0][tid + q * kSmThreads] = sh.hist[1][tid + q * kSmThreads] = 0;
       if (bin < 0) continue;     // fewer tokens than top_k; or a sum missed by a rounding: all are kept
       const SmBorder outer = border;
-      auto in_bin = [&](float x, unsigned key, int i) { return bin_of(x) == bin && outer.keeps(key, i); };
       // (a vector without an element of this bin or a nearer one is passed over: what the bin holds is at least this large)
-      const float reach = steps > 0.f ? M - (float)(bin + 2) / steps : -INFINITY;
+      const float reach = by_weight ? __double2float_rd(Md - (double)(((bin + 1) << coarse) + 1) * 0.02166084939249829 * (double)T)  // ln 2 / 32
+                          : steps > 0.f ? M - (float)(bin + 2) / steps : -INFINITY;
+      const float from = by_weight ? fminf(M, __double2float_ru(Md - (double)((bin << coarse) - 2) * 0.02166084939249829 * (double)T)) : steps > 0.f ? fminf(M, M - (float)(bin - 1) / steps) : M;
+      auto in_bin = [&](float x, int i) { return x >= reach && x <= from && bin_of(x) == bin && outer.keeps(x, i); };
       collect(reach, in_bin);
       sm_cluster_sync(cluster);
       if (rank == 0) {
         const unsigned n = merge();
-        if (n <= kSmList) rank_list(n, by_weight ? 0u : (unsigned)((u64)top_k - above), -1.0, above, by_weight ? goal : -1.0);
+        if (n <= kSmList) rank_list(n, by_weight ? n : (unsigned)((u64)top_k - above), -1.0, above, by_weight ? goal : -1.0, from);
         if (tid == 0) sh.verdict = n <= kSmList ? 1 : 0;
       }
       sm_cluster_sync(cluster);
       if (sm_peer(&sh.verdict, 0) != 0) {
-        border.key = sm_peer(&sh.border.key, 0);
+        border.x = sm_peer(&sh.border.x, 0);
         border.index = sm_peer(&sh.border.index, 0);
         sm_cluster_sync(cluster);
         continue;
@@ -633,7 +800,7 @@ __global__ void __launch_bounds__(kSmThreads, 2) sample_kernel(const __grid_cons
       u64 over = above, one = 0;  // what lies above; a token's weight
       unsigned there = 0;         // tokens of the value
       for (int shift = 24; shift >= 0; shift -= 8) {
-        if (tid < 256) sh.radix_count[tid] = 0, sh.radix_weight[tid] = 0;
+        if (tid < 256) sh.radix_count[tid] = sh.radix_weight[0][tid] = sh.radix_weight[1][tid] = 0;
         __syncthreads();
         for (int v = r.v0 + lane; v < r.v1; v += 32) {
           const uint4 w = r.load(v);
@@ -642,30 +809,30 @@ __global__ void __launch_bounds__(kSmThreads, 2) sample_kernel(const __grid_cons
           for (int e = 0; e < E; ++e) {
             const float x = SmRow<X>::at(w, e);
             const unsigned key = sm_key(x);
-            if (!(x > -INFINITY) || !in_bin(x, key, v * E + e - r.skew) || (shift < 24 && (key ^ lo) >> (shift + 8) != 0)) continue;
+            if (!(x > -INFINITY) || !in_bin(x, v * E + e - r.skew) || (shift < 24 && (key ^ lo) >> (shift + 8) != 0)) continue;
             atomicAdd(&sh.radix_count[(key >> shift) & 255u], 1u);
-            if (by_weight) atomicAdd(&sh.radix_weight[(key >> shift) & 255u], weight_of(x));
+            if (by_weight) sm_add(sh.radix_weight, (int)((key >> shift) & 255u), weight_of(x));
           }
         }
         sm_cluster_sync(cluster);
         if (tid < 256) {
           unsigned c = 0;
           u64 s = 0;
-          for (int k = 0; k < cluster; ++k) c += sm_peer(&sh.radix_count[255 - tid], k), s += sm_peer(&sh.radix_weight[255 - tid], k);
+          for (int k = 0; k < cluster; ++k) c += sm_peer(&sh.radix_count[255 - tid], k), s += sm_peer(&sh.radix_weight[0][255 - tid], k) + ((u64)sm_peer(&sh.radix_weight[1][255 - tid], k) << 32);
           sh.merged_count[tid] = c;  // (from the largest digit down)
           sh.merged_weight[tid] = by_weight ? s : (u64)c;
         }
-        if (tid == 0) sh.bin = -1;
+        if (tid == 0) sh.digit = -1;
         sm_cluster_sync(cluster);
         u64 sum;
         const u64 mine = tid < 256 ? sh.merged_weight[tid] : 0, first = sm_scan(mine, sh.scan, sum) + over;
         if (tid < 256 && sh.merged_count[tid] > 0 && (double)(first + mine) >= goal && (first == 0 || (double)first < goal)) {
-          sh.bin = tid;
-          sh.above = first;
+          sh.digit = tid;
+          sh.below = first;
         }
         __syncthreads();
-        at = (unsigned)max(sh.bin, 0);  // (the step's sum reaches the goal, so a digit does)
-        over = sh.above;
+        at = (unsigned)max(sh.digit, 0);  // (the step's sum reaches the goal, so a digit does)
+        over = sh.below;
         there = sh.merged_count[at];
         one = there > 0 ? sh.merged_weight[at] / there : 0;
         lo |= (255u - at) << shift;
@@ -678,8 +845,8 @@ __global__ void __launch_bounds__(kSmThreads, 2) sample_kernel(const __grid_cons
         ties = need <= 1.0 ? 1u : need >= (double)there ? there : (unsigned)need;
       }
       unsigned mine = 0;
-      auto is_tie = [&](float x, int i) { return sm_key(x) == lo && x > -INFINITY && in_bin(x, lo, i); };
       const float lo_x = sm_value(lo);
+      auto is_tie = [&](float x, int i) { return x == lo_x && in_bin(x, i); };
       for (int v = r.v0 + lane; v < r.v1; v += 32) {
         const uint4 w = r.load(v);
         if (!(SmRow<X>::largest(SmRow<X>::more(SmRow<X>::start(), w)) >= lo_x)) continue;
@@ -715,25 +882,27 @@ __global__ void __launch_bounds__(kSmThreads, 2) sample_kernel(const __grid_cons
           }
       }
       sm_cluster_sync(cluster);
-      border.key = lo;
+      border.x = lo_x;
       border.index = -1;
       for (int k = 0; k < cluster; ++k) border.index = max(border.index, sm_peer(&sh.tie_index, k));
       sm_cluster_sync(cluster);
     }
     // ---- the kept weights, warp by warp; the token lies where their running sum passes the target
-    auto kept_weight = [&](float x, int i) {
-      return x > -INFINITY && (double)x >= least_x && border.keeps(sm_key(x), i) ? weight_of(x) : 0ull;
-    };
-    const float reach = fmaxf(border.key ? sm_value(border.key) : -INFINITY, least_x > -1e38 ? (float)least_x - fabsf((float)least_x) * 1e-6f : -INFINITY);
+    if (least_x > border.x) border = SmBorder{least_x, 0x7fffffff};
+    const bool uncut = border.x == -INFINITY;
+    auto kept_weight = [&](float x, int i) { return uncut || border.keeps(x, i) ? weight_of(x) : 0ull; };
     auto sum_of = [&](int v0, int v1) {
       u64 s = 0;
-#pragma unroll 2
-      for (int v = v0 + lane; v < v1; v += 32) {
-        const uint4 w = r.load(v);
-        if (!(SmRow<X>::largest(SmRow<X>::more(SmRow<X>::start(), w)) >= reach)) continue;
+      if (uncut)
+        each_vector(r, v0, v1, [&](int, const uint4& w) {
+#pragma unroll
+          for (int e = 0; e < E; ++e) s += weight_of(SmRow<X>::at(w, e));
+        });
+      else each_vector(r, v0, v1, [&](int v, const uint4& w) {
+        if (!(SmRow<X>::largest(SmRow<X>::more(SmRow<X>::start(), w)) >= border.x)) return;
 #pragma unroll
         for (int e = 0; e < E; ++e) s += kept_weight(SmRow<X>::at(w, e), v * E + e - r.skew);
-      }
+      });
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
       return s;
