@@ -21,6 +21,7 @@
 #include "decode_stream.cuh"
 #include "evict.cuh"
 #include "extend.cuh"
+#include "extend_few.cuh"
 #include "extend_tc.cuh"
 #include "tree.cuh"
 #include "sample.cuh"
@@ -161,6 +162,7 @@ struct dynts_cache {
   bool attr_generic_f32 = false, attr_generic_bf16 = false, attr_generic_kv8 = false, attr_mma = false, attr_select = false;
   bool attr_stream = false, attr_fused = false, attr_prefill = false, attr_extend = false;
   bool attr_extend_tc[2][2] = {{false, false}, {false, false}};
+  bool attr_extend_few[2][2][4] = {};
   bool have_maps = false;    // tensor maps of the K and V slabs for the streaming kernel
   CUtensorMap map_KV;
   bool have_extend_maps = false;  // tensor maps of the K and V slabs for the chunk kernels
@@ -1705,6 +1707,57 @@ dynts_status_t launch_extend_tc(dynts_cache* c, const dynts::ExtendParams& x, co
   return mods ? launch_extend_tc_as<false, true>(c, p, grid, whole, map, want_mass) : launch_extend_tc_as<false, false>(c, p, grid, whole, map, want_mass);
 }
 
+// Whether few query rows go by extend_few_kernel, and the CTAs of a slab's cluster: as many as fit the GPU at once and have four
+// tiles each (by the host's copy of the lengths, which only guides the choice).  A CTA takes 0.42 us per tile of 32 rows for up to 16 query
+// rows, 0.48 for 32, 0.95 for 64 (the chain of a tile; two groups of warps for the first two), and 8 us beside; the
+// storing, tensor-core and joining kernels take 22 us and 0.75 us per tile of 64 rows and CTA.  Measured (us, this kernel / the three): 8 KV heads of 2048 rows, 4 query
+// rows 10 / 21, 20 rows 13 / 22, 48 rows 16.5 / 23; of 16000 rows, 48 query rows 61 / 46; 64 sequences of 1000 to 2111 rows, 4 rows 75 / 81, 16 rows 78 / 85, 32
+// rows 124 / 90; 8 sequences, 32 rows 23 / 27; 33 sequences of 380, 60 rows 44 / 20; 8-bit, 16 sequences of 4200, 14 rows 23 / 41, 63 rows 69 / 47.
+constexpr int kFewCluster = 8, kFewTiles = 4;
+bool plan_few(const dynts_cache* c, const dynts::ExtendParams& x, int rows, int* cluster) {
+  if (rows > dynts::kFewMaxRows) return false;
+  long long slabs = 0, tiles = 0, longest = 0;
+  for (int s = 0; s < x.seqs.n; ++s) {
+    const int t = x.seqs.tok0[s + 1] - x.seqs.tok0[s];
+    if (t == 0) continue;
+    long long n = c->len_h[x.seqs.b0 + s] + t;
+    if (x.window > 0) n = std::min<long long>(n, (long long)x.window + x.sinks + 2 * dynts::kFewKeys);
+    slabs += (long long)x.n_layers * x.Hkv;
+    tiles += (long long)x.n_layers * x.Hkv * ((n + 63) / 64);
+    longest = std::max(longest, (n + dynts::kFewKeys - 1) / dynts::kFewKeys);
+  }
+  const long long slots = (long long)c->sm_count * (rows <= 8 ? 3 : rows <= 16 ? 2 : 1);  // (FewShape::kPerSm)
+  int k = 1;
+  while (k < kFewCluster && 2 * k * slabs <= slots && longest / (2 * k) >= kFewTiles) k *= 2;
+  *cluster = k;
+  const double waves = (double)((slabs * k + slots - 1) / slots);
+  return 8 + (rows <= 16 ? 0.42 : rows <= 32 ? 0.48 : 0.95) * (double)((longest + k - 1) / k) * waves <= 22 + 0.75 * (double)tiles / (2.0 * c->sm_count);
+}
+
+template <bool KV8, bool MODS, int NB, int RG, int KA>
+dynts_status_t launch_extend_few_as(dynts_cache* c, dynts::FewParams& p, bool* attr) {
+  using S = dynts::FewShape<KV8, NB, RG, KA>;
+  auto kernel = dynts::extend_few_kernel<KV8, MODS, NB, RG, KA>;
+  if (!*attr) {
+    CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S::kSmem));
+    *attr = true;
+  }
+  const dynts::ExtendParams& x = p.x;
+  CUDA_TRY(launch_dependent_clusters(kernel, (unsigned)p.cluster, dim3((unsigned)x.seqs.n * (unsigned)p.cluster, (unsigned)(x.n_layers * x.Hkv), 1), (unsigned)S::kThreads,
+                                     S::kSmem, c->stream, p, c->map_KV));
+  c->launches += 1;
+  return DYNTS_OK;
+}
+
+template <bool KV8, bool MODS>
+dynts_status_t launch_extend_few(dynts_cache* c, dynts::FewParams& p, int rows) {
+  bool* attr = c->attr_extend_few[KV8 ? 1 : 0][MODS ? 1 : 0];
+  if (rows <= 8) return launch_extend_few_as<KV8, MODS, 1, 1, 2>(c, p, attr);
+  if (rows <= 16) return launch_extend_few_as<KV8, MODS, 2, 1, 2>(c, p, attr + 1);
+  if (rows <= 32) return launch_extend_few_as<KV8, MODS, 2, 2, 2>(c, p, attr + 2);
+  return launch_extend_few_as<KV8, MODS, 2, 4, 1>(c, p, attr + 3);
+}
+
 dynts_status_t launch_extend(dynts_cache* c, int layer0, int n_layers, const ExtendCall& a, long long total, bool publish) {
   const dynts_config_t& f = c->cfg;
   {
@@ -1779,6 +1832,27 @@ dynts_status_t launch_extend(dynts_cache* c, int layer0, int n_layers, const Ext
     p.seqs.tok0[n_seq] = (int)tok;
     const int n_tok = p.seqs.tok0[n_seq] - p.seqs.tok0[0];
     if (n_tok == 0) continue;
+    if (tc && c->have_maps && !want_mass) {
+      int longest = 0;
+      for (int s = 0; s < n_seq; ++s) longest = std::max(longest, p.seqs.tok0[s + 1] - p.seqs.tok0[s]);
+      const int rows = longest * c->G;
+      int cluster = 1;
+      if (longest <= dynts::kFewMaxRows && plan_few(c, p, rows, &cluster)) {
+        dynts::FewParams q;
+        q.x = p;
+        q.cluster = cluster;
+        q.scale_log2 = (float)(1.4426950408889634 * (double)p.scale);
+        q.out_scale = kv8 ? c->v_scale : 1.f;
+        q.cap_log2 = (float)(1.4426950408889634 * (double)p.cap_logit);
+        q.cap_arg = p.cap_logit > 0.f ? (float)(2.0 * 1.4426950408889634 * (double)p.scale / (double)p.cap_logit) : 0.f;
+        q.wait_limit = c->wait_limit;
+        const bool mods = p.cap_logit > 0.f || p.slopes || p.window > 0 || p.tree;
+        dynts_status_t st = kv8 ? (mods ? launch_extend_few<true, true>(c, q, rows) : launch_extend_few<true, false>(c, q, rows))
+                                : (mods ? launch_extend_few<false, true>(c, q, rows) : launch_extend_few<false, false>(c, q, rows));
+        if (st != DYNTS_OK) return st;
+        continue;
+      }
+    }
     p.n_counters = tc && want_mass ? m.ctas * (kMassParts / 2) : 0;
     // one 16-byte piece of K and of V (and of the rows to clear, and of the queries to copy) per thread, up to a few CTAs per SM
     const long long pieces = f.head_dim * c->elt / 16, ny = (long long)n_layers * f.kv_heads;
