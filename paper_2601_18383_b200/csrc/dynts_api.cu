@@ -161,7 +161,7 @@ struct dynts_cache {
   size_t stage_bytes = 0;
   bool attr_generic_f32 = false, attr_generic_bf16 = false, attr_generic_kv8 = false, attr_mma = false, attr_select = false;
   bool attr_stream = false, attr_fused = false, attr_prefill = false, attr_extend = false;
-  bool attr_extend_tc[2][2] = {{false, false}, {false, false}};
+  bool attr_extend_tc[2][3] = {};
   bool attr_extend_few[2][2][4] = {};
   bool have_maps = false;    // tensor maps of the K and V slabs for the streaming kernel
   CUtensorMap map_KV;
@@ -1560,12 +1560,13 @@ dynts_status_t extend_maps(dynts_cache* c) {
   return DYNTS_OK;
 }
 
-template <bool KV8, bool MODS>
+template <bool KV8, int MODS>
 dynts_status_t launch_extend_tc_as(dynts_cache* c, dynts::ExtendTcParams& p, unsigned grid, bool whole, const CUtensorMap& mq, bool want_mass) {
-  bool* attr = &c->attr_extend_tc[KV8 ? 1 : 0][MODS ? 1 : 0];
+  bool* attr = &c->attr_extend_tc[KV8 ? 1 : 0][MODS];
+  constexpr bool kMassMods = MODS != dynts::kXtPlain;
   if (!*attr) {
     CUDA_TRY(cudaFuncSetAttribute(dynts::extend_tc_kernel<KV8, MODS>, cudaFuncAttributeMaxDynamicSharedMemorySize, dynts::kXtSmemBytes));
-    CUDA_TRY(cudaFuncSetAttribute(dynts::extend_mass_tc_kernel<KV8, MODS>, cudaFuncAttributeMaxDynamicSharedMemorySize, dynts::kXmSmemBytes));
+    CUDA_TRY(cudaFuncSetAttribute(dynts::extend_mass_tc_kernel<KV8, kMassMods>, cudaFuncAttributeMaxDynamicSharedMemorySize, dynts::kXmSmemBytes));
     *attr = true;
   }
   CUDA_TRY(launch_dependent(dynts::extend_tc_kernel<KV8, MODS>, dim3(grid, 1, 1), (unsigned)dynts::XtShape<KV8, MODS>::kThreads, dynts::kXtSmemBytes, c->stream, p, mq, c->map_XK, c->map_XV));
@@ -1575,7 +1576,7 @@ dynts_status_t launch_extend_tc_as(dynts_cache* c, dynts::ExtendTcParams& p, uns
     c->launches += 1;
   }
   if (want_mass) {
-    CUDA_TRY(launch_dependent(dynts::extend_mass_tc_kernel<KV8, MODS>, dim3((unsigned)(2 * c->sm_count), 1, 1), dynts::kXmThreads, dynts::kXmSmemBytes, c->stream, p, mq,
+    CUDA_TRY(launch_dependent(dynts::extend_mass_tc_kernel<KV8, kMassMods>, dim3((unsigned)(2 * c->sm_count), 1, 1), dynts::kXmThreads, dynts::kXmSmemBytes, c->stream, p, mq,
                               c->map_XK));
     c->launches += 1;
   }
@@ -1701,10 +1702,14 @@ dynts_status_t launch_extend_tc(dynts_cache* c, const dynts::ExtendParams& x, co
                                box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   if (r != CUDA_SUCCESS) return fail(DYNTS_ERR_CUDA, "cuTensorMapEncodeTiled failed (%d)", (int)r);
-  const bool mods = x.cap_logit > 0.f || x.slopes || x.window > 0 || x.tree;
-  if (kv8)
-    return mods ? launch_extend_tc_as<true, true>(c, p, grid, whole, map, want_mass) : launch_extend_tc_as<true, false>(c, p, grid, whole, map, want_mass);
-  return mods ? launch_extend_tc_as<false, true>(c, p, grid, whole, map, want_mass) : launch_extend_tc_as<false, false>(c, p, grid, whole, map, want_mass);
+  const bool mods = x.cap_logit > 0.f || x.slopes || x.window > 0;
+  auto launch = [&](auto how) {
+    constexpr int M = decltype(how)::value;
+    return kv8 ? launch_extend_tc_as<true, M>(c, p, grid, whole, map, want_mass) : launch_extend_tc_as<false, M>(c, p, grid, whole, map, want_mass);
+  };
+  if (mods) return launch(std::integral_constant<int, dynts::kXtMods>{});
+  if (x.tree) return launch(std::integral_constant<int, dynts::kXtTree>{});
+  return launch(std::integral_constant<int, dynts::kXtPlain>{});
 }
 
 // Whether few query rows go by extend_few_kernel, and the CTAs of a slab's cluster: as many as fit the GPU at once and have four
@@ -1716,7 +1721,7 @@ dynts_status_t launch_extend_tc(dynts_cache* c, const dynts::ExtendParams& x, co
 constexpr int kFewCluster = 8, kFewTiles = 4;
 bool plan_few(const dynts_cache* c, const dynts::ExtendParams& x, int rows, int* cluster) {
   if (rows > dynts::kFewMaxRows) return false;
-  long long slabs = 0, tiles = 0, longest = 0;
+  long long slabs = 0, tiles = 0, small = 0, longest = 0;  // tiles of 64 and of 32 rows
   for (int s = 0; s < x.seqs.n; ++s) {
     const int t = x.seqs.tok0[s + 1] - x.seqs.tok0[s];
     if (t == 0) continue;
@@ -1724,14 +1729,15 @@ bool plan_few(const dynts_cache* c, const dynts::ExtendParams& x, int rows, int*
     if (x.window > 0) n = std::min<long long>(n, (long long)x.window + x.sinks + 2 * dynts::kFewKeys);
     slabs += (long long)x.n_layers * x.Hkv;
     tiles += (long long)x.n_layers * x.Hkv * ((n + 63) / 64);
+    small += (long long)x.n_layers * x.Hkv * ((n + dynts::kFewKeys - 1) / dynts::kFewKeys);
     longest = std::max(longest, (n + dynts::kFewKeys - 1) / dynts::kFewKeys);
   }
   const long long slots = (long long)c->sm_count * (rows <= 8 ? 3 : rows <= 16 ? 2 : 1);  // (FewShape::kPerSm)
   int k = 1;
   while (k < kFewCluster && 2 * k * slabs <= slots && longest / (2 * k) >= kFewTiles) k *= 2;
   *cluster = k;
-  const double waves = (double)((slabs * k + slots - 1) / slots);
-  return 8 + (rows <= 16 ? 0.42 : rows <= 32 ? 0.48 : 0.95) * (double)((longest + k - 1) / k) * waves <= 22 + 0.75 * (double)tiles / (2.0 * c->sm_count);
+  const double most = std::max((double)((longest + k - 1) / k), (double)small / slots);
+  return 8 + (rows <= 16 ? 0.42 : rows <= 32 ? 0.48 : 0.95) * most <= 22 + 0.75 * (double)tiles / (2.0 * c->sm_count);
 }
 
 template <bool KV8, bool MODS, int NB, int RG, int KA>

@@ -57,13 +57,16 @@
 
 namespace dynts {
 
+// The row arithmetic: plain; with caps, biases, windows (and trees beside them); plain with the mask of a tree in the tiles of the chunk's
+// rows (as part of the second, a tree of 60 in each of 16 sequences behind 4200 8-bit rows took 144 us; see below for the third).
+constexpr int kXtPlain = 0, kXtMods = 1, kXtTree = 2;
 // 8-bit rows, and the plain row arithmetic: two warps of their own load (12 warps, 80 registers per thread).  With caps, biases
 // and windows the row arithmetic needs the registers more: the warps that issue the products load too (10 warps, 96).
 // (Loading warps against none: 4096 behind 4096, plain, 374 us against 455 us; ragged prompts with a bias 109 against 108 us, 1500
 // capped tokens 136 against 133 us.)
-template <bool KV8, bool MODS>
+template <bool KV8, int MODS>
 struct XtShape {
-  static constexpr bool kLoaders = KV8 || !MODS;
+  static constexpr bool kLoaders = KV8 || MODS != kXtMods;
   static constexpr int kThreads = kLoaders ? 384 : 320;
 };
 constexpr int kXtRows = 128;
@@ -537,7 +540,7 @@ __device__ __noinline__ void xt_epilogue(const ExtendTcParams& p, int d, int ord
   if (redone | bad) xt_rows_again<KV8>(p, d, redone, bad, lse, busy);
 }
 
-template <bool KV8, bool MODS>
+template <bool KV8, int MODS>
 __global__ void __launch_bounds__((XtShape<KV8, MODS>::kThreads), 2)
 extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
                  const __grid_constant__ CUtensorMap tmV) {
@@ -557,7 +560,7 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
   const ExtendParams& x = p.x;
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  constexpr bool kLoaders = XtShape<KV8, MODS>::kLoaders;
+  constexpr bool kLoaders = XtShape<KV8, MODS>::kLoaders, kMods = MODS == kXtMods;
   constexpr int kSWarp = kLoaders ? 10 : 8, kOWarp = kSWarp + 1;  // the warps that issue S and O
   if (tid == 0) {
     for (int i = 0; i < 15; ++i) mbar_init(bar(i), i == 7 ? 2 * kXtRows : (i == 8 || i == 9) ? kXtRows : KV8 && (i == 1 || i == 2) ? 2 : 1);
@@ -634,7 +637,7 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
     for (; slot < slot_end && !*s_abort; go_next()) {
       ask_next();
       const int nkt = word(kPwTiles), v_new = word(kPwFirst) + nkt - 1, slab = word(kPwSlab), end = word(kPwHeld) + word(kPwNew);
-      const int sinks = MODS ? word(kPwSinks) : 0, jump = MODS ? word(kPwJump) : 0;
+      const int sinks = kMods ? word(kPwSinks) : 0, jump = kMods ? word(kPwJump) : 0;
       auto tile_row = [&](int v) { return ext_tile_of(v, sinks, jump) * kPfKeys; };
       // 8-bit rows: this warp's 32 rows of a tile, eight at a time, each eight a whole tile ahead in registers
       XtCodes codes[4];
@@ -715,7 +718,7 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
         }
         if (l_slot >= slot_end) return;
         int row = __shfl_sync(0xffffffffu, l_d, kPwFirst) + l_nkt - 1 - l_j;
-        if constexpr (MODS) row = ext_tile_of(row, __shfl_sync(0xffffffffu, l_d, kPwSinks), __shfl_sync(0xffffffffu, l_d, kPwJump));
+        if constexpr (kMods) row = ext_tile_of(row, __shfl_sync(0xffffffffu, l_d, kPwSinks), __shfl_sync(0xffffffffu, l_d, kPwJump));
         row *= kPfKeys;
         ++l_j;
         load_tile(is_s, gl, row, __shfl_sync(0xffffffffu, l_d, kPwSlab));
@@ -820,20 +823,21 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
       // Tiles that some token of the query tile does not see whole, and one more, are the first group's: after them every row
       // that sees anything has its reference.  (With a window a token of a prefix may see only rows around its own: down to those.)
       // (A tree's nodes see the rows held whole, or with a window around their own rows of the chunk.)
-      const bool tree = MODS && x.tree != nullptr;
-      const int whole_to = held + (tree ? (x.window > 0 ? 0 : -1) : MODS && x.window > 0 ? i0 : max(i0 + 1, prefix) - 1);
-      auto tile_row = [&](int v) { return (MODS ? ext_tile_of(v, word(kPwSinks), word(kPwJump)) : v) * kPfKeys; };
+      const bool tree = MODS == kXtTree || (kMods && x.tree != nullptr);
+      const bool placed = kMods && (x.window > 0 || x.slopes != nullptr);  // positions matter
+      const int whole_to = held + (tree ? (kMods && x.window > 0 ? 0 : -1) : kMods && x.window > 0 ? i0 : max(i0 + 1, prefix) - 1);
+      auto tile_row = [&](int v) { return (kMods ? ext_tile_of(v, word(kPwSinks), word(kPwJump)) : v) * kPfKeys; };
       const int ramp = min(nkt, max(0, tile_row(v_new) / kPfKeys - whole_to / kPfKeys) + 1);
       const int* pos_row = nullptr;
       int tot = 0, place = ti, order = 0;  // place: the token's position, the tokens seen not counted
       float slope = 0.f;
-      if constexpr (MODS) {
+      if (tree) {
+        const int4 node = x.tree[word(kPwTok) - i0 + ti];
+        place = node.z;
+        order = node.x;
+      }
+      if constexpr (kMods) {
         tot = word(kPwSeen);
-        if (tree) {
-          const int4 node = x.tree[word(kPwTok) - i0 + ti];
-          place = node.z;
-          order = node.x;
-        }
         pos_row = x.pos + (size_t)word(kPwSlab) * x.cap;
         if (x.slopes) slope = x.slopes[word(kPwHead) * x.G + r % x.G] * 1.4426950408889634f;
       }
@@ -853,13 +857,13 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
         const int g = g0 + j, key0 = tile_row(v_new - j);
         const uint32_t ts = t_row + 64u * (uint32_t)(g & 1);
         int pos_a = 0, pos_b = 0;
-        if constexpr (MODS) {  // positions, the chunk's first token being 0: two per lane
+        if (placed) {  // positions, the chunk's first token being 0: two per lane
           pos_a = pos_row[min(key0 + lane, x.cap - 1)] - tot;
           pos_b = pos_row[min(key0 + 32 + lane, x.cap - 1)] - tot;
         }
         XtCodes vc[2];
         if constexpr (KV8) {  // this warp's 16 rows of V
-          const int older = MODS && j + 4 < nkt ? tile_row(v_new - j - 4) : key0 - 4 * kPfKeys;
+          const int older = kMods && j + 4 < nkt ? tile_row(v_new - j - 4) : key0 - 4 * kPfKeys;
           xt_load_codes(vc[0], v_codes, key0 + 16 * wq, end, lane);
           xt_load_codes(vc[1], v_codes, key0 + 16 * wq + 8, end, lane);
           if (lane == 0 && j + 4 < nkt)
@@ -873,45 +877,50 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
         };
         // 8-bit rows: V goes to its stage while S is computed, once O += P V of tile g - 2 has read it (4096 behind 4096: 550 -> 540 us);
         // with caps, biases and windows after it, as the two waits cost more than they hide (a capped step of 64: 93 against 98 us).
-        if constexpr (KV8 && !MODS) {
+        if constexpr (KV8 && !kMods) {
           if (g >= 2) xt_wait(bar(10 + (g & 1)), (uint32_t)(((g - 2) >> 1) & 1), abort_flag, p);
           widen_v();
         }
         xt_wait(bar(5 + (g & 1)), (uint32_t)((g >> 1) & 1), abort_flag, p);  // S of this tile is complete
         tc5::fence_after_sync();
-        if constexpr (KV8 && MODS) widen_v();  // (S of this tile was issued after O += P V of tile g - 2 had read the stage)
+        if constexpr (KV8 && kMods) widen_v();  // (S of this tile was issued after O += P V of tile g - 2 had read the stage)
         if (live) {
           constexpr int CH = 32;
           bool border = false, beside = false;
           float at = 0.f;                                       // this row's token
           // (the staging tile: positions counted from the tile's newest row, [64] as integers and [64] as floats)
           int me = 0, sink_to = 0;
-          bool branch = false;  // rows of other branches of the tree
-          if constexpr (MODS) {
+          // rows of other branches of the tree, in tiles that hold rows of the chunk
+          const bool fresh = MODS != 0 && key0 + kPfKeys > held, branch = tree && fresh;
+          if (branch) {
+            const int chunk0 = word(kPwTok) - i0, in = end - held;
+            __syncwarp();
+#pragma unroll
+            for (int o = 0; o < kPfKeys; o += 32) {
+              const ExtNode node = ext_node(x, chunk0, key0 + o + lane - held, in);
+              sts_i(stage + 768u + 4u * (uint32_t)(o + lane), node.order);
+              sts_i(stage + 1024u + 4u * (uint32_t)(o + lane), node.size);
+            }
+            __syncwarp();
+          }
+          if constexpr (kMods) {
             // From the newest: a token is at most 64 positions closer to it than to any row it sees, so both terms of a
             // bias are about as small as the bias.  (From the first, which may have survived evictions from far back, a recent
             // row's bias would be the difference of two large products.)
             const int last = min(kPfKeys, end - key0) - 1, p0 = __shfl_sync(0xffffffffu, last < 32 ? pos_a : pos_b, last & 31);
-            __syncwarp();
-            sts_i(stage + 4u * lane, pos_a - p0);
-            sts_i(stage + 128u + 4u * lane, pos_b - p0);
-            sts_f(stage + 256u + 4u * lane, (float)(pos_a - p0));
-            sts_f(stage + 384u + 4u * lane, (float)(pos_b - p0));
             me = place - p0;
             at = (float)me;
             sink_to = x.sinks - tot - p0;
-            const bool fresh = key0 + kPfKeys > held;  // the tile holds rows of the chunk
+            __syncwarp();
             // the tile's first position against the warp's last token (in tiles with rows of the chunk: always compared)
             border = x.window > 0 && (fresh || __reduce_max_sync(0xffffffffu, place) - __shfl_sync(0xffffffffu, pos_a, 0) >= x.window);
-            branch = tree && fresh;
-            if (branch) {
-              const int chunk0 = word(kPwTok) - i0, in = end - held;
-#pragma unroll
-              for (int o = 0; o < kPfKeys; o += 32) {
-                const ExtNode node = ext_node(x, chunk0, key0 + o + lane - held, in);
-                sts_i(stage + 768u + 4u * (uint32_t)(o + lane), node.order);
-                sts_i(stage + 1024u + 4u * (uint32_t)(o + lane), node.size);
-              }
+            if (border) {
+              sts_i(stage + 4u * lane, pos_a - p0);
+              sts_i(stage + 128u + 4u * lane, pos_b - p0);
+            }
+            if (x.slopes) {
+              sts_f(stage + 256u + 4u * lane, (float)(pos_a - p0));
+              sts_f(stage + 384u + 4u * lane, (float)(pos_b - p0));
             }
             beside = fresh && prefix > 0;  // rows of later positions may be visible
             __syncwarp();
@@ -925,7 +934,7 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
             tc5::tmem_ld32(ts + (uint32_t)hb, sv);
             tc5::tmem_wait_ld();
             float scale_log2 = p.scale_log2;  // logits in base-2 units: scaled in the exponent's multiply-add, or with a bias before it
-            if constexpr (MODS) {
+            if constexpr (kMods) {
               if (x.cap_logit > 0.f) scale_log2 = xt_cap(sv, p);
               const float scale = scale_log2;
               if (x.slopes) scale_log2 = 1.f;
@@ -960,15 +969,15 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
                   if (abs(me - y.w) >= x.window && y.w >= sink_to) sv[c + 3] = 0xff800000u;
                 }
               }
-              if (branch) {
+            }
+            if (branch) {
 #pragma unroll
-                for (int c = 0; c < CH; c += 4) {
-                  const int4 y = lds_i4(stage + 768u + 4u * (uint32_t)(hb + c)), z = lds_i4(stage + 1024u + 4u * (uint32_t)(hb + c));
-                  if ((unsigned)(order - y.x) >= (unsigned)z.x) sv[c] = 0xff800000u;
-                  if ((unsigned)(order - y.y) >= (unsigned)z.y) sv[c + 1] = 0xff800000u;
-                  if ((unsigned)(order - y.z) >= (unsigned)z.z) sv[c + 2] = 0xff800000u;
-                  if ((unsigned)(order - y.w) >= (unsigned)z.w) sv[c + 3] = 0xff800000u;
-                }
+              for (int c = 0; c < CH; c += 4) {
+                const int4 y = lds_i4(stage + 768u + 4u * (uint32_t)(hb + c)), z = lds_i4(stage + 1024u + 4u * (uint32_t)(hb + c));
+                if ((unsigned)(order - y.x) >= (unsigned)z.x) sv[c] = 0xff800000u;
+                if ((unsigned)(order - y.y) >= (unsigned)z.y) sv[c + 1] = 0xff800000u;
+                if ((unsigned)(order - y.z) >= (unsigned)z.z) sv[c + 2] = 0xff800000u;
+                if ((unsigned)(order - y.w) >= (unsigned)z.w) sv[c + 3] = 0xff800000u;
               }
             }
             if (in_ramp) {
