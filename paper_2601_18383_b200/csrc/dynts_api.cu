@@ -13,6 +13,7 @@
 #include <cstdlib>
 #include <cstring>
 #include <mutex>
+#include <numeric>
 #include <new>
 #include <vector>
 
@@ -161,7 +162,7 @@ struct dynts_cache {
   size_t stage_bytes = 0;
   bool attr_generic_f32 = false, attr_generic_bf16 = false, attr_generic_kv8 = false, attr_mma = false, attr_select = false;
   bool attr_stream = false, attr_fused = false, attr_prefill = false, attr_extend = false;
-  bool attr_extend_tc[2][3] = {};
+  bool attr_extend_tc[2][4] = {};
   bool attr_extend_few[2][2][4] = {};
   bool have_maps = false;    // tensor maps of the K and V slabs for the streaming kernel
   CUtensorMap map_KV;
@@ -1604,6 +1605,12 @@ dynts_status_t plan_extend(const dynts_cache* c, const dynts::ExtendParams& x, c
   for (int s = 0; s < n_seq; ++s) {
     const int t = x.seqs.tok0[s + 1] - x.seqs.tok0[s];
     p.tiles[s] = (t + tpt - 1) / tpt;
+    p.turn[s] = 0;
+    if (x.window > 0 && p.tiles[s] > 2) {
+      int m = (int)(0.618 * p.tiles[s]);
+      while (std::gcd(m, p.tiles[s]) != 1) ++m;
+      p.turn[s] = m;
+    }
     // The key tiles of an item, on average over the chunk.  (The host's copy of the lengths only guides the cut: the
     // kernels go by the device's.)
     long long rows = c->len_h[x.seqs.b0 + s] + std::max((t + 1) / 2, x.seqs.prefix[s]), full = c->len_h[x.seqs.b0 + s] + t;
@@ -1702,13 +1709,14 @@ dynts_status_t launch_extend_tc(dynts_cache* c, const dynts::ExtendParams& x, co
                                box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   if (r != CUDA_SUCCESS) return fail(DYNTS_ERR_CUDA, "cuTensorMapEncodeTiled failed (%d)", (int)r);
-  const bool mods = x.cap_logit > 0.f || x.slopes || x.window > 0;
+  const bool mods = x.cap_logit > 0.f || x.slopes || (x.window > 0 && x.tree);
   auto launch = [&](auto how) {
     constexpr int M = decltype(how)::value;
     return kv8 ? launch_extend_tc_as<true, M>(c, p, grid, whole, map, want_mass) : launch_extend_tc_as<false, M>(c, p, grid, whole, map, want_mass);
   };
   if (mods) return launch(std::integral_constant<int, dynts::kXtMods>{});
   if (x.tree) return launch(std::integral_constant<int, dynts::kXtTree>{});
+  if (x.window > 0) return launch(std::integral_constant<int, dynts::kXtWindow>{});
   return launch(std::integral_constant<int, dynts::kXtPlain>{});
 }
 

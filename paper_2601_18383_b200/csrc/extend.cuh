@@ -96,6 +96,7 @@ struct ExtendPlan {
   unsigned per[kExtSeqs];      // shares of an item
   int tiles[kExtSeqs];         // tiles of query rows per (layer, KV head)
   int item0[kExtSeqs + 1];     // items before each sequence's
+  int turn[kExtSeqs];          // the order of a sequence's tiles of query rows, see ext_write_plan
   unsigned share_q, share_rem; // shares per CTA: share_q, one more for the first share_rem
   int tokens_per_tile;         // floor(128 / G)
   int lh;                      // n_layers * Hkv
@@ -172,8 +173,10 @@ __device__ __forceinline__ void ext_write_plan(const ExtendParams& p, const Exte
   for (int item = warp; item < q.item0[p.seqs.n]; item += n_warps) {
     const int s = ext_find(q.item0, p.seqs.n, item);
     const int idx = item - q.item0[s], nq = q.tiles[s], lh = idx / nq, o = idx - lh * nq;
-    // tiles from both ends in turn: neighbours in the list hold about as many key tiles together as any other two
-    const int qt = (o & 1) ? nq - 1 - (o >> 1) : o >> 1;
+    // Tiles from both ends in turn: neighbours in the list hold about as many key tiles together as any other two.  With a window, where
+    // the number grows only up to the window's, in steps of 0.62 of the tiles around (prime to them): any run of the list has its
+    // share of early ones (a prompt of 8000 tokens with a window of 4096: 727 -> 652 us).
+    const int qt = q.turn[s] > 0 ? (int)((long long)o * q.turn[s] % nq) : (o & 1) ? nq - 1 - (o >> 1) : o >> 1;
     const int b = p.seqs.b0 + s, t = p.seqs.tok0[s + 1] - p.seqs.tok0[s], n = p.len[b], prefix = p.seqs.prefix[s];
     const int i0 = qt * q.tokens_per_tile, i1 = min(t, i0 + q.tokens_per_tile);
     const bool ok = n >= 0 && n + t <= p.cap;  // (else nothing is stored and nothing computed)

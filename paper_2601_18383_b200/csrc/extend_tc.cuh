@@ -58,8 +58,9 @@
 namespace dynts {
 
 // The row arithmetic: plain; with caps, biases, windows (and trees beside them); plain with the mask of a tree in the tiles of the chunk's
-// rows (as part of the second, a tree of 60 in each of 16 sequences behind 4200 8-bit rows took 144 us; see below for the third).
-constexpr int kXtPlain = 0, kXtMods = 1, kXtTree = 2;
+// rows (trees of 60 in 16 sequences behind 4200 8-bit rows: 144 us as part of the second, 115 so); plain with the mask of a window in the tiles
+// at its borders.
+constexpr int kXtPlain = 0, kXtMods = 1, kXtTree = 2, kXtWindow = 3;
 // 8-bit rows, and the plain row arithmetic: two warps of their own load (12 warps, 80 registers per thread).  With caps, biases
 // and windows the row arithmetic needs the registers more: the warps that issue the products load too (10 warps, 96).
 // (Loading warps against none: 4096 behind 4096, plain, 374 us against 455 us; ragged prompts with a bias 109 against 108 us, 1500
@@ -560,7 +561,7 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
   const ExtendParams& x = p.x;
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  constexpr bool kLoaders = XtShape<KV8, MODS>::kLoaders, kMods = MODS == kXtMods;
+  constexpr bool kLoaders = XtShape<KV8, MODS>::kLoaders, kMods = MODS == kXtMods, kWin = kMods || MODS == kXtWindow;
   constexpr int kSWarp = kLoaders ? 10 : 8, kOWarp = kSWarp + 1;  // the warps that issue S and O
   if (tid == 0) {
     for (int i = 0; i < 15; ++i) mbar_init(bar(i), i == 7 ? 2 * kXtRows : (i == 8 || i == 9) ? kXtRows : KV8 && (i == 1 || i == 2) ? 2 : 1);
@@ -637,7 +638,7 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
     for (; slot < slot_end && !*s_abort; go_next()) {
       ask_next();
       const int nkt = word(kPwTiles), v_new = word(kPwFirst) + nkt - 1, slab = word(kPwSlab), end = word(kPwHeld) + word(kPwNew);
-      const int sinks = kMods ? word(kPwSinks) : 0, jump = kMods ? word(kPwJump) : 0;
+      const int sinks = kWin ? word(kPwSinks) : 0, jump = kWin ? word(kPwJump) : 0;
       auto tile_row = [&](int v) { return ext_tile_of(v, sinks, jump) * kPfKeys; };
       // 8-bit rows: this warp's 32 rows of a tile, eight at a time, each eight a whole tile ahead in registers
       XtCodes codes[4];
@@ -718,7 +719,7 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
         }
         if (l_slot >= slot_end) return;
         int row = __shfl_sync(0xffffffffu, l_d, kPwFirst) + l_nkt - 1 - l_j;
-        if constexpr (kMods) row = ext_tile_of(row, __shfl_sync(0xffffffffu, l_d, kPwSinks), __shfl_sync(0xffffffffu, l_d, kPwJump));
+        if constexpr (kWin) row = ext_tile_of(row, __shfl_sync(0xffffffffu, l_d, kPwSinks), __shfl_sync(0xffffffffu, l_d, kPwJump));
         row *= kPfKeys;
         ++l_j;
         load_tile(is_s, gl, row, __shfl_sync(0xffffffffu, l_d, kPwSlab));
@@ -824,9 +825,9 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
       // that sees anything has its reference.  (With a window a token of a prefix may see only rows around its own: down to those.)
       // (A tree's nodes see the rows held whole, or with a window around their own rows of the chunk.)
       const bool tree = MODS == kXtTree || (kMods && x.tree != nullptr);
-      const bool placed = kMods && (x.window > 0 || x.slopes != nullptr);  // positions matter
-      const int whole_to = held + (tree ? (kMods && x.window > 0 ? 0 : -1) : kMods && x.window > 0 ? i0 : max(i0 + 1, prefix) - 1);
-      auto tile_row = [&](int v) { return (kMods ? ext_tile_of(v, word(kPwSinks), word(kPwJump)) : v) * kPfKeys; };
+      const bool placed = kWin && (x.window > 0 || x.slopes != nullptr);  // positions matter
+      const int whole_to = held + (tree ? (kWin && x.window > 0 ? 0 : -1) : kWin && x.window > 0 ? i0 : max(i0 + 1, prefix) - 1);
+      auto tile_row = [&](int v) { return (kWin ? ext_tile_of(v, word(kPwSinks), word(kPwJump)) : v) * kPfKeys; };
       const int ramp = min(nkt, max(0, tile_row(v_new) / kPfKeys - whole_to / kPfKeys) + 1);
       const int* pos_row = nullptr;
       int tot = 0, place = ti, order = 0;  // place: the token's position, the tokens seen not counted
@@ -836,10 +837,10 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
         place = node.z;
         order = node.x;
       }
-      if constexpr (kMods) {
+      if constexpr (kWin) {
         tot = word(kPwSeen);
         pos_row = x.pos + (size_t)word(kPwSlab) * x.cap;
-        if (x.slopes) slope = x.slopes[word(kPwHead) * x.G + r % x.G] * 1.4426950408889634f;
+        if (kMods && x.slopes) slope = x.slopes[word(kPwHead) * x.G + r % x.G] * 1.4426950408889634f;
       }
       const uint8_t* v_codes = KV8 ? static_cast<const uint8_t*>(x.V) + (size_t)word(kPwSlab) * x.cap * 128 : nullptr;
       const int end = held + word(kPwNew);
@@ -863,7 +864,7 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
         }
         XtCodes vc[2];
         if constexpr (KV8) {  // this warp's 16 rows of V
-          const int older = kMods && j + 4 < nkt ? tile_row(v_new - j - 4) : key0 - 4 * kPfKeys;
+          const int older = kWin && j + 4 < nkt ? tile_row(v_new - j - 4) : key0 - 4 * kPfKeys;
           xt_load_codes(vc[0], v_codes, key0 + 16 * wq, end, lane);
           xt_load_codes(vc[1], v_codes, key0 + 16 * wq + 8, end, lane);
           if (lane == 0 && j + 4 < nkt)
@@ -903,7 +904,7 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
             }
             __syncwarp();
           }
-          if constexpr (kMods) {
+          if constexpr (kWin) {
             // From the newest: a token is at most 64 positions closer to it than to any row it sees, so both terms of a
             // bias are about as small as the bias.  (From the first, which may have survived evictions from far back, a recent
             // row's bias would be the difference of two large products.)
@@ -918,7 +919,7 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
               sts_i(stage + 4u * lane, pos_a - p0);
               sts_i(stage + 128u + 4u * lane, pos_b - p0);
             }
-            if (x.slopes) {
+            if (kMods && x.slopes) {
               sts_f(stage + 256u + 4u * lane, (float)(pos_a - p0));
               sts_f(stage + 384u + 4u * lane, (float)(pos_b - p0));
             }
@@ -959,15 +960,15 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
                   sv[c + 3] = __float_as_uint(x3);
                 }
               }
-              if (border) {
+            }
+            if (border) {
 #pragma unroll
-                for (int c = 0; c < CH; c += 4) {
-                  const int4 y = lds_i4(stage + 4u * (uint32_t)(hb + c));
-                  if (abs(me - y.x) >= x.window && y.x >= sink_to) sv[c] = 0xff800000u;  // -inf
-                  if (abs(me - y.y) >= x.window && y.y >= sink_to) sv[c + 1] = 0xff800000u;
-                  if (abs(me - y.z) >= x.window && y.z >= sink_to) sv[c + 2] = 0xff800000u;
-                  if (abs(me - y.w) >= x.window && y.w >= sink_to) sv[c + 3] = 0xff800000u;
-                }
+              for (int c = 0; c < CH; c += 4) {
+                const int4 y = lds_i4(stage + 4u * (uint32_t)(hb + c));
+                if (abs(me - y.x) >= x.window && y.x >= sink_to) sv[c] = 0xff800000u;  // -inf
+                if (abs(me - y.y) >= x.window && y.y >= sink_to) sv[c + 1] = 0xff800000u;
+                if (abs(me - y.z) >= x.window && y.z >= sink_to) sv[c + 2] = 0xff800000u;
+                if (abs(me - y.w) >= x.window && y.w >= sink_to) sv[c + 3] = 0xff800000u;
               }
             }
             if (branch) {
