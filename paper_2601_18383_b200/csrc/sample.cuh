@@ -39,7 +39,7 @@ constexpr int kSmWarps = kSmThreads / 32;
 constexpr int kSmWarpList = 128;     // tokens a warp can collect
 constexpr int kSmList = 2048;        // tokens the first CTA can merge
 constexpr int kSmMaxCluster = 8;
-constexpr int kSmListK = 768;        // top_k that lists are tried with
+constexpr int kSmListK = 1024;       // top_k that lists are tried with
 constexpr int kSmBins = 2 * kSmThreads;  // steps of a histogram
 constexpr int kSmTable = 16;
 constexpr int kSmGroups = 16;       // of a lane's vectors, whose maxima are kept
@@ -393,7 +393,7 @@ __global__ void __launch_bounds__(kSmThreads, kSmPerSm) sample_kernel(const __gr
   const bool cut_p = top_p < 1.f;
   const double inv_t = 1.0 / (double)fminf(T, 3.0e38f);
   const int share = (top_k + cluster - 1) / cluster;  // of top_k, for each CTA
-  const bool listed = top_k > 0 && top_k <= kSmListK && share <= kSmThreads / 2;
+  const bool listed = top_k > 0 && top_k <= kSmListK;
 
   // ---- every lane's maximum
   float top;
@@ -435,20 +435,25 @@ __global__ void __launch_bounds__(kSmThreads, kSmPerSm) sample_kernel(const __gr
   if (listed && share == 1) {
     cut = top;
   } else if (listed) {
-    // a value that `share` of the lanes' maxima reach, close to the largest such: by a histogram of 512 equal steps
+    // a value that `share` of the groups' maxima reach, close to the largest such: by a histogram of 512 equal steps
     const float steps = top > least ? (kSmThreads - 1) / (top - least) : 0.f;
-    int b = kSmThreads;
-    if (lane_top > -INFINITY) {
-      b = min(kSmThreads - 1, (int)((top - lane_top) * steps));
-      atomicAdd(&sh.hist[0][b], 1u);
+    const int mine = r.v0 + lane < r.v1 ? (r.v1 - r.v0 - lane + 128 * r.rounds - 1) / (128 * r.rounds) : 0;  // this lane's groups
+    auto step_of = [&](float x) { return x > -INFINITY ? min(kSmThreads - 1, max(0, (int)((top - x) * steps))) : kSmThreads; };
+    for (int g = 0; g < mine; ++g) {
+      const int b = step_of(SmRow<X>::largest(sh.group_max[g][tid]));  // (those below the lanes' maxima: the last step)
+      if (b < kSmThreads) atomicAdd(&sh.hist[0][b], 1u);
     }
     u64 all;
     if (tid == 0) sh.bin = kSmThreads;
     const u64 before = (__syncthreads(), sm_scan(sh.hist[0][tid], sh.scan, all)), here = sh.hist[0][tid];
     if (before < (u64)share && before + here >= (u64)share) sh.bin = tid;
     __syncthreads();
-    if (sh.bin < kSmThreads) {  // (fewer lanes hold anything: all is collected)
-      float reach = b <= sh.bin ? lane_top : INFINITY;
+    if (sh.bin < kSmThreads) {  // (fewer groups hold anything: all is collected)
+      float reach = INFINITY;
+      for (int g = 0; g < mine; ++g) {
+        const float x = SmRow<X>::largest(sh.group_max[g][tid]);
+        if (step_of(x) <= sh.bin) reach = fminf(reach, x);
+      }
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) reach = fminf(reach, __shfl_xor_sync(0xffffffffu, reach, o));
       if (lane == 0) sh.warp_min[warp] = reach;
@@ -487,44 +492,55 @@ __global__ void __launch_bounds__(kSmThreads, kSmPerSm) sample_kernel(const __gr
   };
   // The tokens for which wanted(x, index) holds, of vectors whose largest element is at least `reach`: a list per warp.
   auto collect = [&](float reach, auto wanted) {
-    unsigned count = 0;
-    int g = 0, left = r.rounds;
-    for (int vb = r.v0; vb < r.v1; vb += 128) {
-      const bool look = vb + lane < r.v1 && SmRow<X>::largest(sh.group_max[g][tid]) >= reach;
-      if (--left == 0) ++g, left = r.rounds;
-      if (!__any_sync(0xffffffffu, look)) continue;
-      uint4 ws[4];
-      bool any[4];
+    if (lane == 0) sh.warp_count[warp] = 0;
+    __syncwarp();
+    const int step = 128 * r.rounds;
+    unsigned hits = 0;  // a bit for each of the lane's groups
 #pragma unroll
-      for (int q = 0; q < 4; ++q)
-        if (look && vb + 32 * q + lane < r.v1) ws[q] = r.load(vb + 32 * q + lane);
+    for (int g = 0; g < kSmGroups; ++g)
+      if (r.v0 + lane + g * step < r.v1 && SmRow<X>::largest(sh.group_max[g][tid]) >= reach) hits |= 1u << g;
+    for (; hits; hits &= hits - 1) {
+      const int g0 = r.v0 + lane + (__ffs(hits) - 1) * step, g1 = min(r.v1, g0 + step);
+      for (int v = g0; v < g1; v += 128) {
+        uint4 ws[4];
 #pragma unroll
-      for (int q = 0; q < 4; ++q) any[q] = look && vb + 32 * q + lane < r.v1 && SmRow<X>::largest(SmRow<X>::more(SmRow<X>::start(), ws[q])) >= reach;
-      if (!__any_sync(0xffffffffu, any[0] || any[1] || any[2] || any[3])) continue;
+        for (int q = 0; q < 4; ++q)
+          if (v + 32 * q < g1) ws[q] = r.load(v + 32 * q);
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        if (!__any_sync(0xffffffffu, any[q])) continue;
-        const int v = vb + 32 * q + lane;
-        unsigned hits = 0;  // a bit for each of the lane's elements
-        if (any[q]) {
+        for (int q = 0; q < 4; ++q) {
+          if (v + 32 * q >= g1 || !(SmRow<X>::largest(SmRow<X>::more(SmRow<X>::start(), ws[q])) >= reach)) continue;
 #pragma unroll
           for (int e = 0; e < E; ++e) {
             const float x = SmRow<X>::at(ws[q], e);
-            hits |= (x > -INFINITY && wanted(x, v * E + e - r.skew) ? 1u : 0u) << e;
+            const int i = (v + 32 * q) * E + e - r.skew;
+            if (x > -INFINITY && wanted(x, i)) {
+              const unsigned at = atomicAdd(&sh.warp_count[warp], 1u);
+              if (at < kSmWarpList) sh.list[warp][at] = make_uint2(sm_key(x), (unsigned)i);
+            }
           }
         }
-        const unsigned n = __popc(hits), upto = sm_warp_scan(n);
-        unsigned at = count + upto - n;
-#pragma unroll
-        for (int e = 0; e < E; ++e)
-          if ((hits >> e) & 1u) {
-            if (at < kSmWarpList) sh.list[warp][at] = make_uint2(sm_key(SmRow<X>::at(ws[q], e)), (unsigned)(v * E + e - r.skew));
-            ++at;
-          }
-        count += __shfl_sync(0xffffffffu, upto, 31);
       }
     }
-    if (lane == 0) sh.warp_count[warp] = count;
+    __syncwarp();
+    // in the order of the vocabulary: each token's place is the count of those before it
+    const unsigned count = min(sh.warp_count[warp], (unsigned)kSmWarpList);
+    uint2 mine[kSmWarpList / 32];
+    unsigned place[kSmWarpList / 32];
+#pragma unroll
+    for (int q = 0; q < kSmWarpList / 32; ++q) {
+      place[q] = 0;
+      if (32 * q + lane < count) mine[q] = sh.list[warp][32 * q + lane];
+    }
+    for (unsigned j = 0; j < count; ++j) {
+      const unsigned other = sh.list[warp][j].y;
+#pragma unroll
+      for (int q = 0; q < kSmWarpList / 32; ++q)
+        if (32 * q + lane < count && other < mine[q].y) ++place[q];
+    }
+    __syncwarp();
+#pragma unroll
+    for (int q = 0; q < kSmWarpList / 32; ++q)
+      if (32 * q + lane < count) sh.list[warp][place[q]] = mine[q];
   };
   // By the first CTA, behind a barrier: the lists as one, in order, with their weights.  How many; more than kSmList: overflowed.
   auto merge = [&]() -> unsigned {
