@@ -913,8 +913,9 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
             at = (float)me;
             sink_to = x.sinks - tot - p0;
             __syncwarp();
-            // the tile's first position against the warp's last token (in tiles with rows of the chunk: always compared)
-            border = x.window > 0 && (fresh || __reduce_max_sync(0xffffffffu, place) - __shfl_sync(0xffffffffu, pos_a, 0) >= x.window);
+            // The tile's first position against the warp's last token; among the chunk's rows in a tree, or with a prefix, positions may
+            // also lie behind a token's: always compared there.
+            border = x.window > 0 && ((fresh && (tree || prefix > 0)) || __reduce_max_sync(0xffffffffu, place) - __shfl_sync(0xffffffffu, pos_a, 0) >= x.window);
             if (border) {
               sts_i(stage + 4u * lane, pos_a - p0);
               sts_i(stage + 128u + 4u * lane, pos_b - p0);
