@@ -825,7 +825,6 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
       // that sees anything has its reference.  (With a window a token of a prefix may see only rows around its own: down to those.)
       // (A tree's nodes see the rows held whole, or with a window around their own rows of the chunk.)
       const bool tree = MODS == kXtTree || (kMods && x.tree != nullptr);
-      const bool placed = kWin && (x.window > 0 || x.slopes != nullptr);  // positions matter
       const int whole_to = held + (tree ? (kWin && x.window > 0 ? 0 : -1) : kWin && x.window > 0 ? i0 : max(i0 + 1, prefix) - 1);
       auto tile_row = [&](int v) { return (kWin ? ext_tile_of(v, word(kPwSinks), word(kPwJump)) : v) * kPfKeys; };
       const int ramp = min(nkt, max(0, tile_row(v_new) / kPfKeys - whole_to / kPfKeys) + 1);
@@ -846,6 +845,13 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
       const int end = held + word(kPwNew);
       float ref = -CUDART_INF_F, l = 0.f;
       int j = wg == 0 ? 0 : ramp;
+      int last_place = 0, first_pos = 0;
+      if constexpr (kWin) {
+        if (x.window > 0) {
+          last_place = __reduce_max_sync(0xffffffffu, place);
+          if (j < nkt) first_pos = pos_row[tile_row(v_new - j)] - tot;
+        }
+      }
       if (wg == 1) {  // the reference comes from the first group's first tiles
         pair_sync();
         ref = lds_f(smem_u32(s_out) + (uint32_t)(warp ^ 4) * kXtStageBytes + 512u + 4u * lane);  // (of the warp with the same rows)
@@ -857,10 +863,19 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
         const bool in_ramp = j < ramp;
         const int g = g0 + j, key0 = tile_row(v_new - j);
         const uint32_t ts = t_row + 64u * (uint32_t)(g & 1);
+        // A window's border lies in the tile if its first position (asked for a tile ahead) is outside the window of the warp's last
+        // token; among the chunk's rows in a tree, or with a prefix, positions may also lie behind a token's: always compared there.
+        // There, or with a bias, all positions: two per lane, the chunk's first token being 0.
         int pos_a = 0, pos_b = 0;
-        if (placed) {  // positions, the chunk's first token being 0: two per lane
-          pos_a = pos_row[min(key0 + lane, x.cap - 1)] - tot;
-          pos_b = pos_row[min(key0 + 32 + lane, x.cap - 1)] - tot;
+        bool border = false;
+        if constexpr (kWin) {
+          border = x.window > 0 && ((key0 + kPfKeys > held && (tree || prefix > 0)) || last_place - first_pos >= x.window);
+          if (border || (kMods && x.slopes)) {
+            pos_a = pos_row[min(key0 + lane, x.cap - 1)] - tot;
+            pos_b = pos_row[min(key0 + 32 + lane, x.cap - 1)] - tot;
+          }
+          const int next = wg == 1 || j >= ramp ? j + 2 : j + 1 < ramp ? j + 1 : ramp + 1;
+          if (x.window > 0 && next < nkt) first_pos = pos_row[tile_row(v_new - next)] - tot;
         }
         XtCodes vc[2];
         if constexpr (KV8) {  // this warp's 16 rows of V
@@ -887,7 +902,7 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
         if constexpr (KV8 && kMods) widen_v();  // (S of this tile was issued after O += P V of tile g - 2 had read the stage)
         if (live) {
           constexpr int CH = 32;
-          bool border = false, beside = false;
+          bool beside = false;
           float at = 0.f;                                       // this row's token
           // (the staging tile: positions counted from the tile's newest row, [64] as integers and [64] as floats)
           int me = 0, sink_to = 0;
@@ -904,7 +919,7 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
             }
             __syncwarp();
           }
-          if constexpr (kWin) {
+          if (border || (kMods && x.slopes)) {
             // From the newest: a token is at most 64 positions closer to it than to any row it sees, so both terms of a
             // bias are about as small as the bias.  (From the first, which may have survived evictions from far back, a recent
             // row's bias would be the difference of two large products.)
@@ -913,9 +928,6 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
             at = (float)me;
             sink_to = x.sinks - tot - p0;
             __syncwarp();
-            // The tile's first position against the warp's last token; among the chunk's rows in a tree, or with a prefix, positions may
-            // also lie behind a token's: always compared there.
-            border = x.window > 0 && ((fresh && (tree || prefix > 0)) || __reduce_max_sync(0xffffffffu, place) - __shfl_sync(0xffffffffu, pos_a, 0) >= x.window);
             if (border) {
               sts_i(stage + 4u * lane, pos_a - p0);
               sts_i(stage + 128u + 4u * lane, pos_b - p0);
