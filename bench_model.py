@@ -19,6 +19,11 @@ attention-flop ratio.
 model as one chunk (dynts_rope, dynts_extend_attn_layer) behind the rows each arm holds, and the time
 to its first answer token is reported.
 
+`--temperature T` (with `--top-p P`) draws the tokens from given random numbers (dynts_sample) instead of taking the largest
+logit.  `--draft D` adds the check of a drafted tree: a tree of D levels per sequence, grown by the model itself (the two best
+continuations of its last four nodes), goes through the model in one pass (dynts_tree_plan, dynts_extend_attn_ex), a token is
+drawn for every node (dynts_sample), and the path of drawn tokens is taken over (dynts_tree_accept, dynts_extend_commit_path).
+
 `--late-state` instead times 128 steps in the state a 16384-token decode reaches, the caches
 filled with seeded synthetic K/V rows (no trajectory, no evictions falling due).
 
@@ -119,7 +124,24 @@ class Model:
             x = x + (torch.nn.functional.silu(h @ w["wg"].T) * (h @ w["wu"].T)) @ w["wd"].T
         return (self.rms(x.view(Nb, T, HID)[:, -1], self.nf) @ self.head.T).argmax(-1)
 
-    def step(self, tokens, pos, cache, out_buf, attn_events=None):
+    def check(self, tokens, parents, n_new, cache):
+        """Trees of drafted tokens behind what the cache holds: the logits of every node.  The rows are staged."""
+        import paper_2601_18383_b200 as Dn
+        n = tokens.numel()
+        tree, pos = cache.tree_plan(parents, n_new)
+        x = self.embed[tokens]
+        out = torch.empty((n, HQ, D), dtype=torch.bfloat16, device=x.device)
+        for l, w in enumerate(self.layers):
+            h = self.rms(x, w["n1"])
+            q, k, v = ((h @ w[m].T).view(n, -1, D) for m in ("wq", "wk", "wv"))
+            Dn.rope(q, k, pos, q, k, theta=THETA)
+            cache.extend_attn_layer(l, q, k, v, out, n_new, tree=tree, stage=True)
+            x = x + out.view(n, HQ * D) @ w["wo"].T
+            h = self.rms(x, w["n2"])
+            x = x + (torch.nn.functional.silu(h @ w["wg"].T) * (h @ w["wu"].T)) @ w["wd"].T
+        return self.rms(x, self.nf) @ self.head.T
+
+    def step(self, tokens, pos, cache, out_buf, attn_events=None, draw=None):
         Nb = tokens.shape[0]
         x = self.embed[tokens]
         for l, w in enumerate(self.layers):
@@ -138,7 +160,7 @@ class Model:
             h = self.rms(x, w["n2"])
             x = x + (torch.nn.functional.silu(h @ w["wg"].T) * (h @ w["wu"].T)) @ w["wd"].T
         logits = self.rms(x, self.nf) @ self.head.T
-        return logits.argmax(-1)
+        return logits.argmax(-1) if draw is None else draw(logits)
 
 
 def make_cache(batch, rows, budget, window, interval, capacity, device, seed):
@@ -216,14 +238,47 @@ def run_arm(model, cache, batch, start_pos, steps, interval, evict, device):
             "steps_timed": reps * per_graph}
 
 
+def check_draft(model, args, cache, last, u, limited, device):
+    """Grows a tree per sequence with the model itself, checks it in one pass and takes over the drawn path."""
+    import paper_2601_18383_b200 as Dn
+    batch = args.batch
+    tokens, parents, frontier = [last.clone().long()], [-1], [0]     # a node: a token per sequence, a parent
+    pack = lambda: (torch.stack(tokens, 1).reshape(-1), torch.tensor(parents * batch, dtype=torch.int32, device=device), [len(parents)] * batch)
+    for _ in range(args.draft):
+        best = model.check(*pack(), cache).view(batch, len(parents), VOCAB).topk(2, -1).indices
+        grown = []
+        for node in frontier[-4:]:
+            for c in range(2):
+                grown.append(len(parents))
+                parents.append(node)
+                tokens.append(best[:, node, c])
+        frontier = grown
+    flat, up, n_new = pack()
+    chance = u.repeat_interleave(len(parents))
+    held = cache.len(0)
+    a, b = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+    a.record()
+    drawn, _ = Dn.sample(model.check(flat, up, n_new, cache), chance, temperature=args.temperature, top_p=args.top_p)
+    path, accepted, _ = Dn.tree_accept(up, flat.int(), drawn, n_new, args.draft + 1)
+    counts = accepted.tolist()                                       # synchronises
+    cache.extend_commit_path(counts, path)
+    b.record()
+    torch.cuda.synchronize(device)
+    cache.poll_error()
+    assert cache.len(0) == held + counts[0]
+    if limited:
+        cache.evict(0)
+    return {"nodes": len(parents), "accepted": counts, "ms": round(a.elapsed_time(b), 2)}
+
+
 def run_trajectory(model, args, limited, device):
     """One arm of the whole trajectory: prompt through the model, then args.tokens greedy steps."""
     import paper_2601_18383_b200 as Dn
     batch, M, E, B = args.batch, args.prompt, args.interval, args.budget
     if limited:
-        budget, cap = B, B + E + args.turn
+        budget, cap = B, B + E + args.turn + 16 * args.draft
     else:
-        cap = (M + args.tokens + 48 + args.turn + 31) // 32 * 32
+        cap = (M + args.tokens + 48 + args.turn + 16 * args.draft + 31) // 32 * 32
         budget = cap
     cache = Dn.Cache(L, batch, HQ, HKV, D, budget, args.window, E, dtype="bf16", capacity=cap, device=device)
     g = torch.Generator(device=device).manual_seed(11)
@@ -239,8 +294,15 @@ def run_trajectory(model, args, limited, device):
     tokens = first.clone()
     pos = torch.full((batch,), M, device=device, dtype=torch.int64)
 
+    # (drawn tokens: a random number per sequence and step)
+    chance = torch.rand((args.tokens + 1, batch), generator=g, device=device)
+    u = chance[0].clone()
+    draw = None
+    if args.temperature > 0:
+        draw = lambda logits: Dn.sample(logits, u, temperature=args.temperature, top_p=args.top_p)[0]
+
     def model_step():
-        tokens.copy_(model.step(tokens, pos, cache, out_buf))
+        tokens.copy_(model.step(tokens, pos, cache, out_buf, draw=draw))
         pos.add_(1)
 
     model_step()                                   # eager: first-call set-up; the first decoded token
@@ -263,7 +325,9 @@ def run_trajectory(model, args, limited, device):
         n = min(E - done % E, args.tokens - done)
         a, b = ev(), ev()
         a.record()
-        for _ in range(n):
+        for i in range(n):
+            if draw is not None:
+                u.copy_(chance[done + i])
             graph.replay()
         b.record()
         cache.refresh_lengths()                    # synchronises
@@ -300,6 +364,7 @@ def run_trajectory(model, args, limited, device):
         turn = {"tokens": args.turn, "rows_before": int(held), "ms_to_first_token": round(a.elapsed_time(b), 2)}
         if limited:
             cache.evict(0)
+    draft = check_draft(model, args, cache, tokens, u, limited, device) if args.draft else None
     # attention alone at the end of the run: the 32 layer calls of a step on fixed q, k, v
     gq = torch.Generator(device=device).manual_seed(5)
     aq = torch.randn((batch, HQ, D), generator=gq, device=device).to(torch.bfloat16)
@@ -329,6 +394,8 @@ def run_trajectory(model, args, limited, device):
            "evictions": sum(1 for _, r, a2, _ in chunks if a2 < r), "eviction_ms_total": round(evict_ms_total, 3)}
     if turn:
         res["second_question"] = turn
+    if draft:
+        res["drafted_tree"] = draft
     series = [{"step": d, "rows": r, "rows_after_eviction": a2, "ms_per_step": round(ms, 4)} for d, r, a2, ms in chunks]
     cache.close()
     torch.cuda.empty_cache()
@@ -339,7 +406,7 @@ def main_trajectory(args, device):
     model = Model(device)
     res = {"model": "DeepSeek-R1-Distill-Llama-8B shapes, random init, bf16", "batch": args.batch, "prompt": args.prompt,
            "tokens": args.tokens, "budget": args.budget, "window": args.window, "evict_interval": args.interval,
-           "weight_bytes_per_step": model.weight_bytes, "data": "seeded random prompt ids; the model's own greedy tokens"}
+           "weight_bytes_per_step": model.weight_bytes, "data": "seeded random prompt ids; the model's own " + ("greedy" if args.temperature == 0 else "drawn") + " tokens"}
     res["budget_arm"], s_b = run_trajectory(model, args, True, device)
     res["full_kv_arm"], s_f = run_trajectory(model, args, False, device)
     res["speedup"] = round(res["budget_arm"]["tokens_per_s"] / res["full_kv_arm"]["tokens_per_s"], 3)
@@ -364,6 +431,9 @@ def main():
     ap.add_argument("--prompt", type=int, default=256)
     ap.add_argument("--out", default="", help="also write the summary and the per-chunk series to this JSON file")
     ap.add_argument("--turn", type=int, default=0, help="tokens per sequence of a second question after the run (0: none)")
+    ap.add_argument("--temperature", type=float, default=0.0, help="draw the tokens with this temperature (0: the largest logit)")
+    ap.add_argument("--top-p", type=float, default=1.0, help="beside --temperature: share of the weights that is kept")
+    ap.add_argument("--draft", type=int, default=0, help="levels of a drafted tree that is checked after the run (0: none)")
     ap.add_argument("--late-state", action="store_true", help="time --steps steps in the late-decode state on synthetic K/V fills")
     ap.add_argument("--batch", type=int, default=8)
     ap.add_argument("--steps", type=int, default=128)
