@@ -163,7 +163,7 @@ struct dynts_cache {
   bool attr_generic_f32 = false, attr_generic_bf16 = false, attr_generic_kv8 = false, attr_mma = false, attr_select = false;
   bool attr_stream = false, attr_fused = false, attr_prefill = false, attr_extend = false;
   bool attr_extend_tc[2][4] = {};
-  bool attr_extend_few[2][2][4] = {};
+  bool attr_extend_few[2][2][5] = {};
   bool have_maps = false;    // tensor maps of the K and V slabs for the streaming kernel
   CUtensorMap map_KV;
   bool have_extend_maps = false;  // tensor maps of the K and V slabs for the chunk kernels
@@ -1724,7 +1724,7 @@ dynts_status_t launch_extend_tc(dynts_cache* c, const dynts::ExtendParams& x, co
 // tiles each (by the host's copy of the lengths, which only guides the choice).  A CTA takes 0.42 us per tile of 32 rows for up to 16 query
 // rows, 0.48 for 32, 0.95 for 64 (the chain of a tile; two groups of warps for the first two), and 8 us beside; the
 // storing, tensor-core and joining kernels take 22 us and 0.75 us per tile of 64 rows and CTA.  Measured (us, this kernel / the three): 8 KV heads of 2048 rows, 4 query
-// rows 10 / 21, 20 rows 13 / 22, 48 rows 16.5 / 23; of 16000 rows, 48 query rows 61 / 46; 64 sequences of 1000 to 2111 rows, 4 rows 75 / 81, 16 rows 78 / 85, 32
+// rows 10 / 21, 20 rows 13 / 22, 48 rows 16.5 / 23; of 16000 rows, 48 query rows 61 / 46; 64 sequences of 1000 to 2111 rows, 4 rows 72 / 81, 16 rows 78 / 85, 32
 // rows 124 / 90; 8 sequences, 32 rows 23 / 27; 33 sequences of 380, 60 rows 44 / 20; 8-bit, 16 sequences of 4200, 14 rows 23 / 41, 63 rows 69 / 47.
 constexpr int kFewCluster = 8, kFewTiles = 4;
 bool plan_few(const dynts_cache* c, const dynts::ExtendParams& x, int rows, int* cluster) {
@@ -1748,10 +1748,10 @@ bool plan_few(const dynts_cache* c, const dynts::ExtendParams& x, int rows, int*
   return 8 + (rows <= 16 ? 0.42 : rows <= 32 ? 0.48 : 0.95) * most <= 22 + 0.75 * (double)tiles / (2.0 * c->sm_count);
 }
 
-template <bool KV8, bool MODS, int NB, int RG, int KA>
+template <bool KV8, bool MODS, int NB, int RG, int KA, int PS>
 dynts_status_t launch_extend_few_as(dynts_cache* c, dynts::FewParams& p, bool* attr) {
-  using S = dynts::FewShape<KV8, NB, RG, KA>;
-  auto kernel = dynts::extend_few_kernel<KV8, MODS, NB, RG, KA>;
+  using S = dynts::FewShape<KV8, NB, RG, KA, PS>;
+  auto kernel = dynts::extend_few_kernel<KV8, MODS, NB, RG, KA, PS>;
   if (!*attr) {
     CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S::kSmem));
     *attr = true;
@@ -1766,10 +1766,12 @@ dynts_status_t launch_extend_few_as(dynts_cache* c, dynts::FewParams& p, bool* a
 template <bool KV8, bool MODS>
 dynts_status_t launch_extend_few(dynts_cache* c, dynts::FewParams& p, int rows) {
   bool* attr = c->attr_extend_few[KV8 ? 1 : 0][MODS ? 1 : 0];
-  if (rows <= 8) return launch_extend_few_as<KV8, MODS, 1, 1, 2>(c, p, attr);
-  if (rows <= 16) return launch_extend_few_as<KV8, MODS, 2, 1, 2>(c, p, attr + 1);
-  if (rows <= 32) return launch_extend_few_as<KV8, MODS, 2, 2, 2>(c, p, attr + 2);
-  return launch_extend_few_as<KV8, MODS, 2, 4, 1>(c, p, attr + 3);
+  const long long ctas = (long long)p.x.seqs.n * p.cluster * p.x.n_layers * p.x.Hkv;
+  if (rows <= 8 && ctas > 3ll * c->sm_count) return launch_extend_few_as<KV8, MODS, 1, 1, 2, 4>(c, p, attr);
+  if (rows <= 8) return launch_extend_few_as<KV8, MODS, 1, 1, 2, 3>(c, p, attr + 1);
+  if (rows <= 16) return launch_extend_few_as<KV8, MODS, 2, 1, 2, 2>(c, p, attr + 2);
+  if (rows <= 32) return launch_extend_few_as<KV8, MODS, 2, 2, 2, 1>(c, p, attr + 3);
+  return launch_extend_few_as<KV8, MODS, 2, 4, 1, 1>(c, p, attr + 4);
 }
 
 dynts_status_t launch_extend(dynts_cache* c, int layer0, int n_layers, const ExtendCall& a, long long total, bool publish) {

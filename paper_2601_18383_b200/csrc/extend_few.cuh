@@ -30,16 +30,18 @@ namespace dynts {
 constexpr int kFewKeys = 32;          // rows of a tile
 constexpr int kFewMaxRows = 64;
 
-// NB: blocks of 8 query rows per warp; RG: warps that share a run of keys; KA: groups of 2 RG warps that take the tiles in turn.
-template <bool KV8, int NB, int RG, int KA>
+// NB: blocks of 8 query rows per warp; RG: warps that share a run of keys; KA: groups of 2 RG warps that take the tiles in turn; PS: CTAs per SM.
+// One token of 64 sequences, 512 slabs of 1028 rows, four CTAs per SM with two tiles each in flight 49 us, three with four tiles 60 (what does
+// not fit at once comes after the rest); 8 slabs of 2048 rows in clusters of 8 the other way round, 11.7 and 10.1.
+template <bool KV8, int NB, int RG, int KA, int PS>
 struct FewShape {
   static constexpr int kRows = 8 * NB * RG;
   static constexpr int kWarps = 2 * RG * KA;              // consumers
   static constexpr int kThreads = 32 * (kWarps + 1);
   static constexpr int kTileBytes = kFewKeys * 2 * (KV8 ? 128 : 256);
   static constexpr int kPartBytes = kWarps * 8 * NB * 128 * 4;  // over the ring, when it is done
-  static constexpr int kPerSm = kWarps == 8 ? 1 : NB == 2 ? 2 : 3;
-  static constexpr int kStages = (kPerSm == 1 ? 10 : kPerSm == 2 ? 6 : 4) * (KV8 ? 2 : 1);
+  static constexpr int kPerSm = PS;
+  static constexpr int kStages = PS == 1 ? (KV8 ? 20 : 10) : PS == 2 ? (KV8 ? 12 : 6) : PS == 3 ? (KV8 ? 8 : 4) : (KV8 ? 6 : 2);
   static_assert(kStages % KA == 0 && kStages * kTileBytes >= kPartBytes, "a stage is always the same group's, and the parts fit the ring");
   static constexpr int kMlFloats = 2 * kWarps * 8 * NB;   // a warp's maxima and sums
   static constexpr size_t kSmem = (size_t)kStages * kTileBytes + 1024 + kMlFloats * 4 + kRows * 16 + 2 * kStages * 8 + 64;
@@ -130,10 +132,10 @@ __device__ __noinline__ float4 few_row_again(const ExtendParams& x, int s, int l
   return make_float4(acc.x / l, acc.y / l, acc.z / l, acc.w / l);
 }
 
-template <bool KV8, bool MODS, int NB, int RG, int KA>
-__global__ void __launch_bounds__((FewShape<KV8, NB, RG, KA>::kThreads), (FewShape<KV8, NB, RG, KA>::kPerSm))
+template <bool KV8, bool MODS, int NB, int RG, int KA, int PS>
+__global__ void __launch_bounds__((FewShape<KV8, NB, RG, KA, PS>::kThreads), (FewShape<KV8, NB, RG, KA, PS>::kPerSm))
 extend_few_kernel(const __grid_constant__ FewParams p, const __grid_constant__ CUtensorMap map) {
-  using S = FewShape<KV8, NB, RG, KA>;
+  using S = FewShape<KV8, NB, RG, KA, PS>;
   constexpr int NS = S::kStages;
   extern __shared__ __align__(1024) uint8_t few_raw[];
   uint8_t* ring = few_raw + ((1024u - (smem_u32(few_raw) & 1023u)) & 1023u);
