@@ -162,7 +162,7 @@ struct dynts_cache {
   size_t stage_bytes = 0;
   bool attr_generic_f32 = false, attr_generic_bf16 = false, attr_generic_kv8 = false, attr_mma = false, attr_select = false;
   bool attr_stream = false, attr_fused = false, attr_prefill = false, attr_extend = false;
-  bool attr_extend_tc[2][4] = {};
+  bool attr_extend_tc[2][5] = {};
   bool attr_extend_few[2][2][5] = {};
   bool have_maps = false;    // tensor maps of the K and V slabs for the streaming kernel
   CUtensorMap map_KV;
@@ -1528,8 +1528,7 @@ dynts_status_t launch_extend_generic(dynts_cache* c, dynts::ExtendParams& p, boo
   if (want_mass) {
     // grid over the capacity, not over the host's copy of the lengths: a replayed graph may hold longer sequences
     const unsigned nx = (unsigned)((c->cap + dynts::kExtGenericKeys - 1) / dynts::kExtGenericKeys);
-    dynts::extend_generic_mass_kernel<T, KV8><<<dim3(nx, ny, (unsigned)n_seq), dynts::kExtGenericThreads, smem_m, c->stream>>>(p);
-    CUDA_TRY(cudaGetLastError());
+    CUDA_TRY(launch_dependent(dynts::extend_generic_mass_kernel<T, KV8>, dim3(nx, ny, (unsigned)n_seq), dynts::kExtGenericThreads, smem_m, c->stream, p));
     c->launches += 1;
   }
   return DYNTS_OK;
@@ -1606,7 +1605,7 @@ dynts_status_t plan_extend(const dynts_cache* c, const dynts::ExtendParams& x, c
     const int t = x.seqs.tok0[s + 1] - x.seqs.tok0[s];
     p.tiles[s] = (t + tpt - 1) / tpt;
     p.turn[s] = 0;
-    if (x.window > 0 && p.tiles[s] > 2) {
+    if (x.window > 0 && p.tiles[s] > 2 && p.tiles[s] < 65536) {  // (a place in the list times the step stays below 2^32)
       int m = (int)(0.618 * p.tiles[s]);
       while (std::gcd(m, p.tiles[s]) != 1) ++m;
       p.turn[s] = m;
@@ -1714,6 +1713,7 @@ dynts_status_t launch_extend_tc(dynts_cache* c, const dynts::ExtendParams& x, co
     constexpr int M = decltype(how)::value;
     return kv8 ? launch_extend_tc_as<true, M>(c, p, grid, whole, map, want_mass) : launch_extend_tc_as<false, M>(c, p, grid, whole, map, want_mass);
   };
+  if (mods && (x.tree || x.sinks > 0)) return launch(std::integral_constant<int, dynts::kXtAll>{});
   if (mods) return launch(std::integral_constant<int, dynts::kXtMods>{});
   if (x.tree) return launch(std::integral_constant<int, dynts::kXtTree>{});
   if (x.window > 0) return launch(std::integral_constant<int, dynts::kXtWindow>{});

@@ -95,8 +95,8 @@ struct ExtendPlan {
   unsigned cum[kExtSeqs + 1];  // shares before each sequence's first item
   unsigned per[kExtSeqs];      // shares of an item
   int tiles[kExtSeqs];         // tiles of query rows per (layer, KV head)
-  int item0[kExtSeqs + 1];     // items before each sequence's
   int turn[kExtSeqs];          // the order of a sequence's tiles of query rows, see ext_write_plan
+  int item0[kExtSeqs + 1];     // items before each sequence's
   unsigned share_q, share_rem; // shares per CTA: share_q, one more for the first share_rem
   int tokens_per_tile;         // floor(128 / G)
   int lh;                      // n_layers * Hkv
@@ -176,7 +176,7 @@ __device__ __forceinline__ void ext_write_plan(const ExtendParams& p, const Exte
     // Tiles from both ends in turn: neighbours in the list hold about as many key tiles together as any other two.  With a window, where
     // the number grows only up to the window's, in steps of 0.62 of the tiles around (prime to them): any run of the list has its
     // share of early ones (a prompt of 8000 tokens with a window of 4096: 727 -> 652 us).
-    const int qt = q.turn[s] > 0 ? (int)((long long)o * q.turn[s] % nq) : (o & 1) ? nq - 1 - (o >> 1) : o >> 1;
+    const int qt = q.turn[s] > 0 ? (int)((unsigned)o * (unsigned)q.turn[s] % (unsigned)nq) : (o & 1) ? nq - 1 - (o >> 1) : o >> 1;
     const int b = p.seqs.b0 + s, t = p.seqs.tok0[s + 1] - p.seqs.tok0[s], n = p.len[b], prefix = p.seqs.prefix[s];
     const int i0 = qt * q.tokens_per_tile, i1 = min(t, i0 + q.tokens_per_tile);
     const bool ok = n >= 0 && n + t <= p.cap;  // (else nothing is stored and nothing computed)
@@ -437,6 +437,7 @@ __global__ void __launch_bounds__(kExtGenericThreads) extend_generic_kernel(cons
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int item = (int)blockIdx.x / cluster, rank = (int)blockIdx.x - item * cluster;
   const unsigned piece_inv = 65536u / (unsigned)pieces + 1u;  // x / pieces = (x * piece_inv) >> 16 for x < 256 and up to 64 pieces
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const int s = ext_find(p.seqs.item0, p.seqs.n, item);
   const ExtSeq e = ext_seq(p, s);
@@ -637,6 +638,7 @@ __global__ void __launch_bounds__(kExtGenericThreads) extend_generic_mass_kernel
   float* sS = sQ + kExtGenericRows * d;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const unsigned piece_inv = 65536u / (unsigned)pieces + 1u;  // x / pieces = (x * piece_inv) >> 16 for x < 256 and up to 64 pieces
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const int layer = blockIdx.y / p.Hkv, h = blockIdx.y % p.Hkv, s = blockIdx.z;
   const ExtSeq e = ext_seq(p, s);

@@ -57,17 +57,18 @@
 
 namespace dynts {
 
-// The row arithmetic: plain; with caps, biases, windows (and trees beside them); plain with the mask of a tree in the tiles of the chunk's
+// The row arithmetic: plain; with caps, biases and windows, and the same with trees and sinks (ragged prompts with a bias, where neither is there:
+// 110 us without, 119 with); plain with the mask of a tree in the tiles of the chunk's
 // rows (trees of 60 in 16 sequences behind 4200 8-bit rows: 144 us as part of the second, 115 so); plain with the mask of a window in the tiles
 // at its borders.
-constexpr int kXtPlain = 0, kXtMods = 1, kXtTree = 2, kXtWindow = 3;
+constexpr int kXtPlain = 0, kXtMods = 1, kXtTree = 2, kXtWindow = 3, kXtAll = 4;
 // 8-bit rows, and the plain row arithmetic: two warps of their own load (12 warps, 80 registers per thread).  With caps, biases
 // and windows the row arithmetic needs the registers more: the warps that issue the products load too (10 warps, 96).
 // (Loading warps against none: 4096 behind 4096, plain, 374 us against 455 us; ragged prompts with a bias 109 against 108 us, 1500
 // capped tokens 136 against 133 us.)
 template <bool KV8, int MODS>
 struct XtShape {
-  static constexpr bool kLoaders = KV8 || MODS != kXtMods;
+  static constexpr bool kLoaders = KV8 || (MODS != kXtMods && MODS != kXtAll);
   static constexpr int kThreads = kLoaders ? 384 : 320;
 };
 constexpr int kXtRows = 128;
@@ -561,7 +562,7 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
   const ExtendParams& x = p.x;
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  constexpr bool kLoaders = XtShape<KV8, MODS>::kLoaders, kMods = MODS == kXtMods, kWin = kMods || MODS == kXtWindow;
+  constexpr bool kLoaders = XtShape<KV8, MODS>::kLoaders, kMods = MODS == kXtMods || MODS == kXtAll, kWin = kMods || MODS == kXtWindow, kSinks = kWin && MODS != kXtMods;
   constexpr int kSWarp = kLoaders ? 10 : 8, kOWarp = kSWarp + 1;  // the warps that issue S and O
   if (tid == 0) {
     for (int i = 0; i < 15; ++i) mbar_init(bar(i), i == 7 ? 2 * kXtRows : (i == 8 || i == 9) ? kXtRows : KV8 && (i == 1 || i == 2) ? 2 : 1);
@@ -637,9 +638,10 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
     int g = 0;
     for (; slot < slot_end && !*s_abort; go_next()) {
       ask_next();
-      const int nkt = word(kPwTiles), v_new = word(kPwFirst) + nkt - 1, slab = word(kPwSlab), end = word(kPwHeld) + word(kPwNew);
-      const int sinks = kWin ? word(kPwSinks) : 0, jump = kWin ? word(kPwJump) : 0;
-      auto tile_row = [&](int v) { return ext_tile_of(v, sinks, jump) * kPfKeys; };
+      const int nkt = word(kPwTiles), slab = word(kPwSlab), end = word(kPwHeld) + word(kPwNew);
+      // (without sinks the tiles are one run, counted from its first)
+      const int v_new = word(kPwFirst) + nkt - 1 + (kWin && !kSinks ? word(kPwJump) : 0), sinks = kSinks ? word(kPwSinks) : 0, jump = kSinks ? word(kPwJump) : 0;
+      auto tile_row = [&](int v) { return (kSinks ? ext_tile_of(v, sinks, jump) : v) * kPfKeys; };
       // 8-bit rows: this warp's 32 rows of a tile, eight at a time, each eight a whole tile ahead in registers
       XtCodes codes[4];
       const uint8_t* src = KV8 ? static_cast<const uint8_t*>(x.K) + (size_t)slab * x.cap * 128 : nullptr;
@@ -719,7 +721,8 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
         }
         if (l_slot >= slot_end) return;
         int row = __shfl_sync(0xffffffffu, l_d, kPwFirst) + l_nkt - 1 - l_j;
-        if constexpr (kWin) row = ext_tile_of(row, __shfl_sync(0xffffffffu, l_d, kPwSinks), __shfl_sync(0xffffffffu, l_d, kPwJump));
+        if constexpr (kSinks) row = ext_tile_of(row, __shfl_sync(0xffffffffu, l_d, kPwSinks), __shfl_sync(0xffffffffu, l_d, kPwJump));
+        else if constexpr (kWin) row += __shfl_sync(0xffffffffu, l_d, kPwJump);
         row *= kPfKeys;
         ++l_j;
         load_tile(is_s, gl, row, __shfl_sync(0xffffffffu, l_d, kPwSlab));
@@ -815,7 +818,7 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
       ask_next();
       const int nkt = word(kPwTiles);
       if (nkt == 0) continue;
-      const int v_new = word(kPwFirst) + nkt - 1;  // its newest tile
+      const int v_new = word(kPwFirst) + nkt - 1 + (kWin && !kSinks ? word(kPwJump) : 0);  // its newest tile
       const int rows = word(kPwRows), held = word(kPwHeld), i0 = word(kPwTok0), prefix = word(kPwPrefix);
       const bool live = wq * 32 < rows;
       const int r = min(wq * 32 + lane, rows - 1);  // (a lane without a query repeats the last row's visibility)
@@ -824,9 +827,10 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
       // Tiles that some token of the query tile does not see whole, and one more, are the first group's: after them every row
       // that sees anything has its reference.  (With a window a token of a prefix may see only rows around its own: down to those.)
       // (A tree's nodes see the rows held whole, or with a window around their own rows of the chunk.)
-      const bool tree = MODS == kXtTree || (kMods && x.tree != nullptr);
+      const bool tree = MODS == kXtTree || (MODS == kXtAll && x.tree != nullptr);
+      const bool placed = kMods && (x.window > 0 || x.slopes != nullptr);  // positions matter
       const int whole_to = held + (tree ? (kWin && x.window > 0 ? 0 : -1) : kWin && x.window > 0 ? i0 : max(i0 + 1, prefix) - 1);
-      auto tile_row = [&](int v) { return (kWin ? ext_tile_of(v, word(kPwSinks), word(kPwJump)) : v) * kPfKeys; };
+      auto tile_row = [&](int v) { return (kSinks ? ext_tile_of(v, word(kPwSinks), word(kPwJump)) : v) * kPfKeys; };
       const int ramp = min(nkt, max(0, tile_row(v_new) / kPfKeys - whole_to / kPfKeys) + 1);
       const int* pos_row = nullptr;
       int tot = 0, place = ti, order = 0;  // place: the token's position, the tokens seen not counted
@@ -846,11 +850,9 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
       float ref = -CUDART_INF_F, l = 0.f;
       int j = wg == 0 ? 0 : ramp;
       int last_place = 0, first_pos = 0;
-      if constexpr (kWin) {
-        if (x.window > 0) {
-          last_place = __reduce_max_sync(0xffffffffu, place);
-          if (j < nkt) first_pos = pos_row[tile_row(v_new - j)] - tot;
-        }
+      if constexpr (MODS == kXtWindow) {
+        last_place = __shfl_sync(0xffffffffu, ti, 31);
+        if (j < nkt) first_pos = pos_row[tile_row(v_new - j)] - tot;
       }
       if (wg == 1) {  // the reference comes from the first group's first tiles
         pair_sync();
@@ -863,19 +865,19 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
         const bool in_ramp = j < ramp;
         const int g = g0 + j, key0 = tile_row(v_new - j);
         const uint32_t ts = t_row + 64u * (uint32_t)(g & 1);
-        // A window's border lies in the tile if its first position (asked for a tile ahead) is outside the window of the warp's last
-        // token; among the chunk's rows in a tree, or with a prefix, positions may also lie behind a token's: always compared there.
-        // There, or with a bias, all positions: two per lane, the chunk's first token being 0.
+        // Positions, the chunk's first token being 0: two per lane.  A window's border lies in the tile if its first position is outside the
+        // window of the warp's last token; among the chunk's rows in a tree, or with a prefix, positions may also lie behind a
+        // token's: always compared there.  With a window alone the first is asked for a tile ahead, the others only at a border.
         int pos_a = 0, pos_b = 0;
         bool border = false;
-        if constexpr (kWin) {
-          border = x.window > 0 && ((key0 + kPfKeys > held && (tree || prefix > 0)) || last_place - first_pos >= x.window);
-          if (border || (kMods && x.slopes)) {
-            pos_a = pos_row[min(key0 + lane, x.cap - 1)] - tot;
-            pos_b = pos_row[min(key0 + 32 + lane, x.cap - 1)] - tot;
-          }
+        if constexpr (MODS == kXtWindow) border = (key0 + kPfKeys > held && prefix > 0) || last_place - first_pos >= x.window;
+        if (placed || border) {
+          pos_a = pos_row[min(key0 + lane, x.cap - 1)] - tot;
+          pos_b = pos_row[min(key0 + 32 + lane, x.cap - 1)] - tot;
+        }
+        if constexpr (MODS == kXtWindow) {
           const int next = wg == 1 || j >= ramp ? j + 2 : j + 1 < ramp ? j + 1 : ramp + 1;
-          if (x.window > 0 && next < nkt) first_pos = pos_row[tile_row(v_new - next)] - tot;
+          if (next < nkt) first_pos = pos_row[tile_row(v_new - next)] - tot;
         }
         XtCodes vc[2];
         if constexpr (KV8) {  // this warp's 16 rows of V
@@ -907,7 +909,7 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
           // (the staging tile: positions counted from the tile's newest row, [64] as integers and [64] as floats)
           int me = 0, sink_to = 0;
           // rows of other branches of the tree, in tiles that hold rows of the chunk
-          const bool fresh = MODS != 0 && key0 + kPfKeys > held, branch = tree && fresh;
+          const bool fresh = MODS != kXtPlain && key0 + kPfKeys > held, branch = tree && fresh;
           if (branch) {
             const int chunk0 = word(kPwTok) - i0, in = end - held;
             __syncwarp();
@@ -919,7 +921,7 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
             }
             __syncwarp();
           }
-          if (border || (kMods && x.slopes)) {
+          if (kMods || border) {
             // From the newest: a token is at most 64 positions closer to it than to any row it sees, so both terms of a
             // bias are about as small as the bias.  (From the first, which may have survived evictions from far back, a recent
             // row's bias would be the difference of two large products.)
@@ -928,6 +930,9 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
             at = (float)me;
             sink_to = x.sinks - tot - p0;
             __syncwarp();
+            if constexpr (kMods)
+              border = x.window > 0 && ((fresh && (tree || prefix > 0)) ||
+                                        (MODS == kXtAll ? __reduce_max_sync(0xffffffffu, place) : __shfl_sync(0xffffffffu, ti, 31)) - __shfl_sync(0xffffffffu, pos_a, 0) >= x.window);
             if (border) {
               sts_i(stage + 4u * lane, pos_a - p0);
               sts_i(stage + 128u + 4u * lane, pos_b - p0);
