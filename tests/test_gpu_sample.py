@@ -173,3 +173,28 @@ def test_shares_of_many_draws():
     tokens, _ = D.sample(x, u)
     share = torch.bincount(tokens.cpu().long(), minlength=5) / n
     assert ((share - p).abs() <= 5 * (p * (1 - p) / n).sqrt()).all()
+
+
+@pytest.mark.parametrize("top_p", [0.99999, 1 - 2.0 ** -23, 1 - 2.0 ** -24, 1e-7, 1e-38])
+def test_top_p_near_its_ends(top_p):
+    for n, V, dtype in ((4, 128256, torch.float32), (70, 9001, torch.bfloat16)):
+        x, u = logits(n, V, dtype, 21)
+        check(x, u, top_p=top_p)
+        check(x, u, 1.7, top_k=1500, top_p=top_p)
+        check(x, u, 0.7, top_k=20, top_p=top_p)
+
+
+def test_two_streams_at_once():
+    """Rows of two calls in flight together; no workspace is shared."""
+    sets = [logits(40, 50021, torch.float32, 31), logits(3, 128256, torch.bfloat16, 32)]
+    alone = [D.sample(x, u, 0.9, 0, 0.95) for x, u in sets]
+    streams = [torch.cuda.Stream() for _ in sets]
+    out = []
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for s, (x, u) in zip(streams, sets):
+            with torch.cuda.stream(s):
+                out.append(D.sample(x, u, 0.9, 0, 0.95))
+    torch.cuda.synchronize()
+    for i, (tokens, logprobs) in enumerate(out):
+        assert torch.equal(tokens, alone[i % 2][0]) and torch.equal(logprobs, alone[i % 2][1])
