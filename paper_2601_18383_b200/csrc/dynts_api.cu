@@ -1528,7 +1528,13 @@ dynts_status_t launch_extend_generic(dynts_cache* c, dynts::ExtendParams& p, boo
   if (want_mass) {
     // grid over the capacity, not over the host's copy of the lengths: a replayed graph may hold longer sequences
     const unsigned nx = (unsigned)((c->cap + dynts::kExtGenericKeys - 1) / dynts::kExtGenericKeys);
-    CUDA_TRY(launch_dependent(dynts::extend_generic_mass_kernel<T, KV8>, dim3(nx, ny, (unsigned)n_seq), dynts::kExtGenericThreads, smem_m, c->stream, p));
+    // Clusters while their CTAs stay below two per SM (those behind the rows held end at once) and each has query rows to take.
+    int longest_t = 0;
+    for (int s = 0; s < n_seq; ++s) longest_t = std::max(longest_t, p.seqs.tok0[s + 1] - p.seqs.tok0[s]);
+    unsigned share = 1;
+    while (share < 8 && (long long)nx * ny * n_seq * share * 2 <= 2ll * c->sm_count && (long long)longest_t * c->G > (long long)share * dynts::kExtGenericRows) share *= 2;
+    CUDA_TRY(launch_dependent_clusters(dynts::extend_generic_mass_kernel<T, KV8>, share, dim3(nx * share, ny, (unsigned)n_seq), dynts::kExtGenericThreads, smem_m, c->stream, p,
+                                       (int)share));
     c->launches += 1;
   }
   return DYNTS_OK;

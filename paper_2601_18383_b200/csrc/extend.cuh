@@ -628,9 +628,11 @@ constexpr size_t ext_generic_mass_smem(int d) {  // K [32][d + 4], four query ro
 
 // mass_j = sum over the chunk's tokens and the group's heads of the weight of row j, from the logits and each query
 // row's log-sum-exp.  CTA = 32 rows of one slab; the warps take the query rows in turn, four at once (one read of
-// K for four products), lane = key; the eight partial sums are added in a fixed order.
+// K for four products), lane = key; the eight partial sums are added in a fixed order.  Small calls take a cluster of CTAs per 32 rows,
+// which share the query rows out and add their sums up in the order of the ranks (164 query rows of 64 columns against 172 rows: 18 us
+// without, 6.5 with eight CTAs).
 template <typename T, bool KV8>
-__global__ void __launch_bounds__(kExtGenericThreads) extend_generic_mass_kernel(const __grid_constant__ ExtendParams p) {
+__global__ void __launch_bounds__(kExtGenericThreads) extend_generic_mass_kernel(const __grid_constant__ ExtendParams p, const int cluster) {
   extern __shared__ __align__(16) float ext_sm[];
   const int d = p.d, ldk = d + 4, pieces = d / 4;
   float* sK = ext_sm;
@@ -642,8 +644,9 @@ __global__ void __launch_bounds__(kExtGenericThreads) extend_generic_mass_kernel
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const int layer = blockIdx.y / p.Hkv, h = blockIdx.y % p.Hkv, s = blockIdx.z;
   const ExtSeq e = ext_seq(p, s);
-  const int k0 = blockIdx.x * kExtGenericKeys;
-  if (!e.ok || e.t == 0 || k0 >= e.n + e.t) return;
+  const int tile = (int)blockIdx.x / cluster, rank = (int)blockIdx.x - tile * cluster;
+  const int k0 = tile * kExtGenericKeys;
+  if (!e.ok || e.t == 0 || k0 >= e.n + e.t) return;  // (the same in the whole cluster)
   const size_t tok_base = (size_t)layer * p.total + p.seqs.tok0[s];
   const size_t slab = ((size_t)(p.layer0 + layer) * p.Nb + e.b) * p.Hkv + h;
   const float* lse = p.lse + ext_lse_index(p, layer, h, p.seqs.tok0[s]);
@@ -662,7 +665,15 @@ __global__ void __launch_bounds__(kExtGenericThreads) extend_generic_mass_kernel
   const int first = e.n + prefix > k0 ? 0 : max(0, k0 - e.n) * p.G;
   float* q4 = sQ + warp * 4 * d;
   float sum = 0.f;
-  for (int r = first + 4 * warp; r < all; r += kExtGenericRows) {
+  for (int r = first + rank * kExtGenericRows + 4 * warp; r < all; r += cluster * kExtGenericRows) {
+    float log_sum[4];
+    ExtNode node[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {  // (asked for before the products)
+      const int qr = min(r + u, all - 1);
+      log_sum[u] = lse[qr];
+      node[u] = ext_node(p, p.seqs.tok0[s], qr / p.G, e.t);
+    }
     __syncwarp();
 #pragma unroll 2
     for (int x = lane; x < 4 * pieces; x += 32) {
@@ -685,20 +696,30 @@ __global__ void __launch_bounds__(kExtGenericThreads) extend_generic_mass_kernel
     for (int u = 0; u < 4; ++u) {
       if (r + u >= all) break;
       const int i = (r + u) / p.G, head = h * p.G + r + u - i * p.G;
-      const ExtNode node = ext_node(p, p.seqs.tok0[s], i, e.t);
-      const int apart = abs(e.tot + node.depth - pj);
-      if (j < e.n + max(i + 1, prefix) && ext_in_window(p, apart, pj) && ext_below(node.order, row))
-        sum += exp2f(ext_logit_exact(p, dot[u], p.slopes ? p.slopes[head] : 0.f, apart) - lse[r + u]);
+      const int apart = abs(e.tot + node[u].depth - pj);
+      if (j < e.n + max(i + 1, prefix) && ext_in_window(p, apart, pj) && ext_below(node[u].order, row))
+        sum += exp2f(ext_logit_exact(p, dot[u], p.slopes ? p.slopes[head] : 0.f, apart) - log_sum[u]);
     }
   }
   sS[warp * kExtGenericKeys + lane] = sum;
   __syncthreads();
-  if (warp == 0 && j < e.n + e.t) {
-    float x = 0.f;
+  float x = 0.f;
+  if (warp == 0) {
 #pragma unroll
     for (int w = 0; w < kExtWarps; ++w) x += sS[w * kExtGenericKeys + lane];
-    ext_emit_mass(p, slab * p.cap + j, x);
   }
+  if (cluster > 1) {
+    if (warp == 0) sS[lane] = x;
+    __syncwarp();
+    cluster_arrive();
+    cluster_wait();
+    if (rank == 0 && warp == 0)
+      for (int k = 1; k < cluster; ++k) x += ext_peer_float(sS + lane, k);
+    __syncwarp();
+    cluster_arrive();  // (no CTA ends while another reads from it)
+    cluster_wait();
+  }
+  if (rank == 0 && warp == 0 && j < e.n + e.t) ext_emit_mass(p, slab * p.cap + j, x);
 }
 
 }  // namespace dynts
