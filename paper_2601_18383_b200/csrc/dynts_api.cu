@@ -1726,14 +1726,15 @@ dynts_status_t launch_extend_tc(dynts_cache* c, const dynts::ExtendParams& x, co
   return launch(std::integral_constant<int, dynts::kXtPlain>{});
 }
 
-// Whether few query rows go by extend_few_kernel, and the CTAs of a slab's cluster: as many as fit the GPU at once and have four
-// tiles each (by the host's copy of the lengths, which only guides the choice).  A CTA takes 0.42 us per tile of 32 rows for up to 16 query
-// rows, 0.48 for 32, 0.95 for 64 (the chain of a tile; two groups of warps for the first two), and 8 us beside; the
-// storing, tensor-core and joining kernels take 22 us and 0.75 us per tile of 64 rows and CTA.  Measured (us, this kernel / the three): 8 KV heads of 2048 rows, 4 query
-// rows 10 / 21, 20 rows 13 / 22, 48 rows 16.5 / 23; of 16000 rows, 48 query rows 61 / 46; 64 sequences of 1000 to 2111 rows, 4 rows 72 / 81, 16 rows 78 / 85, 32
-// rows 124 / 90; 8 sequences, 32 rows 23 / 27; 33 sequences of 380, 60 rows 44 / 20; 8-bit, 16 sequences of 4200, 14 rows 23 / 41, 63 rows 69 / 47.
+// Whether few query rows go by extend_few_kernel, in how many clusters per slab (`split`, 32 query rows each), and the CTAs of a cluster: as many
+// as fit the GPU at once and have four tiles each (by the host's copy of the lengths, which only guides the choice).  A CTA takes 0.42 us per
+// tile of 32 rows for up to 16 query rows, 0.48 for 32, 0.95 for 64 (the chain of a tile; two groups of warps for the first two), and 8 us
+// beside; the storing, tensor-core and joining kernels take 22 us and 0.75 us per tile of 64 rows and CTA.  Measured (us, this kernel / the
+// three): 8 KV heads of 2048 rows, 4 query rows 10 / 21, 20 rows 13 / 22, 48 rows 16.5 / 23, 100 rows in four clusters 18 / 24; of 16000 rows,
+// 48 query rows 61 / 46; 64 sequences of 1000 to 2111 rows, 4 rows 72 / 81, 16 rows 78 / 85, 32 rows 124 / 90; 8 sequences, 32 rows 23 / 27; 33
+// sequences of 380, 60 rows 44 / 20; 8-bit, 16 sequences of 4200, 14 rows 23 / 41, 63 rows 69 / 47.
 constexpr int kFewCluster = 8, kFewTiles = 4;
-bool plan_few(const dynts_cache* c, const dynts::ExtendParams& x, int rows, int* cluster) {
+bool plan_few(const dynts_cache* c, const dynts::ExtendParams& x, int rows, int* cluster, int* split) {
   if (rows > dynts::kFewMaxRows) return false;
   long long slabs = 0, tiles = 0, small = 0, longest = 0;  // tiles of 64 and of 32 rows
   for (int s = 0; s < x.seqs.n; ++s) {
@@ -1746,16 +1747,29 @@ bool plan_few(const dynts_cache* c, const dynts::ExtendParams& x, int rows, int*
     small += (long long)x.n_layers * x.Hkv * ((n + dynts::kFewKeys - 1) / dynts::kFewKeys);
     longest = std::max(longest, (n + dynts::kFewKeys - 1) / dynts::kFewKeys);
   }
-  const long long slots = (long long)c->sm_count * (rows <= 8 ? 3 : rows <= 16 ? 2 : 1);  // (FewShape::kPerSm)
-  int k = 1;
-  while (k < kFewCluster && 2 * k * slabs <= slots && longest / (2 * k) >= kFewTiles) k *= 2;
-  *cluster = k;
-  const double most = std::max((double)((longest + k - 1) / k), (double)small / slots);
-  return 8 + (rows <= 16 ? 0.42 : rows <= 32 ? 0.48 : 0.95) * most <= 22 + 0.75 * (double)tiles / (2.0 * c->sm_count);
+  const double tc = 22 + 0.75 * (double)tiles / (2.0 * c->sm_count);
+  // The time with the query rows in so many parts, at the cost of a tile of 32 rows for one of them; k: a cluster's CTAs.
+  auto time = [&](int parts, int per_sm, double tile, int* k) {
+    const long long slots = (long long)c->sm_count * per_sm;
+    *k = 1;
+    // (Clusters of eight with an SM for each CTA: more than eight were measured as sixteen, which do not fit the GPCs at once.  32 query rows, 16 slabs of
+    // 2048 rows: 25.6 us, in clusters of four 16.6.)
+    while (*k < kFewCluster && 2ll * *k * slabs * parts <= slots && longest / (2 * *k) >= kFewTiles && (*k < 4 || per_sm > 1 || slabs * parts <= 8)) *k *= 2;
+    return 8 + tile * std::max((double)((longest + *k - 1) / *k), (double)small * parts / slots);
+  };
+  double best = rows <= 8 ? time(1, 3, 0.42, cluster) : rows <= 16 ? time(1, 2, 0.42, cluster) : rows <= 32 ? time(1, 1, 0.48, cluster) : rows <= 64 ? time(1, 1, 0.95, cluster) : 1e30;
+  *split = 1;
+  if (rows > dynts::kFewSplitRows) {
+    const int parts = (rows + dynts::kFewSplitRows - 1) / dynts::kFewSplitRows;
+    int k = 1;
+    const double t = time(parts, 1, 0.48, &k);
+    if (t < best) best = t, *cluster = k, *split = parts;
+  }
+  return best <= tc;
 }
 
 template <bool KV8, bool MODS, int NB, int RG, int KA, int PS>
-dynts_status_t launch_extend_few_as(dynts_cache* c, dynts::FewParams& p, bool* attr) {
+dynts_status_t launch_extend_few_as(dynts_cache* c, dynts::FewParams& p, bool* attr, int split = 1) {
   using S = dynts::FewShape<KV8, NB, RG, KA, PS>;
   auto kernel = dynts::extend_few_kernel<KV8, MODS, NB, RG, KA, PS>;
   if (!*attr) {
@@ -1763,20 +1777,20 @@ dynts_status_t launch_extend_few_as(dynts_cache* c, dynts::FewParams& p, bool* a
     *attr = true;
   }
   const dynts::ExtendParams& x = p.x;
-  CUDA_TRY(launch_dependent_clusters(kernel, (unsigned)p.cluster, dim3((unsigned)x.seqs.n * (unsigned)p.cluster, (unsigned)(x.n_layers * x.Hkv), 1), (unsigned)S::kThreads,
+  CUDA_TRY(launch_dependent_clusters(kernel, (unsigned)p.cluster, dim3((unsigned)x.seqs.n * (unsigned)p.cluster, (unsigned)(x.n_layers * x.Hkv), (unsigned)split), (unsigned)S::kThreads,
                                      S::kSmem, c->stream, p, c->map_KV));
   c->launches += 1;
   return DYNTS_OK;
 }
 
 template <bool KV8, bool MODS>
-dynts_status_t launch_extend_few(dynts_cache* c, dynts::FewParams& p, int rows) {
+dynts_status_t launch_extend_few(dynts_cache* c, dynts::FewParams& p, int rows, int split) {
   bool* attr = c->attr_extend_few[KV8 ? 1 : 0][MODS ? 1 : 0];
   const long long ctas = (long long)p.x.seqs.n * p.cluster * p.x.n_layers * p.x.Hkv;
   if (rows <= 8 && ctas > 3ll * c->sm_count) return launch_extend_few_as<KV8, MODS, 1, 1, 2, 4>(c, p, attr);
   if (rows <= 8) return launch_extend_few_as<KV8, MODS, 1, 1, 2, 3>(c, p, attr + 1);
   if (rows <= 16) return launch_extend_few_as<KV8, MODS, 2, 1, 2, 2>(c, p, attr + 2);
-  if (rows <= 32) return launch_extend_few_as<KV8, MODS, 2, 2, 2, 1>(c, p, attr + 3);
+  if (rows <= 32 || split > 1) return launch_extend_few_as<KV8, MODS, 2, 2, 2, 1>(c, p, attr + 3, split);
   return launch_extend_few_as<KV8, MODS, 2, 4, 1, 1>(c, p, attr + 4);
 }
 
@@ -1858,8 +1872,8 @@ dynts_status_t launch_extend(dynts_cache* c, int layer0, int n_layers, const Ext
       int longest = 0;
       for (int s = 0; s < n_seq; ++s) longest = std::max(longest, p.seqs.tok0[s + 1] - p.seqs.tok0[s]);
       const int rows = longest * c->G;
-      int cluster = 1;
-      if (longest <= dynts::kFewMaxRows && plan_few(c, p, rows, &cluster)) {
+      int cluster = 1, split = 1;
+      if (longest <= dynts::kFewMaxRows && plan_few(c, p, rows, &cluster, &split)) {
         dynts::FewParams q;
         q.x = p;
         q.cluster = cluster;
@@ -1869,8 +1883,8 @@ dynts_status_t launch_extend(dynts_cache* c, int layer0, int n_layers, const Ext
         q.cap_arg = p.cap_logit > 0.f ? (float)(2.0 * 1.4426950408889634 * (double)p.scale / (double)p.cap_logit) : 0.f;
         q.wait_limit = std::max(c->wait_limit, 2048u);
         const bool mods = p.cap_logit > 0.f || p.slopes || p.window > 0 || p.tree;
-        dynts_status_t st = kv8 ? (mods ? launch_extend_few<true, true>(c, q, rows) : launch_extend_few<true, false>(c, q, rows))
-                                : (mods ? launch_extend_few<false, true>(c, q, rows) : launch_extend_few<false, false>(c, q, rows));
+        dynts_status_t st = kv8 ? (mods ? launch_extend_few<true, true>(c, q, rows, split) : launch_extend_few<true, false>(c, q, rows, split))
+                                : (mods ? launch_extend_few<false, true>(c, q, rows, split) : launch_extend_few<false, false>(c, q, rows, split));
         if (st != DYNTS_OK) return st;
         continue;
       }

@@ -1,8 +1,9 @@
-// The chunk operators for few query rows (definitions in extend.cuh): at most 64 rows (tokens times heads of the group) per
+// The chunk operators for few query rows (definitions in extend.cuh): at most 128 rows (tokens times heads of the group) per
 // sequence and KV head, head_dim 128, bf16 or 8-bit rows, no mass wanted: one token per sequence, drafted tokens,
 // small trees.
 //
-// One launch.  A cluster of CTAs takes a slab's rows, in tiles of 32 dealt in equal runs; what the storing kernel does for the others
+// One launch.  A cluster of CTAs takes a slab's rows, in tiles of 32 dealt in equal runs, for up to 64 query rows; where slabs are few, clusters of
+// their own take 32 query rows each (every one stores the chunk's rows, the same bits, so that it finds its own).  What the storing kernel does for the others
 // (the chunk's rows into the slab, positions, scores, lengths) happens here: the CTA whose run holds a row of the chunk
 // takes it from the caller's tensors into its tile in shared memory, and stores it.  The parts of a row meet
 // in shared memory, the CTAs' through the cluster's.  (As three kernels, with the tensor-core kernel between, a tree of
@@ -28,7 +29,7 @@
 namespace dynts {
 
 constexpr int kFewKeys = 32;          // rows of a tile
-constexpr int kFewMaxRows = 64;
+constexpr int kFewMaxRows = 128, kFewSplitRows = 32;
 
 // NB: blocks of 8 query rows per warp; RG: warps that share a run of keys; KA: groups of 2 RG warps that take the tiles in turn; PS: CTAs per SM.
 // One token of 64 sequences, 512 slabs of 1028 rows, four CTAs per SM with two tiles each in flight 49 us, three with four tiles 60 (what does
@@ -161,8 +162,9 @@ extend_few_kernel(const __grid_constant__ FewParams p, const __grid_constant__ C
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const int b = x.seqs.b0 + s, tok0 = x.seqs.tok0[s], t = x.seqs.tok0[s + 1] - tok0, prefix = x.seqs.prefix[s];
-  const int n = x.len[b], tot = x.tot[b], rows = t * x.G;
-  const bool fits = n >= 0 && n + t <= x.cap, work = t > 0 && fits;  // (the same in the whole cluster)
+  const int q0 = (int)blockIdx.z * S::kRows;  // this cluster's query rows, from here on
+  const int n = x.len[b], tot = x.tot[b], all_rows = t * x.G, rows = min(S::kRows, all_rows - q0);
+  const bool fits = n >= 0 && n + t <= x.cap, work = rows > 0 && fits;  // (the same in the whole cluster)
   if (t > 0 && !fits && tid == 0 && rank == 0) atomicOr(x.err, kErrLenOverflow);
   const size_t slab = ((size_t)(x.layer0 + layer) * x.Nb + b) * x.Hkv + h;
   const ExtTiles tiles = ext_tiles(x.window, x.sinks, x.tree != nullptr, n, 0, kFewKeys);
@@ -171,9 +173,9 @@ extend_few_kernel(const __grid_constant__ FewParams p, const __grid_constant__ C
   if (tid < S::kRows) {
     int4 w = make_int4(0, 0, 0, 0);
     if (work && tid < rows) {
-      const int i = tid / x.G;
+      const int i = (q0 + tid) / x.G;
       const ExtNode node = ext_node(x, tok0, i, t);
-      w = make_int4(n + max(i + 1, prefix), tot + node.depth, node.order, x.slopes ? __float_as_int(x.slopes[h * x.G + tid - i * x.G] * 1.4426950408889634f) : 0);
+      w = make_int4(n + max(i + 1, prefix), tot + node.depth, node.order, x.slopes ? __float_as_int(x.slopes[h * x.G + q0 + tid - i * x.G] * 1.4426950408889634f) : 0);
     }
     s_row[tid] = w;
   }
@@ -211,18 +213,18 @@ extend_few_kernel(const __grid_constant__ FewParams p, const __grid_constant__ C
     uint32_t qa[NB][8][2];
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
-      const int r = r0 + 8 * nb + gid, i = r / x.G;
+      const int r = q0 + r0 + 8 * nb + gid, i = r / x.G;
       const uint32_t* hq = reinterpret_cast<const uint32_t*>(static_cast<const __nv_bfloat16*>(x.q) + ((size_t)layer * x.total + tok0 + i) * x.q_stride +
                                                               (size_t)(h * x.G + r - i * x.G) * 128);
 #pragma unroll
       for (int kk = 0; kk < 8; ++kk) {
         if constexpr (KV8) {
-          const uint2 w = r < rows ? *reinterpret_cast<const uint2*>(hq + 8 * kk + 2 * tig) : make_uint2(0u, 0u);
+          const uint2 w = r < all_rows ? *reinterpret_cast<const uint2*>(hq + 8 * kk + 2 * tig) : make_uint2(0u, 0u);
           qa[nb][kk][0] = bf16x2_to_half2(w.x);
           qa[nb][kk][1] = bf16x2_to_half2(w.y);
         } else {
-          qa[nb][kk][0] = r < rows ? hq[8 * kk + tig] : 0u;
-          qa[nb][kk][1] = r < rows ? hq[8 * kk + 4 + tig] : 0u;
+          qa[nb][kk][0] = r < all_rows ? hq[8 * kk + tig] : 0u;
+          qa[nb][kk][1] = r < all_rows ? hq[8 * kk + 4 + tig] : 0u;
         }
       }
     }
@@ -497,9 +499,9 @@ extend_few_kernel(const __grid_constant__ FewParams p, const __grid_constant__ C
       const float inv = 1.f / L;
       acc = make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
       const bool fine = (acc.x + acc.y) * 0.f == 0.f && (acc.z + acc.w) * 0.f == 0.f;
-      if (!__all_sync(0xffffffffu, fine)) acc = few_row_again<KV8>(x, s, layer, h, r, n, tot, t);
-      const int i = r / x.G;
-      __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(x.out) + (((size_t)layer * x.total + tok0 + i) * x.Hq + h * x.G + r - i * x.G) * 128 + 4 * lane;
+      if (!__all_sync(0xffffffffu, fine)) acc = few_row_again<KV8>(x, s, layer, h, q0 + r, n, tot, t);
+      const int i = (q0 + r) / x.G;
+      __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(x.out) + (((size_t)layer * x.total + tok0 + i) * x.Hq + h * x.G + q0 + r - i * x.G) * 128 + 4 * lane;
       *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16x2(acc.x * p.out_scale, acc.y * p.out_scale), pack_bf16x2(acc.z * p.out_scale, acc.w * p.out_scale));
     }
   }
@@ -507,7 +509,7 @@ extend_few_kernel(const __grid_constant__ FewParams p, const __grid_constant__ C
     // every CTA has read the lengths before it takes its ticket; the last one advances them
     __syncthreads();
     __shared__ int last;
-    if (tid == 0) last = atomicAdd(x.ticket, 1u) == gridDim.x * gridDim.y - 1;
+    if (tid == 0) last = atomicAdd(x.ticket, 1u) == gridDim.x * gridDim.y * gridDim.z - 1;
     __syncthreads();
     if (last) {
       for (int q = tid; q < x.seqs.n; q += S::kThreads) {

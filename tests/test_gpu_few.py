@@ -18,7 +18,7 @@ def launches(c, call):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "bf16_kv8"])
-@pytest.mark.parametrize("q_heads,new", [(2, (1, 1, 1)), (4, (9, 0, 16)), (14, (4, 1, 2)), (16, (8, 0, 7)), (2, (64, 33, 31))])
+@pytest.mark.parametrize("q_heads,new", [(2, (1, 1, 1)), (4, (9, 0, 16)), (14, (4, 1, 2)), (16, (8, 0, 7)), (2, (64, 33, 31)), (4, (64, 0, 33)), (14, (18, 3, 9))])
 @pytest.mark.parametrize("opt", [dict(), dict(window=37, sinks=6), dict(softcap=15.0, slopes=True)], ids=["plain", "sinks", "mods"])
 def test_rows_left_and_lengths(dtype, q_heads, new, opt):
     """Tiles that the chunk begins, ends and crosses; groups of 1 to 8 heads; stored rows, then more behind them."""
@@ -66,6 +66,29 @@ def test_scores_and_a_path(dtype):
                 assert pos.tolist() == pos0.tolist() + list(range(seen[b], seen[b] + len(p)))
                 assert torch.equal(score.double(), torch.cat([score0, s_new[at].double().cpu()]))
     c.close()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "bf16_kv8"])
+def test_more_query_rows_than_a_cluster_takes(dtype):
+    """100 and 128 rows of one sequence, clusters of their own for 32 of them; one of them with values that are not finite beside."""
+    for q_heads, kv_heads, new in ((32, 8, 25), (4, 1, 32), (14, 2, 18), (8, 8, 65)):
+        c, seen = build(dtype=dtype, q_heads=q_heads, kv_heads=kv_heads, past=(700,), cap=900)
+        q, k, v = chunk(c, [new], 7)
+        assert launches(c, lambda: c.extend_attn(q, k, v, torch.empty_like(q), [new], stage=True)) == 1
+        check(c, seen, [new], want_mass=False, scale=0.05, seed=1)
+        check(c, seen, [new], TR.random_trees([new], 3, 6), want_mass=False, scale=0.05, seed=2)
+        bad_k, bad_v = k.clone(), v.clone()
+        bad_k[:, new - 1] = bad_v[:, new - 1] = float("nan")  # a leaf that the others do not see
+        clean, out = torch.empty_like(q), torch.empty_like(q)
+        tree, _ = c.tree_plan(torch.tensor([-1] * new, dtype=torch.int32, device="cuda"), [new])
+        c.extend_attn(q, k, v, clean, [new], stage=True, tree=tree)
+        c.extend_attn(q, bad_k, bad_v, out, [new], tree=tree, stage=True)
+        c.synchronize()
+        keep = slice(0, new - 1)
+        diff = (out[:, keep].double() - clean[:, keep].double()).abs()
+        # (rows computed again: a half step of the weights, and one of the output on either side)
+        assert (diff <= 2 * 2.0 ** -8 * clean[:, keep].double().abs() + 2.0 ** -8 * v.abs().max().double()).all()
+        c.close()
 
 
 def test_steps_replayed_as_the_sequences_grow():
