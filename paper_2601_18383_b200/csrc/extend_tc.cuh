@@ -30,7 +30,7 @@
 // walks the CTA's pieces by the plan the storing kernel wrote (extend.cuh), a word per lane, the next piece's
 // prefetched.  Two CTAs of 384 threads leave 80 registers per thread and hardly any L1: code that spills or does
 // not stay in the instruction caches cost several times its instructions, so the loops are rolled, the end of a piece
-// is a function of its own, and what is rare is called once from its end (spills: 32 bytes in the plain kernel, none with caps
+// is a function of its own, and what is rare is called once from its end (spills: 44 bytes in the plain kernel, none with caps
 // and biases, 16 and 36 with 8-bit rows).  4096 tokens behind 4096 rows: 433 us a call with changing inputs, 0.95 PFLOP/s; 375 to
 // 395 us replayed on one state, 1.04 to 1.10 PFLOP/s, 0.65 to 0.68 of what cuBLAS reaches.  (Cursors in registers and everything
 // unrolled: 453 us when this stood at 388.)  The tensor cores and the exponentials' unit are each busy for a little more than
@@ -57,10 +57,9 @@
 
 namespace dynts {
 
-// The row arithmetic: plain; with caps, biases and windows, and the same with trees and sinks (ragged prompts with a bias, where neither is there:
-// 110 us without, 119 with); plain with the mask of a tree in the tiles of the chunk's
-// rows (trees of 60 in 16 sequences behind 4200 8-bit rows: 144 us as part of the second, 115 so); plain with the mask of a window in the tiles
-// at its borders.
+// The row arithmetic: plain; with caps, biases and windows (ragged prompts with a bias 113 us, 122 with the code of trees and sinks beside); plain
+// with the mask of a tree in the tiles of the chunk's rows (trees of 60 in 16 sequences behind 4200 8-bit rows 115 us, 144 with caps
+// and windows beside); plain with the mask of a window in the tiles at its borders; all of it.
 constexpr int kXtPlain = 0, kXtMods = 1, kXtTree = 2, kXtWindow = 3, kXtAll = 4;
 // 8-bit rows, and the plain row arithmetic: two warps of their own load (12 warps, 80 registers per thread).  With caps, biases
 // and windows the row arithmetic needs the registers more: the warps that issue the products load too (10 warps, 96).

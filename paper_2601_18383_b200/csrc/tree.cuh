@@ -7,7 +7,7 @@
 // one subtraction and one comparison for each (query, row), where a mask of bits would take a word per 32 rows of the
 // chunk and query.  depth_i gives the positions.  Sizes, depths and the sums along a path come by pointer doubling: after k
 // rounds a node knows the 2^k nearest ancestors' part, so a tree takes log2(depth) rounds whatever its shape.
-// One CTA per sequence, a thread per node: bound by the latency of a launch and of about ten barriers (3 us).
+// One CTA per sequence, a thread per node: bound by the latency of a launch and of about ten barriers (2 us).
 //
 // tree_accept_kernel walks down from node 0 while a child's drafted token is the token drawn at the node.
 // tree_move_kernel brings an accepted path's rows together behind the rows held.
