@@ -31,7 +31,7 @@
 // prefetched.  Two CTAs of 384 threads leave 80 registers per thread and hardly any L1: code that spills or does
 // not stay in the instruction caches cost several times its instructions, so the loops are rolled, the end of a piece
 // is a function of its own, and what is rare is called once from its end (spills: 44 bytes in the plain kernel, none with caps
-// and biases, 16 and 36 with 8-bit rows).  4096 tokens behind 4096 rows: 433 us a call with changing inputs, 0.95 PFLOP/s; 375 to
+// and biases, 24 to 36 with 8-bit rows).  4096 tokens behind 4096 rows: 433 us a call with changing inputs, 0.95 PFLOP/s; 375 to
 // 395 us replayed on one state, 1.04 to 1.10 PFLOP/s, 0.65 to 0.68 of what cuBLAS reaches.  (Cursors in registers and everything
 // unrolled: 453 us when this stood at 388.)  The tensor cores and the exponentials' unit are each busy for a little more than
 // half of that time, in turns that the chain of a tile does not let overlap further: tiles of 128 keys with one S buffer,
