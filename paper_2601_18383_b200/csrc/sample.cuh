@@ -808,7 +808,10 @@ __global__ void __launch_bounds__(kSmThreads, kSmPerSm) sample_kernel(const __gr
       const u64 above = sm_peer(&sh.above, 0);
       const double goal = sm_peer(&sh.goal, 0);
       for (int q = 0; q < 2; ++q) sh.hist[0][tid + q * kSmThreads] = sh.hist[1][tid + q * kSmThreads] = 0;
-      if (bin < 0) continue;     // fewer tokens than top_k; or a sum missed by a rounding: all are kept
+      if (bin < 0) {      // fewer tokens than top_k; or a sum missed by a rounding: all are kept
+        __syncthreads();  // (the next histogram begins with cleared words)
+        continue;
+      }
       const SmBorder outer = border;
       // (a vector without an element of this bin or a nearer one is passed over: what the bin holds is at least this large)
       const float reach = by_weight ? __double2float_rd(Md - (double)(((bin + 1) << coarse) + 1) * 0.02166084939249829 * (double)T)  // ln 2 / 32

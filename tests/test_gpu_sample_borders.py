@@ -1,0 +1,31 @@
+"""Sampling where a border is hard to find: fewer tokens than top_k, masks, logits and temperatures at the ends of fp32; against the plain 64-bit form."""
+import math
+
+import pytest
+import torch
+
+import paper_2601_18383_b200 as D
+from tests.test_gpu_sample import check, logits
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("n", [1, 20, 60, 160])  # clusters of eight, four, two CTAs, and single ones
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_fewer_tokens_than_top_k_with_top_p(n, dtype):
+    """The histogram of the tokens finds no border, and that of the weights follows at once: the same answer each time."""
+    V = 20011
+    for finite, where, top_k in ((1200, "spread", 1500), (300, "run", 500), (1100, "run", 5000)):
+        x, u = logits(n, V, dtype, finite + n)
+        g = torch.Generator(device="cuda").manual_seed(n)
+        keep = torch.zeros((n, V), dtype=torch.bool, device="cuda")
+        if where == "spread":
+            keep.scatter_(1, torch.rand((n, V), generator=g, device="cuda").topk(finite, 1).indices, True)
+        else:
+            keep[:, 7000:7000 + finite] = True
+        x = torch.where(keep, x, torch.full_like(x, -math.inf))
+        check(x, u, 0.9, top_k, 0.8)
+        first = D.sample(x, u, 1.1, top_k, 0.9, 0.01)
+        for _ in range(20):
+            again = D.sample(x, u, 1.1, top_k, 0.9, 0.01)
+            assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
