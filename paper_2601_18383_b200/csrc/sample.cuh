@@ -705,15 +705,16 @@ __global__ void __launch_bounds__(kSmThreads, kSmPerSm) sample_kernel(const __gr
       const bool by_weight = which == 1;
       if (by_weight ? !cut_p : top_k == 0) continue;
       // Weights: steps of a thirty-second of a binary order.  What lies beyond ln(V / (1 - p)) in units of T adds up to less than 1 - p of
-      // the largest, so no border lies there and no step is counted.  Tokens: equal steps of the distance to the maximum up to `span`;
+      // the largest, so no border lies there and no step is counted.  Tokens: equal steps of the distance to the maximum up to `half`;
       // the lanes' maxima reach down to low_all; beyond their number, the smallest logit does.
-      float span = 0.f;
+      // (Distances are halved: two logits may be further apart than the largest number.)
+      float half = 0.f;
       int bins = kSmBins, coarse = 0;  // (two steps as one where 1024 do not reach)
       if (by_weight) {
         bins = 2 + (int)(46.17f * (logf((float)p.vocab / (1.f - top_p)) + 0.01f));  // 32 / ln 2
         if (bins > kSmBins) coarse = 1, bins = kSmBins;
       } else if ((unsigned)top_k <= lanes_all) {
-        span = M - low_all;
+        half = 0.5f * M - 0.5f * low_all;
       } else {
         float least_all = INFINITY;
         each_vector(r, r.v0, r.v1, [&](int, const uint4& w) {
@@ -733,16 +734,16 @@ __global__ void __launch_bounds__(kSmThreads, kSmPerSm) sample_kernel(const __gr
         if (tid == 0) sh.low = least_all;
         sm_cluster_sync(cluster);
         for (int k = 0; k < cluster; ++k) least_all = fminf(least_all, sm_peer(&sh.low, k));
-        span = M - least_all;
+        half = 0.5f * M - 0.5f * least_all;
       }
-      const float steps = span > 0.f ? fminf((kSmBins - 1) / span, 1e30f) : 0.f;
-      const float reach_all = M - span * 1.01f;  // (a step more than the span)
+      const float steps = half > 0.f ? fminf((kSmBins - 1) / half, 1e30f) : 0.f;
+      const float reach_all = M - half * 2.02f;  // (a step more than the span)
       auto bin_of = [&](float x) {  // (never grows with x: every rounding is monotone)
         if (by_weight) {
           const int n = weight_of.step(x) >> coarse;
           return n < bins ? n : kSmBins;
         }
-        const float y = (M - x) * steps;
+        const float y = fmaf(x, -0.5f, 0.5f * M) * steps;
         return y < (float)kSmBins ? (int)y : kSmBins;
       };
       u64 outside = 0;
@@ -815,8 +816,8 @@ __global__ void __launch_bounds__(kSmThreads, kSmPerSm) sample_kernel(const __gr
       const SmBorder outer = border;
       // (a vector without an element of this bin or a nearer one is passed over: what the bin holds is at least this large)
       const float reach = by_weight ? __double2float_rd(Md - (double)(((bin + 1) << coarse) + 1) * 0.02166084939249829 * (double)T)  // ln 2 / 32
-                          : steps > 0.f ? M - (float)(bin + 2) / steps : -INFINITY;
-      const float from = by_weight ? fminf(M, __double2float_ru(Md - (double)((bin << coarse) - 2) * 0.02166084939249829 * (double)T)) : steps > 0.f ? fminf(M, M - (float)(bin - 1) / steps) : M;
+                          : steps > 0.f ? 2.f * (0.5f * M - (float)(bin + 2) / steps) : -INFINITY;
+      const float from = by_weight ? fminf(M, __double2float_ru(Md - (double)((bin << coarse) - 2) * 0.02166084939249829 * (double)T)) : steps > 0.f ? fminf(M, 2.f * (0.5f * M - (float)(bin - 1) / steps)) : M;
       auto in_bin = [&](float x, int i) { return x >= reach && x <= from && bin_of(x) == bin && outer.keeps(x, i); };
       collect(reach, from, std::true_type{}, in_bin);
       sm_cluster_sync(cluster);

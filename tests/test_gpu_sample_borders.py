@@ -29,3 +29,15 @@ def test_fewer_tokens_than_top_k_with_top_p(n, dtype):
         for _ in range(20):
             again = D.sample(x, u, 1.1, top_k, 0.9, 0.01)
             assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
+
+
+@pytest.mark.parametrize("temperature", [1e37, 1e38, 3e38])
+def test_logits_further_apart_than_the_largest_number(temperature):
+    """The distance of two fp32 logits overflows; borders by counts of tokens lie on either side of where it does."""
+    for n, V in ((3, 5003), (90, 5003), (2, 40009)):
+        g = torch.Generator(device="cuda").manual_seed(V + n)
+        x = (torch.rand((n, V), generator=g, device="cuda") * 2 - 1) * 3.3e38
+        u = torch.rand((n,), generator=g, device="cuda")
+        for top_k in (20, 1100, V // 2, V - 1000, V - 3):
+            check(x, u, temperature, top_k)
+            check(x, u, temperature, top_k, 0.7)
