@@ -44,6 +44,7 @@ constexpr int kSmBins = 2 * kSmThreads;  // steps of a histogram
 constexpr int kSmTable = 16;
 constexpr int kSmGroups = 16;       // of a lane's vectors, whose maxima are kept
 constexpr int kSmPerSm = 2;         // CTAs
+constexpr double kSmFar = 33.0;      // of a token that weighs nothing, in units of T (32, and one for roundings)
 constexpr int kSmNoStep = 1 << 20;   // of a token that weighs nothing
 constexpr int kSmMaxVocab = (1 << 19) - 1;  // sums of 2^45 for each token fit 64 bits
 
@@ -436,6 +437,7 @@ __global__ void __launch_bounds__(kSmThreads, kSmPerSm) sample_kernel(const __gr
     cut = top;
   } else if (listed) {
     // a value that `share` of the groups' maxima reach, close to the largest such: by a histogram of 512 equal steps
+    least = fmaxf(least, __double2float_rd((double)top - kSmFar * (double)T));
     const float steps = top > least ? (kSmThreads - 1) / (top - least) : 0.f;
     const int mine = r.v0 + lane < r.v1 ? (r.v1 - r.v0 - lane + 128 * r.rounds - 1) / (128 * r.rounds) : 0;  // this lane's groups
     auto step_of = [&](float x) { return x > -INFINITY ? min(kSmThreads - 1, max(0, (int)((top - x) * steps))) : kSmThreads; };
@@ -485,6 +487,11 @@ __global__ void __launch_bounds__(kSmThreads, kSmPerSm) sample_kernel(const __gr
   const double Md = (double)M;
   // what min_p keeps: x >= least_x (min_p > 1 counts as 1)
   const float least_x = min_p > 0.f ? __double2float_ru(fmin(Md + (double)T * log((double)min_p), Md)) : -INFINITY;
+  // Below this a token weighs nothing, and what is counted, collected or kept of such tokens changes no answer: distances end here, so
+  // that logits of the type's lowest value (a usual mask) do not make steps of 3e35.
+  const float far_x = __double2float_rd(Md - kSmFar * (double)T);
+  cut = fmaxf(cut, far_x);
+  low_all = fmaxf(low_all, far_x);
   const SmWeights weight_of{Md, inv_t, sh.table};
   auto answer = [&](int token, float x, u64 total) {
     p.tokens[row] = token;
@@ -734,7 +741,7 @@ __global__ void __launch_bounds__(kSmThreads, kSmPerSm) sample_kernel(const __gr
         if (tid == 0) sh.low = least_all;
         sm_cluster_sync(cluster);
         for (int k = 0; k < cluster; ++k) least_all = fminf(least_all, sm_peer(&sh.low, k));
-        half = 0.5f * M - 0.5f * least_all;
+        half = 0.5f * M - 0.5f * fmaxf(least_all, far_x);
       }
       const float steps = half > 0.f ? fminf((kSmBins - 1) / half, 1e30f) : 0.f;
       const float reach_all = M - half * 2.02f;  // (a step more than the span)
@@ -809,7 +816,7 @@ __global__ void __launch_bounds__(kSmThreads, kSmPerSm) sample_kernel(const __gr
       const u64 above = sm_peer(&sh.above, 0);
       const double goal = sm_peer(&sh.goal, 0);
       for (int q = 0; q < 2; ++q) sh.hist[0][tid + q * kSmThreads] = sh.hist[1][tid + q * kSmThreads] = 0;
-      if (bin < 0) {      // fewer tokens than top_k; or a sum missed by a rounding: all are kept
+      if (bin < 0) {      // fewer tokens of any weight than top_k; or a sum missed by a rounding: all are kept
         __syncthreads();  // (the next histogram begins with cleared words)
         continue;
       }

@@ -41,3 +41,19 @@ def test_logits_further_apart_than_the_largest_number(temperature):
         for top_k in (20, 1100, V // 2, V - 1000, V - 3):
             check(x, u, temperature, top_k)
             check(x, u, temperature, top_k, 0.7)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("n,V", [(2, 30011), (100, 9001)])
+def test_rows_masked_with_the_lowest_value(dtype, n, V):
+    """All but some tokens of a row, whole runs of it, every other one: -inf and the lowest finite value give the same answers."""
+    x, u = logits(n, V, dtype, V)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    masks = [torch.rand((n, V), generator=g, device="cuda") < p for p in (0.99, 0.5)] + [torch.arange(V, device="cuda").expand(n, V) % 2 == 0, torch.arange(V, device="cuda").expand(n, V) > 700]
+    for mask in masks:
+        low, none = (torch.where(mask, torch.full_like(x, f), x) for f in (torch.finfo(dtype).min, -math.inf))
+        for s in (dict(temperature=0.0), dict(temperature=0.7, top_k=50, top_p=0.9), dict(top_k=600), dict(top_k=1500, top_p=0.99), dict(temperature=30.0, top_k=3000), dict(top_p=0.8)):
+            a, b = D.sample(low, u, **s), D.sample(none, u, **s)
+            assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+        check(low[:2], u[:2], 0.7, 50, 0.9)
+        check(low[:2], u[:2], 1.0, 1500, 0.99)
