@@ -364,8 +364,8 @@ dynts_status_t dynts_rope(const void* q, const void* k, const int* pos, void* q_
 
 /* Settings of dynts_sample, for all rows, or where the array is given (device, [n_rows]) for each.  opts == NULL: temperature 1,
  * nothing cut off.  Scalars are checked on the host; array values outside the ranges count as: temperature not above 0 (or NaN)
- * as 0, top_k below 1 as off, top_p above 1 (or NaN) as 1 and below 0 as 0 (the largest token alone), min_p below 0 (or NaN) as
- * 0 and above 1 as 1. */
+ * as 0 and an infinite one as the largest finite number, top_k below 1 as off, top_p above 1 (or NaN) as 1 and below 0 as 0 (the
+ * largest token alone), min_p below 0 (or NaN) as 0 and above 1 as 1. */
 typedef struct dynts_sample_opts {
   float temperature; /* T >= 0, finite; 0: the largest logit, the lowest index among equals, with log-probability 0 */
   int top_k;         /* 0: off */

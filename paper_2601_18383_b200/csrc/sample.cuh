@@ -392,7 +392,8 @@ __global__ void __launch_bounds__(kSmThreads, kSmPerSm) sample_kernel(const __gr
   if (top_k == 1 || !(top_p < 1.f)) top_p = 1.f;
   top_p = fmaxf(top_p, 0.f);
   const bool cut_p = top_p < 1.f;
-  const double inv_t = 1.0 / (double)fminf(T, 3.0e38f);
+  T = fminf(T, 3.402823466e38f);
+  const double inv_t = 1.0 / (double)T;
   const int share = (top_k + cluster - 1) / cluster;  // of top_k, for each CTA
   const bool listed = top_k > 0 && top_k <= kSmListK;
 

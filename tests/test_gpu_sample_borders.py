@@ -57,3 +57,16 @@ def test_rows_masked_with_the_lowest_value(dtype, n, V):
             assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
         check(low[:2], u[:2], 0.7, 50, 0.9)
         check(low[:2], u[:2], 1.0, 1500, 0.99)
+
+
+def test_the_largest_temperatures():
+    """A finite temperature is taken at its value up to the largest number; an infinite one of an array as that."""
+    most = torch.finfo(torch.float32).max
+    g = torch.Generator(device="cuda").manual_seed(4)
+    x = (torch.rand((5, 3001), generator=g, device="cuda") * 2 - 1) * 3.3e38
+    u = torch.rand((5,), generator=g, device="cuda")
+    for s in (dict(), dict(top_p=0.3), dict(top_k=1200, top_p=0.6), dict(min_p=0.5), dict(top_k=40)):
+        check(x, u, most, **s)
+        check(x, u, 3.2e38, **s)
+        a, b = D.sample(x, u, torch.full((5,), math.inf, device="cuda"), **s), D.sample(x, u, most, **s)
+        assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
