@@ -30,6 +30,9 @@ namespace dynts {
 
 constexpr int kFewKeys = 32;          // rows of a tile
 constexpr int kFewMaxRows = 128, kFewSplitRows = 32;
+// Weights for 8-bit rows are f16, whose smallest normal number is 2^-14: they are held times 2^15, and so are their sums, so that a weight keeps
+// its 11 bits down to 2^-29 of the largest (many small ones beside a first token that takes most of the weight and has a small value).
+constexpr float kFewF16Shift = 15.f;
 
 // NB: blocks of 8 query rows per warp; RG: warps that share a run of keys; KA: groups of 2 RG warps that take the tiles in turn; PS: CTAs per SM.
 // One token of 64 sequences, 512 slabs of 1028 rows, four CTAs per SM with two tiles each in flight 49 us, three with four tiles 60 (what does
@@ -386,8 +389,9 @@ extend_few_kernel(const __grid_constant__ FewParams p, const __grid_constant__ C
 #pragma unroll
           for (int o_ = 4; o_ < 32; o_ <<= 1) u[q] = fmaxf(u[q], __shfl_xor_sync(0xffffffffu, u[q], o_));
           const float mn = fmaxf(m[nb][q], u[q]);
-          safe[q] = mn == -CUDART_INF_F ? 0.f : mn;
-          keep[q] = m[nb][q] == mn ? 1.f : fast_exp2(m[nb][q] - safe[q]);  // (also while the row has seen nothing)
+          const float base = mn == -CUDART_INF_F ? 0.f : mn;
+          keep[q] = m[nb][q] == mn ? 1.f : fast_exp2(m[nb][q] - base);  // (also while the row has seen nothing)
+          safe[q] = KV8 ? base - kFewF16Shift : base;
           m[nb][q] = mn;
         }
         const float w0 = fast_exp2(sc[nb][0] - safe[0]), w1 = fast_exp2(sc[nb][1] - safe[1]), w2 = fast_exp2(sc[nb][2] - safe[0]), w3 = fast_exp2(sc[nb][3] - safe[1]);
