@@ -1881,6 +1881,7 @@ dynts_status_t launch_extend(dynts_cache* c, int layer0, int n_layers, const Ext
         q.out_scale = kv8 ? c->v_scale : 1.f;
         q.cap_log2 = (float)(1.4426950408889634 * (double)p.cap_logit);
         q.cap_arg = p.cap_logit > 0.f ? (float)(2.0 * 1.4426950408889634 * (double)p.scale / (double)p.cap_logit) : 0.f;
+        q.cap_y = p.cap_logit > 0.f ? (float)((double)p.scale / (double)p.cap_logit) : 0.f;
         q.wait_limit = std::max(c->wait_limit, 2048u);
         const bool mods = p.cap_logit > 0.f || p.slopes || p.window > 0 || p.tree;
         dynts_status_t st = kv8 ? (mods ? launch_extend_few<true, true>(c, q, rows, split) : launch_extend_few<true, false>(c, q, rows, split))

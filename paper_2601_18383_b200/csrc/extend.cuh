@@ -372,6 +372,11 @@ __device__ __forceinline__ ExtNode ext_node(const ExtendParams& p, int tok0, int
 }
 __device__ __forceinline__ bool ext_below(int order, const ExtNode& row) { return (unsigned)(order - row.order) < (unsigned)row.size; }
 
+// tanh(y) = y P(y^2) for |y| up to 3/4, P of degree 5 and the least greatest relative error there (3e-8, below a rounding): its coefficients.
+__device__ __forceinline__ float ext_cap_term(int i) {
+  return i == 0 ? 0.999999971f : i == 1 ? -0.333329589f : i == 2 ? 0.13325406f : i == 3 ? -0.0533444308f : i == 4 ? 0.0195829087f : -0.00471625728f;
+}
+
 // A logit in base-2 units (before the visibility test), from the raw dot product.
 __device__ __forceinline__ float ext_logit_exact(const ExtendParams& p, float dot, float slope, int apart) {
   float x = dot * p.scale;

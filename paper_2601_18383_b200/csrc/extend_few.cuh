@@ -57,6 +57,7 @@ struct FewParams {
   float scale_log2;   // log2(e) * scale
   float cap_log2;     // c log2(e), or 0
   float cap_arg;      // 2 log2(e) scale / c
+  float cap_y;        // scale / c
   float out_scale;    // v_scale for 8-bit rows
   unsigned int wait_limit;
 };
@@ -342,12 +343,32 @@ extend_few_kernel(const __grid_constant__ FewParams p, const __grid_constant__ C
       }
       // logits, in base-2 units; what is hidden is -inf
       if constexpr (MODS) {
-        // (as c - 2 c / (1 + e^(2 y)): off by a few 2^-24 of c, which is what y itself is off by at c)
+        // c tanh(y), y = logit / c: by the polynomial, off by a rounding or two of the result, while every logit of the warp's tile lies below three
+        // quarters of the cap; else as c - 2 c / (1 + e^(2 y)), off by a few 2^-24 of c (of logits far below the cap nothing would
+        // be left).
         if (x.cap_logit > 0.f) {
+          float top = 0.f;
 #pragma unroll
           for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) sc[nb][e] = fmaf(-2.f * p.cap_log2, few_rcp(1.f + fast_exp2(sc[nb][e] * p.cap_arg)), p.cap_log2);
+            for (int e = 0; e < 4; ++e) top = fmaxf(top, fabsf(sc[nb][e]));
+          if (__all_sync(0xffffffffu, top * p.cap_y <= 0.75f)) {
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const float y = sc[nb][e] * p.cap_y, z = y * y;
+                float f = ext_cap_term(5);
+#pragma unroll
+                for (int i = 4; i >= 0; --i) f = fmaf(f, z, ext_cap_term(i));
+                sc[nb][e] = f * y * p.cap_log2;
+              }
+          } else {
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) sc[nb][e] = fmaf(-2.f * p.cap_log2, few_rcp(1.f + fast_exp2(sc[nb][e] * p.cap_arg)), p.cap_log2);
+          }
         }
       }
       const float scale = MODS && x.cap_logit > 0.f ? 1.f : p.scale_log2;

@@ -304,13 +304,12 @@ __device__ __forceinline__ float xt_cap(uint32_t (&sv)[32], const ExtendTcParams
   for (int c = 0; c < 32; c += 2) top = tc5::f_max3(top, fabsf(__uint_as_float(sv[c])), fabsf(__uint_as_float(sv[c + 1])));
   if (__all_sync(0xffffffffu, top * p.cap_y <= 0.75f)) {
     const uint64_t a2 = tc5::f2_pack(p.cap_y, p.cap_y);
-    const float k[6] = {0.999999971f, -0.333329589f, 0.13325406f, -0.0533444308f, 0.0195829087f, -0.00471625728f};
 #pragma unroll
     for (int c = 0; c < 32; c += 2) {
       const uint64_t y = tc5::f2_mul(tc5::f2_pack(__uint_as_float(sv[c]), __uint_as_float(sv[c + 1])), a2), z = tc5::f2_mul(y, y);
-      uint64_t t = tc5::f2_pack(k[5], k[5]);
+      uint64_t t = tc5::f2_pack(ext_cap_term(5), ext_cap_term(5));
 #pragma unroll
-      for (int e = 4; e >= 0; --e) t = tc5::f2_fma(t, z, tc5::f2_pack(k[e], k[e]));
+      for (int e = 4; e >= 0; --e) t = tc5::f2_fma(t, z, tc5::f2_pack(ext_cap_term(e), ext_cap_term(e)));
       float y0, y1;
       tc5::f2_unpack(tc5::f2_mul(t, y), y0, y1);
       sv[c] = __float_as_uint(y0);

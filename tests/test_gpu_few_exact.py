@@ -45,3 +45,30 @@ def test_small_weights_beside_a_large_one(dtype, gap, new, n):
     c.poll_error()
     assert ((out.double().cpu() - ref).abs() <= tol).all()
     c.close()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "bf16_kv8"])
+@pytest.mark.parametrize("cap", [1e5, 1e8, 1e20])
+@pytest.mark.parametrize("q_heads,new", [(2, (1, 2)), (8, (4, 1)), (8, (6, 2)), (16, (7, 3)), (16, (14, 9))])  # groups of warps for 8, 16, 32 and 64 rows, and parts
+def test_a_cap_far_above_the_logits_is_none(dtype, cap, q_heads, new):
+    """c tanh(z / c) is z to within z^3 / 3 c^2, at most 2e-7 of it here: the plain form without a cap is the answer."""
+    scale = 0.05
+    c = D.Cache(1, 2, q_heads, 2, 128, 320, 0, 1, dtype=dtype, capacity=320)
+    if dtype == "bf16_kv8":
+        c.set_kv_scale(scale, scale)
+    c.set_score_source(D.DYNTS_SCORE_EXTERNAL)
+    g = torch.Generator(device="cuda").manual_seed(len(new) + q_heads)
+    normal = lambda *s: torch.randn(s, generator=g, device="cuda").bfloat16()
+    for b, n in enumerate((200, 77)):
+        c.prefill_seq(b, normal(1, 2, n, 128), normal(1, 2, n, 128), n_pinned=0)
+    c.synchronize()
+    T = sum(new)
+    q, k, v = 2 * normal(1, T, q_heads, 128), normal(1, T, 2, 128), normal(1, T, 2, 128)
+    state = R.State(c, scale, scale) if dtype == "bf16_kv8" else R.State(c)
+    ref, tol, *_ = TR.attend(state, [200, 77], q, k, v, new, None, p_half_step=2.0 ** -8)
+    out = torch.empty_like(q)
+    assert launches(c, lambda: c.extend_attn(q, k, v, out, list(new), stage=True, softcap=cap)) == 1
+    c.synchronize()
+    c.poll_error()
+    assert ((out.double().cpu() - ref).abs() <= tol).all()
+    c.close()
