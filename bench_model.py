@@ -22,7 +22,8 @@ to its first answer token is reported.
 `--temperature T` (with `--top-p P`) draws the tokens from given random numbers (dynts_sample) instead of taking the largest
 logit.  `--draft D` adds the check of a drafted tree: a tree of D levels per sequence, grown by the model itself (the two best
 continuations of its last four nodes), goes through the model in one pass (dynts_tree_plan, dynts_extend_attn_ex), a token is
-drawn for every node (dynts_sample), and the path of drawn tokens is taken over (dynts_tree_accept, dynts_extend_commit_path).
+drawn for every node (dynts_sample, a random number per sequence and depth), and the path of drawn tokens is taken over
+(dynts_tree_accept, dynts_extend_commit_path).
 
 `--late-state` instead times 128 steps in the state a 16384-token decode reaches, the caches
 filled with seeded synthetic K/V rows (no trajectory, no evictions falling due).
@@ -238,7 +239,16 @@ def run_arm(model, cache, batch, start_pos, steps, interval, evict, device):
             "steps_timed": reps * per_graph}
 
 
-def check_draft(model, args, cache, last, u, limited, device):
+def draft_chances(u, parents):
+    """The random number of every node of every sequence's tree, from u [batch, levels]: those of a depth in a sequence share one (at most one
+    of them lies on a path), those of a path have one each."""
+    depths = []
+    for p in parents:
+        depths.append(0 if p < 0 else depths[p] + 1)
+    return u[:, depths].reshape(-1)
+
+
+def check_draft(model, args, cache, last, limited, device):
     """Grows a tree per sequence with the model itself, checks it in one pass and takes over the drawn path."""
     import paper_2601_18383_b200 as Dn
     batch = args.batch
@@ -254,7 +264,7 @@ def check_draft(model, args, cache, last, u, limited, device):
                 tokens.append(best[:, node, c])
         frontier = grown
     flat, up, n_new = pack()
-    chance = u.repeat_interleave(len(parents))
+    chance = draft_chances(torch.rand((batch, args.draft + 1), generator=torch.Generator(device=device).manual_seed(13), device=device), parents)
     held = cache.len(0)
     a, b = (torch.cuda.Event(enable_timing=True) for _ in range(2))
     a.record()
@@ -364,7 +374,7 @@ def run_trajectory(model, args, limited, device):
         turn = {"tokens": args.turn, "rows_before": int(held), "ms_to_first_token": round(a.elapsed_time(b), 2)}
         if limited:
             cache.evict(0)
-    draft = check_draft(model, args, cache, tokens, u, limited, device) if args.draft else None
+    draft = check_draft(model, args, cache, tokens, limited, device) if args.draft else None
     # attention alone at the end of the run: the 32 layer calls of a step on fixed q, k, v
     gq = torch.Generator(device=device).manual_seed(5)
     aq = torch.randn((batch, HQ, D), generator=gq, device=device).to(torch.bfloat16)
