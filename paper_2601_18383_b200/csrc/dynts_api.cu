@@ -2247,16 +2247,21 @@ dynts_status_t dynts_rope(const void* q, const void* k, const int* pos, void* q_
 namespace {
 
 constexpr int kSampleDevices = 64;
-std::atomic<bool> g_sample_attr[kSampleDevices][2];  // function attributes are set once per device
+std::atomic<int> g_sample_sms[kSampleDevices][2];  // a device's SMs, once the kernel's attributes are set there
 
 template <typename X>
-dynts_status_t launch_sample(const dynts::SampleParams& p, int n_rows, int which, cudaStream_t st) {
+dynts_status_t launch_sample(dynts::SampleParams& p, int n_rows, int which, cudaStream_t st) {
   int dev = -1;
   CUDA_TRY(cudaGetDevice(&dev));
-  if (dev < 0 || dev >= kSampleDevices || !g_sample_attr[dev][which]) {
+  int sms = dev >= 0 && dev < kSampleDevices ? g_sample_sms[dev][which].load() : 0;
+  if (sms == 0) {
     CUDA_TRY(cudaFuncSetAttribute(dynts::sample_kernel<X>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)dynts::kSmSmemBytes));
-    if (dev >= 0 && dev < kSampleDevices) g_sample_attr[dev][which] = true;
+    CUDA_TRY(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
+    if (dev >= 0 && dev < kSampleDevices) g_sample_sms[dev][which] = sms;
   }
+  // CTAs per row: while they fit the SMs at once, and have 2048 tokens each.
+  p.cluster = 1;
+  while (p.cluster < dynts::kSmMaxCluster && (long long)p.cluster * n_rows <= sms && p.vocab / (2 * p.cluster) >= 2048) p.cluster *= 2;
   CUDA_TRY(launch_clusters(dynts::sample_kernel<X>, (unsigned)p.cluster, dim3((unsigned)n_rows * (unsigned)p.cluster, 1, 1), dynts::kSmThreads, dynts::kSmSmemBytes, st, p));
   return DYNTS_OK;
 }
@@ -2300,9 +2305,6 @@ dynts_status_t dynts_sample(const void* logits, int dtype, int n_rows, int vocab
   p.top_p = o.top_p;
   p.min_p = o.min_p;
   p.top_k = o.top_k;
-  // CTAs per row: while they fit the SMs at once, and have 2048 tokens each.
-  p.cluster = 1;
-  while (p.cluster < dynts::kSmMaxCluster && 2ll * p.cluster * n_rows <= 2 * 148 && vocab / (2 * p.cluster) >= 2048) p.cluster *= 2;
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
   return dtype == DYNTS_FP32 ? launch_sample<float>(p, n_rows, 0, st) : launch_sample<__nv_bfloat16>(p, n_rows, 1, st);
 }
