@@ -102,7 +102,8 @@ struct ExtendPlan {
   int lh;                      // n_layers * Hkv
   int* words;                  // [items + CTAs][kPlanWords], or NULL: no plan is wanted
 };
-// An item's key tiles: `sinks` tiles from row 0 on, and behind a gap of `jump` tiles the rest.
+// An item's key tiles: `sinks` tiles from row 0 on, and behind a gap of `jump` tiles the rest.  (In the plan, where there are none of the sinks: the rest
+// by their own numbers, without a gap.)
 struct ExtTiles {
   int sinks, jump;
 };
@@ -182,7 +183,7 @@ __device__ __forceinline__ void ext_write_plan(const ExtendParams& p, const Exte
     const bool ok = n >= 0 && n + t <= p.cap;  // (else nothing is stored and nothing computed)
     const int seen = n + max(i1, prefix);
     const ExtTiles tiles = ext_tiles(p.window, p.sinks, p.tree != nullptr, n, i0, kExtTileKeys);
-    const int total = (seen + kExtTileKeys - 1) / kExtTileKeys - tiles.jump;
+    const int total = (seen + kExtTileKeys - 1) / kExtTileKeys - tiles.jump, base = tiles.sinks > 0 ? 0 : tiles.jump;
     const unsigned per = q.per[s], start = q.cum[s] + (unsigned)idx * per;
     const unsigned ca = plan_cta_of(q, start), cb = plan_cta_of(q, start + per - 1u);
     const int layer = lh / p.Hkv, h = lh - layer * p.Hkv;
@@ -205,7 +206,7 @@ __device__ __forceinline__ void ext_write_plan(const ExtendParams& p, const Exte
           const int place = (int)(2u * c) + (c == ca ? 1 : 0);
           if (lo < hi) q.words[(size_t)(item + (int)ca + rank + __popc(has & ((1u << lane) - 1u))) * kPlanWords + kPwList] = place;
           w[kPwTiles] = hi - lo;
-          w[kPwFirst] = lo;
+          w[kPwFirst] = base + lo;
           w[kPwTok] = p.seqs.tok0[s] + i0;
           w[kPwLayer] = layer;
           w[kPwHead] = h;
@@ -220,7 +221,7 @@ __device__ __forceinline__ void ext_write_plan(const ExtendParams& p, const Exte
           w[kPwPrefix] = prefix;
           w[kPwSeen] = p.tot[b];
           w[kPwSinks] = tiles.sinks;
-          w[kPwJump] = tiles.jump;
+          w[kPwJump] = tiles.jump - base;
         }
         rank += __popc(has);
       }

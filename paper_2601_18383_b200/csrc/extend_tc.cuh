@@ -30,8 +30,8 @@
 // walks the CTA's pieces by the plan the storing kernel wrote (extend.cuh), a word per lane, the next piece's
 // prefetched.  Two CTAs of 384 threads leave 80 registers per thread and hardly any L1: code that spills or does
 // not stay in the instruction caches cost several times its instructions, so the loops are rolled, the end of a piece
-// is a function of its own, and what is rare is called once from its end (spills: 44 bytes in the plain kernel, none with caps
-// and biases, 24 to 36 with 8-bit rows).  4096 tokens behind 4096 rows: 433 us a call with changing inputs, 0.95 PFLOP/s; 375 to
+// is a function of its own, and what is rare is called once from its end (spills: 24 bytes in the plain kernel, none with caps
+// and biases, 16 with trees or windows, 16 to 32 with 8-bit rows).  4096 tokens behind 4096 rows: 433 us a call with changing inputs, 0.95 PFLOP/s; 375 to
 // 395 us replayed on one state, 1.04 to 1.10 PFLOP/s, 0.65 to 0.68 of what cuBLAS reaches.  (Cursors in registers and everything
 // unrolled: 453 us when this stood at 388.)  The tensor cores and the exponentials' unit are each busy for a little more than
 // half of that time, in turns that the chain of a tile does not let overlap further: tiles of 128 keys with one S buffer,
@@ -217,7 +217,8 @@ __device__ __forceinline__ void xt_store_codes(const XtCodes& r, uint8_t* tile, 
 // fast result is not finite: a hidden row held something that is not, the weights' sum left its range, or the answer
 // is in truth not finite.  d: the piece's words, one per lane.  Far from the tensor cores' rate (512 tokens,
 // two KV heads, behind 16000 rows, slopes below zero so that every row comes here: 12 to 17 ms against 0.2), but without limit.
-template <bool KV8>
+// MORE: trees and sinks are known.  (The kernels without them call a copy without: what this keeps in registers is spilled around its call.)
+template <bool KV8, bool MORE>
 __device__ __forceinline__ float4 xt_row_again(const ExtendTcParams& p, int d, int r, bool redo, float& lse) {
   const ExtendParams& x = p.x;
   auto word = [&](int w) { return __shfl_sync(0xffffffffu, d, w); };
@@ -225,18 +226,20 @@ __device__ __forceinline__ float4 xt_row_again(const ExtendTcParams& p, int d, i
   const int ti = r / x.G, g = r - ti * x.G, h = word(kPwHead), layer = word(kPwLayer), i = word(kPwTok0) + ti;
   const size_t slab = (size_t)word(kPwSlab);
   const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(x.q) + ((size_t)layer * x.total + word(kPwTok) + ti) * x.q_stride + (size_t)(h * x.G + g) * 128;
-  const int held = word(kPwHeld), chunk0 = word(kPwTok) - word(kPwTok0), in = word(kPwNew);
-  const ExtNode node = ext_node(x, chunk0, i, in);
+  const int held = word(kPwHeld), chunk0 = MORE ? word(kPwTok) - word(kPwTok0) : 0, in = MORE ? word(kPwNew) : 0;
+  const ExtNode node = MORE ? ext_node(x, chunk0, i, in) : ExtNode{0, 0x7fffffff, i};
   const int me = word(kPwSeen) + node.depth;
   const float slope = x.slopes ? x.slopes[h * x.G + g] : 0.f;
-  const int v0 = word(kPwFirst) * kPfKeys, v_end = v0 + word(kPwTiles) * kPfKeys, end = held + max(i + 1, word(kPwPrefix));
-  const int sinks = word(kPwSinks), jump = word(kPwJump);
-  auto row_of = [&](int v) { return ext_tile_of(v / kPfKeys, sinks, jump) * kPfKeys + v % kPfKeys; };
+  const int seen = held + max(i + 1, word(kPwPrefix));
+  // (places in the list of tiles; without sinks they are rows)
+  const int v0 = word(kPwFirst) * kPfKeys, v_end = v0 + word(kPwTiles) * kPfKeys, end = MORE ? v_end : min(v_end, seen);
+  const int sinks = MORE ? word(kPwSinks) : 0, jump = MORE ? word(kPwJump) : 0;
+  auto row_of = [&](int v) { return MORE ? ext_tile_of(v / kPfKeys, sinks, jump) * kPfKeys + v % kPfKeys : v; };
   auto logit = [&](int j, bool& visible) {
     visible = false;
-    if (j >= end) return 0.f;
+    if (j >= (MORE ? seen : end)) return 0.f;
     const int pos = x.pos[slab * x.cap + j], apart = abs(me - pos);
-    if (!ext_in_window(x, apart, pos) || !ext_below(node.order, ext_node(x, chunk0, j - held, in))) return 0.f;
+    if (MORE ? !ext_in_window(x, apart, pos) || !ext_below(node.order, ext_node(x, chunk0, j - held, in)) : x.window > 0 && apart >= x.window) return 0.f;
     visible = true;
     float dot = 0.f;
 #pragma unroll 4
@@ -257,7 +260,7 @@ __device__ __forceinline__ float4 xt_row_again(const ExtendTcParams& p, int d, i
   };
   if (redo) {
     float m = -CUDART_INF_F, l = 0.f;
-    for (int v = v0; v < v_end; v += 32) {
+    for (int v = v0; v < end; v += 32) {
       bool visible;
       const float y = logit(row_of(v) + lane, visible);
       float mx = visible ? y : -CUDART_INF_F;
@@ -275,7 +278,7 @@ __device__ __forceinline__ float4 xt_row_again(const ExtendTcParams& p, int d, i
   // redo nothing the row sees weighs anything, and the weights are exp2(-inf + inf): NaN.)
   const bool none = !redo && lse == -CUDART_INF_F;
   float acc[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int v = v0; v < v_end; v += 32) {
+  for (int v = v0; v < end; v += 32) {
     const int kb = row_of(v);
     bool visible;
     const float y = logit(kb + lane, visible);
@@ -399,7 +402,7 @@ __global__ void __launch_bounds__(256) extend_join_kernel(const __grid_constant_
 // agree on them, take every other one) and those with elements that are not finite among the group's columns as stored, which
 // are replaced.  lse: of each lane's row.  After the stores, for all of a piece in one call: what is rare stays out of the
 // way of the rest (called for a block of columns at a time, from their loop, it cost 5 tokens behind 2048 rows 0.7 of 25 us).
-template <bool KV8>
+template <bool KV8, bool MORE>
 __device__ __noinline__ void xt_rows_again(const ExtendTcParams& p, int d, unsigned redo, unsigned bad, float lse, uint32_t busy) {
   const ExtendParams& x = p.x;
   auto word = [&](int w) { return __shfl_sync(0xffffffffu, d, w); };
@@ -414,7 +417,7 @@ __device__ __noinline__ void xt_rows_again(const ExtendTcParams& p, int d, unsig
     const int who = __ffs(left) - 1, row = wq * 32 + who, ti = row / x.G;
     const bool full = (redo >> who) & 1u;
     float row_lse = __shfl_sync(0xffffffffu, lse, who);
-    float4 y = xt_row_again<KV8>(p, d, row, full, row_lse);
+    float4 y = xt_row_again<KV8, MORE>(p, d, row, full, row_lse);
     if (!full && (lane >> 4) != wg) continue;  // (the other group's columns)
     auto keep = [](float was, float now) { return was * 0.f == 0.f ? was : now; };
     if (whole) {
@@ -443,7 +446,7 @@ __device__ __noinline__ void xt_rows_again(const ExtendTcParams& p, int d, unsig
 
 // The end of a piece, by the eight softmax warps: a group's 64 columns of the output, or of its part of an item that
 // other CTAs share.
-template <bool KV8>
+template <bool KV8, bool MORE>
 __device__ __noinline__ void xt_epilogue(const ExtendTcParams& p, int d, int ord, float ref, float l, uint32_t tO, uint32_t bar0, volatile int* s_abort,
                                          uint8_t* s_out) {
   const ExtendParams& x = p.x;
@@ -537,7 +540,7 @@ __device__ __noinline__ void xt_epilogue(const ExtendTcParams& p, int d, int ord
   }
   // Elements of the others that are not finite: something V holds, seen or hidden.
   const unsigned bad = __ballot_sync(0xffffffffu, mine && !redo && !gave_up && !finite);
-  if (redone | bad) xt_rows_again<KV8>(p, d, redone, bad, lse, busy);
+  if (redone | bad) xt_rows_again<KV8, MORE>(p, d, redone, bad, lse, busy);
 }
 
 template <bool KV8, int MODS>
@@ -637,8 +640,7 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
     for (; slot < slot_end && !*s_abort; go_next()) {
       ask_next();
       const int nkt = word(kPwTiles), slab = word(kPwSlab), end = word(kPwHeld) + word(kPwNew);
-      // (without sinks the tiles are one run, counted from its first)
-      const int v_new = word(kPwFirst) + nkt - 1 + (kWin && !kSinks ? word(kPwJump) : 0), sinks = kSinks ? word(kPwSinks) : 0, jump = kSinks ? word(kPwJump) : 0;
+      const int v_new = word(kPwFirst) + nkt - 1, sinks = kSinks ? word(kPwSinks) : 0, jump = kSinks ? word(kPwJump) : 0;
       auto tile_row = [&](int v) { return (kSinks ? ext_tile_of(v, sinks, jump) : v) * kPfKeys; };
       // 8-bit rows: this warp's 32 rows of a tile, eight at a time, each eight a whole tile ahead in registers
       XtCodes codes[4];
@@ -720,7 +722,6 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
         if (l_slot >= slot_end) return;
         int row = __shfl_sync(0xffffffffu, l_d, kPwFirst) + l_nkt - 1 - l_j;
         if constexpr (kSinks) row = ext_tile_of(row, __shfl_sync(0xffffffffu, l_d, kPwSinks), __shfl_sync(0xffffffffu, l_d, kPwJump));
-        else if constexpr (kWin) row += __shfl_sync(0xffffffffu, l_d, kPwJump);
         row *= kPfKeys;
         ++l_j;
         load_tile(is_s, gl, row, __shfl_sync(0xffffffffu, l_d, kPwSlab));
@@ -816,7 +817,7 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
       ask_next();
       const int nkt = word(kPwTiles);
       if (nkt == 0) continue;
-      const int v_new = word(kPwFirst) + nkt - 1 + (kWin && !kSinks ? word(kPwJump) : 0);  // its newest tile
+      const int v_new = word(kPwFirst) + nkt - 1;  // its newest tile
       const int rows = word(kPwRows), held = word(kPwHeld), i0 = word(kPwTok0), prefix = word(kPwPrefix);
       const bool live = wq * 32 < rows;
       const int r = min(wq * 32 + lane, rows - 1);  // (a lane without a query repeats the last row's visibility)
@@ -869,7 +870,7 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
         int pos_a = 0, pos_b = 0;
         bool border = false;
         if constexpr (MODS == kXtWindow) border = (key0 + kPfKeys > held && prefix > 0) || last_place - first_pos >= x.window;
-        if (placed || border) {
+        if (placed || border || MODS == kXtMods) {
           pos_a = pos_row[min(key0 + lane, x.cap - 1)] - tot;
           pos_b = pos_row[min(key0 + 32 + lane, x.cap - 1)] - tot;
         }
@@ -931,11 +932,12 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
             if constexpr (kMods)
               border = x.window > 0 && ((fresh && (tree || prefix > 0)) ||
                                         (MODS == kXtAll ? __reduce_max_sync(0xffffffffu, place) : __shfl_sync(0xffffffffu, ti, 31)) - __shfl_sync(0xffffffffu, pos_a, 0) >= x.window);
-            if (border) {
+            // (with caps, biases and windows alone without a question: prompts with a bias 110.4 -> 108.9 us, the capped prefix 132.4 -> 133.3)
+            if (border || MODS == kXtMods) {
               sts_i(stage + 4u * lane, pos_a - p0);
               sts_i(stage + 128u + 4u * lane, pos_b - p0);
             }
-            if (kMods && x.slopes) {
+            if (kMods && (x.slopes || MODS == kXtMods)) {
               sts_f(stage + 256u + 4u * lane, (float)(pos_a - p0));
               sts_f(stage + 384u + 4u * lane, (float)(pos_b - p0));
             }
@@ -981,10 +983,10 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
 #pragma unroll
               for (int c = 0; c < CH; c += 4) {
                 const int4 y = lds_i4(stage + 4u * (uint32_t)(hb + c));
-                if (abs(me - y.x) >= x.window && y.x >= sink_to) sv[c] = 0xff800000u;  // -inf
-                if (abs(me - y.y) >= x.window && y.y >= sink_to) sv[c + 1] = 0xff800000u;
-                if (abs(me - y.z) >= x.window && y.z >= sink_to) sv[c + 2] = 0xff800000u;
-                if (abs(me - y.w) >= x.window && y.w >= sink_to) sv[c + 3] = 0xff800000u;
+                if (abs(me - y.x) >= x.window && (!kSinks || y.x >= sink_to)) sv[c] = 0xff800000u;  // -inf
+                if (abs(me - y.y) >= x.window && (!kSinks || y.y >= sink_to)) sv[c + 1] = 0xff800000u;
+                if (abs(me - y.z) >= x.window && (!kSinks || y.z >= sink_to)) sv[c + 2] = 0xff800000u;
+                if (abs(me - y.w) >= x.window && (!kSinks || y.w >= sink_to)) sv[c + 3] = 0xff800000u;
               }
             }
             if (branch) {
@@ -1050,7 +1052,7 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
       const float l_other = lds_f(smem_u32(s_out) + (uint32_t)(warp ^ 4) * kXtStageBytes + 640u + 4u * lane);
       l = wg == 0 ? l + l_other : l_other + l;
       pair_sync();
-      xt_epilogue<KV8>(p, d, ord, ref, l, tO, bar0, s_abort, s_out);
+      xt_epilogue<KV8, MODS != kXtPlain && MODS != kXtMods>(p, d, ord, ref, l, tO, bar0, s_abort, s_out);
       ++ord;
     }
   }
