@@ -161,7 +161,8 @@ struct dynts_cache {
   char* stage_dev = nullptr;
   size_t stage_bytes = 0;
   bool attr_generic_f32 = false, attr_generic_bf16 = false, attr_generic_kv8 = false, attr_mma = false, attr_select = false;
-  bool attr_stream = false, attr_fused = false, attr_prefill = false, attr_extend = false;
+  bool attr_stream = false, attr_fused = false, attr_prefill = false;
+  bool attr_extend[2] = {false, false};
   bool attr_extend_tc[2][5] = {};
   bool attr_extend_few[2][2][5] = {};
   bool have_maps = false;    // tensor maps of the K and V slabs for the streaming kernel
@@ -1497,16 +1498,16 @@ cudaError_t launch_dependent(Kern kern, dim3 grid, unsigned threads, size_t smem
   return launch_dependent_clusters(kern, 1, grid, threads, smem, st, args...);
 }
 
-template <typename T, bool KV8>
-dynts_status_t launch_extend_generic(dynts_cache* c, dynts::ExtendParams& p, bool want_mass) {
+template <typename T, bool KV8, bool MORE>
+dynts_status_t launch_extend_generic_as(dynts_cache* c, dynts::ExtendParams& p, bool want_mass) {
   const int d = p.d;
   const size_t smem = dynts::ext_generic_smem(d), smem_m = dynts::ext_generic_mass_smem(d);
-  if (!c->attr_extend) {  // (the largest head size's need: the attribute belongs to the kernel, not to the cache)
-    CUDA_TRY(cudaFuncSetAttribute(dynts::extend_generic_kernel<T, KV8>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+  if (!c->attr_extend[MORE]) {  // (the largest head size's need: the attribute belongs to the kernel, not to the cache)
+    CUDA_TRY(cudaFuncSetAttribute(dynts::extend_generic_kernel<T, KV8, MORE>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                   (int)dynts::ext_generic_smem(256)));
-    CUDA_TRY(cudaFuncSetAttribute(dynts::extend_generic_mass_kernel<T, KV8>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+    CUDA_TRY(cudaFuncSetAttribute(dynts::extend_generic_mass_kernel<T, KV8, MORE>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                   (int)dynts::ext_generic_mass_smem(256)));
-    c->attr_extend = true;
+    c->attr_extend[MORE] = true;
   }
   const int n_seq = p.seqs.n;
   p.seqs.item0[0] = 0;
@@ -1522,22 +1523,36 @@ dynts_status_t launch_extend_generic(dynts_cache* c, dynts::ExtendParams& p, boo
   if (p.window > 0) longest = std::min<long long>(longest, (long long)p.window + dynts::kExtGenericRows + p.sinks);
   unsigned cluster = 1;
   while (cluster < 8 && (long long)p.seqs.item0[n_seq] * ny * cluster * 2 <= c->sm_count && (long long)cluster * dynts::kExtGenericKeys < longest) cluster *= 2;
-  CUDA_TRY(launch_dependent_clusters(dynts::extend_generic_kernel<T, KV8>, cluster, dim3((unsigned)p.seqs.item0[n_seq] * cluster, ny, 1),
-                                     dynts::kExtGenericThreads, smem, c->stream, p, (int)cluster));
-  c->launches += 1;
+  // The mass: its grid is over the capacity, not over the host's copy of the lengths (a replayed graph may hold longer sequences).  In clusters while
+  // their CTAs stay below two per SM (those behind the rows held end at once) and each has query rows to take.
+  const unsigned nx = (unsigned)((c->cap + dynts::kExtGenericKeys - 1) / dynts::kExtGenericKeys);
+  unsigned share = 1;
   if (want_mass) {
-    // grid over the capacity, not over the host's copy of the lengths: a replayed graph may hold longer sequences
-    const unsigned nx = (unsigned)((c->cap + dynts::kExtGenericKeys - 1) / dynts::kExtGenericKeys);
-    // Clusters while their CTAs stay below two per SM (those behind the rows held end at once) and each has query rows to take.
     int longest_t = 0;
     for (int s = 0; s < n_seq; ++s) longest_t = std::max(longest_t, p.seqs.tok0[s + 1] - p.seqs.tok0[s]);
-    unsigned share = 1;
     while (share < 8 && (long long)nx * ny * n_seq * share * 2 <= 2ll * c->sm_count && (long long)longest_t * c->G > (long long)share * dynts::kExtGenericRows) share *= 2;
-    CUDA_TRY(launch_dependent_clusters(dynts::extend_generic_mass_kernel<T, KV8>, share, dim3(nx * share, ny, (unsigned)n_seq), dynts::kExtGenericThreads, smem_m, c->stream, p,
-                                       (int)share));
+  }
+  // A small mass kernel begins beside the end of its attention.  A larger one does not: its CTAs would gather on the SMs that are free first (4
+  // sequences of 200 tokens behind 1000 rows of 128, 304 CTAs: 597 us against 500).
+  CUDA_TRY(launch_dependent_clusters(dynts::extend_generic_kernel<T, KV8, MORE>, cluster, dim3((unsigned)p.seqs.item0[n_seq] * cluster, ny, 1),
+                                     dynts::kExtGenericThreads, smem, c->stream, p, (int)cluster, share > 1 ? 1 : 0));
+  c->launches += 1;
+  if (want_mass) {
+    const dim3 grid(nx * share, ny, (unsigned)n_seq);
+    if (share > 1)
+      CUDA_TRY(launch_dependent_clusters(dynts::extend_generic_mass_kernel<T, KV8, MORE>, share, grid, dynts::kExtGenericThreads, smem_m, c->stream, p, (int)share));
+    else
+      CUDA_TRY(launch_clusters(dynts::extend_generic_mass_kernel<T, KV8, MORE>, 1, grid, dynts::kExtGenericThreads, smem_m, c->stream, p, 1));
     c->launches += 1;
   }
   return DYNTS_OK;
+}
+
+// Trees and sinks have instances of their own: 8 sequences of 100 tokens behind 2000 rows of head_dim 64, 1070 us with their tests, 1035 without
+// (with the mass 1463 and 1348).
+template <typename T, bool KV8>
+dynts_status_t launch_extend_generic(dynts_cache* c, dynts::ExtendParams& p, bool want_mass) {
+  return p.tree || p.sinks > 0 ? launch_extend_generic_as<T, KV8, true>(c, p, want_mass) : launch_extend_generic_as<T, KV8, false>(c, p, want_mass);
 }
 
 // Tensor maps of the K and V slabs, [slabs][cap][128] bf16 in boxes of 64 rows x 64 elements: made once per cache.

@@ -371,6 +371,11 @@ __device__ __forceinline__ ExtNode ext_node(const ExtendParams& p, int tok0, int
   }
   return e;
 }
+template <bool MORE>  // false: no tree, and no sinks
+__device__ __forceinline__ ExtNode ext_node_if(const ExtendParams& p, int tok0, int i, int in) {
+  if constexpr (MORE) return ext_node(p, tok0, i, in);
+  return ExtNode{0, 0x7fffffff, i};
+}
 __device__ __forceinline__ bool ext_below(int order, const ExtNode& row) { return (unsigned)(order - row.order) < (unsigned)row.size; }
 
 // tanh(y) = y P(y^2) for |y| up to 3/4, P of degree 5 and the least greatest relative error there (3e-8, below a rounding): its coefficients.
@@ -431,8 +436,8 @@ constexpr size_t ext_generic_smem(int d) {  // Q [32][d], K [32][d + 4], V [32][
 // steps, so the key tiles of an item are dealt to a cluster of up to eight CTAs, which join their parts through
 // one another's shared memory, in the order of their ranks (fp32, head_dim 64, 48 tokens behind 131 rows, six items:
 // 44 us with a CTA per item, 11 to 12 us with clusters, the storing kernel included).
-template <typename T, bool KV8>
-__global__ void __launch_bounds__(kExtGenericThreads) extend_generic_kernel(const __grid_constant__ ExtendParams p, int cluster) {
+template <typename T, bool KV8, bool MORE>
+__global__ void __launch_bounds__(kExtGenericThreads) extend_generic_kernel(const __grid_constant__ ExtendParams p, int cluster, int early) {
   extern __shared__ __align__(16) float ext_sm[];
   const int d = p.d, ldk = d + 4, pieces = d / 4;
   float* sQ = ext_sm;
@@ -443,7 +448,7 @@ __global__ void __launch_bounds__(kExtGenericThreads) extend_generic_kernel(cons
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int item = (int)blockIdx.x / cluster, rank = (int)blockIdx.x - item * cluster;
   const unsigned piece_inv = 65536u / (unsigned)pieces + 1u;  // x / pieces = (x * piece_inv) >> 16 for x < 256 and up to 64 pieces
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  if (early) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // (see the launch)
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const int s = ext_find(p.seqs.item0, p.seqs.n, item);
   const ExtSeq e = ext_seq(p, s);
@@ -469,7 +474,7 @@ __global__ void __launch_bounds__(kExtGenericThreads) extend_generic_kernel(cons
   for (int u = 0; u < 4; ++u) {
     const int r = r0 + warp * 4 + u;
     tok[u] = min(r / p.G, e.t - 1);
-    const ExtNode node = ext_node(p, p.seqs.tok0[s], tok[u], e.t);
+    const ExtNode node = ext_node_if<MORE>(p, p.seqs.tok0[s], tok[u], e.t);
     at[u] = node.depth;
     order[u] = node.order;
     slope[u] = p.slopes ? p.slopes[h * p.G + r % p.G] : 0.f;
@@ -481,9 +486,9 @@ __global__ void __launch_bounds__(kExtGenericThreads) extend_generic_kernel(cons
   const int prefix = p.seqs.prefix[s];
   const int i0 = r0 / p.G, i1 = min(e.t - 1, (r0 + rows - 1) / p.G);
   const int end = e.n + max(i1 + 1, prefix);
-  const ExtTiles tiles = ext_tiles(p.window, p.sinks, p.tree != nullptr, e.n, i0, kExtGenericKeys);
+  const ExtTiles tiles = ext_tiles(p.window, MORE ? p.sinks : 0, MORE && p.tree != nullptr, e.n, i0, kExtGenericKeys);
   for (int v = rank;; v += cluster) {
-    const int k0 = ext_tile_of(v, tiles.sinks, tiles.jump) * kExtGenericKeys;
+    const int k0 = (MORE ? ext_tile_of(v, tiles.sinks, tiles.jump) : v + tiles.jump) * kExtGenericKeys;
     if (k0 >= end) break;
     __syncthreads();
 #pragma unroll 2
@@ -512,12 +517,12 @@ __global__ void __launch_bounds__(kExtGenericThreads) extend_generic_kernel(cons
       }
     }
     const int j = k0 + lane;
-    const ExtNode row = ext_node(p, p.seqs.tok0[s], j - e.n, e.t);
+    const ExtNode row = ext_node_if<MORE>(p, p.seqs.tok0[s], j - e.n, e.t);
     float w[4];
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
       const int apart = abs(e.tot + at[u] - sP[lane]);
-      const bool visible = j < e.n + max(tok[u] + 1, prefix) && ext_in_window(p, apart, sP[lane]) && ext_below(order[u], row);
+      const bool visible = j < e.n + max(tok[u] + 1, prefix) && (MORE ? ext_in_window(p, apart, sP[lane]) && ext_below(order[u], row) : p.window == 0 || apart < p.window);
       const float x = visible ? ext_logit_exact(p, dot[u], slope[u], apart) : -CUDART_INF_F;
       float mx = x;
 #pragma unroll
@@ -637,7 +642,7 @@ constexpr size_t ext_generic_mass_smem(int d) {  // K [32][d + 4], four query ro
 // K for four products), lane = key; the eight partial sums are added in a fixed order.  Small calls take a cluster of CTAs per 32 rows,
 // which share the query rows out and add their sums up in the order of the ranks (164 query rows of 64 columns against 172 rows: 18 us
 // without, 6.5 with eight CTAs).
-template <typename T, bool KV8>
+template <typename T, bool KV8, bool MORE>
 __global__ void __launch_bounds__(kExtGenericThreads) extend_generic_mass_kernel(const __grid_constant__ ExtendParams p, const int cluster) {
   extern __shared__ __align__(16) float ext_sm[];
   const int d = p.d, ldk = d + 4, pieces = d / 4;
@@ -646,7 +651,6 @@ __global__ void __launch_bounds__(kExtGenericThreads) extend_generic_mass_kernel
   float* sS = sQ + kExtGenericRows * d;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const unsigned piece_inv = 65536u / (unsigned)pieces + 1u;  // x / pieces = (x * piece_inv) >> 16 for x < 256 and up to 64 pieces
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const int layer = blockIdx.y / p.Hkv, h = blockIdx.y % p.Hkv, s = blockIdx.z;
   const ExtSeq e = ext_seq(p, s);
@@ -665,20 +669,22 @@ __global__ void __launch_bounds__(kExtGenericThreads) extend_generic_mass_kernel
   __syncthreads();
   const int j = k0 + lane;
   const int pj = j < e.n + e.t ? p.pos[slab * p.cap + j] : 0;
-  const ExtNode row = ext_node(p, p.seqs.tok0[s], j - e.n, e.t);
+  const ExtNode row = ext_node_if<MORE>(p, p.seqs.tok0[s], j - e.n, e.t);
   const int prefix = p.seqs.prefix[s], all = e.t * p.G;
   // (a token that sees row j: i >= j - n, or any where j lies before n + prefix)
   const int first = e.n + prefix > k0 ? 0 : max(0, k0 - e.n) * p.G;
   float* q4 = sQ + warp * 4 * d;
   float sum = 0.f;
   for (int r = first + rank * kExtGenericRows + 4 * warp; r < all; r += cluster * kExtGenericRows) {
-    float log_sum[4];
-    ExtNode node[4];
+    [[maybe_unused]] float log_sum[4];
+    [[maybe_unused]] ExtNode node[4];
+    if constexpr (MORE) {
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {  // (asked for before the products)
-      const int qr = min(r + u, all - 1);
-      log_sum[u] = lse[qr];
-      node[u] = ext_node(p, p.seqs.tok0[s], qr / p.G, e.t);
+      for (int u = 0; u < 4; ++u) {  // (asked for before the products)
+        const int qr = min(r + u, all - 1);
+        log_sum[u] = lse[qr];
+        node[u] = ext_node(p, p.seqs.tok0[s], qr / p.G, e.t);
+      }
     }
     __syncwarp();
 #pragma unroll 2
@@ -702,9 +708,9 @@ __global__ void __launch_bounds__(kExtGenericThreads) extend_generic_mass_kernel
     for (int u = 0; u < 4; ++u) {
       if (r + u >= all) break;
       const int i = (r + u) / p.G, head = h * p.G + r + u - i * p.G;
-      const int apart = abs(e.tot + node[u].depth - pj);
-      if (j < e.n + max(i + 1, prefix) && ext_in_window(p, apart, pj) && ext_below(node[u].order, row))
-        sum += exp2f(ext_logit_exact(p, dot[u], p.slopes ? p.slopes[head] : 0.f, apart) - log_sum[u]);
+      const int apart = abs(e.tot + (MORE ? node[u].depth : i) - pj);
+      if (j < e.n + max(i + 1, prefix) && (MORE ? ext_in_window(p, apart, pj) && ext_below(node[u].order, row) : p.window == 0 || apart < p.window))
+        sum += exp2f(ext_logit_exact(p, dot[u], p.slopes ? p.slopes[head] : 0.f, apart) - (MORE ? log_sum[u] : lse[r + u]));
     }
   }
   sS[warp * kExtGenericKeys + lane] = sum;
