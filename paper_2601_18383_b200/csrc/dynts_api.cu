@@ -1584,10 +1584,17 @@ dynts_status_t extend_maps(dynts_cache* c) {
 template <bool KV8, int MODS>
 dynts_status_t launch_extend_tc_as(dynts_cache* c, dynts::ExtendTcParams& p, unsigned grid, bool whole, const CUtensorMap& mq, bool want_mass) {
   bool* attr = &c->attr_extend_tc[KV8 ? 1 : 0][MODS];
-  constexpr bool kMassMods = MODS != dynts::kXtPlain;
+  // (the mass: plain, with caps, biases and windows, or with trees and sinks too)
+  auto* mass = MODS == dynts::kXtPlain ? dynts::extend_mass_tc_kernel<KV8, dynts::kXtPlain>
+               : p.x.tree || p.x.sinks > 0 ? dynts::extend_mass_tc_kernel<KV8, dynts::kXtAll> : dynts::extend_mass_tc_kernel<KV8, dynts::kXtMods>;
   if (!*attr) {
     CUDA_TRY(cudaFuncSetAttribute(dynts::extend_tc_kernel<KV8, MODS>, cudaFuncAttributeMaxDynamicSharedMemorySize, dynts::kXtSmemBytes));
-    CUDA_TRY(cudaFuncSetAttribute(dynts::extend_mass_tc_kernel<KV8, kMassMods>, cudaFuncAttributeMaxDynamicSharedMemorySize, dynts::kXmSmemBytes));
+    if (MODS == dynts::kXtPlain)
+      CUDA_TRY(cudaFuncSetAttribute(dynts::extend_mass_tc_kernel<KV8, dynts::kXtPlain>, cudaFuncAttributeMaxDynamicSharedMemorySize, dynts::kXmSmemBytes));
+    else {
+      CUDA_TRY(cudaFuncSetAttribute(dynts::extend_mass_tc_kernel<KV8, dynts::kXtMods>, cudaFuncAttributeMaxDynamicSharedMemorySize, dynts::kXmSmemBytes));
+      CUDA_TRY(cudaFuncSetAttribute(dynts::extend_mass_tc_kernel<KV8, dynts::kXtAll>, cudaFuncAttributeMaxDynamicSharedMemorySize, dynts::kXmSmemBytes));
+    }
     *attr = true;
   }
   CUDA_TRY(launch_dependent(dynts::extend_tc_kernel<KV8, MODS>, dim3(grid, 1, 1), (unsigned)dynts::XtShape<KV8, MODS>::kThreads, dynts::kXtSmemBytes, c->stream, p, mq, c->map_XK, c->map_XV));
@@ -1597,7 +1604,7 @@ dynts_status_t launch_extend_tc_as(dynts_cache* c, dynts::ExtendTcParams& p, uns
     c->launches += 1;
   }
   if (want_mass) {
-    CUDA_TRY(launch_dependent(dynts::extend_mass_tc_kernel<KV8, kMassMods>, dim3((unsigned)(2 * c->sm_count), 1, 1), dynts::kXmThreads, dynts::kXmSmemBytes, c->stream, p, mq,
+    CUDA_TRY(launch_dependent(mass, dim3((unsigned)(2 * c->sm_count), 1, 1), dynts::kXmThreads, dynts::kXmSmemBytes, c->stream, p, mq,
                               c->map_XK));
     c->launches += 1;
   }

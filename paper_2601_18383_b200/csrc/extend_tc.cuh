@@ -1128,9 +1128,10 @@ __device__ __forceinline__ void xm_seek(XmCursor& c, int it, int n_items, const 
   c.it = it;
 }
 
-template <bool KV8, bool MODS>
+template <bool KV8, int HOW>
 __global__ void __launch_bounds__(kXmThreads, 2)
 extend_mass_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK) {
+  constexpr bool MODS = HOW != kXtPlain, ALL = HOW == kXtAll;
   extern __shared__ __align__(1024) uint8_t pf_smem[];
   uint8_t* sm = pf_smem;
   const uint32_t sK = smem_u32(sm);             // [2 groups][2 halves of head_dim][128 rows][128 B]
@@ -1331,14 +1332,14 @@ extend_mass_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_con
       // the tokens that see row j: [i_lo, i_hi)
       int i_lo = j < cur.n + prefix ? 0 : j - cur.n, i_hi = mine ? cur.t : 0;
       float rel = 0.f;
-      const bool tree = MODS && x.tree != nullptr;
+      const bool tree = ALL && x.tree != nullptr;
       ExtNode mine_node{0, 0x7fffffff, 0};
       bool sink = true;  // no window concerns the row
       int at = 0;
       if constexpr (MODS) {
         at = mine ? x.pos[row] - x.held[kExtSeqs + cur.s] : 0;  // the row's position, the chunk's first token being 0
         rel = (float)at;
-        sink = x.window == 0 || at + x.held[kExtSeqs + cur.s] < x.sinks;
+        sink = x.window == 0 || (ALL && at + x.held[kExtSeqs + cur.s] < x.sinks);
         if (tree) {
           mine_node = ext_node(x, x.seqs.tok0[cur.s], j - cur.n, cur.t);
         } else if (!sink) {
@@ -1434,7 +1435,7 @@ extend_mass_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_con
 #pragma unroll
                 for (int u = 0; u < 4; ++u)
                   if (hb + c + u < c_lo || hb + c + u >= c_hi) y[u] = -CUDART_INF_F;  // weight 0, whatever the logit is
-                if constexpr (MODS) {
+                if constexpr (ALL) {
                   if (tree) {
 #pragma unroll
                     for (int u = 0; u < 4; ++u) {
