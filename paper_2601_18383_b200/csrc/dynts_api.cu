@@ -1749,45 +1749,67 @@ dynts_status_t launch_extend_tc(dynts_cache* c, const dynts::ExtendParams& x, co
 }
 
 // Whether few query rows go by extend_few_kernel, in how many clusters per slab (`split`, 32 query rows each), and the CTAs of a cluster: as many
-// as fit the GPU at once and have four tiles each (by the host's copy of the lengths, which only guides the choice).  A CTA takes 0.42 us per
-// tile of 32 rows for up to 16 query rows, 0.48 for 32, 0.95 for 64 (the chain of a tile; two groups of warps for the first two), and 8 us
-// beside; the storing, tensor-core and joining kernels take 22 us and 0.75 us per tile of 64 rows and CTA.  Measured (us, this kernel / the
-// three): 8 KV heads of 2048 rows, 4 query rows 10 / 21, 20 rows 13 / 22, 48 rows 16.5 / 23, 100 rows in four clusters 18 / 24; of 16000 rows,
-// 48 query rows 61 / 46; 64 sequences of 1000 to 2111 rows, 4 rows 72 / 81, 16 rows 78 / 85, 32 rows 124 / 90; 8 sequences, 32 rows 23 / 27; 33
-// sequences of 380, 60 rows 44 / 20; 8-bit, 16 sequences of 4200, 14 rows 23 / 41, 63 rows 69 / 47.
+// as fit the GPU at once and have four tiles each (by the host's copy of the lengths, which only guides the choice).  Both sides' times are
+// estimated in us from fits to 3568 calls (16 to 4100 rows held, 1 to 128 sequences, 4 to 128 query rows, 8, 4 and 1 KV heads), at 6.3 TB/s
+// at best:
+//   this kernel: a wave of CTAs takes `fix`, and `tile` per tile of 32 rows, with the SMs full (1 + `crowd`) times that (the 8 query rows of a
+//   warp four, three, two or one CTA per SM, or two of 32 rows' clusters).  A wave beyond the first costs as much again.
+//   the others (storing, tensor cores, joining): whole items of a query tile, or items cut into parts of four key tiles and more.
+// Within 8 % in the mean (the cut 11 %); by the smaller estimate 1 % of those calls took 3 % or more longer than by the other kernels, none of them
+// in more waves than one.  Measured (us, this kernel / the others): 8 KV heads of 2048 rows, 4 query rows 10 / 21, 20 rows 13 / 22, 48
+// rows 17 / 23; 64 sequences of 1500 rows, 4 rows 60 / 81; 33 sequences of 48 rows and 8 heads, 128 rows 84 / 16; 16 sequences of 183 to
+// 366, 36 rows 25 / 16.
 constexpr int kFewCluster = 8, kFewTiles = 4;
+struct FewCost {
+  int per_sm;
+  double fix, tile, crowd;
+};
 bool plan_few(const dynts_cache* c, const dynts::ExtendParams& x, int rows, int* cluster, int* split) {
   if (rows > dynts::kFewMaxRows) return false;
-  long long slabs = 0, tiles = 0, small = 0, longest = 0;  // tiles of 64 and of 32 rows
+  const bool kv8 = c->cfg.dtype == DYNTS_BF16_KV8;
+  const long long lh = (long long)x.n_layers * x.Hkv;
+  long long slabs = 0, keys = 0, tiles = 0, small = 0, longest = 0, q_rows = 0;  // tiles of 64 and of 32 rows
   for (int s = 0; s < x.seqs.n; ++s) {
     const int t = x.seqs.tok0[s + 1] - x.seqs.tok0[s];
     if (t == 0) continue;
     long long n = c->len_h[x.seqs.b0 + s] + t;
     if (x.window > 0) n = std::min<long long>(n, (long long)x.window + x.sinks + 2 * dynts::kFewKeys);
-    slabs += (long long)x.n_layers * x.Hkv;
-    tiles += (long long)x.n_layers * x.Hkv * ((n + 63) / 64);
-    small += (long long)x.n_layers * x.Hkv * ((n + dynts::kFewKeys - 1) / dynts::kFewKeys);
+    slabs += lh;
+    keys += lh * n;
+    tiles += lh * ((n + 63) / 64);
+    small += lh * ((n + dynts::kFewKeys - 1) / dynts::kFewKeys);
     longest = std::max(longest, (n + dynts::kFewKeys - 1) / dynts::kFewKeys);
+    q_rows += lh * t * c->G;
   }
-  const double tc = 22 + 0.75 * (double)tiles / (2.0 * c->sm_count);
-  // The time with the query rows in so many parts, at the cost of a tile of 32 rows for one of them; k: a cluster's CTAs.
-  auto time = [&](int parts, int per_sm, double tile, int* k) {
-    const long long slots = (long long)c->sm_count * per_sm;
+  const double sms = c->sm_count, ctas = 2 * sms, read = (double)keys * (kv8 ? 256 : 512) / 6.3e6;
+  // the others
+  const double avg = (double)tiles / slabs, most = (longest + 1) / 2, cut = std::max(1.0, std::min(ctas, std::floor(tiles / 4.0))), kr = q_rows / 1000.0, part = cut / slabs * rows / 1000;
+  const double waves = std::ceil(slabs / ctas);
+  const double whole = kv8 ? std::max(6 + 0.25 * kr + waves * (4.4 + 1.33 * avg) + 0.7 * (most - avg), 8 + read) : std::max(6.2 + 0.19 * kr + waves * (3.6 + 0.75 * avg) + 0.4 * (most - avg), 10.5 + read);
+  const double parts = kv8 ? std::max(12.3 + 1.38 * tiles / cut + 0.42 * kr + 9.1 * cut / ctas + 8 * part, 3.5 + read)
+                           : std::max(9.5 + 1.5 * tiles / cut + 0.25 * kr + (7.6 + 0.5 * rows / 128) * cut / ctas + 8 * part, 5.5 + read);
+  const double others = std::min(whole, parts);
+  // this one, with the query rows in so many clusters
+  auto time = [&](int n_parts, const FewCost& cost, int* k) {
+    const double slots = sms * cost.per_sm;
     *k = 1;
     // (Clusters of eight with an SM for each CTA: more than eight were measured as sixteen, which do not fit the GPCs at once.  32 query rows, 16 slabs of
     // 2048 rows: 25.6 us, in clusters of four 16.6.)
-    while (*k < kFewCluster && 2ll * *k * slabs * parts <= slots && longest / (2 * *k) >= kFewTiles && (*k < 4 || per_sm > 1 || slabs * parts <= 8)) *k *= 2;
-    return 8 + tile * std::max((double)((longest + *k - 1) / *k), (double)small * parts / slots);
+    while (*k < kFewCluster && 2.0 * *k * slabs * n_parts <= slots && longest / (2 * *k) >= kFewTiles && (*k < 4 || cost.per_sm > 1 || slabs * n_parts <= 8)) *k *= 2;
+    const double n_ctas = (double)slabs * n_parts * *k, room = cost.per_sm == 3 && n_ctas > slots ? 4 * sms : slots;  // (see launch_extend_few)
+    const double tile = cost.tile * (1 + cost.crowd * std::min(1.0, n_ctas / room)), mean = (double)small / slabs;
+    return std::max(std::max(cost.fix + tile * ((longest + *k - 1) / *k), std::ceil(n_ctas / room) * (cost.fix + tile * mean / *k)), 6 + read);
   };
-  double best = rows <= 8 ? time(1, 3, 0.42, cluster) : rows <= 16 ? time(1, 2, 0.42, cluster) : rows <= 32 ? time(1, 1, 0.48, cluster) : rows <= 64 ? time(1, 1, 0.95, cluster) : 1e30;
+  static const FewCost one[4] = {{3, 5.9, 0.26, 2.2}, {2, 8.2, 0.26, 1.4}, {1, 8.4, 0.42, 0.2}, {1, 10.7, 0.33, 2.0}}, several = {1, 9.3, 0.39, 0.35};
+  double best = rows <= 64 ? time(1, one[rows <= 8 ? 0 : rows <= 16 ? 1 : rows <= 32 ? 2 : 3], cluster) : 1e30;
   *split = 1;
   if (rows > dynts::kFewSplitRows) {
-    const int parts = (rows + dynts::kFewSplitRows - 1) / dynts::kFewSplitRows;
+    const int n_parts = (rows + dynts::kFewSplitRows - 1) / dynts::kFewSplitRows;
     int k = 1;
-    const double t = time(parts, 1, 0.48, &k);
-    if (t < best) best = t, *cluster = k, *split = parts;
+    const double t = time(n_parts, several, &k);
+    if (t < best) best = t, *cluster = k, *split = n_parts;
   }
-  return best <= tc;
+  return best <= others;
 }
 
 template <bool KV8, bool MODS, int NB, int RG, int KA, int PS>
