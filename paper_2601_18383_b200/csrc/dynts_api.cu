@@ -1633,7 +1633,7 @@ dynts_status_t plan_extend(const dynts_cache* c, const dynts::ExtendParams& x, c
     const int t = x.seqs.tok0[s + 1] - x.seqs.tok0[s];
     p.tiles[s] = (t + tpt - 1) / tpt;
     p.turn[s] = 0;
-    if (x.window > 0 && p.tiles[s] > 2 && p.tiles[s] < 65536) {  // (a place in the list times the step stays below 2^32)
+    if (x.window > 0 && x.seqs.prefix[s] == 0 && p.tiles[s] > 2 && p.tiles[s] < 65536) {  // (a place in the list times the step stays below 2^32)
       int m = (int)(0.618 * p.tiles[s]);
       while (std::gcd(m, p.tiles[s]) != 1) ++m;
       p.turn[s] = m;
@@ -1736,7 +1736,11 @@ dynts_status_t launch_extend_tc(dynts_cache* c, const dynts::ExtendParams& x, co
                                box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   if (r != CUDA_SUCCESS) return fail(DYNTS_ERR_CUDA, "cuTensorMapEncodeTiled failed (%d)", (int)r);
-  const bool mods = x.cap_logit > 0.f || x.slopes || (x.window > 0 && x.tree);
+  // A narrow window alone goes by the kernel that reads all positions beforehand: nearly all of its tiles are at a border (2000 tokens of 28 / 4 heads, window
+  // of 64: 26.5 us and 29.4 by the other; mean of 72 calls, of what they took when all windows went that way: window 64 0.96 and 1.01, 256 0.92 and 0.93,
+  // 384 0.92 and 0.91, 1000 0.92 and 0.89; 8-bit rows 64 0.945 and 0.953, 192 0.913 and 0.904).
+  const bool narrow = x.window > 0 && x.sinks == 0 && x.window <= (kv8 ? 64 : 256);
+  const bool mods = x.cap_logit > 0.f || x.slopes || (x.window > 0 && x.tree) || narrow;
   auto launch = [&](auto how) {
     constexpr int M = decltype(how)::value;
     return kv8 ? launch_extend_tc_as<true, M>(c, p, grid, whole, map, want_mass) : launch_extend_tc_as<false, M>(c, p, grid, whole, map, want_mass);

@@ -176,7 +176,8 @@ __device__ __forceinline__ void ext_write_plan(const ExtendParams& p, const Exte
     const int idx = item - q.item0[s], nq = q.tiles[s], lh = idx / nq, o = idx - lh * nq;
     // Tiles from both ends in turn: neighbours in the list hold about as many key tiles together as any other two.  With a window, where
     // the number grows only up to the window's, in steps of 0.62 of the tiles around (prime to them): any run of the list has its
-    // share of early ones (a prompt of 8000 tokens with a window of 4096: 727 -> 652 us).
+    // share of early ones (a prompt of 8000 tokens with a window of 4096: 727 -> 652 us).  Beside a prefix from both ends: a tile's number falls
+    // with its place up to the prefix's end.
     const int qt = q.turn[s] > 0 ? (int)((unsigned)o * (unsigned)q.turn[s] % (unsigned)nq) : (o & 1) ? nq - 1 - (o >> 1) : o >> 1;
     const int b = p.seqs.b0 + s, t = p.seqs.tok0[s + 1] - p.seqs.tok0[s], n = p.len[b], prefix = p.seqs.prefix[s];
     const int i0 = qt * q.tokens_per_tile, i1 = min(t, i0 + q.tokens_per_tile);

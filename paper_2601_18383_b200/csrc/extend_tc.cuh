@@ -848,9 +848,10 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
       const int end = held + word(kPwNew);
       float ref = -CUDART_INF_F, l = 0.f;
       int j = wg == 0 ? 0 : ramp;
-      int last_place = 0, first_pos = 0;
+      int last_place = 0, first_place = 0, first_pos = 0;
       if constexpr (MODS == kXtWindow) {
         last_place = __shfl_sync(0xffffffffu, ti, 31);
+        first_place = __shfl_sync(0xffffffffu, ti, 0);
         if (j < nkt) first_pos = pos_row[tile_row(v_new - j)] - tot;
       }
       if (wg == 1) {  // the reference comes from the first group's first tiles
@@ -865,11 +866,12 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
         const int g = g0 + j, key0 = tile_row(v_new - j);
         const uint32_t ts = t_row + 64u * (uint32_t)(g & 1);
         // Positions, the chunk's first token being 0: two per lane.  A window's border lies in the tile if its first position is outside the
-        // window of the warp's last token; among the chunk's rows in a tree, or with a prefix, positions may also lie behind a
-        // token's: always compared there.  With a window alone the first is asked for a tile ahead, the others only at a border.
+        // window of the warp's last token, or with a prefix its last row of that outside the window of the warp's first token; among
+        // the chunk's rows in a tree positions may also lie behind a token's: always compared there.  With a window alone the first
+        // is asked for a tile ahead, the others only at a border.
         int pos_a = 0, pos_b = 0;
         bool border = false;
-        if constexpr (MODS == kXtWindow) border = (key0 + kPfKeys > held && prefix > 0) || last_place - first_pos >= x.window;
+        if constexpr (MODS == kXtWindow) border = last_place - first_pos >= x.window || min(key0 + kPfKeys - 1 - held, prefix - 1) - first_place >= x.window;
         if (placed || border || MODS == kXtMods) {
           pos_a = pos_row[min(key0 + lane, x.cap - 1)] - tot;
           pos_b = pos_row[min(key0 + 32 + lane, x.cap - 1)] - tot;
