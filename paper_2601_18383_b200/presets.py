@@ -135,9 +135,11 @@ class PresetRun:
         """Known tokens as a chunk instead of one step each: the next question of a conversation, a text put in front.
 
         q, out [L, Nb, T, Hq, d], k, v [L, Nb, T, Hkv, d], scores [Nb, T]; options as of `Cache.extend_attn` (softcap,
-        slopes, window).  The chunk is cut where the row count reaches the budget, and a selection follows each piece, so
+        slopes, window, sinks).  The chunk is cut where the row count reaches the budget, and a selection follows each piece, so
         the rows held and the events are those of T steps.  In order with torch's current stream, whichever stream the cache
-        works on."""
+        works on.  Drafted tokens (stage, tree) are for a `Cache` of one's own, with room for them behind the budget: a preset's holds one row more."""
+        if options.get("stage") or options.get("tree") is not None:
+            raise ValueError("a preset's schedule takes known tokens: drafted ones (stage, tree) need a Cache with room behind its budget")
         c = self.cache
         current, own = c.torch.cuda.current_stream(c.device), c.torch_stream()
         if own.cuda_stream == current.cuda_stream:
