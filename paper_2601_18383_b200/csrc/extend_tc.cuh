@@ -666,7 +666,7 @@ extend_tc_kernel(const __grid_constant__ ExtendTcParams p, const __grid_constant
           const int k0 = tile_row(v_new - j - 1) + sub;  // (of the piece's tiles, while j + 1 < nkt)
           // (four tiles further on towards the older rows: asked into L2)
           if (lane == 0 && j + 4 < nkt)
-            asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(src + (size_t)(tile_row(v_new - j - 4) + sub) * 128), "r"(32 * 128) : "memory");
+            asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(src + (size_t)(kSinks ? tile_row(v_new - j - 4) + sub : k0 - 3 * kPfKeys) * 128), "r"(32 * 128) : "memory");
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             xt_store_codes<false>(codes[i], tile, kPfKvBytes / 2, sub + 8 * i, lane);

@@ -12,13 +12,14 @@
 //
 // A cluster of CTAs takes a row, every warp a run of it.  Every cut keeps a prefix of the ranking, so a row's cuts come down to
 // one border, a (value, index) pair.  The first reading takes every lane's maximum; what follows depends on the row's settings:
-//   * top_k up to 768: with c the q-th largest of a CTA's 512 lanes' maxima, q tokens or more of the CTA lie at or above it; with
-//     q = top_k / CTAs and the smallest c of the cluster's, top_k tokens or more do.  The tokens from there on, about 1.2 top_k, are
-//     collected in a second reading, a list per warp and so in order; the first CTA merges the lists, sorts them, and decides alone.
-//   * top_p alone, or a larger top_k: a histogram of the weights (or of the tokens) over 512 equal steps of the
-//     distance to the maximum, a second reading of the step in which the border lies, and the first CTA sorts that.  Steps of many
-//     equal logits that overflow the lists are narrowed down by the bits of the value instead, and a border inside equal
-//     values is a count of them.
+//   * top_k up to 1024: a lane keeps the maxima of up to 16 groups of its vectors.  With c a value that q of a CTA's groups' maxima reach (the edge of a
+//     step of a histogram of theirs), q tokens or more of the CTA lie at or above it; with q = top_k / CTAs and the smallest c of the
+//     cluster's, top_k tokens or more do.  The tokens from there on are collected in a second reading of the groups that reach
+//     it, a list per warp and so in order; the first CTA merges the lists, ranks them, and decides alone.
+//   * top_p alone, a larger top_k, or lists that overflowed: a histogram over up to 1024 steps, of the tokens by the distance to the maximum, of the
+//     weights by the 32nd part of a binary order; a second reading of the step in which the border lies, and the first CTA
+//     ranks that.  Steps of many equal logits that overflow the lists are narrowed down by the bits of the value instead, and a
+//     border inside equal values is a count of them.
 //   * nothing cut off, or by min_p alone: no border is needed.
 // Where the kept tokens are not in a list, the warps add up theirs, exchange the sums, and the CTA in which the token lies looks
 // for it: sixteenths of the one warp's run, then the run of one warp.
@@ -361,6 +362,7 @@ __device__ __noinline__ int sm_pick(SmShared& sh, unsigned n, u64 above, double 
   return found;
 }
 
+// (64 registers for two CTAs per SM, with 224 bytes of spill stores: the ways to a border are many, and a row walks through one or two.)
 template <typename X>
 __global__ void __launch_bounds__(kSmThreads, kSmPerSm) sample_kernel(const __grid_constant__ SampleParams p) {
   constexpr int E = SmRow<X>::E;
