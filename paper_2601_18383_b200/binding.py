@@ -697,7 +697,7 @@ class Cache:
             _invalid("sinks must be an int of 32 bits, not negative")
         if tree is not None and (tree.dtype is not t.int32 or tree.get_device() != dev or tree.shape != (total, 4) or not tree.is_contiguous()):
             _invalid(f"tree must be a contiguous int32 tensor {(total, 4)} on cuda:{dev}, as tree_plan returns it")
-        more = dynts_extend_more_t(sinks, None if tree is None else tree.data_ptr())
+        more = None if tree is None and sinks == 0 else C.byref(dynts_extend_more_t(sinks, None if tree is None else tree.data_ptr()))
         opts = dynts_extend_opts_t(softcap, None if slopes is None else slopes.data_ptr(), window, prefixes, None if s_new is None else s_new.data_ptr(),
                                    None if mass is None else mass.data_ptr(), 1 if stage else 0, *strides)
         need = lib.dynts_extend_scratch_bytes(self.handle, counts, self.layers if layer is None else 1)
@@ -707,8 +707,10 @@ class Cache:
             with t.torch.cuda.stream(self.torch_stream()):
                 self._scratch.append(t.torch.empty(max(need, 2 * self._scratch_bytes), dtype=t.torch.uint8, device=self.device))
             self._scratch_ptr, self._scratch_bytes = self._scratch[-1].data_ptr(), self._scratch[-1].numel()
-        args = (self.handle, -1 if layer is None else layer, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), counts, C.byref(opts), C.byref(more),
+        args = (self.handle, -1 if layer is None else layer, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), counts, C.byref(opts), more,
                 self._scratch_ptr, self._scratch_bytes)
+        if t.device() == dev:
+            return _check(lib.dynts_extend_attn_ex(*args))
         return self._on_device(lib.dynts_extend_attn_ex, args)
 
     def _on_device(self, call, args):
