@@ -17,6 +17,9 @@
 //   O^T[d][query] += V^T P    16 columns of head_dim on M; P through movmatrix
 // Bound by HBM for long caches and many sequences, by the latency of launch, tile and exchange for few.
 //
+// A wave of CTAs takes 6 to 11 us whatever it reads (lengths, ring, exchange), so batches whose slabs need many waves go by the other kernels (the
+// rule is at the launch).
+//
 // A weight of zero times a value that is not finite is not a number: V rows behind the chunk's end are zeroed in the
 // tile, and an output row that is not finite is computed again by its warp from the rows it sees.
 #pragma once

@@ -31,8 +31,8 @@
 // prefetched.  Two CTAs of 384 threads leave 80 registers per thread and hardly any L1: code that spills or does
 // not stay in the instruction caches cost several times its instructions, so the loops are rolled, the end of a piece
 // is a function of its own, and what is rare is called once from its end (spills: 24 bytes in the plain kernel, none with caps
-// and biases, 16 with trees or windows, 16 to 32 with 8-bit rows).  4096 tokens behind 4096 rows: 433 us a call with changing inputs, 0.95 PFLOP/s; 375 to
-// 395 us replayed on one state, 1.04 to 1.10 PFLOP/s, 0.65 to 0.68 of what cuBLAS reaches.  (Cursors in registers and everything
+// and biases, 16 with trees or windows, 16 to 32 with 8-bit rows).  4096 tokens behind 4096 rows: 435 us a call with changing inputs, 0.95 PFLOP/s; 375 to
+// 425 us replayed on one state by the clocks, 0.97 to 1.10 PFLOP/s, 0.60 to 0.68 of what cuBLAS reaches.  (Cursors in registers and everything
 // unrolled: 453 us when this stood at 388.)  The tensor cores and the exponentials' unit are each busy for a little more than
 // half of that time, in turns that the chain of a tile does not let overlap further: tiles of 128 keys with one S buffer,
 // or P over another CTA's wait, measured 2 to 12 us more.  Short items are bound by their own chain, about 7 us from the
@@ -57,7 +57,7 @@
 
 namespace dynts {
 
-// The row arithmetic: plain; with caps, biases and windows (ragged prompts with a bias 113 us, 122 with the code of trees and sinks beside); plain
+// The row arithmetic: plain; with caps, biases and windows (ragged prompts with a bias 110 us, 122 with the code of trees and sinks beside); plain
 // with the mask of a tree in the tiles of the chunk's rows (trees of 60 in 16 sequences behind 4200 8-bit rows 115 us, 144 with caps
 // and windows beside); plain with the mask of a window in the tiles at its borders; all of it.
 constexpr int kXtPlain = 0, kXtMods = 1, kXtTree = 2, kXtWindow = 3, kXtAll = 4;
