@@ -221,8 +221,10 @@ __device__ __forceinline__ void ext_write_plan(const ExtendParams& p, const Exte
           w[kPwBase] = item + (int)ca;
           w[kPwPrefix] = prefix;
           w[kPwSeen] = p.tot[b];
-          w[kPwSinks] = tiles.sinks;
-          w[kPwJump] = tiles.jump - base;
+          if (p.window > 0 || p.tree) {  // (no other kernel asks)
+            w[kPwSinks] = tiles.sinks;
+            w[kPwJump] = tiles.jump - base;
+          }
         }
         rank += __popc(has);
       }
