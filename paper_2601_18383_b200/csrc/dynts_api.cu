@@ -1759,8 +1759,7 @@ dynts_status_t launch_extend_tc(dynts_cache* c, const dynts::ExtendParams& x, co
 //   this kernel: a wave of CTAs takes `fix`, and `tile` per tile of 32 rows, with the SMs full (1 + `crowd`) times that (the 8 query rows of a
 //   warp four, three, two or one CTA per SM, or two of 32 rows' clusters).  A wave beyond the first costs as much again.
 //   the others (storing, tensor cores, joining): whole items of a query tile, or items cut into parts of four key tiles and more.
-// Within 8 % in the mean (the cut 11 %); by the smaller estimate 1 % of those calls took 3 % or more longer than by the other kernels, none of them
-// in more waves than one.  Measured (us, this kernel / the others): 8 KV heads of 2048 rows, 4 query rows 10 / 21, 20 rows 13 / 22, 48
+// Within 8 % in the mean (the cut 11 %); by the smaller estimate 14 of those calls take 3 to 7 % longer than by the other kernels.  Measured (us, this kernel / the others): 8 KV heads of 2048 rows, 4 query rows 10 / 21, 20 rows 13 / 22, 48
 // rows 17 / 23; 64 sequences of 1500 rows, 4 rows 60 / 81; 33 sequences of 48 rows and 8 heads, 128 rows 84 / 16; 16 sequences of 183 to
 // 366, 36 rows 25 / 16.
 constexpr int kFewCluster = 8, kFewTiles = 4;
